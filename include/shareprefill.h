@@ -428,6 +428,143 @@ int sp_prefill_attn_layer(sp_ctx* ctx, sp_pattern_dict* dict, const sp_tensor* q
                           float tau, int block, int pooled_construction, sp_tensor* out,
                           uint8_t* mask_out, int32_t* pattern_out, void* stream);
 
+/* ------------------------------------------------------------------------
+ * From prefill into decoding.  (The paper decodes densely, Section 6; it says
+ * nothing about caches, and the calls below have no counterpart in it.)
+ *
+ * A decoding step of a batch of requests takes a few new tokens per request:
+ * one, a chain, or a tree of drafted tokens.  Its calls, in order:
+ *   sp_page_tables    once per step: the requests' lengths -> page tables that
+ *                     hold the new tokens, a slot and a position per token
+ *   sp_qk_norm_rope   per layer: norm and rotate the queries and keys, put keys
+ *                     and values into the cache (and, for a prompt, head-major
+ *                     q, k, v as sp_prefill_attn reads them)
+ *   sp_tree_attn      per layer: attention of the new tokens over the cache
+ *   sp_cache_keep     per layer, after drafted tokens were verified: the accepted
+ *                     ones move to the front of the drafted region
+ *
+ * Conventions on top of the general ones
+ *   - Rows are packed: the new tokens of request b are rows row_start[b] ..
+ *     row_start[b + 1] - 1 of every per-token array, in order.  Rows from
+ *     row_start[n_req] on belong to nobody (a batch padded for a captured graph):
+ *     per-token outputs are left as they were there.
+ *   - A cache tensor is bf16 [pages, n_kv_heads, page, head_dim] with any strides
+ *     that are multiples of 8 elements and at least head_dim (size-1 dimensions: any);
+ *     page in {16, 32, 64, 128, 256}, head_dim in {64, 128}.  So a contiguous
+ *     [n_kv_heads, seq, head_dim] tensor is a cache too (strides page * head_dim,
+ *     seq * head_dim, head_dim; table 0, 1, 2, ...).  Slot s is token s % page of
+ *     page s / page; pages * page must fit 31 bits (element offsets are 64-bit).
+ *   - block_table: device i32 [n_req, max_pages]; token p of request b lies on page
+ *     block_table[b][p / page].  Entries behind a request's last page are not read.
+ *   - Any number of rows >= 1, any lengths (0 included); n_req <= 4096 (0: nothing
+ *     is done).  All sizes that vary from step to step are read on the device, so a
+ *     captured graph serves every step of the same n_req and row capacity.
+ *   - A page or slot that is not one of the cache's is never followed: the access is
+ *     left out (a key on such a page counts as not visible), the request's results
+ *     are then unspecified, and sp_get_status reports SP_ERR_RANGE with where = 70
+ *     (sp_tree_attn; also a length that its table row cannot hold), 75
+ *     (sp_qk_norm_rope) or 80 (sp_cache_keep).  Unlike a timeout this does not keep
+ *     the calls of this section from working; the calls above work again once the
+ *     status has been read.
+ */
+
+/*
+ * sp_page_tables - page tables and slot maps from request lengths, one launch.
+ *   past_lens    device i32 [n_req]: tokens each request has in the cache.
+ *   new_lens     device i32 [n_req]: tokens it gets in this step (0: none).
+ *   free_pages   device i32 [n_free]: pages to take, in this order, requests in
+ *                theirs; the caller drops the first info[1] of them afterwards.
+ *   block_table  in/out: entries 0 .. ceil(past / page) - 1 of a row are given, the
+ *                entries up to ceil((past + new) / page) - 1 are written, the rest is
+ *                left as it was.  Pages that the written entries named before (of drafted
+ *                tokens that were not kept) are the caller's to put back into free_pages.
+ *   parents      device i32 [n_rows] or NULL.  For drafted trees: index, inside its
+ *                request, of the token that each new token follows: a smaller index,
+ *                or -1 (anything else is read as -1): the last cached token.
+ *   seq_lens     out [n_req]: past + new.         row_start  out [n_req + 1].
+ *   slots        out [n_rows]: cache slot of each new token, past + index in order;
+ *                -1 where no page was left or the table row is too short.
+ *   positions    out [n_rows]: past + index, or with parents past + depth (number of
+ *                ancestors among the new tokens): the position for the rotation.
+ *   tree_mask    out u32 [n_rows, mask_words], given iff parents is: bit x of a row
+ *                (word x / 32, bit x % 32) = new token x is an ancestor of the row's
+ *                token or the token itself.  mask_words in 1 .. 8.
+ *   n_rows       capacity of the per-token arrays; rows that do not fit are left out.
+ *   info         out [4]: rows needed, pages taken, failed requests, longest past + new.
+ *                A request fails when a length is negative (read as 0), its table row is
+ *                too short, no page is left for it, or it has more than 32 * mask_words
+ *                drafted tokens (the bits that do not fit are left out).
+ *   Calling it again with the same lengths writes the same values.
+ */
+int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_lens, int n_req, int page,
+                   const int32_t* free_pages, int n_free, int32_t* block_table, int max_pages,
+                   const int32_t* parents, int32_t* seq_lens, int32_t* row_start, int32_t* positions,
+                   int32_t* slots, uint32_t* tree_mask, int mask_words, int n_rows, int32_t* info, void* stream);
+
+/*
+ * sp_qk_norm_rope - norms of queries and keys for each head with the position
+ *   rotation in the same pass, from the projection's rows to where they are used.
+ *     y = x / sqrt(mean(x^2) + eps) * weight    per head of q and k (if weights are given)
+ *     (a, b) -> (a cos - b sin, b cos + a sin)  per pair i < n_freq,
+ *                                               angle = position * inv_freq[i]
+ *   Values are moved as they are.  fp32 arithmetic, one rounding; the angle is exact
+ *   modulo one turn at any 32-bit position.
+ *   q            [1, n_q_heads, rows, head_dim]; k, v [1, n_kv_heads, rows, head_dim]: any
+ *                strides (multiples of 8 elements, at least head_dim), so slices of one
+ *                projected [rows, heads, head_dim] tensor will do.
+ *   q_weight, k_weight  device bf16 [head_dim], 16-byte aligned; both or neither (NULL:
+ *                no norm).
+ *   inv_freq     HOST double [n_freq], 0 <= inv_freq < 1e9; n_freq a multiple of 8 and at
+ *                most head_dim / 2.  The first 2 * n_freq elements of a head turn; 0: none.
+ *   interleaved  0: pairs (i, i + n_freq); else pairs (2 i, 2 i + 1).
+ *   positions    device i32 [rows].
+ *   q_out        like q, its own strides; it may be q itself (same data and strides).
+ *   k_out, v_out like k, or both NULL; may be k and v themselves likewise.
+ *   k_cache, v_cache, slots   the paged cache and the slot of each row (device i32 [rows];
+ *                negative: the row is not cached), or all NULL.  At least one destination
+ *                must be given for k and v.  No two rows may name the same slot.
+ *   Other overlaps of inputs and outputs are not allowed.
+ */
+int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const sp_tensor* v, const void* q_weight,
+                    const void* k_weight, float eps, const double* inv_freq /* host */, int n_freq, int interleaved,
+                    const int32_t* positions, const sp_tensor* q_out, const sp_tensor* k_out, const sp_tensor* v_out,
+                    const sp_tensor* k_cache, const sp_tensor* v_cache, const int32_t* slots, void* stream);
+
+/*
+ * sp_tree_attn - attention of the new tokens of every request over its cached keys
+ *   and values, those of the new tokens included (put there before):
+ *     out = softmax(q k^T / sqrt(head_dim), visible keys) v
+ *   With seq = seq_lens[b], n = row_start[b + 1] - row_start[b] and past = seq - n, key
+ *   p < seq is visible to new token j iff p < past, or with x = p - past
+ *     tree_mask NULL:  x <= j                       (a chain; one token: all keys)
+ *     else:            bit x of the token's row is set (x >= 32 * mask_words: not visible)
+ *   A row that sees nothing gets zeros and lse -infinity.  What lies in masked or
+ *   unused places of the cache (NaN included) does not reach the outputs.
+ *   q            [1, n_q_heads, rows, head_dim], any strides as for sp_qk_norm_rope;
+ *                n_q_heads a multiple of the cache's heads, at most 128.
+ *   tree_mask    device u32 [rows, mask_words], mask_words in 1 .. 8, or NULL.
+ *   out          like q, its own strides.
+ *   lse_out      device fp32 [n_q_heads, rows]: natural-log-sum-exp of the scaled logits
+ *                of each row's visible keys, or NULL.
+ */
+int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, const sp_tensor* v_cache,
+                 const int32_t* block_table, int max_pages, const int32_t* seq_lens, const int32_t* row_start, int n_req,
+                 const uint32_t* tree_mask, int mask_words, const sp_tensor* out, float* lse_out, void* stream);
+
+/*
+ * sp_cache_keep - compaction after verification: for each request b and i < n_kept[b]
+ *   the key and value of every head at token past_lens[b] + kept[b][i] move to token
+ *   past_lens[b] + i, in place.
+ *   kept       device i32 [n_req, max_kept]: indices among the request's new tokens,
+ *              strictly ascending (an accepted path in the order of sp_page_tables);
+ *              entries from n_kept[b] on are not read.
+ *   n_kept     device i32 [n_req], read as 0 .. max_kept.
+ *   past_lens  as given to sp_page_tables.     lens_out  out [n_req]: past + n_kept.
+ */
+int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cache, const int32_t* block_table,
+                  int max_pages, const int32_t* past_lens, int n_req, const int32_t* kept, const int32_t* n_kept,
+                  int max_kept, int32_t* lens_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

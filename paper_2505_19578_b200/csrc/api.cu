@@ -6,25 +6,8 @@
 #include <string.h>
 
 #include <new>
-#include <vector>
 
-#include "common.cuh"
-
-struct sp_ctx {
-  int device = 0;
-  void* ws = nullptr;
-  size_t ws_bytes = 0;
-  int* status = nullptr;  // device int[4]: {code, where, work counter of the paired kernel, unused}
-  int kernel = 0;         // 0 tensor-core (paired where supported), 1 CUDA-core cross-check, 2 tensor-core single-tile
-  int64_t launches = 0;
-  long long* trace = nullptr;  // caller's device buffer for the phase trace, or null
-  int trace_cap = 0;
-  // sp_prefill_attn_host: device copies of q, k, v, out (+ masks) and the copy streams
-  void* stage = nullptr;
-  size_t stage_bytes = 0;
-  cudaStream_t s_in = nullptr, s_out = nullptr;
-  std::vector<cudaEvent_t> events;
-};
+#include "ctx.cuh"
 
 // Cross-layer dictionary of pivotal patterns: cluster id -> (mask, compacted lists, representative a~).
 // List slots 0..C-1 belong to the clusters, slots C..C+H-1 are scratch for the vertical-slash lists of a layer.
@@ -43,20 +26,6 @@ struct sp_pattern_dict {
 namespace {
 
 using namespace sp;
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-    target = dev;
-  }
-  ~DeviceGuard() {
-    if (prev >= 0 && prev != target) cudaSetDevice(prev);
-  }
-  int target = -1;
-};
 
 size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
@@ -278,6 +247,7 @@ int sp_ctx_destroy(sp_ctx* ctx) {
   if (ctx->ws) cudaFree(ctx->ws);
   if (ctx->status) cudaFree(ctx->status);
   if (ctx->stage) cudaFree(ctx->stage);
+  if (ctx->split_ws) cudaFree(ctx->split_ws);
   if (ctx->s_in) cudaStreamDestroy(ctx->s_in);
   if (ctx->s_out) cudaStreamDestroy(ctx->s_out);
   for (cudaEvent_t e : ctx->events) cudaEventDestroy(e);

@@ -1,0 +1,192 @@
+// Host side of the decode-side calls: argument validation and launches.
+#include <math.h>
+#include <string.h>
+
+#include "ctx.cuh"
+#include "decode.cuh"
+
+namespace {
+
+using namespace sp;
+
+// A bf16 view whose size-1 dimensions may carry any stride (they are never stepped).
+int check_view(const sp_tensor* t) {
+  if (!t || !t->data) return SP_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(t->data) & 15) != 0) return SP_ERR_INVALID_ARG;
+  for (int x = 0; x < 4; ++x)
+    if (t->shape[x] <= 0 || t->shape[x] > INT32_MAX) return SP_ERR_INVALID_ARG;
+  if (t->shape[3] > 1 && t->stride[3] != 1) return SP_ERR_INVALID_ARG;
+  for (int x = 0; x < 3; ++x)
+    if (t->shape[x] > 1 && (t->stride[x] < t->shape[3] || t->stride[x] % 8 != 0)) return SP_ERR_INVALID_ARG;
+  return SP_OK;
+}
+bool same_shape(const sp_tensor* a, const sp_tensor* b) { return memcmp(a->shape, b->shape, sizeof(a->shape)) == 0; }
+int64_t step(const sp_tensor* t, int x) { return t->shape[x] > 1 ? t->stride[x] : 0; }
+
+int log2_of_page(int64_t page) {          // -1: not a supported page size
+  for (int l = 4; l <= 8; ++l)
+    if (page == (int64_t)1 << l) return l;
+  return -1;
+}
+
+struct CacheShape {
+  int pages, hkv, d, page_log2;
+};
+int check_cache(const sp_tensor* k, const sp_tensor* v, CacheShape* c) {
+  int rc;
+  if ((rc = check_view(k)) || (rc = check_view(v))) return rc;
+  if (!same_shape(k, v)) return SP_ERR_INVALID_ARG;
+  c->page_log2 = log2_of_page(k->shape[2]);
+  if (c->page_log2 < 0 || (k->shape[3] != 64 && k->shape[3] != 128) || k->shape[1] > kMaxHeads) return SP_ERR_UNSUPPORTED;
+  if (k->shape[0] > (INT32_MAX >> c->page_log2)) return SP_ERR_UNSUPPORTED;    // slots are 32-bit
+  c->pages = (int)k->shape[0]; c->hkv = (int)k->shape[1]; c->d = (int)k->shape[3];
+  return SP_OK;
+}
+PagedCache cache_of(const sp_tensor* t) {
+  return PagedCache{static_cast<__nv_bfloat16*>(t->data), step(t, 0), step(t, 1), step(t, 2)};
+}
+
+}  // namespace
+
+extern "C" {
+
+int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_lens, int n_req, int page,
+                   const int32_t* free_pages, int n_free, int32_t* block_table, int max_pages, const int32_t* parents,
+                   int32_t* seq_lens, int32_t* row_start, int32_t* positions, int32_t* slots, uint32_t* tree_mask,
+                   int mask_words, int n_rows, int32_t* info, void* stream) {
+  if (!ctx || n_req < 0 || n_free < 0 || max_pages <= 0 || n_rows < 0) return SP_ERR_INVALID_ARG;
+  if (!past_lens || !new_lens || !block_table || !seq_lens || !row_start || !info) return SP_ERR_INVALID_ARG;
+  if ((n_free > 0 && !free_pages) || (n_rows > 0 && (!positions || !slots))) return SP_ERR_INVALID_ARG;
+  if ((parents != nullptr) != (tree_mask != nullptr)) return SP_ERR_INVALID_ARG;
+  const int pl = log2_of_page(page);
+  if (pl < 0 || n_req > kMaxRequests || max_pages > (INT32_MAX >> pl)) return SP_ERR_UNSUPPORTED;
+  if (tree_mask && (mask_words < 1 || mask_words > kMaxMaskWords)) return SP_ERR_UNSUPPORTED;
+  if (n_req == 0) return SP_OK;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  PageTablesArgs a{past_lens, new_lens, free_pages, parents, block_table, seq_lens, row_start, positions, slots,
+                   tree_mask, info, n_req, n_free, max_pages, pl, n_rows, tree_mask ? mask_words : 0, ctx->status};
+  if (launch_page_tables(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const sp_tensor* v, const void* q_weight,
+                    const void* k_weight, float eps, const double* inv_freq, int n_freq, int interleaved,
+                    const int32_t* positions, const sp_tensor* q_out, const sp_tensor* k_out, const sp_tensor* v_out,
+                    const sp_tensor* k_cache, const sp_tensor* v_cache, const int32_t* slots, void* stream) {
+  if (!ctx || !positions || n_freq < 0 || (n_freq > 0 && !inv_freq)) return SP_ERR_INVALID_ARG;
+  int rc;
+  if ((rc = check_view(q)) || (rc = check_view(k)) || (rc = check_view(v)) || (rc = check_view(q_out))) return rc;
+  if (!same_shape(q, q_out) || !same_shape(k, v)) return SP_ERR_INVALID_ARG;
+  if (q->shape[0] != 1 || k->shape[0] != 1) return SP_ERR_UNSUPPORTED;
+  if (q->shape[2] != k->shape[2] || q->shape[3] != k->shape[3]) return SP_ERR_INVALID_ARG;
+  const int64_t d = q->shape[3];
+  if ((d != 64 && d != 128) || q->shape[1] > kMaxHeads || k->shape[1] > kMaxHeads) return SP_ERR_UNSUPPORTED;
+  if (2 * (int64_t)n_freq > d || n_freq % 8 != 0) return SP_ERR_UNSUPPORTED;
+  if ((q_weight != nullptr) != (k_weight != nullptr)) return SP_ERR_INVALID_ARG;
+  if (((reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight)) & 15) != 0) return SP_ERR_INVALID_ARG;
+  if (q_weight && !(eps >= 0.f && eps < INFINITY)) return SP_ERR_INVALID_ARG;
+  if ((k_out != nullptr) != (v_out != nullptr) || (k_cache != nullptr) != (v_cache != nullptr)) return SP_ERR_INVALID_ARG;
+  if (!k_out && !k_cache) return SP_ERR_INVALID_ARG;
+  if (k_out) {
+    if ((rc = check_view(k_out)) || (rc = check_view(v_out))) return rc;
+    if (!same_shape(k, k_out) || !same_shape(v, v_out)) return SP_ERR_INVALID_ARG;
+  }
+  RopeArgs a;
+  memset(&a, 0, sizeof(a));
+  if (k_cache) {
+    CacheShape c;
+    if (!slots) return SP_ERR_INVALID_ARG;
+    if ((rc = check_cache(k_cache, v_cache, &c))) return rc;
+    if (c.hkv != k->shape[1] || c.d != d) return SP_ERR_INVALID_ARG;
+    a.kc = cache_of(k_cache);
+    a.vc = cache_of(v_cache);
+    a.page_log2 = c.page_log2;
+    a.n_slots = c.pages << c.page_log2;
+    a.slots = slots;
+  }
+  for (int i = 0; i < n_freq; ++i) {
+    if (!(inv_freq[i] >= 0.0 && inv_freq[i] < 1e9)) return SP_ERR_INVALID_ARG;
+    // turns per position, modulo one turn, in units of 2^-64
+    const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559L;
+    const long double part = turns - floorl(turns);
+    a.phase[i] = (uint64_t)floorl(part * 18446744073709551616.0L);
+  }
+  a.q = static_cast<const __nv_bfloat16*>(q->data);
+  a.k = static_cast<const __nv_bfloat16*>(k->data);
+  a.v = static_cast<const __nv_bfloat16*>(v->data);
+  a.q_out = static_cast<__nv_bfloat16*>(q_out->data);
+  a.q_sh = step(q, 1); a.q_sn = step(q, 2); a.k_sh = step(k, 1); a.k_sn = step(k, 2); a.v_sh = step(v, 1); a.v_sn = step(v, 2);
+  a.qo_sh = step(q_out, 1); a.qo_sn = step(q_out, 2);
+  if (k_out) {
+    a.k_out = static_cast<__nv_bfloat16*>(k_out->data);
+    a.v_out = static_cast<__nv_bfloat16*>(v_out->data);
+    a.ko_sh = step(k_out, 1); a.ko_sn = step(k_out, 2); a.vo_sh = step(v_out, 1); a.vo_sn = step(v_out, 2);
+  }
+  a.q_weight = static_cast<const __nv_bfloat16*>(q_weight);
+  a.k_weight = static_cast<const __nv_bfloat16*>(k_weight);
+  a.positions = positions;
+  a.hq = (int)q->shape[1]; a.hkv = (int)k->shape[1]; a.tokens = (int)q->shape[2]; a.d = (int)d;
+  a.rot = 2 * n_freq; a.interleaved = interleaved != 0; a.eps = eps; a.status = ctx->status;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  if (launch_qk_norm_rope(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, const sp_tensor* v_cache,
+                 const int32_t* block_table, int max_pages, const int32_t* seq_lens, const int32_t* row_start, int n_req,
+                 const uint32_t* tree_mask, int mask_words, const sp_tensor* out, float* lse_out, void* stream) {
+  if (!ctx || !block_table || !seq_lens || !row_start || n_req < 0 || max_pages <= 0) return SP_ERR_INVALID_ARG;
+  int rc;
+  CacheShape c;
+  if ((rc = check_view(q)) || (rc = check_view(out))) return rc;
+  if ((rc = check_cache(k_cache, v_cache, &c))) return rc;
+  if (!same_shape(q, out) || q->shape[3] != c.d) return SP_ERR_INVALID_ARG;
+  if (q->shape[0] != 1 || q->shape[1] > kMaxHeads || q->shape[1] % c.hkv != 0) return SP_ERR_UNSUPPORTED;
+  if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
+  if (tree_mask && (mask_words < 1 || mask_words > kMaxMaskWords)) return SP_ERR_UNSUPPORTED;
+  if (n_req == 0) return SP_OK;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  TreeAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = static_cast<const __nv_bfloat16*>(q->data);
+  a.o = static_cast<__nv_bfloat16*>(out->data);
+  a.lse = lse_out;
+  a.q_sh = step(q, 1); a.q_sn = step(q, 2); a.o_sh = step(out, 1); a.o_sn = step(out, 2);
+  a.kc = cache_of(k_cache);
+  a.vc = cache_of(v_cache);
+  a.table = block_table; a.seq_lens = seq_lens; a.row_start = row_start;
+  a.bits = tree_mask; a.words = tree_mask ? mask_words : 0;
+  a.hq = (int)q->shape[1]; a.hkv = c.hkv; a.group = a.hq / a.hkv; a.d = c.d; a.rows = (int)q->shape[2];
+  a.n_req = n_req; a.max_pages = max_pages; a.page_log2 = c.page_log2; a.n_pages = c.pages;
+  a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d));
+  a.status = ctx->status;
+  if (launch_tree_attn_simt(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cache, const int32_t* block_table, int max_pages,
+                  const int32_t* past_lens, int n_req, const int32_t* kept, const int32_t* n_kept, int max_kept,
+                  int32_t* lens_out, void* stream) {
+  if (!ctx || !block_table || !past_lens || !kept || !n_kept || !lens_out) return SP_ERR_INVALID_ARG;
+  if (n_req < 0 || max_pages <= 0 || max_kept <= 0) return SP_ERR_INVALID_ARG;
+  int rc;
+  CacheShape c;
+  if ((rc = check_cache(k_cache, v_cache, &c))) return rc;
+  if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
+  if (n_req == 0) return SP_OK;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  KeepArgs a{cache_of(k_cache), cache_of(v_cache), block_table, past_lens, kept, n_kept, lens_out, n_req, max_pages, max_kept,
+             c.hkv, c.d, c.page_log2, c.pages, ctx->status};
+  if (launch_cache_keep(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+}  // extern "C"

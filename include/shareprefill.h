@@ -468,6 +468,10 @@ int sp_prefill_attn_layer(sp_ctx* ctx, sp_pattern_dict* dict, const sp_tensor* q
  *     status has been read.
  */
 
+/* Allocate the workspace of sp_tree_attn (39 MB with 148 SMs; it depends on the device alone and never moves).  Its
+ * first call does so otherwise; inside a stream capture that call returns SP_ERR_WORKSPACE and enqueues nothing. */
+int sp_ctx_reserve_decode(sp_ctx* ctx);
+
 /*
  * sp_page_tables - page tables and slot maps from request lengths, one launch.
  *   past_lens    device i32 [n_req]: tokens each request has in the cache.

@@ -38,7 +38,7 @@ EXPORTS = (
     "sp_dict_create", "sp_dict_destroy", "sp_dict_clear", "sp_dict_count", "sp_prefill_attn_layer",
     "sp_selftest_wait_timeout", "sp_fixed_scratch_status", "sp_workspace_bytes_patterns",
     "sp_internal_pair_work_order",
-    "sp_page_tables", "sp_qk_norm_rope", "sp_tree_attn", "sp_cache_keep",
+    "sp_page_tables", "sp_qk_norm_rope", "sp_tree_attn", "sp_cache_keep", "sp_ctx_reserve_decode",
 )
 
 
@@ -94,6 +94,7 @@ def load() -> ctypes.CDLL:
     lib.sp_dict_clear.argtypes = [P]
     lib.sp_dict_count.argtypes = [P]
     lib.sp_prefill_attn_layer.argtypes = [P, P, T, T, T, IP, F, F, F, I, I, T, P, P, P]
+    lib.sp_ctx_reserve_decode.argtypes = [P]
     lib.sp_page_tables.argtypes = [P, P, P, I, I, P, I, P, I, P, P, P, P, P, P, I, I, P, P]
     lib.sp_qk_norm_rope.argtypes = [P, P, P, P, P, P, F, P, I, I, P, P, P, P, P, P, P, P]
     lib.sp_tree_attn.argtypes = [P, P, P, P, P, I, P, P, I, P, I, P, P, P]
@@ -210,6 +211,10 @@ class Context:
 
     def reserve(self, nbytes: int):
         _check(self._lib.sp_ctx_reserve(self._h, nbytes), "sp_ctx_reserve")
+
+    def reserve_decode(self):
+        """Allocate the workspace of sp_tree_attn ahead of its first call (a call inside a stream capture cannot)."""
+        _check(self._lib.sp_ctx_reserve_decode(self._h), "sp_ctx_reserve_decode")
 
     def status(self):
         """(code, where) of the device status word; call after synchronising."""

@@ -46,9 +46,28 @@ PagedCache cache_of(const sp_tensor* t) {
   return PagedCache{static_cast<__nv_bfloat16*>(t->data), step(t, 0), step(t, 1), step(t, 2)};
 }
 
+// The workspace of sp_tree_attn, with the context's device current.
+int reserve_split(sp_ctx* ctx) {
+  if (ctx->split_ws) return SP_OK;
+  int n_sm = 0;
+  if (cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, ctx->device) != cudaSuccess) return SP_ERR_CUDA;
+  void* p = nullptr;
+  if (cudaMalloc(&p, tree_attn_workspace_bytes(n_sm)) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
+  ctx->split_ws = p;
+  ctx->n_sm = n_sm;
+  return SP_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int sp_ctx_reserve_decode(sp_ctx* ctx) {
+  if (!ctx) return SP_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  return reserve_split(ctx);
+}
 
 int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_lens, int n_req, int page,
                    const int32_t* free_pages, int n_free, int32_t* block_table, int max_pages, const int32_t* parents,
@@ -146,6 +165,7 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
   if ((rc = check_cache(k_cache, v_cache, &c))) return rc;
   if (!same_shape(q, out) || q->shape[3] != c.d) return SP_ERR_INVALID_ARG;
   if (q->shape[0] != 1 || q->shape[1] > kMaxHeads || q->shape[1] % c.hkv != 0) return SP_ERR_UNSUPPORTED;
+  if (q->shape[2] * (q->shape[1] / c.hkv) > INT32_MAX) return SP_ERR_UNSUPPORTED;
   if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
   if (tree_mask && (mask_words < 1 || mask_words > kMaxMaskWords)) return SP_ERR_UNSUPPORTED;
   if (n_req == 0) return SP_OK;
@@ -165,8 +185,21 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
   a.n_req = n_req; a.max_pages = max_pages; a.page_log2 = c.page_log2; a.n_pages = c.pages;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d));
   a.status = ctx->status;
-  if (launch_tree_attn_simt(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
-  ctx->launches += 1;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (ctx->kernel == 1) {
+    if (launch_tree_attn_simt(a, s) != cudaSuccess) return SP_ERR_CUDA;
+    ctx->launches += 1;
+    return SP_OK;
+  }
+  if (!ctx->split_ws) {
+    // an allocation inside a stream capture would spoil the capture
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
+    if (capturing != cudaStreamCaptureStatusNone) return SP_ERR_WORKSPACE;
+    if ((rc = reserve_split(ctx))) return rc;
+  }
+  if (launch_tree_attn(a, ctx->split_ws, ctx->n_sm, s) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 2;
   return SP_OK;
 }
 

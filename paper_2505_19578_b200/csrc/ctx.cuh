@@ -22,6 +22,7 @@ struct sp_ctx {
   // sp_tree_attn: partial results of units that several CTAs share.  Sized by the device alone, allocated once and never
   // moved, so that captured graphs keep a valid address.
   void* split_ws = nullptr;
+  int n_sm = 0;           // set with it
 };
 
 namespace sp {

@@ -93,6 +93,8 @@ struct TreeAttnArgs {
 cudaError_t launch_page_tables(const PageTablesArgs& a, cudaStream_t s);
 cudaError_t launch_qk_norm_rope(RopeArgs& a, cudaStream_t s);
 cudaError_t launch_cache_keep(const KeepArgs& a, cudaStream_t s);
+size_t tree_attn_workspace_bytes(int n_sm);
+cudaError_t launch_tree_attn(const TreeAttnArgs& a, void* ws, int n_sm, cudaStream_t s);
 cudaError_t launch_tree_attn_simt(const TreeAttnArgs& a, cudaStream_t s);
 
 }  // namespace sp

@@ -1,0 +1,807 @@
+// Attention of a few new tokens per request (one, a chain, a tree of drafted ones) over the paged cache: tcgen05 / TMEM /
+// TMA, split along the keys.
+//
+//   out_r = sum_c p_rc v_c / sum_c p_rc,  p_rc = 2^(scale q_r.k_c - m_r) over the visible keys c.
+//
+// The rows of a unit are the new tokens of one request times the query heads that share a KV head (row = token * group +
+// head), at most 256 of them, so that every key and value is read once for all of them.  Work is counted in key tiles of
+// 128: the tiles of all units (request, KV head, 256 rows) stand in one line, which is cut into one equal run per SM
+// wherever that falls; a unit that is cut leaves partial results (unnormalised sums, reference maxima, weights) that a
+// second kernel joins in the order of the keys.  All lengths are read on the device: a prefix sum over the requests
+// tells each CTA where its run begins.
+//
+// What bounds it: the cache's bytes.  A tile is 64 KB (head_dim 128), 2700 cycles of an SM's share of the measured HBM
+// rate; its matrix products take 1020 cycles for up to 128 rows (the tensor core takes 128 rows at a time, however few
+// are in use), 2040 for 256.  With 256 rows its 32768 exponentials (2048 cycles of the SM's special-function units) come
+// close to the bytes.
+//
+// Two streams of (key tile, 128 rows) jobs share the tensor core, each with its own S and O columns in TMEM and its own
+// four softmax warps, so that one stream's exponentials overlap the other's products.  With more than 128 rows the
+// streams are the two halves of the rows and walk the same tiles; with fewer they take the tiles in turn and their sums
+// are joined at the end of the unit (both groups of warps read both O's from TMEM, half the columns each).
+//
+//   warps 0-3, 4-7  softmax and epilogue of stream 0 / 1: thread = TMEM lane = row
+//   warp 8          producer: page ids from the table, TMA loads of K and V pages into a ring of tile slots
+//   warp 9          issuer (one thread): S = Q K^T and O += P V of whichever stream is ready
+//   warp 10         scheduler: walks the run, publishes units, gathers their Q rows into shared memory (cp.async)
+//
+// Masks.  Only tiles that hold a key at or behind the first new token need one.  There the row's visibility bits are
+// shifted into place 32 keys at a time.  A masked probability is zero, but zero times a NaN in V is not: in those tiles
+// the values behind the sequence are set to zero in shared memory, and non-finite values of new tokens too; if there were
+// any, each row adds those that it sees at the end (from the cache: they are what the sum comes to anyway).
+//
+// Rounding: products bf16 x bf16 in fp32, softmax statistics and O in fp32, P rounded to bf16 for the second product (the
+// sum of weights is taken before that rounding), the result once.  The reference maximum moves only when the row maximum
+// has grown by more than 2^8 (P stays below 2^8, exact scaling otherwise).
+//
+// Every wait is bounded as in the other tensor-core kernels: a wait that runs out raises the abort flag and the status
+// word, and all roles fall through to the common end.
+#include <limits.h>
+
+#include "decode.cuh"
+#include "tc_ptx.cuh"
+
+namespace sp {
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 128;                       // keys of a tile
+constexpr int kUnitRows = 256;
+constexpr int kThreads = 352;
+constexpr int kSoftmaxWarps = 8, kProducer = 8, kIssuer = 9, kScheduler = 10;
+constexpr int kUnitRing = 4;
+constexpr float kNoMax = -1e30f;                 // reference maximum before any visible key: finite, below any logit
+
+template <int D>
+struct Plan {
+  static constexpr int NBOX = D / 64;                       // 64-column (128-byte) boxes
+  static constexpr int QBOX = 128 * 128, QHALF = NBOX * QBOX;
+  static constexpr int KBOX = kTile * 128, SLOT = NBOX * KBOX;
+  static constexpr int SLOTS = D == 128 ? 5 : 10;
+  static constexpr int RING_OFF = 2 * QHALF;
+  static constexpr int MISC_OFF = RING_OFF + SLOTS * SLOT;
+  static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + SLOTS, BAR_S = BAR_FREE + SLOTS, BAR_P = BAR_S + 2, BAR_PV = BAR_P + 2,
+                       BAR_QFULL = BAR_PV + 2, BAR_QFREE = BAR_QFULL + 2, BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + kUnitRing,
+                       BAR_EX = BAR_UFREE + kUnitRing, BAR_EXDONE = BAR_EX + 1, BARS = BAR_EXDONE + 1;
+  static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;
+  static constexpr int EX_OFF = (UNIT_OFF + kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // float2 [2][128]
+  static constexpr int SCAN_OFF = EX_OFF + 2048;                                       // int64 [11], then small words
+  static constexpr int TOTAL = SCAN_OFF + 11 * 8 + 64;
+  static constexpr int S_COL = 0, O_COL = 256, O_STEP = D;  // S: 128 columns a stream; O: D columns a stream
+};
+
+struct Unit {
+  int n_tiles;      // key tiles of this CTA's part; 0: no more units
+  int kt0;          // first of them
+  int kt_all;       // key tiles of the whole unit
+  int start;        // first row of the request
+  int r0, rows;     // first of the unit's rows (token * group + head) inside the request, and their number
+  int g, b;
+  int len, past;
+  int half;         // Q half in use (more than 128 rows: both)
+  int last_cta;     // CTA that has the unit's last tile
+};
+static_assert(sizeof(Unit) == 48, "");
+
+struct Meta {       // what the join kernel needs of a unit that begins in this CTA and goes on in later ones
+  int last_cta;     // < 0: there is none
+  int start, r0, rows, g, pad[3];
+};
+
+struct Work {
+  float* part;      // [cta][2][256][D] unnormalised sums: part 0 of a unit begun by an earlier CTA, part 1 of one begun here
+  float2* ml;       // [cta][2][256] reference maximum, weight
+  Meta* meta;       // [cta]
+};
+
+struct Request {
+  int start, n, len, past, passes, kt;
+  long long tiles;
+};
+__device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) {
+  Request q;
+  const int s0 = a.row_start[b], s1 = a.row_start[b + 1], seq = a.seq_lens[b];
+  q.start = min(max(s0, 0), a.rows);
+  q.n = s0 < 0 ? 0 : max(min(s1, a.rows) - q.start, 0);
+  q.len = min(max(seq, 0), a.max_pages << a.page_log2);
+  q.past = seq - (s1 - s0);
+  q.passes = (int)(((long long)q.n * a.group + kUnitRows - 1) / kUnitRows);
+  q.kt = max((q.len + kTile - 1) / kTile, 1);
+  q.tiles = (long long)a.hkv * q.passes * q.kt;
+  return q;
+}
+
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// Which of the 32 keys from k0 on a row sees: bit i = key k0 + i.
+__device__ __forceinline__ uint32_t seen32(const TreeAttnArgs& a, const Unit& u, int token, int k0) {
+  const int left = u.len - k0;                                       // keys of the sequence from here on
+  uint32_t live = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+  const long long x0 = (long long)k0 - u.past;                       // index of key k0 among the new tokens
+  if (x0 + 31 < 0) return live;
+  if (!a.bits) {
+    const long long upto = token - x0;                               // keys 0 .. upto of these are seen
+    return live & (upto >= 31 ? 0xffffffffu : upto < 0 ? 0u : (2u << upto) - 1u);
+  }
+  const uint32_t* row = a.bits + (size_t)(u.start + token) * a.words;
+  const long long w0 = x0 >> 5;                                      // floor: keys before the new tokens are words of ones
+  auto word = [&](long long w) { return w < 0 ? 0xffffffffu : w < a.words ? row[w] : 0u; };
+  return live & __funnelshift_r(word(w0), word(w0 + 1), (uint32_t)(x0 & 31));
+}
+
+// The non-finite values of new tokens that a row sees, added to 32 of its columns (they were left out of the products).
+__device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, int col, float (&o)[32]) {
+  const int k_from = max(u.kt0 * kTile, u.past), k_to = min((u.kt0 + u.n_tiles) * kTile, u.len);
+  for (int key = k_from; key < k_to; ++key) {
+    const int id = a.table[(size_t)u.b * a.max_pages + (key >> a.page_log2)];
+    if (id < 0 || id >= a.n_pages || !(seen32(a, u, token, key) & 1)) continue;
+    const __nv_bfloat16* v = a.vc.data + id * a.vc.s_page + u.g * a.vc.s_head + (key & ((1 << a.page_log2) - 1)) * a.vc.s_tok + col;
+    for (int c = 0; c < 32; ++c) {
+      const float x = __bfloat162float(v[c]);
+      if (!isfinite(x)) o[c] += x;
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const __grid_constant__ CUtensorMap tm_k,
+                 const __grid_constant__ CUtensorMap tm_v) {
+  using P = Plan<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t base = smem_u32(smem);
+  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  float2* ex = reinterpret_cast<float2*>(smem + P::EX_OFF);
+  long long* scan = reinterpret_cast<long long*>(smem + P::SCAN_OFF);
+  int* words = reinterpret_cast<int*>(smem + P::SCAN_OFF + 11 * 8);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(words);
+  volatile int* abort_flag = words + 1;
+  volatile int* bad_tag = words + 2;               // number of the unit in which a non-finite value was last met
+  int* start_b = words + 3;
+  long long* start_rem = reinterpret_cast<long long*>(words + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cta = blockIdx.x, n_cta = gridDim.x;
+  const Abort ab{abort_flag, a.status};
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const bool poisoned = decode_poisoned(a.status);
+  const bool misplaced = (base & 1023u) != 0;      // the tiles' swizzle needs the window's alignment
+
+  // ---- where this CTA's run begins
+  const int per = (a.n_req + kThreads - 1) / kThreads;
+  const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
+  long long mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) mine += request(a, b).tiles;
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) scan[warp] = incl;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < P::SLOTS; ++s) { mbar_init(bar(P::BAR_FULL + s), 1); mbar_init(bar(P::BAR_FREE + s), 1); }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(bar(P::BAR_S + x), 1);
+      mbar_init(bar(P::BAR_P + x), 128);
+      mbar_init(bar(P::BAR_PV + x), 1);
+      mbar_init(bar(P::BAR_QFULL + x), 1);
+      mbar_init(bar(P::BAR_QFREE + x), 1);
+    }
+    for (int e = 0; e < kUnitRing; ++e) { mbar_init(bar(P::BAR_UNIT + e), 1); mbar_init(bar(P::BAR_UFREE + e), kSoftmaxWarps + 2); }
+    mbar_init(bar(P::BAR_EX), 256);
+    mbar_init(bar(P::BAR_EXDONE), 256);
+    *abort_flag = 0;
+    *bad_tag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
+  }
+  if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  long long before = incl - mine, total = 0;
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += scan[w];
+    total += scan[w];
+  }
+  const long long quota = total / n_cta, extra = total % n_cta;      // the first `extra` runs are one tile longer
+  const long long w0 = cta * quota + min((long long)cta, extra), w1 = w0 + quota + (cta < extra ? 1 : 0);
+  if (before <= w0 && w0 < before + mine) {
+    long long at = before;
+    for (int b = b_lo; b < b_hi; ++b) {
+      const long long t = request(a, b).tiles;
+      if (w0 < at + t) { *start_b = b; *start_rem = w0 - at; break; }
+      at += t;
+    }
+  }
+  __syncthreads();
+  const bool idle = poisoned || misplaced || w0 >= w1;
+
+  if (warp == kScheduler) {
+    // ------------------------------------------------------------ units and their queries
+    bool ok = true;
+    int seq = 0, uses[2] = {0, 0}, half = 0;
+    if (lane == 0) work.meta[cta].last_cta = -1;
+    if (__all_sync(0xffffffffu, !idle)) {
+      int b = *start_b;
+      long long rem = *start_rem, w = w0;
+      Request q = request(a, b);
+      while (w < w1 && ok) {
+        while (rem >= q.tiles && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
+        if (rem >= q.tiles) break;                   // not reached while the lengths stand still
+        Unit u;
+        const long long nth = rem / q.kt;
+        u.kt0 = (int)(rem - nth * q.kt);
+        u.kt_all = q.kt;
+        u.n_tiles = (int)min((long long)(q.kt - u.kt0), w1 - w);
+        u.g = (int)(nth / q.passes);
+        u.b = b;
+        u.start = q.start;
+        u.r0 = (int)(nth - (long long)u.g * q.passes) * kUnitRows;
+        u.rows = min(kUnitRows, q.n * a.group - u.r0);
+        u.len = q.len;
+        u.past = q.past;
+        u.half = u.rows > 128 ? 0 : half;
+        const long long z = w - u.kt0 + u.kt_all - 1, cut = extra * (quota + 1);
+        u.last_cta = (int)(z < cut ? z / (quota + 1) : extra + (z - cut) / quota);
+        const int e = seq % kUnitRing;
+        if (seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
+        if (!ok) break;
+        if (lane == 0) {
+          units[e] = u;
+          if (u.kt0 == 0 && u.n_tiles < u.kt_all) {
+            Meta m{u.last_cta, u.start, u.r0, u.rows, u.g, {0, 0, 0}};
+            work.meta[cta] = m;
+          }
+          if (a.seq_lens[b] > q.len) report_range(a.status, kWhereTreePage);   // longer than its table row
+          mbar_arrive(bar(P::BAR_UNIT + e));
+        }
+        ++seq;
+        // its queries: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA descriptors say
+        for (int h = u.half; h * 128 - u.half * 128 < u.rows && ok; ++h) {
+          if (uses[h] > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + h), (uses[h] - 1) & 1, ab, 41));
+          if (!ok) break;
+          const int first = (h - u.half) * 128, n_here = min(128, u.rows - first);
+          for (int i = lane; i < n_here * (D / 8); i += 32) {
+            const int r = i / (D / 8), piece = i % (D / 8);
+            const int abs_row = u.r0 + first + r;
+            const int token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
+            const __nv_bfloat16* src = a.q + head * a.q_sh + (u.start + token) * a.q_sn + piece * 8;
+            cp_async16(base + h * P::QHALF + (piece >> 3) * P::QBOX + r * 128 + (((piece & 7) ^ (r & 7)) << 4), src);
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + h));
+          ++uses[h];
+        }
+        if (u.rows <= 128) half ^= 1;
+        w += u.n_tiles;
+        rem += u.n_tiles;
+      }
+    }
+    // no more units
+    const int e = seq % kUnitRing;
+    if (ok && seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
+    if (ok && lane == 0) {
+      units[e].n_tiles = 0;
+      mbar_arrive(bar(P::BAR_UNIT + e));
+    }
+  } else if (warp == kProducer) {
+    // ------------------------------------------------------------ K and V tiles
+    bool ok = true;
+    long long step = 0;                              // tiles put into the ring, K and V counted apart
+    const int page = 1 << a.page_log2;
+    const int per_tile = max(kTile >> a.page_log2, 1), rows = min(page, kTile);
+    for (int seq = 0; ok; ++seq) {
+      const int e = seq % kUnitRing;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
+      if (!ok) break;
+      const Unit u = units[e];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+      if (u.n_tiles == 0) break;
+      const int32_t* row = a.table + (size_t)u.b * a.max_pages;
+      // lane p looks up page p of the tile, one tile ahead
+      auto lookup = [&](int kt) {
+        const int key = kt * kTile + lane * page;
+        return lane < per_tile && key < u.len ? row[key >> a.page_log2] : -1;
+      };
+      int id = lookup(u.kt0);
+      for (int t = 0; t < u.n_tiles && ok; ++t) {
+        const int kt = u.kt0 + t, key = kt * kTile + lane * page;
+        const int next = t + 1 < u.n_tiles ? lookup(kt + 1) : -1;
+        const bool live = lane < per_tile && key < u.len;
+        const int n_live = __popc(__ballot_sync(0xffffffffu, live));
+        if (live && (id < 0 || id >= a.n_pages)) {
+          report_range(a.status, kWhereTreePage);
+          id = a.n_pages;                            // outside the tensor map: the load fills in zeros
+        }
+        for (int kv = 0; kv < 2 && ok; ++kv, ++step) {
+          const int s = (int)(step % P::SLOTS);
+          if (step >= P::SLOTS) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (uint32_t)(step / P::SLOTS - 1) & 1, ab, 51));
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(bar(P::BAR_FULL + s), n_live * rows * D * 2);
+          __syncwarp();
+          if (live) {
+            const uint32_t dst = base + P::RING_OFF + s * P::SLOT + lane * rows * 128;
+#pragma unroll
+            for (int x = 0; x < P::NBOX; ++x)
+              tma_load_4d(dst + x * P::KBOX, kv ? &tm_v : &tm_k, bar(P::BAR_FULL + s), x * 64, key & (page - 1), u.g, id);
+          }
+          __syncwarp();
+        }
+        id = next;
+      }
+    }
+    if (*abort_flag && lane == 0) {
+      // let the copies already in flight land before the CTA gives its shared memory back
+      const long long t0 = clock64();
+      for (long long i = step > P::SLOTS ? step - P::SLOTS : 0; i < step; ++i)
+        while (!mbar_test(bar(P::BAR_FULL + (int)(i % P::SLOTS)), (uint32_t)(i / P::SLOTS) & 1) && clock64() - t0 < kWaitCycles / 8) {}
+    }
+  } else if (warp == kIssuer) {
+    // ------------------------------------------------------------ products
+    if (lane == 0) {
+      constexpr uint32_t idesc_qk = instr_desc(128, kTile, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
+      // Jobs alternate between the streams: job i belongs to stream i & 1.  S of a job may be computed once the stream's
+      // previous P has been handed to its product, so at most two jobs are between their two products.
+      struct Job {
+        long long v_step;      // ring position of its V tile
+        bool first, frees;     // first of the stream in its unit; last reader of the V tile
+      } job[2];
+      Unit u;
+      u.n_tiles = 0;
+      int seq = 0, sub = 0, tile = 0;      // the unit being entered, and the next job in it
+      bool open = false, done = false;
+      bool fresh[2] = {false, false};
+      int q_uses[2] = {0, 0}, s_count[2] = {0, 0};
+      bool q_ready[2] = {false, false};
+      long long tiles_before = 0;                    // tiles of earlier units
+      long long n_qk = 0, n_pv = 0, idle_since = 0;
+      uint32_t polls = 0;
+      while (!(done && n_pv == n_qk)) {
+        bool moved = false;
+        if (!done && !open) {
+          const int e = seq % kUnitRing;
+          if (mbar_test(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1)) {
+            u = units[e];
+            mbar_arrive(bar(P::BAR_UFREE + e));
+            ++seq;
+            tile = sub = 0;
+            open = u.n_tiles > 0;
+            done = !open;
+            fresh[0] = fresh[1] = true;
+            q_ready[0] = q_ready[1] = false;
+            moved = true;
+          }
+        }
+        if (open && n_qk < n_pv + 2) {
+          const int x = (int)(n_qk & 1);
+          const bool both = u.rows > 128;
+          const int h = both ? x : u.half;
+          const long long k_step = 2 * (tiles_before + tile);
+          const int s = (int)(k_step % P::SLOTS);
+          if (!q_ready[h] && mbar_test(bar(P::BAR_QFULL + h), q_uses[h] & 1)) { q_ready[h] = true; ++q_uses[h]; }
+          if (q_ready[h] && mbar_test(bar(P::BAR_FULL + s), (uint32_t)(k_step / P::SLOTS) & 1)) {
+            tc_fence_after();
+            const uint32_t sq = base + h * P::QHALF, sk = base + P::RING_OFF + s * P::SLOT;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_ss(tmem + P::S_COL + x * 128, smem_desc(sq + (kk >> 2) * P::QBOX + (kk & 3) * 32, 16, 1024),
+                     smem_desc(sk + (kk >> 2) * P::KBOX + (kk & 3) * 32, 16, 1024), idesc_qk, kk > 0);
+            mma_commit(bar(P::BAR_S + x));
+            const bool last_sub = !both || sub == 1;
+            if (last_sub) mma_commit(bar(P::BAR_FREE + s));
+            job[x].v_step = k_step + 1;
+            job[x].first = fresh[x];
+            job[x].frees = last_sub;
+            fresh[x] = false;
+            if (tile == u.n_tiles - 1) mma_commit(bar(P::BAR_QFREE + h));        // the unit's last use of this half
+            if (last_sub) { sub = 0; ++tile; } else { sub = 1; }
+            if (tile == u.n_tiles) { tiles_before += u.n_tiles; open = false; }
+            ++n_qk;
+            moved = true;
+          }
+        }
+        if (n_pv < n_qk) {
+          const int x = (int)(n_pv & 1);
+          const long long v_step = job[x].v_step;
+          const int s = (int)(v_step % P::SLOTS);
+          if (mbar_test(bar(P::BAR_P + x), s_count[x] & 1) && mbar_test(bar(P::BAR_FULL + s), (uint32_t)(v_step / P::SLOTS) & 1)) {
+            tc_fence_after();
+            const uint32_t sv = base + P::RING_OFF + s * P::SLOT;
+#pragma unroll
+            for (int kk = 0; kk < kTile / 16; ++kk)
+              mma_ts(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, smem_desc(sv + kk * 16 * 128, P::KBOX, 1024), idesc_pv,
+                     !job[x].first || kk > 0);
+            mma_commit(bar(P::BAR_PV + x));
+            if (job[x].frees) mma_commit(bar(P::BAR_FREE + s));
+            ++s_count[x];
+            ++n_pv;
+            moved = true;
+          }
+        }
+        if (moved) {
+          idle_since = 0;
+          polls = 0;
+        } else if ((++polls & 63u) == 0u) {
+          if (*abort_flag) break;
+          if ((polls & 4095u) == 0u) {
+            const long long now = clock64();
+            if (idle_since == 0) idle_since = now;
+            else if (now - idle_since > kWaitCycles) {
+              *abort_flag = 1;
+              if (atomicCAS(a.status, 0, (int)SP_ERR_TIMEOUT) == 0) a.status[1] = 60;
+              break;
+            }
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ softmax and epilogue
+    const int x = warp >> 2;                          // stream
+    const int row = threadIdx.x & 127;                // TMEM lane
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lanes + P::S_COL + x * 128, t_o = tmem + lanes + P::O_COL + x * P::O_STEP;
+    const float scale = a.scale_log2;
+    bool ok = true;
+    long long jobs_before = 0, tiles_before = 0;
+    uint32_t n_jobs = 0, n_joins = 0;                 // of this stream so far; joins of both streams
+    for (int seq = 0; ok; ++seq) {
+      const int e = seq % kUnitRing;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
+      if (!ok) break;
+      const Unit u = units[e];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+      if (u.n_tiles == 0) break;
+      const bool both = u.rows > 128;                 // the streams are halves of the rows; else they take turns at the tiles
+      const int my_row = both ? x * 128 + row : row;  // row of the unit
+      const bool warp_live = (both ? x * 128 : 0) + (warp & 3) * 32 < u.rows;
+      const int abs_row = u.r0 + my_row;
+      const int token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
+      const int t_first = both ? 0 : (int)((jobs_before + x) & 1), t_step = both ? 1 : 2;
+      float m_ref = kNoMax, l = 0.f;
+      for (int t = t_first; t < u.n_tiles && ok; t += t_step) {
+        const int k0 = (u.kt0 + t) * kTile;
+        const bool special = k0 + kTile > min(u.past, u.len);
+        ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + x), n_jobs & 1, ab, 31));
+        if (!ok) break;
+        tc_fence_after();
+        if (special) {
+          // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite)
+          const long long v_step = 2 * (tiles_before + t) + 1;
+          const int s = (int)(v_step % P::SLOTS);
+          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (uint32_t)(v_step / P::SLOTS) & 1, ab, 32));
+          if (!ok) break;
+          const int key = k0 + row;
+          if (key >= min(u.past, u.len)) {
+            bool wrote = false;
+#pragma unroll
+            for (int b = 0; b < P::NBOX; ++b) {
+              uint4* v = reinterpret_cast<uint4*>(smem + P::RING_OFF + s * P::SLOT + b * P::KBOX + row * 128);
+              for (int i = 0; i < 8; ++i) {
+                if (key >= u.len) {
+                  v[i] = make_uint4(0, 0, 0, 0);
+                  wrote = true;
+                } else {
+                  uint4 y = v[i];
+                  if (nonfinite2(y.x) || nonfinite2(y.y) || nonfinite2(y.z) || nonfinite2(y.w)) {
+                    *bad_tag = seq + 1;
+                    __threadfence_block();            // whoever finds the zeros finds the tag too
+                    uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                    for (int c = 0; c < 4; ++c) {
+                      if ((w[c] & 0x7f80u) == 0x7f80u) w[c] &= 0xffff0000u;
+                      if ((w[c] & 0x7f800000u) == 0x7f800000u) w[c] &= 0xffffu;
+                    }
+                    v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    wrote = true;
+                  }
+                }
+              }
+            }
+            if (wrote) fence_async_smem();
+          }
+          __syncwarp();
+        }
+        if (warp_live) {
+          uint32_t s[kTile];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+          float mx = -CUDART_INF_F;
+          if (special) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t seen = my_row < u.rows ? seen32(a, u, token, k0 + c * 32) : 0u;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float y = (seen >> i) & 1 ? __uint_as_float(s[c * 32 + i]) : -CUDART_INF_F;
+                s[c * 32 + i] = __float_as_uint(y);
+                mx = fmaxf(mx, y);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < kTile; ++c) mx = fmaxf(mx, __uint_as_float(s[c]));
+          }
+          mx *= scale;
+          const float m_new = mx > m_ref + 8.f ? mx : m_ref;
+          const float alpha = ex2_approx(m_ref - m_new);
+          float sum = 0.f;
+          uint32_t p[kTile / 2];
+#pragma unroll
+          for (int c = 0; c < kTile; c += 2) {
+            const float p0 = ex2_approx(fmaf(__uint_as_float(s[c]), scale, -m_new));
+            const float p1 = ex2_approx(fmaf(__uint_as_float(s[c + 1]), scale, -m_new));
+            sum += p0 + p1;
+            p[c / 2] = pack_bf16(p0, p1);
+          }
+          l = l * alpha + sum;
+          if (t != t_first && __any_sync(0xffffffffu, m_new != m_ref)) {
+            // O so far is relative to the old reference (the stream's previous product came before this S)
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[32];
+              tmem_ld32(t_o + c * 32, o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+              tmem_st32(t_o + c * 32, o);
+            }
+          }
+          m_ref = m_new;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) tmem_st32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&p[c * 32]));
+          tmem_wait_st();
+        }
+        tc_fence_before();
+        mbar_arrive(bar(P::BAR_P + x));
+        ++n_jobs;
+      }
+      const int mine_jobs = t_first < u.n_tiles ? (u.n_tiles - t_first + t_step - 1) / t_step : 0;
+      if (ok && mine_jobs > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + x), (n_jobs - 1) & 1, ab, 33));
+      // join the streams' weights
+      float m_all = m_ref, l_all = l, f0 = 1.f, f1 = 1.f;           // factors of O of stream 0 and 1
+      bool use0 = l != 0.f, use1 = use0;
+      if (!both && ok) {
+        tc_fence_before();
+        ex[x * 128 + row] = make_float2(m_ref, l);
+        mbar_arrive(bar(P::BAR_EX));
+        ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_EX), n_joins & 1, ab, 34));
+        if (ok) {
+          const float2 e0 = ex[row], e1 = ex[128 + row];
+          use0 = e0.y != 0.f;                         // a NaN counts as in use
+          use1 = e1.y != 0.f;
+          m_all = fmaxf(use0 ? e0.x : kNoMax, use1 ? e1.x : kNoMax);
+          f0 = use0 ? ex2_approx(e0.x - m_all) : 0.f;
+          f1 = use1 ? ex2_approx(e1.x - m_all) : 0.f;
+          l_all = (use0 ? e0.y * f0 : 0.f) + (use1 ? e1.y * f1 : 0.f);
+        }
+      }
+      if (ok) {
+        tc_fence_after();
+        const bool whole = u.kt0 == 0 && u.n_tiles == u.kt_all;
+        const float inv = l_all != 0.f ? 1.f / l_all : 0.f;
+        const int c_lo = both ? 0 : x * (D / 64), c_n = both ? D / 32 : D / 64;   // 32-column chunks that this group writes
+        const bool repair = *bad_tag == seq + 1;
+        const size_t slot = ((size_t)cta * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + my_row;
+        if (warp_live) {
+          const bool live = my_row < u.rows;
+          for (int c = c_lo; c < c_lo + c_n; ++c) {
+            float o[32];
+            uint32_t y[32];
+            if (both) {
+              tmem_ld32(t_o + c * 32, y);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = use0 ? __uint_as_float(y[i]) : 0.f;
+            } else {
+              const uint32_t at = tmem + lanes + P::O_COL + c * 32;
+              tmem_ld32(at, y);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = use0 ? __uint_as_float(y[i]) * f0 : 0.f;
+              tmem_ld32(at + P::O_STEP, y);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] += use1 ? __uint_as_float(y[i]) * f1 : 0.f;
+            }
+            if (!live) continue;
+            if (whole) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] *= inv;
+            }
+            if (repair) add_nonfinite(a, u, token, c * 32, o);
+            if (whole) {
+              uint4* dst = reinterpret_cast<uint4*>(a.o + head * a.o_sh + (u.start + token) * a.o_sn + c * 32);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                dst[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]),
+                                    pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+            } else {
+              float4* dst = reinterpret_cast<float4*>(work.part + slot * D + c * 32);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+          }
+          if (live && (both || x == 0)) {
+            if (!whole) work.ml[slot] = make_float2(m_all, l_all);
+            else if (a.lse)
+              a.lse[(size_t)head * a.rows + u.start + token] = l_all != 0.f ? (m_all + log2f(l_all)) * 0.6931471805599453f : -CUDART_INF_F;
+          }
+        }
+        if (!both) {
+          // neither stream's next product may overwrite an O that the other group is still reading
+          tc_fence_before();
+          mbar_arrive(bar(P::BAR_EXDONE));
+          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_EXDONE), n_joins & 1, ab, 35));
+          tc_fence_after();
+          ++n_joins;
+        }
+      }
+      jobs_before += both ? 2ll * u.n_tiles : u.n_tiles;
+      tiles_before += u.n_tiles;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kIssuer) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the parts of a cut unit, in the order of the keys: the part of the CTA in which the unit begins, then those of
+// the CTAs after it.  Block (c, y): the unit that begins in CTA c and goes on, rows 8 y, 8 y + 8 gridDim.y, ...  With
+// fewer than eight rows the warps share a row's parts.
+constexpr int kJoinWarps = 8;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinWarps * 32) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a, const Work work) {
+  constexpr int E = D / 32;
+  __shared__ float s_m[kJoinWarps], s_l[kJoinWarps], s_o[kJoinWarps][D];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (decode_poisoned(a.status)) return;
+  const Meta m = work.meta[blockIdx.x];
+  if (m.last_cta < 0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int parts = m.last_cta - (int)blockIdx.x + 1;
+  for (int r0 = blockIdx.y * kJoinWarps; r0 < m.rows; r0 += gridDim.y * kJoinWarps) {
+    const int n_here = min(kJoinWarps, m.rows - r0);
+    const int share = n_here > 4 ? 1 : n_here > 2 ? 2 : n_here > 1 ? 4 : 8;   // warps of a row
+    const int r = r0 + warp / share, turn = warp % share;
+    float mx = kNoMax, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    if (r < m.rows) {
+#pragma unroll 4
+      for (int p = turn; p < parts; p += share) {
+        const size_t slot = ((size_t)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kUnitRows + r;
+        const float2 ml = work.ml[slot];
+        float y[E];
+        if (E == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(work.part + slot * D + lane * 4);
+          y[0] = v.x; y[1] = v.y; y[2 % E] = v.z; y[3 % E] = v.w;
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(work.part + slot * D + lane * 2);
+          y[0] = v.x; y[1] = v.y;
+        }
+        if (ml.y == 0.f) continue;
+        const float top = fmaxf(mx, ml.x), f_old = exp2f(mx - top), f = exp2f(ml.x - top);
+        l = l * f_old + ml.y * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = o[e] * f_old + y[e] * f;
+        mx = top;
+      }
+    }
+    if (lane == 0) { s_m[warp] = mx; s_l[warp] = l; }
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
+    __syncthreads();
+    if (turn == 0 && r < m.rows) {
+      for (int w = warp + 1; w < warp + share; ++w) {
+        if (s_l[w] == 0.f) continue;
+        const float top = fmaxf(mx, s_m[w]), f_old = exp2f(mx - top), f = exp2f(s_m[w] - top);
+        l = l * f_old + s_l[w] * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = o[e] * f_old + s_o[w][lane * E + e] * f;
+        mx = top;
+      }
+      const int abs_row = m.r0 + r, token = abs_row / a.group, head = m.g * a.group + abs_row % a.group;
+      const float inv = l != 0.f ? 1.f / l : 0.f;
+      __nv_bfloat16* dst = a.o + head * a.o_sh + (m.start + token) * a.o_sn + lane * E;
+      uint32_t w[E / 2];
+#pragma unroll
+      for (int e = 0; e < E; e += 2) w[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
+      if (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[E / 2 - 1]);
+      else *reinterpret_cast<uint32_t*>(dst) = w[0];
+      if (a.lse && lane == 0)
+        a.lse[(size_t)head * a.rows + m.start + token] = l != 0.f ? (mx + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+// [pages, heads, page, D] cache -> 4-D tensor map with a (64 columns x page rows, 128 at most) box, 128-byte swizzle.
+bool make_cache_map(CUtensorMap* m, const PagedCache& c, int d, int page, int heads, int pages) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  // the stride of a size-1 dimension is never used, but the encoder wants a valid one
+  const cuuint64_t any = (cuuint64_t)d * 2;
+  cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)page, (cuuint64_t)heads, (cuuint64_t)pages};
+  cuuint64_t strides[3] = {(cuuint64_t)c.s_tok * 2, heads > 1 ? (cuuint64_t)c.s_head * 2 : any, pages > 1 ? (cuuint64_t)c.s_page * 2 : any};
+  cuuint32_t box[4] = {64, (cuuint32_t)(page < kTile ? page : kTile), 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, c.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
+  CUtensorMap tk, tv;
+  if (!make_cache_map(&tk, a.kc, D, 1 << a.page_log2, a.hkv, a.n_pages) || !make_cache_map(&tv, a.vc, D, 1 << a.page_log2, a.hkv, a.n_pages))
+    return cudaErrorInvalidValue;
+  Work w;
+  const size_t slots = (size_t)n_cta * 2 * kUnitRows;
+  w.part = static_cast<float*>(ws);
+  w.ml = reinterpret_cast<float2*>(w.part + slots * 128);
+  w.meta = reinterpret_cast<Meta*>(w.ml + slots);
+  constexpr int smem = Plan<D>::TOTAL > 120 * 1024 ? Plan<D>::TOTAL : 120 * 1024;      // one CTA per SM (it takes all of TMEM)
+  static_assert(smem <= 232448, "");
+  cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  tree_attn_kernel<D><<<n_cta, kThreads, smem, s>>>(a, w, tk, tv);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  // started early, it waits for the first kernel's end on the device
+  const long long most = (long long)a.rows * a.group;
+  const int y = (int)((most < kUnitRows ? most : kUnitRows) + kJoinWarps - 1) / kJoinWarps;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n_cta, y < 8 ? y : 8);
+  cfg.blockDim = dim3(kJoinWarps * 32);
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, tree_attn_join_kernel<D>, a, w);
+}
+
+}  // namespace
+
+size_t tree_attn_workspace_bytes(int n_sm) {
+  return (size_t)n_sm * (2 * kUnitRows * (128 * sizeof(float) + sizeof(float2)) + sizeof(Meta));
+}
+
+cudaError_t launch_tree_attn(const TreeAttnArgs& a, void* ws, int n_sm, cudaStream_t s) {
+  return a.d == 128 ? launch<128>(a, ws, n_sm, s) : launch<64>(a, ws, n_sm, s);
+}
+
+}  // namespace sp

@@ -129,6 +129,14 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
       : "memory");
 }
+// registers -> 16 consecutive 32-bit columns of this thread's TMEM lane (does not wait)
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -315,7 +323,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   } else if (warp == kProducer) {
     // ------------------------------------------------------------ K and V tiles
     bool ok = true;
-    long long step = 0;                              // tiles put into the ring, K and V counted apart
+    uint32_t s = 0, lap = 0;                         // next slot of the ring, times round
     const int page = 1 << a.page_log2;
     const int per_tile = max(kTile >> a.page_log2, 1), rows = min(page, kTile);
     for (int seq = 0; ok; ++seq) {
@@ -342,9 +350,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
           report_range(a.status, kWhereTreePage);
           id = a.n_pages;                            // outside the tensor map: the load fills in zeros
         }
-        for (int kv = 0; kv < 2 && ok; ++kv, ++step) {
-          const int s = (int)(step % P::SLOTS);
-          if (step >= P::SLOTS) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (uint32_t)(step / P::SLOTS - 1) & 1, ab, 51));
+        for (int kv = 0; kv < 2; ++kv) {
+          if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (lap - 1) & 1, ab, 51));
           if (!ok) break;
           if (lane == 0) mbar_expect_tx(bar(P::BAR_FULL + s), n_live * rows * D * 2);
           __syncwarp();
@@ -355,6 +362,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
               tma_load_4d(dst + x * P::KBOX, kv ? &tm_v : &tm_k, bar(P::BAR_FULL + s), x * 64, key & (page - 1), u.g, id);
           }
           __syncwarp();
+          if (++s == P::SLOTS) { s = 0; ++lap; }
         }
         id = next;
       }
@@ -362,33 +370,54 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
     if (*abort_flag && lane == 0) {
       // let the copies already in flight land before the CTA gives its shared memory back
       const long long t0 = clock64();
-      for (long long i = step > P::SLOTS ? step - P::SLOTS : 0; i < step; ++i)
-        while (!mbar_test(bar(P::BAR_FULL + (int)(i % P::SLOTS)), (uint32_t)(i / P::SLOTS) & 1) && clock64() - t0 < kWaitCycles / 8) {}
+      for (uint32_t i = 0; i < P::SLOTS; ++i) {
+        const uint32_t laps = lap + (i < s);          // loads that this slot has been given
+        while (laps > 0 && !mbar_test(bar(P::BAR_FULL + i), (laps - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {}
+      }
     }
   } else if (warp == kIssuer) {
     // ------------------------------------------------------------ products
     if (lane == 0) {
       constexpr uint32_t idesc_qk = instr_desc(128, kTile, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
+      const uint64_t d_q = smem_desc(base, 16, 1024), d_k = smem_desc(base + P::RING_OFF, 16, 1024),
+                     d_v = smem_desc(base + P::RING_OFF, P::KBOX, 1024);
       // Jobs alternate between the streams: job i belongs to stream i & 1.  S of a job may be computed once the stream's
-      // previous P has been handed to its product, so at most two jobs are between their two products.
-      struct Job {
-        long long v_step;      // ring position of its V tile
-        bool first, frees;     // first of the stream in its unit; last reader of the V tile
-      } job[2];
+      // previous P has been handed to its product, so at most two jobs are between their two products.  One thread does
+      // all of this, and every instruction of the loop delays both streams: 32-bit counters, ring positions that advance
+      // by comparison, and per-stream flags in the bits of one register each.
       Unit u;
       u.n_tiles = 0;
-      int seq = 0, sub = 0, tile = 0;      // the unit being entered, and the next job in it
+      uint32_t seq = 0, tile = 0, sub = 0;           // the unit being entered, and the next job in it
       bool open = false, done = false;
-      bool fresh[2] = {false, false};
-      int q_uses[2] = {0, 0}, s_count[2] = {0, 0};
-      bool q_ready[2] = {false, false};
-      long long tiles_before = 0;                    // tiles of earlier units
-      long long n_qk = 0, n_pv = 0, idle_since = 0;
-      uint32_t polls = 0;
+      uint32_t first = 0, frees = 0;                 // bit x: the job of stream x opens its sum / is the last reader of its tile
+      uint32_t fresh = 0, q_ready = 0, q_phase = 0, p_phase = 0;
+      uint32_t k_slot = 0, k_phase = 0, v_slot = 1, v_phase = 0;       // ring positions of the next K and V tile
+      uint32_t n_qk = 0, n_pv = 0, polls = 0;
+      long long idle_since = 0;
       while (!(done && n_pv == n_qk)) {
         bool moved = false;
-        if (!done && !open) {
-          const int e = seq % kUnitRing;
+        if (n_pv != n_qk) {
+          const uint32_t x = n_pv & 1, bit = 1u << x;
+          if (mbar_test(bar(P::BAR_P + x), (p_phase >> x) & 1) && mbar_test(bar(P::BAR_FULL + v_slot), v_phase)) {
+            tc_fence_after();
+            const uint64_t dv = d_v + v_slot * (P::SLOT >> 4);
+            const uint32_t acc = (first & bit) ? 0u : 1u;
+#pragma unroll
+            for (int kk = 0; kk < kTile / 16; ++kk)
+              mma_ts(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, dv + kk * (16 * 128 >> 4), idesc_pv, kk > 0 ? 1u : acc);
+            mma_commit(bar(P::BAR_PV + x));
+            if (frees & bit) {
+              mma_commit(bar(P::BAR_FREE + v_slot));
+              v_slot += 2;
+              if (v_slot >= P::SLOTS) { v_slot -= P::SLOTS; v_phase ^= 1; }
+            }
+            p_phase ^= bit;
+            ++n_pv;
+            moved = true;
+          }
+        }
+        if (!open && !done) {
+          const uint32_t e = seq % kUnitRing;
           if (mbar_test(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1)) {
             u = units[e];
             mbar_arrive(bar(P::BAR_UFREE + e));
@@ -396,54 +425,40 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
             tile = sub = 0;
             open = u.n_tiles > 0;
             done = !open;
-            fresh[0] = fresh[1] = true;
-            q_ready[0] = q_ready[1] = false;
+            fresh = 3;
+            q_ready = 0;
             moved = true;
           }
         }
-        if (open && n_qk < n_pv + 2) {
-          const int x = (int)(n_qk & 1);
+        if (open && n_qk - n_pv < 2) {
+          const uint32_t x = n_qk & 1, bit = 1u << x;
           const bool both = u.rows > 128;
-          const int h = both ? x : u.half;
-          const long long k_step = 2 * (tiles_before + tile);
-          const int s = (int)(k_step % P::SLOTS);
-          if (!q_ready[h] && mbar_test(bar(P::BAR_QFULL + h), q_uses[h] & 1)) { q_ready[h] = true; ++q_uses[h]; }
-          if (q_ready[h] && mbar_test(bar(P::BAR_FULL + s), (uint32_t)(k_step / P::SLOTS) & 1)) {
+          const uint32_t h = both ? x : (uint32_t)u.half;
+          if (!((q_ready >> h) & 1) && mbar_test(bar(P::BAR_QFULL + h), (q_phase >> h) & 1)) { q_ready |= 1u << h; q_phase ^= 1u << h; }
+          if (((q_ready >> h) & 1) && mbar_test(bar(P::BAR_FULL + k_slot), k_phase)) {
             tc_fence_after();
-            const uint32_t sq = base + h * P::QHALF, sk = base + P::RING_OFF + s * P::SLOT;
+            const uint64_t dq = d_q + h * (P::QHALF >> 4), dk = d_k + k_slot * (P::SLOT >> 4);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
-              mma_ss(tmem + P::S_COL + x * 128, smem_desc(sq + (kk >> 2) * P::QBOX + (kk & 3) * 32, 16, 1024),
-                     smem_desc(sk + (kk >> 2) * P::KBOX + (kk & 3) * 32, 16, 1024), idesc_qk, kk > 0);
+              mma_ss(tmem + P::S_COL + x * 128, dq + (kk >> 2) * (P::QBOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::KBOX >> 4) + (kk & 3) * 2, idesc_qk,
+                     kk > 0);
             mma_commit(bar(P::BAR_S + x));
             const bool last_sub = !both || sub == 1;
-            if (last_sub) mma_commit(bar(P::BAR_FREE + s));
-            job[x].v_step = k_step + 1;
-            job[x].first = fresh[x];
-            job[x].frees = last_sub;
-            fresh[x] = false;
-            if (tile == u.n_tiles - 1) mma_commit(bar(P::BAR_QFREE + h));        // the unit's last use of this half
-            if (last_sub) { sub = 0; ++tile; } else { sub = 1; }
-            if (tile == u.n_tiles) { tiles_before += u.n_tiles; open = false; }
+            first = (first & ~bit) | (fresh & bit);
+            fresh &= ~bit;
+            frees = last_sub ? frees | bit : frees & ~bit;
+            if (tile + 1 == (uint32_t)u.n_tiles) mma_commit(bar(P::BAR_QFREE + h));        // the unit's last use of this half
+            if (last_sub) {
+              mma_commit(bar(P::BAR_FREE + k_slot));
+              k_slot += 2;
+              if (k_slot >= P::SLOTS) { k_slot -= P::SLOTS; k_phase ^= 1; }
+              sub = 0;
+              ++tile;
+              open = tile != (uint32_t)u.n_tiles;
+            } else {
+              sub = 1;
+            }
             ++n_qk;
-            moved = true;
-          }
-        }
-        if (n_pv < n_qk) {
-          const int x = (int)(n_pv & 1);
-          const long long v_step = job[x].v_step;
-          const int s = (int)(v_step % P::SLOTS);
-          if (mbar_test(bar(P::BAR_P + x), s_count[x] & 1) && mbar_test(bar(P::BAR_FULL + s), (uint32_t)(v_step / P::SLOTS) & 1)) {
-            tc_fence_after();
-            const uint32_t sv = base + P::RING_OFF + s * P::SLOT;
-#pragma unroll
-            for (int kk = 0; kk < kTile / 16; ++kk)
-              mma_ts(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, smem_desc(sv + kk * 16 * 128, P::KBOX, 1024), idesc_pv,
-                     !job[x].first || kk > 0);
-            mma_commit(bar(P::BAR_PV + x));
-            if (job[x].frees) mma_commit(bar(P::BAR_FREE + s));
-            ++s_count[x];
-            ++n_pv;
             moved = true;
           }
         }
@@ -473,7 +488,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
     const uint32_t t_s = tmem + lanes + P::S_COL + x * 128, t_o = tmem + lanes + P::O_COL + x * P::O_STEP;
     const float scale = a.scale_log2;
     bool ok = true;
-    long long jobs_before = 0, tiles_before = 0;
+    uint32_t jobs_before = 0, tiles_before = 0;
     uint32_t n_jobs = 0, n_joins = 0;                 // of this stream so far; joins of both streams
     for (int seq = 0; ok; ++seq) {
       const int e = seq % kUnitRing;
@@ -498,9 +513,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         tc_fence_after();
         if (special) {
           // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite)
-          const long long v_step = 2 * (tiles_before + t) + 1;
-          const int s = (int)(v_step % P::SLOTS);
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (uint32_t)(v_step / P::SLOTS) & 1, ab, 32));
+          const uint32_t v_step = 2 * (tiles_before + t) + 1, s = v_step % P::SLOTS;
+          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (v_step / P::SLOTS) & 1, ab, 32));
           if (!ok) break;
           const int key = k0 + row;
           if (key >= min(u.past, u.len)) {
@@ -533,36 +547,46 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
           __syncwarp();
         }
         if (warp_live) {
-          uint32_t s[kTile];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+          // The 128 logits are read from TMEM twice, for the maximum and for the exponentials: held in registers they
+          // would spill.  P (bf16 pairs) takes the first half of the columns; each chunk of it lands on logits already used.
           float mx = -CUDART_INF_F;
+          uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
           if (special) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t seen = my_row < u.rows ? seen32(a, u, token, k0 + c * 32) : 0u;
+            for (int c = 0; c < 4; ++c) seen[c] = my_row < u.rows ? seen32(a, u, token, k0 + c * 32) : 0u;
+          }
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float y = (seen >> i) & 1 ? __uint_as_float(s[c * 32 + i]) : -CUDART_INF_F;
-                s[c * 32 + i] = __float_as_uint(y);
-                mx = fmaxf(mx, y);
-              }
+          for (int c = 0; c < 4; ++c) {
+            uint32_t s[32];
+            tmem_ld32(t_s + c * 32, s);
+            if (special) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (seen[c] >> i) & 1 ? __uint_as_float(s[i]) : -CUDART_INF_F);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(s[i]));
             }
-          } else {
-#pragma unroll
-            for (int c = 0; c < kTile; ++c) mx = fmaxf(mx, __uint_as_float(s[c]));
           }
           mx *= scale;
           const float m_new = mx > m_ref + 8.f ? mx : m_ref;
           const float alpha = ex2_approx(m_ref - m_new);
           float sum = 0.f;
-          uint32_t p[kTile / 2];
 #pragma unroll
-          for (int c = 0; c < kTile; c += 2) {
-            const float p0 = ex2_approx(fmaf(__uint_as_float(s[c]), scale, -m_new));
-            const float p1 = ex2_approx(fmaf(__uint_as_float(s[c + 1]), scale, -m_new));
-            sum += p0 + p1;
-            p[c / 2] = pack_bf16(p0, p1);
+          for (int c = 0; c < 4; ++c) {
+            uint32_t s[32], p[16];
+            tmem_ld32(t_s + c * 32, s);
+            if (special) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) s[i] = (seen[c] >> i) & 1 ? s[i] : 0xff800000u;      // -infinity
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const float p0 = ex2_approx(fmaf(__uint_as_float(s[i]), scale, -m_new));
+              const float p1 = ex2_approx(fmaf(__uint_as_float(s[i + 1]), scale, -m_new));
+              sum += p0 + p1;
+              p[i / 2] = pack_bf16(p0, p1);
+            }
+            tmem_st16(t_s + c * 16, p);
           }
           l = l * alpha + sum;
           if (t != t_first && __any_sync(0xffffffffu, m_new != m_ref)) {
@@ -577,8 +601,6 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
             }
           }
           m_ref = m_new;
-#pragma unroll
-          for (int c = 0; c < 2; ++c) tmem_st32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&p[c * 32]));
           tmem_wait_st();
         }
         tc_fence_before();
@@ -663,7 +685,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
           ++n_joins;
         }
       }
-      jobs_before += both ? 2ll * u.n_tiles : u.n_tiles;
+      jobs_before += both ? 2 * u.n_tiles : u.n_tiles;
       tiles_before += u.n_tiles;
     }
   }

@@ -21,9 +21,12 @@
 // are joined at the end of the unit (both groups of warps read both O's from TMEM, half the columns each).
 //
 //   warps 0-3, 4-7  softmax and epilogue of stream 0 / 1: thread = TMEM lane = row
-//   warp 8          producer: page ids from the table, TMA loads of K and V pages into a ring of tile slots
+//   warp 8          producer: page ids from the table, TMA loads of K and V pages into a ring of tile slots, in the order
+//                   in which the products need them: K0 K1 V0 K2 V1 ... (a V tile that arrived with its K would hold a
+//                   slot for the whole softmax)
 //   warp 9          issuer (one thread): S = Q K^T and O += P V of whichever stream is ready
-//   warp 10         scheduler: walks the run, publishes units, gathers their Q rows into shared memory (cp.async)
+//   warp 10         scheduler: walks the run, publishes units
+//   warps 10, 11    gather the units' Q rows into shared memory (cp.async), every other pair of rows each
 //
 // Masks.  Only tiles that hold a key at or behind the first new token need one.  There the row's visibility bits are
 // shifted into place 32 keys at a time.  A masked probability is zero, but zero times a NaN in V is not: in those tiles
@@ -48,8 +51,8 @@ using namespace tc;
 
 constexpr int kTile = 128;                       // keys of a tile
 constexpr int kUnitRows = 256;
-constexpr int kThreads = 352;
-constexpr int kSoftmaxWarps = 8, kProducer = 8, kIssuer = 9, kScheduler = 10;
+constexpr int kThreads = 384;
+constexpr int kSoftmaxWarps = 8, kProducer = 8, kIssuer = 9, kScheduler = 10, kLoader = 11;
 constexpr int kUnitRing = 4;
 constexpr float kNoMax = -1e30f;                 // reference maximum before any visible key: finite, below any logit
 
@@ -66,8 +69,8 @@ struct Plan {
                        BAR_EX = BAR_UFREE + kUnitRing, BAR_EXDONE = BAR_EX + 1, BARS = BAR_EXDONE + 1;
   static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;
   static constexpr int EX_OFF = (UNIT_OFF + kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // float2 [2][128]
-  static constexpr int SCAN_OFF = EX_OFF + 2048;                                       // int64 [11], then small words
-  static constexpr int TOTAL = SCAN_OFF + 11 * 8 + 64;
+  static constexpr int SCAN_OFF = EX_OFF + 2048;                                       // int64 [12], then small words
+  static constexpr int TOTAL = SCAN_OFF + 12 * 8 + 64;
   static constexpr int S_COL = 0, O_COL = 256, O_STEP = D;  // S: 128 columns a stream; O: D columns a stream
 };
 
@@ -129,14 +132,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
       : "memory");
 }
-// registers -> 16 consecutive 32-bit columns of this thread's TMEM lane (does not wait)
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -159,18 +154,103 @@ __device__ __forceinline__ uint32_t seen32(const TreeAttnArgs& a, const Unit& u,
   return live & __funnelshift_r(word(w0), word(w0 + 1), (uint32_t)(x0 & 31));
 }
 
-// The non-finite values of new tokens that a row sees, added to 32 of its columns (they were left out of the products).
-__device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, int col, float (&o)[32]) {
+// The non-finite values of new tokens that a row sees, added to columns lo .. hi - 1 of what its thread has just written
+// (they were left out of the products): bf16 results, or fp32 partial sums.
+template <typename T>
+__device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, T* out, int lo, int hi) {
   const int k_from = max(u.kt0 * kTile, u.past), k_to = min((u.kt0 + u.n_tiles) * kTile, u.len);
   for (int key = k_from; key < k_to; ++key) {
     const int id = a.table[(size_t)u.b * a.max_pages + (key >> a.page_log2)];
     if (id < 0 || id >= a.n_pages || !(seen32(a, u, token, key) & 1)) continue;
-    const __nv_bfloat16* v = a.vc.data + id * a.vc.s_page + u.g * a.vc.s_head + (key & ((1 << a.page_log2) - 1)) * a.vc.s_tok + col;
-    for (int c = 0; c < 32; ++c) {
+    const __nv_bfloat16* v = a.vc.data + id * a.vc.s_page + u.g * a.vc.s_head + (key & ((1 << a.page_log2) - 1)) * a.vc.s_tok;
+    for (int c = lo; c < hi; ++c) {
       const float x = __bfloat162float(v[c]);
-      if (!isfinite(x)) o[c] += x;
+      if (!isfinite(x)) out[c] = static_cast<T>(static_cast<float>(out[c]) + x);
     }
   }
+}
+
+// Rare path of the softmax: the row's reference maximum has moved, so O of the earlier tiles (when there are any) and
+// the P chunks of this tile that are already stored are brought to the new one.  alpha is a power of two (references are
+// whole numbers), so nothing is rounded again.  Called by whole warps.
+template <int D>
+__device__ __noinline__ void rescale_tmem(uint32_t t_o, uint32_t t_s, float alpha, int stored, bool with_o) {
+  if (with_o) {
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tmem_ld32(t_o + c * 32, o);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+      tmem_st32(t_o + c * 32, o);
+    }
+  }
+#pragma unroll 1
+  for (int c = 0; c < stored; ++c) {
+    uint32_t p[16];
+    tmem_ld16(t_s + c * 16, p);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) p[e] = cvt_bf16x2(__uint_as_float(p[e] << 16) * alpha, __uint_as_float(p[e] & 0xffff0000u) * alpha);
+    tmem_st16(t_s + c * 16, p);
+  }
+}
+
+// The logits of the keys that a row does not see are set to -infinity in TMEM before the common path reads them.  Called
+// by whole warps; a row that is not the unit's (token < 0) sees nothing.
+__device__ __noinline__ void mask_tmem(const TreeAttnArgs& a, const Unit& u, int token, int k0, uint32_t t_s) {
+#pragma unroll 1
+  for (int c = 0; c < kTile / 32; ++c) {
+    const uint32_t seen = token >= 0 ? seen32(a, u, token, k0 + c * 32) : 0u;
+    if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
+    uint32_t s[32];
+    tmem_ld32(t_s + c * 32, s);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = (seen >> e) & 1 ? s[e] : 0xff800000u;
+    tmem_st32(t_s + c * 32, s);
+  }
+  tmem_wait_st();
+}
+
+// Values behind the sequence become zero in a V tile, and so do non-finite ones of new tokens (reported: see
+// add_nonfinite).  Rows lo .. hi - 1 of the tile, one after the other, the warp's lanes across the columns; eight rows of
+// loads in flight.  v: this lane's first word of row 0.
+template <int D>
+__device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first_behind, volatile int* tag, int mark) {
+  constexpr int BOXES = D / 64, BOX_WORDS = kTile * 128 / 4;
+  bool met = false;
+  int r = lo;
+#pragma unroll 1
+  for (; r < min(hi, first_behind); r += 8) {
+    uint32_t w[8 * BOXES];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int b = 0; b < BOXES; ++b) w[e * BOXES + b] = r + e < min(hi, first_behind) ? v[b * BOX_WORDS + (r + e) * 32] : 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int b = 0; b < BOXES; ++b) {
+        uint32_t x = w[e * BOXES + b];
+        if (!nonfinite2(x)) continue;
+        met = true;
+        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+        w[e * BOXES + b] = x;
+      }
+    if (met) {
+      *tag = mark;
+      __threadfence_block();
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int b = 0; b < BOXES; ++b)
+          if (r + e < min(hi, first_behind)) v[b * BOX_WORDS + (r + e) * 32] = w[e * BOXES + b];
+    }
+  }
+#pragma unroll 4
+  for (r = max(lo, first_behind); r < hi; ++r)
+#pragma unroll
+    for (int b = 0; b < BOXES; ++b) v[b * BOX_WORDS + r * 32] = 0u;
 }
 
 template <int D>
@@ -184,7 +264,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   float2* ex = reinterpret_cast<float2*>(smem + P::EX_OFF);
   long long* scan = reinterpret_cast<long long*>(smem + P::SCAN_OFF);
-  int* words = reinterpret_cast<int*>(smem + P::SCAN_OFF + 11 * 8);
+  int* words = reinterpret_cast<int*>(smem + P::SCAN_OFF + 12 * 8);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(words);
   volatile int* abort_flag = words + 1;
   volatile int* bad_tag = words + 2;               // number of the unit in which a non-finite value was last met
@@ -214,14 +294,14 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
     for (int s = 0; s < P::SLOTS; ++s) { mbar_init(bar(P::BAR_FULL + s), 1); mbar_init(bar(P::BAR_FREE + s), 1); }
     for (int x = 0; x < 2; ++x) {
       mbar_init(bar(P::BAR_S + x), 1);
-      mbar_init(bar(P::BAR_P + x), 128);
+      mbar_init(bar(P::BAR_P + x), 4);
       mbar_init(bar(P::BAR_PV + x), 1);
-      mbar_init(bar(P::BAR_QFULL + x), 1);
+      mbar_init(bar(P::BAR_QFULL + x), 2);
       mbar_init(bar(P::BAR_QFREE + x), 1);
     }
-    for (int e = 0; e < kUnitRing; ++e) { mbar_init(bar(P::BAR_UNIT + e), 1); mbar_init(bar(P::BAR_UFREE + e), kSoftmaxWarps + 2); }
-    mbar_init(bar(P::BAR_EX), 256);
-    mbar_init(bar(P::BAR_EXDONE), 256);
+    for (int e = 0; e < kUnitRing; ++e) { mbar_init(bar(P::BAR_UNIT + e), 1); mbar_init(bar(P::BAR_UFREE + e), kSoftmaxWarps + 3); }
+    mbar_init(bar(P::BAR_EX), kSoftmaxWarps);
+    mbar_init(bar(P::BAR_EXDONE), kSoftmaxWarps);
     *abort_flag = 0;
     *bad_tag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -250,10 +330,46 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   __syncthreads();
   const bool idle = poisoned || misplaced || w0 >= w1;
 
+  // A unit's queries into its half (halves) of the Q area: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA
+  // descriptors say.  Two warps share it; a lane keeps its piece of every (64 / pieces)-th row, whose token and head
+  // advance without division (one warp with a division per piece took 13000 cycles for 128 rows).
+  uint32_t q_loads = 0;                              // bit h: parity of the loads into half h so far; bit 2 + h: any
+  auto gather = [&](const Unit& u, int which) -> bool {
+    constexpr int PIECES = D / 8, STEP = 64 / PIECES;
+    const int piece = lane % PIECES, n_half = u.rows > 128 ? 2 : 1;
+    int r = lane / PIECES + which * (STEP / 2), hg = (u.r0 + r) % a.group;
+    const __nv_bfloat16* src = a.q + (int64_t)(u.g * a.group + hg) * a.q_sh + (int64_t)(u.start + (u.r0 + r) / a.group) * a.q_sn + piece * 8;
+    const int64_t down = STEP * a.q_sh, wrap = a.q_sn - a.group * a.q_sh;
+    for (int i = 0; i < n_half; ++i) {
+      const int h = u.half + i, end = min((i + 1) * 128, u.rows);
+      if ((q_loads >> (2 + h)) & 1)
+        if (!__all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + h), ((q_loads >> h) & 1) ^ 1, ab, 41))) return false;
+      q_loads = (q_loads ^ (1u << h)) | (4u << h);
+      const uint32_t box = base + h * P::QHALF + (piece >> 3) * P::QBOX;
+#pragma unroll 2
+      for (; r < end; r += STEP) {
+        const int in_half = r & 127;
+        cp_async16(box + in_half * 128 + (((piece & 7) ^ (in_half & 7)) << 4), src);
+        src += down;
+        hg += STEP;
+        while (hg >= a.group) { hg -= a.group; src += wrap; }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    for (int i = 0; i < n_half; ++i) {
+      if (i + 1 < n_half) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + u.half + i));
+    }
+    return true;
+  };
+
   if (warp == kScheduler) {
-    // ------------------------------------------------------------ units and their queries
+    // ------------------------------------------------------------ units
     bool ok = true;
-    int seq = 0, uses[2] = {0, 0}, half = 0;
+    int seq = 0, half = 0;
     if (lane == 0) work.meta[cta].last_cta = -1;
     if (__all_sync(0xffffffffu, !idle)) {
       int b = *start_b;
@@ -290,24 +406,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
           mbar_arrive(bar(P::BAR_UNIT + e));
         }
         ++seq;
-        // its queries: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA descriptors say
-        for (int h = u.half; h * 128 - u.half * 128 < u.rows && ok; ++h) {
-          if (uses[h] > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + h), (uses[h] - 1) & 1, ab, 41));
-          if (!ok) break;
-          const int first = (h - u.half) * 128, n_here = min(128, u.rows - first);
-          for (int i = lane; i < n_here * (D / 8); i += 32) {
-            const int r = i / (D / 8), piece = i % (D / 8);
-            const int abs_row = u.r0 + first + r;
-            const int token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
-            const __nv_bfloat16* src = a.q + head * a.q_sh + (u.start + token) * a.q_sn + piece * 8;
-            cp_async16(base + h * P::QHALF + (piece >> 3) * P::QBOX + r * 128 + (((piece & 7) ^ (r & 7)) << 4), src);
-          }
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + h));
-          ++uses[h];
-        }
+        ok = gather(u, 0);
+        if (!ok) break;
         if (u.rows <= 128) half ^= 1;
         w += u.n_tiles;
         rem += u.n_tiles;
@@ -320,12 +420,44 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       units[e].n_tiles = 0;
       mbar_arrive(bar(P::BAR_UNIT + e));
     }
+  } else if (warp == kLoader) {
+    // ------------------------------------------------------------ the other half of the queries
+    bool ok = true;
+    for (int seq = 0; ok; ++seq) {
+      const int e = seq % kUnitRing;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 45));
+      if (!ok) break;
+      const Unit u = units[e];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+      if (u.n_tiles == 0) break;
+      ok = gather(u, 1);
+    }
   } else if (warp == kProducer) {
     // ------------------------------------------------------------ K and V tiles
     bool ok = true;
     uint32_t s = 0, lap = 0;                         // next slot of the ring, times round
     const int page = 1 << a.page_log2;
     const int per_tile = max(kTile >> a.page_log2, 1), rows = min(page, kTile);
+    struct Tile {                                    // this lane's page of a tile
+      int id, off, g;
+      bool live;
+    } last{0, 0, 0, false};
+    bool any = false;                                // a V tile is outstanding: that of `last`
+    auto load = [&](const Tile& tile, const CUtensorMap& map) {
+      if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (lap - 1) & 1, ab, 51));
+      if (!ok) return;
+      const int n_live = __popc(__ballot_sync(0xffffffffu, tile.live));
+      if (lane == 0) mbar_expect_tx(bar(P::BAR_FULL + s), n_live * rows * D * 2);
+      __syncwarp();
+      if (tile.live) {
+        const uint32_t dst = base + P::RING_OFF + s * P::SLOT + lane * rows * 128;
+#pragma unroll
+        for (int x = 0; x < P::NBOX; ++x) tma_load_4d(dst + x * P::KBOX, &map, bar(P::BAR_FULL + s), x * 64, tile.off, tile.g, tile.id);
+      }
+      __syncwarp();
+      if (++s == P::SLOTS) { s = 0; ++lap; }
+    };
     for (int seq = 0; ok; ++seq) {
       const int e = seq % kUnitRing;
       ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
@@ -345,28 +477,19 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         const int kt = u.kt0 + t, key = kt * kTile + lane * page;
         const int next = t + 1 < u.n_tiles ? lookup(kt + 1) : -1;
         const bool live = lane < per_tile && key < u.len;
-        const int n_live = __popc(__ballot_sync(0xffffffffu, live));
         if (live && (id < 0 || id >= a.n_pages)) {
           report_range(a.status, kWhereTreePage);
           id = a.n_pages;                            // outside the tensor map: the load fills in zeros
         }
-        for (int kv = 0; kv < 2; ++kv) {
-          if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (lap - 1) & 1, ab, 51));
-          if (!ok) break;
-          if (lane == 0) mbar_expect_tx(bar(P::BAR_FULL + s), n_live * rows * D * 2);
-          __syncwarp();
-          if (live) {
-            const uint32_t dst = base + P::RING_OFF + s * P::SLOT + lane * rows * 128;
-#pragma unroll
-            for (int x = 0; x < P::NBOX; ++x)
-              tma_load_4d(dst + x * P::KBOX, kv ? &tm_v : &tm_k, bar(P::BAR_FULL + s), x * 64, key & (page - 1), u.g, id);
-          }
-          __syncwarp();
-          if (++s == P::SLOTS) { s = 0; ++lap; }
-        }
+        const Tile now{id, key & (page - 1), u.g, live};
+        load(now, tm_k);
+        if (any) load(last, tm_v);
+        last = now;
+        any = true;
         id = next;
       }
     }
+    if (ok && any) load(last, tm_v);
     if (*abort_flag && lane == 0) {
       // let the copies already in flight land before the CTA gives its shared memory back
       const long long t0 = clock64();
@@ -391,14 +514,23 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       bool open = false, done = false;
       uint32_t first = 0, frees = 0;                 // bit x: the job of stream x opens its sum / is the last reader of its tile
       uint32_t fresh = 0, q_ready = 0, q_phase = 0, p_phase = 0;
-      uint32_t k_slot = 0, k_phase = 0, v_slot = 1, v_phase = 0;       // ring positions of the next K and V tile
+      // ring positions of the next K and V tile: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1)
+      const uint32_t n_tiles = (uint32_t)(w1 - w0);
+      uint32_t k_slot = 0, k_phase = 0, k_tile = 0, v_slot = n_tiles > 1 ? 2 : 1, v_phase = 0, v_tile = 0;
       uint32_t n_qk = 0, n_pv = 0, polls = 0;
+      bool k_here = false, v_here = false;           // looked up ahead: a poll on the way from P to the products costs 200 cycles
       long long idle_since = 0;
       while (!(done && n_pv == n_qk)) {
+        // all polls of a round first: each is a round trip to shared memory, 200 cycles while the tensor core streams from
+        // it, and they overlap only if no product stands between them
         bool moved = false;
-        if (n_pv != n_qk) {
-          const uint32_t x = n_pv & 1, bit = 1u << x;
-          if (mbar_test(bar(P::BAR_P + x), (p_phase >> x) & 1) && mbar_test(bar(P::BAR_FULL + v_slot), v_phase)) {
+        const uint32_t px = n_pv & 1;
+        if (n_pv != n_qk && !v_here) v_here = mbar_test(bar(P::BAR_FULL + v_slot), v_phase);
+        const bool p_here = n_pv != n_qk && mbar_test(bar(P::BAR_P + px), (p_phase >> px) & 1);
+        if (open && !k_here) k_here = mbar_test(bar(P::BAR_FULL + k_slot), k_phase);
+        {
+          const uint32_t x = px, bit = 1u << x;
+          if (v_here && p_here) {
             tc_fence_after();
             const uint64_t dv = d_v + v_slot * (P::SLOT >> 4);
             const uint32_t acc = (first & bit) ? 0u : 1u;
@@ -408,7 +540,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
             mma_commit(bar(P::BAR_PV + x));
             if (frees & bit) {
               mma_commit(bar(P::BAR_FREE + v_slot));
-              v_slot += 2;
+              v_here = false;
+              v_slot += ++v_tile + 1 == n_tiles ? 1 : 2;
               if (v_slot >= P::SLOTS) { v_slot -= P::SLOTS; v_phase ^= 1; }
             }
             p_phase ^= bit;
@@ -430,12 +563,12 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
             moved = true;
           }
         }
-        if (open && n_qk - n_pv < 2) {
+        if (open) {
           const uint32_t x = n_qk & 1, bit = 1u << x;
           const bool both = u.rows > 128;
           const uint32_t h = both ? x : (uint32_t)u.half;
           if (!((q_ready >> h) & 1) && mbar_test(bar(P::BAR_QFULL + h), (q_phase >> h) & 1)) { q_ready |= 1u << h; q_phase ^= 1u << h; }
-          if (((q_ready >> h) & 1) && mbar_test(bar(P::BAR_FULL + k_slot), k_phase)) {
+          if (n_qk - n_pv < 2 && ((q_ready >> h) & 1) && k_here) {
             tc_fence_after();
             const uint64_t dq = d_q + h * (P::QHALF >> 4), dk = d_k + k_slot * (P::SLOT >> 4);
 #pragma unroll
@@ -450,7 +583,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
             if (tile + 1 == (uint32_t)u.n_tiles) mma_commit(bar(P::BAR_QFREE + h));        // the unit's last use of this half
             if (last_sub) {
               mma_commit(bar(P::BAR_FREE + k_slot));
-              k_slot += 2;
+              k_here = false;
+              k_slot += k_tile++ == 0 ? 1 : 2;
               if (k_slot >= P::SLOTS) { k_slot -= P::SLOTS; k_phase ^= 1; }
               sub = 0;
               ++tile;
@@ -494,13 +628,12 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       const int e = seq % kUnitRing;
       ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
       if (!ok) break;
-      const Unit u = units[e];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+      const Unit& u = units[e];                       // stays in shared memory until the unit is done: registers are short
       if (u.n_tiles == 0) break;
       const bool both = u.rows > 128;                 // the streams are halves of the rows; else they take turns at the tiles
       const int my_row = both ? x * 128 + row : row;  // row of the unit
       const bool warp_live = (both ? x * 128 : 0) + (warp & 3) * 32 < u.rows;
+      const bool live = my_row < u.rows;
       const int abs_row = u.r0 + my_row;
       const int token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
       const int t_first = both ? 0 : (int)((jobs_before + x) & 1), t_step = both ? 1 : 2;
@@ -513,118 +646,100 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         tc_fence_after();
         if (special) {
           // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite)
-          const uint32_t v_step = 2 * (tiles_before + t) + 1, s = v_step % P::SLOTS;
+          const uint32_t tile = tiles_before + t, v_step = 2 * tile + (tile + 1 == (uint32_t)(w1 - w0) ? 1 : 2), s = v_step % P::SLOTS;
           ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (v_step / P::SLOTS) & 1, ab, 32));
           if (!ok) break;
-          const int key = k0 + row;
-          if (key >= min(u.past, u.len)) {
-            bool wrote = false;
-#pragma unroll
-            for (int b = 0; b < P::NBOX; ++b) {
-              uint4* v = reinterpret_cast<uint4*>(smem + P::RING_OFF + s * P::SLOT + b * P::KBOX + row * 128);
-              for (int i = 0; i < 8; ++i) {
-                if (key >= u.len) {
-                  v[i] = make_uint4(0, 0, 0, 0);
-                  wrote = true;
-                } else {
-                  uint4 y = v[i];
-                  if (nonfinite2(y.x) || nonfinite2(y.y) || nonfinite2(y.z) || nonfinite2(y.w)) {
-                    *bad_tag = seq + 1;
-                    __threadfence_block();            // whoever finds the zeros finds the tag too
-                    uint32_t w[4] = {y.x, y.y, y.z, y.w};
-                    for (int c = 0; c < 4; ++c) {
-                      if ((w[c] & 0x7f80u) == 0x7f80u) w[c] &= 0xffff0000u;
-                      if ((w[c] & 0x7f800000u) == 0x7f800000u) w[c] &= 0xffffu;
-                    }
-                    v[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                    wrote = true;
-                  }
-                }
-              }
-            }
-            if (wrote) fence_async_smem();
+          // each warp of the stream 32 keys
+          const int r_lo = (warp & 3) * 32, behind = u.len - k0;
+          const int lo = max(min(u.past, u.len) - k0, r_lo);
+          if (lo < r_lo + 32) {
+            uint32_t* v = reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane;
+            // the tag before the zeros: with more than 128 rows both streams clean the same tile, and who finds zeros finds the tag
+            clean_values<D>(v, lo, r_lo + 32, behind, bad_tag, seq + 1);
           }
+          fence_async_smem();
           __syncwarp();
         }
         if (warp_live) {
-          // The 128 logits are read from TMEM twice, for the maximum and for the exponentials: held in registers they
-          // would spill.  P (bf16 pairs) takes the first half of the columns; each chunk of it lands on logits already used.
-          float mx = -CUDART_INF_F;
-          uint32_t seen[4] = {~0u, ~0u, ~0u, ~0u};
-          if (special) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) seen[c] = my_row < u.rows ? seen32(a, u, token, k0 + c * 32) : 0u;
-          }
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t s[32];
-            tmem_ld32(t_s + c * 32, s);
-            if (special) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (seen[c] >> i) & 1 ? __uint_as_float(s[i]) : -CUDART_INF_F);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(s[i]));
-            }
-          }
-          mx *= scale;
-          const float m_new = mx > m_ref + 8.f ? mx : m_ref;
-          const float alpha = ex2_approx(m_ref - m_new);
+          // Four chunks of 32 logits, the next one's load in flight, each a step of the running softmax.  The reference
+          // moves, to a whole number, when the row maximum has grown by more than 2^8.
+          if (special) mask_tmem(a, u, live ? token : -1, k0, t_s);
+          uint32_t s[2][32];
           float sum = 0.f;
+          tmem_ld32_async(t_s, s[0]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            uint32_t s[32], p[16];
-            tmem_ld32(t_s + c * 32, s);
-            if (special) {
+            tmem_ld_wait();
+            reg_fence32(s[c & 1]);
+            const uint32_t* y = s[c & 1];
+            auto val = [&](int e) { return __uint_as_float(y[e]); };
+            float m0 = max3(val(0), val(1), val(2)), m1 = max3(val(3), val(4), val(5)), m2 = max3(val(6), val(7), val(8)),
+                  m3 = max3(val(9), val(10), val(11));
 #pragma unroll
-              for (int i = 0; i < 32; ++i) s[i] = (seen[c] >> i) & 1 ? s[i] : 0xff800000u;      // -infinity
+            for (int e = 12; e < 28; e += 8) {
+              m0 = max3(m0, val(e), val(e + 1));
+              m1 = max3(m1, val(e + 2), val(e + 3));
+              m2 = max3(m2, val(e + 4), val(e + 5));
+              m3 = max3(m3, val(e + 6), val(e + 7));
             }
+            m0 = max3(m0, val(28), val(29));
+            m1 = max3(m1, val(30), val(31));
+            const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
+            const bool grown = live && mx > m_ref + 8.f;       // lanes without a row hold anything
+            if (__any_sync(0xffffffffu, grown)) {
+              const float m_new = grown ? ceilf(mx) : m_ref;
+              const float alpha = ex2_approx(m_ref - m_new);
+              // the stream's previous product came before this S, and nothing of this P has been handed over
+              rescale_tmem<D>(t_o, t_s, alpha, c, t != t_first);
+              l *= alpha;
+              sum *= alpha;
+              m_ref = m_new;
+            }
+            // not before the call above: its registers must not be moved while the load is under way
+            if (c < 3) tmem_ld32_async(t_s + (c + 1) * 32, s[(c + 1) & 1]);
+            const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-m_ref, -m_ref);
+            float2 sum01 = make_float2(0.f, 0.f), sum23 = make_float2(0.f, 0.f);
+            uint32_t p[16];
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const float p0 = ex2_approx(fmaf(__uint_as_float(s[i]), scale, -m_new));
-              const float p1 = ex2_approx(fmaf(__uint_as_float(s[i + 1]), scale, -m_new));
-              sum += p0 + p1;
-              p[i / 2] = pack_bf16(p0, p1);
+            for (int e = 0; e < 32; e += 4) {
+              float2 x01 = __ffma2_rn(make_float2(val(e), val(e + 1)), sc2, nm2);
+              float2 x23 = __ffma2_rn(make_float2(val(e + 2), val(e + 3)), sc2, nm2);
+              x01.x = ex2_approx(x01.x);
+              x01.y = ex2_approx(x01.y);
+              x23.x = ex2_approx(x23.x);
+              x23.y = ex2_approx(x23.y);
+              sum01 = __fadd2_rn(sum01, x01);
+              sum23 = __fadd2_rn(sum23, x23);
+              p[e / 2] = cvt_bf16x2(x01.x, x01.y);
+              p[e / 2 + 1] = cvt_bf16x2(x23.x, x23.y);
             }
+            sum += (sum01.x + sum01.y) + (sum23.x + sum23.y);
             tmem_st16(t_s + c * 16, p);
           }
-          l = l * alpha + sum;
-          if (t != t_first && __any_sync(0xffffffffu, m_new != m_ref)) {
-            // O so far is relative to the old reference (the stream's previous product came before this S)
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t o[32];
-              tmem_ld32(t_o + c * 32, o);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-              tmem_st32(t_o + c * 32, o);
-            }
-          }
-          m_ref = m_new;
+          l += sum;
           tmem_wait_st();
         }
         tc_fence_before();
-        mbar_arrive(bar(P::BAR_P + x));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(P::BAR_P + x));
         ++n_jobs;
       }
       const int mine_jobs = t_first < u.n_tiles ? (u.n_tiles - t_first + t_step - 1) / t_step : 0;
       if (ok && mine_jobs > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + x), (n_jobs - 1) & 1, ab, 33));
       // join the streams' weights
-      float m_all = m_ref, l_all = l, f0 = 1.f, f1 = 1.f;           // factors of O of stream 0 and 1
-      bool use0 = l != 0.f, use1 = use0;
+      float m_all = m_ref, l_all = l, f0 = 1.f, f1 = 0.f;           // factors of this group's two O's
       if (!both && ok) {
         tc_fence_before();
         ex[x * 128 + row] = make_float2(m_ref, l);
-        mbar_arrive(bar(P::BAR_EX));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(P::BAR_EX));
         ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_EX), n_joins & 1, ab, 34));
         if (ok) {
           const float2 e0 = ex[row], e1 = ex[128 + row];
-          use0 = e0.y != 0.f;                         // a NaN counts as in use
-          use1 = e1.y != 0.f;
-          m_all = fmaxf(use0 ? e0.x : kNoMax, use1 ? e1.x : kNoMax);
-          f0 = use0 ? ex2_approx(e0.x - m_all) : 0.f;
-          f1 = use1 ? ex2_approx(e1.x - m_all) : 0.f;
-          l_all = (use0 ? e0.y * f0 : 0.f) + (use1 ? e1.y * f1 : 0.f);
+          m_all = fmaxf(e0.x, e1.x);
+          f0 = ex2_approx(e0.x - m_all);
+          f1 = ex2_approx(e1.x - m_all);
+          l_all = e0.y * f0 + e1.y * f1;
         }
       }
       if (ok) {
@@ -635,40 +750,40 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         const bool repair = *bad_tag == seq + 1;
         const size_t slot = ((size_t)cta * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + my_row;
         if (warp_live) {
-          const bool live = my_row < u.rows;
+          __nv_bfloat16* out = a.o + head * a.o_sh + (u.start + token) * a.o_sn;
+          float* part = work.part + slot * D;
+          if (whole) { f0 *= inv; f1 *= inv; }
+          // an O that no tile has gone into holds anything: with a single tile the other stream's
+          const bool one = both || u.n_tiles == 1;
+          const uint32_t at = tmem + lanes + P::O_COL, at0 = at + ((both ? x : one ? (int)(jobs_before & 1) : 0) * P::O_STEP);
+          if (one && !both && (jobs_before & 1)) f0 = f1;
+#pragma unroll 1
           for (int c = c_lo; c < c_lo + c_n; ++c) {
-            float o[32];
             uint32_t y[32];
-            if (both) {
-              tmem_ld32(t_o + c * 32, y);
+            float o[32];
+            tmem_ld32(at0 + c * 32, y);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = use0 ? __uint_as_float(y[i]) : 0.f;
-            } else {
-              const uint32_t at = tmem + lanes + P::O_COL + c * 32;
-              tmem_ld32(at, y);
+            for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(y[i]) * f0;
+            if (!one) {
+              tmem_ld32(at + P::O_STEP + c * 32, y);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = use0 ? __uint_as_float(y[i]) * f0 : 0.f;
-              tmem_ld32(at + P::O_STEP, y);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] += use1 ? __uint_as_float(y[i]) * f1 : 0.f;
+              for (int i = 0; i < 32; ++i) o[i] = fmaf(__uint_as_float(y[i]), f1, o[i]);
             }
-            if (!live) continue;
-            if (whole) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] *= inv;
-            }
-            if (repair) add_nonfinite(a, u, token, c * 32, o);
-            if (whole) {
-              uint4* dst = reinterpret_cast<uint4*>(a.o + head * a.o_sh + (u.start + token) * a.o_sn + c * 32);
+            if (live && whole) {
+              uint4* dst = reinterpret_cast<uint4*>(out + c * 32);
 #pragma unroll
               for (int i = 0; i < 4; ++i)
                 dst[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]),
                                     pack_bf16(o[8 * i + 6], o[8 * i + 7]));
-            } else {
-              float4* dst = reinterpret_cast<float4*>(work.part + slot * D + c * 32);
+            } else if (live) {
+              float4* dst = reinterpret_cast<float4*>(part + c * 32);
 #pragma unroll
               for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             }
+          }
+          if (live && repair) {
+            if (whole) add_nonfinite(a, u, token, out, c_lo * 32, (c_lo + c_n) * 32);
+            else add_nonfinite(a, u, token, part, c_lo * 32, (c_lo + c_n) * 32);
           }
           if (live && (both || x == 0)) {
             if (!whole) work.ml[slot] = make_float2(m_all, l_all);
@@ -679,7 +794,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         if (!both) {
           // neither stream's next product may overwrite an O that the other group is still reading
           tc_fence_before();
-          mbar_arrive(bar(P::BAR_EXDONE));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(P::BAR_EXDONE));
           ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_EXDONE), n_joins & 1, ab, 35));
           tc_fence_after();
           ++n_joins;
@@ -687,6 +803,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       }
       jobs_before += both ? 2 * u.n_tiles : u.n_tiles;
       tiles_before += u.n_tiles;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
     }
   }
 

@@ -132,6 +132,27 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
       : "memory");
 }
+// Products with operand descriptors given by their low words (address and leading offset); the high word is the same for
+// all tiles here (1024 bytes between 8-row groups, 128-byte swizzle).
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void mma_ss_lo(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accum), "n"(kDescHigh)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts_lo(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accum), "n"(kDescHigh)
+      : "memory");
+}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -308,6 +329,9 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
     if (misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
   }
   if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
+  // rows of the Q area that no unit fills stay zero: products of whatever lay there would cost power, and with it clock
+  for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+  fence_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -502,8 +526,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
     // ------------------------------------------------------------ products
     if (lane == 0) {
       constexpr uint32_t idesc_qk = instr_desc(128, kTile, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
-      const uint64_t d_q = smem_desc(base, 16, 1024), d_k = smem_desc(base + P::RING_OFF, 16, 1024),
-                     d_v = smem_desc(base + P::RING_OFF, P::KBOX, 1024);
+      const uint32_t d_q = (uint32_t)smem_desc(base, 16, 1024), d_k = (uint32_t)smem_desc(base + P::RING_OFF, 16, 1024),
+                     d_v = (uint32_t)smem_desc(base + P::RING_OFF, P::KBOX, 1024);
       // Jobs alternate between the streams: job i belongs to stream i & 1.  S of a job may be computed once the stream's
       // previous P has been handed to its product, so at most two jobs are between their two products.  One thread does
       // all of this, and every instruction of the loop delays both streams: 32-bit counters, ring positions that advance
@@ -526,17 +550,19 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         bool moved = false;
         const uint32_t px = n_pv & 1;
         if (n_pv != n_qk && !v_here) v_here = mbar_test(bar(P::BAR_FULL + v_slot), v_phase);
-        const bool p_here = n_pv != n_qk && mbar_test(bar(P::BAR_P + px), (p_phase >> px) & 1);
         if (open && !k_here) k_here = mbar_test(bar(P::BAR_FULL + k_slot), k_phase);
+        // with both streams between their products nothing else can be done: the wait that the hardware wakes
+        const uint32_t p_bar = bar(P::BAR_P + px), p_parity = (p_phase >> px) & 1;
+        const bool p_here = n_pv != n_qk && (v_here && n_qk - n_pv == 2 ? mbar_try_wait(p_bar, p_parity) : mbar_test(p_bar, p_parity));
         {
           const uint32_t x = px, bit = 1u << x;
           if (v_here && p_here) {
             tc_fence_after();
-            const uint64_t dv = d_v + v_slot * (P::SLOT >> 4);
+            const uint32_t dv = d_v + v_slot * (P::SLOT >> 4);
             const uint32_t acc = (first & bit) ? 0u : 1u;
 #pragma unroll
             for (int kk = 0; kk < kTile / 16; ++kk)
-              mma_ts(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, dv + kk * (16 * 128 >> 4), idesc_pv, kk > 0 ? 1u : acc);
+              mma_ts_lo(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, dv + kk * (16 * 128 >> 4), idesc_pv, kk > 0 ? 1u : acc);
             mma_commit(bar(P::BAR_PV + x));
             if (frees & bit) {
               mma_commit(bar(P::BAR_FREE + v_slot));
@@ -570,10 +596,10 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
           if (!((q_ready >> h) & 1) && mbar_test(bar(P::BAR_QFULL + h), (q_phase >> h) & 1)) { q_ready |= 1u << h; q_phase ^= 1u << h; }
           if (n_qk - n_pv < 2 && ((q_ready >> h) & 1) && k_here) {
             tc_fence_after();
-            const uint64_t dq = d_q + h * (P::QHALF >> 4), dk = d_k + k_slot * (P::SLOT >> 4);
+            const uint32_t dq = d_q + h * (P::QHALF >> 4), dk = d_k + k_slot * (P::SLOT >> 4);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
-              mma_ss(tmem + P::S_COL + x * 128, dq + (kk >> 2) * (P::QBOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::KBOX >> 4) + (kk & 3) * 2, idesc_qk,
+              mma_ss_lo(tmem + P::S_COL + x * 128, dq + (kk >> 2) * (P::QBOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::KBOX >> 4) + (kk & 3) * 2, idesc_qk,
                      kk > 0);
             mma_commit(bar(P::BAR_S + x));
             const bool last_sub = !both || sub == 1;
@@ -637,7 +663,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       const int abs_row = u.r0 + my_row;
       const int token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
       const int t_first = both ? 0 : (int)((jobs_before + x) & 1), t_step = both ? 1 : 2;
-      float m_ref = kNoMax, l = 0.f;
+      float m_ref = live ? kNoMax : -kNoMax, l = 0.f;       // lanes without a row: all weights zero
       for (int t = t_first; t < u.n_tiles && ok; t += t_step) {
         const int k0 = (u.kt0 + t) * kTile;
         const bool special = k0 + kTile > min(u.past, u.len);
@@ -816,53 +842,102 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   }
 }
 
-// Joins the parts of a cut unit, in the order of the keys: the part of the CTA in which the unit begins, then those of
-// the CTAs after it.  Block (c, y): the unit that begins in CTA c and goes on, rows 8 y, 8 y + 8 gridDim.y, ...  With
-// fewer than eight rows the warps share a row's parts.
-constexpr int kJoinWarps = 8;
+// Joins the parts of the cut units, in the order of the keys: the part of the CTA in which a unit begins, then those of
+// the CTAs after it.  A warp reads a row's part at once (its 32 lanes the columns).  The work is a few MB from L2 at most
+// and all latency, so it is spread as widely as it goes: every block lists the cut units (one per CTA of the first kernel
+// at most) and takes every gridDim.x-th run of rows; as long as the device has warps to spare, 2, 4 or 8 of them share
+// the parts of a row.
+constexpr int kJoinWarps = 8, kJoinBlocksPerSm = 4;
 
 template <int D>
-__global__ void __launch_bounds__(kJoinWarps * 32) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a, const Work work) {
+__global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, int n_cta) {
   constexpr int E = D / 32;
   __shared__ float s_m[kJoinWarps], s_l[kJoinWarps], s_o[kJoinWarps][D];
+  __shared__ int s_sum[kJoinWarps], s_owner, s_first;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (decode_poisoned(a.status)) return;
-  const Meta m = work.meta[blockIdx.x];
-  if (m.last_cta < 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int parts = m.last_cta - (int)blockIdx.x + 1;
-  for (int r0 = blockIdx.y * kJoinWarps; r0 < m.rows; r0 += gridDim.y * kJoinWarps) {
-    const int n_here = min(kJoinWarps, m.rows - r0);
-    const int share = n_here > 4 ? 1 : n_here > 2 ? 2 : n_here > 1 ? 4 : 8;   // warps of a row
-    const int r = r0 + warp / share, turn = warp % share;
+  // rows of the unit that begins in CTA i and goes on in later ones; thread t looks after CTAs per * t ...
+  const int per = (n_cta + kJoinWarps * 32 - 1) / (kJoinWarps * 32);
+  auto rows_of = [&](int i) { return i < n_cta && work.meta[i].last_cta >= 0 ? work.meta[i].rows : 0; };
+  auto block_scan = [&](int mine, int* total) {      // sum over the threads before this one
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    __syncthreads();
+    if (lane == 31) s_sum[warp] = incl;
+    __syncthreads();
+    int before = incl - mine;
+    *total = 0;
+    for (int w = 0; w < kJoinWarps; ++w) {
+      if (w < warp) before += s_sum[w];
+      *total += s_sum[w];
+    }
+    return before;
+  };
+  int mine = 0, rows = 0;
+  for (int i = threadIdx.x * per; i < (threadIdx.x + 1) * per; ++i) mine += rows_of(i);
+  block_scan(mine, &rows);
+  if (rows == 0) return;
+  const int spare = (int)gridDim.x * kJoinWarps / rows;
+  const int share = spare >= 8 ? 8 : spare >= 4 ? 4 : spare >= 2 ? 2 : 1, here = kJoinWarps / share;   // warps of a row, rows of a block
+  mine = 0;
+  for (int i = threadIdx.x * per; i < (threadIdx.x + 1) * per; ++i) mine += (rows_of(i) + here - 1) / here;
+  int runs;
+  const int before = block_scan(mine, &runs);
+  for (int run = blockIdx.x; run < runs; run += gridDim.x) {
+    __syncthreads();
+    if (before <= run && run < before + mine) {
+      int at = before;
+      for (int i = threadIdx.x * per;; ++i) {
+        const int n = (rows_of(i) + here - 1) / here;
+        if (run < at + n) { s_owner = i; s_first = (run - at) * here; break; }
+        at += n;
+      }
+    }
+    __syncthreads();
+    const int owner = s_owner, r = s_first + warp / share, turn = warp % share;
+    const Meta m = work.meta[owner];
+    const int parts = m.last_cta - owner + 1;
     float mx = kNoMax, l = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     if (r < m.rows) {
-#pragma unroll 4
-      for (int p = turn; p < parts; p += share) {
-        const size_t slot = ((size_t)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * kUnitRows + r;
-        const float2 ml = work.ml[slot];
-        float y[E];
-        if (E == 4) {
-          const float4 v = *reinterpret_cast<const float4*>(work.part + slot * D + lane * 4);
-          y[0] = v.x; y[1] = v.y; y[2 % E] = v.z; y[3 % E] = v.w;
-        } else {
-          const float2 v = *reinterpret_cast<const float2*>(work.part + slot * D + lane * 2);
-          y[0] = v.x; y[1] = v.y;
-        }
-        if (ml.y == 0.f) continue;
-        const float top = fmaxf(mx, ml.x), f_old = exp2f(mx - top), f = exp2f(ml.x - top);
-        l = l * f_old + ml.y * f;
+      constexpr int RUN = 4;                         // parts in flight
+      for (int p0 = turn; p0 < parts; p0 += RUN * share) {
+        float2 ml[RUN];
+        float y[RUN][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f_old + y[e] * f;
-        mx = top;
+        for (int i = 0; i < RUN; ++i) {
+          const int p = p0 + i * share;
+          ml[i] = make_float2(kNoMax, 0.f);
+          if (p < parts) {
+            const size_t slot = ((size_t)(owner + p) * 2 + (p == 0 ? 1 : 0)) * kUnitRows + r;
+            ml[i] = work.ml[slot];
+            if (E == 4) *reinterpret_cast<float4*>(y[i]) = *reinterpret_cast<const float4*>(work.part + slot * D + lane * 4);
+            else *reinterpret_cast<float2*>(y[i]) = *reinterpret_cast<const float2*>(work.part + slot * D + lane * 2);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+          if (ml[i].y == 0.f) continue;              // no part, or nothing visible in it
+          const float top = fmaxf(mx, ml[i].x), f_old = exp2f(mx - top), f = exp2f(ml[i].x - top);
+          l = l * f_old + ml[i].y * f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] = o[e] * f_old + y[i][e] * f;
+          mx = top;
+        }
       }
     }
-    if (lane == 0) { s_m[warp] = mx; s_l[warp] = l; }
+    if (share > 1) {
+      if (lane == 0) { s_m[warp] = mx; s_l[warp] = l; }
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
-    __syncthreads();
+      for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
+      __syncthreads();
+    }
     if (turn == 0 && r < m.rows) {
       for (int w = warp + 1; w < warp + share; ++w) {
         if (s_l[w] == 0.f) continue;
@@ -883,7 +958,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_attn_join_kernel(const _
       if (a.lse && lane == 0)
         a.lse[(size_t)head * a.rows + m.start + token] = l != 0.f ? (mx + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
     }
-    __syncthreads();
   }
 }
 
@@ -920,10 +994,8 @@ cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
   tree_attn_kernel<D><<<n_cta, kThreads, smem, s>>>(a, w, tk, tv);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   // started early, it waits for the first kernel's end on the device
-  const long long most = (long long)a.rows * a.group;
-  const int y = (int)((most < kUnitRows ? most : kUnitRows) + kJoinWarps - 1) / kJoinWarps;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_cta, y < 8 ? y : 8);
+  cfg.gridDim = dim3(n_cta * kJoinBlocksPerSm);
   cfg.blockDim = dim3(kJoinWarps * 32);
   cfg.stream = s;
   cudaLaunchAttribute attr;
@@ -931,7 +1003,7 @@ cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, tree_attn_join_kernel<D>, a, w);
+  return cudaLaunchKernelEx(&cfg, tree_attn_join_kernel<D>, a, w, n_cta);
 }
 
 }  // namespace

@@ -4,29 +4,29 @@
 //   out_r = sum_c p_rc v_c / sum_c p_rc,  p_rc = 2^(scale q_r.k_c - m_r) over the visible keys c.
 //
 // The rows of a unit are the new tokens of one request times the query heads that share a KV head (row = token * group +
-// head), at most 256 of them, so that every key and value is read once for all of them.  Work is counted in key tiles of
-// 128: the tiles of all units (request, KV head, 256 rows) stand in one line, which is cut into one equal run per SM
-// wherever that falls; a unit that is cut leaves partial results (unnormalised sums, reference maxima, weights) that a
-// second kernel joins in the order of the keys.  All lengths are read on the device: a prefix sum over the requests
-// tells each CTA where its run begins.
+// head), so that every key and value is read once for all of them.  Work is counted in key tiles of 128: the tiles of all
+// units (request, KV head, rows) stand in one line, which is cut into one equal run per worker wherever that falls; a unit
+// that is cut leaves partial results (unnormalised sums, reference maxima, weights) that a second kernel joins in the
+// order of the keys.  All lengths are read on the device: a prefix sum over the requests tells each worker where its run
+// begins.
 //
 // What bounds it: the cache's bytes.  A tile is 64 KB (head_dim 128), 2700 cycles of an SM's share of the measured HBM
 // rate; its matrix products take 1020 cycles for up to 128 rows (the tensor core takes 128 rows at a time, however few
 // are in use), 2040 for 256.  With 256 rows its 32768 exponentials (2048 cycles of the SM's special-function units) come
 // close to the bytes.
 //
-// Two streams of (key tile, 128 rows) jobs share the tensor core, each with its own S and O columns in TMEM and its own
-// four softmax warps, so that one stream's exponentials overlap the other's products.  With more than 128 rows the
-// streams are the two halves of the rows and walk the same tiles; with fewer they take the tiles in turn and their sums
-// are joined at the end of the unit (both groups of warps read both O's from TMEM, half the columns each).
+// Two streams per CTA, each with its own Q, its own S and O columns in TMEM, its own four softmax warps and its own
+// loader, share the tensor core and the ring of K and V tiles, so that one stream's softmax, waits and epilogues overlap
+// the other's products.  If no request has more than 128 rows the streams are workers of their own, with a run of tiles
+// each (a unit's beginning and end then cost one stream a wait, not the SM).  Otherwise ("wide") a CTA is a worker, units
+// have up to 256 rows, and the streams are the two halves of them and walk the same tiles.
 //
 //   warps 0-3, 4-7  softmax and epilogue of stream 0 / 1: thread = TMEM lane = row
 //   warp 8          producer: page ids from the table, TMA loads of K and V pages into a ring of tile slots, in the order
 //                   in which the products need them: K0 K1 V0 K2 V1 ... (a V tile that arrived with its K would hold a
-//                   slot for the whole softmax)
+//                   slot for the whole softmax); with separate runs the streams' tiles in turn
 //   warp 9          issuer (one thread): S = Q K^T and O += P V of whichever stream is ready
-//   warp 10         scheduler: walks the run, publishes units
-//   warps 10, 11    gather the units' Q rows into shared memory (cp.async), every other pair of rows each
+//   warps 10, 11    loader of stream 0 / 1: walks the run, publishes units, gathers their Q rows into shared memory
 //
 // Masks.  Only tiles that hold a key at or behind the first new token need one.  There the row's visibility bits are
 // shifted into place 32 keys at a time.  A masked probability is zero, but zero times a NaN in V is not: in those tiles
@@ -52,7 +52,7 @@ using namespace tc;
 constexpr int kTile = 128;                       // keys of a tile
 constexpr int kUnitRows = 256;
 constexpr int kThreads = 384;
-constexpr int kSoftmaxWarps = 8, kProducer = 8, kIssuer = 9, kScheduler = 10, kLoader = 11;
+constexpr int kProducer = 8, kIssuer = 9, kLoader = 10;
 constexpr int kUnitRing = 4;
 constexpr float kNoMax = -1e30f;                 // reference maximum before any visible key: finite, below any logit
 
@@ -65,42 +65,41 @@ struct Plan {
   static constexpr int RING_OFF = 2 * QHALF;
   static constexpr int MISC_OFF = RING_OFF + SLOTS * SLOT;
   static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + SLOTS, BAR_S = BAR_FREE + SLOTS, BAR_P = BAR_S + 2, BAR_PV = BAR_P + 2,
-                       BAR_QFULL = BAR_PV + 2, BAR_QFREE = BAR_QFULL + 2, BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + kUnitRing,
-                       BAR_EX = BAR_UFREE + kUnitRing, BAR_EXDONE = BAR_EX + 1, BARS = BAR_EXDONE + 1;
-  static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;
-  static constexpr int EX_OFF = (UNIT_OFF + kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // float2 [2][128]
-  static constexpr int SCAN_OFF = EX_OFF + 2048;                                       // int64 [12], then small words
-  static constexpr int TOTAL = SCAN_OFF + 12 * 8 + 64;
+                       BAR_QFULL = BAR_PV + 2, BAR_QFREE = BAR_QFULL + 2, BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + 2 * kUnitRing,
+                       BARS = BAR_UFREE + 2 * kUnitRing;
+  static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;               // [stream][kUnitRing]
+  static constexpr int SCAN_OFF = (UNIT_OFF + 2 * kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // int64 [12], then small words
+  static constexpr int TOTAL = SCAN_OFF + 12 * 8 + 112;
   static constexpr int S_COL = 0, O_COL = 256, O_STEP = D;  // S: 128 columns a stream; O: D columns a stream
 };
 
-struct Unit {
-  int n_tiles;      // key tiles of this CTA's part; 0: no more units
+struct Unit {       // of one stream
+  int n_tiles;      // key tiles of this worker's part; 0: no more units
   int kt0;          // first of them
   int kt_all;       // key tiles of the whole unit
   int start;        // first row of the request
-  int r0, rows;     // first of the unit's rows (token * group + head) inside the request, and their number
+  int r0, rows;     // first of the stream's rows (token * group + head) inside the request, and their number
   int g, b;
   int len, past;
-  int half;         // Q half in use (more than 128 rows: both)
-  int last_cta;     // CTA that has the unit's last tile
+  int pad[2];
 };
 static_assert(sizeof(Unit) == 48, "");
 
-struct Meta {       // what the join kernel needs of a unit that begins in this CTA and goes on in later ones
-  int last_cta;     // < 0: there is none
-  int start, r0, rows, g, pad[3];
+struct Meta {       // what the join kernel needs of a unit that begins in this worker and goes on in later ones
+  int last;         // worker that has the unit's last tile; < 0: there is no such unit
+  int start, r0, rows, g, wide, pad[2];
 };
 
+// Worker w is stream w / n_cta of CTA w % n_cta (wide: CTA w), so that few tiles spread over the SMs first.
 struct Work {
-  float* part;      // [cta][2][256][D] unnormalised sums: part 0 of a unit begun by an earlier CTA, part 1 of one begun here
+  float* part;      // [cta][2][256][D] unnormalised sums (stream 1: rows 128 on): part 0 of a unit begun by an earlier
+                    // worker, part 1 of one begun here
   float2* ml;       // [cta][2][256] reference maximum, weight
-  Meta* meta;       // [cta]
+  Meta* meta;       // [worker]
 };
 
 struct Request {
-  int start, n, len, past, passes, kt;
-  long long tiles;
+  int start, n, len, past, kt;
 };
 __device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) {
   Request q;
@@ -109,10 +108,14 @@ __device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) {
   q.n = s0 < 0 ? 0 : max(min(s1, a.rows) - q.start, 0);
   q.len = min(max(seq, 0), a.max_pages << a.page_log2);
   q.past = seq - (s1 - s0);
-  q.passes = (int)(((long long)q.n * a.group + kUnitRows - 1) / kUnitRows);
   q.kt = max((q.len + kTile - 1) / kTile, 1);
-  q.tiles = (long long)a.hkv * q.passes * q.kt;
   return q;
+}
+// units of the request per KV head (n * group fits 32 bits: the host has checked)
+__device__ __forceinline__ int passes(const TreeAttnArgs& a, const Request& q) { return (q.n * a.group + kUnitRows - 1) / kUnitRows; }
+__device__ __forceinline__ long long tiles(const TreeAttnArgs& a, const Request& q) { return (long long)(a.hkv * passes(a, q)) * q.kt; }
+__device__ __forceinline__ long long divide(long long x, long long y) {       // both are small as a rule
+  return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
@@ -175,16 +178,16 @@ __device__ __forceinline__ uint32_t seen32(const TreeAttnArgs& a, const Unit& u,
   return live & __funnelshift_r(word(w0), word(w0 + 1), (uint32_t)(x0 & 31));
 }
 
-// The non-finite values of new tokens that a row sees, added to columns lo .. hi - 1 of what its thread has just written
-// (they were left out of the products): bf16 results, or fp32 partial sums.
+// The non-finite values of new tokens that a row sees, added to the d columns that its thread has just written (they were
+// left out of the products): bf16 results, or fp32 partial sums.
 template <typename T>
-__device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, T* out, int lo, int hi) {
+__device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, T* out, int d) {
   const int k_from = max(u.kt0 * kTile, u.past), k_to = min((u.kt0 + u.n_tiles) * kTile, u.len);
   for (int key = k_from; key < k_to; ++key) {
     const int id = a.table[(size_t)u.b * a.max_pages + (key >> a.page_log2)];
     if (id < 0 || id >= a.n_pages || !(seen32(a, u, token, key) & 1)) continue;
     const __nv_bfloat16* v = a.vc.data + id * a.vc.s_page + u.g * a.vc.s_head + (key & ((1 << a.page_log2) - 1)) * a.vc.s_tok;
-    for (int c = lo; c < hi; ++c) {
+    for (int c = 0; c < d; ++c) {
       const float x = __bfloat162float(v[c]);
       if (!isfinite(x)) out[c] = static_cast<T>(static_cast<float>(out[c]) + x);
     }
@@ -236,7 +239,7 @@ __device__ __noinline__ void mask_tmem(const TreeAttnArgs& a, const Unit& u, int
 // add_nonfinite).  Rows lo .. hi - 1 of the tile, one after the other, the warp's lanes across the columns; eight rows of
 // loads in flight.  v: this lane's first word of row 0.
 template <int D>
-__device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first_behind, volatile int* tag, int mark) {
+__device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first_behind, volatile int* tags, int tag_lo, int tag_hi, int mark) {
   constexpr int BOXES = D / 64, BOX_WORDS = kTile * 128 / 4;
   bool met = false;
   int r = lo;
@@ -259,7 +262,7 @@ __device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first
         w[e * BOXES + b] = x;
       }
     if (met) {
-      *tag = mark;
+      for (int x = tag_lo; x <= tag_hi; ++x) tags[x * 8 + mark % 8] = mark;
       __threadfence_block();
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -283,14 +286,15 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   const uint32_t base = smem_u32(smem);
   auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
-  float2* ex = reinterpret_cast<float2*>(smem + P::EX_OFF);
   long long* scan = reinterpret_cast<long long*>(smem + P::SCAN_OFF);
   int* words = reinterpret_cast<int*>(smem + P::SCAN_OFF + 12 * 8);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(words);
   volatile int* abort_flag = words + 1;
-  volatile int* bad_tag = words + 2;               // number of the unit in which a non-finite value was last met
-  int* start_b = words + 3;
-  long long* start_rem = reinterpret_cast<long long*>(words + 4);
+  int* start_b = words + 2;                        // [stream]
+  long long* start_rem = reinterpret_cast<long long*>(words + 4);   // [stream]
+  // [stream][8]: number, from 1, of a unit in which a non-finite value was met, at that number modulo 8 (the streams of
+  // wide units write each other's and are two units apart at most)
+  volatile int* bad_tag = words + 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = blockIdx.x, n_cta = gridDim.x;
   const Abort ab{abort_flag, a.status};
@@ -299,11 +303,16 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   const bool poisoned = decode_poisoned(a.status);
   const bool misplaced = (base & 1023u) != 0;      // the tiles' swizzle needs the window's alignment
 
-  // ---- where this CTA's run begins
+  // ---- where the runs begin
   const int per = (a.n_req + kThreads - 1) / kThreads;
   const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
   long long mine = 0;
-  for (int b = b_lo; b < b_hi; ++b) mine += request(a, b).tiles;
+  bool many = false;
+  for (int b = b_lo; b < b_hi; ++b) {
+    const Request q = request(a, b);
+    mine += tiles(a, q);
+    many |= q.n * a.group > 128;
+  }
   long long incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -312,20 +321,16 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   }
   if (lane == 31) scan[warp] = incl;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < P::SLOTS; ++s) { mbar_init(bar(P::BAR_FULL + s), 1); mbar_init(bar(P::BAR_FREE + s), 1); }
+    for (int s = 0; s < P::SLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(bar(P::BAR_S + x), 1);
       mbar_init(bar(P::BAR_P + x), 4);
       mbar_init(bar(P::BAR_PV + x), 1);
-      mbar_init(bar(P::BAR_QFULL + x), 2);
+      mbar_init(bar(P::BAR_QFULL + x), 1);
       mbar_init(bar(P::BAR_QFREE + x), 1);
     }
-    for (int e = 0; e < kUnitRing; ++e) { mbar_init(bar(P::BAR_UNIT + e), 1); mbar_init(bar(P::BAR_UFREE + e), kSoftmaxWarps + 3); }
-    mbar_init(bar(P::BAR_EX), kSoftmaxWarps);
-    mbar_init(bar(P::BAR_EXDONE), kSoftmaxWarps);
     *abort_flag = 0;
-    *bad_tag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int i = 0; i < 16; ++i) bad_tag[i] = 0;
     if (misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
   }
   if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
@@ -333,7 +338,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   fence_async_smem();
   tc_fence_before();
-  __syncthreads();
+  const bool wide = __syncthreads_or(many) != 0;
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   long long before = incl - mine, total = 0;
@@ -341,124 +346,121 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
     if (w < warp) before += scan[w];
     total += scan[w];
   }
-  const long long quota = total / n_cta, extra = total % n_cta;      // the first `extra` runs are one tile longer
-  const long long w0 = cta * quota + min((long long)cta, extra), w1 = w0 + quota + (cta < extra ? 1 : 0);
-  if (before <= w0 && w0 < before + mine) {
-    long long at = before;
-    for (int b = b_lo; b < b_hi; ++b) {
-      const long long t = request(a, b).tiles;
-      if (w0 < at + t) { *start_b = b; *start_rem = w0 - at; break; }
-      at += t;
+  const int workers = wide ? n_cta : 2 * n_cta;
+  const long long quota = divide(total, workers), extra = total - quota * workers;      // the first `extra` runs are one tile longer
+  auto run_begin = [&](int w) { return w * quota + min((long long)w, extra); };
+  for (int x = 0; x < 2; ++x) {
+    const long long w0 = run_begin(wide ? cta : x * n_cta + cta);
+    if (before <= w0 && w0 < before + mine) {
+      long long at = before;
+      for (int b = b_lo; b < b_hi; ++b) {
+        const long long t = tiles(a, request(a, b));
+        if (w0 < at + t) { start_b[x] = b; start_rem[x] = w0 - at; break; }
+        at += t;
+      }
     }
   }
-  __syncthreads();
-  const bool idle = poisoned || misplaced || w0 >= w1;
-
-  // A unit's queries into its half (halves) of the Q area: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA
-  // descriptors say.  Two warps share it; a lane keeps its piece of every (64 / pieces)-th row, whose token and head
-  // advance without division (one warp with a division per piece took 13000 cycles for 128 rows).
-  uint32_t q_loads = 0;                              // bit h: parity of the loads into half h so far; bit 2 + h: any
-  auto gather = [&](const Unit& u, int which) -> bool {
-    constexpr int PIECES = D / 8, STEP = 64 / PIECES;
-    const int piece = lane % PIECES, n_half = u.rows > 128 ? 2 : 1;
-    int r = lane / PIECES + which * (STEP / 2), hg = (u.r0 + r) % a.group;
-    const __nv_bfloat16* src = a.q + (int64_t)(u.g * a.group + hg) * a.q_sh + (int64_t)(u.start + (u.r0 + r) / a.group) * a.q_sn + piece * 8;
-    const int64_t down = STEP * a.q_sh, wrap = a.q_sn - a.group * a.q_sh;
-    for (int i = 0; i < n_half; ++i) {
-      const int h = u.half + i, end = min((i + 1) * 128, u.rows);
-      if ((q_loads >> (2 + h)) & 1)
-        if (!__all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + h), ((q_loads >> h) & 1) ^ 1, ab, 41))) return false;
-      q_loads = (q_loads ^ (1u << h)) | (4u << h);
-      const uint32_t box = base + h * P::QHALF + (piece >> 3) * P::QBOX;
-#pragma unroll 2
-      for (; r < end; r += STEP) {
-        const int in_half = r & 127;
-        cp_async16(box + in_half * 128 + (((piece & 7) ^ (in_half & 7)) << 4), src);
-        src += down;
-        hg += STEP;
-        while (hg >= a.group) { hg -= a.group; src += wrap; }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+  if (threadIdx.x == 0) {
+    // a tile of a wide unit is let go by both streams; its unit is read by the producer in ring 0 only
+    for (int s = 0; s < P::SLOTS; ++s) mbar_init(bar(P::BAR_FREE + s), wide ? 2 : 1);
+    for (int e = 0; e < 2 * kUnitRing; ++e) {
+      mbar_init(bar(P::BAR_UNIT + e), 1);
+      mbar_init(bar(P::BAR_UFREE + e), 4 + 1 + (wide && e >= kUnitRing ? 0 : 1));
     }
-    for (int i = 0; i < n_half; ++i) {
-      if (i + 1 < n_half) asm volatile("cp.async.wait_group 1;" ::: "memory");
-      else asm volatile("cp.async.wait_group 0;" ::: "memory");
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + u.half + i));
-    }
-    return true;
-  };
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  const bool idle = __syncthreads_or(poisoned || misplaced) != 0;
+  // tiles of the streams' runs, and of the CTA; job i of a stream is job 2 i + x of the CTA (wide: its i-th tile)
+  uint32_t n_run[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int w = wide ? cta : x * n_cta + cta;
+    n_run[x] = idle ? 0u : (uint32_t)(run_begin(w + 1) - run_begin(w));
+  }
+  const uint32_t n_steps = wide ? n_run[0] : n_run[0] + n_run[1];
+  // ring positions of the K and V tiles of step j: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1)
+  auto k_pos = [&](uint32_t j) { return j == 0 ? 0u : 2 * j - 1; };
+  auto v_pos = [&](uint32_t j) { return j + 1 == n_steps ? 2 * j + 1 : 2 * j + 2; };
 
-  if (warp == kScheduler) {
-    // ------------------------------------------------------------ units
+  if (warp >= kLoader) {
+    // ------------------------------------------------------------ units of stream x and their queries
+    const int x = warp - kLoader, me = wide ? cta : x * n_cta + cta;
     bool ok = true;
-    int seq = 0, half = 0;
-    if (lane == 0) work.meta[cta].last_cta = -1;
-    if (__all_sync(0xffffffffu, !idle)) {
-      int b = *start_b;
-      long long rem = *start_rem, w = w0;
+    int seq = 0;
+    if (lane == 0) work.meta[x * n_cta + cta].last = -1;
+    if (n_run[x] > 0) {
+      int b = start_b[x];
+      long long rem = start_rem[x], w = run_begin(me);
+      const long long w1 = w + n_run[x];
       Request q = request(a, b);
       while (w < w1 && ok) {
-        while (rem >= q.tiles && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
-        if (rem >= q.tiles) break;                   // not reached while the lengths stand still
+        while (rem >= tiles(a, q) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
+        if (rem >= tiles(a, q)) break;               // not reached while the lengths stand still
         Unit u;
-        const long long nth = rem / q.kt;
-        u.kt0 = (int)(rem - nth * q.kt);
+        const int n_pass = passes(a, q);
+        const int nth = (int)divide(rem, q.kt), all_rows = q.n * a.group;
+        u.kt0 = (int)(rem - (long long)nth * q.kt);
         u.kt_all = q.kt;
         u.n_tiles = (int)min((long long)(q.kt - u.kt0), w1 - w);
-        u.g = (int)(nth / q.passes);
+        u.g = n_pass == 1 ? nth : nth / n_pass;
         u.b = b;
         u.start = q.start;
-        u.r0 = (int)(nth - (long long)u.g * q.passes) * kUnitRows;
-        u.rows = min(kUnitRows, q.n * a.group - u.r0);
+        u.r0 = (nth - u.g * n_pass) * kUnitRows + (wide ? x * 128 : 0);
+        u.rows = min(128, max(all_rows - u.r0, 0));
         u.len = q.len;
         u.past = q.past;
-        u.half = u.rows > 128 ? 0 : half;
-        const long long z = w - u.kt0 + u.kt_all - 1, cut = extra * (quota + 1);
-        u.last_cta = (int)(z < cut ? z / (quota + 1) : extra + (z - cut) / quota);
-        const int e = seq % kUnitRing;
+        const int e = x * kUnitRing + seq % kUnitRing;
         if (seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
         if (!ok) break;
         if (lane == 0) {
           units[e] = u;
-          if (u.kt0 == 0 && u.n_tiles < u.kt_all) {
-            Meta m{u.last_cta, u.start, u.r0, u.rows, u.g, {0, 0, 0}};
-            work.meta[cta] = m;
+          mbar_arrive(bar(P::BAR_UNIT + e));
+          if (u.kt0 == 0 && u.n_tiles < u.kt_all && !(wide && x == 1)) {
+            const long long z = w + u.kt_all - 1, cut = extra * (quota + 1);     // the unit's last tile
+            Meta m{(int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota)), u.start, u.r0,
+                   wide ? min(all_rows - u.r0, kUnitRows) : u.rows, u.g, wide, {0, 0}};
+            work.meta[me] = m;
           }
           if (a.seq_lens[b] > q.len) report_range(a.status, kWhereTreePage);   // longer than its table row
-          mbar_arrive(bar(P::BAR_UNIT + e));
         }
-        ++seq;
-        ok = gather(u, 0);
+        // its queries: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA descriptors say.  A lane keeps its
+        // piece of every (32 / pieces)-th row, whose token and head advance without division.
+        if (seq > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + x), (seq - 1) & 1, ab, 41));
         if (!ok) break;
-        if (u.rows <= 128) half ^= 1;
+        {
+          constexpr int PIECES = D / 8, STEP = 32 / PIECES;
+          const int piece = lane % PIECES;
+          int r = lane / PIECES, hg = (u.r0 + r) % a.group;
+          const __nv_bfloat16* src = a.q + (int64_t)(u.g * a.group + hg) * a.q_sh + (int64_t)(u.start + (u.r0 + r) / a.group) * a.q_sn + piece * 8;
+          const int64_t down = STEP * a.q_sh, wrap = a.q_sn - a.group * a.q_sh;
+          const uint32_t box = base + x * P::QHALF + (piece >> 3) * P::QBOX;
+#pragma unroll 2
+          for (; r < u.rows; r += STEP) {
+            cp_async16(box + r * 128 + (((piece & 7) ^ (r & 7)) << 4), src);
+            src += down;
+            hg += STEP;
+            while (hg >= a.group) { hg -= a.group; src += wrap; }
+          }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + x));
+        ++seq;
         w += u.n_tiles;
         rem += u.n_tiles;
       }
     }
     // no more units
-    const int e = seq % kUnitRing;
+    const int e = x * kUnitRing + seq % kUnitRing;
     if (ok && seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
     if (ok && lane == 0) {
       units[e].n_tiles = 0;
       mbar_arrive(bar(P::BAR_UNIT + e));
     }
-  } else if (warp == kLoader) {
-    // ------------------------------------------------------------ the other half of the queries
-    bool ok = true;
-    for (int seq = 0; ok; ++seq) {
-      const int e = seq % kUnitRing;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 45));
-      if (!ok) break;
-      const Unit u = units[e];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
-      if (u.n_tiles == 0) break;
-      ok = gather(u, 1);
-    }
   } else if (warp == kProducer) {
     // ------------------------------------------------------------ K and V tiles
+    if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
     bool ok = true;
     uint32_t s = 0, lap = 0;                         // next slot of the ring, times round
     const int page = 1 << a.page_log2;
@@ -467,7 +469,6 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       int id, off, g;
       bool live;
     } last{0, 0, 0, false};
-    bool any = false;                                // a V tile is outstanding: that of `last`
     auto load = [&](const Tile& tile, const CUtensorMap& map) {
       if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (lap - 1) & 1, ab, 51));
       if (!ok) return;
@@ -482,38 +483,47 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       __syncwarp();
       if (++s == P::SLOTS) { s = 0; ++lap; }
     };
-    for (int seq = 0; ok; ++seq) {
-      const int e = seq % kUnitRing;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
-      if (!ok) break;
-      const Unit u = units[e];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
-      if (u.n_tiles == 0) break;
-      const int32_t* row = a.table + (size_t)u.b * a.max_pages;
-      // lane p looks up page p of the tile, one tile ahead
-      auto lookup = [&](int kt) {
-        const int key = kt * kTile + lane * page;
-        return lane < per_tile && key < u.len ? row[key >> a.page_log2] : -1;
-      };
-      int id = lookup(u.kt0);
-      for (int t = 0; t < u.n_tiles && ok; ++t) {
-        const int kt = u.kt0 + t, key = kt * kTile + lane * page;
-        const int next = t + 1 < u.n_tiles ? lookup(kt + 1) : -1;
-        const bool live = lane < per_tile && key < u.len;
-        if (live && (id < 0 || id >= a.n_pages)) {
-          report_range(a.status, kWhereTreePage);
-          id = a.n_pages;                            // outside the tensor map: the load fills in zeros
-        }
-        const Tile now{id, key & (page - 1), u.g, live};
-        load(now, tm_k);
-        if (any) load(last, tm_v);
-        last = now;
-        any = true;
-        id = next;
+    // where each stream's walk stands (wide: stream 0's serves both)
+    struct Walk {
+      int seq, kt, kt_end, len, g, b, id;            // id: this lane's page of tile kt
+    } walk[2];
+    walk[0].seq = walk[1].seq = 0;
+    walk[0].kt = walk[0].kt_end = walk[1].kt = walk[1].kt_end = 0;
+    // lane p looks up page p of the tile, a tile ahead
+    auto lookup = [&](const Walk& k, int kt) {
+      const int key = kt * kTile + lane * page;
+      return lane < per_tile && key < k.len ? a.table[(size_t)k.b * a.max_pages + (key >> a.page_log2)] : -1;
+    };
+    auto step = [&](Walk& k, int x) -> Tile {
+      if (k.kt == k.kt_end) {
+        const int e = x * kUnitRing + k.seq % kUnitRing;
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (k.seq / kUnitRing) & 1, ab, 50));
+        if (!ok) return Tile{0, 0, 0, false};
+        const Unit& u = units[e];
+        k.kt = u.kt0; k.kt_end = u.kt0 + u.n_tiles; k.len = u.len; k.g = u.g; k.b = u.b;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+        ++k.seq;
+        k.id = lookup(k, k.kt);
       }
+      const int key = k.kt * kTile + lane * page;
+      Tile tile{k.id, key & (page - 1), k.g, lane < per_tile && key < k.len};
+      if (tile.live && (tile.id < 0 || tile.id >= a.n_pages)) {
+        report_range(a.status, kWhereTreePage);
+        tile.id = a.n_pages;                         // outside the tensor map: the load fills in zeros
+      }
+      ++k.kt;
+      if (k.kt < k.kt_end) k.id = lookup(k, k.kt);
+      return tile;
+    };
+    for (uint32_t j = 0; j < n_steps && ok; ++j) {
+      const Tile now = wide || (j & 1) == 0 ? step(walk[0], 0) : step(walk[1], 1);
+      load(now, tm_k);
+      if (j > 0) load(last, tm_v);
+      last = now;
     }
-    if (ok && any) load(last, tm_v);
+    if (n_steps > 0) load(last, tm_v);
+    // the last entry of each ring that this warp reads says that there are no more units: nothing to take from it
     if (*abort_flag && lane == 0) {
       // let the copies already in flight land before the CTA gives its shared memory back
       const long long t0 = clock64();
@@ -528,98 +538,80 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       constexpr uint32_t idesc_qk = instr_desc(128, kTile, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
       const uint32_t d_q = (uint32_t)smem_desc(base, 16, 1024), d_k = (uint32_t)smem_desc(base + P::RING_OFF, 16, 1024),
                      d_v = (uint32_t)smem_desc(base + P::RING_OFF, P::KBOX, 1024);
-      // Jobs alternate between the streams: job i belongs to stream i & 1.  S of a job may be computed once the stream's
-      // previous P has been handed to its product, so at most two jobs are between their two products.  One thread does
-      // all of this, and every instruction of the loop delays both streams: 32-bit counters, ring positions that advance
-      // by comparison, and per-stream flags in the bits of one register each.
-      Unit u;
-      u.n_tiles = 0;
-      uint32_t seq = 0, tile = 0, sub = 0;           // the unit being entered, and the next job in it
-      bool open = false, done = false;
-      uint32_t first = 0, frees = 0;                 // bit x: the job of stream x opens its sum / is the last reader of its tile
-      uint32_t fresh = 0, q_ready = 0, q_phase = 0, p_phase = 0;
-      // ring positions of the next K and V tile: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1)
-      const uint32_t n_tiles = (uint32_t)(w1 - w0);
-      uint32_t k_slot = 0, k_phase = 0, k_tile = 0, v_slot = n_tiles > 1 ? 2 : 1, v_phase = 0, v_tile = 0;
-      uint32_t n_qk = 0, n_pv = 0, polls = 0;
-      bool k_here = false, v_here = false;           // looked up ahead: a poll on the way from P to the products costs 200 cycles
+      // One thread does all of this, and every instruction of the loop delays both streams: 32-bit counters, everything
+      // about a stream in registers (the loop over the streams is unrolled).  A stream's next S is computed when its last
+      // P has gone into its product.
+      struct Stream {
+        uint32_t n_qk, n_pv;                         // products issued
+        uint32_t left, seq;                          // tiles left in the unit, units taken
+        uint32_t k_at, k_slot, v_at, v_slot;         // ring positions of the next K and V tile
+        bool first, q_here;                          // the next O opens a sum; the unit's Q has been seen
+      } st[2];
+      auto set_k = [&](Stream& t, int x) { t.k_at = k_pos(wide ? t.n_qk : 2 * t.n_qk + x); t.k_slot = t.k_at % P::SLOTS; };
+      auto set_v = [&](Stream& t, int x) { t.v_at = v_pos(wide ? t.n_pv : 2 * t.n_pv + x); t.v_slot = t.v_at % P::SLOTS; };
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        st[x].n_qk = st[x].n_pv = st[x].left = st[x].seq = 0;
+        st[x].first = st[x].q_here = false;
+        set_k(st[x], x);
+        set_v(st[x], x);
+      }
+      // Tiles are seen to arrive in the order of the ring, whichever stream they are for: a barrier's parity says which
+      // phase is over only to one who has seen the phase before it, and a slot's phase before may be the other stream's.
+      uint32_t arrived = 0, a_slot = 0, a_phase = 0;
+      uint32_t polls = 0;
       long long idle_since = 0;
-      while (!(done && n_pv == n_qk)) {
-        // all polls of a round first: each is a round trip to shared memory, 200 cycles while the tensor core streams from
-        // it, and they overlap only if no product stands between them
+      while (st[0].n_pv != n_run[0] || st[1].n_pv != n_run[1]) {
         bool moved = false;
-        const uint32_t px = n_pv & 1;
-        if (n_pv != n_qk && !v_here) v_here = mbar_test(bar(P::BAR_FULL + v_slot), v_phase);
-        if (open && !k_here) k_here = mbar_test(bar(P::BAR_FULL + k_slot), k_phase);
-        // with both streams between their products nothing else can be done: the wait that the hardware wakes
-        const uint32_t p_bar = bar(P::BAR_P + px), p_parity = (p_phase >> px) & 1;
-        const bool p_here = n_pv != n_qk && (v_here && n_qk - n_pv == 2 ? mbar_try_wait(p_bar, p_parity) : mbar_test(p_bar, p_parity));
-        {
-          const uint32_t x = px, bit = 1u << x;
-          if (v_here && p_here) {
+        if (arrived != 2 * n_steps && mbar_test(bar(P::BAR_FULL + a_slot), a_phase)) {
+          ++arrived;
+          if (++a_slot == P::SLOTS) { a_slot = 0; a_phase ^= 1; }
+          moved = true;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          Stream& t = st[x];
+          if (t.n_qk != t.n_pv && t.v_at < arrived && mbar_test(bar(P::BAR_P + x), t.n_pv & 1)) {
             tc_fence_after();
-            const uint32_t dv = d_v + v_slot * (P::SLOT >> 4);
-            const uint32_t acc = (first & bit) ? 0u : 1u;
+            const uint32_t dv = d_v + t.v_slot * (P::SLOT >> 4);
 #pragma unroll
             for (int kk = 0; kk < kTile / 16; ++kk)
-              mma_ts_lo(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, dv + kk * (16 * 128 >> 4), idesc_pv, kk > 0 ? 1u : acc);
+              mma_ts_lo(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, dv + kk * (16 * 128 >> 4), idesc_pv, kk > 0 || !t.first);
             mma_commit(bar(P::BAR_PV + x));
-            if (frees & bit) {
-              mma_commit(bar(P::BAR_FREE + v_slot));
-              v_here = false;
-              v_slot += ++v_tile + 1 == n_tiles ? 1 : 2;
-              if (v_slot >= P::SLOTS) { v_slot -= P::SLOTS; v_phase ^= 1; }
+            mma_commit(bar(P::BAR_FREE + t.v_slot));
+            ++t.n_pv;
+            t.first = false;
+            set_v(t, x);
+            moved = true;
+          }
+          if (t.n_qk == t.n_pv && t.n_qk != n_run[x]) {
+            if (t.left == 0) {
+              const uint32_t e = x * kUnitRing + t.seq % kUnitRing;
+              if (mbar_test(bar(P::BAR_UNIT + e), (t.seq / kUnitRing) & 1)) {
+                t.left = units[e].n_tiles;
+                mbar_arrive(bar(P::BAR_UFREE + e));
+                ++t.seq;
+                t.q_here = false;
+                t.first = true;
+              }
             }
-            p_phase ^= bit;
-            ++n_pv;
-            moved = true;
-          }
-        }
-        if (!open && !done) {
-          const uint32_t e = seq % kUnitRing;
-          if (mbar_test(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1)) {
-            u = units[e];
-            mbar_arrive(bar(P::BAR_UFREE + e));
-            ++seq;
-            tile = sub = 0;
-            open = u.n_tiles > 0;
-            done = !open;
-            fresh = 3;
-            q_ready = 0;
-            moved = true;
-          }
-        }
-        if (open) {
-          const uint32_t x = n_qk & 1, bit = 1u << x;
-          const bool both = u.rows > 128;
-          const uint32_t h = both ? x : (uint32_t)u.half;
-          if (!((q_ready >> h) & 1) && mbar_test(bar(P::BAR_QFULL + h), (q_phase >> h) & 1)) { q_ready |= 1u << h; q_phase ^= 1u << h; }
-          if (n_qk - n_pv < 2 && ((q_ready >> h) & 1) && k_here) {
-            tc_fence_after();
-            const uint32_t dq = d_q + h * (P::QHALF >> 4), dk = d_k + k_slot * (P::SLOT >> 4);
+            if (t.left != 0 && t.k_at < arrived) {
+              if (!t.q_here) t.q_here = mbar_test(bar(P::BAR_QFULL + x), (t.seq - 1) & 1);
+              if (t.q_here) {
+                tc_fence_after();
+                const uint32_t dq = d_q + x * (P::QHALF >> 4), dk = d_k + t.k_slot * (P::SLOT >> 4);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-              mma_ss_lo(tmem + P::S_COL + x * 128, dq + (kk >> 2) * (P::QBOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::KBOX >> 4) + (kk & 3) * 2, idesc_qk,
-                     kk > 0);
-            mma_commit(bar(P::BAR_S + x));
-            const bool last_sub = !both || sub == 1;
-            first = (first & ~bit) | (fresh & bit);
-            fresh &= ~bit;
-            frees = last_sub ? frees | bit : frees & ~bit;
-            if (tile + 1 == (uint32_t)u.n_tiles) mma_commit(bar(P::BAR_QFREE + h));        // the unit's last use of this half
-            if (last_sub) {
-              mma_commit(bar(P::BAR_FREE + k_slot));
-              k_here = false;
-              k_slot += k_tile++ == 0 ? 1 : 2;
-              if (k_slot >= P::SLOTS) { k_slot -= P::SLOTS; k_phase ^= 1; }
-              sub = 0;
-              ++tile;
-              open = tile != (uint32_t)u.n_tiles;
-            } else {
-              sub = 1;
+                for (int kk = 0; kk < D / 16; ++kk)
+                  mma_ss_lo(tmem + P::S_COL + x * 128, dq + (kk >> 2) * (P::QBOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::KBOX >> 4) + (kk & 3) * 2,
+                            idesc_qk, kk > 0);
+                mma_commit(bar(P::BAR_S + x));
+                mma_commit(bar(P::BAR_FREE + t.k_slot));
+                if (--t.left == 0) mma_commit(bar(P::BAR_QFREE + x));
+                ++t.n_qk;
+                set_k(t, x);
+                moved = true;
+              }
             }
-            ++n_qk;
-            moved = true;
           }
         }
         if (moved) {
@@ -643,45 +635,42 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   } else {
     // ------------------------------------------------------------ softmax and epilogue
     const int x = warp >> 2;                          // stream
-    const int row = threadIdx.x & 127;                // TMEM lane
+    const int row = threadIdx.x & 127;                // TMEM lane, row of the stream
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + P::S_COL + x * 128, t_o = tmem + lanes + P::O_COL + x * P::O_STEP;
     const float scale = a.scale_log2;
     bool ok = true;
-    uint32_t jobs_before = 0, tiles_before = 0;
-    uint32_t n_jobs = 0, n_joins = 0;                 // of this stream so far; joins of both streams
+    uint32_t n_jobs = 0;                              // of this stream so far
     for (int seq = 0; ok; ++seq) {
-      const int e = seq % kUnitRing;
+      const int e = x * kUnitRing + seq % kUnitRing;
       ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
       if (!ok) break;
       const Unit& u = units[e];                       // stays in shared memory until the unit is done: registers are short
-      if (u.n_tiles == 0) break;
-      const bool both = u.rows > 128;                 // the streams are halves of the rows; else they take turns at the tiles
-      const int my_row = both ? x * 128 + row : row;  // row of the unit
-      const bool warp_live = (both ? x * 128 : 0) + (warp & 3) * 32 < u.rows;
-      const bool live = my_row < u.rows;
-      const int abs_row = u.r0 + my_row;
+      const int n_tiles = u.n_tiles;
+      if (n_tiles == 0) break;
+      const bool warp_live = (warp & 3) * 32 < u.rows, live = row < u.rows;
+      const int abs_row = u.r0 + row;
       const int token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
-      const int t_first = both ? 0 : (int)((jobs_before + x) & 1), t_step = both ? 1 : 2;
-      float m_ref = live ? kNoMax : -kNoMax, l = 0.f;       // lanes without a row: all weights zero
-      for (int t = t_first; t < u.n_tiles && ok; t += t_step) {
-        const int k0 = (u.kt0 + t) * kTile;
-        const bool special = k0 + kTile > min(u.past, u.len);
+      const int kt0 = u.kt0, no_mask = min(u.past, u.len);      // keys before it are seen by every row
+      float m_ref = live ? kNoMax : -kNoMax, l = 0.f;           // lanes without a row: all weights zero
+      for (int t = 0; t < n_tiles && ok; ++t) {
+        const int k0 = (kt0 + t) * kTile;
+        const bool special = k0 + kTile > no_mask;
         ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + x), n_jobs & 1, ab, 31));
         if (!ok) break;
         tc_fence_after();
         if (special) {
-          // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite)
-          const uint32_t tile = tiles_before + t, v_step = 2 * tile + (tile + 1 == (uint32_t)(w1 - w0) ? 1 : 2), s = v_step % P::SLOTS;
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (v_step / P::SLOTS) & 1, ab, 32));
+          // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite).  S of the
+          // tile is there, so every tile up to its K has arrived, the one before V in V's slot among them.
+          const uint32_t p = v_pos(wide ? n_jobs : 2 * n_jobs + x), s = p % P::SLOTS;
+          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
           if (!ok) break;
           // each warp of the stream 32 keys
-          const int r_lo = (warp & 3) * 32, behind = u.len - k0;
-          const int lo = max(min(u.past, u.len) - k0, r_lo);
+          const int r_lo = (warp & 3) * 32, lo = max(no_mask - k0, r_lo);
           if (lo < r_lo + 32) {
             uint32_t* v = reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane;
-            // the tag before the zeros: with more than 128 rows both streams clean the same tile, and who finds zeros finds the tag
-            clean_values<D>(v, lo, r_lo + 32, behind, bad_tag, seq + 1);
+            // the tags before the zeros: in a wide unit both streams clean the same tile, and who finds zeros finds its tag
+            clean_values<D>(v, lo, r_lo + 32, u.len - k0, bad_tag, wide ? 0 : x, wide ? 1 : x, seq + 1);
           }
           fence_async_smem();
           __syncwarp();
@@ -711,12 +700,12 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
             m0 = max3(m0, val(28), val(29));
             m1 = max3(m1, val(30), val(31));
             const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
-            const bool grown = live && mx > m_ref + 8.f;       // lanes without a row hold anything
+            const bool grown = mx > m_ref + 8.f;              // never in lanes without a row
             if (__any_sync(0xffffffffu, grown)) {
               const float m_new = grown ? ceilf(mx) : m_ref;
               const float alpha = ex2_approx(m_ref - m_new);
               // the stream's previous product came before this S, and nothing of this P has been handed over
-              rescale_tmem<D>(t_o, t_s, alpha, c, t != t_first);
+              rescale_tmem<D>(t_o, t_s, alpha, c, t > 0);
               l *= alpha;
               sum *= alpha;
               m_ref = m_new;
@@ -750,85 +739,48 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         if (lane == 0) mbar_arrive(bar(P::BAR_P + x));
         ++n_jobs;
       }
-      const int mine_jobs = t_first < u.n_tiles ? (u.n_tiles - t_first + t_step - 1) / t_step : 0;
-      if (ok && mine_jobs > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + x), (n_jobs - 1) & 1, ab, 33));
-      // join the streams' weights
-      float m_all = m_ref, l_all = l, f0 = 1.f, f1 = 0.f;           // factors of this group's two O's
-      if (!both && ok) {
-        tc_fence_before();
-        ex[x * 128 + row] = make_float2(m_ref, l);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(P::BAR_EX));
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_EX), n_joins & 1, ab, 34));
-        if (ok) {
-          const float2 e0 = ex[row], e1 = ex[128 + row];
-          m_all = fmaxf(e0.x, e1.x);
-          f0 = ex2_approx(e0.x - m_all);
-          f1 = ex2_approx(e1.x - m_all);
-          l_all = e0.y * f0 + e1.y * f1;
-        }
-      }
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + x), (n_jobs - 1) & 1, ab, 33));
       if (ok) {
         tc_fence_after();
-        const bool whole = u.kt0 == 0 && u.n_tiles == u.kt_all;
-        const float inv = l_all != 0.f ? 1.f / l_all : 0.f;
-        const int c_lo = both ? 0 : x * (D / 64), c_n = both ? D / 32 : D / 64;   // 32-column chunks that this group writes
-        const bool repair = *bad_tag == seq + 1;
-        const size_t slot = ((size_t)cta * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + my_row;
         if (warp_live) {
+          const bool whole = kt0 == 0 && n_tiles == u.kt_all;
+          const float f = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
+          const size_t slot = ((size_t)cta * 2 + (kt0 > 0 ? 0 : 1)) * kUnitRows + x * 128 + row;
           __nv_bfloat16* out = a.o + head * a.o_sh + (u.start + token) * a.o_sn;
           float* part = work.part + slot * D;
-          if (whole) { f0 *= inv; f1 *= inv; }
-          // an O that no tile has gone into holds anything: with a single tile the other stream's
-          const bool one = both || u.n_tiles == 1;
-          const uint32_t at = tmem + lanes + P::O_COL, at0 = at + ((both ? x : one ? (int)(jobs_before & 1) : 0) * P::O_STEP);
-          if (one && !both && (jobs_before & 1)) f0 = f1;
-#pragma unroll 1
-          for (int c = c_lo; c < c_lo + c_n; ++c) {
-            uint32_t y[32];
-            float o[32];
-            tmem_ld32(at0 + c * 32, y);
+          uint32_t y[2][32];
+          tmem_ld32_async(t_o, y[0]);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(y[i]) * f0;
-            if (!one) {
-              tmem_ld32(at + P::O_STEP + c * 32, y);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = fmaf(__uint_as_float(y[i]), f1, o[i]);
-            }
-            if (live && whole) {
+          for (int c = 0; c < D / 32; ++c) {
+            tmem_ld_wait();
+            reg_fence32(y[c & 1]);
+            if (c + 1 < D / 32) tmem_ld32_async(t_o + (c + 1) * 32, y[(c + 1) & 1]);
+            if (!live) continue;
+            auto val = [&](int i) { return __uint_as_float(y[c & 1][i]) * f; };
+            if (whole) {
               uint4* dst = reinterpret_cast<uint4*>(out + c * 32);
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                dst[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]),
-                                    pack_bf16(o[8 * i + 6], o[8 * i + 7]));
-            } else if (live) {
+                dst[i] = make_uint4(pack_bf16(val(8 * i), val(8 * i + 1)), pack_bf16(val(8 * i + 2), val(8 * i + 3)), pack_bf16(val(8 * i + 4), val(8 * i + 5)),
+                                    pack_bf16(val(8 * i + 6), val(8 * i + 7)));
+            } else {
               float4* dst = reinterpret_cast<float4*>(part + c * 32);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+              for (int i = 0; i < 8; ++i) dst[i] = make_float4(val(4 * i), val(4 * i + 1), val(4 * i + 2), val(4 * i + 3));
             }
           }
-          if (live && repair) {
-            if (whole) add_nonfinite(a, u, token, out, c_lo * 32, (c_lo + c_n) * 32);
-            else add_nonfinite(a, u, token, part, c_lo * 32, (c_lo + c_n) * 32);
+          if (live) {
+            if (bad_tag[x * 8 + (seq + 1) % 8] == seq + 1) {
+              if (whole) add_nonfinite(a, u, token, out, D);
+              else add_nonfinite(a, u, token, part, D);
+            }
+            if (!whole) work.ml[slot] = make_float2(m_ref, l);
+            else if (a.lse) a.lse[(size_t)head * a.rows + u.start + token] = l != 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
           }
-          if (live && (both || x == 0)) {
-            if (!whole) work.ml[slot] = make_float2(m_all, l_all);
-            else if (a.lse)
-              a.lse[(size_t)head * a.rows + u.start + token] = l_all != 0.f ? (m_all + log2f(l_all)) * 0.6931471805599453f : -CUDART_INF_F;
-          }
-        }
-        if (!both) {
-          // neither stream's next product may overwrite an O that the other group is still reading
-          tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(P::BAR_EXDONE));
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_EXDONE), n_joins & 1, ab, 35));
-          tc_fence_after();
-          ++n_joins;
         }
+        tc_fence_before();                            // O has left TMEM: before the P after which the next product overwrites it
       }
-      jobs_before += both ? 2 * u.n_tiles : u.n_tiles;
-      tiles_before += u.n_tiles;
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
     }
@@ -842,10 +794,10 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
   }
 }
 
-// Joins the parts of the cut units, in the order of the keys: the part of the CTA in which a unit begins, then those of
-// the CTAs after it.  A warp reads a row's part at once (its 32 lanes the columns).  The work is a few MB from L2 at most
-// and all latency, so it is spread as widely as it goes: every block lists the cut units (one per CTA of the first kernel
-// at most) and takes every gridDim.x-th run of rows; as long as the device has warps to spare, 2, 4 or 8 of them share
+// Joins the parts of the cut units, in the order of the keys: the part of the worker in which a unit begins, then those
+// of the workers after it.  A warp reads a row's part at once (its 32 lanes the columns).  The work is a few MB from L2 at most
+// and all latency, so it is spread as widely as it goes: every block lists the cut units (one per worker of the first
+// kernel at most) and takes every gridDim.x-th run of rows; as long as the device has warps to spare, 2, 4 or 8 of them share
 // the parts of a row.
 constexpr int kJoinWarps = 8, kJoinBlocksPerSm = 4;
 
@@ -857,9 +809,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_j
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (decode_poisoned(a.status)) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // rows of the unit that begins in CTA i and goes on in later ones; thread t looks after CTAs per * t ...
-  const int per = (n_cta + kJoinWarps * 32 - 1) / (kJoinWarps * 32);
-  auto rows_of = [&](int i) { return i < n_cta && work.meta[i].last_cta >= 0 ? work.meta[i].rows : 0; };
+  // rows of the unit that begins in worker i and goes on in later ones; thread t looks after workers per * t ...
+  const int per = (2 * n_cta + kJoinWarps * 32 - 1) / (kJoinWarps * 32);
+  auto rows_of = [&](int i) { return i < 2 * n_cta && work.meta[i].last >= 0 ? work.meta[i].rows : 0; };
   auto block_scan = [&](int mine, int* total) {      // sum over the threads before this one
     int incl = mine;
 #pragma unroll
@@ -901,7 +853,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_j
     __syncthreads();
     const int owner = s_owner, r = s_first + warp / share, turn = warp % share;
     const Meta m = work.meta[owner];
-    const int parts = m.last_cta - owner + 1;
+    const int parts = m.last - owner + 1;
     float mx = kNoMax, l = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -915,7 +867,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_j
           const int p = p0 + i * share;
           ml[i] = make_float2(kNoMax, 0.f);
           if (p < parts) {
-            const size_t slot = ((size_t)(owner + p) * 2 + (p == 0 ? 1 : 0)) * kUnitRows + r;
+            const int w = owner + p, stream = w >= n_cta;          // wide: never
+            const size_t slot = ((size_t)(w - stream * n_cta) * 2 + (p == 0 ? 1 : 0)) * kUnitRows + stream * 128 + r;
             ml[i] = work.ml[slot];
             if (E == 4) *reinterpret_cast<float4*>(y[i]) = *reinterpret_cast<const float4*>(work.part + slot * D + lane * 4);
             else *reinterpret_cast<float2*>(y[i]) = *reinterpret_cast<const float2*>(work.part + slot * D + lane * 2);
@@ -1009,7 +962,7 @@ cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
 }  // namespace
 
 size_t tree_attn_workspace_bytes(int n_sm) {
-  return (size_t)n_sm * (2 * kUnitRows * (128 * sizeof(float) + sizeof(float2)) + sizeof(Meta));
+  return (size_t)n_sm * (2 * kUnitRows * (128 * sizeof(float) + sizeof(float2)) + 2 * sizeof(Meta));
 }
 
 cudaError_t launch_tree_attn(const TreeAttnArgs& a, void* ws, int n_sm, cudaStream_t s) {

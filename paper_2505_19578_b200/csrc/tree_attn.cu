@@ -129,6 +129,20 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// Three barriers polled at once (bit i: phase of barrier i over): the round trips overlap.
+__device__ __forceinline__ uint32_t mbar_test3(uint32_t b0, uint32_t par0, uint32_t b1, uint32_t par1, uint32_t b2, uint32_t par2) {
+  uint32_t r0, r1, r2;
+  asm volatile(
+      "{\n\t.reg .pred p, q, r;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%3], %4;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 q, [%5], %6;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 r, [%7], %8;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\tselp.u32 %1, 2, 0, q;\n\tselp.u32 %2, 4, 0, r;\n\t}"
+      : "=r"(r0), "=r"(r1), "=r"(r2)
+      : "r"(b0), "r"(par0), "r"(b1), "r"(par1), "r"(b2), "r"(par2)
+      : "memory");
+  return r0 | r1 | r2;
+}
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -547,14 +561,19 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         uint32_t k_at, k_slot, v_at, v_slot;         // ring positions of the next K and V tile
         bool first, q_here;                          // the next O opens a sum; the unit's Q has been seen
       } st[2];
-      auto set_k = [&](Stream& t, int x) { t.k_at = k_pos(wide ? t.n_qk : 2 * t.n_qk + x); t.k_slot = t.k_at % P::SLOTS; };
-      auto set_v = [&](Stream& t, int x) { t.v_at = v_pos(wide ? t.n_pv : 2 * t.n_pv + x); t.v_slot = t.v_at % P::SLOTS; };
+      const uint32_t stride = wide ? 2 : 4;          // between a stream's tiles in the ring
+      auto advance = [&](uint32_t& at, uint32_t& slot, uint32_t by) {
+        at += by;
+        slot += by;
+        if (slot >= P::SLOTS) slot -= P::SLOTS;
+      };
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         st[x].n_qk = st[x].n_pv = st[x].left = st[x].seq = 0;
         st[x].first = st[x].q_here = false;
-        set_k(st[x], x);
-        set_v(st[x], x);
+        const uint32_t j = wide ? 0 : x;
+        st[x].k_at = k_pos(j); st[x].k_slot = st[x].k_at % P::SLOTS;
+        st[x].v_at = v_pos(j); st[x].v_slot = st[x].v_at % P::SLOTS;
       }
       // Tiles are seen to arrive in the order of the ring, whichever stream they are for: a barrier's parity says which
       // phase is over only to one who has seen the phase before it, and a slot's phase before may be the other stream's.
@@ -563,7 +582,9 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       long long idle_since = 0;
       while (st[0].n_pv != n_run[0] || st[1].n_pv != n_run[1]) {
         bool moved = false;
-        if (arrived != 2 * n_steps && mbar_test(bar(P::BAR_FULL + a_slot), a_phase)) {
+        // a poll is a round trip to shared memory, 200 cycles and more while the tensor core streams from it
+        const uint32_t polled = mbar_test3(bar(P::BAR_P), st[0].n_pv & 1, bar(P::BAR_P + 1), st[1].n_pv & 1, bar(P::BAR_FULL + a_slot), a_phase);
+        if ((polled & 4) && arrived != 2 * n_steps) {
           ++arrived;
           if (++a_slot == P::SLOTS) { a_slot = 0; a_phase ^= 1; }
           moved = true;
@@ -571,7 +592,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           Stream& t = st[x];
-          if (t.n_qk != t.n_pv && t.v_at < arrived && mbar_test(bar(P::BAR_P + x), t.n_pv & 1)) {
+          if (t.n_qk != t.n_pv && t.v_at < arrived && ((polled >> x) & 1)) {
             tc_fence_after();
             const uint32_t dv = d_v + t.v_slot * (P::SLOT >> 4);
 #pragma unroll
@@ -581,7 +602,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
             mma_commit(bar(P::BAR_FREE + t.v_slot));
             ++t.n_pv;
             t.first = false;
-            set_v(t, x);
+            // the last V of the CTA has no K ahead of it
+            advance(t.v_at, t.v_slot, (wide ? t.n_pv : 2 * t.n_pv + x) + 1 == n_steps ? stride - 1 : stride);
             moved = true;
           }
           if (t.n_qk == t.n_pv && t.n_qk != n_run[x]) {
@@ -608,7 +630,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
                 mma_commit(bar(P::BAR_FREE + t.k_slot));
                 if (--t.left == 0) mma_commit(bar(P::BAR_QFREE + x));
                 ++t.n_qk;
-                set_k(t, x);
+                advance(t.k_at, t.k_slot, t.k_at == 0 ? stride - 1 : stride);      // the first K has no V ahead of the next
                 moved = true;
               }
             }

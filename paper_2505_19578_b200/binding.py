@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 
 import torch
 
@@ -135,31 +134,22 @@ def _view(t: torch.Tensor) -> SpTensor:
     return s
 
 
-# sp_tensor as bytes: data, shape[4], stride[4].  Decode-side calls take a few microseconds on the device; a packed
-# struct costs a fraction of filling a ctypes one.
-_PACK = struct.Struct("P8q").pack
+_native = None
 
 
-def _bf16(t, dim, device, what):
-    """A [heads, rows, dim] / [1, heads, rows, dim] view (dim = 3) or a [pages, heads, page, dim] cache (dim = 4)."""
-    if t.dtype is not torch.bfloat16 or t.device.type != "cuda" or t.device.index != device:
-        raise ValueError(f"{what}: expected a bf16 tensor on cuda:{device}")
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 4:
-        return _PACK(t.data_ptr(), *shape, *stride)
-    if len(shape) != 3 or dim != 3:
-        raise ValueError(f"{what}: expected {'[heads, rows, dim]' if dim == 3 else '[pages, heads, page, dim]'}")
-    return _PACK(t.data_ptr(), 1, *shape, 0, *stride)
-
-
-def _ints(t, shape, device, what):
-    """Address of a contiguous int32 tensor of this shape (None in it: any size)."""
-    if t.dtype is not torch.int32 or t.device.type != "cuda" or t.device.index != device or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous int32 tensor on cuda:{device}")
-    got = t.shape
-    if len(got) != len(shape) or any(w is not None and w != g for w, g in zip(shape, got)):
-        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(got)}")
-    return t.data_ptr()
+def _decode_calls():
+    """The compiled Python entry of the decode-side calls (argument checks and marshalling), wired to the loaded library."""
+    global _native
+    if _native is None:
+        path = os.path.join(_HERE, "_decode_calls.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} not found: build it with `python -m paper_2505_19578_b200.build`")
+        from . import _decode_calls as native
+        lib = load()
+        native.set_functions(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
+                               for f in ("sp_page_tables", "sp_qk_norm_rope", "sp_tree_attn", "sp_cache_keep")))
+        _native = native
+    return _native
 
 
 def _i32(xs):
@@ -306,70 +296,44 @@ class Context:
 
 
     # ---- from prefill into decoding ------------------------------------------
-
-    def _decode_stream(self, stream):
-        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+    # `stream`: a torch stream; the context's device's current one otherwise.
 
     def sp_page_tables(self, past_lens, new_lens, page, free_pages, block_table, seq_lens, row_start, positions, slots, info,
                        parents=None, tree_mask=None, stream=None):
         """past_lens, new_lens, seq_lens [n]; free_pages [any]; block_table [n, max_pages]; row_start [n + 1]; positions,
         slots, parents [rows]; tree_mask [rows, words] (the bit patterns as int32); info [4].  All int32 on the device."""
-        dev, n, rows = self.device, past_lens.shape[0], slots.shape[0]
-        words = tree_mask.shape[1] if tree_mask is not None else 0
-        _check(self._lib.sp_page_tables(
-            self._h, _ints(past_lens, (n,), dev, "past_lens"), _ints(new_lens, (n,), dev, "new_lens"), n, page,
-            _ints(free_pages, (None,), dev, "free_pages"), free_pages.shape[0], _ints(block_table, (n, None), dev, "block_table"),
-            block_table.shape[1], None if parents is None else _ints(parents, (rows,), dev, "parents"),
-            _ints(seq_lens, (n,), dev, "seq_lens"), _ints(row_start, (n + 1,), dev, "row_start"),
-            _ints(positions, (rows,), dev, "positions"), _ints(slots, (rows,), dev, "slots"),
-            None if tree_mask is None else _ints(tree_mask, (rows, words), dev, "tree_mask"), words, rows,
-            _ints(info, (4,), dev, "info"), self._decode_stream(stream)), "sp_page_tables")
+        code = (_native or _decode_calls()).page_tables(
+            self._h.value, self.device, past_lens, new_lens, page, free_pages, block_table, seq_lens, row_start, positions, slots,
+            info, parents, tree_mask, None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_page_tables")
 
     def sp_qk_norm_rope(self, q, k, v, positions, inv_freq, q_out, k_out=None, v_out=None, k_cache=None, v_cache=None, slots=None,
                         q_weight=None, k_weight=None, eps=1e-6, interleaved=False, stream=None):
         """q, q_out [Hq, rows, d]; k, v, k_out, v_out [Hkv, rows, d]; caches [pages, Hkv, page, d]; positions, slots int32
         [rows]; weights bf16 [d]; inv_freq: host float64 tensor (2 * its length elements of a head turn)."""
-        dev, rows, d = self.device, q.shape[-2], q.shape[-1]
-        if inv_freq.is_cuda or inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
-            raise ValueError("inv_freq: expected a contiguous one-dimensional float64 tensor on the host")
-        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if w is not None and (w.dtype is not torch.bfloat16 or w.device.type != "cuda" or w.device.index != dev or
-                                  tuple(w.shape) != (d,) or not w.is_contiguous()):
-                raise ValueError(f"{name}: expected a contiguous bf16 tensor [{d}] on cuda:{dev}")
-        view = lambda t, dim, name: None if t is None else _bf16(t, dim, dev, name)
-        _check(self._lib.sp_qk_norm_rope(
-            self._h, _bf16(q, 3, dev, "q"), _bf16(k, 3, dev, "k"), _bf16(v, 3, dev, "v"),
-            None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
-            inv_freq.data_ptr(), inv_freq.shape[0], int(bool(interleaved)), _ints(positions, (rows,), dev, "positions"),
-            _bf16(q_out, 3, dev, "q_out"), view(k_out, 3, "k_out"), view(v_out, 3, "v_out"), view(k_cache, 4, "k_cache"),
-            view(v_cache, 4, "v_cache"), None if slots is None else _ints(slots, (rows,), dev, "slots"),
-            self._decode_stream(stream)), "sp_qk_norm_rope")
+        code = (_native or _decode_calls()).qk_norm_rope(
+            self._h.value, self.device, q, k, v, positions, inv_freq, q_out, k_out, v_out, k_cache, v_cache, slots, q_weight,
+            k_weight, eps, interleaved, None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_qk_norm_rope")
 
     def sp_tree_attn(self, q, k_cache, v_cache, block_table, seq_lens, row_start, out, tree_mask=None, lse_out=None, stream=None):
         """q, out [Hq, rows, d]; caches [pages, Hkv, page, d]; block_table int32 [n, max_pages]; seq_lens [n]; row_start
         [n + 1]; tree_mask int32 [rows, words]; lse_out fp32 [Hq, rows]."""
-        dev, n, rows = self.device, seq_lens.shape[0], q.shape[-2]
-        words = tree_mask.shape[1] if tree_mask is not None else 0
-        if lse_out is not None and (lse_out.dtype is not torch.float32 or lse_out.device.type != "cuda" or
-                                    lse_out.device.index != dev or tuple(lse_out.shape) != (q.shape[-3], rows) or
-                                    not lse_out.is_contiguous()):
-            raise ValueError(f"lse_out: expected a contiguous fp32 tensor [{q.shape[-3]}, {rows}] on cuda:{dev}")
-        _check(self._lib.sp_tree_attn(
-            self._h, _bf16(q, 3, dev, "q"), _bf16(k_cache, 4, dev, "k_cache"), _bf16(v_cache, 4, dev, "v_cache"),
-            _ints(block_table, (n, None), dev, "block_table"), block_table.shape[1], _ints(seq_lens, (n,), dev, "seq_lens"),
-            _ints(row_start, (n + 1,), dev, "row_start"), n,
-            None if tree_mask is None else _ints(tree_mask, (rows, words), dev, "tree_mask"), words,
-            _bf16(out, 3, dev, "out"), None if lse_out is None else lse_out.data_ptr(), self._decode_stream(stream)),
-            "sp_tree_attn")
+        code = (_native or _decode_calls()).tree_attn(
+            self._h.value, self.device, q, k_cache, v_cache, block_table, seq_lens, row_start, out, tree_mask, lse_out,
+            None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_tree_attn")
 
     def sp_cache_keep(self, k_cache, v_cache, block_table, past_lens, kept, n_kept, lens_out, stream=None):
         """caches [pages, Hkv, page, d]; block_table int32 [n, max_pages]; past_lens, n_kept, lens_out [n]; kept [n, any]."""
-        dev, n = self.device, past_lens.shape[0]
-        _check(self._lib.sp_cache_keep(
-            self._h, _bf16(k_cache, 4, dev, "k_cache"), _bf16(v_cache, 4, dev, "v_cache"),
-            _ints(block_table, (n, None), dev, "block_table"), block_table.shape[1], _ints(past_lens, (n,), dev, "past_lens"), n,
-            _ints(kept, (n, None), dev, "kept"), _ints(n_kept, (n,), dev, "n_kept"), kept.shape[1],
-            _ints(lens_out, (n,), dev, "lens_out"), self._decode_stream(stream)), "sp_cache_keep")
+        code = (_native or _decode_calls()).cache_keep(
+            self._h.value, self.device, k_cache, v_cache, block_table, past_lens, kept, n_kept, lens_out,
+            None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_cache_keep")
 
 
 class PatternDict:

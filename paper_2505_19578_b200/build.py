@@ -4,13 +4,15 @@
 
 Output: paper_2505_19578_b200/libshareprefill.so (cudart linked statically; the
 driver API is resolved at run time, so the library loads on a machine without a
-GPU driver).
+GPU driver), and paper_2505_19578_b200/_decode_calls.so, the Python entry of the
+decode-side calls (g++ against torch's headers).
 """
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -19,6 +21,8 @@ LIB = os.path.join(HERE, "libshareprefill.so")
 LIB_DEBUG = os.path.join(HERE, "libshareprefill_debug.so")   # the same sources with -DSP_DEBUG: range-checked indices
 SOURCES = ["api.cu", "attn_pair.cu", "attn_tc.cu", "attn_simt.cu", "mask_kernel.cu", "pooled_pattern.cu", "vslash.cu",
            "api_decode.cu", "page_tables.cu", "qk_norm_rope.cu", "tree_attn.cu", "tree_attn_simt.cu"]
+CALLS = os.path.join(HERE, "_decode_calls.so")
+CALLS_SOURCE = os.path.join(CSRC, "decode_calls.cpp")
 HEADERS = [os.path.join(CSRC, "common.cuh"), os.path.join(ROOT, "include", "shareprefill.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -43,11 +47,42 @@ def needs_build(lib: str = LIB) -> bool:
     return any(os.path.getmtime(d) > t for d in deps + extra)
 
 
+def _start_calls_build():
+    """Starts the compiler on the Python entry of the decode-side calls (half a minute: torch's headers)."""
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", "/usr/local/cuda/include",
+           *[f"-I{p}" for p in cpp_extension.include_paths()], CALLS_SOURCE, "-o", CALLS, "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def calls_need_build() -> bool:
+    if not os.path.exists(CALLS):
+        return True
+    t = os.path.getmtime(CALLS)
+    return any(os.path.getmtime(d) > t for d in (CALLS_SOURCE, os.path.join(ROOT, "include", "shareprefill.h")))
+
+
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     """Builds the library (debug=True: the range-checked flavour, libshareprefill_debug.so, from the same sources)."""
     lib = LIB_DEBUG if debug else LIB
-    if not force and not needs_build(lib):
-        return lib
+    calls = _start_calls_build() if calls_need_build() or (force and not debug) else None
+    try:
+        if force or needs_build(lib):
+            _build_library(lib, verbose, debug)
+    finally:
+        if calls is not None:
+            out, _ = calls.communicate()
+            if calls.returncode != 0:
+                sys.stderr.write(out)
+    if calls is not None and calls.returncode != 0:
+        raise RuntimeError("the compiler failed on decode_calls.cpp")
+    return lib
+
+
+def _build_library(lib: str, verbose: bool, debug: bool) -> None:
     objs = []
     procs = []
     for s in SOURCES:
@@ -69,7 +104,6 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     if r.returncode != 0:
         sys.stderr.write(r.stdout)
         raise RuntimeError("link failed")
-    return lib
 
 
 if __name__ == "__main__":

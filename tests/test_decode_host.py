@@ -1,6 +1,7 @@
 """The decode-side calls refuse what they do not support, before anything is launched, and the plain statements that the
 GPU tests compare with say what they should.  No GPU."""
 import ctypes
+import struct
 
 import numpy as np
 import pytest
@@ -23,10 +24,10 @@ CTX = ADDR + 4096                                                 # likewise the
 
 
 def view(shape, stride=None, data=ADDR):
-    from paper_2505_19578_b200 import binding
+    """An sp_tensor as bytes."""
     if stride is None:
         stride = [shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3], 1]
-    return binding._PACK(data, *shape, *stride)
+    return struct.pack("P8q", data, *shape, *stride)
 
 
 CACHE = (10, 2, 16, 64)
@@ -129,12 +130,25 @@ def test_valid_calls_without_a_device_are_errors_not_crashes(lib):
     assert attn(lib) == rope(lib) == tables(lib) == keep(lib) == -4
 
 
-def test_binding_refuses_host_tensors():
+def test_binding_refuses_what_is_not_on_the_device(lib):
     from paper_2505_19578_b200 import binding
-    with pytest.raises(ValueError, match="int32"):
-        binding._ints(torch.zeros(3, dtype=torch.int64), (3,), 0, "x")
-    with pytest.raises(ValueError, match="bf16"):
-        binding._bf16(torch.zeros(2, 3, 64), 3, 0, "x")
+    native = binding._decode_calls()
+    i = torch.zeros(3, dtype=torch.int32)
+    x = torch.zeros(2, 3, 64, dtype=torch.bfloat16)
+    for wrong in (i, i.long(), None, 7):
+        with pytest.raises(ValueError, match="past_lens: expected a contiguous int32 tensor on cuda:0"):
+            native.page_tables(0, 0, wrong, i, 16, i, i, i, i, i, i, i, None, None, None)
+    for wrong in (x, x.float(), "q"):
+        with pytest.raises(ValueError, match="q: expected a bf16 tensor on cuda:0"):
+            native.tree_attn(0, 0, wrong, x, x, i, i, i, x, None, None, None)
+        with pytest.raises(ValueError, match="q: expected a bf16 tensor on cuda:0"):
+            native.qk_norm_rope(0, 0, wrong, x, x, i, x, x, None, None, None, None, None, None, None, 1e-6, False, None)
+    with pytest.raises(ValueError, match="k_cache: expected a bf16 tensor"):
+        native.cache_keep(0, 0, x, x, i, i, i, i, i, None)
+    with pytest.raises(TypeError, match="expected 10 arguments, got 1"):
+        native.cache_keep(0)
+    with pytest.raises(OverflowError):
+        native.cache_keep(0, 1 << 40, x, x, i, i, i, i, i, None)
 
 
 # ---------------------------------------------------------------- the plain statements

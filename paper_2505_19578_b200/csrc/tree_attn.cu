@@ -180,16 +180,16 @@ __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) ==
 __device__ __forceinline__ uint32_t seen32(const TreeAttnArgs& a, const Unit& u, int token, int k0) {
   const int left = u.len - k0;                                       // keys of the sequence from here on
   uint32_t live = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
-  const long long x0 = (long long)k0 - u.past;                       // index of key k0 among the new tokens
+  const int x0 = k0 - u.past;                                        // index of key k0 among the new tokens
   if (x0 + 31 < 0) return live;
   if (!a.bits) {
-    const long long upto = token - x0;                               // keys 0 .. upto of these are seen
+    const int upto = token - x0;                                     // keys 0 .. upto of these are seen
     return live & (upto >= 31 ? 0xffffffffu : upto < 0 ? 0u : (2u << upto) - 1u);
   }
   const uint32_t* row = a.bits + (size_t)(u.start + token) * a.words;
-  const long long w0 = x0 >> 5;                                      // floor: keys before the new tokens are words of ones
-  auto word = [&](long long w) { return w < 0 ? 0xffffffffu : w < a.words ? row[w] : 0u; };
-  return live & __funnelshift_r(word(w0), word(w0 + 1), (uint32_t)(x0 & 31));
+  const int w0 = x0 >> 5;                                            // floor: keys before the new tokens are words of ones
+  auto word = [&](int w) { return w < 0 ? 0xffffffffu : w < a.words ? row[w] : 0u; };
+  return live & __funnelshift_r(word(w0), word(w0 + 1), (uint32_t)x0 & 31u);
 }
 
 // The non-finite values of new tokens that a row sees, added to the d columns that its thread has just written (they were
@@ -291,9 +291,46 @@ __device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first
     for (int b = 0; b < BOXES; ++b) v[b * BOX_WORDS + r * 32] = 0u;
 }
 
+// Epilogue of a stream's unit, out of the hot loop: the rows' results, or their part for the join.  Called by whole warps.
+template <int D>
+__device__ __noinline__ void write_rows(const TreeAttnArgs& a, const Work& work, const Unit& u, int x, int row, int token, int head, uint32_t t_o,
+                                        float m_ref, float l, bool repair) {
+  const bool live = row < u.rows, whole = u.kt0 == 0 && u.n_tiles == u.kt_all;
+  const float f = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
+  const size_t slot = ((size_t)blockIdx.x * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + x * 128 + row;
+  __nv_bfloat16* out = a.o + head * a.o_sh + (u.start + token) * a.o_sn;
+  float* part = work.part + slot * D;
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t y[32];
+    tmem_ld32(t_o + c * 32, y);
+    if (!live) continue;
+    auto val = [&](int i) { return __uint_as_float(y[i]) * f; };
+    if (whole) {
+      uint4* dst = reinterpret_cast<uint4*>(out + c * 32);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        dst[i] = make_uint4(pack_bf16(val(8 * i), val(8 * i + 1)), pack_bf16(val(8 * i + 2), val(8 * i + 3)), pack_bf16(val(8 * i + 4), val(8 * i + 5)),
+                            pack_bf16(val(8 * i + 6), val(8 * i + 7)));
+    } else {
+      float4* dst = reinterpret_cast<float4*>(part + c * 32);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dst[i] = make_float4(val(4 * i), val(4 * i + 1), val(4 * i + 2), val(4 * i + 3));
+    }
+  }
+  if (live) {
+    if (repair) {
+      if (whole) add_nonfinite(a, u, token, out, D);
+      else add_nonfinite(a, u, token, part, D);
+    }
+    if (!whole) work.ml[slot] = make_float2(m_ref, l);
+    else if (a.lse) a.lse[(size_t)head * a.rows + u.start + token] = l != 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
-tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const __grid_constant__ CUtensorMap tm_k,
+tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ Work work, const __grid_constant__ CUtensorMap tm_k,
                  const __grid_constant__ CUtensorMap tm_v) {
   using P = Plan<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -681,22 +718,6 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
         ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + x), n_jobs & 1, ab, 31));
         if (!ok) break;
         tc_fence_after();
-        if (special) {
-          // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite).  S of the
-          // tile is there, so every tile up to its K has arrived, the one before V in V's slot among them.
-          const uint32_t p = v_pos(wide ? n_jobs : 2 * n_jobs + x), s = p % P::SLOTS;
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
-          if (!ok) break;
-          // each warp of the stream 32 keys
-          const int r_lo = (warp & 3) * 32, lo = max(no_mask - k0, r_lo);
-          if (lo < r_lo + 32) {
-            uint32_t* v = reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane;
-            // the tags before the zeros: in a wide unit both streams clean the same tile, and who finds zeros finds its tag
-            clean_values<D>(v, lo, r_lo + 32, u.len - k0, bad_tag, wide ? 0 : x, wide ? 1 : x, seq + 1);
-          }
-          fence_async_smem();
-          __syncwarp();
-        }
         if (warp_live) {
           // Four chunks of 32 logits, the next one's load in flight, each a step of the running softmax.  The reference
           // moves, to a whole number, when the row maximum has grown by more than 2^8.
@@ -756,6 +777,22 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
           l += sum;
           tmem_wait_st();
         }
+        if (special) {
+          // Values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite).  V comes
+          // after K, hence not before the softmax.  S of the tile was there, so every tile up to its K has arrived, the one
+          // before V in V's slot among them: the barrier's parity can be told.
+          const uint32_t p = v_pos(wide ? n_jobs : 2 * n_jobs + x), s = p % P::SLOTS;
+          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
+          if (!ok) break;
+          // each warp of the stream 32 keys
+          const int r_lo = (warp & 3) * 32, lo = max(no_mask - k0, r_lo);
+          if (lo < r_lo + 32) {
+            uint32_t* v = reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane;
+            // the tags before the zeros: in a wide unit both streams clean the same tile, and who finds zeros finds its tag
+            clean_values<D>(v, lo, r_lo + 32, u.len - k0, bad_tag, wide ? 0 : x, wide ? 1 : x, seq + 1);
+          }
+          fence_async_smem();
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(P::BAR_P + x));
@@ -765,40 +802,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const Work work, const 
       if (ok) {
         tc_fence_after();
         if (warp_live) {
-          const bool whole = kt0 == 0 && n_tiles == u.kt_all;
-          const float f = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
-          const size_t slot = ((size_t)cta * 2 + (kt0 > 0 ? 0 : 1)) * kUnitRows + x * 128 + row;
-          __nv_bfloat16* out = a.o + head * a.o_sh + (u.start + token) * a.o_sn;
-          float* part = work.part + slot * D;
-          uint32_t y[2][32];
-          tmem_ld32_async(t_o, y[0]);
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            tmem_ld_wait();
-            reg_fence32(y[c & 1]);
-            if (c + 1 < D / 32) tmem_ld32_async(t_o + (c + 1) * 32, y[(c + 1) & 1]);
-            if (!live) continue;
-            auto val = [&](int i) { return __uint_as_float(y[c & 1][i]) * f; };
-            if (whole) {
-              uint4* dst = reinterpret_cast<uint4*>(out + c * 32);
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                dst[i] = make_uint4(pack_bf16(val(8 * i), val(8 * i + 1)), pack_bf16(val(8 * i + 2), val(8 * i + 3)), pack_bf16(val(8 * i + 4), val(8 * i + 5)),
-                                    pack_bf16(val(8 * i + 6), val(8 * i + 7)));
-            } else {
-              float4* dst = reinterpret_cast<float4*>(part + c * 32);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) dst[i] = make_float4(val(4 * i), val(4 * i + 1), val(4 * i + 2), val(4 * i + 3));
-            }
-          }
-          if (live) {
-            if (bad_tag[x * 8 + (seq + 1) % 8] == seq + 1) {
-              if (whole) add_nonfinite(a, u, token, out, D);
-              else add_nonfinite(a, u, token, part, D);
-            }
-            if (!whole) work.ml[slot] = make_float2(m_ref, l);
-            else if (a.lse) a.lse[(size_t)head * a.rows + u.start + token] = l != 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
-          }
+          write_rows<D>(a, work, u, x, row, token, head, t_o, m_ref, l, bad_tag[x * 8 + (seq + 1) % 8] == seq + 1);
           __syncwarp();
         }
         tc_fence_before();                            // O has left TMEM: before the P after which the next product overwrites it

@@ -542,8 +542,9 @@ int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const s
  *   p < seq is visible to new token j iff p < past, or with x = p - past
  *     tree_mask NULL:  x <= j                       (a chain; one token: all keys)
  *     else:            bit x of the token's row is set (x >= 32 * mask_words: not visible)
- *   A row that sees nothing gets zeros and lse -infinity.  What lies in masked or
- *   unused places of the cache (NaN included) does not reach the outputs.
+ *   A logit of -infinity weighs nothing, like a masked key.  A row that sees nothing
+ *   gets zeros and lse -infinity.  What lies in masked or unused places of the cache
+ *   (NaN included) does not reach the outputs.
  *   q            [1, n_q_heads, rows, head_dim], any strides as for sp_qk_norm_rope;
  *                n_q_heads a multiple of the cache's heads, at most 128.
  *   tree_mask    device u32 [rows, mask_words], mask_words in 1 .. 8, or NULL.

@@ -21,6 +21,14 @@
 // each (a unit's beginning and end then cost one stream a wait, not the SM).  Otherwise ("wide") a CTA is a worker, units
 // have up to 256 rows, and the streams are the two halves of them and walk the same tiles.
 //
+// With at most 16 rows in every request (single tokens as a rule) the tensor core's 128-row products are the wrong tool:
+// a tile costs the issuing thread 16 of them, 1400 cycles, and the softmax 128 exponentials in a row by one warp of four.
+// Then ("narrow") the eight softmax warps are on their own: each takes 16 keys of every tile, S (16 rows x 16 keys) and
+// O (16 rows x head) in registers by mma.sync m16n8k16, K and V by ldmatrix from the same ring, no hand-over between K
+// and V; their sums are added up at the unit's end.  16 mma.sync for each product and warp are a few hundred cycles of
+// the 2700 that the tile's bytes take.  (256 chats of 60 to 4000 tokens: 253 us by tcgen05 with the rows in the lanes, 291 us
+// by tcgen05 with the keys in the lanes, XXX us so.)
+//
 //   warps 0-3, 4-7  softmax and epilogue of stream 0 / 1: thread = TMEM lane = row
 //   warp 8          producer: page ids from the table, TMA loads of K and V pages into a ring of tile slots, in the order
 //                   in which the products need them: K0 K1 V0 K2 V1 ... (a V tile that arrived with its K would hold a
@@ -54,6 +62,7 @@ constexpr int kUnitRows = 256;
 constexpr int kThreads = 384;
 constexpr int kProducer = 8, kIssuer = 9, kLoader = 10;
 constexpr int kUnitRing = 4;
+constexpr int kNarrowRows = 16;
 constexpr float kNoMax = -1e30f;                 // reference maximum before any visible key: finite, below any logit
 
 template <int D>
@@ -64,12 +73,19 @@ struct Plan {
   static constexpr int SLOTS = D == 128 ? 5 : 10;
   static constexpr int RING_OFF = 2 * QHALF;
   static constexpr int MISC_OFF = RING_OFF + SLOTS * SLOT;
-  static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + SLOTS, BAR_S = BAR_FREE + SLOTS, BAR_P = BAR_S + 2, BAR_PV = BAR_P + 2,
+  // narrow: one slot more, in the second half of the Q area; two sets of 16 Q rows and the sums' exchange in the first
+  static constexpr int NSLOTS = SLOTS + 1, NRING_OFF = RING_OFF - SLOT;
+  static constexpr int NQ_BYTES = NBOX * kNarrowRows * 128, SUM_OFF = 2 * NQ_BYTES;
+  static constexpr int SUM_ROWS = 4, SUM_STRIDE = D + 8;                  // rows exchanged at a time; 8 columns more against bank conflicts
+  static_assert(SLOT == QHALF && SUM_OFF + 8 * SUM_ROWS * SUM_STRIDE * 4 <= QHALF, "");
+  static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + NSLOTS, BAR_S = BAR_FREE + NSLOTS, BAR_P = BAR_S + 2, BAR_PV = BAR_P + 2,
                        BAR_QFULL = BAR_PV + 2, BAR_QFREE = BAR_QFULL + 2, BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + 2 * kUnitRing,
                        BARS = BAR_UFREE + 2 * kUnitRing;
   static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;               // [stream][kUnitRing]
   static constexpr int SCAN_OFF = (UNIT_OFF + 2 * kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // int64 [12], then small words
-  static constexpr int TOTAL = SCAN_OFF + 12 * 8 + 112;
+  static constexpr int TAG_OFF = SCAN_OFF + 12 * 8 + 8 * 4;
+  static constexpr int EX_OFF = SCAN_OFF + 12 * 8 + 112;                              // narrow: float2 [8][16]
+  static constexpr int TOTAL = EX_OFF + 8 * kNarrowRows * 8;
   static constexpr int S_COL = 0, O_COL = 256, O_STEP = D;  // S: 128 columns a stream; O: D columns a stream
 };
 
@@ -173,6 +189,19 @@ __device__ __forceinline__ void mma_ts_lo(uint32_t d_tmem, uint32_t a_tmem, uint
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// Four 8x8 blocks of 16-bit elements from shared memory (lanes 8 i .. 8 i + 7: the rows of block i), as they are or
+// transposed, and D += A B of 16x16 by 16x8 fragments, bf16 in, fp32 out.
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
@@ -250,42 +279,35 @@ __device__ __noinline__ void mask_tmem(const TreeAttnArgs& a, const Unit& u, int
 }
 
 // Values behind the sequence become zero in a V tile, and so do non-finite ones of new tokens (reported: see
-// add_nonfinite).  Rows lo .. hi - 1 of the tile, one after the other, the warp's lanes across the columns; eight rows of
-// loads in flight.  v: this lane's first word of row 0.
+// add_nonfinite).  Rows lo .. hi - 1 of the tile, one after the other, the warp's lanes across the columns.  v: this lane's
+// first word of row 0.  Rolled loops: the code runs once a unit and is fetched anew each time; unrolled by eight rows it
+// took 2000 cycles for sixteen.
 template <int D>
 __device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first_behind, volatile int* tags, int tag_lo, int tag_hi, int mark) {
   constexpr int BOXES = D / 64, BOX_WORDS = kTile * 128 / 4;
-  bool met = false;
   int r = lo;
 #pragma unroll 1
-  for (; r < min(hi, first_behind); r += 8) {
-    uint32_t w[8 * BOXES];
+  for (; r < min(hi, first_behind); ++r) {
+    uint32_t w[BOXES];
+    bool met = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int b = 0; b < BOXES; ++b) w[e * BOXES + b] = r + e < min(hi, first_behind) ? v[b * BOX_WORDS + (r + e) * 32] : 0u;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int b = 0; b < BOXES; ++b) {
-        uint32_t x = w[e * BOXES + b];
-        if (!nonfinite2(x)) continue;
-        met = true;
-        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
-        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
-        w[e * BOXES + b] = x;
-      }
+    for (int b = 0; b < BOXES; ++b) {
+      w[b] = v[b * BOX_WORDS + r * 32];
+      met |= nonfinite2(w[b]);
+    }
     if (met) {
       for (int x = tag_lo; x <= tag_hi; ++x) tags[x * 8 + mark % 8] = mark;
       __threadfence_block();
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int b = 0; b < BOXES; ++b)
-          if (r + e < min(hi, first_behind)) v[b * BOX_WORDS + (r + e) * 32] = w[e * BOXES + b];
+      for (int b = 0; b < BOXES; ++b) {
+        uint32_t x = w[b];
+        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+        v[b * BOX_WORDS + r * 32] = x;
+      }
     }
   }
-#pragma unroll 4
+#pragma unroll 2
   for (r = max(lo, first_behind); r < hi; ++r)
 #pragma unroll
     for (int b = 0; b < BOXES; ++b) v[b * BOX_WORDS + r * 32] = 0u;
@@ -328,6 +350,213 @@ __device__ __noinline__ void write_rows(const TreeAttnArgs& a, const Work& work,
   }
 }
 
+// Requests of at most 16 rows: products and softmax in the registers of the eight warps, one call for the whole run.
+// (A function of its own, so that the registers of the other modes' loops are not allotted around it.)
+template <int D>
+__device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& work, uint8_t* smem, const Abort& ab) {
+  using P = Plan<D>;
+  const uint32_t base = smem_u32(smem);
+  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x;
+  // Fragments of mma.sync m16n8k16: lane = (row g = lane / 4, and g + 8; columns 2 q, 2 q + 1, q = lane % 4).
+  const int g = lane >> 2, q = lane & 3;
+  float2* ex = reinterpret_cast<float2*>(smem + P::EX_OFF);          // [warp][row] reference, weight
+  float* sums = reinterpret_cast<float*>(smem + P::SUM_OFF);         // [warp][row % 4][SUM_STRIDE]
+  // ldmatrix addresses of this lane: a row of the four 8x8 blocks, whose 16-byte pieces are swizzled by the row
+  const int k_row = warp * 16 + (lane & 7) + ((lane >> 4) << 3), k_piece = (lane >> 3) & 1;   // K: keys 0-7, 8-15 by piece, piece + 1
+  const int v_row = warp * 16 + (lane & 15), v_piece = lane >> 4;                            // V (and Q): rows 0-7, 8-15, then the next piece
+  const uint32_t ring = base + P::NRING_OFF;
+  auto at = [](uint32_t tile, int box, int row, int piece) {
+    return tile + (piece >> 3) * box + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+  };
+  const float scale = a.scale_log2;
+  uint32_t slot = 0, phase = 0;                     // of the next tile in the ring
+  bool ok = true;
+  for (int seq = 0;; ++seq) {
+    const int e = seq % kUnitRing;
+    ok = __all_sync(0xffffffffu, ok && mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 70));
+    // the eight warps go on together or stop together: none is left at the barriers below
+    if (!bar_and(1, 256, ok)) break;
+    const Unit& u = units[e];
+    const int n_tiles = u.n_tiles;
+    if (n_tiles == 0) break;
+    const int rows = u.rows, no_mask = min(u.past, u.len);
+    uint32_t qf[D / 16][4];
+    ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFULL + (seq & 1)), (seq >> 1) & 1, ab, 71));
+    if (ok) {
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+        ldmatrix4(at(base + (seq & 1) * P::NQ_BYTES, kNarrowRows * 128, lane & 15, 2 * kk + v_piece), qf[kk]);
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(P::BAR_QFREE + (seq & 1)));
+    float o[D / 8][4];
+#pragma unroll
+    for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+    float m0 = g < rows ? kNoMax : -kNoMax, m1 = g + 8 < rows ? kNoMax : -kNoMax, l0 = 0.f, l1 = 0.f;   // no row: all weights zero
+    for (int t = 0; t < n_tiles && ok; ++t) {
+      const int k0 = (u.kt0 + t) * kTile;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + slot), phase, ab, 72));
+      if (!ok) break;
+      float s[2][4] = {};
+      {
+        const uint32_t tile = ring + slot * P::SLOT;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          uint32_t b[4];
+          ldmatrix4(at(tile, P::KBOX, k_row, 2 * kk + k_piece), b);
+          mma16816(s[0], qf[kk], b[0], b[1]);
+          mma16816(s[1], qf[kk], b[2], b[3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_FREE + slot));
+      if (++slot == P::NSLOTS) { slot = 0; phase ^= 1; }
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] *= scale;
+      const bool special = k0 + kTile > no_mask;
+      if (special) {
+        const int key = k0 + warp * 16;
+        const uint32_t seen0 = g < rows ? seen32(a, u, g / a.group, key) : 0u, seen1 = g + 8 < rows ? seen32(a, u, (g + 8) / a.group, key) : 0u;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (!((seen0 >> (n * 8 + 2 * q + i)) & 1)) s[n][i] = -CUDART_INF_F;
+            if (!((seen1 >> (n * 8 + 2 * q + i)) & 1)) s[n][2 + i] = -CUDART_INF_F;
+          }
+      }
+      const float x0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), x1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+      if (__any_sync(0xffffffffu, x0 > m0 + 8.f || x1 > m1 + 8.f)) {
+        // the row's maximum over its four lanes; references are whole numbers, as above
+        float t0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1)), t1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
+        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, 2));
+        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, 2));
+        const float n0 = t0 > m0 + 8.f ? ceilf(t0) : m0, n1 = t1 > m1 + 8.f ? ceilf(t1) : m1;
+        const float f0 = ex2_approx(m0 - n0), f1 = ex2_approx(m1 - n1);
+        l0 *= f0;
+        l1 *= f1;
+        m0 = n0;
+        m1 = n1;
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n) { o[n][0] *= f0; o[n][1] *= f0; o[n][2] *= f1; o[n][3] *= f1; }
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        s[n][0] = ex2_approx(s[n][0] - m0);
+        s[n][1] = ex2_approx(s[n][1] - m0);
+        s[n][2] = ex2_approx(s[n][2] - m1);
+        s[n][3] = ex2_approx(s[n][3] - m1);
+        l0 += s[n][0] + s[n][1];
+        l1 += s[n][2] + s[n][3];
+      }
+      const uint32_t pf[4] = {cvt_bf16x2(s[0][0], s[0][1]), cvt_bf16x2(s[0][2], s[0][3]), cvt_bf16x2(s[1][0], s[1][1]), cvt_bf16x2(s[1][2], s[1][3])};
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + slot), phase, ab, 73));
+      if (!ok) break;
+      if (special) {
+        // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite)
+        const int lo = max(no_mask - k0, warp * 16);
+        if (lo < warp * 16 + 16) {
+          clean_values<D>(reinterpret_cast<uint32_t*>(smem + P::NRING_OFF + slot * P::SLOT) + lane, lo, warp * 16 + 16, u.len - k0, bad_tag, 0, 0, seq + 1);
+          fence_async_smem();
+        }
+        __syncwarp();
+      }
+      {
+        const uint32_t tile = ring + slot * P::SLOT;
+#pragma unroll
+        for (int n = 0; n < D / 8; n += 2) {
+          uint32_t b[4];
+          ldmatrix4t(at(tile, P::KBOX, v_row, n + v_piece), b);
+          mma16816(o[n], pf, b[0], b[1]);
+          mma16816(o[n + 1], pf, b[2], b[3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_FREE + slot));
+      if (++slot == P::NSLOTS) { slot = 0; phase ^= 1; }
+    }
+    // the row's weight over its four lanes, then the eight warps' references and weights
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+    if (q == 0) {
+      ex[warp * kNarrowRows + g] = make_float2(m0, l0);
+      ex[warp * kNarrowRows + g + 8] = make_float2(m1, l1);
+    }
+    if (!bar_and(1, 256, ok)) break;
+    const bool whole = u.kt0 == 0 && n_tiles == u.kt_all;
+    float top0 = kNoMax, top1 = kNoMax;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      top0 = fmaxf(top0, ex[w * kNarrowRows + g].x);
+      top1 = fmaxf(top1, ex[w * kNarrowRows + g + 8].x);
+    }
+    const float f0 = ex2_approx(m0 - top0), f1 = ex2_approx(m1 - top1);
+    // four rows at a time: each warp its sums, then each thread two columns (one) of a row from the eight warps
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += P::SUM_ROWS) {
+      if (r0 > 0) bar_sync(1, 256);
+      const int in = g - (r0 & 7);                  // this lane's row among them
+      if (in >= 0 && in < P::SUM_ROWS) {
+        float* mine_at = sums + (warp * P::SUM_ROWS + in) * P::SUM_STRIDE + 2 * q;
+        if (r0 < 8) {
+#pragma unroll
+          for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(mine_at + n * 8) = make_float2(o[n][0] * f0, o[n][1] * f0);
+        } else {
+#pragma unroll
+          for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(mine_at + n * 8) = make_float2(o[n][2] * f1, o[n][3] * f1);
+        }
+      }
+      bar_sync(1, 256);
+      constexpr int PER = P::SUM_ROWS * D / 256;    // columns of a thread
+      const int sub = threadIdx.x >> 6, row = r0 + sub, col = (threadIdx.x & 63) * PER;
+      if (row < rows) {
+        float top = kNoMax, all = 0.f, y[PER] = {};
+#pragma unroll
+        for (int w = 0; w < 8; ++w) top = fmaxf(top, ex[w * kNarrowRows + row].x);
+#pragma unroll 4
+        for (int w = 0; w < 8; ++w) {
+          all += ex[w * kNarrowRows + row].y * ex2_approx(ex[w * kNarrowRows + row].x - top);
+#pragma unroll
+          for (int i = 0; i < PER; ++i) y[i] += sums[(w * P::SUM_ROWS + sub) * P::SUM_STRIDE + col + i];
+        }
+        const int token = row / a.group, head = u.g * a.group + row % a.group;
+        const size_t part = ((size_t)cta * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + row;
+        __nv_bfloat16* out = a.o + head * a.o_sh + (u.start + token) * a.o_sn;
+        const float inv = all != 0.f ? 1.f / all : 0.f;
+        if (!whole) {
+#pragma unroll
+          for (int i = 0; i < PER; ++i) work.part[part * D + col + i] = y[i];
+        } else if constexpr (PER == 2) {
+          *reinterpret_cast<uint32_t*>(out + col) = pack_bf16(y[0] * inv, y[1] * inv);
+        } else {
+          out[col] = __float2bfloat16(y[0] * inv);
+        }
+        if ((threadIdx.x & 63) == 0) {
+          if (!whole) work.ml[part] = make_float2(top, all);
+          else if (a.lse) a.lse[(size_t)head * a.rows + u.start + token] = all != 0.f ? (top + log2f(all)) * 0.6931471805599453f : -CUDART_INF_F;
+        }
+      }
+    }
+    if (bad_tag[(seq + 1) % 8] == seq + 1) {
+      bar_sync(1, 256);                             // the rows are written
+      if (threadIdx.x < rows) {
+        const int row = threadIdx.x, token = row / a.group, head = u.g * a.group + row % a.group;
+        if (whole) add_nonfinite(a, u, token, a.o + head * a.o_sh + (u.start + token) * a.o_sn, D);
+        else add_nonfinite(a, u, token, work.part + (((size_t)cta * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + row) * D, D);
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ Work work, const __grid_constant__ CUtensorMap tm_k,
@@ -345,7 +574,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   long long* start_rem = reinterpret_cast<long long*>(words + 4);   // [stream]
   // [stream][8]: number, from 1, of a unit in which a non-finite value was met, at that number modulo 8 (the streams of
   // wide units write each other's and are two units apart at most)
-  volatile int* bad_tag = words + 8;
+  volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = blockIdx.x, n_cta = gridDim.x;
   const Abort ab{abort_flag, a.status};
@@ -358,11 +587,12 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   const int per = (a.n_req + kThreads - 1) / kThreads;
   const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
   long long mine = 0;
-  bool many = false;
+  bool many = false, some = false;
   for (int b = b_lo; b < b_hi; ++b) {
     const Request q = request(a, b);
     mine += tiles(a, q);
     many |= q.n * a.group > 128;
+    some |= q.n * a.group > kNarrowRows;
   }
   long long incl = mine;
 #pragma unroll
@@ -372,36 +602,32 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   }
   if (lane == 31) scan[warp] = incl;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < P::SLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
+    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(bar(P::BAR_S + x), 1);
       mbar_init(bar(P::BAR_P + x), 4);
       mbar_init(bar(P::BAR_PV + x), 1);
-      mbar_init(bar(P::BAR_QFULL + x), 1);
-      mbar_init(bar(P::BAR_QFREE + x), 1);
     }
     *abort_flag = 0;
     for (int i = 0; i < 16; ++i) bad_tag[i] = 0;
     if (misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
   }
-  if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
   // rows of the Q area that no unit fills stay zero: products of whatever lay there would cost power, and with it clock
   for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   fence_async_smem();
-  tc_fence_before();
-  const bool wide = __syncthreads_or(many) != 0;
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const bool wide = __syncthreads_or(many) != 0, narrow = __syncthreads_or(some) == 0;
+  const bool by_cta = wide || narrow;              // a CTA is a worker
+  if (warp == kIssuer && !narrow) tmem_alloc(smem_u32(tmem_slot), 512);
   long long before = incl - mine, total = 0;
   for (int w = 0; w < kThreads / 32; ++w) {
     if (w < warp) before += scan[w];
     total += scan[w];
   }
-  const int workers = wide ? n_cta : 2 * n_cta;
+  const int workers = by_cta ? n_cta : 2 * n_cta;
   const long long quota = divide(total, workers), extra = total - quota * workers;      // the first `extra` runs are one tile longer
   auto run_begin = [&](int w) { return w * quota + min((long long)w, extra); };
   for (int x = 0; x < 2; ++x) {
-    const long long w0 = run_begin(wide ? cta : x * n_cta + cta);
+    const long long w0 = run_begin(by_cta ? cta : x * n_cta + cta);
     if (before <= w0 && w0 < before + mine) {
       long long at = before;
       for (int b = b_lo; b < b_hi; ++b) {
@@ -412,30 +638,38 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     }
   }
   if (threadIdx.x == 0) {
-    // a tile of a wide unit is let go by both streams; its unit is read by the producer in ring 0 only
-    for (int s = 0; s < P::SLOTS; ++s) mbar_init(bar(P::BAR_FREE + s), wide ? 2 : 1);
+    // who lets a tile go: the stream's issuer, both streams', or the eight warps; likewise the queries
+    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FREE + s), narrow ? 8 : wide ? 2 : 1);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(bar(P::BAR_QFULL + x), narrow ? 32 : 1);
+      mbar_init(bar(P::BAR_QFREE + x), narrow ? 8 : 1);
+    }
+    // a unit is read by four softmax warps, the issuer and the producer (wide: in ring 0 only), or by eight warps and the producer
     for (int e = 0; e < 2 * kUnitRing; ++e) {
       mbar_init(bar(P::BAR_UNIT + e), 1);
-      mbar_init(bar(P::BAR_UFREE + e), 4 + 1 + (wide && e >= kUnitRing ? 0 : 1));
+      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : 4 + 1 + (wide && e >= kUnitRing ? 0 : 1));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  tc_fence_before();
   const bool idle = __syncthreads_or(poisoned || misplaced) != 0;
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
   // tiles of the streams' runs, and of the CTA; job i of a stream is job 2 i + x of the CTA (wide: its i-th tile)
   uint32_t n_run[2];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
-    const int w = wide ? cta : x * n_cta + cta;
-    n_run[x] = idle ? 0u : (uint32_t)(run_begin(w + 1) - run_begin(w));
+    const int w = by_cta ? cta : x * n_cta + cta;
+    n_run[x] = idle || (narrow && x == 1) ? 0u : (uint32_t)(run_begin(w + 1) - run_begin(w));
   }
   const uint32_t n_steps = wide ? n_run[0] : n_run[0] + n_run[1];
-  // ring positions of the K and V tiles of step j: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1)
+  // ring positions of the K and V tiles of step j: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1); narrow: K0 V0 K1 V1 ...
   auto k_pos = [&](uint32_t j) { return j == 0 ? 0u : 2 * j - 1; };
   auto v_pos = [&](uint32_t j) { return j + 1 == n_steps ? 2 * j + 1 : 2 * j + 2; };
 
   if (warp >= kLoader) {
     // ------------------------------------------------------------ units of stream x and their queries
-    const int x = warp - kLoader, me = wide ? cta : x * n_cta + cta;
+    const int x = warp - kLoader, me = by_cta ? cta : x * n_cta + cta;
     bool ok = true;
     int seq = 0;
     if (lane == 0) work.meta[x * n_cta + cta].last = -1;
@@ -476,7 +710,9 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
         }
         // its queries: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA descriptors say.  A lane keeps its
         // piece of every (32 / pieces)-th row, whose token and head advance without division.
-        if (seq > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + x), (seq - 1) & 1, ab, 41));
+        // (narrow: two sets of rows in turn)
+        const int set = narrow ? seq & 1 : x, lap = narrow ? seq >> 1 : seq;
+        if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + set), (lap - 1) & 1, ab, 41));
         if (!ok) break;
         {
           constexpr int PIECES = D / 8, STEP = 32 / PIECES;
@@ -484,7 +720,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
           int r = lane / PIECES, hg = (u.r0 + r) % a.group;
           const __nv_bfloat16* src = a.q + (int64_t)(u.g * a.group + hg) * a.q_sh + (int64_t)(u.start + (u.r0 + r) / a.group) * a.q_sn + piece * 8;
           const int64_t down = STEP * a.q_sh, wrap = a.q_sn - a.group * a.q_sh;
-          const uint32_t box = base + x * P::QHALF + (piece >> 3) * P::QBOX;
+          const uint32_t box = narrow ? base + set * P::NQ_BYTES + (piece >> 3) * (kNarrowRows * 128) : base + x * P::QHALF + (piece >> 3) * P::QBOX;
 #pragma unroll 2
           for (; r < u.rows; r += STEP) {
             cp_async16(box + r * 128 + (((piece & 7) ^ (r & 7)) << 4), src);
@@ -493,10 +729,14 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
             while (hg >= a.group) { hg -= a.group; src += wrap; }
           }
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + x));
+        if (narrow) {                                // read by ldmatrix: the copies' arrival is enough, and nobody waits for it here
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar(P::BAR_QFULL + set)) : "memory");
+        } else {
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + set));
+        }
         ++seq;
         w += u.n_tiles;
         rem += u.n_tiles;
@@ -513,6 +753,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     // ------------------------------------------------------------ K and V tiles
     if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
     bool ok = true;
+    const uint32_t ring = base + (narrow ? P::NRING_OFF : P::RING_OFF), slots = narrow ? P::NSLOTS : P::SLOTS;
     uint32_t s = 0, lap = 0;                         // next slot of the ring, times round
     const int page = 1 << a.page_log2;
     const int per_tile = max(kTile >> a.page_log2, 1), rows = min(page, kTile);
@@ -527,12 +768,12 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       if (lane == 0) mbar_expect_tx(bar(P::BAR_FULL + s), n_live * rows * D * 2);
       __syncwarp();
       if (tile.live) {
-        const uint32_t dst = base + P::RING_OFF + s * P::SLOT + lane * rows * 128;
+        const uint32_t dst = ring + s * P::SLOT + lane * rows * 128;
 #pragma unroll
         for (int x = 0; x < P::NBOX; ++x) tma_load_4d(dst + x * P::KBOX, &map, bar(P::BAR_FULL + s), x * 64, tile.off, tile.g, tile.id);
       }
       __syncwarp();
-      if (++s == P::SLOTS) { s = 0; ++lap; }
+      if (++s == slots) { s = 0; ++lap; }
     };
     // where each stream's walk stands (wide: stream 0's serves both)
     struct Walk {
@@ -568,24 +809,25 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       return tile;
     };
     for (uint32_t j = 0; j < n_steps && ok; ++j) {
-      const Tile now = wide || (j & 1) == 0 ? step(walk[0], 0) : step(walk[1], 1);
+      const Tile now = by_cta || (j & 1) == 0 ? step(walk[0], 0) : step(walk[1], 1);
       load(now, tm_k);
-      if (j > 0) load(last, tm_v);
+      if (narrow) load(now, tm_v);
+      else if (j > 0) load(last, tm_v);
       last = now;
     }
-    if (n_steps > 0) load(last, tm_v);
+    if (n_steps > 0 && !narrow) load(last, tm_v);
     // the last entry of each ring that this warp reads says that there are no more units: nothing to take from it
     if (*abort_flag && lane == 0) {
       // let the copies already in flight land before the CTA gives its shared memory back
       const long long t0 = clock64();
-      for (uint32_t i = 0; i < P::SLOTS; ++i) {
+      for (uint32_t i = 0; i < slots; ++i) {
         const uint32_t laps = lap + (i < s);          // loads that this slot has been given
         while (laps > 0 && !mbar_test(bar(P::BAR_FULL + i), (laps - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {}
       }
     }
   } else if (warp == kIssuer) {
     // ------------------------------------------------------------ products
-    if (lane == 0) {
+    if (lane == 0 && !narrow) {
       constexpr uint32_t idesc_qk = instr_desc(128, kTile, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
       const uint32_t d_q = (uint32_t)smem_desc(base, 16, 1024), d_k = (uint32_t)smem_desc(base + P::RING_OFF, 16, 1024),
                      d_v = (uint32_t)smem_desc(base + P::RING_OFF, P::KBOX, 1024);
@@ -691,6 +933,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       }
     }
     __syncwarp();
+  } else if (narrow) {
+    narrow_warps<D>(a, work, smem, ab);
   } else {
     // ------------------------------------------------------------ softmax and epilogue
     const int x = warp >> 2;                          // stream
@@ -814,7 +1058,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
 
   tc_fence_before();
   __syncthreads();
-  if (warp == kIssuer) {
+  if (warp == kIssuer && !narrow) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }

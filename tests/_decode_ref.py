@@ -81,14 +81,15 @@ def visible(n, past, bits_rows=None):
 
 def attention(q, k, v, seen):
     """One head of one request: q [n, d], k, v [len, d], seen [n, len] -> out, lse, bound of out's error, all float64.
-    Masked keys take no part whatever they hold."""
+    Masked keys take no part whatever they hold; a logit of -infinity weighs nothing, as a mask would."""
     n, d = q.shape
     out, lse, tol = np.zeros((n, d)), np.full(n, -np.inf), np.zeros((n, d))
     for j in range(n):
         idx = np.nonzero(seen[j])[0]
+        z = k[idx] @ q[j] / np.sqrt(d)
+        idx, z = idx[~np.isneginf(z)], z[~np.isneginf(z)]
         if len(idx) == 0:
             continue
-        z = k[idx] @ q[j] / np.sqrt(d)
         top = z.max()
         p = np.exp(z - top)
         total = p.sum()

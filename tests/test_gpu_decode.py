@@ -328,6 +328,11 @@ ATTN = [
     (128, 128, 64, 16, [(50, 2)], "chain", 0, "paged"),
     (128, 1, 128, 16, [(50, 3)], "tree", 0, "paged"),
     (2, 2, 64, 16, [(0, 0), (0, 0), (0, 1), (0, 0)], "chain", 0, "paged"),
+    # at most eight rows per request and key head
+    (8, 8, 128, 16, [(0, 8), (3, 1), (200, 5), (0, 0), (1000, 8), (121, 7)], "tree", 1, "paged"),
+    (16, 8, 128, 64, [(0, 4), (300, 3), (127, 1), (128, 2), (0, 1)], "any", 3, "contiguous"),
+    (14, 2, 128, 256, [(5000, 1), (7, 1), (0, 1), (511, 1), (512, 1)], "chain", 0, "token_major"),
+    (8, 1, 128, 32, [(9, 1)] * 200 + [(1900, 1)], "chain", 0, "paged"),
 ]
 
 
@@ -345,17 +350,24 @@ def test_tree_attn(attn_ctx, case):
 
 
 @pytest.mark.parametrize("spoil", ["nan", "inf", "-inf"])
-@pytest.mark.parametrize("d,page", [(64, 16), (128, 64)])
-def test_tree_attn_masked_and_unused_places_hold_anything(attn_ctx, spoil, d, page):
-    s = Step(7, 8, 2, d, page, [(130, 40), (0, 5), (1, 70), (127, 1)], "tree", 2, "paged", spoil)
+@pytest.mark.parametrize("d,page,hq,reqs", [(64, 16, 8, [(130, 40), (0, 5), (1, 70), (127, 1)]), (128, 64, 8, [(130, 40), (0, 5), (1, 70), (127, 1)]),
+                                            (128, 16, 4, [(130, 4), (0, 3), (1, 4), (127, 1), (700, 4)]), (64, 32, 4, [(130, 20), (0, 3), (600, 31)])],
+                         ids=["64-16", "128-64", "128-16-few", "64-32"])
+def test_tree_attn_masked_and_unused_places_hold_anything(attn_ctx, spoil, d, page, hq, reqs):
+    s = Step(7, hq, 2, d, page, reqs, "tree", 2, "paged", spoil)
     s.call(attn_ctx)
     clean(attn_ctx)
     s.check()
 
 
-def test_tree_attn_large_logits(attn_ctx):
-    """Logits of several hundred: one key takes all."""
-    s = Step(3, 4, 2, 128, 32, [(200, 3), (77, 10)], "tree", 0, "paged", scale=64.0)
+@pytest.mark.parametrize("reqs", [[(200, 3), (77, 10)], [(900, 3), (77, 4), (2000, 1)]], ids=["many rows", "few rows"])
+def test_tree_attn_large_logits(attn_ctx, reqs):
+    """Logits of several hundred, whose running maximum climbs from tile to tile: one key takes all."""
+    s = Step(3, 4, 2, 128, 32, reqs, "tree", 0, "paged", scale=64.0)
+    for b, (p, n) in enumerate(reqs):                                          # keys that get longer along the sequence
+        for x in range(p + n):
+            s.k[s.table[b, x // 32], :, x % 32] *= 2.0 ** -(4 - 4 * x // (p + n))
+    s.kd = dev(s.k)
     s.call(attn_ctx)
     clean(attn_ctx)
     out = host(s.out)

@@ -4,11 +4,12 @@
 //   out_r = sum_c p_rc v_c / sum_c p_rc,  p_rc = 2^(scale q_r.k_c - m_r) over the visible keys c.
 //
 // The rows of a unit are the new tokens of one request times the query heads that share a KV head (row = token * group +
-// head), so that every key and value is read once for all of them.  Work is counted in key tiles of 128: the tiles of all
-// units (request, KV head, rows) stand in one line, which is cut into one equal run per worker wherever that falls; a unit
-// that is cut leaves partial results (unnormalised sums, reference maxima, weights) that a second kernel joins in the
-// order of the keys.  All lengths are read on the device: a prefix sum over the requests tells each worker where its run
-// begins.
+// head), so that every key and value is read once for all of them.  Work is counted in steps: one for the unit (request,
+// KV head, rows) and one for each of its key tiles of 128.  The steps of all units stand in one line, which is cut into one
+// equal run per worker wherever that falls; a unit that is cut leaves partial results (unnormalised sums, reference maxima,
+// weights) that a second kernel joins in the order of the keys.  All lengths are read on the device: a prefix sum over the
+// requests tells each worker where its run begins.  (Without the step for the unit itself, workers with many short requests
+// finish late: XXX.)
 //
 // What bounds it: the cache's bytes.  A tile is 64 KB (head_dim 128), 2700 cycles of an SM's share of the measured HBM
 // rate; its matrix products take 1020 cycles for up to 128 rows (the tensor core takes 128 rows at a time, however few
@@ -82,9 +83,10 @@ struct Plan {
                        BAR_QFULL = BAR_PV + 2, BAR_QFREE = BAR_QFULL + 2, BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + 2 * kUnitRing,
                        BARS = BAR_UFREE + 2 * kUnitRing;
   static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;               // [stream][kUnitRing]
-  static constexpr int SCAN_OFF = (UNIT_OFF + 2 * kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // int64 [12], then small words
-  static constexpr int TAG_OFF = SCAN_OFF + 12 * 8 + 8 * 4;
-  static constexpr int EX_OFF = SCAN_OFF + 12 * 8 + 112;                              // narrow: float2 [8][16]
+  static constexpr int SCAN_OFF = (UNIT_OFF + 2 * kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // int64 [24]
+  static constexpr int RUN_OFF = SCAN_OFF + 24 * 8;                                   // int64 [6], int [4]
+  static constexpr int TAG_OFF = RUN_OFF + 6 * 8 + 4 * 4;                             // int [16]
+  static constexpr int EX_OFF = TAG_OFF + 16 * 4;                                     // narrow: float2 [8][16]
   static constexpr int TOTAL = EX_OFF + 8 * kNarrowRows * 8;
   static constexpr int S_COL = 0, O_COL = 256, O_STEP = D;  // S: 128 columns a stream; O: D columns a stream
 };
@@ -129,7 +131,7 @@ __device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) {
 }
 // units of the request per KV head (n * group fits 32 bits: the host has checked)
 __device__ __forceinline__ int passes(const TreeAttnArgs& a, const Request& q) { return (q.n * a.group + kUnitRows - 1) / kUnitRows; }
-__device__ __forceinline__ long long tiles(const TreeAttnArgs& a, const Request& q) { return (long long)(a.hkv * passes(a, q)) * q.kt; }
+__device__ __forceinline__ long long units_of(const TreeAttnArgs& a, const Request& q) { return (long long)a.hkv * passes(a, q); }
 __device__ __forceinline__ long long divide(long long x, long long y) {       // both are small as a rule
   return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
@@ -567,11 +569,12 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   long long* scan = reinterpret_cast<long long*>(smem + P::SCAN_OFF);
-  int* words = reinterpret_cast<int*>(smem + P::SCAN_OFF + 12 * 8);
+  long long* start_rem = reinterpret_cast<long long*>(smem + P::RUN_OFF);      // [stream] steps of the request before the run
+  long long* tiles_at = start_rem + 2;             // [stream][2] tiles before the run's begin and end
+  int* words = reinterpret_cast<int*>(smem + P::RUN_OFF + 6 * 8);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(words);
   volatile int* abort_flag = words + 1;
-  int* start_b = words + 2;                        // [stream]
-  long long* start_rem = reinterpret_cast<long long*>(words + 4);   // [stream]
+  int* start_b = words + 2;                        // [stream] request in which the run begins
   // [stream][8]: number, from 1, of a unit in which a non-finite value was met, at that number modulo 8 (the streams of
   // wide units write each other's and are two units apart at most)
   volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
@@ -586,21 +589,23 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   // ---- where the runs begin
   const int per = (a.n_req + kThreads - 1) / kThreads;
   const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
-  long long mine = 0;
+  long long mine_t = 0, mine_u = 0;                // tiles, units
   bool many = false, some = false;
   for (int b = b_lo; b < b_hi; ++b) {
     const Request q = request(a, b);
-    mine += tiles(a, q);
+    const long long n = units_of(a, q);
+    mine_u += n;
+    mine_t += n * q.kt;
     many |= q.n * a.group > 128;
     some |= q.n * a.group > kNarrowRows;
   }
-  long long incl = mine;
+  long long incl_t = mine_t, incl_u = mine_u;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long up = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += up;
+    const long long up_t = __shfl_up_sync(0xffffffffu, incl_t, o), up_u = __shfl_up_sync(0xffffffffu, incl_u, o);
+    if (lane >= o) { incl_t += up_t; incl_u += up_u; }
   }
-  if (lane == 31) scan[warp] = incl;
+  if (lane == 31) { scan[warp] = incl_t; scan[12 + warp] = incl_u; }
   if (threadIdx.x == 0) {
     for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
     for (int x = 0; x < 2; ++x) {
@@ -618,22 +623,34 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   const bool wide = __syncthreads_or(many) != 0, narrow = __syncthreads_or(some) == 0;
   const bool by_cta = wide || narrow;              // a CTA is a worker
   if (warp == kIssuer && !narrow) tmem_alloc(smem_u32(tmem_slot), 512);
-  long long before = incl - mine, total = 0;
+  long long before_t = incl_t - mine_t, before_u = incl_u - mine_u, total_t = 0, total = 0;
+#pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) before += scan[w];
-    total += scan[w];
+    if (w < warp) { before_t += scan[w]; before_u += scan[12 + w]; }
+    total_t += scan[w];
+    total += scan[w] + scan[12 + w];
   }
   const int workers = by_cta ? n_cta : 2 * n_cta;
-  const long long quota = divide(total, workers), extra = total - quota * workers;      // the first `extra` runs are one tile longer
+  const long long quota = divide(total, workers), extra = total - quota * workers;      // the first `extra` runs are one step longer
   auto run_begin = [&](int w) { return w * quota + min((long long)w, extra); };
-  for (int x = 0; x < 2; ++x) {
-    const long long w0 = run_begin(by_cta ? cta : x * n_cta + cta);
-    if (before <= w0 && w0 < before + mine) {
-      long long at = before;
+  for (int i = 0; i < (by_cta ? 2 : 4); ++i) {
+    const int x = i >> 1, end = i & 1;
+    const long long w = run_begin((by_cta ? cta : x * n_cta + cta) + end);
+    long long step = before_t + before_u, tile = before_t;
+    if (w >= total) {
+      if (threadIdx.x == 0) tiles_at[i] = total_t;
+    } else if (step <= w && w < step + mine_t + mine_u) {
       for (int b = b_lo; b < b_hi; ++b) {
-        const long long t = tiles(a, request(a, b));
-        if (w0 < at + t) { start_b[x] = b; start_rem[x] = w0 - at; break; }
-        at += t;
+        const Request q = request(a, b);
+        const long long n = units_of(a, q);
+        if (w < step + n * (q.kt + 1)) {
+          const long long rem = w - step, nth = divide(rem, q.kt + 1), in = rem - nth * (q.kt + 1);
+          tiles_at[i] = tile + nth * q.kt + max(in - 1, 0ll);
+          if (!end) { start_b[x] = b; start_rem[x] = rem; }
+          break;
+        }
+        step += n * (q.kt + 1);
+        tile += n * q.kt;
       }
     }
   }
@@ -655,15 +672,14 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   const bool idle = __syncthreads_or(poisoned || misplaced) != 0;
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  // tiles of the streams' runs, and of the CTA; job i of a stream is job 2 i + x of the CTA (wide: its i-th tile)
+  // tiles of the streams' runs, and of the CTA.  Job j of the CTA is a tile of one stream, the streams in turn as long as both
+  // have some; wide: a tile of both.
   uint32_t n_run[2];
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const int w = by_cta ? cta : x * n_cta + cta;
-    n_run[x] = idle || (narrow && x == 1) ? 0u : (uint32_t)(run_begin(w + 1) - run_begin(w));
-  }
-  const uint32_t n_steps = wide ? n_run[0] : n_run[0] + n_run[1];
-  // ring positions of the K and V tiles of step j: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1); narrow: K0 V0 K1 V1 ...
+  for (int x = 0; x < 2; ++x) n_run[x] = idle || (narrow && x == 1) ? 0u : (uint32_t)(tiles_at[by_cta ? 1 : 2 * x + 1] - tiles_at[by_cta ? 0 : 2 * x]);
+  const uint32_t n_steps = wide ? n_run[0] : n_run[0] + n_run[1], in_turn = min(n_run[0], n_run[1]);
+  auto job_of = [&](int x, uint32_t i) { return wide ? i : i < in_turn ? 2 * i + x : in_turn + i; };
+  // ring positions of the K and V tiles of job j: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1); narrow: K0 V0 K1 V1 ...
   auto k_pos = [&](uint32_t j) { return j == 0 ? 0u : 2 * j - 1; };
   auto v_pos = [&](uint32_t j) { return j + 1 == n_steps ? 2 * j + 1 : 2 * j + 2; };
 
@@ -674,19 +690,23 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     int seq = 0;
     if (lane == 0) work.meta[x * n_cta + cta].last = -1;
     if (n_run[x] > 0) {
-      int b = start_b[x];
-      long long rem = start_rem[x], w = run_begin(me);
-      const long long w1 = w + n_run[x];
+      int b = start_b[by_cta ? 0 : x];
+      long long rem = start_rem[by_cta ? 0 : x], w = run_begin(me);
+      const long long w1 = run_begin(me + 1);
       Request q = request(a, b);
       while (w < w1 && ok) {
-        while (rem >= tiles(a, q) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
-        if (rem >= tiles(a, q)) break;               // not reached while the lengths stand still
+        while (rem >= units_of(a, q) * (q.kt + 1) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
+        if (rem >= units_of(a, q) * (q.kt + 1)) break;       // not reached while the lengths stand still
         Unit u;
-        const int n_pass = passes(a, q);
-        const int nth = (int)divide(rem, q.kt), all_rows = q.n * a.group;
-        u.kt0 = (int)(rem - (long long)nth * q.kt);
+        const int n_pass = passes(a, q), all_rows = q.n * a.group;
+        const int nth = (int)divide(rem, q.kt + 1), in = (int)(rem - (long long)nth * (q.kt + 1));       // step of the unit: tile `in - 1`
+        const int take = (int)min((long long)(q.kt + 1 - in), w1 - w);
+        w += take;
+        rem += take;
+        u.kt0 = max(in - 1, 0);
         u.kt_all = q.kt;
-        u.n_tiles = (int)min((long long)(q.kt - u.kt0), w1 - w);
+        u.n_tiles = in + take - 1 - u.kt0;
+        if (u.n_tiles == 0) continue;                // only the unit's own step: its tiles are the next worker's
         u.g = n_pass == 1 ? nth : nth / n_pass;
         u.b = b;
         u.start = q.start;
@@ -701,7 +721,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
           units[e] = u;
           mbar_arrive(bar(P::BAR_UNIT + e));
           if (u.kt0 == 0 && u.n_tiles < u.kt_all && !(wide && x == 1)) {
-            const long long z = w + u.kt_all - 1, cut = extra * (quota + 1);     // the unit's last tile
+            const long long z = w - take - in + u.kt_all, cut = extra * (quota + 1);     // the step of the unit's last tile
             Meta m{(int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota)), u.start, u.r0,
                    wide ? min(all_rows - u.r0, kUnitRows) : u.rows, u.g, wide, {0, 0}};
             work.meta[me] = m;
@@ -738,8 +758,6 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
           if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + set));
         }
         ++seq;
-        w += u.n_tiles;
-        rem += u.n_tiles;
       }
     }
     // no more units
@@ -809,7 +827,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       return tile;
     };
     for (uint32_t j = 0; j < n_steps && ok; ++j) {
-      const Tile now = by_cta || (j & 1) == 0 ? step(walk[0], 0) : step(walk[1], 1);
+      const Tile now = by_cta || (j < 2 * in_turn ? (j & 1) == 0 : n_run[0] > n_run[1]) ? step(walk[0], 0) : step(walk[1], 1);
       load(now, tm_k);
       if (narrow) load(now, tm_v);
       else if (j > 0) load(last, tm_v);
@@ -840,17 +858,16 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
         uint32_t k_at, k_slot, v_at, v_slot;         // ring positions of the next K and V tile
         bool first, q_here;                          // the next O opens a sum; the unit's Q has been seen
       } st[2];
-      const uint32_t stride = wide ? 2 : 4;          // between a stream's tiles in the ring
-      auto advance = [&](uint32_t& at, uint32_t& slot, uint32_t by) {
-        at += by;
-        slot += by;
+      auto advance = [&](uint32_t& at, uint32_t& slot, uint32_t to) {        // a stream's tiles are at most four apart
+        slot += to - at;
+        at = to;
         if (slot >= P::SLOTS) slot -= P::SLOTS;
       };
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         st[x].n_qk = st[x].n_pv = st[x].left = st[x].seq = 0;
         st[x].first = st[x].q_here = false;
-        const uint32_t j = wide ? 0 : x;
+        const uint32_t j = job_of(x, 0);
         st[x].k_at = k_pos(j); st[x].k_slot = st[x].k_at % P::SLOTS;
         st[x].v_at = v_pos(j); st[x].v_slot = st[x].v_at % P::SLOTS;
       }
@@ -881,8 +898,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
             mma_commit(bar(P::BAR_FREE + t.v_slot));
             ++t.n_pv;
             t.first = false;
-            // the last V of the CTA has no K ahead of it
-            advance(t.v_at, t.v_slot, (wide ? t.n_pv : 2 * t.n_pv + x) + 1 == n_steps ? stride - 1 : stride);
+            advance(t.v_at, t.v_slot, v_pos(job_of(x, t.n_pv)));
             moved = true;
           }
           if (t.n_qk == t.n_pv && t.n_qk != n_run[x]) {
@@ -909,7 +925,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
                 mma_commit(bar(P::BAR_FREE + t.k_slot));
                 if (--t.left == 0) mma_commit(bar(P::BAR_QFREE + x));
                 ++t.n_qk;
-                advance(t.k_at, t.k_slot, t.k_at == 0 ? stride - 1 : stride);      // the first K has no V ahead of the next
+                advance(t.k_at, t.k_slot, k_pos(job_of(x, t.n_qk)));
                 moved = true;
               }
             }
@@ -1025,7 +1041,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
           // Values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite).  V comes
           // after K, hence not before the softmax.  S of the tile was there, so every tile up to its K has arrived, the one
           // before V in V's slot among them: the barrier's parity can be told.
-          const uint32_t p = v_pos(wide ? n_jobs : 2 * n_jobs + x), s = p % P::SLOTS;
+          const uint32_t p = v_pos(job_of(x, n_jobs)), s = p % P::SLOTS;
           ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
           if (!ok) break;
           // each warp of the stream 32 keys

@@ -2,6 +2,8 @@
 // over a paged cache, cache compaction).  Nothing here is part of the C ABI.
 #pragma once
 
+#include <utility>
+
 #include "common.cuh"
 
 namespace sp {
@@ -20,6 +22,27 @@ __device__ __forceinline__ bool decode_poisoned(const int* status) {
 }
 __device__ __forceinline__ void report_range(int* status, int where) {
   if (atomicCAS(status, 0, (int)SP_ERR_RANGE) == 0) status[1] = where;
+}
+
+// The decode-side kernels take a few microseconds, of which a launch that waits for the kernel before it to drain is one
+// or more.  They are launched as programmatic dependents: a kernel may be brought onto the device while the one before it
+// still runs, does what needs no memory, and waits (wait_for_previous, in every CTA) until that one has ended and its
+// writes are visible.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... Params, typename... Args>
+cudaError_t launch_dependent(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
 
 struct PageTablesArgs {

@@ -38,6 +38,8 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const PageTa
   int32_t* take0 = sm + a.n_req + 1;        // [n_req + 1] first position in the free list, then the end
   __shared__ Sums warp_sum[kTableThreads / 32];
   __shared__ int s_failed, s_longest;
+  let_next_start();
+  wait_for_previous();
   if (decode_poisoned(a.status)) return;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -158,6 +160,8 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const PageTa
 constexpr int kKeepThreads = 128, kKeepRun = 8;
 
 __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const KeepArgs a) {
+  let_next_start();
+  wait_for_previous();
   if (decode_poisoned(a.status)) return;
   const int b = blockIdx.x;
   const int past = a.past[b];
@@ -209,14 +213,12 @@ cudaError_t launch_page_tables(const PageTablesArgs& a, cudaStream_t s) {
   const long long want = (items > a.n_free ? items : a.n_free) / kTableThreads;
   const int grid = (int)(want < 1 ? 1 : want > 148 ? 148 : want);
   const int smem = 2 * (a.n_req + 1) * (int)sizeof(int32_t);
-  page_tables_kernel<<<grid, kTableThreads, smem, s>>>(a);
-  return cudaGetLastError();
+  return launch_dependent(page_tables_kernel, dim3(grid), dim3(kTableThreads), smem, s, a);
 }
 
 cudaError_t launch_cache_keep(const KeepArgs& a, cudaStream_t s) {
   const int columns = 2 * a.hkv * a.d / 8;
-  cache_keep_kernel<<<dim3(a.n_req, (columns + kKeepThreads - 1) / kKeepThreads), kKeepThreads, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch_dependent(cache_keep_kernel, dim3(a.n_req, (columns + kKeepThreads - 1) / kKeepThreads), dim3(kKeepThreads), 0, s, a);
 }
 
 }  // namespace sp

@@ -43,6 +43,8 @@ template <int D>
 __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int LPH = D / 16;      // lanes per head
   constexpr int HPW = 32 / LPH;    // heads per pass of a warp
+  let_next_start();
+  wait_for_previous();
   if (decode_poisoned(a.status)) return;
   const int lane = threadIdx.x & 31;
   const long long unit = (long long)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
@@ -173,9 +175,7 @@ cudaError_t launch_qk_norm_rope(RopeArgs& a, cudaStream_t s) {
   a.splits = (int)(splits > passes ? passes : splits);
   const long long warps = (long long)a.tokens * a.splits;
   const unsigned grid = (unsigned)((warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32));
-  if (a.d == 128) qk_norm_rope_kernel<128><<<grid, kRopeThreads, 0, s>>>(a);
-  else qk_norm_rope_kernel<64><<<grid, kRopeThreads, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch_dependent(a.d == 128 ? qk_norm_rope_kernel<128> : qk_norm_rope_kernel<64>, dim3(grid), dim3(kRopeThreads), 0, s, a);
 }
 
 }  // namespace sp

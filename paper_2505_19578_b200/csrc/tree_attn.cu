@@ -582,9 +582,21 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   const int cta = blockIdx.x, n_cta = gridDim.x;
   const Abort ab{abort_flag, a.status};
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const bool poisoned = decode_poisoned(a.status);
+  let_next_start();
   const bool misplaced = (base & 1023u) != 0;      // the tiles' swizzle needs the window's alignment
+  if (warp == kProducer && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(bar(P::BAR_S + x), 1);
+      mbar_init(bar(P::BAR_P + x), 4);
+      mbar_init(bar(P::BAR_PV + x), 1);
+    }
+    *abort_flag = 0;
+    for (int i = 0; i < 16; ++i) bad_tag[i] = 0;
+  }
+  wait_for_previous();
+  const bool poisoned = decode_poisoned(a.status);
 
   // ---- where the runs begin
   const int per = (a.n_req + kThreads - 1) / kThreads;
@@ -606,23 +618,15 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     if (lane >= o) { incl_t += up_t; incl_u += up_u; }
   }
   if (lane == 31) { scan[warp] = incl_t; scan[12 + warp] = incl_u; }
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(bar(P::BAR_S + x), 1);
-      mbar_init(bar(P::BAR_P + x), 4);
-      mbar_init(bar(P::BAR_PV + x), 1);
-    }
-    *abort_flag = 0;
-    for (int i = 0; i < 16; ++i) bad_tag[i] = 0;
-    if (misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
-  }
-  // rows of the Q area that no unit fills stay zero: products of whatever lay there would cost power, and with it clock
-  for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
-  fence_async_smem();
+  if (threadIdx.x == 0 && misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
   const bool wide = __syncthreads_or(many) != 0, narrow = __syncthreads_or(some) == 0;
   const bool by_cta = wide || narrow;              // a CTA is a worker
-  if (warp == kIssuer && !narrow) tmem_alloc(smem_u32(tmem_slot), 512);
+  if (!narrow) {
+    if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
+    // rows of the Q area that no unit fills stay zero: products of whatever lay there would cost power, and with it clock
+    for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+    fence_async_smem();
+  }
   long long before_t = incl_t - mine_t, before_u = incl_u - mine_u, total_t = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
@@ -769,7 +773,6 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     }
   } else if (warp == kProducer) {
     // ------------------------------------------------------------ K and V tiles
-    if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
     bool ok = true;
     const uint32_t ring = base + (narrow ? P::NRING_OFF : P::RING_OFF), slots = narrow ? P::NSLOTS : P::SLOTS;
     uint32_t s = 0, lap = 0;                         // next slot of the ring, times round
@@ -1092,7 +1095,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_j
   constexpr int E = D / 32;
   __shared__ float s_m[kJoinWarps], s_l[kJoinWarps], s_o[kJoinWarps][D];
   __shared__ int s_sum[kJoinWarps], s_owner, s_first;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  let_next_start();
+  wait_for_previous();
   if (decode_poisoned(a.status)) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // rows of the unit that begins in worker i and goes on in later ones; thread t looks after workers per * t ...
@@ -1230,19 +1234,9 @@ cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
   static_assert(smem <= 232448, "");
   cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  tree_attn_kernel<D><<<n_cta, kThreads, smem, s>>>(a, w, tk, tv);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  // started early, it waits for the first kernel's end on the device
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_cta * kJoinBlocksPerSm);
-  cfg.blockDim = dim3(kJoinWarps * 32);
-  cfg.stream = s;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, tree_attn_join_kernel<D>, a, w, n_cta);
+  e = launch_dependent(tree_attn_kernel<D>, dim3(n_cta), dim3(kThreads), smem, s, a, w, tk, tv);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(tree_attn_join_kernel<D>, dim3(n_cta * kJoinBlocksPerSm), dim3(kJoinWarps * 32), 0, s, a, w, n_cta);
 }
 
 }  // namespace

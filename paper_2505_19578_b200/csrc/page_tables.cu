@@ -32,7 +32,7 @@ __device__ __forceinline__ int last_not_above(const int32_t* start, int n, int x
   return lo;
 }
 
-__global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const PageTablesArgs a) {
+__global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const __grid_constant__ PageTablesArgs a) {
   extern __shared__ int32_t sm[];
   int32_t* row0 = sm;                       // [n_req + 1] first row of each request, then the end
   int32_t* take0 = sm + a.n_req + 1;        // [n_req + 1] first position in the free list, then the end
@@ -155,11 +155,13 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(const PageTa
 
 // cache_keep_kernel: kept[b][0] < kept[b][1] < ... are the accepted tokens of request b among its new ones; the key and
 // value at past_b + kept[b][i] move to past_b + i.  In place: a thread owns 16 bytes of every token of one head, and
-// kept[b][i] >= i, so a destination is never a source that is still to be read.  Eight loads are in flight before the
-// first store (a run of them may overlap its own destinations, hence loads first).
-constexpr int kKeepThreads = 128, kKeepRun = 8;
+// kept[b][i] >= i, so a destination is never a source that is still to be read.  All latency: the places of up to 64 moves
+// are looked up by as many threads at once, then a thread has 16 loads in flight before its first store (a run of them
+// may overlap its own destinations, hence loads first).
+constexpr int kKeepThreads = 128, kKeepRun = 16, kKeepChunk = 64;
 
-__global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const KeepArgs a) {
+__global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const __grid_constant__ KeepArgs a) {
+  __shared__ int2 s_from[kKeepChunk], s_to[kKeepChunk];      // page, token in the page; page < 0: nothing to move
   let_next_start();
   wait_for_previous();
   if (decode_poisoned(a.status)) return;
@@ -169,41 +171,53 @@ __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const KeepArgs
   if (blockIdx.y == 0 && threadIdx.x == 0) a.lens_out[b] = past + n;
   const int pieces = a.d / 8;
   const int x = blockIdx.y * kKeepThreads + threadIdx.x;
-  if (x >= 2 * a.hkv * pieces) return;
+  const bool mine = x < 2 * a.hkv * pieces;
   const int piece = x % pieces, head = (x / pieces) % a.hkv;
   const PagedCache& c = x < a.hkv * pieces ? a.kc : a.vc;
   __nv_bfloat16* base = c.data + head * c.s_head + piece * 8;
   const int32_t* row = a.table + (size_t)b * a.max_pages;
-  bool bad = false;
-  auto place = [&](long long p) -> uint4* {          // null: not a place of this request's pages
+  auto place = [&](long long p) -> int2 {            // page -1: not a place of this request's pages
     const long long col = p >> a.page_log2;
-    if (p < 0 || col >= a.max_pages) { bad = true; return nullptr; }
-    const int id = row[col];
-    if (id < 0 || id >= a.n_pages) { bad = true; return nullptr; }
-    return reinterpret_cast<uint4*>(base + id * c.s_page + (p & ((1 << a.page_log2) - 1)) * c.s_tok);
+    int id = -1;
+    if (p >= 0 && col < a.max_pages) id = row[col];
+    if (id >= a.n_pages) id = -1;
+    return make_int2(max(id, -1), (int)(p & ((1 << a.page_log2) - 1)));
   };
-  for (int i0 = 0; i0 < n; i0 += kKeepRun) {
-    uint4 val[kKeepRun];
-    bool have[kKeepRun];
+  for (int i0 = 0; i0 < n; i0 += kKeepChunk) {
+    const int i = i0 + threadIdx.x;
+    if (i0 > 0) __syncthreads();
+    if (threadIdx.x < kKeepChunk && i < n) {
+      const int kept = a.kept[(size_t)b * a.max_kept + i];
+      int2 from = place((long long)past + kept), to = place((long long)past + i);
+      if (kept < 0 || from.x < 0 || to.x < 0) {
+        if (kept != i) report_range(a.status, kWhereKeepPage);
+        from.x = -1;
+      }
+      if (kept == i) from.x = -1;
+      s_from[threadIdx.x] = from;
+      s_to[threadIdx.x] = to;
+    }
+    __syncthreads();
+    if (!mine) continue;
+    const int here = min(kKeepChunk, n - i0);
+    for (int j0 = 0; j0 < here; j0 += kKeepRun) {
+      uint4 val[kKeepRun];
 #pragma unroll
-    for (int u = 0; u < kKeepRun; ++u) {
-      have[u] = false;
-      if (i0 + u < n) {
-        const int from = a.kept[(size_t)b * a.max_kept + i0 + u];
-        if (from != i0 + u) {
-          const uint4* src = from < 0 ? (bad = true, nullptr) : place((long long)past + from);
-          if (src) { val[u] = *src; have[u] = true; }
+      for (int u = 0; u < kKeepRun; ++u) {
+        val[u] = make_uint4(0, 0, 0, 0);
+        if (j0 + u < here) {
+          const int2 from = s_from[j0 + u];
+          if (from.x >= 0) val[u] = *reinterpret_cast<const uint4*>(base + from.x * c.s_page + from.y * c.s_tok);
         }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < kKeepRun; ++u)
-      if (have[u]) {
-        uint4* dst = place((long long)past + i0 + u);
-        if (dst) *dst = val[u];
-      }
+      for (int u = 0; u < kKeepRun; ++u)
+        if (j0 + u < here && s_from[j0 + u].x >= 0) {
+          const int2 to = s_to[j0 + u];
+          *reinterpret_cast<uint4*>(base + to.x * c.s_page + to.y * c.s_tok) = val[u];
+        }
+    }
   }
-  if (bad) report_range(a.status, kWhereKeepPage);
 }
 
 }  // namespace

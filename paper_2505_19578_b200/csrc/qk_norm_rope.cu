@@ -7,8 +7,8 @@
 //
 // Bound by memory: every element is read once and written once per destination.  A head is held by D / 16 lanes, each
 // with two 8-element pieces chosen so that both members of every rotated pair sit in one lane: nothing is exchanged but
-// the sum of squares.  The sine and cosine of a token's pairs are computed once per warp and serve all the heads that
-// the warp walks.
+// the sum of squares.  The sines and cosines of a token's pairs are computed by the warp's lanes, two pairs each, handed
+// round by shuffles and used for all the heads that the warp walks.
 //
 // Angles: the turns per position of each pair are a 64-bit fraction of a turn, so that position * frequency modulo one
 // turn is one wrapping integer product, exact at any position; its top 32 bits (2^-33 of a turn off at most) go to
@@ -17,9 +17,6 @@
 
 namespace sp {
 namespace {
-
-constexpr int kRopeThreads = 128;
-constexpr int kRopeRun = 4;        // passes whose loads are in flight together
 
 __device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -39,143 +36,270 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// A pass of a warp: 32 / (D / 16) heads of one token, this lane two pieces of one of them.
+struct Pass {
+  int kind, head;                  // 0 q, 1 k, 2 v, -1 nothing for this lane
+};
+template <int D>
+struct Lane {
+  static constexpr int LPH = D / 16, HPW = 32 / LPH;      // lanes per head, heads per pass
+  int l, hw, c0, c1;               // lane in the head, head in the pass, the two pieces
+  int from0, from1;
+  bool turn0, turn1;               // which of the pieces turn
+  __device__ __forceinline__ Lane(const RopeArgs& a, int lane) {
+    l = lane % LPH;
+    hw = lane / LPH;
+    // neighbouring lanes have neighbouring pieces: 2 l, 2 l + 1 would read and write every 32-byte sector twice
+    const int turning = a.rot / 16;                // half: the first `turning` lanes have pairs (piece l, piece l + turning)
+    const bool rest = !a.interleaved && l >= turning;
+    c0 = rest ? l + turning : l;
+    c1 = a.interleaved || rest ? l + LPH : l + turning;
+    turn0 = a.interleaved ? c0 < 2 * turning : !rest;
+    turn1 = a.interleaved ? c1 < 2 * turning : !rest;
+    // the pairs of the lane's angles 0-3 and 4-7, four at a time: pair 4 i + e was computed by lane 2 i + e / 2
+    from0 = 2 * (a.interleaved ? c0 : 2 * l);
+    from1 = 2 * (a.interleaved ? c1 : 2 * l + 1);
+  }
+  __device__ __forceinline__ Pass pass(const RopeArgs& a, int p) const {
+    const int pq = (a.hq + HPW - 1) / HPW, pkv = (a.hkv + HPW - 1) / HPW;
+    const int kind = p < pq ? 0 : p < pq + pkv ? 1 : 2;
+    const int head = (p - (kind == 0 ? 0 : kind == 1 ? pq : pq + pkv)) * HPW + hw;
+    return {p < pq + 2 * pkv && head < (kind == 0 ? a.hq : a.hkv) ? kind : -1, head};
+  }
+  __device__ __forceinline__ const __nv_bfloat16* source(const RopeArgs& a, const Pass& p, int t) const {
+    return p.kind == 0 ? a.q + p.head * a.q_sh + t * a.q_sn : p.kind == 1 ? a.k + p.head * a.k_sh + t * a.k_sn : a.v + p.head * a.v_sh + t * a.v_sn;
+  }
+};
+
+// Turns per position of the two pairs whose sine and cosine this lane computes (pairs 2 lane, 2 lane + 1).
+__device__ __forceinline__ void lane_phases(const RopeArgs& a, int lane, uint64_t (&f)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) f[i] = 2 * lane + i < a.rot / 2 ? a.phase[2 * lane + i] : 0;
+}
+// Cosine and sine of the eight pairs of this lane's pieces (1 and 0 where nothing turns).  Whole warps.
+template <int D>
+__device__ __forceinline__ void angles(const uint64_t (&f)[2], int pos, const Lane<D>& ln, float (&cs)[8], float (&sn)[8]) {
+  float c[2], s[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint64_t turns = f[i] * (uint64_t)(int64_t)pos;                      // modulo one turn
+    sincospif((float)(int32_t)(uint32_t)(turns >> 32) * 4.656612873077393e-10f /* 2^-31: half turns */, &s[i], &c[i]);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int from = ((e < 4 ? ln.from0 : ln.from1) + ((e & 3) >> 1)) & 31;
+    const float ce = __shfl_sync(0xffffffffu, c[e & 1], from), se = __shfl_sync(0xffffffffu, s[e & 1], from);
+    const bool turn = e < 4 ? ln.turn0 : ln.turn1;
+    cs[e] = turn ? ce : 1.f;
+    sn[e] = turn ? se : 0.f;
+  }
+}
+
+// Norm and rotation of one pass (q and k; v goes through as it is) and its stores.  Whole warps.
+template <int D>
+__device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln, const Pass& p, bool is_v, bool is_q, int t, int slot, uint4 in0, uint4 in1,
+                                            const float (&cs)[8], const float (&sn)[8]) {
+  if (!is_v) {                                     // uniform over the warp
+    float x[8], y[8];
+    unpack8(in0, x);
+    unpack8(in1, y);
+    const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
+    if (weight) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += x[e] * x[e] + y[e] * y[e];
+#pragma unroll
+      for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      const float inv = 1.f / sqrtf(ss * (1.f / D) + a.eps);
+      float wx[8], wy[8];
+      unpack8(__ldg(reinterpret_cast<const uint4*>(weight + ln.c0 * 8)), wx);
+      unpack8(__ldg(reinterpret_cast<const uint4*>(weight + ln.c1 * 8)), wy);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { x[e] *= inv * wx[e]; y[e] *= inv * wy[e]; }
+    }
+    if (ln.turn0 || ln.turn1) {
+      if (a.interleaved) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const float xa = x[e], xb = x[e + 1], ya = y[e], yb = y[e + 1];
+          const int i = e / 2, j = 4 + e / 2;
+          x[e] = xa * cs[i] - xb * sn[i];
+          x[e + 1] = xb * cs[i] + xa * sn[i];
+          y[e] = ya * cs[j] - yb * sn[j];
+          y[e + 1] = yb * cs[j] + ya * sn[j];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float xa = x[e], xb = y[e];
+          x[e] = xa * cs[e] - xb * sn[e];
+          y[e] = xb * cs[e] + xa * sn[e];
+        }
+      }
+    }
+    in0 = pack8(x);
+    in1 = pack8(y);
+  }
+  if (p.kind < 0) return;
+  auto put = [&](__nv_bfloat16* dst) {
+    *reinterpret_cast<uint4*>(dst + ln.c0 * 8) = in0;
+    *reinterpret_cast<uint4*>(dst + ln.c1 * 8) = in1;
+  };
+  if (p.kind == 0) {
+    put(a.q_out + p.head * a.qo_sh + t * a.qo_sn);
+    return;
+  }
+  const bool k = p.kind == 1;
+  if (k ? a.k_out != nullptr : a.v_out != nullptr) put(k ? a.k_out + p.head * a.ko_sh + t * a.ko_sn : a.v_out + p.head * a.vo_sh + t * a.vo_sn);
+  if (slot >= 0 && slot < a.n_slots) {             // a negative slot: a row that no request owns
+    const PagedCache& c = k ? a.kc : a.vc;
+    put(c.data + (int64_t)(slot >> a.page_log2) * c.s_page + (slot & ((1 << a.page_log2) - 1)) * c.s_tok + p.head * c.s_head);
+  }
+}
+
+// Few rows: as many warps per token as fill the device, each its share of the token's passes.
+constexpr int kRopeThreads = 128;
+
 template <int D>
 __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const __grid_constant__ RopeArgs a) {
-  constexpr int LPH = D / 16;      // lanes per head
-  constexpr int HPW = 32 / LPH;    // heads per pass of a warp
+  constexpr int RUN = 2;                           // passes whose loads are in flight together
+  const int lane = threadIdx.x & 31;
+  const long long unit = (long long)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
+  const int t = (int)(unit / a.splits), split = (int)(unit - (long long)t * a.splits);
+  const Lane<D> ln(a, lane);
+  uint64_t f[2];
+  lane_phases(a, lane, f);
+  let_next_start();
+  wait_for_previous();
+  if (decode_poisoned(a.status) || t >= a.tokens) return;
+  const int pq = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW, pkv = (a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW, passes = pq + 2 * pkv;
+  const int pos = a.positions[t], slot = a.kc.data ? a.slots[t] : -1;
+  if (slot >= a.n_slots && a.kc.data && lane == 0) report_range(a.status, kWhereRopeSlot);
+  float cs[8], sn[8];
+  bool have = false;
+  for (int p0 = split; p0 < passes; p0 += RUN * a.splits) {
+    uint4 in0[RUN], in1[RUN];
+    Pass pass[RUN];
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      pass[u] = ln.pass(a, p0 + u * a.splits);
+      in0[u] = in1[u] = make_uint4(0, 0, 0, 0);
+      if (pass[u].kind >= 0) {
+        const __nv_bfloat16* src = ln.source(a, pass[u], t);
+        in0[u] = __ldcs(reinterpret_cast<const uint4*>(src + ln.c0 * 8));
+        in1[u] = __ldcs(reinterpret_cast<const uint4*>(src + ln.c1 * 8));
+      }
+    }
+    if (!have) {                                   // with the first loads under way
+      angles<D>(f, pos, ln, cs, sn);
+      have = true;
+    }
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      const int p = p0 + u * a.splits;
+      if (p < passes) finish_pass<D>(a, ln, pass[u], p >= pq + pkv, p < pq, t, slot, in0[u], in1[u], cs, sn);
+    }
+  }
+}
+
+// Many rows: one CTA per SM, each warp an equal run of (token, three passes) items, which it fetches three items ahead into
+// a ring of its own in shared memory (cp.async; a lane reads back only what it has copied, so nothing is synchronised).
+// 16 warps have 144 KB under way then, which registers could not hold.  Four passes, two items ahead: 2 % faster for
+// 131072 rows of 48 heads, 7 % slower for 1000 rows of 36, whose 9 passes do not divide.
+constexpr int kStreamWarps = 16, kStreamStages = 4, kStreamRun = 3;
+constexpr int kStreamItem = kStreamRun * 1024 + 32;        // bytes of an item: 32 lanes x two pieces a pass, position and slot
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
+
+template <int D>
+__global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kernel(const __grid_constant__ RopeArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Lane<D> ln(a, lane);
+  uint64_t f[2];
+  lane_phases(a, lane, f);
+  const int pq = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW, pkv = (a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW, passes = pq + 2 * pkv;
+  const int per_token = (passes + kStreamRun - 1) / kStreamRun;
+  const long long items = (long long)a.tokens * per_token, n_warps = (long long)gridDim.x * kStreamWarps, me = (long long)blockIdx.x * kStreamWarps + warp;
+  const long long from = items * me / n_warps, to = items * (me + 1) / n_warps;
+  uint8_t* mine = smem + warp * kStreamStages * kStreamItem;
+  const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
   let_next_start();
   wait_for_previous();
   if (decode_poisoned(a.status)) return;
-  const int lane = threadIdx.x & 31;
-  const long long unit = (long long)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
-  if (unit >= (long long)a.tokens * a.splits) return;
-  const int t = (int)(unit / a.splits), split = (int)(unit - (long long)t * a.splits);
-  const int l = lane % LPH, hw = lane / LPH;
 
-  // this lane's two pieces and the first of their pairs
-  const int turning = a.rot / 16;                // lanes of a head whose pieces turn
-  const bool turn = l < turning;
-  const int c0 = (a.interleaved || !turn) ? 2 * l : l;
-  const int c1 = (a.interleaved || !turn) ? 2 * l + 1 : l + turning;
+  int ft = (int)(from / per_token), fb = (int)(from - (long long)ft * per_token), fstage = 0;       // the item to fetch next
+  long long fetched = from;
+  auto fetch = [&] {
+    if (fetched < to) {
+      const uint32_t at = mine_at + fstage * kStreamItem;
+#pragma unroll
+      for (int u = 0; u < kStreamRun; ++u) {
+        const Pass p = ln.pass(a, fb * kStreamRun + u);
+        if (p.kind >= 0) {
+          const __nv_bfloat16* src = ln.source(a, p, ft);
+          copy16(at + u * 1024 + lane * 16, src + ln.c0 * 8);
+          copy16(at + u * 1024 + 512 + lane * 16, src + ln.c1 * 8);
+        }
+      }
+      if (lane == 0) copy4(at + kStreamRun * 1024, a.positions + ft);
+      if (lane == 1 && a.kc.data) copy4(at + kStreamRun * 1024 + 4, a.slots + ft);
+      ++fetched;
+      if (++fb == per_token) { fb = 0; ++ft; }
+      if (++fstage == kStreamStages) fstage = 0;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");       // an empty one at the end keeps the count
+  };
+#pragma unroll
+  for (int i = 0; i + 1 < kStreamStages; ++i) fetch();
+  int t = (int)(from / per_token), b = (int)(from - (long long)t * per_token), stage = 0, angle_of = -1;
   float cs[8], sn[8];
-  const int pos = a.positions[t];
+  for (long long item = from; item < to; ++item) {
+    fetch();
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStreamStages - 1) : "memory");
+    __syncwarp();                                  // position and slot were copied by lanes 0 and 1
+    const uint8_t* at = mine + stage * kStreamItem;
+    const int pos = *reinterpret_cast<const int*>(at + kStreamRun * 1024);
+    const int slot = a.kc.data ? *reinterpret_cast<const int*>(at + kStreamRun * 1024 + 4) : -1;
+    if (angle_of != t) {
+      angles<D>(f, pos, ln, cs, sn);
+      angle_of = t;
+      if (slot >= a.n_slots && a.kc.data && lane == 0) report_range(a.status, kWhereRopeSlot);
+    }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    cs[e] = 1.f;
-    sn[e] = 0.f;
-    if (turn) {
-      const uint64_t turns = a.phase[8 * l + e] * (uint64_t)(int64_t)pos;      // modulo one turn
-      sincospif((float)(int32_t)(uint32_t)(turns >> 32) * 4.656612873077393e-10f /* 2^-31: half turns */, &sn[e], &cs[e]);
+    for (int u = 0; u < kStreamRun; ++u) {
+      const int p = b * kStreamRun + u;
+      if (p < passes)
+        finish_pass<D>(a, ln, ln.pass(a, p), p >= pq + pkv, p < pq, t, slot, *reinterpret_cast<const uint4*>(at + u * 1024 + lane * 16),
+                       *reinterpret_cast<const uint4*>(at + u * 1024 + 512 + lane * 16), cs, sn);
     }
+    __syncwarp();                                  // all have read position and slot before the stage is filled again
+    if (++b == per_token) { b = 0; ++t; }
+    if (++stage == kStreamStages) stage = 0;
   }
-  int64_t cache_off_k = -1, cache_off_v = -1;
-  if (a.kc.data) {
-    const int slot = a.slots[t];
-    if (slot >= a.n_slots) {
-      report_range(a.status, kWhereRopeSlot);
-    } else if (slot >= 0) {                      // a negative slot: a row that no request owns
-      const int64_t page = slot >> a.page_log2, off = slot & ((1 << a.page_log2) - 1);
-      cache_off_k = page * a.kc.s_page + off * a.kc.s_tok;
-      cache_off_v = page * a.vc.s_page + off * a.vc.s_tok;
-    }
-  }
+}
 
-  const int pq = (a.hq + HPW - 1) / HPW, pkv = (a.hkv + HPW - 1) / HPW;
-  const int passes = pq + 2 * pkv;
-  for (int p0 = split; p0 < passes; p0 += kRopeRun * a.splits) {
-    uint4 in0[kRopeRun], in1[kRopeRun];
-    int kind[kRopeRun], head[kRopeRun];          // 0 q, 1 k, 2 v, -1 nothing
-#pragma unroll
-    for (int u = 0; u < kRopeRun; ++u) {
-      const int p = p0 + u * a.splits;
-      kind[u] = p < pq ? 0 : p < pq + pkv ? 1 : 2;
-      head[u] = (p - (kind[u] == 0 ? 0 : kind[u] == 1 ? pq : pq + pkv)) * HPW + hw;
-      if (p >= passes || head[u] >= (kind[u] == 0 ? a.hq : a.hkv)) kind[u] = -1;
-      in0[u] = in1[u] = make_uint4(0, 0, 0, 0);
-      if (kind[u] >= 0) {
-        const __nv_bfloat16* src = kind[u] == 0 ? a.q + head[u] * a.q_sh + t * a.q_sn
-                                 : kind[u] == 1 ? a.k + head[u] * a.k_sh + t * a.k_sn
-                                                : a.v + head[u] * a.v_sh + t * a.v_sn;
-        in0[u] = __ldcs(reinterpret_cast<const uint4*>(src + c0 * 8));
-        in1[u] = __ldcs(reinterpret_cast<const uint4*>(src + c1 * 8));
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kRopeRun; ++u) {
-      const int p = p0 + u * a.splits;
-      if (p >= passes) break;                    // uniform over the warp
-      if (p < pq + pkv) {
-        float x[8], y[8];
-        unpack8(in0[u], x);
-        unpack8(in1[u], y);
-        const __nv_bfloat16* weight = p < pq ? a.q_weight : a.k_weight;
-        if (weight) {
-          float ss = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss += x[e] * x[e] + y[e] * y[e];
-#pragma unroll
-          for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const float inv = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-          float wx[8], wy[8];
-          unpack8(__ldg(reinterpret_cast<const uint4*>(weight + c0 * 8)), wx);
-          unpack8(__ldg(reinterpret_cast<const uint4*>(weight + c1 * 8)), wy);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { x[e] *= inv * wx[e]; y[e] *= inv * wy[e]; }
-        }
-        if (turn) {
-          if (a.interleaved) {
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              const float xa = x[e], xb = x[e + 1], ya = y[e], yb = y[e + 1];
-              const int i = e / 2, j = 4 + e / 2;
-              x[e] = xa * cs[i] - xb * sn[i];
-              x[e + 1] = xb * cs[i] + xa * sn[i];
-              y[e] = ya * cs[j] - yb * sn[j];
-              y[e + 1] = yb * cs[j] + ya * sn[j];
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float xa = x[e], xb = y[e];
-              x[e] = xa * cs[e] - xb * sn[e];
-              y[e] = xb * cs[e] + xa * sn[e];
-            }
-          }
-        }
-        in0[u] = pack8(x);
-        in1[u] = pack8(y);
-      }
-      if (kind[u] < 0) continue;
-      auto put = [&](__nv_bfloat16* dst) {
-        *reinterpret_cast<uint4*>(dst + c0 * 8) = in0[u];
-        *reinterpret_cast<uint4*>(dst + c1 * 8) = in1[u];
-      };
-      if (kind[u] == 0) {
-        put(a.q_out + head[u] * a.qo_sh + t * a.qo_sn);
-      } else if (kind[u] == 1) {
-        if (a.k_out) put(a.k_out + head[u] * a.ko_sh + t * a.ko_sn);
-        if (cache_off_k >= 0) put(a.kc.data + cache_off_k + head[u] * a.kc.s_head);
-      } else {
-        if (a.v_out) put(a.v_out + head[u] * a.vo_sh + t * a.vo_sn);
-        if (cache_off_v >= 0) put(a.vc.data + cache_off_v + head[u] * a.vc.s_head);
-      }
-    }
+template <int D>
+cudaError_t launch(RopeArgs& a, cudaStream_t s) {
+  // From an item for each of the device's warps on, the streaming kernel (131072 rows of 48 heads, head-major and cached:
+  // 666 us against 723 us with the other one; 1000 rows of 36: 8.9 against 9.4).
+  const int passes = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW + 2 * ((a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW);
+  const long long items = (long long)a.tokens * ((passes + kStreamRun - 1) / kStreamRun);
+  if (items >= 148 * kStreamWarps) {
+    constexpr int smem = kStreamWarps * kStreamStages * kStreamItem;
+    const cudaError_t e = cudaFuncSetAttribute(qk_norm_rope_stream_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(qk_norm_rope_stream_kernel<D>, dim3(148), dim3(kStreamWarps * 32), smem, s, a);
   }
+  const long long splits = (148ll * 32 + a.tokens - 1) / a.tokens;             // warps to fill the device
+  a.splits = (int)(splits > passes ? passes : splits);
+  const long long warps = (long long)a.tokens * a.splits;
+  return launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)((warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32))), dim3(kRopeThreads), 0, s, a);
 }
 
 }  // namespace
 
-cudaError_t launch_qk_norm_rope(RopeArgs& a, cudaStream_t s) {
-  // A warp walks all the heads of a token once there are tokens enough to fill the device (the sines are then computed
-  // once per token); with few tokens the heads of a token are spread over as many warps as there are passes.
-  const int hpw = 32 / (a.d / 16);
-  const int passes = (a.hq + hpw - 1) / hpw + 2 * ((a.hkv + hpw - 1) / hpw);
-  const long long full = 148ll * 32;             // warps
-  long long splits = (full + a.tokens - 1) / a.tokens;
-  a.splits = (int)(splits > passes ? passes : splits);
-  const long long warps = (long long)a.tokens * a.splits;
-  const unsigned grid = (unsigned)((warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32));
-  return launch_dependent(a.d == 128 ? qk_norm_rope_kernel<128> : qk_norm_rope_kernel<64>, dim3(grid), dim3(kRopeThreads), 0, s, a);
-}
+cudaError_t launch_qk_norm_rope(RopeArgs& a, cudaStream_t s) { return a.d == 128 ? launch<128>(a, s) : launch<64>(a, s); }
 
 }  // namespace sp

@@ -454,6 +454,9 @@ int sp_prefill_attn_layer(sp_ctx* ctx, sp_pattern_dict* dict, const sp_tensor* q
  *     [n_kv_heads, seq, head_dim] tensor is a cache too (strides page * head_dim,
  *     seq * head_dim, head_dim; table 0, 1, 2, ...).  Slot s is token s % page of
  *     page s / page; pages * page must fit 31 bits (element offsets are 64-bit).
+ *     sp_tree_attn: the strides of pages and heads, in units of their greatest common
+ *     divisor, must place the last head of the last page below 2^31 (else
+ *     SP_ERR_UNSUPPORTED; no cache whose strides are multiples of head_dim comes near).
  *   - block_table: device i32 [n_req, max_pages]; token p of request b lies on page
  *     block_table[b][p / page].  Entries behind a request's last page are not read.
  *   - Any number of rows >= 1, any lengths (0 included); n_req <= 4096 (0: nothing

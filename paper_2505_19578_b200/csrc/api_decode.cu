@@ -168,6 +168,8 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
   if (q->shape[2] * (q->shape[1] / c.hkv) > INT32_MAX) return SP_ERR_UNSUPPORTED;
   if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
   if (tree_mask && (mask_words < 1 || mask_words > kMaxMaskWords)) return SP_ERR_UNSUPPORTED;
+  CacheSteps steps;
+  if (!cache_steps(cache_of(k_cache), c.hkv, c.pages, &steps) || !cache_steps(cache_of(v_cache), c.hkv, c.pages, &steps)) return SP_ERR_UNSUPPORTED;
   if (n_req == 0) return SP_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;

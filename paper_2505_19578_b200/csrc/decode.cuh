@@ -66,6 +66,25 @@ struct PagedCache {            // one cache tensor [pages, heads, page, d]; stri
   int64_t s_page, s_head, s_tok;
 };
 
+// Heads and pages as one dimension of a tensor map, in steps of `unit` elements (their strides' greatest common divisor):
+// head h of page p is its element p * page + h * head.  False: more than 2^31 - 1 of them.
+struct CacheSteps {
+  int page, head, extent;
+  int64_t unit;
+};
+inline bool cache_steps(const PagedCache& c, int heads, int pages, CacheSteps* s) {
+  const int64_t sp = pages > 1 ? c.s_page : 0, sh = heads > 1 ? c.s_head : 0;       // never stepped: any stride
+  int64_t a = sp, b = sh;
+  while (b != 0) { const int64_t r = a % b; a = b; b = r; }
+  s->unit = a != 0 ? a : 64;
+  const int64_t page = sp / s->unit, head = sh / s->unit;
+  if (page > INT32_MAX / (pages > 1 ? pages - 1 : 1) || head > INT32_MAX / (heads > 1 ? heads - 1 : 1)) return false;
+  const int64_t extent = page * (pages - 1) + head * (heads - 1) + 1;
+  if (extent > INT32_MAX) return false;
+  s->page = (int)page; s->head = (int)head; s->extent = (int)extent;
+  return true;
+}
+
 struct RopeArgs {
   const __nv_bfloat16* q;
   const __nv_bfloat16* k;

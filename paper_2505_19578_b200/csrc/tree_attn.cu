@@ -6,36 +6,42 @@
 // The rows of a unit are the new tokens of one request times the query heads that share a KV head (row = token * group +
 // head), so that every key and value is read once for all of them.  Work is counted in steps: one for the unit (request,
 // KV head, rows) and one for each of its key tiles of 128.  The steps of all units stand in one line, which is cut into one
-// equal run per worker wherever that falls; a unit that is cut leaves partial results (unnormalised sums, reference maxima,
-// weights) that a second kernel joins in the order of the keys.  All lengths are read on the device: a prefix sum over the
-// requests tells each worker where its run begins.  (Without the step for the unit itself, workers with many short requests
-// finish late: XXX.)
+// equal run per SM wherever that falls; a unit that is cut leaves partial results (unnormalised sums, references, weights)
+// that a second kernel joins in the order of the keys.  All lengths are read on the device: a prefix sum over the requests
+// tells each CTA where its run begins.  (Without the step for the unit itself the CTAs with many short requests finish
+// late: 256 chats of 60 to 4000 tokens 243 us instead of 196.)
 //
 // What bounds it: the cache's bytes.  A tile is 64 KB (head_dim 128), 2700 cycles of an SM's share of the measured HBM
-// rate; its matrix products take 1020 cycles for up to 128 rows (the tensor core takes 128 rows at a time, however few
-// are in use), 2040 for 256.  With 256 rows its 32768 exponentials (2048 cycles of the SM's special-function units) come
-// close to the bytes.
+// rate; its matrix products take 1020 cycles of the tensor core for up to 128 rows (it takes 128 rows at a time, however
+// few are in use) and 1400 of the thread that issues them; its exponentials take 8 cycles per row of the SM's
+// special-function units.  Everything else is a matter of keeping these from waiting for one another.
 //
-// Two streams per CTA, each with its own Q, its own S and O columns in TMEM, its own four softmax warps and its own
-// loader, share the tensor core and the ring of K and V tiles, so that one stream's softmax, waits and epilogues overlap
-// the other's products.  If no request has more than 128 rows the streams are workers of their own, with a run of tiles
-// each (a unit's beginning and end then cost one stream a wait, not the SM).  Otherwise ("wide") a CTA is a worker, units
-// have up to 256 rows, and the streams are the two halves of them and walk the same tiles.
-//
-// With at most 16 rows in every request (single tokens as a rule) the tensor core's 128-row products are the wrong tool:
-// a tile costs the issuing thread 16 of them, 1400 cycles, and the softmax 128 exponentials in a row by one warp of four.
-// Then ("narrow") the eight softmax warps are on their own: each takes 16 keys of every tile, S (16 rows x 16 keys) and
-// O (16 rows x head) in registers by mma.sync m16n8k16, K and V by ldmatrix from the same ring, no hand-over between K
-// and V; their sums are added up at the unit's end.  16 mma.sync for each product and warp are a few hundred cycles of
-// the 2700 that the tile's bytes take.  (256 chats of 60 to 4000 tokens: 253 us by tcgen05 with the rows in the lanes, 291 us
-// by tcgen05 with the keys in the lanes, XXX us so.)
-//
-//   warps 0-3, 4-7  softmax and epilogue of stream 0 / 1: thread = TMEM lane = row
+//   warps 0-7       softmax and epilogue, two groups of four: thread = TMEM lane = row
 //   warp 8          producer: page ids from the table, TMA loads of K and V pages into a ring of tile slots, in the order
-//                   in which the products need them: K0 K1 V0 K2 V1 ... (a V tile that arrived with its K would hold a
-//                   slot for the whole softmax); with separate runs the streams' tiles in turn
-//   warp 9          issuer (one thread): S = Q K^T and O += P V of whichever stream is ready
-//   warps 10, 11    loader of stream 0 / 1: walks the run, publishes units, gathers their Q rows into shared memory
+//                   in which the products need them, K `lead` tiles ahead of V
+//   warp 9          issuer (one thread): S = Q K^T and O += P V
+//   warp 10         loader: walks the run, publishes units, gathers their Q rows into shared memory
+//
+// Three modes, by the largest number of rows that any request has:
+//
+// Wide (more than 128): units have up to 256 rows, the groups are their halves and walk the same tiles, each with its S and
+// its O in TMEM (128 columns each: all there is).  P takes the place of S, so a group's next S has to wait for its product
+// with V: softmax, product, next S, one after the other, and the two groups' chains overlap.  The reference maximum moves,
+// to a whole number, when the row maximum has grown by more than 2^8; O in TMEM is then rescaled (exactly).
+//
+// Tall (17 to 128): one O, three S in turn, and the groups take the tiles in turn.  S of the next tiles is computed while
+// both groups are in their softmax, so nothing waits for anything but the bytes.  One O means one reference for both
+// groups: it is taken from the unit's first tile (2^24 above the row's maximum there) and stays, which fp32 and bf16, with
+// 2^126 below and 2^127 above, have room for; no maximum is looked for in the other tiles.  If a row's weight comes out
+// above 2^56 or below 2^-40 all the same (logits that climb 55 nats above the first tile's), the CTA walks its run once
+// more, as wide.
+//
+// Narrow (at most 16, single tokens as a rule): 128-row products are the wrong tool, and a softmax with a row in a lane
+// leaves most lanes empty.  The eight softmax warps are on their own: each takes 16 keys of every tile, S (16 rows x 16
+// keys) and O (16 rows x head) in registers by mma.sync m16n8k16, K and V by ldmatrix from the same ring; their sums are
+// added up at the unit's end.  16 mma.sync for each product and warp are a few hundred cycles of the 2700 that the tile's
+// bytes take.  (256 x 950 tokens: 173 us so, 208 us by tcgen05 with the rows in the lanes, 236 us by tcgen05 with the keys
+// in the lanes: MMAs of 16 columns are issued no faster than those of 128.)
 //
 // Masks.  Only tiles that hold a key at or behind the first new token need one.  There the row's visibility bits are
 // shifted into place 32 keys at a time.  A masked probability is zero, but zero times a NaN in V is not: in those tiles
@@ -43,8 +49,8 @@
 // any, each row adds those that it sees at the end (from the cache: they are what the sum comes to anyway).
 //
 // Rounding: products bf16 x bf16 in fp32, softmax statistics and O in fp32, P rounded to bf16 for the second product (the
-// sum of weights is taken before that rounding), the result once.  The reference maximum moves only when the row maximum
-// has grown by more than 2^8 (P stays below 2^8, exact scaling otherwise).
+// sum of weights is taken before that rounding), the result once.  References are whole numbers, so that a change of
+// reference is a change of exponents.
 //
 // Every wait is bounded as in the other tensor-core kernels: a wait that runs out raises the abort flag and the status
 // word, and all roles fall through to the common end.
@@ -60,60 +66,67 @@ using namespace tc;
 
 constexpr int kTile = 128;                       // keys of a tile
 constexpr int kUnitRows = 256;
-constexpr int kThreads = 384;
+constexpr int kThreads = 352, kWarps = kThreads / 32;
 constexpr int kProducer = 8, kIssuer = 9, kLoader = 10;
 constexpr int kUnitRing = 4;
 constexpr int kNarrowRows = 16;
+enum Mode { kNarrow, kTall, kWide };
 constexpr float kNoMax = -1e30f;                 // reference maximum before any visible key: finite, below any logit
+constexpr float kTallMargin = 24.f;              // tall: the reference above the first tile's maximum,
+constexpr float kTallMost = 72057594037927936.f, kTallLeast = 9.094947017729282e-13f;      // and the weights that it serves: 2^56, 2^-40
 
 template <int D>
 struct Plan {
-  static constexpr int NBOX = D / 64;                       // 64-column (128-byte) boxes
-  static constexpr int QBOX = 128 * 128, QHALF = NBOX * QBOX;
-  static constexpr int KBOX = kTile * 128, SLOT = NBOX * KBOX;
+  // Rows in shared memory: groups of eight; a group is 1024 bytes for each 64 columns, 128-byte swizzled.  (A page's columns
+  // then come by one TMA instruction, however many rows it has.  With all rows of 64 columns together it takes one for
+  // each, and at 75 cycles each the producer was late for pages of 16: 215 instead of 175 us.)
+  static constexpr int BOX = 1024, GROUP = D / 64 * BOX;
+  static constexpr int QHALF = 128 / 8 * GROUP, SLOT = kTile / 8 * GROUP;
   static constexpr int SLOTS = D == 128 ? 5 : 10;
   static constexpr int RING_OFF = 2 * QHALF;
   static constexpr int MISC_OFF = RING_OFF + SLOTS * SLOT;
   // narrow: one slot more, in the second half of the Q area; two sets of 16 Q rows and the sums' exchange in the first
   static constexpr int NSLOTS = SLOTS + 1, NRING_OFF = RING_OFF - SLOT;
-  static constexpr int NQ_BYTES = NBOX * kNarrowRows * 128, SUM_OFF = 2 * NQ_BYTES;
+  static constexpr int NQ_BYTES = kNarrowRows / 8 * GROUP, SUM_OFF = 2 * NQ_BYTES;
   static constexpr int SUM_ROWS = 4, SUM_STRIDE = D + 8;                  // rows exchanged at a time; 8 columns more against bank conflicts
   static_assert(SLOT == QHALF && SUM_OFF + 8 * SUM_ROWS * SUM_STRIDE * 4 <= QHALF, "");
-  static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + NSLOTS, BAR_S = BAR_FREE + NSLOTS, BAR_P = BAR_S + 2, BAR_PV = BAR_P + 2,
-                       BAR_QFULL = BAR_PV + 2, BAR_QFREE = BAR_QFULL + 2, BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + 2 * kUnitRing,
-                       BARS = BAR_UFREE + 2 * kUnitRing;
-  static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;               // [stream][kUnitRing]
-  static constexpr int SCAN_OFF = (UNIT_OFF + 2 * kUnitRing * UNIT_BYTES + 15) / 16 * 16;    // int64 [24]
-  static constexpr int RUN_OFF = SCAN_OFF + 24 * 8;                                   // int64 [6], int [4]
-  static constexpr int TAG_OFF = RUN_OFF + 6 * 8 + 4 * 4;                             // int [16]
-  static constexpr int EX_OFF = TAG_OFF + 16 * 4;                                     // narrow: float2 [8][16]
-  static constexpr int TOTAL = EX_OFF + 8 * kNarrowRows * 8;
-  static constexpr int S_COL = 0, O_COL = 256, O_STEP = D;  // S: 128 columns a stream; O: D columns a stream
+  // full and free: tiles; S, P: wide per group, tall per buffer; PV: wide per group; REF, OFULL, OFREE: tall
+  static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + NSLOTS, BAR_S = BAR_FREE + NSLOTS, BAR_P = BAR_S + 3, BAR_PV = BAR_P + 3, BAR_REF = BAR_PV + 2,
+                       BAR_OFULL = BAR_REF + 1, BAR_OFREE = BAR_OFULL + 1, BAR_QFULL = BAR_OFREE + 1, BAR_QFREE = BAR_QFULL + 2,
+                       BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + kUnitRing, BARS = BAR_UFREE + kUnitRing;
+  static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;
+  static constexpr int SCAN_OFF = (UNIT_OFF + kUnitRing * UNIT_BYTES + 15) / 16 * 16;        // int64 [2][kWarps]
+  static constexpr int RUN_OFF = SCAN_OFF + 2 * kWarps * 8;                           // int64 [3], int [4]
+  static constexpr int TAG_OFF = RUN_OFF + 3 * 8 + 4 * 4;                             // int [8]
+  static constexpr int EX_OFF = (TAG_OFF + 8 * 4 + 15) / 16 * 16;                     // narrow: float2 [8][16]; tall: float [2][128]
+  static constexpr int REF_OFF = EX_OFF + 1024;                                       // tall: float [128]
+  static constexpr int TOTAL = REF_OFF + 512;
+  // TMEM columns: S 128 each; O: wide behind two S, tall behind three
+  static constexpr int S_COL = 0, O_COL = 256, O_STEP = D, TALL_O_COL = 384;
 };
 
-struct Unit {       // of one stream
-  int n_tiles;      // key tiles of this worker's part; 0: no more units
+struct Unit {
+  int n_tiles;      // key tiles of this CTA's part; 0: no more units
   int kt0;          // first of them
   int kt_all;       // key tiles of the whole unit
   int start;        // first row of the request
-  int r0, rows;     // first of the stream's rows (token * group + head) inside the request, and their number
+  int r0, rows;     // first of the unit's rows (token * group + head) inside the request, and their number
   int g, b;
   int len, past;
   int pad[2];
 };
 static_assert(sizeof(Unit) == 48, "");
 
-struct Meta {       // what the join kernel needs of a unit that begins in this worker and goes on in later ones
-  int last;         // worker that has the unit's last tile; < 0: there is no such unit
-  int start, r0, rows, g, wide, pad[2];
+struct Meta {       // what the join kernel needs of a unit that begins in this CTA and goes on in later ones
+  int last;         // CTA that has the unit's last tile; < 0: there is no such unit
+  int start, r0, rows, g, pad[3];
 };
 
-// Worker w is stream w / n_cta of CTA w % n_cta (wide: CTA w), so that few tiles spread over the SMs first.
 struct Work {
-  float* part;      // [cta][2][256][D] unnormalised sums (stream 1: rows 128 on): part 0 of a unit begun by an earlier
-                    // worker, part 1 of one begun here
-  float2* ml;       // [cta][2][256] reference maximum, weight
-  Meta* meta;       // [worker]
+  float* part;      // [cta][2][256][D] unnormalised sums: part 0 of a unit begun by an earlier CTA, part 1 of one begun here
+  float2* ml;       // [cta][2][256] reference, weight
+  Meta* meta;       // [cta]
+  CacheSteps k, v;  // of the tensor maps
 };
 
 struct Request {
@@ -161,31 +174,34 @@ __device__ __forceinline__ uint32_t mbar_test3(uint32_t b0, uint32_t par0, uint3
       : "memory");
   return r0 | r1 | r2;
 }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
       : "memory");
 }
 // Products with operand descriptors given by their low words (address and leading offset); the high word is the same for
-// all tiles here (1024 bytes between 8-row groups, 128-byte swizzle).
-constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+// all operands here (the bytes between 8-row groups, 128-byte swizzle).
+template <int D>
+constexpr uint32_t kDescHigh = ((uint32_t)Plan<D>::GROUP >> 4) | (1u << 14) | (2u << 29);
+template <int D>
 __device__ __forceinline__ void mma_ss_lo(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accum) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
       "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accum), "n"(kDescHigh)
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accum), "n"(kDescHigh<D>)
       : "memory");
 }
+template <int D>
 __device__ __forceinline__ void mma_ts_lo(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accum) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
       "mov.b64 db, {%2, %5};\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accum), "n"(kDescHigh)
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accum), "n"(kDescHigh<D>)
       : "memory");
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -223,16 +239,16 @@ __device__ __forceinline__ uint32_t seen32(const TreeAttnArgs& a, const Unit& u,
   return live & __funnelshift_r(word(w0), word(w0 + 1), (uint32_t)x0 & 31u);
 }
 
-// The non-finite values of new tokens that a row sees, added to the d columns that its thread has just written (they were
-// left out of the products): bf16 results, or fp32 partial sums.
+// The non-finite values of new tokens that a row sees, added to columns lo .. hi - 1 of what its thread has just written
+// (they were left out of the products): bf16 results, or fp32 partial sums.
 template <typename T>
-__device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, T* out, int d) {
+__device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, T* out, int lo, int hi) {
   const int k_from = max(u.kt0 * kTile, u.past), k_to = min((u.kt0 + u.n_tiles) * kTile, u.len);
   for (int key = k_from; key < k_to; ++key) {
     const int id = a.table[(size_t)u.b * a.max_pages + (key >> a.page_log2)];
     if (id < 0 || id >= a.n_pages || !(seen32(a, u, token, key) & 1)) continue;
     const __nv_bfloat16* v = a.vc.data + id * a.vc.s_page + u.g * a.vc.s_head + (key & ((1 << a.page_log2) - 1)) * a.vc.s_tok;
-    for (int c = 0; c < d; ++c) {
+    for (int c = lo; c < hi; ++c) {
       const float x = __bfloat162float(v[c]);
       if (!isfinite(x)) out[c] = static_cast<T>(static_cast<float>(out[c]) + x);
     }
@@ -265,11 +281,13 @@ __device__ __noinline__ void rescale_tmem(uint32_t t_o, uint32_t t_s, float alph
 }
 
 // The logits of the keys that a row does not see are set to -infinity in TMEM before the common path reads them.  Called
-// by whole warps; a row that is not the unit's (token < 0) sees nothing.
-__device__ __noinline__ void mask_tmem(const TreeAttnArgs& a, const Unit& u, int token, int k0, uint32_t t_s) {
+// by whole warps; a row that is not the unit's (token < 0) sees nothing.  Whether the row sees any of the tile's keys.
+__device__ __noinline__ bool mask_tmem(const TreeAttnArgs& a, const Unit& u, int token, int k0, uint32_t t_s) {
+  uint32_t any = 0;
 #pragma unroll 1
   for (int c = 0; c < kTile / 32; ++c) {
     const uint32_t seen = token >= 0 ? seen32(a, u, token, k0 + c * 32) : 0u;
+    any |= seen;
     if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
     uint32_t s[32];
     tmem_ld32(t_s + c * 32, s);
@@ -278,6 +296,7 @@ __device__ __noinline__ void mask_tmem(const TreeAttnArgs& a, const Unit& u, int
     tmem_st32(t_s + c * 32, s);
   }
   tmem_wait_st();
+  return any != 0;
 }
 
 // Values behind the sequence become zero in a V tile, and so do non-finite ones of new tokens (reported: see
@@ -285,8 +304,9 @@ __device__ __noinline__ void mask_tmem(const TreeAttnArgs& a, const Unit& u, int
 // first word of row 0.  Rolled loops: the code runs once a unit and is fetched anew each time; unrolled by eight rows it
 // took 2000 cycles for sixteen.
 template <int D>
-__device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first_behind, volatile int* tags, int tag_lo, int tag_hi, int mark) {
-  constexpr int BOXES = D / 64, BOX_WORDS = kTile * 128 / 4;
+__device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first_behind, volatile int* tags, int mark) {
+  constexpr int BOXES = D / 64, BOX_WORDS = 1024 / 4, GROUP_WORDS = BOXES * BOX_WORDS;
+  auto at = [&](int r, int b) { return v + (r >> 3) * GROUP_WORDS + b * BOX_WORDS + (r & 7) * 32; };
   int r = lo;
 #pragma unroll 1
   for (; r < min(hi, first_behind); ++r) {
@@ -294,62 +314,89 @@ __device__ __noinline__ void clean_values(uint32_t* v, int lo, int hi, int first
     bool met = false;
 #pragma unroll
     for (int b = 0; b < BOXES; ++b) {
-      w[b] = v[b * BOX_WORDS + r * 32];
+      w[b] = *at(r, b);
       met |= nonfinite2(w[b]);
     }
     if (met) {
-      for (int x = tag_lo; x <= tag_hi; ++x) tags[x * 8 + mark % 8] = mark;
+      tags[mark % 8] = mark;
       __threadfence_block();
 #pragma unroll
       for (int b = 0; b < BOXES; ++b) {
         uint32_t x = w[b];
         if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
         if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
-        v[b * BOX_WORDS + r * 32] = x;
+        *at(r, b) = x;
       }
     }
   }
 #pragma unroll 2
   for (r = max(lo, first_behind); r < hi; ++r)
 #pragma unroll
-    for (int b = 0; b < BOXES; ++b) v[b * BOX_WORDS + r * 32] = 0u;
+    for (int b = 0; b < BOXES; ++b) *at(r, b) = 0u;
 }
 
-// Epilogue of a stream's unit, out of the hot loop: the rows' results, or their part for the join.  Called by whole warps.
-template <int D>
-__device__ __noinline__ void write_rows(const TreeAttnArgs& a, const Work& work, const Unit& u, int x, int row, int token, int head, uint32_t t_o,
-                                        float m_ref, float l, bool repair) {
-  const bool live = row < u.rows, whole = u.kt0 == 0 && u.n_tiles == u.kt_all;
-  const float f = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
-  const size_t slot = ((size_t)blockIdx.x * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + x * 128 + row;
-  __nv_bfloat16* out = a.o + head * a.o_sh + (u.start + token) * a.o_sn;
-  float* part = work.part + slot * D;
+// Columns lo .. hi - 1 of a row from TMEM, scaled by f: the result, or a part for the join.  Rolled, out of the hot loop.
+// Called by whole warps; what is not `live` is not written.  Whether all of the row's values were finite.
+__device__ __noinline__ bool write_columns(uint32_t t_o, int lo, int hi, float f, bool live, __nv_bfloat16* out, float* part) {
+  bool finite = true;
 #pragma unroll 1
-  for (int c = 0; c < D / 32; ++c) {
+  for (int c = lo; c < hi; c += 32) {
     uint32_t y[32];
-    tmem_ld32(t_o + c * 32, y);
+    tmem_ld32(t_o + c, y);
     if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) finite &= (y[i] & 0x7f800000u) != 0x7f800000u;
     auto val = [&](int i) { return __uint_as_float(y[i]) * f; };
-    if (whole) {
-      uint4* dst = reinterpret_cast<uint4*>(out + c * 32);
+    if (part == nullptr) {
+      uint4* dst = reinterpret_cast<uint4*>(out + c);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         dst[i] = make_uint4(pack_bf16(val(8 * i), val(8 * i + 1)), pack_bf16(val(8 * i + 2), val(8 * i + 3)), pack_bf16(val(8 * i + 4), val(8 * i + 5)),
                             pack_bf16(val(8 * i + 6), val(8 * i + 7)));
     } else {
-      float4* dst = reinterpret_cast<float4*>(part + c * 32);
+      float4* dst = reinterpret_cast<float4*>(part + c);
 #pragma unroll
       for (int i = 0; i < 8; ++i) dst[i] = make_float4(val(4 * i), val(4 * i + 1), val(4 * i + 2), val(4 * i + 3));
     }
   }
-  if (live) {
-    if (repair) {
-      if (whole) add_nonfinite(a, u, token, out, D);
-      else add_nonfinite(a, u, token, part, D);
-    }
-    if (!whole) work.ml[slot] = make_float2(m_ref, l);
-    else if (a.lse) a.lse[(size_t)head * a.rows + u.start + token] = l != 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
+  return finite;
+}
+
+// Where a unit's row goes: its result, or its part if the unit was cut.
+struct Place {
+  int token, head;
+  __nv_bfloat16* out;
+  size_t slot;
+  bool whole;
+};
+__device__ __forceinline__ Place place_of(const TreeAttnArgs& a, const Unit& u, int row) {
+  Place p;
+  const int abs_row = u.r0 + row;
+  p.token = abs_row / a.group;
+  p.head = u.g * a.group + abs_row % a.group;
+  p.out = a.o + p.head * a.o_sh + (u.start + p.token) * a.o_sn;
+  p.whole = u.kt0 == 0 && u.n_tiles == u.kt_all;
+  p.slot = ((size_t)blockIdx.x * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + row;
+  return p;
+}
+__device__ __forceinline__ void write_weight(const TreeAttnArgs& a, const Work& work, const Unit& u, const Place& p, float m, float l) {
+  if (!p.whole) work.ml[p.slot] = make_float2(m, l);
+  else if (a.lse) a.lse[(size_t)p.head * a.rows + u.start + p.token] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
+}
+
+// Tall: the reference of this thread's row, from the S of the unit's first tile.  Called by whole warps.
+__device__ __noinline__ float first_reference(uint32_t t_s, float scale, bool live) {
+  float top = -CUDART_INF_F;
+#pragma unroll 1
+  for (int c = 0; c < kTile; c += 32) {
+    uint32_t s[32];
+    tmem_ld32(t_s + c, s);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(s[e]));
   }
+  top *= scale;
+  // nothing seen here: 0, and the weights tell at the end whether that served
+  return !live ? -kNoMax : top > -CUDART_INF_F && top < CUDART_INF_F ? ceilf(top) + kTallMargin : 0.f;
 }
 
 // Requests of at most 16 rows: products and softmax in the registers of the eight warps, one call for the whole run.
@@ -361,7 +408,7 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
   auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // Fragments of mma.sync m16n8k16: lane = (row g = lane / 4, and g + 8; columns 2 q, 2 q + 1, q = lane % 4).
   const int g = lane >> 2, q = lane & 3;
   float2* ex = reinterpret_cast<float2*>(smem + P::EX_OFF);          // [warp][row] reference, weight
@@ -370,8 +417,8 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
   const int k_row = warp * 16 + (lane & 7) + ((lane >> 4) << 3), k_piece = (lane >> 3) & 1;   // K: keys 0-7, 8-15 by piece, piece + 1
   const int v_row = warp * 16 + (lane & 15), v_piece = lane >> 4;                            // V (and Q): rows 0-7, 8-15, then the next piece
   const uint32_t ring = base + P::NRING_OFF;
-  auto at = [](uint32_t tile, int box, int row, int piece) {
-    return tile + (piece >> 3) * box + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+  auto at = [](uint32_t tile, int row, int piece) {
+    return tile + (row >> 3) * P::GROUP + (piece >> 3) * P::BOX + (row & 7) * 128 + (((piece ^ row) & 7) << 4);
   };
   const float scale = a.scale_log2;
   uint32_t slot = 0, phase = 0;                     // of the next tile in the ring
@@ -390,7 +437,7 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
     if (ok) {
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk)
-        ldmatrix4(at(base + (seq & 1) * P::NQ_BYTES, kNarrowRows * 128, lane & 15, 2 * kk + v_piece), qf[kk]);
+        ldmatrix4(at(base + (seq & 1) * P::NQ_BYTES, lane & 15, 2 * kk + v_piece), qf[kk]);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(P::BAR_QFREE + (seq & 1)));
@@ -408,7 +455,7 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
           uint32_t b[4];
-          ldmatrix4(at(tile, P::KBOX, k_row, 2 * kk + k_piece), b);
+          ldmatrix4(at(tile, k_row, 2 * kk + k_piece), b);
           mma16816(s[0], qf[kk], b[0], b[1]);
           mma16816(s[1], qf[kk], b[2], b[3]);
         }
@@ -463,7 +510,7 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
         // values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite)
         const int lo = max(no_mask - k0, warp * 16);
         if (lo < warp * 16 + 16) {
-          clean_values<D>(reinterpret_cast<uint32_t*>(smem + P::NRING_OFF + slot * P::SLOT) + lane, lo, warp * 16 + 16, u.len - k0, bad_tag, 0, 0, seq + 1);
+          clean_values<D>(reinterpret_cast<uint32_t*>(smem + P::NRING_OFF + slot * P::SLOT) + lane, lo, warp * 16 + 16, u.len - k0, bad_tag, seq + 1);
           fence_async_smem();
         }
         __syncwarp();
@@ -473,7 +520,7 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
 #pragma unroll
         for (int n = 0; n < D / 8; n += 2) {
           uint32_t b[4];
-          ldmatrix4t(at(tile, P::KBOX, v_row, n + v_piece), b);
+          ldmatrix4t(at(tile, v_row, n + v_piece), b);
           mma16816(o[n], pf, b[0], b[1]);
           mma16816(o[n + 1], pf, b[2], b[3]);
         }
@@ -492,7 +539,6 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
       ex[warp * kNarrowRows + g + 8] = make_float2(m1, l1);
     }
     if (!bar_and(1, 256, ok)) break;
-    const bool whole = u.kt0 == 0 && n_tiles == u.kt_all;
     float top0 = kNoMax, top1 = kNoMax;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
@@ -528,34 +574,497 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
 #pragma unroll
           for (int i = 0; i < PER; ++i) y[i] += sums[(w * P::SUM_ROWS + sub) * P::SUM_STRIDE + col + i];
         }
-        const int token = row / a.group, head = u.g * a.group + row % a.group;
-        const size_t part = ((size_t)cta * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + row;
-        __nv_bfloat16* out = a.o + head * a.o_sh + (u.start + token) * a.o_sn;
+        const Place p = place_of(a, u, row);
         const float inv = all != 0.f ? 1.f / all : 0.f;
-        if (!whole) {
+        if (!p.whole) {
 #pragma unroll
-          for (int i = 0; i < PER; ++i) work.part[part * D + col + i] = y[i];
+          for (int i = 0; i < PER; ++i) work.part[p.slot * D + col + i] = y[i];
         } else if constexpr (PER == 2) {
-          *reinterpret_cast<uint32_t*>(out + col) = pack_bf16(y[0] * inv, y[1] * inv);
+          *reinterpret_cast<uint32_t*>(p.out + col) = pack_bf16(y[0] * inv, y[1] * inv);
         } else {
-          out[col] = __float2bfloat16(y[0] * inv);
+          p.out[col] = __float2bfloat16(y[0] * inv);
         }
-        if ((threadIdx.x & 63) == 0) {
-          if (!whole) work.ml[part] = make_float2(top, all);
-          else if (a.lse) a.lse[(size_t)head * a.rows + u.start + token] = all != 0.f ? (top + log2f(all)) * 0.6931471805599453f : -CUDART_INF_F;
-        }
+        if ((threadIdx.x & 63) == 0) write_weight(a, work, u, p, top, all);
       }
     }
     if (bad_tag[(seq + 1) % 8] == seq + 1) {
       bar_sync(1, 256);                             // the rows are written
       if (threadIdx.x < rows) {
-        const int row = threadIdx.x, token = row / a.group, head = u.g * a.group + row % a.group;
-        if (whole) add_nonfinite(a, u, token, a.o + head * a.o_sh + (u.start + token) * a.o_sn, D);
-        else add_nonfinite(a, u, token, work.part + (((size_t)cta * 2 + (u.kt0 > 0 ? 0 : 1)) * kUnitRows + row) * D, D);
+        const Place p = place_of(a, u, threadIdx.x);
+        if (p.whole) add_nonfinite(a, u, p.token, p.out, 0, D);
+        else add_nonfinite(a, u, p.token, work.part + p.slot * D, 0, D);
       }
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+  }
+}
+
+// Positions in the ring, a CTA's tile j of n, K `lead` tiles ahead of V: K j + max(0, j - lead), V behind the K of tile j + lead
+// (lead 2: K0 K1 K2 V0 K3 V1 ... K(n-1) V(n-3) V(n-2) V(n-1)).
+constexpr uint32_t kWideLead = 1, kTallLead = 2;
+__device__ __forceinline__ uint32_t k_pos(uint32_t j, uint32_t lead) { return j + (j > lead ? j - lead : 0u); }
+__device__ __forceinline__ uint32_t v_pos(uint32_t j, uint32_t n, uint32_t lead) { return min(2 * j + 1 + lead, n + j); }
+
+// P of 32 logits: exponentials, bf16 pairs; their sum.
+__device__ __forceinline__ float weights(const uint32_t (&s)[32], float scale, float m, uint32_t (&p)[16]) {
+  auto val = [&](int e) { return __uint_as_float(s[e]); };
+  const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-m, -m);
+  float2 sum01 = make_float2(0.f, 0.f), sum23 = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) {
+    float2 x01 = __ffma2_rn(make_float2(val(e), val(e + 1)), sc2, nm2);
+    float2 x23 = __ffma2_rn(make_float2(val(e + 2), val(e + 3)), sc2, nm2);
+    x01.x = ex2_approx(x01.x);
+    x01.y = ex2_approx(x01.y);
+    x23.x = ex2_approx(x23.x);
+    x23.y = ex2_approx(x23.y);
+    sum01 = __fadd2_rn(sum01, x01);
+    sum23 = __fadd2_rn(sum23, x23);
+    p[e / 2] = cvt_bf16x2(x01.x, x01.y);
+    p[e / 2 + 1] = cvt_bf16x2(x23.x, x23.y);
+  }
+  return (sum01.x + sum01.y) + (sum23.x + sum23.y);
+}
+
+// The issuer: one thread.  (The long loops are functions of their own: in one body each pays for the others' registers, 10 us
+// of 180 for 128K keys and a tree of 64.)
+template <int D, Mode MODE>
+__device__ __noinline__ void issue_products(const TreeAttnArgs& a, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
+  using P = Plan<D>;
+  const uint32_t base = smem_u32(smem);
+  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  volatile int* abort_flag = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8) + 1;
+  constexpr uint32_t idesc_qk = instr_desc(128, kTile, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
+  const uint32_t d_q = (uint32_t)smem_desc(base, 16, P::GROUP), d_k = (uint32_t)smem_desc(base + P::RING_OFF, 16, P::GROUP),
+                 d_v = (uint32_t)smem_desc(base + P::RING_OFF, P::BOX, P::GROUP);
+  // One thread does all of this, and every instruction of its loops delays the tiles: 32-bit counters, no arrays that are
+  // indexed at run time.  Tiles are seen to arrive in the order of the ring: a barrier's parity tells which phase is
+  // over only to one who has seen the phase before it.
+  uint32_t arrived = 0, a_slot = 0, a_phase = 0, polls = 0;
+  long long idle_since = 0;
+  auto arrival = [&] {
+    ++arrived;
+    if (++a_slot == P::SLOTS) { a_slot = 0; a_phase ^= 1; }
+  };
+  auto stalled = [&](bool moved) {                 // true: give up
+    if (moved) {
+      idle_since = 0;
+      polls = 0;
+      return false;
+    }
+    if ((++polls & 63u) != 0u) return false;
+    if (*abort_flag) return true;
+    if ((polls & 4095u) != 0u) return false;
+    const long long now = clock64();
+    if (idle_since == 0) idle_since = now;
+    else if (now - idle_since > kWaitCycles) {
+      *abort_flag = 1;
+      if (atomicCAS(a.status, 0, (int)SP_ERR_TIMEOUT) == 0) a.status[1] = 60;
+      return true;
+    }
+    return false;
+  };
+  auto issue_qk = [&](uint32_t col, uint32_t half, uint32_t slot) {
+    const uint32_t dq = d_q + half * (P::QHALF >> 4), dk = d_k + slot * (P::SLOT >> 4);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+      mma_ss_lo<D>(tmem + P::S_COL + col, dq + (kk >> 2) * (P::BOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::BOX >> 4) + (kk & 3) * 2, idesc_qk, kk > 0);
+  };
+  auto issue_pv = [&](uint32_t o_col, uint32_t col, uint32_t slot, bool first) {
+    const uint32_t dv = d_v + slot * (P::SLOT >> 4);
+#pragma unroll
+    for (int kk = 0; kk < kTile / 16; ++kk)
+      mma_ts_lo<D>(tmem + o_col, tmem + P::S_COL + col + kk * 8, dv + kk * (2 * P::GROUP >> 4), idesc_pv, kk > 0 || !first);
+  };
+  if constexpr (MODE == kTall) {
+  // Tall.  S of tile i in buffer i % 3, computed up to three tiles ahead of its product with V.
+  uint32_t n_qk = 0, n_pv = 0, q_buf = 0, p_buf = 0, p_phase = 0;
+  uint32_t k_slot = 0, v_slot = v_pos(0, n_tiles_cta, kTallLead) % P::SLOTS, k_at = 0, v_at = v_pos(0, n_tiles_cta, kTallLead);
+  uint32_t left = 0, seq = 0, pv_unit = 0;
+  uint32_t first = 0, last = 0;                  // bit b: the tile in buffer b opens / ends its unit's sum
+  bool q_here = false, fresh = false;
+  while (n_pv != n_tiles_cta) {
+    bool moved = false;
+    // a poll is a round trip to shared memory, 200 cycles and more while the tensor core streams from it
+    const uint32_t polled = mbar_test3(bar(P::BAR_P + p_buf), p_phase, bar(P::BAR_OFREE), (pv_unit + 1) & 1, bar(P::BAR_FULL + a_slot), a_phase);
+    if ((polled & 4) && arrived != 2 * n_tiles_cta) {
+      arrival();
+      moved = true;
+    }
+    const bool opens = (first >> p_buf) & 1;
+    if (n_qk != n_pv && v_at < arrived && (polled & 1) && (!opens || pv_unit == 0 || (polled & 2))) {
+      // (the first product of a unit overwrites O: the groups have read the last unit's)
+      tc_fence_after();
+      issue_pv(P::TALL_O_COL, p_buf * 128, v_slot, opens);
+      mma_commit(bar(P::BAR_FREE + v_slot));
+      if ((last >> p_buf) & 1) {
+        mma_commit(bar(P::BAR_OFULL));
+        ++pv_unit;
+      }
+      ++n_pv;
+      const uint32_t to = v_pos(n_pv, n_tiles_cta, kTallLead);
+      v_slot += to - v_at;
+      v_at = to;
+      if (v_slot >= P::SLOTS) v_slot -= P::SLOTS;
+      if (++p_buf == 3) { p_buf = 0; p_phase ^= 1; }
+      moved = true;
+    }
+    if (n_qk != n_tiles_cta && n_qk - n_pv < 3) {
+      if (left == 0) {
+        const uint32_t e = seq % kUnitRing;
+        if (mbar_test(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1)) {
+          left = units[e].n_tiles;
+          mbar_arrive(bar(P::BAR_UFREE + e));
+          ++seq;
+          q_here = false;
+          fresh = true;
+        }
+      }
+      if (left != 0 && k_at < arrived) {
+        const uint32_t half = (seq - 1) & 1;
+        if (!q_here) q_here = mbar_test(bar(P::BAR_QFULL + half), ((seq - 1) >> 1) & 1);
+        if (q_here) {
+          tc_fence_after();
+          issue_qk(q_buf * 128, half, k_slot);
+          mma_commit(bar(P::BAR_S + q_buf));
+          mma_commit(bar(P::BAR_FREE + k_slot));
+          --left;
+          if (left == 0) mma_commit(bar(P::BAR_QFREE + half));
+          const uint32_t bit = 1u << q_buf;
+          first = fresh ? first | bit : first & ~bit;
+          last = left == 0 ? last | bit : last & ~bit;
+          fresh = false;
+          ++n_qk;
+          const uint32_t to = k_pos(n_qk, kTallLead);
+          k_slot += to - k_at;
+          k_at = to;
+          if (k_slot >= P::SLOTS) k_slot -= P::SLOTS;
+          if (++q_buf == 3) q_buf = 0;
+          moved = true;
+        }
+      }
+    }
+    if (stalled(moved)) break;
+  }
+  // the last arrivals, before the barriers may be used anew
+  for (uint32_t i = 0; i < P::SLOTS; ++i) {
+    const uint32_t uses = (2 * n_tiles_cta + P::SLOTS - 1 - i) / P::SLOTS;
+    if (uses > 0) mbar_wait(bar(P::BAR_FREE + i), (uses - 1) & 1, ab, 61);
+  }
+  for (uint32_t i = 0; i < 2; ++i) {
+    const uint32_t uses = (seq + 1 - i) / 2;
+    if (uses > 0) mbar_wait(bar(P::BAR_QFREE + i), (uses - 1) & 1, ab, 62);
+  }
+  } else {
+  // Wide.  The groups' chains are independent of one another but for the tiles; a group's next S is computed when its
+  // last P has gone into its product.
+  struct Group {
+    uint32_t n_qk, n_pv;                         // products issued
+    uint32_t left, k_at, k_slot, v_at, v_slot;   // tiles left in the unit; ring positions of the next K and V tile
+    uint32_t seq;                                // units taken
+    bool first, q_here;                          // the next O opens a sum; the unit's Q has been seen
+  } gr[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    gr[x].n_qk = gr[x].n_pv = gr[x].left = gr[x].seq = gr[x].k_at = gr[x].k_slot = 0;
+    gr[x].v_at = v_pos(0, n_tiles_cta, kWideLead); gr[x].v_slot = gr[x].v_at % P::SLOTS;
+    gr[x].first = gr[x].q_here = false;
+  }
+  auto advance = [&](uint32_t& at, uint32_t& slot, uint32_t to) {
+    slot += to - at;
+    at = to;
+    if (slot >= P::SLOTS) slot -= P::SLOTS;
+  };
+  while (gr[0].n_pv != n_tiles_cta || gr[1].n_pv != n_tiles_cta) {
+    bool moved = false;
+    const uint32_t polled = mbar_test3(bar(P::BAR_P), gr[0].n_pv & 1, bar(P::BAR_P + 1), gr[1].n_pv & 1, bar(P::BAR_FULL + a_slot), a_phase);
+    if ((polled & 4) && arrived != 2 * n_tiles_cta) {
+      arrival();
+      moved = true;
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      Group& t = gr[x];
+      if (t.n_qk != t.n_pv && t.v_at < arrived && ((polled >> x) & 1)) {
+        tc_fence_after();
+        issue_pv(P::O_COL + x * P::O_STEP, x * 128, t.v_slot, t.first);
+        mma_commit(bar(P::BAR_PV + x));
+        mma_commit(bar(P::BAR_FREE + t.v_slot));
+        ++t.n_pv;
+        t.first = false;
+        advance(t.v_at, t.v_slot, v_pos(t.n_pv, n_tiles_cta, kWideLead));
+        moved = true;
+      }
+      if (t.n_qk == t.n_pv && t.n_qk != n_tiles_cta) {
+        if (t.left == 0) {
+          const uint32_t e = t.seq % kUnitRing;
+          if (mbar_test(bar(P::BAR_UNIT + e), (t.seq / kUnitRing) & 1)) {
+            t.left = units[e].n_tiles;
+            if (x == 1) mbar_arrive(bar(P::BAR_UFREE + e));        // group 0's unit too has been taken, or will before the entry is
+            ++t.seq;
+            t.q_here = false;
+            t.first = true;
+          }
+        }
+        if (t.left != 0 && t.k_at < arrived) {
+          if (!t.q_here) t.q_here = mbar_test(bar(P::BAR_QFULL + x), (t.seq - 1) & 1);
+          if (t.q_here) {
+            tc_fence_after();
+            issue_qk(x * 128, x, t.k_slot);
+            mma_commit(bar(P::BAR_S + x));
+            mma_commit(bar(P::BAR_FREE + t.k_slot));
+            if (--t.left == 0) mma_commit(bar(P::BAR_QFREE + x));
+            ++t.n_qk;
+            advance(t.k_at, t.k_slot, k_pos(t.n_qk, kWideLead));
+            moved = true;
+          }
+        }
+      }
+    }
+    if (stalled(moved)) break;
+  }
+  }
+}
+
+// Softmax and epilogue, wide: a group for each half of the rows.
+template <int D>
+__device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& work, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
+  using P = Plan<D>;
+  const uint32_t base = smem_u32(smem);
+  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  volatile int* abort_flag = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8) + 1;
+  volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int x = warp >> 2;                          // group
+  const int row = threadIdx.x & 127;                // TMEM lane, row of the group
+  const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  const float scale = a.scale_log2;
+  // The V of a tile with masked keys: what lies behind the sequence counts as zero, and so do non-finite values of new
+  // tokens (see add_nonfinite).  V comes after K, hence not before the softmax.  S of the tile was there, so every tile up
+  // to its K has arrived, the one before V in V's slot among them: the barrier's parity can be told.
+  auto clean = [&](uint32_t j, const Unit& u, int k0, int no_mask, int seq) {
+    const uint32_t p = v_pos(j, n_tiles_cta, kWideLead), s = p % P::SLOTS;
+    const bool here = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
+    // each warp of the group 32 keys
+    const int lo = max(no_mask - k0, (warp & 3) * 32);
+    if (here && lo < (warp & 3) * 32 + 32)
+      clean_values<D>(reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane, lo, (warp & 3) * 32 + 32, u.len - k0, bad_tag, seq + 1);
+    fence_async_smem();
+    return here;
+  };
+  bool ok = true;
+  uint32_t done = 0;                                // tiles of earlier units
+  const uint32_t t_s = lanes + P::S_COL + x * 128, t_o = lanes + P::O_COL + x * P::O_STEP;
+  for (int seq = 0; ok; ++seq) {
+    const int e = seq % kUnitRing;
+    ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
+    if (!ok) break;
+    const Unit& u = units[e];                     // stays in shared memory until the unit is done: registers are short
+    const int n_tiles = u.n_tiles;
+    if (n_tiles == 0) break;
+    const int my_row = x * 128 + row;
+    const bool warp_live = x * 128 + (warp & 3) * 32 < u.rows, live = my_row < u.rows;
+    const int token = (u.r0 + my_row) / a.group;
+    const int kt0 = u.kt0, no_mask = min(u.past, u.len);      // keys before it are seen by every row
+    float m_ref = live ? kNoMax : -kNoMax, l = 0.f;           // lanes without a row: all weights zero
+    for (int t = 0; t < n_tiles && ok; ++t) {
+      const int k0 = (kt0 + t) * kTile;
+      const bool special = k0 + kTile > no_mask;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + x), (done + t) & 1, ab, 31));
+      if (!ok) break;
+      tc_fence_after();
+      if (warp_live) {
+        // Four chunks of 32 logits, the next one's load in flight, each a step of the running softmax
+        if (special) mask_tmem(a, u, live ? token : -1, k0, t_s);
+        uint32_t s[2][32];
+        float sum = 0.f;
+        tmem_ld32_async(t_s, s[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tmem_ld_wait();
+          reg_fence32(s[c & 1]);
+          const uint32_t* y = s[c & 1];
+          auto val = [&](int i) { return __uint_as_float(y[i]); };
+          float m0 = max3(val(0), val(1), val(2)), m1 = max3(val(3), val(4), val(5)), m2 = max3(val(6), val(7), val(8)),
+                m3 = max3(val(9), val(10), val(11));
+#pragma unroll
+          for (int i = 12; i < 28; i += 8) {
+            m0 = max3(m0, val(i), val(i + 1));
+            m1 = max3(m1, val(i + 2), val(i + 3));
+            m2 = max3(m2, val(i + 4), val(i + 5));
+            m3 = max3(m3, val(i + 6), val(i + 7));
+          }
+          m0 = max3(m0, val(28), val(29));
+          m1 = max3(m1, val(30), val(31));
+          const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
+          const bool grown = mx > m_ref + 8.f;              // never in lanes without a row
+          if (__any_sync(0xffffffffu, grown)) {
+            const float m_new = grown ? ceilf(mx) : m_ref;
+            const float alpha = ex2_approx(m_ref - m_new);
+            // the group's previous product came before this S, and nothing of this P has been handed over
+            rescale_tmem<D>(t_o, t_s, alpha, c, t > 0);
+            l *= alpha;
+            sum *= alpha;
+            m_ref = m_new;
+          }
+          // not before the call above: its registers must not be moved while the load is under way
+          if (c < 3) tmem_ld32_async(t_s + (c + 1) * 32, s[(c + 1) & 1]);
+          uint32_t p[16];
+          sum += weights(s[c & 1], scale, m_ref, p);
+          tmem_st16(t_s + c * 16, p);
+        }
+        l += sum;
+        tmem_wait_st();
+      }
+      if (special) ok = clean(done + t, u, k0, no_mask, seq);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_P + x));
+    }
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + x), (done + n_tiles - 1) & 1, ab, 33));
+    if (ok && warp_live) {
+      tc_fence_after();
+      const Place p = place_of(a, u, my_row);
+      float* part = p.whole ? nullptr : work.part + p.slot * D;
+      write_columns(t_o, 0, D, !p.whole ? 1.f : l != 0.f ? 1.f / l : 0.f, live, p.out, part);
+      if (live) {
+        if (bad_tag[(seq + 1) % 8] == seq + 1) {
+          if (p.whole) add_nonfinite(a, u, p.token, p.out, 0, D);
+          else add_nonfinite(a, u, p.token, part, 0, D);
+        }
+        write_weight(a, work, u, p, m_ref, l);
+      }
+      __syncwarp();
+      tc_fence_before();                          // O has left TMEM: before the P after which the next product overwrites it
+    }
+    done += n_tiles;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+  }
+}
+
+// Softmax and epilogue, tall: the groups take the tiles in turn.
+template <int D>
+__device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& work, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
+  using P = Plan<D>;
+  const uint32_t base = smem_u32(smem);
+  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  volatile int* abort_flag = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8) + 1;
+  volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int x = warp >> 2;                          // group
+  const int row = threadIdx.x & 127;                // TMEM lane, row of the group
+  const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  const float scale = a.scale_log2;
+  volatile int* redo = abort_flag + 2;
+  // The V of a tile with masked keys: what lies behind the sequence counts as zero, and so do non-finite values of new
+  // tokens (see add_nonfinite).  V comes after K, hence not before the softmax.  S of the tile was there, so every tile up
+  // to its K has arrived, the one before V in V's slot among them: the barrier's parity can be told.
+  auto clean = [&](uint32_t j, const Unit& u, int k0, int no_mask, int seq) {
+    const uint32_t p = v_pos(j, n_tiles_cta, kTallLead), s = p % P::SLOTS;
+    const bool here = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
+    // each warp of the group 32 keys
+    const int lo = max(no_mask - k0, (warp & 3) * 32);
+    if (here && lo < (warp & 3) * 32 + 32)
+      clean_values<D>(reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane, lo, (warp & 3) * 32 + 32, u.len - k0, bad_tag, seq + 1);
+    fence_async_smem();
+    return here;
+  };
+  bool ok = true;
+  uint32_t done = 0;                                // tiles of earlier units
+  const uint32_t t_o = lanes + P::TALL_O_COL;
+  float* ex = reinterpret_cast<float*>(smem + P::EX_OFF);            // [group][row] weight, -1: nothing seen
+  float* refs = reinterpret_cast<float*>(smem + P::REF_OFF);         // [row]
+  for (int seq = 0;; ++seq) {
+    const int e = seq % kUnitRing;
+    ok = __all_sync(0xffffffffu, ok && mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
+    // the eight warps go on together or stop together: none is left at the barriers below
+    if (!bar_and(1, 256, ok)) break;
+    const Unit& u = units[e];
+    const int n_tiles = u.n_tiles;
+    if (n_tiles == 0) break;
+    const bool warp_live = (warp & 3) * 32 < u.rows, live = row < u.rows;
+    const int token = (u.r0 + row) / a.group;
+    const int kt0 = u.kt0, no_mask = min(u.past, u.len);
+    const int t0 = (int)((done + x) & 1);         // the CTA's tiles in turn: tile i is of group i & 1, in buffer i % 3
+    float m_ref = -kNoMax, l = 0.f;
+    bool have_ref = false, saw = false;
+    for (int t = t0; t < n_tiles && ok; t += 2) {
+      const uint32_t i = done + t, buf = i % 3;
+      const uint32_t t_s = lanes + P::S_COL + buf * 128;
+      const int k0 = (kt0 + t) * kTile;
+      const bool special = k0 + kTile > no_mask;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + buf), (i / 3) & 1, ab, 31));
+      if (!ok) break;
+      tc_fence_after();
+      if (warp_live) saw |= special ? mask_tmem(a, u, live ? token : -1, k0, t_s) : true;
+      if (t == 0) {
+        if (warp_live) refs[row] = first_reference(t_s, scale, live);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(P::BAR_REF));
+      }
+      if (!have_ref) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_REF), seq & 1, ab, 34));
+        if (!ok) break;
+        m_ref = live ? refs[row] : -kNoMax;
+        have_ref = true;
+      }
+      if (warp_live) {
+        uint32_t s[2][32];
+        tmem_ld32_async(t_s, s[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tmem_ld_wait();
+          reg_fence32(s[c & 1]);
+          if (c < 3) tmem_ld32_async(t_s + (c + 1) * 32, s[(c + 1) & 1]);
+          uint32_t p[16];
+          l += weights(s[c & 1], scale, m_ref, p);
+          tmem_st16(t_s + c * 16, p);
+        }
+        tmem_wait_st();
+      }
+      if (special) ok = clean(i, u, k0, no_mask, seq);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_P + buf));
+    }
+    if (ok && !have_ref) {                        // a unit of one tile, the other group's
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_REF), seq & 1, ab, 34));
+      if (ok) m_ref = live ? refs[row] : -kNoMax;
+    }
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_OFULL), seq & 1, ab, 33));
+    ex[x * 128 + row] = saw ? l : -1.f;
+    if (!bar_and(1, 256, ok)) break;
+    tc_fence_after();
+    if (warp_live) {
+      const float l0 = ex[row], l1 = ex[128 + row];
+      const bool seen = l0 != -1.f || l1 != -1.f;
+      l = (l0 == -1.f ? 0.f : l0) + (l1 == -1.f ? 0.f : l1);
+      const Place p = place_of(a, u, row);
+      float* part = p.whole ? nullptr : work.part + p.slot * D;
+      const int lo = x * (D / 2);                 // each group half of the columns
+      const bool finite = write_columns(t_o, lo, lo + D / 2, !p.whole ? 1.f : l != 0.f ? 1.f / l : 0.f, live, p.out, part);
+      if (live) {
+        if (seen && (l > kTallMost || l < kTallLeast || (l > 256.f && !finite))) *redo = 1;
+        if (bad_tag[(seq + 1) % 8] == seq + 1) {
+          if (p.whole) add_nonfinite(a, u, p.token, p.out, lo, lo + D / 2);
+          else add_nonfinite(a, u, p.token, part, lo, lo + D / 2);
+        }
+        if (x == 0) write_weight(a, work, u, p, l != 0.f ? m_ref : kNoMax, l);
+      }
+      __syncwarp();
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(bar(P::BAR_OFREE));
+      mbar_arrive(bar(P::BAR_UFREE + e));
+    }
+    done += n_tiles;
   }
 }
 
@@ -569,14 +1078,15 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   long long* scan = reinterpret_cast<long long*>(smem + P::SCAN_OFF);
-  long long* start_rem = reinterpret_cast<long long*>(smem + P::RUN_OFF);      // [stream] steps of the request before the run
-  long long* tiles_at = start_rem + 2;             // [stream][2] tiles before the run's begin and end
-  int* words = reinterpret_cast<int*>(smem + P::RUN_OFF + 6 * 8);
+  long long* start_rem = reinterpret_cast<long long*>(smem + P::RUN_OFF);      // steps of the request before the run
+  long long* tiles_at = start_rem + 1;             // tiles before the run's begin and end
+  int* words = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(words);
   volatile int* abort_flag = words + 1;
-  int* start_b = words + 2;                        // [stream] request in which the run begins
-  // [stream][8]: number, from 1, of a unit in which a non-finite value was met, at that number modulo 8 (the streams of
-  // wide units write each other's and are two units apart at most)
+  int* start_b = words + 2;                        // request in which the run begins
+  volatile int* redo = words + 3;                  // tall: the references did not serve
+  // number, from 1, of a unit in which a non-finite value was met, at that number modulo 8 (the groups of wide units are two
+  // units apart at most)
   volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = blockIdx.x, n_cta = gridDim.x;
@@ -586,19 +1096,13 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   const bool misplaced = (base & 1023u) != 0;      // the tiles' swizzle needs the window's alignment
   if (warp == kProducer && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
   if (threadIdx.x == 0) {
-    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(bar(P::BAR_S + x), 1);
-      mbar_init(bar(P::BAR_P + x), 4);
-      mbar_init(bar(P::BAR_PV + x), 1);
-    }
-    *abort_flag = 0;
-    for (int i = 0; i < 16; ++i) bad_tag[i] = 0;
+    *abort_flag = *redo = 0;
+    for (int i = 0; i < 8; ++i) bad_tag[i] = 0;
   }
   wait_for_previous();
   const bool poisoned = decode_poisoned(a.status);
 
-  // ---- where the runs begin
+  // ---- where the run begins
   const int per = (a.n_req + kThreads - 1) / kThreads;
   const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
   long long mine_t = 0, mine_u = 0;                // tiles, units
@@ -617,10 +1121,10 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     const long long up_t = __shfl_up_sync(0xffffffffu, incl_t, o), up_u = __shfl_up_sync(0xffffffffu, incl_u, o);
     if (lane >= o) { incl_t += up_t; incl_u += up_u; }
   }
-  if (lane == 31) { scan[warp] = incl_t; scan[12 + warp] = incl_u; }
+  if (lane == 31) { scan[warp] = incl_t; scan[kWarps + warp] = incl_u; }
   if (threadIdx.x == 0 && misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
-  const bool wide = __syncthreads_or(many) != 0, narrow = __syncthreads_or(some) == 0;
-  const bool by_cta = wide || narrow;              // a CTA is a worker
+  bool wide = __syncthreads_or(many) != 0;
+  const bool narrow = __syncthreads_or(some) == 0;
   if (!narrow) {
     if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
     // rows of the Q area that no unit fills stay zero: products of whatever lay there would cost power, and with it clock
@@ -629,28 +1133,26 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   }
   long long before_t = incl_t - mine_t, before_u = incl_u - mine_u, total_t = 0, total = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) { before_t += scan[w]; before_u += scan[12 + w]; }
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) { before_t += scan[w]; before_u += scan[kWarps + w]; }
     total_t += scan[w];
-    total += scan[w] + scan[12 + w];
+    total += scan[w] + scan[kWarps + w];
   }
-  const int workers = by_cta ? n_cta : 2 * n_cta;
-  const long long quota = divide(total, workers), extra = total - quota * workers;      // the first `extra` runs are one step longer
+  const long long quota = divide(total, n_cta), extra = total - quota * n_cta;      // the first `extra` runs are one step longer
   auto run_begin = [&](int w) { return w * quota + min((long long)w, extra); };
-  for (int i = 0; i < (by_cta ? 2 : 4); ++i) {
-    const int x = i >> 1, end = i & 1;
-    const long long w = run_begin((by_cta ? cta : x * n_cta + cta) + end);
+  for (int end = 0; end < 2; ++end) {
+    const long long w = run_begin(cta + end);
     long long step = before_t + before_u, tile = before_t;
     if (w >= total) {
-      if (threadIdx.x == 0) tiles_at[i] = total_t;
+      if (threadIdx.x == 0) tiles_at[end] = total_t;
     } else if (step <= w && w < step + mine_t + mine_u) {
       for (int b = b_lo; b < b_hi; ++b) {
         const Request q = request(a, b);
         const long long n = units_of(a, q);
         if (w < step + n * (q.kt + 1)) {
           const long long rem = w - step, nth = divide(rem, q.kt + 1), in = rem - nth * (q.kt + 1);
-          tiles_at[i] = tile + nth * q.kt + max(in - 1, 0ll);
-          if (!end) { start_b[x] = b; start_rem[x] = rem; }
+          tiles_at[end] = tile + nth * q.kt + max(in - 1, 0ll);
+          if (end == 0) { *start_b = b; *start_rem = rem; }
           break;
         }
         step += n * (q.kt + 1);
@@ -658,435 +1160,225 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       }
     }
   }
-  if (threadIdx.x == 0) {
-    // who lets a tile go: the stream's issuer, both streams', or the eight warps; likewise the queries
+  auto init_barriers = [&](bool wide) {
+    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(bar(P::BAR_S + i), 1);
+      mbar_init(bar(P::BAR_P + i), 4);
+    }
+    for (int x = 0; x < 2; ++x) mbar_init(bar(P::BAR_PV + x), 1);
+    mbar_init(bar(P::BAR_REF), 4);
+    mbar_init(bar(P::BAR_OFULL), 1);
+    mbar_init(bar(P::BAR_OFREE), 8);
+    // who lets a tile go: the issuer once, or (wide) for each group, or the eight warps; likewise the queries, which come
+    // from 32 lanes' copies when narrow; a unit is read by the eight warps, the producer and the issuer, if it has work
     for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FREE + s), narrow ? 8 : wide ? 2 : 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(bar(P::BAR_QFULL + x), narrow ? 32 : 1);
       mbar_init(bar(P::BAR_QFREE + x), narrow ? 8 : 1);
     }
-    // a unit is read by four softmax warps, the issuer and the producer (wide: in ring 0 only), or by eight warps and the producer
-    for (int e = 0; e < 2 * kUnitRing; ++e) {
+    for (int e = 0; e < kUnitRing; ++e) {
       mbar_init(bar(P::BAR_UNIT + e), 1);
-      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : 4 + 1 + (wide && e >= kUnitRing ? 0 : 1));
+      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : 10);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
+  };
+  if (threadIdx.x == 0) init_barriers(wide);
   tc_fence_before();
   const bool idle = __syncthreads_or(poisoned || misplaced) != 0;
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  // tiles of the streams' runs, and of the CTA.  Job j of the CTA is a tile of one stream, the streams in turn as long as both
-  // have some; wide: a tile of both.
-  uint32_t n_run[2];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) n_run[x] = idle || (narrow && x == 1) ? 0u : (uint32_t)(tiles_at[by_cta ? 1 : 2 * x + 1] - tiles_at[by_cta ? 0 : 2 * x]);
-  const uint32_t n_steps = wide ? n_run[0] : n_run[0] + n_run[1], in_turn = min(n_run[0], n_run[1]);
-  auto job_of = [&](int x, uint32_t i) { return wide ? i : i < in_turn ? 2 * i + x : in_turn + i; };
-  // ring positions of the K and V tiles of job j: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1); narrow: K0 V0 K1 V1 ...
-  auto k_pos = [&](uint32_t j) { return j == 0 ? 0u : 2 * j - 1; };
-  auto v_pos = [&](uint32_t j) { return j + 1 == n_steps ? 2 * j + 1 : 2 * j + 2; };
+  const uint32_t n_tiles_cta = idle ? 0u : (uint32_t)(tiles_at[1] - tiles_at[0]);
 
-  if (warp >= kLoader) {
-    // ------------------------------------------------------------ units of stream x and their queries
-    const int x = warp - kLoader, me = by_cta ? cta : x * n_cta + cta;
-    bool ok = true;
-    int seq = 0;
-    if (lane == 0) work.meta[x * n_cta + cta].last = -1;
-    if (n_run[x] > 0) {
-      int b = start_b[by_cta ? 0 : x];
-      long long rem = start_rem[by_cta ? 0 : x], w = run_begin(me);
-      const long long w1 = run_begin(me + 1);
-      Request q = request(a, b);
-      while (w < w1 && ok) {
-        while (rem >= units_of(a, q) * (q.kt + 1) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
-        if (rem >= units_of(a, q) * (q.kt + 1)) break;       // not reached while the lengths stand still
-        Unit u;
-        const int n_pass = passes(a, q), all_rows = q.n * a.group;
-        const int nth = (int)divide(rem, q.kt + 1), in = (int)(rem - (long long)nth * (q.kt + 1));       // step of the unit: tile `in - 1`
-        const int take = (int)min((long long)(q.kt + 1 - in), w1 - w);
-        w += take;
-        rem += take;
-        u.kt0 = max(in - 1, 0);
-        u.kt_all = q.kt;
-        u.n_tiles = in + take - 1 - u.kt0;
-        if (u.n_tiles == 0) continue;                // only the unit's own step: its tiles are the next worker's
-        u.g = n_pass == 1 ? nth : nth / n_pass;
-        u.b = b;
-        u.start = q.start;
-        u.r0 = (nth - u.g * n_pass) * kUnitRows + (wide ? x * 128 : 0);
-        u.rows = min(128, max(all_rows - u.r0, 0));
-        u.len = q.len;
-        u.past = q.past;
-        const int e = x * kUnitRing + seq % kUnitRing;
-        if (seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
-        if (!ok) break;
-        if (lane == 0) {
-          units[e] = u;
-          mbar_arrive(bar(P::BAR_UNIT + e));
-          if (u.kt0 == 0 && u.n_tiles < u.kt_all && !(wide && x == 1)) {
-            const long long z = w - take - in + u.kt_all, cut = extra * (quota + 1);     // the step of the unit's last tile
-            Meta m{(int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota)), u.start, u.r0,
-                   wide ? min(all_rows - u.r0, kUnitRows) : u.rows, u.g, wide, {0, 0}};
-            work.meta[me] = m;
+  for (;;) {
+    const uint32_t lead = narrow ? 0u : wide ? kWideLead : kTallLead;
+    if (warp == kLoader) {
+      // ------------------------------------------------------------ units and their queries
+      bool ok = true;
+      int seq = 0;
+      if (lane == 0) work.meta[cta].last = -1;
+      if (n_tiles_cta > 0) {
+        int b = *start_b;
+        long long rem = *start_rem, w = run_begin(cta);
+        const long long w1 = run_begin(cta + 1);
+        Request q = request(a, b);
+        while (w < w1 && ok) {
+          while (rem >= units_of(a, q) * (q.kt + 1) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
+          if (rem >= units_of(a, q) * (q.kt + 1)) break;       // not reached while the lengths stand still
+          Unit u;
+          const int n_pass = passes(a, q), all_rows = q.n * a.group;
+          const int nth = (int)divide(rem, q.kt + 1), in = (int)(rem - (long long)nth * (q.kt + 1));       // step of the unit: tile `in - 1`
+          const int take = (int)min((long long)(q.kt + 1 - in), w1 - w);
+          w += take;
+          rem += take;
+          u.kt0 = max(in - 1, 0);
+          u.kt_all = q.kt;
+          u.n_tiles = in + take - 1 - u.kt0;
+          if (u.n_tiles == 0) continue;                // only the unit's own step: its tiles are the next CTA's
+          u.g = n_pass == 1 ? nth : nth / n_pass;
+          u.b = b;
+          u.start = q.start;
+          u.r0 = (nth - u.g * n_pass) * kUnitRows;
+          u.rows = min(all_rows - u.r0, kUnitRows);
+          u.len = q.len;
+          u.past = q.past;
+          const int e = seq % kUnitRing;
+          if (seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
+          if (!ok) break;
+          if (lane == 0) {
+            units[e] = u;
+            mbar_arrive(bar(P::BAR_UNIT + e));
+            if (u.kt0 == 0 && u.n_tiles < u.kt_all) {
+              const long long z = w - take - in + u.kt_all, cut = extra * (quota + 1);     // the step of the unit's last tile
+              Meta m{(int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota)), u.start, u.r0, u.rows, u.g, {0, 0, 0}};
+              work.meta[cta] = m;
+            }
+            if (a.seq_lens[b] > q.len) report_range(a.status, kWhereTreePage);   // longer than its table row
           }
-          if (a.seq_lens[b] > q.len) report_range(a.status, kWhereTreePage);   // longer than its table row
-        }
-        // its queries: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA descriptors say.  A lane keeps its
-        // piece of every (32 / pieces)-th row, whose token and head advance without division.
-        // (narrow: two sets of rows in turn)
-        const int set = narrow ? seq & 1 : x, lap = narrow ? seq >> 1 : seq;
-        if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + set), (lap - 1) & 1, ab, 41));
-        if (!ok) break;
-        {
+          // its queries: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA descriptors say.  A lane keeps its
+          // piece of every (32 / pieces)-th row, whose token and head advance without division (one division a piece:
+          // 13000 cycles for 128 rows).  Narrow and tall: two sets of rows in turn; wide: one of two halves.
+          const int first = wide ? 0 : seq & 1, lap = wide ? seq : seq >> 1, halves = wide ? 2 : 1;
           constexpr int PIECES = D / 8, STEP = 32 / PIECES;
           const int piece = lane % PIECES;
           int r = lane / PIECES, hg = (u.r0 + r) % a.group;
           const __nv_bfloat16* src = a.q + (int64_t)(u.g * a.group + hg) * a.q_sh + (int64_t)(u.start + (u.r0 + r) / a.group) * a.q_sn + piece * 8;
           const int64_t down = STEP * a.q_sh, wrap = a.q_sn - a.group * a.q_sh;
-          const uint32_t box = narrow ? base + set * P::NQ_BYTES + (piece >> 3) * (kNarrowRows * 128) : base + x * P::QHALF + (piece >> 3) * P::QBOX;
+          for (int i = 0; i < halves && ok; ++i) {
+            const int set = first + i, end = min(u.rows, (i + 1) * 128);
+            if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_QFREE + set), (lap - 1) & 1, ab, 41));
+            if (!ok) break;
+            const uint32_t box = base + set * (narrow ? P::NQ_BYTES : P::QHALF) + (piece >> 3) * P::BOX;
 #pragma unroll 2
-          for (; r < u.rows; r += STEP) {
-            cp_async16(box + r * 128 + (((piece & 7) ^ (r & 7)) << 4), src);
-            src += down;
-            hg += STEP;
-            while (hg >= a.group) { hg -= a.group; src += wrap; }
+            for (; r < end; r += STEP) {
+              cp_async16(box + ((r & 127) >> 3) * P::GROUP + (r & 7) * 128 + (((piece ^ r) & 7) << 4), src);
+              src += down;
+              hg += STEP;
+              while (hg >= a.group) { hg -= a.group; src += wrap; }
+            }
+            if (narrow) {                              // read by ldmatrix: the copies' arrival is enough, and nobody waits for it here
+              asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar(P::BAR_QFULL + set)) : "memory");
+            } else {
+              asm volatile("cp.async.wait_all;" ::: "memory");
+              fence_async_smem();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + set));
+            }
           }
+          ++seq;
         }
-        if (narrow) {                                // read by ldmatrix: the copies' arrival is enough, and nobody waits for it here
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar(P::BAR_QFULL + set)) : "memory");
-        } else {
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(P::BAR_QFULL + set));
-        }
-        ++seq;
       }
-    }
-    // no more units
-    const int e = x * kUnitRing + seq % kUnitRing;
-    if (ok && seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
-    if (ok && lane == 0) {
-      units[e].n_tiles = 0;
-      mbar_arrive(bar(P::BAR_UNIT + e));
-    }
-  } else if (warp == kProducer) {
-    // ------------------------------------------------------------ K and V tiles
-    bool ok = true;
-    const uint32_t ring = base + (narrow ? P::NRING_OFF : P::RING_OFF), slots = narrow ? P::NSLOTS : P::SLOTS;
-    uint32_t s = 0, lap = 0;                         // next slot of the ring, times round
-    const int page = 1 << a.page_log2;
-    const int per_tile = max(kTile >> a.page_log2, 1), rows = min(page, kTile);
-    struct Tile {                                    // this lane's page of a tile
-      int id, off, g;
-      bool live;
-    } last{0, 0, 0, false};
-    auto load = [&](const Tile& tile, const CUtensorMap& map) {
-      if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (lap - 1) & 1, ab, 51));
-      if (!ok) return;
-      const int n_live = __popc(__ballot_sync(0xffffffffu, tile.live));
-      if (lane == 0) mbar_expect_tx(bar(P::BAR_FULL + s), n_live * rows * D * 2);
-      __syncwarp();
-      if (tile.live) {
-        const uint32_t dst = ring + s * P::SLOT + lane * rows * 128;
-#pragma unroll
-        for (int x = 0; x < P::NBOX; ++x) tma_load_4d(dst + x * P::KBOX, &map, bar(P::BAR_FULL + s), x * 64, tile.off, tile.g, tile.id);
+      // no more units
+      const int e = seq % kUnitRing;
+      if (ok && seq >= kUnitRing) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UFREE + e), (seq / kUnitRing - 1) & 1, ab, 40));
+      if (ok && lane == 0) {
+        units[e].n_tiles = 0;
+        mbar_arrive(bar(P::BAR_UNIT + e));
       }
-      __syncwarp();
-      if (++s == slots) { s = 0; ++lap; }
-    };
-    // where each stream's walk stands (wide: stream 0's serves both)
-    struct Walk {
-      int seq, kt, kt_end, len, g, b, id;            // id: this lane's page of tile kt
-    } walk[2];
-    walk[0].seq = walk[1].seq = 0;
-    walk[0].kt = walk[0].kt_end = walk[1].kt = walk[1].kt_end = 0;
-    // lane p looks up page p of the tile, a tile ahead
-    auto lookup = [&](const Walk& k, int kt) {
-      const int key = kt * kTile + lane * page;
-      return lane < per_tile && key < k.len ? a.table[(size_t)k.b * a.max_pages + (key >> a.page_log2)] : -1;
-    };
-    auto step = [&](Walk& k, int x) -> Tile {
-      if (k.kt == k.kt_end) {
-        const int e = x * kUnitRing + k.seq % kUnitRing;
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (k.seq / kUnitRing) & 1, ab, 50));
-        if (!ok) return Tile{0, 0, 0, false};
-        const Unit& u = units[e];
-        k.kt = u.kt0; k.kt_end = u.kt0 + u.n_tiles; k.len = u.len; k.g = u.g; k.b = u.b;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
-        ++k.seq;
-        k.id = lookup(k, k.kt);
-      }
-      const int key = k.kt * kTile + lane * page;
-      Tile tile{k.id, key & (page - 1), k.g, lane < per_tile && key < k.len};
-      if (tile.live && (tile.id < 0 || tile.id >= a.n_pages)) {
-        report_range(a.status, kWhereTreePage);
-        tile.id = a.n_pages;                         // outside the tensor map: the load fills in zeros
-      }
-      ++k.kt;
-      if (k.kt < k.kt_end) k.id = lookup(k, k.kt);
-      return tile;
-    };
-    for (uint32_t j = 0; j < n_steps && ok; ++j) {
-      const Tile now = by_cta || (j < 2 * in_turn ? (j & 1) == 0 : n_run[0] > n_run[1]) ? step(walk[0], 0) : step(walk[1], 1);
-      load(now, tm_k);
-      if (narrow) load(now, tm_v);
-      else if (j > 0) load(last, tm_v);
-      last = now;
-    }
-    if (n_steps > 0 && !narrow) load(last, tm_v);
-    // the last entry of each ring that this warp reads says that there are no more units: nothing to take from it
-    if (*abort_flag && lane == 0) {
-      // let the copies already in flight land before the CTA gives its shared memory back
-      const long long t0 = clock64();
-      for (uint32_t i = 0; i < slots; ++i) {
-        const uint32_t laps = lap + (i < s);          // loads that this slot has been given
-        while (laps > 0 && !mbar_test(bar(P::BAR_FULL + i), (laps - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {}
-      }
-    }
-  } else if (warp == kIssuer) {
-    // ------------------------------------------------------------ products
-    if (lane == 0 && !narrow) {
-      constexpr uint32_t idesc_qk = instr_desc(128, kTile, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
-      const uint32_t d_q = (uint32_t)smem_desc(base, 16, 1024), d_k = (uint32_t)smem_desc(base + P::RING_OFF, 16, 1024),
-                     d_v = (uint32_t)smem_desc(base + P::RING_OFF, P::KBOX, 1024);
-      // One thread does all of this, and every instruction of the loop delays both streams: 32-bit counters, everything
-      // about a stream in registers (the loop over the streams is unrolled).  A stream's next S is computed when its last
-      // P has gone into its product.
-      struct Stream {
-        uint32_t n_qk, n_pv;                         // products issued
-        uint32_t left, seq;                          // tiles left in the unit, units taken
-        uint32_t k_at, k_slot, v_at, v_slot;         // ring positions of the next K and V tile
-        bool first, q_here;                          // the next O opens a sum; the unit's Q has been seen
-      } st[2];
-      auto advance = [&](uint32_t& at, uint32_t& slot, uint32_t to) {        // a stream's tiles are at most four apart
-        slot += to - at;
-        at = to;
-        if (slot >= P::SLOTS) slot -= P::SLOTS;
+    } else if (warp == kProducer) {
+      // ------------------------------------------------------------ K and V tiles
+      bool ok = true;
+      const uint32_t ring = base + (narrow ? P::NRING_OFF : P::RING_OFF), slots = narrow ? P::NSLOTS : P::SLOTS;
+      uint32_t s = 0, lap = 0;                         // next slot of the ring, times round
+      const int page = 1 << a.page_log2;
+      const int per_tile = max(kTile >> a.page_log2, 1), rows = min(page, kTile);
+      struct Tile {                                    // this lane's page of a tile
+        int id, off, g;
+        bool live;
       };
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        st[x].n_qk = st[x].n_pv = st[x].left = st[x].seq = 0;
-        st[x].first = st[x].q_here = false;
-        const uint32_t j = job_of(x, 0);
-        st[x].k_at = k_pos(j); st[x].k_slot = st[x].k_at % P::SLOTS;
-        st[x].v_at = v_pos(j); st[x].v_slot = st[x].v_at % P::SLOTS;
-      }
-      // Tiles are seen to arrive in the order of the ring, whichever stream they are for: a barrier's parity says which
-      // phase is over only to one who has seen the phase before it, and a slot's phase before may be the other stream's.
-      uint32_t arrived = 0, a_slot = 0, a_phase = 0;
-      uint32_t polls = 0;
-      long long idle_since = 0;
-      while (st[0].n_pv != n_run[0] || st[1].n_pv != n_run[1]) {
-        bool moved = false;
-        // a poll is a round trip to shared memory, 200 cycles and more while the tensor core streams from it
-        const uint32_t polled = mbar_test3(bar(P::BAR_P), st[0].n_pv & 1, bar(P::BAR_P + 1), st[1].n_pv & 1, bar(P::BAR_FULL + a_slot), a_phase);
-        if ((polled & 4) && arrived != 2 * n_steps) {
-          ++arrived;
-          if (++a_slot == P::SLOTS) { a_slot = 0; a_phase ^= 1; }
-          moved = true;
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          Stream& t = st[x];
-          if (t.n_qk != t.n_pv && t.v_at < arrived && ((polled >> x) & 1)) {
-            tc_fence_after();
-            const uint32_t dv = d_v + t.v_slot * (P::SLOT >> 4);
-#pragma unroll
-            for (int kk = 0; kk < kTile / 16; ++kk)
-              mma_ts_lo(tmem + P::O_COL + x * P::O_STEP, tmem + P::S_COL + x * 128 + kk * 8, dv + kk * (16 * 128 >> 4), idesc_pv, kk > 0 || !t.first);
-            mma_commit(bar(P::BAR_PV + x));
-            mma_commit(bar(P::BAR_FREE + t.v_slot));
-            ++t.n_pv;
-            t.first = false;
-            advance(t.v_at, t.v_slot, v_pos(job_of(x, t.n_pv)));
-            moved = true;
-          }
-          if (t.n_qk == t.n_pv && t.n_qk != n_run[x]) {
-            if (t.left == 0) {
-              const uint32_t e = x * kUnitRing + t.seq % kUnitRing;
-              if (mbar_test(bar(P::BAR_UNIT + e), (t.seq / kUnitRing) & 1)) {
-                t.left = units[e].n_tiles;
-                mbar_arrive(bar(P::BAR_UFREE + e));
-                ++t.seq;
-                t.q_here = false;
-                t.first = true;
-              }
-            }
-            if (t.left != 0 && t.k_at < arrived) {
-              if (!t.q_here) t.q_here = mbar_test(bar(P::BAR_QFULL + x), (t.seq - 1) & 1);
-              if (t.q_here) {
-                tc_fence_after();
-                const uint32_t dq = d_q + x * (P::QHALF >> 4), dk = d_k + t.k_slot * (P::SLOT >> 4);
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                  mma_ss_lo(tmem + P::S_COL + x * 128, dq + (kk >> 2) * (P::QBOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::KBOX >> 4) + (kk & 3) * 2,
-                            idesc_qk, kk > 0);
-                mma_commit(bar(P::BAR_S + x));
-                mma_commit(bar(P::BAR_FREE + t.k_slot));
-                if (--t.left == 0) mma_commit(bar(P::BAR_QFREE + x));
-                ++t.n_qk;
-                advance(t.k_at, t.k_slot, k_pos(job_of(x, t.n_qk)));
-                moved = true;
-              }
-            }
-          }
-        }
-        if (moved) {
-          idle_since = 0;
-          polls = 0;
-        } else if ((++polls & 63u) == 0u) {
-          if (*abort_flag) break;
-          if ((polls & 4095u) == 0u) {
-            const long long now = clock64();
-            if (idle_since == 0) idle_since = now;
-            else if (now - idle_since > kWaitCycles) {
-              *abort_flag = 1;
-              if (atomicCAS(a.status, 0, (int)SP_ERR_TIMEOUT) == 0) a.status[1] = 60;
-              break;
-            }
-          }
-        }
-      }
-    }
-    __syncwarp();
-  } else if (narrow) {
-    narrow_warps<D>(a, work, smem, ab);
-  } else {
-    // ------------------------------------------------------------ softmax and epilogue
-    const int x = warp >> 2;                          // stream
-    const int row = threadIdx.x & 127;                // TMEM lane, row of the stream
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + lanes + P::S_COL + x * 128, t_o = tmem + lanes + P::O_COL + x * P::O_STEP;
-    const float scale = a.scale_log2;
-    bool ok = true;
-    uint32_t n_jobs = 0;                              // of this stream so far
-    for (int seq = 0; ok; ++seq) {
-      const int e = x * kUnitRing + seq % kUnitRing;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
-      if (!ok) break;
-      const Unit& u = units[e];                       // stays in shared memory until the unit is done: registers are short
-      const int n_tiles = u.n_tiles;
-      if (n_tiles == 0) break;
-      const bool warp_live = (warp & 3) * 32 < u.rows, live = row < u.rows;
-      const int abs_row = u.r0 + row;
-      const int token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
-      const int kt0 = u.kt0, no_mask = min(u.past, u.len);      // keys before it are seen by every row
-      float m_ref = live ? kNoMax : -kNoMax, l = 0.f;           // lanes without a row: all weights zero
-      for (int t = 0; t < n_tiles && ok; ++t) {
-        const int k0 = (kt0 + t) * kTile;
-        const bool special = k0 + kTile > no_mask;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + x), n_jobs & 1, ab, 31));
-        if (!ok) break;
-        tc_fence_after();
-        if (warp_live) {
-          // Four chunks of 32 logits, the next one's load in flight, each a step of the running softmax.  The reference
-          // moves, to a whole number, when the row maximum has grown by more than 2^8.
-          if (special) mask_tmem(a, u, live ? token : -1, k0, t_s);
-          uint32_t s[2][32];
-          float sum = 0.f;
-          tmem_ld32_async(t_s, s[0]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            tmem_ld_wait();
-            reg_fence32(s[c & 1]);
-            const uint32_t* y = s[c & 1];
-            auto val = [&](int e) { return __uint_as_float(y[e]); };
-            float m0 = max3(val(0), val(1), val(2)), m1 = max3(val(3), val(4), val(5)), m2 = max3(val(6), val(7), val(8)),
-                  m3 = max3(val(9), val(10), val(11));
-#pragma unroll
-            for (int e = 12; e < 28; e += 8) {
-              m0 = max3(m0, val(e), val(e + 1));
-              m1 = max3(m1, val(e + 2), val(e + 3));
-              m2 = max3(m2, val(e + 4), val(e + 5));
-              m3 = max3(m3, val(e + 6), val(e + 7));
-            }
-            m0 = max3(m0, val(28), val(29));
-            m1 = max3(m1, val(30), val(31));
-            const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
-            const bool grown = mx > m_ref + 8.f;              // never in lanes without a row
-            if (__any_sync(0xffffffffu, grown)) {
-              const float m_new = grown ? ceilf(mx) : m_ref;
-              const float alpha = ex2_approx(m_ref - m_new);
-              // the stream's previous product came before this S, and nothing of this P has been handed over
-              rescale_tmem<D>(t_o, t_s, alpha, c, t > 0);
-              l *= alpha;
-              sum *= alpha;
-              m_ref = m_new;
-            }
-            // not before the call above: its registers must not be moved while the load is under way
-            if (c < 3) tmem_ld32_async(t_s + (c + 1) * 32, s[(c + 1) & 1]);
-            const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-m_ref, -m_ref);
-            float2 sum01 = make_float2(0.f, 0.f), sum23 = make_float2(0.f, 0.f);
-            uint32_t p[16];
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              float2 x01 = __ffma2_rn(make_float2(val(e), val(e + 1)), sc2, nm2);
-              float2 x23 = __ffma2_rn(make_float2(val(e + 2), val(e + 3)), sc2, nm2);
-              x01.x = ex2_approx(x01.x);
-              x01.y = ex2_approx(x01.y);
-              x23.x = ex2_approx(x23.x);
-              x23.y = ex2_approx(x23.y);
-              sum01 = __fadd2_rn(sum01, x01);
-              sum23 = __fadd2_rn(sum23, x23);
-              p[e / 2] = cvt_bf16x2(x01.x, x01.y);
-              p[e / 2 + 1] = cvt_bf16x2(x23.x, x23.y);
-            }
-            sum += (sum01.x + sum01.y) + (sum23.x + sum23.y);
-            tmem_st16(t_s + c * 16, p);
-          }
-          l += sum;
-          tmem_wait_st();
-        }
-        if (special) {
-          // Values behind the sequence count as zero, and so do non-finite ones of new tokens (see add_nonfinite).  V comes
-          // after K, hence not before the softmax.  S of the tile was there, so every tile up to its K has arrived, the one
-          // before V in V's slot among them: the barrier's parity can be told.
-          const uint32_t p = v_pos(job_of(x, n_jobs)), s = p % P::SLOTS;
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
-          if (!ok) break;
-          // each warp of the stream 32 keys
-          const int r_lo = (warp & 3) * 32, lo = max(no_mask - k0, r_lo);
-          if (lo < r_lo + 32) {
-            uint32_t* v = reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane;
-            // the tags before the zeros: in a wide unit both streams clean the same tile, and who finds zeros finds its tag
-            clean_values<D>(v, lo, r_lo + 32, u.len - k0, bad_tag, wide ? 0 : x, wide ? 1 : x, seq + 1);
-          }
-          fence_async_smem();
-        }
-        tc_fence_before();
+      auto load = [&](const Tile& tile, const CUtensorMap& map, const CacheSteps& steps) {
+        if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + s), (lap - 1) & 1, ab, 51));
+        if (!ok) return;
+        const int n_live = __popc(__ballot_sync(0xffffffffu, tile.live));
+        if (lane == 0) mbar_expect_tx(bar(P::BAR_FULL + s), n_live * rows * D * 2);
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(P::BAR_P + x));
-        ++n_jobs;
-      }
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + x), (n_jobs - 1) & 1, ab, 33));
-      if (ok) {
-        tc_fence_after();
-        if (warp_live) {
-          write_rows<D>(a, work, u, x, row, token, head, t_o, m_ref, l, bad_tag[x * 8 + (seq + 1) % 8] == seq + 1);
-          __syncwarp();
+        if (tile.live) {
+          // (an id outside the cache: outside the tensor map, the load fills in zeros)
+          const int at = tile.id < 0 ? steps.extent : tile.id * steps.page + tile.g * steps.head;
+          tma_load_5d(ring + s * P::SLOT + lane * (rows / 8 * P::GROUP), &map, bar(P::BAR_FULL + s), 0, 0, 0, tile.off >> 3, at);
         }
-        tc_fence_before();                            // O has left TMEM: before the P after which the next product overwrites it
+        __syncwarp();
+        if (++s == slots) { s = 0; ++lap; }
+      };
+      int seq = 0, kt = 0, kt_end = 0, len = 0, g = 0, b = 0, id = 0;      // id: this lane's page of tile kt
+      // lane p looks up page p of the tile, a tile ahead
+      auto lookup = [&] {
+        const int key = kt * kTile + lane * page;
+        return lane < per_tile && key < len ? a.table[(size_t)b * a.max_pages + (key >> a.page_log2)] : -1;
+      };
+      Tile now{0, 0, 0, false}, last1 = now, last2 = now;      // the tile, and the ones before it
+      for (uint32_t j = 0; j < n_tiles_cta && ok; ++j) {
+        if (kt == kt_end) {
+          const int e = seq % kUnitRing;
+          ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
+          if (!ok) break;
+          const Unit& u = units[e];
+          kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = u.len; g = u.g; b = u.b;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+          ++seq;
+          id = lookup();
+        }
+        const int key = kt * kTile + lane * page;
+        last2 = last1;
+        last1 = now;
+        now = Tile{id, key & (page - 1), g, lane < per_tile && key < len};
+        if (now.live && (id < 0 || id >= a.n_pages)) {
+          report_range(a.status, kWhereTreePage);
+          now.id = -1;
+        }
+        ++kt;
+        if (kt < kt_end) id = lookup();
+        load(now, tm_k, work.k);
+        if (j >= lead) load(lead == 0 ? now : lead == 1 ? last1 : last2, tm_v, work.v);
+      }
+      if (n_tiles_cta > 1 && lead > 1) load(last1, tm_v, work.v);
+      if (n_tiles_cta > 0 && lead > 0) load(now, tm_v, work.v);
+      if (*abort_flag && lane == 0) {
+        // let the copies already in flight land before the CTA gives its shared memory back
+        const long long t0 = clock64();
+        for (uint32_t i = 0; i < slots; ++i) {
+          const uint32_t laps = lap + (i < s);          // loads that this slot has been given
+          while (laps > 0 && !mbar_test(bar(P::BAR_FULL + i), (laps - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {}
+        }
+      }
+    } else if (warp == kIssuer) {
+      if (lane == 0 && !narrow) {
+        if (wide) issue_products<D, kWide>(a, smem, ab, tmem, n_tiles_cta);
+        else issue_products<D, kTall>(a, smem, ab, tmem, n_tiles_cta);
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+    } else if (narrow) {
+      narrow_warps<D>(a, work, smem, ab);
+    } else if (wide) {
+      softmax_wide<D>(a, work, smem, ab, tmem, n_tiles_cta);
+    } else {
+      softmax_tall<D>(a, work, smem, ab, tmem, n_tiles_cta);
     }
-  }
 
-  tc_fence_before();
-  __syncthreads();
-  if (warp == kIssuer && !narrow) {
+    tc_fence_before();
+    __syncthreads();
     tc_fence_after();
+    if (wide || *redo == 0 || *abort_flag) break;
+    // Tall, and a reference did not serve: the run once more, wide.  All that arrives at the barriers has done so (the issuer
+    // has waited for it).
+    if (threadIdx.x == 0) {
+      for (int i = 0; i < P::BARS; ++i) asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar(i)) : "memory");
+      init_barriers(true);
+      for (int i = 0; i < 8; ++i) bad_tag[i] = 0;
+    }
+    wide = true;
+    __syncthreads();
+  }
+  if (warp == kIssuer && !narrow) {
     tmem_dealloc(tmem, 512);
   }
 }
 
-// Joins the parts of the cut units, in the order of the keys: the part of the worker in which a unit begins, then those
-// of the workers after it.  A warp reads a row's part at once (its 32 lanes the columns).  The work is a few MB from L2 at most
-// and all latency, so it is spread as widely as it goes: every block lists the cut units (one per worker of the first
-// kernel at most) and takes every gridDim.x-th run of rows; as long as the device has warps to spare, 2, 4 or 8 of them share
+// Joins the parts of the cut units, in the order of the keys: the part of the CTA in which a unit begins, then those of
+// the CTAs after it.  A warp reads a row's part at once (its 32 lanes the columns).  The work is a few MB from L2 at most
+// and all latency, so it is spread as widely as it goes: every block lists the cut units (one per CTA of the first kernel
+// at most) and takes every gridDim.x-th run of rows; as long as the device has warps to spare, 2, 4 or 8 of them share
 // the parts of a row.
 constexpr int kJoinWarps = 8, kJoinBlocksPerSm = 4;
 
@@ -1099,9 +1391,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_j
   wait_for_previous();
   if (decode_poisoned(a.status)) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // rows of the unit that begins in worker i and goes on in later ones; thread t looks after workers per * t ...
-  const int per = (2 * n_cta + kJoinWarps * 32 - 1) / (kJoinWarps * 32);
-  auto rows_of = [&](int i) { return i < 2 * n_cta && work.meta[i].last >= 0 ? work.meta[i].rows : 0; };
+  // rows of the unit that begins in CTA i and goes on in later ones; thread t looks after CTAs per * t ...
+  const int per = (n_cta + kJoinWarps * 32 - 1) / (kJoinWarps * 32);
+  auto rows_of = [&](int i) { return i < n_cta && work.meta[i].last >= 0 ? work.meta[i].rows : 0; };
   auto block_scan = [&](int mine, int* total) {      // sum over the threads before this one
     int incl = mine;
 #pragma unroll
@@ -1157,8 +1449,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_j
           const int p = p0 + i * share;
           ml[i] = make_float2(kNoMax, 0.f);
           if (p < parts) {
-            const int w = owner + p, stream = w >= n_cta;          // wide: never
-            const size_t slot = ((size_t)(w - stream * n_cta) * 2 + (p == 0 ? 1 : 0)) * kUnitRows + stream * 128 + r;
+            const size_t slot = ((size_t)(owner + p) * 2 + (p == 0 ? 1 : 0)) * kUnitRows + r;
             ml[i] = work.ml[slot];
             if (E == 4) *reinterpret_cast<float4*>(y[i]) = *reinterpret_cast<const float4*>(work.part + slot * D + lane * 4);
             else *reinterpret_cast<float2*>(y[i]) = *reinterpret_cast<const float2*>(work.part + slot * D + lane * 2);
@@ -1206,26 +1497,25 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocksPerSm) tree_attn_j
 
 // ------------------------------------------------------------------ host side
 
-// [pages, heads, page, D] cache -> 4-D tensor map with a (64 columns x page rows, 128 at most) box, 128-byte swizzle.
-bool make_cache_map(CUtensorMap* m, const PagedCache& c, int d, int page, int heads, int pages) {
+// [pages, heads, page, D] cache -> tensor map of 64 columns, 8 rows, D / 64, the page's groups of 8 rows, and heads and pages
+// together; a box is all of a page (of 128 of its rows), 128-byte swizzle.
+bool make_cache_map(CUtensorMap* m, const PagedCache& c, int d, int page, const CacheSteps& steps) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
-  // the stride of a size-1 dimension is never used, but the encoder wants a valid one
-  const cuuint64_t any = (cuuint64_t)d * 2;
-  cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)page, (cuuint64_t)heads, (cuuint64_t)pages};
-  cuuint64_t strides[3] = {(cuuint64_t)c.s_tok * 2, heads > 1 ? (cuuint64_t)c.s_head * 2 : any, pages > 1 ? (cuuint64_t)c.s_page * 2 : any};
-  cuuint32_t box[4] = {64, (cuuint32_t)(page < kTile ? page : kTile), 1, 1};
-  cuuint32_t estr[4] = {1, 1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, c.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  cuuint64_t dims[5] = {64, 8, (cuuint64_t)d / 64, (cuuint64_t)page / 8, (cuuint64_t)steps.extent};
+  cuuint64_t strides[4] = {(cuuint64_t)c.s_tok * 2, 128, (cuuint64_t)c.s_tok * 16, (cuuint64_t)steps.unit * 2};
+  cuuint32_t box[5] = {64, 8, (cuuint32_t)d / 64, (cuuint32_t)(page < kTile ? page : kTile) / 8, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, c.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D>
 cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
   CUtensorMap tk, tv;
-  if (!make_cache_map(&tk, a.kc, D, 1 << a.page_log2, a.hkv, a.n_pages) || !make_cache_map(&tv, a.vc, D, 1 << a.page_log2, a.hkv, a.n_pages))
-    return cudaErrorInvalidValue;
   Work w;
+  if (!cache_steps(a.kc, a.hkv, a.n_pages, &w.k) || !cache_steps(a.vc, a.hkv, a.n_pages, &w.v)) return cudaErrorInvalidValue;
+  if (!make_cache_map(&tk, a.kc, D, 1 << a.page_log2, w.k) || !make_cache_map(&tv, a.vc, D, 1 << a.page_log2, w.v)) return cudaErrorInvalidValue;
   const size_t slots = (size_t)n_cta * 2 * kUnitRows;
   w.part = static_cast<float*>(ws);
   w.ml = reinterpret_cast<float2*>(w.part + slots * 128);
@@ -1242,7 +1532,7 @@ cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
 }  // namespace
 
 size_t tree_attn_workspace_bytes(int n_sm) {
-  return (size_t)n_sm * (2 * kUnitRows * (128 * sizeof(float) + sizeof(float2)) + 2 * sizeof(Meta));
+  return (size_t)n_sm * (2 * kUnitRows * (128 * sizeof(float) + sizeof(float2)) + sizeof(Meta));
 }
 
 cudaError_t launch_tree_attn(const TreeAttnArgs& a, void* ws, int n_sm, cudaStream_t s) {

@@ -59,6 +59,17 @@ def test_tree_attn_refusals(lib, over, code):
     assert attn(lib, **over) == code
 
 
+@pytest.mark.parametrize("pages,s_page,s_head,code", [
+    (1 << 26, 2 * 1024 + 8, 1024, UNS),                  # strides with no common divisor but 8: 2^26 x 257 steps
+    (1 << 22, 8 * ((1 << 27) + 1), 1024, UNS), (2, 8 * ((1 << 33) + 1), 8 * (1 << 33), UNS),
+    (1 << 22, 2 * 1024 + 64, 1024, 0), (1 << 26, 2 * 1024, 1024, 0), (1, 8, 1 << 45, 0), (1 << 26, 64, 1 << 32, 0),
+])
+def test_tree_attn_cache_strides(lib, pages, s_page, s_head, code):
+    """Heads and pages have to fit 31 bits in steps of their strides' greatest common divisor (no request: nothing launched)."""
+    c = view((pages, 2, 16, 64), (s_page, s_head, 64, 1))
+    assert attn(lib, kc=c, vc=c, n=0 if code == 0 else 3) == code
+
+
 def rope(lib, **over):
     freq = (ctypes.c_double * 32)(*[10000.0 ** (-i / 32) for i in range(32)])
     a = dict(ctx=CTX, q=view((1, 4, 5, 64)), k=view((1, 2, 5, 64)), v=view((1, 2, 5, 64)), qw=None, kw=None, eps=1e-6, freq=ctypes.addressof(freq), n=32,

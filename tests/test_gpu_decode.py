@@ -611,3 +611,27 @@ def test_prompt_then_tree_steps(binding):
         back = [p for p in row[used:] if p >= 0]
         table[0, used:] = -1
         free = torch.cat([free, i32(back)]).contiguous()
+
+
+@pytest.mark.parametrize("rise", [40.0, -40.0, 400.0], ids=["climbing", "falling", "far"])
+@pytest.mark.parametrize("hq,hkv,d,reqs", [(4, 2, 128, [(700, 10), (1, 20)]), (8, 1, 64, [(513, 16), (300, 3)]), (4, 4, 128, [(260, 17)]), (2, 2, 64, [(700, 1), (200, 16)])])
+def test_tree_attn_logits_far_from_the_first_tiles(attn_ctx, hq, hkv, d, reqs, rise):
+    """Logits that move by `rise` from each 128 keys to the next, hundreds of nats in all."""
+    s = Step(17, hq, hkv, d, 32, reqs, "tree", 0, "paged")
+    # the first column carries the level
+    s.q[..., 0] = 8.0
+    far = 0.0
+    for b, (p, n) in enumerate(reqs):
+        for x in range(p + n):
+            level = x // 128 * rise
+            far = max(far, abs(level))
+            s.k[s.table[b, x // 32], :, x % 32, 0] = float(torch.tensor(level * np.sqrt(d) / 8).to(torch.bfloat16))
+    s.qd, s.kd = dev(s.q).transpose(0, 1), dev(s.k)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    out = host(s.out)
+    # an fp32 sum of d terms of which one is `far` sqrt(d): off by d 2^-23 far nats at most (truncation counted, scaled), and
+    # the weights by as much of themselves
+    off = d * 2.0 ** -23 * far
+    for h, rows, want, want_lse, tol in s.reference():
+        assert np.all(np.abs(out[h, rows] - want) <= tol + 2 * off * np.abs(s.v).max())

@@ -4,12 +4,14 @@
 //   out_r = sum_c p_rc v_c / sum_c p_rc,  p_rc = 2^(scale q_r.k_c - m_r) over the visible keys c.
 //
 // The rows of a unit are the new tokens of one request times the query heads that share a KV head (row = token * group +
-// head), so that every key and value is read once for all of them.  Work is counted in steps: one for the unit (request,
-// KV head, rows) and one for each of its key tiles of 128.  The steps of all units stand in one line, which is cut into one
-// equal run per SM wherever that falls; a unit that is cut leaves partial results (unnormalised sums, references, weights)
-// that a second kernel joins in the order of the keys.  All lengths are read on the device: a prefix sum over the requests
-// tells each CTA where its run begins.  (Without the step for the unit itself the CTAs with many short requests finish
-// late: 256 chats of 60 to 4000 tokens 243 us instead of 196.)
+// head), so that every key and value is read once for all of them.  Work is counted in steps: one for each key tile of 128
+// of a unit (request, KV head, rows), and some for the unit itself: two if it is narrow, four otherwise (see below).  The
+// steps of all units stand in one line, which is cut into one equal run per SM wherever that falls; a unit that is cut
+// leaves partial results (unnormalised sums, references, weights) that a second kernel joins in the order of the keys.  All
+// lengths are read on the device: a prefix sum over the requests tells each CTA where its run begins.  (With too few steps
+// for the unit itself the CTAs with many short requests finish late, with too many those with long ones.  256 chats of 60 to
+// 4000 tokens and a new one each: 243, 200, 171, 173, 180, 194 us for 0, 1, 2, 3, 4, 6 steps; with trees of 8: 306, 255, 227,
+// 219, 236 us for 1, 2, 3, 4, 6.)
 //
 // What bounds it: the cache's bytes.  A tile is 64 KB (head_dim 128), 2700 cycles of an SM's share of the measured HBM
 // rate; its matrix products take 1020 cycles of the tensor core for up to 128 rows (it takes 128 rows at a time, however
@@ -19,15 +21,18 @@
 //   warps 0-7       softmax and epilogue, two groups of four: thread = TMEM lane = row
 //   warp 8          producer: page ids from the table, TMA loads of K and V pages into a ring of tile slots, in the order
 //                   in which the products need them, K `lead` tiles ahead of V
-//   warp 9          issuer (one thread): S = Q K^T and O += P V
+//   warps 9, 11     issuers (one thread each; warp 11 in wide units only): S = Q K^T and O += P V
 //   warp 10         loader: walks the run, publishes units, gathers their Q rows into shared memory
 //
 // Three modes, by the largest number of rows that any request has:
 //
-// Wide (more than 128): units have up to 256 rows, the groups are their halves and walk the same tiles, each with its S and
-// its O in TMEM (128 columns each: all there is).  P takes the place of S, so a group's next S has to wait for its product
-// with V: softmax, product, next S, one after the other, and the two groups' chains overlap.  The reference maximum moves,
-// to a whole number, when the row maximum has grown by more than 2^8; O in TMEM is then rescaled (exactly).
+// Wide (more than 128): units have up to 256 rows, the groups are their halves and walk the same tiles 64 keys at a time,
+// each with its O and two S of 64 columns in TMEM (all there is), so that the next S is computed during the softmax of this
+// one.  The reference maximum moves, to a whole number, when the row maximum has grown by more than 2^8; O in TMEM is then
+// rescaled (exactly).  The tensor core's operands bound it: 128 rows of Q for 64 keys are 6 KB of shared memory for each
+// product of 48 cycles, 2500 cycles a tile in all, and the two groups' chains do not fill the gaps: 4000 a tile.  (With one
+// S of 128 columns each: 5 % slower.  Two CTAs, a half each, on the same tiles: 208 us instead of 161 for 128K keys, L2 does
+// not serve both at the rate of HBM.)
 //
 // Tall (17 to 128): one O, three S in turn, and the groups take the tiles in turn.  S of the next tiles is computed while
 // both groups are in their softmax, so nothing waits for anything but the bytes.  One O means one reference for both
@@ -66,9 +71,10 @@ using namespace tc;
 
 constexpr int kTile = 128;                       // keys of a tile
 constexpr int kUnitRows = 256;
-constexpr int kThreads = 352, kWarps = kThreads / 32;
-constexpr int kProducer = 8, kIssuer = 9, kLoader = 10;
+constexpr int kThreads = 384, kWarps = kThreads / 32;
+constexpr int kProducer = 8, kIssuer = 9, kLoader = 10, kIssuer1 = 11;
 constexpr int kUnitRing = 4;
+constexpr int kNarrowSteps = 2, kTallSteps = 4;  // steps of a unit besides those of its tiles (narrow; tall and wide)
 constexpr int kNarrowRows = 16;
 enum Mode { kNarrow, kTall, kWide };
 constexpr float kNoMax = -1e30f;                 // reference maximum before any visible key: finite, below any logit
@@ -90,8 +96,8 @@ struct Plan {
   static constexpr int NQ_BYTES = kNarrowRows / 8 * GROUP, SUM_OFF = 2 * NQ_BYTES;
   static constexpr int SUM_ROWS = 4, SUM_STRIDE = D + 8;                  // rows exchanged at a time; 8 columns more against bank conflicts
   static_assert(SLOT == QHALF && SUM_OFF + 8 * SUM_ROWS * SUM_STRIDE * 4 <= QHALF, "");
-  // full and free: tiles; S, P: wide per group, tall per buffer; PV: wide per group; REF, OFULL, OFREE: tall
-  static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + NSLOTS, BAR_S = BAR_FREE + NSLOTS, BAR_P = BAR_S + 3, BAR_PV = BAR_P + 3, BAR_REF = BAR_PV + 2,
+  // full and free: tiles; S, P: tall per buffer, wide [group][buffer], and PV likewise; REF, OFULL, OFREE: tall
+  static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + NSLOTS, BAR_S = BAR_FREE + NSLOTS, BAR_P = BAR_S + 4, BAR_PV = BAR_P + 4, BAR_REF = BAR_PV + 4,
                        BAR_OFULL = BAR_REF + 1, BAR_OFREE = BAR_OFULL + 1, BAR_QFULL = BAR_OFREE + 1, BAR_QFREE = BAR_QFULL + 2,
                        BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + kUnitRing, BARS = BAR_UFREE + kUnitRing;
   static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;
@@ -173,6 +179,18 @@ __device__ __forceinline__ uint32_t mbar_test3(uint32_t b0, uint32_t par0, uint3
       : "r"(b0), "r"(par0), "r"(b1), "r"(par1), "r"(b2), "r"(par2)
       : "memory");
   return r0 | r1 | r2;
+}
+__device__ __forceinline__ uint32_t mbar_test2(uint32_t b0, uint32_t par0, uint32_t b1, uint32_t par1) {
+  uint32_t r0, r1;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%2], %3;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 q, [%4], %5;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\tselp.u32 %1, 2, 0, q;\n\t}"
+      : "=r"(r0), "=r"(r1)
+      : "r"(b0), "r"(par0), "r"(b1), "r"(par1)
+      : "memory");
+  return r0 | r1;
 }
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
   asm volatile(
@@ -282,10 +300,10 @@ __device__ __noinline__ void rescale_tmem(uint32_t t_o, uint32_t t_s, float alph
 
 // The logits of the keys that a row does not see are set to -infinity in TMEM before the common path reads them.  Called
 // by whole warps; a row that is not the unit's (token < 0) sees nothing.  Whether the row sees any of the tile's keys.
-__device__ __noinline__ bool mask_tmem(const TreeAttnArgs& a, const Unit& u, int token, int k0, uint32_t t_s) {
+__device__ __noinline__ bool mask_tmem(const TreeAttnArgs& a, const Unit& u, int token, int k0, int keys, uint32_t t_s) {
   uint32_t any = 0;
 #pragma unroll 1
-  for (int c = 0; c < kTile / 32; ++c) {
+  for (int c = 0; c < keys / 32; ++c) {
     const uint32_t seen = token >= 0 ? seen32(a, u, token, k0 + c * 32) : 0u;
     any |= seen;
     if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
@@ -627,10 +645,10 @@ __device__ __forceinline__ float weights(const uint32_t (&s)[32], float scale, f
   return (sum01.x + sum01.y) + (sum23.x + sum23.y);
 }
 
-// The issuer: one thread.  (The long loops are functions of their own: in one body each pays for the others' registers, 10 us
+// The issuer of the tall mode: one thread.  (The long loops are functions of their own: in one body each pays for the others' registers, 10 us
 // of 180 for 128K keys and a tree of 64.)
-template <int D, Mode MODE>
-__device__ __noinline__ void issue_products(const TreeAttnArgs& a, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
+template <int D>
+__device__ __noinline__ void issue_tall(const TreeAttnArgs& a, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
   using P = Plan<D>;
   const uint32_t base = smem_u32(smem);
   auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
@@ -678,7 +696,6 @@ __device__ __noinline__ void issue_products(const TreeAttnArgs& a, uint8_t* smem
     for (int kk = 0; kk < kTile / 16; ++kk)
       mma_ts_lo<D>(tmem + o_col, tmem + P::S_COL + col + kk * 8, dv + kk * (2 * P::GROUP >> 4), idesc_pv, kk > 0 || !first);
   };
-  if constexpr (MODE == kTall) {
   // Tall.  S of tile i in buffer i % 3, computed up to three tiles ahead of its product with V.
   uint32_t n_qk = 0, n_pv = 0, q_buf = 0, p_buf = 0, p_phase = 0;
   uint32_t k_slot = 0, v_slot = v_pos(0, n_tiles_cta, kTallLead) % P::SLOTS, k_at = 0, v_at = v_pos(0, n_tiles_cta, kTallLead);
@@ -757,74 +774,111 @@ __device__ __noinline__ void issue_products(const TreeAttnArgs& a, uint8_t* smem
     const uint32_t uses = (seq + 1 - i) / 2;
     if (uses > 0) mbar_wait(bar(P::BAR_QFREE + i), (uses - 1) & 1, ab, 62);
   }
-  } else {
-  // Wide.  The groups' chains are independent of one another but for the tiles; a group's next S is computed when its
-  // last P has gone into its product.
-  struct Group {
-    uint32_t n_qk, n_pv;                         // products issued
-    uint32_t left, k_at, k_slot, v_at, v_slot;   // tiles left in the unit; ring positions of the next K and V tile
-    uint32_t seq;                                // units taken
-    bool first, q_here;                          // the next O opens a sum; the unit's Q has been seen
-  } gr[2];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    gr[x].n_qk = gr[x].n_pv = gr[x].left = gr[x].seq = gr[x].k_at = gr[x].k_slot = 0;
-    gr[x].v_at = v_pos(0, n_tiles_cta, kWideLead); gr[x].v_slot = gr[x].v_at % P::SLOTS;
-    gr[x].first = gr[x].q_here = false;
-  }
+}
+
+// The issuer of a wide unit's group x (there are two such threads).  Keys come 64 at a time here: S of 128 rows is 64 columns,
+// and each group has two of them, so that the next S is computed during the softmax of this one.
+template <int D>
+__device__ __noinline__ void issue_wide(const TreeAttnArgs& a, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta, uint32_t x) {
+  using P = Plan<D>;
+  const uint32_t base = smem_u32(smem);
+  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  volatile int* abort_flag = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8) + 1;
+  constexpr uint32_t idesc_qk = instr_desc(128, kTile / 2, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
+  const uint32_t d_q = (uint32_t)smem_desc(base, 16, P::GROUP), d_k = (uint32_t)smem_desc(base + P::RING_OFF, 16, P::GROUP),
+                 d_v = (uint32_t)smem_desc(base + P::RING_OFF, P::BOX, P::GROUP);
+  uint32_t arrived = 0, a_slot = 0, a_phase = 0, polls = 0;
+  long long idle_since = 0;
+  auto arrival = [&] {
+    ++arrived;
+    if (++a_slot == P::SLOTS) { a_slot = 0; a_phase ^= 1; }
+  };
+  auto stalled = [&](bool moved) {                 // true: give up
+    if (moved) {
+      idle_since = 0;
+      polls = 0;
+      return false;
+    }
+    if ((++polls & 63u) != 0u) return false;
+    if (*abort_flag) return true;
+    if ((polls & 4095u) != 0u) return false;
+    const long long now = clock64();
+    if (idle_since == 0) idle_since = now;
+    else if (now - idle_since > kWaitCycles) {
+      *abort_flag = 1;
+      if (atomicCAS(a.status, 0, (int)SP_ERR_TIMEOUT) == 0) a.status[1] = 60;
+      return true;
+    }
+    return false;
+  };
+  const uint32_t s_col = P::S_COL + x * 128, o_col = P::O_COL + x * P::O_STEP, n = 2 * n_tiles_cta, lead = kWideLead;
+  const uint32_t dq = d_q + x * (P::QHALF >> 4);
+  constexpr uint32_t half = kTile / 2 / 8 * P::GROUP >> 4;          // from the first 64 keys of a tile to the others
+  uint32_t n_qk = 0, n_pv = 0, left = 0, seq = 0;      // products issued; halves left of the unit; units taken
+  uint32_t k_at = 0, k_slot = 0, v_at = v_pos(0, n_tiles_cta, lead), v_slot = v_at % P::SLOTS;
+  uint32_t first = 0;                                  // bit b: what is in buffer b opens its unit's sum
+  bool q_here = false, fresh = false;
   auto advance = [&](uint32_t& at, uint32_t& slot, uint32_t to) {
     slot += to - at;
     at = to;
     if (slot >= P::SLOTS) slot -= P::SLOTS;
   };
-  while (gr[0].n_pv != n_tiles_cta || gr[1].n_pv != n_tiles_cta) {
+  while (n_pv != n) {
     bool moved = false;
-    const uint32_t polled = mbar_test3(bar(P::BAR_P), gr[0].n_pv & 1, bar(P::BAR_P + 1), gr[1].n_pv & 1, bar(P::BAR_FULL + a_slot), a_phase);
-    if ((polled & 4) && arrived != 2 * n_tiles_cta) {
+    const uint32_t polled = mbar_test2(bar(P::BAR_P + 2 * x + (n_pv & 1)), (n_pv >> 1) & 1, bar(P::BAR_FULL + a_slot), a_phase);
+    if ((polled & 2) && arrived != n) {
       arrival();
       moved = true;
     }
+    if (n_qk != n_pv && v_at < arrived && (polled & 1)) {
+      const uint32_t b = n_pv & 1, dv = d_v + v_slot * (P::SLOT >> 4) + b * half;
+      const bool opens = (first >> b) & 1;
+      tc_fence_after();
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      Group& t = gr[x];
-      if (t.n_qk != t.n_pv && t.v_at < arrived && ((polled >> x) & 1)) {
-        tc_fence_after();
-        issue_pv(P::O_COL + x * P::O_STEP, x * 128, t.v_slot, t.first);
-        mma_commit(bar(P::BAR_PV + x));
-        mma_commit(bar(P::BAR_FREE + t.v_slot));
-        ++t.n_pv;
-        t.first = false;
-        advance(t.v_at, t.v_slot, v_pos(t.n_pv, n_tiles_cta, kWideLead));
-        moved = true;
+      for (int kk = 0; kk < kTile / 32; ++kk)
+        mma_ts_lo<D>(tmem + o_col, tmem + s_col + b * 64 + kk * 8, dv + kk * (2 * P::GROUP >> 4), idesc_pv, kk > 0 || !opens);
+      mma_commit(bar(P::BAR_PV + 2 * x + b));
+      if (b == 1) {
+        mma_commit(bar(P::BAR_FREE + v_slot));
+        advance(v_at, v_slot, v_pos((n_pv + 1) >> 1, n_tiles_cta, lead));
       }
-      if (t.n_qk == t.n_pv && t.n_qk != n_tiles_cta) {
-        if (t.left == 0) {
-          const uint32_t e = t.seq % kUnitRing;
-          if (mbar_test(bar(P::BAR_UNIT + e), (t.seq / kUnitRing) & 1)) {
-            t.left = units[e].n_tiles;
-            if (x == 1) mbar_arrive(bar(P::BAR_UFREE + e));        // group 0's unit too has been taken, or will before the entry is
-            ++t.seq;
-            t.q_here = false;
-            t.first = true;
-          }
+      ++n_pv;
+      moved = true;
+    }
+    if (n_qk != n && n_qk - n_pv < 2) {
+      if (left == 0) {
+        const uint32_t e = seq % kUnitRing;
+        if (mbar_test(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1)) {
+          left = 2 * units[e].n_tiles;
+          mbar_arrive(bar(P::BAR_UFREE + e));
+          ++seq;
+          q_here = false;
+          fresh = true;
         }
-        if (t.left != 0 && t.k_at < arrived) {
-          if (!t.q_here) t.q_here = mbar_test(bar(P::BAR_QFULL + x), (t.seq - 1) & 1);
-          if (t.q_here) {
-            tc_fence_after();
-            issue_qk(x * 128, x, t.k_slot);
-            mma_commit(bar(P::BAR_S + x));
-            mma_commit(bar(P::BAR_FREE + t.k_slot));
-            if (--t.left == 0) mma_commit(bar(P::BAR_QFREE + x));
-            ++t.n_qk;
-            advance(t.k_at, t.k_slot, k_pos(t.n_qk, kWideLead));
-            moved = true;
+      }
+      if (left != 0 && k_at < arrived) {
+        if (!q_here) q_here = mbar_test(bar(P::BAR_QFULL + x), (seq - 1) & 1);
+        if (q_here) {
+          const uint32_t b = n_qk & 1, dk = d_k + k_slot * (P::SLOT >> 4) + b * half;
+          tc_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_ss_lo<D>(tmem + s_col + b * 64, dq + (kk >> 2) * (P::BOX >> 4) + (kk & 3) * 2, dk + (kk >> 2) * (P::BOX >> 4) + (kk & 3) * 2, idesc_qk, kk > 0);
+          mma_commit(bar(P::BAR_S + 2 * x + b));
+          if (--left == 0) mma_commit(bar(P::BAR_QFREE + x));
+          if (b == 1) {
+            mma_commit(bar(P::BAR_FREE + k_slot));
+            advance(k_at, k_slot, k_pos((n_qk + 1) >> 1, lead));
           }
+          first = fresh ? first | 1u << b : first & ~(1u << b);
+          fresh = false;
+          ++n_qk;
+          moved = true;
         }
       }
     }
     if (stalled(moved)) break;
-  }
   }
 }
 
@@ -845,19 +899,19 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
   // The V of a tile with masked keys: what lies behind the sequence counts as zero, and so do non-finite values of new
   // tokens (see add_nonfinite).  V comes after K, hence not before the softmax.  S of the tile was there, so every tile up
   // to its K has arrived, the one before V in V's slot among them: the barrier's parity can be told.
-  auto clean = [&](uint32_t j, const Unit& u, int k0, int no_mask, int seq) {
+  auto clean = [&](uint32_t j, const Unit& u, int k0, int half, int no_mask, int seq) {
     const uint32_t p = v_pos(j, n_tiles_cta, kWideLead), s = p % P::SLOTS;
     const bool here = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FULL + s), (p / P::SLOTS) & 1, ab, 32));
-    // each warp of the group 32 keys
-    const int lo = max(no_mask - k0, (warp & 3) * 32);
-    if (here && lo < (warp & 3) * 32 + 32)
-      clean_values<D>(reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane, lo, (warp & 3) * 32 + 32, u.len - k0, bad_tag, seq + 1);
+    // each warp of the group 16 keys
+    const int from = half * 64 + (warp & 3) * 16, lo = max(no_mask - k0, from);
+    if (here && lo < from + 16)
+      clean_values<D>(reinterpret_cast<uint32_t*>(smem + P::RING_OFF + s * P::SLOT) + lane, lo, from + 16, u.len - k0, bad_tag, seq + 1);
     fence_async_smem();
     return here;
   };
   bool ok = true;
   uint32_t done = 0;                                // tiles of earlier units
-  const uint32_t t_s = lanes + P::S_COL + x * 128, t_o = lanes + P::O_COL + x * P::O_STEP;
+  const uint32_t t_o = lanes + P::O_COL + x * P::O_STEP;
   for (int seq = 0; ok; ++seq) {
     const int e = seq % kUnitRing;
     ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
@@ -870,20 +924,21 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
     const int token = (u.r0 + my_row) / a.group;
     const int kt0 = u.kt0, no_mask = min(u.past, u.len);      // keys before it are seen by every row
     float m_ref = live ? kNoMax : -kNoMax, l = 0.f;           // lanes without a row: all weights zero
-    for (int t = 0; t < n_tiles && ok; ++t) {
-      const int k0 = (kt0 + t) * kTile;
-      const bool special = k0 + kTile > no_mask;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + x), (done + t) & 1, ab, 31));
+    for (int t = 0; t < 2 * n_tiles && ok; ++t) {
+      const int k0 = (kt0 + (t >> 1)) * kTile, half = t & 1;      // half a tile in buffer `half`
+      const uint32_t t_s = lanes + P::S_COL + x * 128 + half * 64, phase = (done + (t >> 1)) & 1;
+      const bool special = k0 + half * 64 + 64 > no_mask;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + 2 * x + half), phase, ab, 31));
       if (!ok) break;
       tc_fence_after();
       if (warp_live) {
-        // Four chunks of 32 logits, the next one's load in flight, each a step of the running softmax
-        if (special) mask_tmem(a, u, live ? token : -1, k0, t_s);
+        // Two chunks of 32 logits, the next one's load in flight, each a step of the running softmax
+        if (special) mask_tmem(a, u, live ? token : -1, k0 + half * 64, 64, t_s);
         uint32_t s[2][32];
         float sum = 0.f;
         tmem_ld32_async(t_s, s[0]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
           tmem_ld_wait();
           reg_fence32(s[c & 1]);
           const uint32_t* y = s[c & 1];
@@ -904,14 +959,19 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
           if (__any_sync(0xffffffffu, grown)) {
             const float m_new = grown ? ceilf(mx) : m_ref;
             const float alpha = ex2_approx(m_ref - m_new);
-            // the group's previous product came before this S, and nothing of this P has been handed over
+            // nothing of this P has been handed over; the product of the P before it has to be in O (those before that are:
+            // their buffer is this S's, and the barrier's parity can be told)
+            if (t > 0) {
+              ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + 2 * x + (half ^ 1)), half ? phase : phase ^ 1, ab, 35));
+              tc_fence_after();
+            }
             rescale_tmem<D>(t_o, t_s, alpha, c, t > 0);
             l *= alpha;
             sum *= alpha;
             m_ref = m_new;
           }
           // not before the call above: its registers must not be moved while the load is under way
-          if (c < 3) tmem_ld32_async(t_s + (c + 1) * 32, s[(c + 1) & 1]);
+          if (c < 1) tmem_ld32_async(t_s + 32, s[1]);
           uint32_t p[16];
           sum += weights(s[c & 1], scale, m_ref, p);
           tmem_st16(t_s + c * 16, p);
@@ -919,12 +979,12 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
         l += sum;
         tmem_wait_st();
       }
-      if (special) ok = clean(done + t, u, k0, no_mask, seq);
+      if (special && ok) ok = clean(done + (t >> 1), u, k0, half, no_mask, seq);
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_P + x));
+      if (lane == 0) mbar_arrive(bar(P::BAR_P + 2 * x + half));
     }
-    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + x), (done + n_tiles - 1) & 1, ab, 33));
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_PV + 2 * x + 1), (done + n_tiles - 1) & 1, ab, 33));
     if (ok && warp_live) {
       tc_fence_after();
       const Place p = place_of(a, u, my_row);
@@ -1001,7 +1061,7 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
       ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + buf), (i / 3) & 1, ab, 31));
       if (!ok) break;
       tc_fence_after();
-      if (warp_live) saw |= special ? mask_tmem(a, u, live ? token : -1, k0, t_s) : true;
+      if (warp_live) saw |= special ? mask_tmem(a, u, live ? token : -1, k0, kTile, t_s) : true;
       if (t == 0) {
         if (warp_live) refs[row] = first_reference(t_s, scale, live);
         __syncwarp();
@@ -1131,47 +1191,48 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
     fence_async_smem();
   }
+  const int own = narrow ? kNarrowSteps : kTallSteps;         // a unit's steps besides its tiles'
   long long before_t = incl_t - mine_t, before_u = incl_u - mine_u, total_t = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
     if (w < warp) { before_t += scan[w]; before_u += scan[kWarps + w]; }
     total_t += scan[w];
-    total += scan[w] + scan[kWarps + w];
+    total += scan[w] + own * scan[kWarps + w];
   }
   const long long quota = divide(total, n_cta), extra = total - quota * n_cta;      // the first `extra` runs are one step longer
   auto run_begin = [&](int w) { return w * quota + min((long long)w, extra); };
   for (int end = 0; end < 2; ++end) {
     const long long w = run_begin(cta + end);
-    long long step = before_t + before_u, tile = before_t;
+    long long step = before_t + own * before_u, tile = before_t;
     if (w >= total) {
       if (threadIdx.x == 0) tiles_at[end] = total_t;
-    } else if (step <= w && w < step + mine_t + mine_u) {
+    } else if (step <= w && w < step + mine_t + own * mine_u) {
       for (int b = b_lo; b < b_hi; ++b) {
         const Request q = request(a, b);
         const long long n = units_of(a, q);
-        if (w < step + n * (q.kt + 1)) {
-          const long long rem = w - step, nth = divide(rem, q.kt + 1), in = rem - nth * (q.kt + 1);
-          tiles_at[end] = tile + nth * q.kt + max(in - 1, 0ll);
+        if (w < step + n * (q.kt + own)) {
+          const long long rem = w - step, nth = divide(rem, q.kt + own), in = rem - nth * (q.kt + own);
+          tiles_at[end] = tile + nth * q.kt + max(in - own, 0ll);
           if (end == 0) { *start_b = b; *start_rem = rem; }
           break;
         }
-        step += n * (q.kt + 1);
+        step += n * (q.kt + own);
         tile += n * q.kt;
       }
     }
   }
   auto init_barriers = [&](bool wide) {
     for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(bar(P::BAR_S + i), 1);
       mbar_init(bar(P::BAR_P + i), 4);
+      mbar_init(bar(P::BAR_PV + i), 1);
     }
-    for (int x = 0; x < 2; ++x) mbar_init(bar(P::BAR_PV + x), 1);
     mbar_init(bar(P::BAR_REF), 4);
     mbar_init(bar(P::BAR_OFULL), 1);
     mbar_init(bar(P::BAR_OFREE), 8);
     // who lets a tile go: the issuer once, or (wide) for each group, or the eight warps; likewise the queries, which come
-    // from 32 lanes' copies when narrow; a unit is read by the eight warps, the producer and the issuer, if it has work
+    // from 32 lanes' copies when narrow; a unit is read by the eight warps, the producer and the issuers, if it has work
     for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FREE + s), narrow ? 8 : wide ? 2 : 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(bar(P::BAR_QFULL + x), narrow ? 32 : 1);
@@ -1179,7 +1240,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     }
     for (int e = 0; e < kUnitRing; ++e) {
       mbar_init(bar(P::BAR_UNIT + e), 1);
-      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : 10);
+      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : wide ? 11 : 10);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   };
@@ -1203,17 +1264,17 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
         const long long w1 = run_begin(cta + 1);
         Request q = request(a, b);
         while (w < w1 && ok) {
-          while (rem >= units_of(a, q) * (q.kt + 1) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
-          if (rem >= units_of(a, q) * (q.kt + 1)) break;       // not reached while the lengths stand still
+          while (rem >= units_of(a, q) * (q.kt + own) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
+          if (rem >= units_of(a, q) * (q.kt + own)) break;       // not reached while the lengths stand still
           Unit u;
           const int n_pass = passes(a, q), all_rows = q.n * a.group;
-          const int nth = (int)divide(rem, q.kt + 1), in = (int)(rem - (long long)nth * (q.kt + 1));       // step of the unit: tile `in - 1`
-          const int take = (int)min((long long)(q.kt + 1 - in), w1 - w);
+          const int nth = (int)divide(rem, q.kt + own), in = (int)(rem - (long long)nth * (q.kt + own));       // step of the unit: tile `in - own`
+          const int take = (int)min((long long)(q.kt + own - in), w1 - w);
           w += take;
           rem += take;
-          u.kt0 = max(in - 1, 0);
+          u.kt0 = max(in - own, 0);
           u.kt_all = q.kt;
-          u.n_tiles = in + take - 1 - u.kt0;
+          u.n_tiles = max(in + take - own, 0) - u.kt0;
           if (u.n_tiles == 0) continue;                // only the unit's own step: its tiles are the next CTA's
           u.g = n_pass == 1 ? nth : nth / n_pass;
           u.b = b;
@@ -1229,7 +1290,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
             units[e] = u;
             mbar_arrive(bar(P::BAR_UNIT + e));
             if (u.kt0 == 0 && u.n_tiles < u.kt_all) {
-              const long long z = w - take - in + u.kt_all, cut = extra * (quota + 1);     // the step of the unit's last tile
+              const long long z = w - take - in + own - 1 + u.kt_all, cut = extra * (quota + 1);     // the step of the unit's last tile
               Meta m{(int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota)), u.start, u.r0, u.rows, u.g, {0, 0, 0}};
               work.meta[cta] = m;
             }
@@ -1342,11 +1403,9 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
           while (laps > 0 && !mbar_test(bar(P::BAR_FULL + i), (laps - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {}
         }
       }
-    } else if (warp == kIssuer) {
-      if (lane == 0 && !narrow) {
-        if (wide) issue_products<D, kWide>(a, smem, ab, tmem, n_tiles_cta);
-        else issue_products<D, kTall>(a, smem, ab, tmem, n_tiles_cta);
-      }
+    } else if (warp == kIssuer || warp == kIssuer1) {
+      if (lane == 0 && wide) issue_wide<D>(a, smem, ab, tmem, n_tiles_cta, warp == kIssuer1);
+      else if (lane == 0 && !narrow && warp == kIssuer) issue_tall<D>(a, smem, ab, tmem, n_tiles_cta);
       __syncwarp();
     } else if (narrow) {
       narrow_warps<D>(a, work, smem, ab);

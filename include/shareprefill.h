@@ -551,7 +551,7 @@ int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const s
  *   q            [1, n_q_heads, rows, head_dim], any strides as for sp_qk_norm_rope;
  *                n_q_heads a multiple of the cache's heads, at most 128.
  *   tree_mask    device u32 [rows, mask_words], mask_words in 1 .. 8, or NULL.
- *   out          like q, its own strides.
+ *   out          like q, its own strides; it must not overlap q or the cache.
  *   lse_out      device fp32 [n_q_heads, rows]: natural-log-sum-exp of the scaled logits
  *                of each row's visible keys, or NULL.
  */

@@ -173,6 +173,7 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
   if (n_req == 0) return SP_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
+  if (q->data == out->data) return SP_ERR_INVALID_ARG;         // in place: a run may be walked twice
   TreeAttnArgs a;
   memset(&a, 0, sizeof(a));
   a.q = static_cast<const __nv_bfloat16*>(q->data);

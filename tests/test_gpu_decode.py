@@ -635,3 +635,119 @@ def test_tree_attn_logits_far_from_the_first_tiles(attn_ctx, hq, hkv, d, reqs, r
     off = d * 2.0 ** -23 * far
     for h, rows, want, want_lse, tol in s.reference():
         assert np.all(np.abs(out[h, rows] - want) <= tol + 2 * off * np.abs(s.v).max())
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 32)])
+@pytest.mark.parametrize("n", [16, 17, 128, 129, 256, 257])
+def test_tree_attn_row_counts_at_the_modes_edges(attn_ctx, n, d, page):
+    """One query head per key head: n rows of a long and of a short request, the runs cut across both."""
+    s = Step(n, 2, 2, d, page, [(1500, n), (0, min(n, 5)), (129, 1)], "tree" if n <= 256 else "chain", 1, "paged")
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    s.check()
+
+
+def test_tree_attn_first_call_inside_a_capture(binding):
+    """The workspace cannot be allocated there: an error, nothing enqueued; with the workspace reserved the call is captured."""
+    ctx = binding.Context()
+    s = Step(3, 4, 2, 64, 16, [(40, 3)])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(binding.SpError) as e:
+            s.call(ctx)
+        s.lse.add_(0)
+    assert e.value.code == -3 and bool((s.out == 9).all())
+    ctx.reserve_decode()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.call(ctx)
+    assert bool((s.out == 9).all())
+    g.replay()
+    clean(ctx)
+    s.check()
+
+
+def test_tree_attn_contexts_on_two_streams(binding):
+    """Two contexts at once, several calls each, one after the other on their streams."""
+    steps = [Step(21, 8, 2, 128, 32, [(700, 9), (3, 1)], "tree"), Step(22, 4, 4, 64, 16, [(300, 1)] * 40)]
+    ctxs, streams = [binding.Context() for _ in steps], [torch.cuda.Stream() for _ in steps]
+    for c in ctxs:
+        c.reserve_decode()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, c, st in zip(steps, ctxs, streams):
+            with torch.cuda.stream(st):
+                s.out.fill_(9)
+                s.lse.fill_(9)
+                s.call(c)
+    for s, c in zip(steps, ctxs):
+        clean(c)
+        s.check()
+
+
+def test_tree_attn_graph_replays_across_the_modes(attn_ctx):
+    """One captured graph, whose replays have a few, a hundred and several hundred rows in a request."""
+    a = Step(31, 8, 2, 64, 16, [(300, 64), (90, 1)], "tree", 0)
+    a.call(attn_ctx)
+    clean(attn_ctx)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        a.call(attn_ctx)
+    for seed, reqs in ((32, [(310, 3), (80, 2)]), (33, [(250, 20), (70, 30)]), (34, [(0, 1), (0, 64)]), (35, [(300, 62), (5, 2)])):
+        pad = a.rows - sum(n for _, n in reqs)
+        b = Step(seed, 8, 2, 64, 16, reqs, "tree", pad)
+        assert b.rows == a.rows and b.k.shape[0] <= a.k.shape[0]
+        a.bits_d.fill_(-1)
+        a.bits_d[:, : b.words].copy_(b.bits_d)
+        a.bits_d[:, b.words:].fill_(0)
+        a.table_d.fill_(2 ** 31 - 1)
+        a.table_d[:, : b.table.shape[1]].copy_(b.table_d[:, : a.table.shape[1]])
+        for name in ("qd", "lens_d", "start_d"):
+            getattr(a, name).copy_(getattr(b, name))
+        a.kd[: b.k.shape[0]].copy_(b.kd)
+        a.vd[: b.k.shape[0]].copy_(b.vd)
+        a.out.fill_(9)
+        a.lse.fill_(9)
+        g.replay()
+        clean(attn_ctx)
+        b.out, b.lse = a.out, a.lse
+        b.check()
+
+
+def test_tree_attn_as_many_requests_as_allowed(attn_ctx):
+    """4096 requests, most of one token, some of none and some empty."""
+    r = random.Random(5)
+    reqs = [(r.choice([0, 1, 15, 16, 40]), r.choice([1, 1, 1, 0])) for _ in range(4096)]
+    s = Step(41, 2, 1, 64, 16, reqs, "chain", 3)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    s.check()
+
+
+@pytest.mark.parametrize("n", [1, 20, 70])
+def test_tree_attn_a_bad_row_stays_its_own(attn_ctx, n):
+    """NaN in one request's queries, and infinities in another's: no other row is touched."""
+    s = Step(51, 4, 2, 128, 32, [(200, n), (300, n), (5, n)], "tree", 0)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    want = s.out.clone()
+    s.qd[:, n // 2, 3] = float("nan")
+    s.qd[:, n + n // 2, 5] = float("inf")
+    s.out.fill_(9)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    rows = [x for x in range(3 * n) if x not in (n // 2, n + n // 2)]
+    # the same but for the reference that a row is given (exact), or for the walk with which a run was done: twice the bound of
+    # a bf16 result
+    assert torch.isfinite(s.out[:, rows].float()).all()
+    assert float((s.out[:, rows].float() - want[:, rows].float()).abs().max()) <= 2.0 ** -6 * float(want.float().abs().max())
+    assert bool(torch.isnan(s.out[:, n // 2].float()).all())
+
+
+def test_tree_attn_in_place_is_refused(binding):
+    s = Step(61, 4, 2, 64, 16, [(20, 3)])
+    before = s.qd.clone()
+    with pytest.raises(binding.SpError) as e:
+        binding.Context().sp_tree_attn(s.qd, s.kd, s.vd, s.table_d, s.lens_d, s.start_d, s.qd)
+    torch.cuda.synchronize()
+    assert e.value.code == -1 and bool((s.qd == before).all())

@@ -45,7 +45,7 @@
 // leaves most lanes empty.  The eight softmax warps are on their own: each takes 16 keys of every tile, S (16 rows x 16
 // keys) and O (16 rows x head) in registers by mma.sync m16n8k16, K and V by ldmatrix from the same ring; their sums are
 // added up at the unit's end.  16 mma.sync for each product and warp are a few hundred cycles of the 2700 that the tile's
-// bytes take.  (256 x 950 tokens: 173 us so, 208 us by tcgen05 with the rows in the lanes, 236 us by tcgen05 with the keys
+// bytes take.  (256 x 950 tokens: 164 us so, 208 us by tcgen05 with the rows in the lanes, 236 us by tcgen05 with the keys
 // in the lanes: MMAs of 16 columns are issued no faster than those of 128.)
 //
 // Masks.  Only tiles that hold a key at or behind the first new token need one.  There the row's visibility bits are

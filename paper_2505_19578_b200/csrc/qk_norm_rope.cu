@@ -18,23 +18,23 @@
 namespace sp {
 namespace {
 
-__device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
+// Arithmetic on pairs of neighbouring elements, one instruction for both.  (With single ones a pass over four heads was 320
+// instructions and the schedulers two thirds busy: 1000 rows of 36 heads 8.9 instead of 7.5 us, 16384 rows 67 instead of 60.)
+__device__ __forceinline__ void unpack8(const uint4& u, float2 (&x)[4]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+  for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+__device__ __forceinline__ uint4 pack8(const float2 (&x)[4]) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    __nv_bfloat162 h = __floats2bfloat162_rn(x[i].x, x[i].y);
     w[i] = *reinterpret_cast<uint32_t*>(&h);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // A pass of a warp: 32 / (D / 16) heads of one token, this lane two pieces of one of them.
 struct Pass {
@@ -100,40 +100,37 @@ template <int D>
 __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln, const Pass& p, bool is_v, bool is_q, int t, int slot, uint4 in0, uint4 in1,
                                             const float (&cs)[8], const float (&sn)[8]) {
   if (!is_v) {                                     // uniform over the warp
-    float x[8], y[8];
+    float2 x[4], y[4];
     unpack8(in0, x);
     unpack8(in1, y);
     const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
     if (weight) {
-      float ss = 0.f;
+      float2 sum = __fmul2_rn(x[0], x[0]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss += x[e] * x[e] + y[e] * y[e];
+      for (int i = 1; i < 4; ++i) sum = __ffma2_rn(x[i], x[i], sum);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum = __ffma2_rn(y[i], y[i], sum);
+      float ss = sum.x + sum.y;
 #pragma unroll
       for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const float inv = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-      float wx[8], wy[8];
+      const float2 inv = both(rsqrtf(ss * (1.f / D) + a.eps));       // 2 ulp of fp32
+      float2 wx[4], wy[4];
       unpack8(__ldg(reinterpret_cast<const uint4*>(weight + ln.c0 * 8)), wx);
       unpack8(__ldg(reinterpret_cast<const uint4*>(weight + ln.c1 * 8)), wy);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { x[e] *= inv * wx[e]; y[e] *= inv * wy[e]; }
+      for (int i = 0; i < 4; ++i) { x[i] = __fmul2_rn(x[i], __fmul2_rn(inv, wx[i])); y[i] = __fmul2_rn(y[i], __fmul2_rn(inv, wy[i])); }
     }
     if (ln.turn0 || ln.turn1) {
       if (a.interleaved) {
+        auto turn = [](float2 v, float c, float s) { return __ffma2_rn(v, both(c), __fmul2_rn(make_float2(v.y, v.x), make_float2(-s, s))); };
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const float xa = x[e], xb = x[e + 1], ya = y[e], yb = y[e + 1];
-          const int i = e / 2, j = 4 + e / 2;
-          x[e] = xa * cs[i] - xb * sn[i];
-          x[e + 1] = xb * cs[i] + xa * sn[i];
-          y[e] = ya * cs[j] - yb * sn[j];
-          y[e + 1] = yb * cs[j] + ya * sn[j];
-        }
+        for (int i = 0; i < 4; ++i) { x[i] = turn(x[i], cs[i], sn[i]); y[i] = turn(y[i], cs[4 + i], sn[4 + i]); }
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float xa = x[e], xb = y[e];
-          x[e] = xa * cs[e] - xb * sn[e];
-          y[e] = xb * cs[e] + xa * sn[e];
+        for (int i = 0; i < 4; ++i) {
+          const float2 xa = x[i], xb = y[i], c = make_float2(cs[2 * i], cs[2 * i + 1]), s = make_float2(sn[2 * i], sn[2 * i + 1]);
+          x[i] = __ffma2_rn(xa, c, __fmul2_rn(xb, make_float2(-s.x, -s.y)));
+          y[i] = __ffma2_rn(xb, c, __fmul2_rn(xa, s));
         }
       }
     }
@@ -202,7 +199,7 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const __grid
   }
 }
 
-// Many rows: one CTA per SM, each warp an equal run of (token, three passes) items, which it fetches three items ahead into
+// Many rows: one CTA per SM, each warp a share of the (token, three passes) items, which it fetches three items ahead into
 // a ring of its own in shared memory (cp.async; a lane reads back only what it has copied, so nothing is synchronised).
 // 16 warps have 144 KB under way then, which registers could not hold.  Four passes, two items ahead: 2 % faster for
 // 131072 rows of 48 heads, 7 % slower for 1000 rows of 36, whose 9 passes do not divide.
@@ -221,41 +218,53 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
   lane_phases(a, lane, f);
   const int pq = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW, pkv = (a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW, passes = pq + 2 * pkv;
   const int per_token = (passes + kStreamRun - 1) / kStreamRun;
-  const long long items = (long long)a.tokens * per_token, n_warps = (long long)gridDim.x * kStreamWarps, me = (long long)blockIdx.x * kStreamWarps + warp;
-  const long long from = items * me / n_warps, to = items * (me + 1) / n_warps;
+  // The warps' tokens (items, if there are fewer tokens than warps) in turn, so that what is read and written at a time lies
+  // together (a run of tokens for each warp: 695 us instead of 640 for 131072 rows).
+  const int n_warps = gridDim.x * kStreamWarps, me = warp * gridDim.x + blockIdx.x, span = a.tokens >= n_warps ? per_token : 1;
+  const int jump_t = span > 1 ? n_warps : n_warps / per_token, jump_b = span > 1 ? 1 - per_token : n_warps % per_token;
+  struct At {                                      // an item
+    int t, b;
+  };
+  auto next = [&](At& x) {
+    if (span > 1 && x.b + 1 < per_token) { ++x.b; return; }
+    x.t += jump_t;
+    x.b += jump_b;
+    if (x.b >= per_token) { x.b -= per_token; ++x.t; }
+  };
   uint8_t* mine = smem + warp * kStreamStages * kStreamItem;
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
   let_next_start();
   wait_for_previous();
   if (decode_poisoned(a.status)) return;
 
-  int ft = (int)(from / per_token), fb = (int)(from - (long long)ft * per_token), fstage = 0;       // the item to fetch next
-  long long fetched = from;
+  const At begin = span > 1 ? At{me, 0} : At{me / per_token, me % per_token};
+  At ahead = begin;                                // the item to fetch next
+  int fstage = 0;
   auto fetch = [&] {
-    if (fetched < to) {
+    if (ahead.t < a.tokens) {
       const uint32_t at = mine_at + fstage * kStreamItem;
 #pragma unroll
       for (int u = 0; u < kStreamRun; ++u) {
-        const Pass p = ln.pass(a, fb * kStreamRun + u);
+        const Pass p = ln.pass(a, ahead.b * kStreamRun + u);
         if (p.kind >= 0) {
-          const __nv_bfloat16* src = ln.source(a, p, ft);
+          const __nv_bfloat16* src = ln.source(a, p, ahead.t);
           copy16(at + u * 1024 + lane * 16, src + ln.c0 * 8);
           copy16(at + u * 1024 + 512 + lane * 16, src + ln.c1 * 8);
         }
       }
-      if (lane == 0) copy4(at + kStreamRun * 1024, a.positions + ft);
-      if (lane == 1 && a.kc.data) copy4(at + kStreamRun * 1024 + 4, a.slots + ft);
-      ++fetched;
-      if (++fb == per_token) { fb = 0; ++ft; }
+      if (lane == 0) copy4(at + kStreamRun * 1024, a.positions + ahead.t);
+      if (lane == 1 && a.kc.data) copy4(at + kStreamRun * 1024 + 4, a.slots + ahead.t);
+      next(ahead);
       if (++fstage == kStreamStages) fstage = 0;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");       // an empty one at the end keeps the count
   };
 #pragma unroll
   for (int i = 0; i + 1 < kStreamStages; ++i) fetch();
-  int t = (int)(from / per_token), b = (int)(from - (long long)t * per_token), stage = 0, angle_of = -1;
+  int stage = 0, angle_of = -1;
   float cs[8], sn[8];
-  for (long long item = from; item < to; ++item) {
+  for (At x = begin; x.t < a.tokens; next(x)) {
+    const int t = x.t;
     fetch();
     asm volatile("cp.async.wait_group %0;" ::"n"(kStreamStages - 1) : "memory");
     __syncwarp();                                  // position and slot were copied by lanes 0 and 1
@@ -269,24 +278,24 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
     }
 #pragma unroll
     for (int u = 0; u < kStreamRun; ++u) {
-      const int p = b * kStreamRun + u;
+      const int p = x.b * kStreamRun + u;
       if (p < passes)
         finish_pass<D>(a, ln, ln.pass(a, p), p >= pq + pkv, p < pq, t, slot, *reinterpret_cast<const uint4*>(at + u * 1024 + lane * 16),
                        *reinterpret_cast<const uint4*>(at + u * 1024 + 512 + lane * 16), cs, sn);
     }
     __syncwarp();                                  // all have read position and slot before the stage is filled again
-    if (++b == per_token) { b = 0; ++t; }
     if (++stage == kStreamStages) stage = 0;
   }
 }
 
 template <int D>
 cudaError_t launch(RopeArgs& a, cudaStream_t s) {
-  // From an item for each of the device's warps on, the streaming kernel (131072 rows of 48 heads, head-major and cached:
-  // 666 us against 723 us with the other one; 1000 rows of 36: 8.9 against 9.4).
+  // From an item for every other of the device's warps on, the streaming kernel (36 heads, with it and with the other one:
+  // 250 rows 4.8 and 4.2 us, 500 rows 5.5 and 7.0, 1000 rows 7.6 and 8.8; 131072 rows of 48 heads, head-major and cached: 662
+  // and 688).
   const int passes = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW + 2 * ((a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW);
   const long long items = (long long)a.tokens * ((passes + kStreamRun - 1) / kStreamRun);
-  if (items >= 148 * kStreamWarps) {
+  if (items >= 148 * kStreamWarps / 2) {
     constexpr int smem = kStreamWarps * kStreamStages * kStreamItem;
     const cudaError_t e = cudaFuncSetAttribute(qk_norm_rope_stream_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;

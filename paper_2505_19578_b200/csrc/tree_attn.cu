@@ -24,7 +24,7 @@
 //   warps 9, 11     issuers (one thread each; warp 11 in wide units only): S = Q K^T and O += P V
 //   warp 10         loader: walks the run, publishes units, gathers their Q rows into shared memory
 //
-// Three modes, by the largest number of rows that any request has:
+// Three modes, by the largest number of rows that any request has (wide only where it saves enough tiles, see the kernel):
 //
 // Wide (more than 128): units have up to 256 rows, the groups are their halves and walk the same tiles 64 keys at a time,
 // each with its O and two S of 64 columns in TMEM (all there is), so that the next S is computed during the softmax of this
@@ -148,9 +148,9 @@ __device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) {
   q.kt = max((q.len + kTile - 1) / kTile, 1);
   return q;
 }
-// units of the request per KV head (n * group fits 32 bits: the host has checked)
-__device__ __forceinline__ int passes(const TreeAttnArgs& a, const Request& q) { return (q.n * a.group + kUnitRows - 1) / kUnitRows; }
-__device__ __forceinline__ long long units_of(const TreeAttnArgs& a, const Request& q) { return (long long)a.hkv * passes(a, q); }
+// units of the request per KV head, of 128 or 256 rows (n * group fits 32 bits: the host has checked)
+__device__ __forceinline__ int passes(const TreeAttnArgs& a, const Request& q, int rows) { return (int)(((uint32_t)(q.n * a.group) + rows - 1) >> (rows == 128 ? 7 : 8)); }
+__device__ __forceinline__ long long units_of(const TreeAttnArgs& a, const Request& q, int rows) { return (long long)a.hkv * passes(a, q, rows); }
 __device__ __forceinline__ long long divide(long long x, long long y) {       // both are small as a rule
   return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
@@ -1165,26 +1165,59 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   // ---- where the run begins
   const int per = (a.n_req + kThreads - 1) / kThreads;
   const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
-  long long mine_t = 0, mine_u = 0;                // tiles, units
+  int unit_rows = kUnitRows;
+  long long mine_t = 0, mine_u = 0, more_t = 0;    // tiles, units; tiles in addition with units of 128 rows
   bool many = false, some = false;
   for (int b = b_lo; b < b_hi; ++b) {
     const Request q = request(a, b);
-    const long long n = units_of(a, q);
+    const long long n = units_of(a, q, unit_rows);
     mine_u += n;
     mine_t += n * q.kt;
+    more_t += (units_of(a, q, 128) - n) * q.kt;
     many |= q.n * a.group > 128;
     some |= q.n * a.group > kNarrowRows;
   }
-  long long incl_t = mine_t, incl_u = mine_u;
+  long long incl_t, incl_u;
+  auto sums = [&] {                                // over the threads before and this one; over the warps, in `scan`
+    incl_t = mine_t;
+    incl_u = mine_u;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long up_t = __shfl_up_sync(0xffffffffu, incl_t, o), up_u = __shfl_up_sync(0xffffffffu, incl_u, o);
-    if (lane >= o) { incl_t += up_t; incl_u += up_u; }
-  }
-  if (lane == 31) { scan[warp] = incl_t; scan[kWarps + warp] = incl_u; }
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up_t = __shfl_up_sync(0xffffffffu, incl_t, o), up_u = __shfl_up_sync(0xffffffffu, incl_u, o);
+      if (lane >= o) { incl_t += up_t; incl_u += up_u; }
+    }
+    if (lane == 31) { scan[warp] = incl_t; scan[kWarps + warp] = incl_u; }
+  };
+  sums();
   if (threadIdx.x == 0 && misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
   bool wide = __syncthreads_or(many) != 0;
   const bool narrow = __syncthreads_or(some) == 0;
+  if (wide) {
+    // Units of 256 rows take half as many tiles again of the time of those of 128 (2.5 and 1.6 us a tile): tall, if cutting
+    // them adds no more than that half (one chunk of a prompt among many single tokens, or 257 to 384 rows each: a request of
+    // 256 rows among 255 of one token 251 us so, 317 as wide; one of 1024 rows 297 and 487).
+    long long tiles = 0;
+    for (int w = 0; w < kWarps; ++w) tiles += scan[w];
+    __syncthreads();
+    for (int o = 16; o > 0; o >>= 1) more_t += __shfl_down_sync(0xffffffffu, more_t, o);
+    if (lane == 0) scan[warp] = more_t;
+    __syncthreads();
+    long long more = 0;
+    for (int w = 0; w < kWarps; ++w) more += scan[w];
+    __syncthreads();
+    wide = 2 * more > tiles;
+    if (!wide) {
+      unit_rows = 128;
+      mine_t = mine_u = 0;
+      for (int b = b_lo; b < b_hi; ++b) {
+        const Request q = request(a, b);
+        mine_u += units_of(a, q, unit_rows);
+        mine_t += units_of(a, q, unit_rows) * q.kt;
+      }
+    }
+    sums();
+    __syncthreads();
+  }
   if (!narrow) {
     if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
     // rows of the Q area that no unit fills stay zero: products of whatever lay there would cost power, and with it clock
@@ -1209,7 +1242,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     } else if (step <= w && w < step + mine_t + own * mine_u) {
       for (int b = b_lo; b < b_hi; ++b) {
         const Request q = request(a, b);
-        const long long n = units_of(a, q);
+        const long long n = units_of(a, q, unit_rows);
         if (w < step + n * (q.kt + own)) {
           const long long rem = w - step, nth = divide(rem, q.kt + own), in = rem - nth * (q.kt + own);
           tiles_at[end] = tile + nth * q.kt + max(in - own, 0ll);
@@ -1264,10 +1297,10 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
         const long long w1 = run_begin(cta + 1);
         Request q = request(a, b);
         while (w < w1 && ok) {
-          while (rem >= units_of(a, q) * (q.kt + own) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
-          if (rem >= units_of(a, q) * (q.kt + own)) break;       // not reached while the lengths stand still
+          while (rem >= units_of(a, q, unit_rows) * (q.kt + own) && b + 1 < a.n_req) { rem = 0; q = request(a, ++b); }
+          if (rem >= units_of(a, q, unit_rows) * (q.kt + own)) break;       // not reached while the lengths stand still
           Unit u;
-          const int n_pass = passes(a, q), all_rows = q.n * a.group;
+          const int n_pass = passes(a, q, unit_rows), all_rows = q.n * a.group;
           const int nth = (int)divide(rem, q.kt + own), in = (int)(rem - (long long)nth * (q.kt + own));       // step of the unit: tile `in - own`
           const int take = (int)min((long long)(q.kt + own - in), w1 - w);
           w += take;
@@ -1279,8 +1312,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
           u.g = n_pass == 1 ? nth : nth / n_pass;
           u.b = b;
           u.start = q.start;
-          u.r0 = (nth - u.g * n_pass) * kUnitRows;
-          u.rows = min(all_rows - u.r0, kUnitRows);
+          u.r0 = (nth - u.g * n_pass) * unit_rows;
+          u.rows = min(all_rows - u.r0, unit_rows);
           u.len = q.len;
           u.past = q.past;
           const int e = seq % kUnitRing;

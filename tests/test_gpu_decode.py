@@ -751,3 +751,14 @@ def test_tree_attn_in_place_is_refused(binding):
         binding.Context().sp_tree_attn(s.qd, s.kd, s.vd, s.table_d, s.lens_d, s.start_d, s.qd)
     torch.cuda.synchronize()
     assert e.value.code == -1 and bool((s.qd == before).all())
+
+
+@pytest.mark.parametrize("hq,hkv,d,page,reqs", [
+    (8, 2, 128, 32, [(300, 1)] * 30 + [(500, 100)] + [(40, 2)] * 10),          # 400 rows among few: cut into units of 128
+    (4, 4, 64, 16, [(900, 257), (300, 300)]), (4, 1, 128, 64, [(700, 65), (200, 64), (30, 1)]), (2, 1, 64, 16, [(5, 255), (900, 130)]),
+])
+def test_tree_attn_long_chunks_beside_single_tokens(attn_ctx, hq, hkv, d, page, reqs):
+    s = Step(71, hq, hkv, d, page, reqs, "tree" if max(n for _, n in reqs) <= 256 else "chain", 2)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    s.check()

@@ -100,7 +100,7 @@ struct Plan {
   static constexpr int BAR_FULL = 0, BAR_FREE = BAR_FULL + NSLOTS, BAR_S = BAR_FREE + NSLOTS, BAR_P = BAR_S + 4, BAR_PV = BAR_P + 4, BAR_REF = BAR_PV + 4,
                        BAR_OFULL = BAR_REF + 1, BAR_OFREE = BAR_OFULL + 1, BAR_QFULL = BAR_OFREE + 1, BAR_QFREE = BAR_QFULL + 2,
                        BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + kUnitRing, BARS = BAR_UFREE + kUnitRing;
-  static constexpr int UNIT_OFF = MISC_OFF + BARS * 8, UNIT_BYTES = 48;
+  static constexpr int UNIT_OFF = MISC_OFF + 2 * BARS * 8, UNIT_BYTES = 48;                  // a second set of barriers: for a run walked again
   static constexpr int SCAN_OFF = (UNIT_OFF + kUnitRing * UNIT_BYTES + 15) / 16 * 16;        // int64 [2][kWarps]
   static constexpr int RUN_OFF = SCAN_OFF + 2 * kWarps * 8;                           // int64 [3], int [4]
   static constexpr int TAG_OFF = RUN_OFF + 3 * 8 + 4 * 4;                             // int [8]
@@ -765,24 +765,15 @@ __device__ __noinline__ void issue_tall(const TreeAttnArgs& a, uint8_t* smem, co
     }
     if (stalled(moved)) break;
   }
-  // the last arrivals, before the barriers may be used anew
-  for (uint32_t i = 0; i < P::SLOTS; ++i) {
-    const uint32_t uses = (2 * n_tiles_cta + P::SLOTS - 1 - i) / P::SLOTS;
-    if (uses > 0) mbar_wait(bar(P::BAR_FREE + i), (uses - 1) & 1, ab, 61);
-  }
-  for (uint32_t i = 0; i < 2; ++i) {
-    const uint32_t uses = (seq + 1 - i) / 2;
-    if (uses > 0) mbar_wait(bar(P::BAR_QFREE + i), (uses - 1) & 1, ab, 62);
-  }
 }
 
 // The issuer of a wide unit's group x (there are two such threads).  Keys come 64 at a time here: S of 128 rows is 64 columns,
 // and each group has two of them, so that the next S is computed during the softmax of this one.
 template <int D>
-__device__ __noinline__ void issue_wide(const TreeAttnArgs& a, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta, uint32_t x) {
+__device__ __noinline__ void issue_wide(const TreeAttnArgs& a, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta, uint32_t x) {
   using P = Plan<D>;
   const uint32_t base = smem_u32(smem);
-  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  auto bar = [&](int which) { return bars + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   volatile int* abort_flag = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8) + 1;
   constexpr uint32_t idesc_qk = instr_desc(128, kTile / 2, 0, 0), idesc_pv = instr_desc(128, D, 0, 1);
@@ -884,10 +875,10 @@ __device__ __noinline__ void issue_wide(const TreeAttnArgs& a, uint8_t* smem, co
 
 // Softmax and epilogue, wide: a group for each half of the rows.
 template <int D>
-__device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& work, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
+__device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& work, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
   using P = Plan<D>;
   const uint32_t base = smem_u32(smem);
-  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  auto bar = [&](int which) { return bars + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   volatile int* abort_flag = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8) + 1;
   volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
@@ -1135,7 +1126,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   using P = Plan<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
-  auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
+  uint32_t bars = base + P::MISC_OFF;
+  auto bar = [&](int which) { return bars + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   long long* scan = reinterpret_cast<long long*>(smem + P::SCAN_OFF);
   long long* start_rem = reinterpret_cast<long long*>(smem + P::RUN_OFF);      // steps of the request before the run
@@ -1254,7 +1246,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       }
     }
   }
-  auto init_barriers = [&](bool wide) {
+  auto init_barriers = [&](uint32_t bars, bool wide) {
+    auto bar = [&](int which) { return bars + which * 8; };
     for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(P::BAR_S + i), 1);
@@ -1277,7 +1270,8 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   };
-  if (threadIdx.x == 0) init_barriers(wide);
+  if (threadIdx.x == 0) init_barriers(bars, wide);
+  if (threadIdx.x == 32 && !wide && !narrow) init_barriers(bars + P::BARS * 8, true);
   tc_fence_before();
   const bool idle = __syncthreads_or(poisoned || misplaced) != 0;
   tc_fence_after();
@@ -1437,13 +1431,13 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
         }
       }
     } else if (warp == kIssuer || warp == kIssuer1) {
-      if (lane == 0 && wide) issue_wide<D>(a, smem, ab, tmem, n_tiles_cta, warp == kIssuer1);
+      if (lane == 0 && wide) issue_wide<D>(a, smem, bars, ab, tmem, n_tiles_cta, warp == kIssuer1);
       else if (lane == 0 && !narrow && warp == kIssuer) issue_tall<D>(a, smem, ab, tmem, n_tiles_cta);
       __syncwarp();
     } else if (narrow) {
       narrow_warps<D>(a, work, smem, ab);
     } else if (wide) {
-      softmax_wide<D>(a, work, smem, ab, tmem, n_tiles_cta);
+      softmax_wide<D>(a, work, smem, bars, ab, tmem, n_tiles_cta);
     } else {
       softmax_tall<D>(a, work, smem, ab, tmem, n_tiles_cta);
     }
@@ -1452,13 +1446,10 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     if (wide || *redo == 0 || *abort_flag) break;
-    // Tall, and a reference did not serve: the run once more, wide.  All that arrives at the barriers has done so (the issuer
-    // has waited for it).
-    if (threadIdx.x == 0) {
-      for (int i = 0; i < P::BARS; ++i) asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar(i)) : "memory");
-      init_barriers(true);
-      for (int i = 0; i < 8; ++i) bad_tag[i] = 0;
-    }
+    // Tall, and a reference did not serve: the run once more, wide, with barriers of its own (some of the first walk's end in
+    // odd phases).  All products of the first walk are in O, which has been read.
+    if (threadIdx.x < 8) bad_tag[threadIdx.x] = 0;
+    bars += P::BARS * 8;
     wide = true;
     __syncthreads();
   }

@@ -762,3 +762,23 @@ def test_tree_attn_long_chunks_beside_single_tokens(attn_ctx, hq, hkv, d, page, 
     s.call(attn_ctx)
     clean(attn_ctx)
     s.check()
+
+
+@pytest.mark.parametrize("hq,d,new", [(4, 64, 10), (2, 128, 33)])
+@pytest.mark.parametrize("rise", [40.0, -40.0], ids=["climbing", "falling"])
+def test_tree_attn_levels_that_change_along_long_runs(attn_ctx, hq, d, new, rise):
+    """Several tiles of 128 keys for every SM, each 40 nats above (below) the one before, eight in a row."""
+    s = Step(19, hq, 2, d, 64, [(60000, new), (50, 2)], "tree", 1, "paged")
+    s.q[..., 0] = 8.0
+    x = np.arange(60000 + new)
+    level = (x // 128 % 8) * rise
+    s.k[s.table[0, x // 64], :, x % 64, 0] = torch.tensor(level * np.sqrt(d) / 8).to(torch.bfloat16).double().numpy()[:, None]
+    s.qd, s.kd = dev(s.q).transpose(0, 1), dev(s.k)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    out = host(s.out)
+    off = d * 2.0 ** -23 * 7 * 40                                              # as above
+    for h, rows, want, want_lse, tol in s.reference():
+        assert np.all(np.abs(out[h, rows] - want) <= tol + 2 * off * np.abs(s.v).max())
+    end = sum(n for _, n in s.reqs)
+    assert np.all(out[:, end:] == 9)

@@ -275,9 +275,11 @@ __device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u,
 
 // Rare path of the softmax: the row's reference maximum has moved, so O of the earlier tiles (when there are any) and
 // the P chunks of this tile that are already stored are brought to the new one.  alpha is a power of two (references are
-// whole numbers), so nothing is rounded again.  Called by whole warps.
+// whole numbers), so nothing is rounded again.  What is read here may just have been stored (P of the chunk before, O by
+// the call before), and a load does not wait for earlier stores by itself.  Called by whole warps.
 template <int D>
 __device__ __noinline__ void rescale_tmem(uint32_t t_o, uint32_t t_s, float alpha, int stored, bool with_o) {
+  tmem_wait_st();
   if (with_o) {
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {

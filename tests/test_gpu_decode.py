@@ -782,3 +782,36 @@ def test_tree_attn_levels_that_change_along_long_runs(attn_ctx, hq, d, new, rise
         assert np.all(np.abs(out[h, rows] - want) <= tol + 2 * off * np.abs(s.v).max())
     end = sum(n for _, n in s.reqs)
     assert np.all(out[:, end:] == 9)
+
+
+def climb(s, step):
+    """Gives key x of each request the level `step(x)` (in nats) through the first column; the farthest level."""
+    s.q[..., 0] = 8.0
+    far = 0.0
+    for b, (p, n) in enumerate(s.reqs):
+        for x in range(p + n):
+            level = step(x)
+            far = max(far, abs(level))
+            s.k[s.table[b, x // s.page], :, x % s.page, 0] = float(torch.tensor(level * np.sqrt(s.d) / 8).to(torch.bfloat16))
+    s.qd, s.kd = dev(s.q).transpose(0, 1), dev(s.k)
+    return far
+
+
+def close_to_reference(s, far):
+    out = host(s.out)
+    off = s.d * 2.0 ** -23 * far                                               # an fp32 sum of d terms of which one is `far` sqrt(d)
+    for h, rows, want, want_lse, tol in s.reference():
+        assert np.all(np.abs(out[h, rows] - want) <= tol + 2 * off * np.abs(s.v).max())
+
+
+@pytest.mark.parametrize("hq,hkv,d,page,reqs", [(4, 1, 128, 16, [(700, 40), (3, 1)]), (2, 2, 64, 64, [(600, 130)]), (8, 2, 128, 128, [(1000, 64), (300, 50)]),
+                                                (2, 2, 128, 32, [(500, 20)]), (2, 2, 64, 16, [(500, 3)])])
+@pytest.mark.parametrize("rise", [9.0, 40.0])
+def test_tree_attn_logits_that_climb_within_a_tile(attn_ctx, hq, hkv, d, page, reqs, rise):
+    """Every 32 keys the maximum grows: references move in each chunk of a tile, with sums of earlier tiles and weights of
+    the chunk before just written."""
+    s = Step(23, hq, hkv, d, page, reqs, "tree", 1)
+    far = climb(s, lambda x: x // 32 * rise)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    close_to_reference(s, far)

@@ -242,8 +242,11 @@ __host__ __device__ inline WorkItemTiles resolve_item(const HeadTable& order, co
 
 // Rare path of the softmax, kept out of the hot loop: the row's reference max has moved, so O of the earlier
 // steps (when there are any) and the P chunks of this key-block that are already stored are brought to the new
-// reference.  alpha = 2^(old reference - new reference), 1 for a row whose reference stays.  Called by whole warps.
+// reference.  alpha = 2^(old reference - new reference), 1 for a row whose reference stays.  What is read here may just
+// have been stored (P of the chunk before, O by the call before), and a load does not wait for earlier stores by itself.
+// Called by whole warps.
 static __device__ __noinline__ void rescale_tmem(uint32_t tO, uint32_t tS, float alpha, int stored, bool with_o) {
+  tmem_wait_st();
   if (with_o) {
 #pragma unroll 1
     for (int oc = 0; oc < D / 32; ++oc) {
@@ -678,13 +681,19 @@ attn_pair_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap tm_q, con
           mx1 = max3(mx1, __uint_as_float(sc[30]), __uint_as_float(sc[31]));
           return fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
         };
-        // mx: scaled max of the columns about to be exponentiated; stored: P chunks of this key-block already in TMEM
-        auto move_reference = [&](const float mx, const int stored) {
+        // mx: scaled max of the columns about to be exponentiated; stored: P chunks of this key-block already in TMEM;
+        // loading: the registers of the load in flight, or null
+        auto move_reference = [&](const float mx, const int stored, uint32_t* loading) {
           // the reference max only moves when the row max has grown by more than 2^8 (rare after the first chunk of
           // the first key-block; a fully masked chunk has mx = -inf and leaves it alone)
           if (__any_sync(0xffffffffu, mx > m_ref + 8.f)) {
             const float m_new = (mx > m_ref + 8.f) ? mx : m_ref;
             const float alpha = ex2_approx(m_ref - m_new);
+            // a call may move registers: none whose load is still under way
+            if (loading) {
+              tmem_ld_wait();
+              reg_fence32(loading);
+            }
             // O of the previous steps is relative to the old reference (S of this step is complete, so the PV of
             // the previous step, issued before it, is too); none of the stored P chunks has been handed over yet
             rescale_tmem(tO, tS, alpha, stored, t > 0);
@@ -716,22 +725,22 @@ attn_pair_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap tm_q, con
         tmem_ld_wait();
         reg_fence32(sa);
         tmem_ld32_async(tS + 32, sb);
-        move_reference(chunk_max(sa) * scale, 0);
+        move_reference(chunk_max(sa) * scale, 0, sb);
         chunk_exps(sa, 0);
         tmem_ld_wait();
         reg_fence32(sb);
         tmem_ld32_async(tS + 64, sa);
-        move_reference(chunk_max(sb) * scale, 1);
+        move_reference(chunk_max(sb) * scale, 1, sa);
         chunk_exps(sb, 1);
         tmem_ld_wait();
         reg_fence32(sa);
         tmem_ld32_async(tS + 96, sb);
-        move_reference(chunk_max(sa) * scale, 2);
+        move_reference(chunk_max(sa) * scale, 2, sb);
         chunk_exps(sa, 2);
         tmem_ld_wait();
         reg_fence32(sb);
         if (tthread) trace(trole, 13, t);
-        move_reference(chunk_max(sb) * scale, 3);
+        move_reference(chunk_max(sb) * scale, 3, nullptr);
         chunk_exps(sb, 3);
         tmem_wait_st();
         tc_fence_before();

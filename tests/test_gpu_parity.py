@@ -490,3 +490,21 @@ def test_random_lists_heads_and_host_call(binding):
                                  cfg.block, ho)
         _sync_ok(ctx)
         assert torch.equal(ho, o_dev.cpu()), what
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("rise", [9.0, 40.0])
+def test_dense_logits_that_climb_within_a_tile(binding, kernel, rise):
+    """Every 32 keys the row maximum grows: references move in each chunk of a tile, with sums of earlier tiles and
+    weights of the chunk before just written."""
+    Hq, Hkv, N, d, B = 4, 2, 640, 128, 128
+    q, k, v = _rand_layer(17, Hq, Hkv, N, d)
+    q[..., 0] = 8.0
+    k[..., 0] = (torch.arange(N) // 32 * (rise * d ** 0.5 / 8)).to(torch.bfloat16)
+    ctx = binding.Context(kernel=kernel)
+    out = torch.zeros_like(q, device="cuda")
+    ctx.sp_dense_pivot_attn(q.cuda(), k.cuda(), v.cuda(), list(range(Hq)), B, out)
+    _sync_ok(ctx)
+    ref = orc.dense_causal_attention(par.f64(q), par.f64(k), par.f64(v), B=B, heads=list(range(Hq)))
+    for h in range(Hq):
+        par.assert_out_close(par.f64(out[h]), ref[h], f"head {h}")

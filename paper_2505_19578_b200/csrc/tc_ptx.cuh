@@ -42,6 +42,14 @@ struct Abort {
   int* status;         // global int[2]
 };
 
+// Records a wait that ran out, also over a range failure: that one is a single request's and stops nobody, this one leaves
+// the call's outputs unfinished.
+__device__ __forceinline__ void report_timeout(int* status, int where) {
+  int before = atomicCAS(status, 0, (int)SP_ERR_TIMEOUT);
+  if (before == (int)SP_ERR_RANGE && atomicCAS(status, (int)SP_ERR_RANGE, (int)SP_ERR_TIMEOUT) == (int)SP_ERR_RANGE) before = 0;
+  if (before == 0) status[1] = where;
+}
+
 // Bounded wait.  Returns false if the wait ran out or another role already gave up.
 // The checks are kept off the fast path: the CTA's own abort flag (shared memory) every 64
 // polls, the time limit and the global status word (a trip to L2 that would delay the wake-up
@@ -56,7 +64,8 @@ static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity
     if ((it & 63u) == 0u) {
       if (*flag) return false;
       if ((it & 4095u) == 0u) {
-        if (*reinterpret_cast<volatile int*>(status) != 0) {   // another CTA already gave up
+        const int code = *reinterpret_cast<volatile int*>(status);
+        if (code != 0 && code != (int)SP_ERR_RANGE) {          // another CTA already gave up (a range failure is no reason to)
           *flag = 1;
           return false;
         }
@@ -67,7 +76,7 @@ static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity
     }
   }
   *flag = 1;
-  if (atomicCAS(status, 0, (int)SP_ERR_TIMEOUT) == 0) status[1] = where;
+  report_timeout(status, where);
   return false;
 }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Abort& ab, int where,

@@ -681,7 +681,7 @@ __device__ __noinline__ void issue_tall(const TreeAttnArgs& a, uint8_t* smem, co
     if (idle_since == 0) idle_since = now;
     else if (now - idle_since > kWaitCycles) {
       *abort_flag = 1;
-      if (atomicCAS(a.status, 0, (int)SP_ERR_TIMEOUT) == 0) a.status[1] = 60;
+      report_timeout(a.status, 60);
       return true;
     }
     return false;
@@ -800,7 +800,7 @@ __device__ __noinline__ void issue_wide(const TreeAttnArgs& a, uint8_t* smem, ui
     if (idle_since == 0) idle_since = now;
     else if (now - idle_since > kWaitCycles) {
       *abort_flag = 1;
-      if (atomicCAS(a.status, 0, (int)SP_ERR_TIMEOUT) == 0) a.status[1] = 60;
+      report_timeout(a.status, 60);
       return true;
     }
     return false;

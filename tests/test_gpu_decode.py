@@ -815,3 +815,24 @@ def test_tree_attn_logits_that_climb_within_a_tile(attn_ctx, hq, hkv, d, page, r
     s.call(attn_ctx)
     clean(attn_ctx)
     close_to_reference(s, far)
+
+
+@pytest.mark.parametrize("n_req,n", [(600, 1), (450, 40), (300, 200)], ids=["narrow", "tall", "wide"])
+def test_tree_attn_long_waits_while_a_range_failure_has_not_been_read(binding, n_req, n):
+    """A bad page of an earlier call stops nobody, not even waits of a millisecond (several requests of 128000 keys for each SM)."""
+    ctx, fresh = binding.Context(), binding.Context()
+    s = Step(31, 4, 2, 64, 16, [(100, 2), (50, 3)], "chain")
+    s.table_d[0, 2] = -1
+    s.call(ctx)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    normal = lambda *shape: torch.randn(*shape, generator=g, device="cuda").to(torch.bfloat16)
+    pages = 1002
+    kc, vc, q = normal(pages, 1, 128, 64), normal(pages, 1, 128, 64), normal(1, n_req * n, 64)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(n_req, 1)           # all of them read the same pages
+    lens, start = i32([128000 + n - b for b in range(n_req)]), i32([b * n for b in range(n_req + 1)])
+    out, want = torch.zeros_like(q), torch.zeros_like(q)
+    ctx.sp_tree_attn(q, kc, vc, table, lens, start, out)
+    fresh.sp_tree_attn(q, kc, vc, table, lens, start, want)
+    clean(fresh)
+    assert ctx.status() == (binding.SP_ERR_RANGE, 70)
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and bool((want != 0).any(-1).all())

@@ -501,7 +501,9 @@ int sp_ctx_reserve_decode(sp_ctx* ctx);
  *                A request fails when a length is negative (read as 0), its table row is
  *                too short, no page is left for it, or it has more than 32 * mask_words
  *                drafted tokens (the bits that do not fit are left out).
- *   Calling it again with the same lengths writes the same values.
+ *   Calling it again with the same lengths writes the same values.  No output (block_table
+ *   included) may share memory with another array of the call, seq_lens not with past_lens
+ *   either: SP_ERR_INVALID_ARG.
  */
 int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_lens, int n_req, int page,
                    const int32_t* free_pages, int n_free, int32_t* block_table, int max_pages,
@@ -567,7 +569,9 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
  *              strictly ascending (an accepted path in the order of sp_page_tables);
  *              entries from n_kept[b] on are not read.
  *   n_kept     device i32 [n_req], read as 0 .. max_kept.
- *   past_lens  as given to sp_page_tables.     lens_out  out [n_req]: past + n_kept.
+ *   past_lens  as given to sp_page_tables.     lens_out  out [n_req]: past + n_kept; it may
+ *              not share memory with the call's other arrays, past_lens among them
+ *              (SP_ERR_INVALID_ARG).
  */
 int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cache, const int32_t* block_table,
                   int max_pages, const int32_t* past_lens, int n_req, const int32_t* kept, const int32_t* n_kept,

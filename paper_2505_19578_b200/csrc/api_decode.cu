@@ -46,6 +46,25 @@ PagedCache cache_of(const sp_tensor* t) {
   return PagedCache{static_cast<__nv_bfloat16*>(t->data), step(t, 0), step(t, 1), step(t, 2)};
 }
 
+// An int32 array of a call; `out`: the call writes it (in and out included).
+struct Array {
+  const void* p;
+  int64_t n;
+  bool out;
+};
+// Whether something written shares memory with another array of the call.  The blocks of a launch run in any order, so an
+// output in place of an input would be read by some of them.
+template <int N>
+bool overlapping(const Array (&x)[N]) {
+  for (int i = 0; i < N; ++i)
+    for (int j = 0; j < i; ++j) {
+      if (!x[i].out && !x[j].out) continue;
+      const uintptr_t a = reinterpret_cast<uintptr_t>(x[i].p), b = reinterpret_cast<uintptr_t>(x[j].p);
+      if (a && b && a < b + 4 * (uintptr_t)x[j].n && b < a + 4 * (uintptr_t)x[i].n) return true;
+    }
+  return false;
+}
+
 // The workspace of sp_tree_attn, with the context's device current.
 int reserve_split(sp_ctx* ctx) {
   if (ctx->split_ws) return SP_OK;
@@ -83,6 +102,11 @@ int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_len
   if (n_req == 0) return SP_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
+  const Array arrays[] = {{past_lens, n_req, false}, {new_lens, n_req, false}, {free_pages, n_free, false},
+                          {parents, n_rows, false}, {block_table, (int64_t)n_req * max_pages, true},
+                          {seq_lens, n_req, true}, {row_start, (int64_t)n_req + 1, true}, {positions, n_rows, true},
+                          {slots, n_rows, true}, {tree_mask, (int64_t)n_rows * mask_words, true}, {info, 4, true}};
+  if (overlapping(arrays)) return SP_ERR_INVALID_ARG;
   PageTablesArgs a{past_lens, new_lens, free_pages, parents, block_table, seq_lens, row_start, positions, slots,
                    tree_mask, info, n_req, n_free, max_pages, pl, n_rows, tree_mask ? mask_words : 0, ctx->status};
   if (launch_page_tables(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
@@ -218,6 +242,9 @@ int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cach
   if (n_req == 0) return SP_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
+  const Array arrays[] = {{block_table, (int64_t)n_req * max_pages, false}, {past_lens, n_req, false},
+                          {kept, (int64_t)n_req * max_kept, false}, {n_kept, n_req, false}, {lens_out, n_req, true}};
+  if (overlapping(arrays)) return SP_ERR_INVALID_ARG;
   KeepArgs a{cache_of(k_cache), cache_of(v_cache), block_table, past_lens, kept, n_kept, lens_out, n_req, max_pages, max_kept,
              c.hkv, c.d, c.page_log2, c.pages, ctx->status};
   if (launch_cache_keep(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;

@@ -836,3 +836,35 @@ def test_tree_attn_long_waits_while_a_range_failure_has_not_been_read(binding, n
     clean(fresh)
     assert ctx.status() == (binding.SP_ERR_RANGE, 70)
     assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and bool((want != 0).any(-1).all())
+
+
+def test_lengths_in_place_are_refused(binding):
+    """Lengths that would be read and written by different blocks of one launch."""
+    ctx = binding.Context()
+
+    def refused(call, *args, **kw):
+        before = [a.clone() if torch.is_tensor(a) else a for a in args]
+        with pytest.raises(binding.SpError) as e:
+            call(*args, **kw)
+        torch.cuda.synchronize()
+        assert e.value.code == -1 and all(torch.equal(a, b) for a, b in zip(args, before) if torch.is_tensor(a))
+
+    def tables(**over):
+        a = dict(past_lens=i32([3, 20]), new_lens=i32([2, 1]), page=16, free_pages=i32([5, 6, 7]), block_table=i32([[0, -1], [1, 2]]), seq_lens=i32([0, 0]),
+                 row_start=i32([0] * 3), positions=i32([0] * 3), slots=i32([0] * 3), info=i32([0] * 4))
+        a.update(over)
+        return a
+    lens, both, table = i32([3, 20]), i32([3, 20, 2, 1, 0]), i32([[0, -1], [1, 2]])
+    for over in (dict(past_lens=lens, seq_lens=lens), dict(new_lens=lens, seq_lens=lens), dict(past_lens=both[:2], seq_lens=both[1:3]),
+                 dict(new_lens=both[2:4], row_start=both[:3]), dict(positions=both[:3], slots=both[:3]), dict(free_pages=both, info=both[:4]),
+                 dict(block_table=table, free_pages=table.view(-1)), dict(block_table=table, slots=table.view(-1)[:3])):
+        refused(ctx.sp_page_tables, *tables(**over).values())
+    parents = i32([-1, 0, -1])
+    refused(ctx.sp_page_tables, *tables().values(), parents=parents, tree_mask=parents.view(3, 1))
+    ctx.sp_page_tables(*tables(past_lens=both[:2], new_lens=both[2:4]).values())            # inputs may lie side by side
+    kc, vc = (torch.zeros(3, 1, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    kept = i32([[0, 1], [0, 1]])
+    for past, n_kept, out in ((lens, i32([1, 1]), lens), (i32([3, 20]), lens, lens), (i32([3, 20]), i32([1, 1]), kept.view(-1)[2:]),
+                              (i32([3, 20]), i32([1, 1]), table.view(-1)[:2])):
+        refused(ctx.sp_cache_keep, kc, vc, table, past, kept, n_kept, out)
+    clean(ctx)

@@ -516,8 +516,8 @@ int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_len
  *     y = x / sqrt(mean(x^2) + eps) * weight    per head of q and k (if weights are given)
  *     (a, b) -> (a cos - b sin, b cos + a sin)  per pair i < n_freq,
  *                                               angle = position * inv_freq[i]
- *   Values are moved as they are.  fp32 arithmetic, one rounding; the angle is exact
- *   modulo one turn at any 32-bit position.
+ *   Values are moved as they are.  fp32 arithmetic, one rounding.  At any 32-bit position the
+ *   angle, modulo one turn, is off by under 2^-25 of a turn (the fp32 it is handed on in).
  *   q            [1, n_q_heads, rows, head_dim]; k, v [1, n_kv_heads, rows, head_dim]: any
  *                strides (multiples of 8 elements, at least head_dim), so slices of one
  *                projected [rows, heads, head_dim] tensor will do.

@@ -65,6 +65,24 @@ bool overlapping(const Array (&x)[N]) {
   return false;
 }
 
+// inv_freq / (2 pi) modulo one turn, in units of 2^-64, rounded down; 0 <= inv_freq < 2^30.  The double's 53 bits times 192 bits
+// of 1 / (2 pi): the whole turns that drop out take none of the fraction's bits with them.
+uint64_t turns_per_position(double inv_freq) {
+  static const uint64_t kInvTwoPi[3] = {0x36d8a5664f10e410ull, 0x7f09d5f47d4d3770ull, 0x28be60db9391054aull};   // 2^-192 .. 2^-1
+  int e;
+  const double m = frexp(inv_freq, &e);
+  const uint64_t bits = (uint64_t)ldexp(m, 53);          // inv_freq = bits * 2^(e - 53)
+  uint64_t p[4] = {0, 0, 0, 0};                          // bits / (2 pi) * 2^192
+  for (int i = 0; i < 3; ++i) {
+    const unsigned __int128 x = (unsigned __int128)bits * kInvTwoPi[i] + p[i];
+    p[i] = (uint64_t)x;
+    p[i + 1] = (uint64_t)(x >> 64);
+  }
+  const int down = 128 + 53 - e, word = down / 64, off = down % 64;       // e <= 30: word >= 2
+  if (word > 3) return 0;
+  return p[word] >> off | (word < 3 && off > 0 ? p[word + 1] << (64 - off) : 0);
+}
+
 // The workspace of sp_tree_attn, with the context's device current.
 int reserve_split(sp_ctx* ctx) {
   if (ctx->split_ws) return SP_OK;
@@ -151,10 +169,7 @@ int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const s
   }
   for (int i = 0; i < n_freq; ++i) {
     if (!(inv_freq[i] >= 0.0 && inv_freq[i] < 1e9)) return SP_ERR_INVALID_ARG;
-    // turns per position, modulo one turn, in units of 2^-64
-    const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559L;
-    const long double part = turns - floorl(turns);
-    a.phase[i] = (uint64_t)floorl(part * 18446744073709551616.0L);
+    a.phase[i] = turns_per_position(inv_freq[i]);
   }
   a.q = static_cast<const __nv_bfloat16*>(q->data);
   a.k = static_cast<const __nv_bfloat16*>(k->data);

@@ -10,9 +10,10 @@
 // the sum of squares.  The sines and cosines of a token's pairs are computed by the warp's lanes, two pairs each, handed
 // round by shuffles and used for all the heads that the warp walks.
 //
-// Angles: the turns per position of each pair are a 64-bit fraction of a turn, so that position * frequency modulo one
-// turn is one wrapping integer product, exact at any position; its top 32 bits (2^-33 of a turn off at most) go to
-// sincospif.  fp32 products would be off by 4e-3 rad at position 1e5.  Everything else is fp32, rounded once to bf16.
+// Angles: the turns per position of each pair are a 64-bit fraction of a turn (rounded down: 2^-33 of a turn at a 31-bit
+// position), so that position * frequency modulo one turn is one wrapping integer product; its top 32 bits (2^-32 cut off) go
+// to sincospif as fp32 half turns (24 bits: 2^-26 of a turn).  Under 2^-25 of a turn in all, at any position; fp32 products would be off by
+// 4e-3 rad at position 1e5.  Everything else is fp32, rounded once to bf16.
 #include "decode.cuh"
 
 namespace sp {

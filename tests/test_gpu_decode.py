@@ -868,3 +868,27 @@ def test_lengths_in_place_are_refused(binding):
                               (i32([3, 20]), i32([1, 1]), table.view(-1)[:2])):
         refused(ctx.sp_cache_keep, kc, vc, table, past, kept, n_kept, out)
     clean(ctx)
+
+
+def test_norm_rope_angles_at_any_position_and_frequency(binding):
+    """Angles of millions of turns a position: the fraction of a turn has to come from all bits of the frequency."""
+    from fractions import Fraction
+    pi = Fraction(31415926535897932384626433832795028841971693993751058209749445923078164062862089986280348253421170679, 10 ** 100)
+    freq = [9.9e8, 1.2345678e6, 4321.1, 7.0, 1.0, 1e-3, 2.0 ** -40, 0.0]
+    pos = [2 ** 31 - 1, 2 ** 31 - 2, 10 ** 9 + 7, 131071, 1, 0, -1, -(2 ** 31)]
+    rng = np.random.default_rng(9)
+    x = ref.bf16_values(rng, len(pos), 3, 64)
+    q, k, v = (y.transpose(0, 1) for y in dev(x).split([1, 1, 1], 1))
+    q_out, k_out, v_out = (torch.empty_like(y) for y in (q, k, v))
+    ctx = binding.Context()
+    ctx.sp_qk_norm_rope(q, k, v, i32(pos), torch.tensor(freq, dtype=torch.float64), q_out, k_out, v_out)
+    clean(ctx)
+    turns = np.array([[float(Fraction(f) * p / (2 * pi) % 1) for f in freq] for p in pos])       # exact, rounded once
+    c, s = np.cos(2 * np.pi * turns), np.sin(2 * np.pi * turns)
+    for got, y in ((q_out, x[:, 0]), (k_out, x[:, 1])):
+        a, b = y[:, :8], y[:, 8:16]
+        want, size = y.copy(), np.abs(y)
+        want[:, :8], want[:, 8:16] = a * c - b * s, b * c + a * s
+        size[:, :8] = size[:, 8:16] = np.abs(a) + np.abs(b)
+        # as in the plain statement: the angle is off by under 2^-25 of a turn, its sine and cosine by under 2^-21
+        assert np.all(np.abs(host(got)[0] - want) <= ref.EPS_BF16 * np.abs(want) + size * 2.0 ** -18)

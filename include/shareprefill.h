@@ -459,9 +459,10 @@ int sp_prefill_attn_layer(sp_ctx* ctx, sp_pattern_dict* dict, const sp_tensor* q
  *     SP_ERR_UNSUPPORTED; no cache whose strides are multiples of head_dim comes near).
  *   - block_table: device i32 [n_req, max_pages]; token p of request b lies on page
  *     block_table[b][p / page].  Entries behind a request's last page are not read.
- *   - Any number of rows >= 1, any lengths (0 included); n_req <= 4096 (0: nothing
- *     is done).  All sizes that vary from step to step are read on the device, so a
- *     captured graph serves every step of the same n_req and row capacity.
+ *   - Any number of rows >= 1, any lengths (0 included); n_req <= 4096.  n_req 0: nothing
+ *     is done (the arrays may be NULL, and q and out of sp_tree_attn without rows).  All
+ *     sizes that vary from step to step are read on the device, so a captured graph serves
+ *     every step of the same n_req and row capacity.
  *   - A page or slot that is not one of the cache's is never followed: the access is
  *     left out (a key on such a page counts as not visible), the request's results
  *     are then unspecified, and sp_get_status reports SP_ERR_RANGE with where = 70

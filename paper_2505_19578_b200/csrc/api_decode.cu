@@ -110,14 +110,14 @@ int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_len
                    const int32_t* free_pages, int n_free, int32_t* block_table, int max_pages, const int32_t* parents,
                    int32_t* seq_lens, int32_t* row_start, int32_t* positions, int32_t* slots, uint32_t* tree_mask,
                    int mask_words, int n_rows, int32_t* info, void* stream) {
-  if (!ctx || n_req < 0 || n_free < 0 || max_pages <= 0 || n_rows < 0) return SP_ERR_INVALID_ARG;
-  if (!past_lens || !new_lens || !block_table || !seq_lens || !row_start || !info) return SP_ERR_INVALID_ARG;
-  if ((n_free > 0 && !free_pages) || (n_rows > 0 && (!positions || !slots))) return SP_ERR_INVALID_ARG;
-  if ((parents != nullptr) != (tree_mask != nullptr)) return SP_ERR_INVALID_ARG;
+  if (!ctx || n_req < 0 || n_free < 0 || n_rows < 0) return SP_ERR_INVALID_ARG;
   const int pl = log2_of_page(page);
   if (pl < 0 || n_req > kMaxRequests || max_pages > (INT32_MAX >> pl)) return SP_ERR_UNSUPPORTED;
+  if (n_req == 0) return SP_OK;            // before the arrays are looked at: without elements they may have no address
+  if (!past_lens || !new_lens || !block_table || !seq_lens || !row_start || !info || max_pages <= 0) return SP_ERR_INVALID_ARG;
+  if ((n_free > 0 && !free_pages) || (n_rows > 0 && (!positions || !slots))) return SP_ERR_INVALID_ARG;
+  if ((parents != nullptr) != (tree_mask != nullptr)) return SP_ERR_INVALID_ARG;
   if (tree_mask && (mask_words < 1 || mask_words > kMaxMaskWords)) return SP_ERR_UNSUPPORTED;
-  if (n_req == 0) return SP_OK;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
   const Array arrays[] = {{past_lens, n_req, false}, {new_lens, n_req, false}, {free_pages, n_free, false},
@@ -197,7 +197,8 @@ int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const s
 int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, const sp_tensor* v_cache,
                  const int32_t* block_table, int max_pages, const int32_t* seq_lens, const int32_t* row_start, int n_req,
                  const uint32_t* tree_mask, int mask_words, const sp_tensor* out, float* lse_out, void* stream) {
-  if (!ctx || !block_table || !seq_lens || !row_start || n_req < 0 || max_pages <= 0) return SP_ERR_INVALID_ARG;
+  if (!ctx || n_req < 0) return SP_ERR_INVALID_ARG;
+  if (n_req == 0 && q && q->shape[2] == 0) return SP_OK;      // nobody, no rows: tensors without elements
   int rc;
   CacheShape c;
   if ((rc = check_view(q)) || (rc = check_view(out))) return rc;
@@ -209,7 +210,8 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
   if (tree_mask && (mask_words < 1 || mask_words > kMaxMaskWords)) return SP_ERR_UNSUPPORTED;
   CacheSteps steps;
   if (!cache_steps(cache_of(k_cache), c.hkv, c.pages, &steps) || !cache_steps(cache_of(v_cache), c.hkv, c.pages, &steps)) return SP_ERR_UNSUPPORTED;
-  if (n_req == 0) return SP_OK;
+  if (n_req == 0) return SP_OK;            // as in sp_page_tables
+  if (!block_table || !seq_lens || !row_start || max_pages <= 0) return SP_ERR_INVALID_ARG;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
   if (q->data == out->data) return SP_ERR_INVALID_ARG;         // in place: a run may be walked twice
@@ -248,13 +250,14 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
 int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cache, const int32_t* block_table, int max_pages,
                   const int32_t* past_lens, int n_req, const int32_t* kept, const int32_t* n_kept, int max_kept,
                   int32_t* lens_out, void* stream) {
-  if (!ctx || !block_table || !past_lens || !kept || !n_kept || !lens_out) return SP_ERR_INVALID_ARG;
-  if (n_req < 0 || max_pages <= 0 || max_kept <= 0) return SP_ERR_INVALID_ARG;
+  if (!ctx || n_req < 0) return SP_ERR_INVALID_ARG;
   int rc;
   CacheShape c;
   if ((rc = check_cache(k_cache, v_cache, &c))) return rc;
   if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
-  if (n_req == 0) return SP_OK;
+  if (n_req == 0) return SP_OK;            // as in sp_page_tables
+  if (!block_table || !past_lens || !kept || !n_kept || !lens_out) return SP_ERR_INVALID_ARG;
+  if (max_pages <= 0 || max_kept <= 0) return SP_ERR_INVALID_ARG;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
   const Array arrays[] = {{block_table, (int64_t)n_req * max_pages, false}, {past_lens, n_req, false},

@@ -136,6 +136,15 @@ def test_no_requests_is_no_work(lib):
     assert attn(lib, n=0) == 0 and tables(lib, n=0) == 0 and keep(lib, n=0) == 0
 
 
+def test_no_requests_need_no_arrays(lib):
+    """What a framework hands over for tensors without elements."""
+    q = view((1, 4, 0, 64), data=0)
+    assert attn(lib, n=0, table=None, lens=None, start=None) == 0 and attn(lib, n=0, q=q, out=q, table=None, lens=None, start=None) == 0
+    assert tables(lib, n=0, past=None, new=None, free=None, n_free=0, table=None, lens=None, pos=None, slots=None, rows=0) == 0
+    assert keep(lib, n=0, table=None, past=None, kept=None, n_kept=None, lens=None) == 0
+    assert attn(lib, n=0, ctx=None) == tables(lib, n=0, ctx=None) == keep(lib, n=0, ctx=None) == INV
+
+
 @pytest.mark.skipif(torch.cuda.is_available(), reason="a valid call would be launched")
 def test_valid_calls_without_a_device_are_errors_not_crashes(lib):
     assert attn(lib) == rope(lib) == tables(lib) == keep(lib) == -4

@@ -892,3 +892,20 @@ def test_norm_rope_angles_at_any_position_and_frequency(binding):
         size[:, :8] = size[:, 8:16] = np.abs(a) + np.abs(b)
         # as in the plain statement: the angle is off by under 2^-25 of a turn, its sine and cosine by under 2^-21
         assert np.all(np.abs(host(got)[0] - want) <= ref.EPS_BF16 * np.abs(want) + size * 2.0 ** -18)
+
+
+def test_a_step_without_requests_is_no_work(binding):
+    """Tensors without elements have no address."""
+    ctx = binding.Context()
+    none, ints = torch.empty(0, dtype=torch.int32, device="cuda"), lambda *shape: torch.full(shape, 5, dtype=torch.int32, device="cuda")
+    start, info, pos, slots = ints(1), ints(4), ints(3), ints(3)
+    ctx.sp_page_tables(none, none, 16, none, none.view(0, 4), none, start, pos, slots, info)
+    ctx.sp_page_tables(none, none, 16, none, none.view(0, 4), none, start, none, none, info, parents=none, tree_mask=none.view(0, 1))
+    kc, vc = (torch.ones(2, 2, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for rows in (0, 3):
+        q, out = (torch.ones(rows, 4, 64, dtype=torch.bfloat16, device="cuda").transpose(0, 1) for _ in range(2))
+        ctx.sp_tree_attn(q, kc, vc, none.view(0, 4), none, start, out, lse_out=torch.ones(4, rows, device="cuda"))
+        assert bool((out == 1).all())
+    ctx.sp_cache_keep(kc, vc, none.view(0, 4), none, none.view(0, 3), none, none)
+    clean(ctx)
+    assert all(bool((x == 5).all()) for x in (start, info, pos, slots)) and bool((kc == 1).all()) and bool((vc == 1).all())

@@ -568,7 +568,7 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
  *   past_lens[b] + i, in place.
  *   kept       device i32 [n_req, max_kept]: indices among the request's new tokens,
  *              strictly ascending (an accepted path in the order of sp_page_tables);
- *              entries from n_kept[b] on are not read.
+ *              entries from n_kept[b] on are not read.  NULL with max_kept 0: nothing moves.
  *   n_kept     device i32 [n_req], read as 0 .. max_kept.
  *   past_lens  as given to sp_page_tables.     lens_out  out [n_req]: past + n_kept; it may
  *              not share memory with the call's other arrays, past_lens among them

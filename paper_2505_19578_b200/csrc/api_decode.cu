@@ -256,8 +256,8 @@ int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cach
   if ((rc = check_cache(k_cache, v_cache, &c))) return rc;
   if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
   if (n_req == 0) return SP_OK;            // as in sp_page_tables
-  if (!block_table || !past_lens || !kept || !n_kept || !lens_out) return SP_ERR_INVALID_ARG;
-  if (max_pages <= 0 || max_kept <= 0) return SP_ERR_INVALID_ARG;
+  if (!block_table || !past_lens || !n_kept || !lens_out || max_pages <= 0) return SP_ERR_INVALID_ARG;
+  if (kept ? max_kept <= 0 : max_kept != 0) return SP_ERR_INVALID_ARG;     // no column: a list without elements
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
   const Array arrays[] = {{block_table, (int64_t)n_req * max_pages, false}, {past_lens, n_req, false},

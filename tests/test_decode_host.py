@@ -146,6 +146,11 @@ def test_no_requests_need_no_arrays(lib):
 
 
 @pytest.mark.skipif(torch.cuda.is_available(), reason="a valid call would be launched")
+def test_keeping_nothing_is_a_valid_call(lib):
+    assert keep(lib, kept=None, max_kept=0) == -4 and keep(lib, kept=None, max_kept=-1) == INV        # without a device: it gets to the launch
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a valid call would be launched")
 def test_valid_calls_without_a_device_are_errors_not_crashes(lib):
     assert attn(lib) == rope(lib) == tables(lib) == keep(lib) == -4
 

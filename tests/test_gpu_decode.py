@@ -909,3 +909,13 @@ def test_a_step_without_requests_is_no_work(binding):
     ctx.sp_cache_keep(kc, vc, none.view(0, 4), none, none.view(0, 3), none, none)
     clean(ctx)
     assert all(bool((x == 5).all()) for x in (start, info, pos, slots)) and bool((kc == 1).all()) and bool((vc == 1).all())
+
+
+def test_cache_keep_of_nothing(binding):
+    """No column of kept tokens: nothing moves, the lengths are those of before."""
+    ctx = binding.Context()
+    kc, vc = (torch.randn(3, 2, 16, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    before, lens = kc.clone(), i32([7, 7])
+    ctx.sp_cache_keep(kc, vc, i32([[0], [1]]), i32([3, 0]), torch.empty(2, 0, dtype=torch.int32, device="cuda"), i32([0, 0]), lens)
+    clean(ctx)
+    assert lens.tolist() == [3, 0] and torch.equal(kc, before)

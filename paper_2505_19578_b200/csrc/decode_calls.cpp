@@ -175,6 +175,7 @@ PyObject* tree_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const int n = lens.n0;
     const Ints table = ints(a[5], "block_table", dev, 2, n), start = ints(a[7], "row_start", dev, 1, (int64_t)n + 1);
     const Ints bits = maybe_ints(a[9], "tree_mask", dev, 2, q.shape[2]);
+    if (a[9] != Py_None && bits.n1 < 1) { PyErr_SetString(PyExc_ValueError, "tree_mask: expected at least one word a row"); throw Refused(); }   // its address would be null: a chain
     float* lse = nullptr;
     if (a[10] != Py_None) {
       const at::Tensor& t = tensor(a[10], "lse_out", "a contiguous fp32 tensor [heads, rows]", dev, at::kFloat);

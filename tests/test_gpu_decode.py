@@ -919,3 +919,12 @@ def test_cache_keep_of_nothing(binding):
     ctx.sp_cache_keep(kc, vc, i32([[0], [1]]), i32([3, 0]), torch.empty(2, 0, dtype=torch.int32, device="cuda"), i32([0, 0]), lens)
     clean(ctx)
     assert lens.tolist() == [3, 0] and torch.equal(kc, before)
+
+
+def test_tree_attn_mask_without_words_is_refused(binding):
+    """Not taken for no mask at all, which means a chain."""
+    s = Step(5, 4, 2, 64, 16, [(20, 3)])
+    with pytest.raises(ValueError, match="tree_mask"):
+        binding.Context().sp_tree_attn(s.qd, s.kd, s.vd, s.table_d, s.lens_d, s.start_d, s.out, tree_mask=torch.empty(s.rows, 0, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert bool((s.out == 9).all())

@@ -53,7 +53,8 @@ Ints ints(PyObject* o, const char* what, int device, int dims, int64_t n0, int64
   const at::Tensor& t = tensor(o, what, "a contiguous int32 tensor", device, at::kInt);
   if (!t.is_contiguous()) refuse(what, "a contiguous int32 tensor", device);
   if (t.dim() != dims || (n0 >= 0 && t.size(0) != n0) || (dims > 1 && n1 >= 0 && t.size(1) != n1)) {
-    if (dims == 1) PyErr_Format(PyExc_ValueError, "%s: expected %lld elements in one dimension", what, (long long)n0);
+    if (dims == 1 && n0 < 0) PyErr_Format(PyExc_ValueError, "%s: expected one dimension", what);
+    else if (dims == 1) PyErr_Format(PyExc_ValueError, "%s: expected %lld elements in one dimension", what, (long long)n0);
     else PyErr_Format(PyExc_ValueError, "%s: expected a two-dimensional tensor of %lld rows", what, (long long)n0);
     throw Refused();
   }

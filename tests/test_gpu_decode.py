@@ -928,3 +928,13 @@ def test_tree_attn_mask_without_words_is_refused(binding):
         binding.Context().sp_tree_attn(s.qd, s.kd, s.vd, s.table_d, s.lens_d, s.start_d, s.out, tree_mask=torch.empty(s.rows, 0, dtype=torch.int32, device="cuda"))
     torch.cuda.synchronize()
     assert bool((s.out == 9).all())
+
+
+def test_wrong_shapes_are_named(binding):
+    ctx, x, t = binding.Context(), i32([1, 2]), i32([[1, 2], [3, 4]])
+    with pytest.raises(ValueError, match="^past_lens: expected one dimension$"):
+        ctx.sp_page_tables(t, x, 16, x, t, x, i32([0] * 3), x, x, i32([0] * 4))
+    with pytest.raises(ValueError, match="^new_lens: expected 2 elements in one dimension$"):
+        ctx.sp_page_tables(x, i32([1, 2, 3]), 16, x, t, x, i32([0] * 3), x, x, i32([0] * 4))
+    with pytest.raises(ValueError, match="^block_table: expected a two-dimensional tensor of 2 rows$"):
+        ctx.sp_page_tables(x, x, 16, x, x, x, i32([0] * 3), x, x, i32([0] * 4))

@@ -144,6 +144,9 @@ def _decode_calls():
         path = os.path.join(_HERE, "_decode_calls.so")
         if not os.path.exists(path):
             raise RuntimeError(f"{path} not found: build it with `python -m paper_2505_19578_b200.build`")
+        from . import build
+        if not build.calls_match(path):
+            raise RuntimeError(f"{path} was built for another torch or Python: build it again with `python -m paper_2505_19578_b200.build`")
         from . import _decode_calls as native
         lib = load()
         native.set_functions(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value

@@ -5,11 +5,12 @@
 Output: paper_2505_19578_b200/libshareprefill.so (cudart linked statically; the
 driver API is resolved at run time, so the library loads on a machine without a
 GPU driver), and paper_2505_19578_b200/_decode_calls.so, the Python entry of the
-decode-side calls (g++ against torch's headers).
+decode-side calls (g++ against torch's headers; without torch it is left out).
 """
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -47,26 +48,72 @@ def needs_build(lib: str = LIB) -> bool:
     return any(os.path.getmtime(d) > t for d in deps + extra)
 
 
+def _built_against() -> str | None:
+    """What the Python entry is compiled against, as it is written into it; None without torch."""
+    try:
+        import torch
+    except ImportError:
+        return None
+    return f"shareprefill calls for torch {torch.__version__}, Python {sysconfig.get_python_version()};"
+
+
+def calls_match(path: str = CALLS) -> bool:
+    """Whether the built Python entry is for the torch and the Python that run: it uses their C++ and C interfaces."""
+    mark = _built_against()
+    with open(path, "rb") as f:
+        return mark is not None and mark.encode() in f.read()
+
+
 def _start_calls_build():
-    """Starts the compiler on the Python entry of the decode-side calls (half a minute: torch's headers)."""
+    """Starts the compiler on the Python entry of the decode-side calls (half a minute: torch's headers); None without torch.
+    The result goes to _new(CALLS)."""
+    mark = _built_against()
+    if mark is None:
+        return None
     import torch
     from torch.utils import cpp_extension
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    nvcc = shutil.which(_nvcc())
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc))) if nvcc else "/usr/local/cuda"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", "/usr/local/cuda/include",
-           *[f"-I{p}" for p in cpp_extension.include_paths()], CALLS_SOURCE, "-o", CALLS, "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
-    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+           f'-DSP_BUILT_AGAINST="{mark}"', "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"),
+           *[f"-I{p}" for p in cpp_extension.include_paths()], CALLS_SOURCE, "-o", _new(CALLS), "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    try:
+        return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    except OSError as e:
+        _no_calls(f"{e}\n")
+        return None
+
+
+def _new(path: str) -> str:
+    return path[:-len(".so")] + ".new.so"
+
+
+def _no_calls(out: str) -> None:
+    """Without a working entry there is none: the decode-side calls then raise, and the library serves everything else."""
+    if os.path.exists(CALLS):
+        os.remove(CALLS)
+    sys.stderr.write(out + "the compiler failed on decode_calls.cpp: the decode-side calls cannot be made from Python\n")
+
+
+def _finish_calls_build(process) -> None:
+    out, _ = process.communicate()
+    if process.returncode == 0:
+        os.replace(_new(CALLS), CALLS)
+    else:
+        _no_calls(out)
 
 
 def calls_need_build() -> bool:
-    if not os.path.exists(CALLS):
+    if not os.path.exists(CALLS) or not calls_match(CALLS):
         return True
     t = os.path.getmtime(CALLS)
     return any(os.path.getmtime(d) > t for d in (CALLS_SOURCE, os.path.join(ROOT, "include", "shareprefill.h")))
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    """Builds the library (debug=True: the range-checked flavour, libshareprefill_debug.so, from the same sources)."""
+    """Builds the library (debug=True: the range-checked flavour, libshareprefill_debug.so, from the same sources), and
+    beside it, where torch is installed, the Python entry of the decode-side calls."""
     lib = LIB_DEBUG if debug else LIB
     calls = _start_calls_build() if calls_need_build() or (force and not debug) else None
     try:
@@ -74,11 +121,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
             _build_library(lib, verbose, debug)
     finally:
         if calls is not None:
-            out, _ = calls.communicate()
-            if calls.returncode != 0:
-                sys.stderr.write(out)
-    if calls is not None and calls.returncode != 0:
-        raise RuntimeError("the compiler failed on decode_calls.cpp")
+            _finish_calls_build(calls)
     return lib
 
 

@@ -12,6 +12,9 @@
 
 namespace {
 
+// Read from the file before it is loaded: an entry that was compiled for another torch or Python is not.
+__attribute__((used)) const char kBuiltAgainst[] = SP_BUILT_AGAINST;
+
 struct Functions {
   decltype(&sp_page_tables) page_tables;
   decltype(&sp_qk_norm_rope) qk_norm_rope;

@@ -938,3 +938,75 @@ def test_wrong_shapes_are_named(binding):
         ctx.sp_page_tables(x, i32([1, 2, 3]), 16, x, t, x, i32([0] * 3), x, x, i32([0] * 4))
     with pytest.raises(ValueError, match="^block_table: expected a two-dimensional tensor of 2 rows$"):
         ctx.sp_page_tables(x, x, 16, x, x, x, i32([0] * 3), x, x, i32([0] * 4))
+
+
+# rows at which the streaming kernel of the rotation starts to hand whole tokens to its warps (148 x 16), several items a token
+@pytest.mark.parametrize("hq,hkv,d,rows,n_freq,interleaved,norm,outs,page,major", [
+    (8, 2, 128, 2367, 64, False, True, True, 16, True), (8, 2, 128, 2368, 64, False, True, True, 16, False), (8, 2, 128, 2369, 64, True, True, False, 64, True),
+    (28, 4, 128, 5000, 64, False, True, True, 128, False), (24, 8, 64, 3001, 16, False, True, True, 32, True), (24, 8, 64, 4800, 32, True, False, True, 0, True)])
+def test_norm_rope_of_many_rows(binding, hq, hkv, d, rows, n_freq, interleaved, norm, outs, page, major):
+    rope_case(binding, hq, hkv, d, rows, n_freq, interleaved, norm, outs, page, major, seed=rows)
+
+
+@pytest.mark.parametrize("rows", [1000, 5000])
+def test_norm_rope_of_many_rows_in_place(binding, rows):
+    rng = np.random.default_rng(rows)
+    x = ref.bf16_values(rng, rows, 12, 128)
+    w = [ref.bf16_values(rng, 128) for _ in range(2)]
+    freq = 5e5 ** (-np.arange(64) / 64.0)
+    pos = rng.integers(0, 131072, rows)
+    t = dev(x)
+    q, k, v = (y.transpose(0, 1) for y in t.split([8, 2, 2], 1))
+    ctx = binding.Context()
+    ctx.sp_qk_norm_rope(q, k, v, i32(pos), torch.tensor(freq), q, k, v, q_weight=dev(w[0]), k_weight=dev(w[1]))
+    clean(ctx)
+    x = x.transpose(1, 0, 2)
+    got = host(t).transpose(1, 0, 2)
+    for heads, weight in ((slice(0, 8), w[0]), (slice(8, 10), w[1])):
+        want, err = ref.norm_rope(x[heads], weight, 1e-6, freq, False, pos)
+        assert np.all(np.abs(got[heads] - want) <= err + ref.EPS_BF16 * np.abs(want))
+    assert np.array_equal(got[10:], x[10:])
+
+
+def test_norm_rope_of_many_rows_with_slots_behind_the_cache(binding):
+    rows, page, pages = 3000, 16, 100
+    ctx = binding.Context()
+    x = torch.randn(rows, 14, 128, device="cuda").to(torch.bfloat16)
+    q, k, v = (y.transpose(0, 1) for y in x.split([8, 3, 3], 1))
+    kc, vc = (torch.zeros(pages, 3, page, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    slots = torch.full((rows,), -1, dtype=torch.int32)
+    some = torch.randperm(rows)
+    slots[some[:1000]] = torch.randperm(pages * page)[:1000].int()
+    slots[some[1000:1100]] = pages * page + torch.arange(100, dtype=torch.int32) * 7
+    ctx.sp_qk_norm_rope(q, k, v, i32(range(rows)), torch.zeros(0, dtype=torch.float64), torch.empty_like(q), k_cache=kc, v_cache=vc, slots=slots.cuda())
+    torch.cuda.synchronize()
+    assert ctx.status() == (binding.SP_ERR_RANGE, 75) and ctx.status() == (0, 0)
+    for cache, y in ((kc, k), (vc, v)):
+        want = torch.zeros(pages * page, 3, 128, dtype=torch.bfloat16, device="cuda")
+        want[slots[some[:1000]].long().cuda()] = y.transpose(0, 1)[some[:1000].cuda()]
+        assert torch.equal(cache.transpose(1, 2).reshape(-1, 3, 128), want)
+
+
+@pytest.mark.parametrize("hq,hkv,d,page,reqs", [(8, 2, 128, 32, [(300, 9), (40, 1)]), (4, 4, 64, 256, [(700, 3), (90, 1)]), (4, 1, 128, 16, [(500, 70)])])
+def test_tree_attn_of_other_orders(attn_ctx, hq, hkv, d, page, reqs):
+    """Keys with the pages of a head side by side, values token-major, queries and results head-major and four-dimensional."""
+    s = Step(81, hq, hkv, d, page, reqs, "tree", 2)
+    total = s.k.shape[0]
+    s.kd = dev(s.k.transpose(1, 0, 2, 3)).reshape(hkv, total * page, d).unflatten(1, (total, page)).transpose(0, 1)
+    s.vd = dev(s.v.transpose(0, 2, 1, 3)).transpose(1, 2)
+    s.qd = s.qd.contiguous().unsqueeze(0)
+    s.out = torch.full((1, hq, s.rows, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    s.out = s.out[0]
+    s.check()
+
+
+@pytest.mark.parametrize("d,page", [(64, 256), (128, 256), (128, 128)])
+def test_tree_attn_far_references_with_pages_as_long_as_a_tile_or_longer(attn_ctx, d, page):
+    """Runs that are walked again."""
+    s = Step(83, 4, 2, d, page, [(2000, 10), (700, 20)], "tree", 1)
+    far = climb(s, lambda x: x // 128 * 40.0)
+    s.call(attn_ctx)
+    clean(attn_ctx)
+    close_to_reference(s, far)

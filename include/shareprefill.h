@@ -29,7 +29,8 @@
  *     out) are reported by sp_get_status after the caller has synchronised.
  *   - The caller owns every tensor and the stream.  The library owns only the
  *     sp_ctx (its workspace and status word).  A context belongs to one device
- *     and must not be used from two streams at the same time.
+ *     and must not be used from two streams at the same time (replays of
+ *     captured graphs use the context that their calls were captured with).
  *   - Tensors are bf16, logical shape [batch, heads, seq, head_dim], element
  *     strides given explicitly; stride[3] must be 1 and the other strides must
  *     be multiples of 8 elements (16 bytes); data must be 16-byte aligned.
@@ -60,7 +61,8 @@ enum {
   SP_ERR_CUDA = -4,        /* a CUDA runtime / driver call failed                      */
   SP_ERR_TIMEOUT = -5,     /* a bounded device-side wait ran out (see sp_get_status)   */
   SP_ERR_SCRATCH_LIMIT = -6, /* sp_dense_pivot_attn_fixed_scratch: problem too large for the fixed array */
-  SP_ERR_RANGE = -7         /* range-checked debug build only: an index left its range (see sp_get_status) */
+  SP_ERR_RANGE = -7         /* a page, slot or length that is not the cache's (decode-side calls), or, in the
+                               range-checked debug build, an index that left its range (see sp_get_status) */
 };
 
 /* bf16 tensor view: device pointer, sizes and strides in ELEMENTS. */
@@ -106,6 +108,8 @@ int sp_ctx_reserve(sp_ctx* ctx, size_t bytes);
 /* Read and clear the device status word.  The caller must have synchronised
  * the stream(s) it used.  *code is SP_OK or SP_ERR_TIMEOUT; *where identifies
  * the wait that gave up (kernel-internal id).  Either pointer may be NULL.
+ * The decode-side calls ("From prefill into decoding") also report SP_ERR_RANGE:
+ * see there.  A timeout takes the place of a range failure that was not read.
  * SP_ERR_UNSUPPORTED with *where = 90 means the device laid out a CTA's shared
  * memory window or tensor memory differently from what the attention kernel was
  * built for (it then does no work).
@@ -460,12 +464,12 @@ int sp_prefill_attn_layer(sp_ctx* ctx, sp_pattern_dict* dict, const sp_tensor* q
  *   - block_table: device i32 [n_req, max_pages]; token p of request b lies on page
  *     block_table[b][p / page].  Entries behind a request's last page are not read.
  *   - Any number of rows >= 1, any lengths (0 included); n_req <= 4096.  n_req 0: nothing
- *     is done (the arrays may be NULL, and q and out of sp_tree_attn without rows).  All
- *     sizes that vary from step to step are read on the device, so a captured graph serves
- *     every step of the same n_req and row capacity.
+ *     is done (the arrays may be NULL, and q and out of sp_tree_attn without rows).  Lengths,
+ *     tables and row ranges are read on the device, so a captured graph serves every step of
+ *     the same n_req and row capacity; what is an argument by value stays as captured, the
+ *     length n_free of the list of free pages too.
  *   - A page or slot that is not one of the cache's is never followed: the access is
- *     left out (a key on such a page counts as not visible), the request's results
- *     are then unspecified, and sp_get_status reports SP_ERR_RANGE with where = 70
+ *     left out, the results of that request are then unspecified, and sp_get_status reports SP_ERR_RANGE with where = 70
  *     (sp_tree_attn; also a length that its table row cannot hold), 75
  *     (sp_qk_norm_rope) or 80 (sp_cache_keep).  Unlike a timeout this does not keep
  *     the calls of this section from working; the calls above work again once the
@@ -481,7 +485,8 @@ int sp_ctx_reserve_decode(sp_ctx* ctx);
  *   past_lens    device i32 [n_req]: tokens each request has in the cache.
  *   new_lens     device i32 [n_req]: tokens it gets in this step (0: none).
  *   free_pages   device i32 [n_free]: pages to take, in this order, requests in
- *                theirs; the caller drops the first info[1] of them afterwards.
+ *                theirs; the caller drops the first info[1] of them afterwards (for a
+ *                captured graph: rewrites the list in place, n_free pages each time).
  *   block_table  in/out: entries 0 .. ceil(past / page) - 1 of a row are given, the
  *                entries up to ceil((past + new) / page) - 1 are written, the rest is
  *                left as it was.  Pages that the written entries named before (of drafted
@@ -550,7 +555,10 @@ int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const s
  *     else:            bit x of the token's row is set (x >= 32 * mask_words: not visible)
  *   A logit of -infinity weighs nothing, like a masked key.  A row that sees nothing
  *   gets zeros and lse -infinity.  What lies in masked or unused places of the cache
- *   (NaN included) does not reach the outputs.
+ *   (NaN included) does not reach the outputs.  Probabilities are rounded to bf16 for the
+ *   product with v; sums, log-sum-exp and the partial results of long rows are fp32.  The
+ *   same call gives the same bits; beside other requests a request's may differ in their
+ *   last places (how the work is cut, and in which form it is done, depends on the batch).
  *   q            [1, n_q_heads, rows, head_dim], any strides as for sp_qk_norm_rope;
  *                n_q_heads a multiple of the cache's heads, at most 128.
  *   tree_mask    device u32 [rows, mask_words], mask_words in 1 .. 8, or NULL.

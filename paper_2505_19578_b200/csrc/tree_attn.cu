@@ -31,8 +31,9 @@
 // one.  The reference maximum moves, to a whole number, when the row maximum has grown by more than 2^8; O in TMEM is then
 // rescaled (exactly).  The tensor core's operands bound it: 128 rows of Q for 64 keys are 6 KB of shared memory for each
 // product of 48 cycles, 2500 cycles a tile in all, and the two groups' chains do not fill the gaps: 4000 a tile.  (With one
-// S of 128 columns each: 5 % slower.  Two CTAs, a half each, on the same tiles: 208 us instead of 161 for 128K keys, L2 does
-// not serve both at the rate of HBM.)
+// S of 128 columns each: 5 % slower.  Two CTAs, a half each, on the same tiles: 208 us instead of 160 for 128K keys, L2 does
+// not serve both at the rate of HBM.)  The prefill's paired kernel takes 3500 for tiles of this shape at
+// head_dim 128, with one issuer, constant descriptors and hand-overs by named barriers: not tried here.
 //
 // Tall (17 to 128): one O, three S in turn, and the groups take the tiles in turn.  S of the next tiles is computed while
 // both groups are in their softmax, so nothing waits for anything but the bytes.  One O means one reference for both
@@ -74,9 +75,8 @@ constexpr int kUnitRows = 256;
 constexpr int kThreads = 384, kWarps = kThreads / 32;
 constexpr int kProducer = 8, kIssuer = 9, kLoader = 10, kIssuer1 = 11;
 constexpr int kUnitRing = 4;
-constexpr int kNarrowSteps = 2, kTallSteps = 4;  // steps of a unit besides those of its tiles (narrow; tall and wide)
+constexpr int kNarrowSteps = 2, kTallSteps = 4;  // steps of a unit besides those of its tiles (narrow; tall and wide); measured at head_dim 128
 constexpr int kNarrowRows = 16;
-enum Mode { kNarrow, kTall, kWide };
 constexpr float kNoMax = -1e30f;                 // reference maximum before any visible key: finite, below any logit
 constexpr float kTallMargin = 24.f;              // tall: the reference above the first tile's maximum,
 constexpr float kTallMost = 72057594037927936.f, kTallLeast = 9.094947017729282e-13f;      // and the weights that it serves: 2^56, 2^-40

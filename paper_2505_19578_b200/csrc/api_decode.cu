@@ -58,7 +58,7 @@ template <int N>
 bool overlapping(const Array (&x)[N]) {
   for (int i = 0; i < N; ++i)
     for (int j = 0; j < i; ++j) {
-      if (!x[i].out && !x[j].out) continue;
+      if ((!x[i].out && !x[j].out) || x[i].n == 0 || x[j].n == 0) continue;
       const uintptr_t a = reinterpret_cast<uintptr_t>(x[i].p), b = reinterpret_cast<uintptr_t>(x[j].p);
       if (a && b && a < b + 4 * (uintptr_t)x[j].n && b < a + 4 * (uintptr_t)x[i].n) return true;
     }

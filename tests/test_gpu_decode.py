@@ -1010,3 +1010,14 @@ def test_tree_attn_far_references_with_pages_as_long_as_a_tile_or_longer(attn_ct
     s.call(attn_ctx)
     clean(attn_ctx)
     close_to_reference(s, far)
+
+
+def test_page_tables_with_an_empty_list_whose_address_is_anywhere(binding):
+    """Through the C call: no free page and no row, their addresses inside another array of the call."""
+    ctx = binding.Context()
+    past, new, table, lens, start, info = i32([3, 20]), i32([0, 0]), i32([[0, -1], [1, 2]]), i32([0, 0]), i32([9] * 3), i32([9] * 4)
+    inside = table.data_ptr() + 4
+    code = binding.load().sp_page_tables(ctx._h, past.data_ptr(), new.data_ptr(), 2, 16, inside, 0, table.data_ptr(), 2, None, lens.data_ptr(), start.data_ptr(),
+                                         inside, inside, None, 0, 0, info.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    clean(ctx)
+    assert code == 0 and lens.tolist() == [3, 20] and start.tolist() == [0, 0, 0] and info.tolist() == [0, 0, 0, 20] and table.tolist() == [[0, -1], [1, 2]]

@@ -586,6 +586,64 @@ int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cach
                   int max_pages, const int32_t* past_lens, int n_req, const int32_t* kept, const int32_t* n_kept,
                   int max_kept, int32_t* lens_out, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The same over a paged cache held in 4 bits.  (No counterpart in the paper.)  A step is sp_page_tables, then per layer
+ * sp_qk_norm_rope_q4 and sp_tree_attn_q4, and sp_cache_keep_q4 after verification; sp_cache_read_q4 gives cached tokens
+ * back as the bf16 tensors that sp_prefill_attn reads.  At head_dim 128 a token and head take 136 bytes instead of 512.
+ *
+ * Conventions on top of those above
+ *   - A value is (c - 8) * s: c a code of 4 bits, s a scale for 32 neighbouring elements of a token's head, one byte
+ *     e << 3 | m standing for (1 + m / 8) * 2^(e - 20).  bf16 holds every such value exactly.
+ *   - Quantising 32 elements: s = max |x| / 7 rounded to four significant bits, at least 2^-20 and at most 1.875 * 2^11;
+ *     c - 8 = x / s rounded to a whole number, at least -7 and at most 7; both to the nearest, ties to even.  A NaN is
+ *     stored as 0, an infinity as 7 * s.  No stored byte stands for a NaN or an infinity.
+ *   - A page of one head is page / 16 blocks of 17 * head_dim bytes, one for 16 tokens in order; keys and values lie in one
+ *     tensor.  Where a token's codes and scales are inside a block is the library's own (csrc/q4.cuh); a zeroed page is valid.
+ *   - Range failures: where = 71 (sp_tree_attn_q4), 76 (sp_qk_norm_rope_q4), 81 (sp_cache_keep_q4), 86 (sp_cache_read_q4);
+ *     they are this section's kind: they keep none of the decode-side calls from working.
+ */
+typedef struct {
+  void* data;              /* 16-byte aligned */
+  int64_t pages, heads;    /* n_kv_heads */
+  int64_t page, head_dim;  /* page in {16, 32, 64, 128, 256} tokens, head_dim in {64, 128} */
+  int64_t stride_page, stride_head; /* in BYTES: multiples of 16, at least page / 16 * 17 * head_dim (size-1: any) */
+} sp_q4_cache;
+
+/* Bytes of one head's page: page / 16 * 17 * head_dim. */
+int sp_q4_page_bytes(int page, int head_dim, int64_t* bytes /* host, out */);
+
+/*
+ * sp_qk_norm_rope_q4 - sp_qk_norm_rope with the 4-bit cache as destination of keys and values: they are quantised on the
+ *   way.  Arguments as there; k_out and v_out (bf16, unquantised) or both NULL.  The codes are those of exact arithmetic on
+ *   the bf16 inputs, not of k_out's rounding: a key within fp32's error of the border between two codes is computed again
+ *   in 64 bits.  cache and slots must be given.  The outputs may not overlap the cache.
+ */
+int sp_qk_norm_rope_q4(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const sp_tensor* v, const void* q_weight,
+                       const void* k_weight, float eps, const double* inv_freq /* host */, int n_freq, int interleaved,
+                       const int32_t* positions, const sp_tensor* q_out, const sp_tensor* k_out, const sp_tensor* v_out,
+                       const sp_q4_cache* cache, const int32_t* slots, void* stream);
+
+/*
+ * sp_tree_attn_q4 - sp_tree_attn over a 4-bit cache: the same rows, masks, results and roundings, the products' keys and
+ *   values being the stored ones exactly.  out must not overlap q or the cache.
+ */
+int sp_tree_attn_q4(sp_ctx* ctx, const sp_tensor* q, const sp_q4_cache* cache, const int32_t* block_table, int max_pages,
+                    const int32_t* seq_lens, const int32_t* row_start, int n_req, const uint32_t* tree_mask, int mask_words,
+                    const sp_tensor* out, float* lse_out, void* stream);
+
+/* sp_cache_keep_q4 - sp_cache_keep on a 4-bit cache: codes and scales move as they are. */
+int sp_cache_keep_q4(sp_ctx* ctx, const sp_q4_cache* cache, const int32_t* block_table, int max_pages, const int32_t* past_lens,
+                     int n_req, const int32_t* kept, const int32_t* n_kept, int max_kept, int32_t* lens_out, void* stream);
+
+/*
+ * sp_cache_read_q4 - cached tokens as bf16 rows (exactly the stored values).  Row row_start[b] + i is token
+ *   seq_lens[b] - n + i of request b, n = row_start[b + 1] - row_start[b]: its last n tokens before seq_lens[b] (with
+ *   n = seq_lens[b]: all of them).  Rows behind row_start[n_req] are left as they were.
+ *   k_out, v_out  bf16 [1, n_kv_heads, rows, head_dim], their own strides; they may not overlap each other or the cache.
+ */
+int sp_cache_read_q4(sp_ctx* ctx, const sp_q4_cache* cache, const int32_t* block_table, int max_pages, const int32_t* seq_lens,
+                     const int32_t* row_start, int n_req, const sp_tensor* k_out, const sp_tensor* v_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

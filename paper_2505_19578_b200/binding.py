@@ -38,6 +38,7 @@ EXPORTS = (
     "sp_selftest_wait_timeout", "sp_fixed_scratch_status", "sp_workspace_bytes_patterns",
     "sp_internal_pair_work_order",
     "sp_page_tables", "sp_qk_norm_rope", "sp_tree_attn", "sp_cache_keep", "sp_ctx_reserve_decode",
+    "sp_q4_page_bytes", "sp_qk_norm_rope_q4", "sp_tree_attn_q4", "sp_cache_keep_q4", "sp_cache_read_q4",
 )
 
 
@@ -98,6 +99,11 @@ def load() -> ctypes.CDLL:
     lib.sp_qk_norm_rope.argtypes = [P, P, P, P, P, P, F, P, I, I, P, P, P, P, P, P, P, P]
     lib.sp_tree_attn.argtypes = [P, P, P, P, P, I, P, P, I, P, I, P, P, P]
     lib.sp_cache_keep.argtypes = [P, P, P, P, I, P, I, P, P, I, P, P]
+    lib.sp_q4_page_bytes.argtypes = [I, I, ctypes.POINTER(ctypes.c_int64)]
+    lib.sp_qk_norm_rope_q4.argtypes = [P, P, P, P, P, P, F, P, I, I, P, P, P, P, P, P, P]
+    lib.sp_tree_attn_q4.argtypes = [P, P, P, P, I, P, P, I, P, I, P, P, P]
+    lib.sp_cache_keep_q4.argtypes = [P, P, P, I, P, I, P, P, I, P, P]
+    lib.sp_cache_read_q4.argtypes = [P, P, P, I, P, P, I, P, P, P]
     lib.sp_ctx_set_kernel.argtypes = [P, I]
     lib.sp_selftest_wait_timeout.argtypes = [P, ctypes.c_int64, P]
     lib.sp_ctx_set_trace.argtypes = [P, P, I]
@@ -150,7 +156,8 @@ def _decode_calls():
         from . import _decode_calls as native
         lib = load()
         native.set_functions(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
-                               for f in ("sp_page_tables", "sp_qk_norm_rope", "sp_tree_attn", "sp_cache_keep")))
+                               for f in ("sp_page_tables", "sp_qk_norm_rope", "sp_tree_attn", "sp_cache_keep",
+                                         "sp_qk_norm_rope_q4", "sp_tree_attn_q4", "sp_cache_keep_q4", "sp_cache_read_q4")))
         _native = native
     return _native
 
@@ -339,6 +346,43 @@ class Context:
             _check(code, "sp_cache_keep")
 
 
+    # ---- the same over a paged cache held in 4 bits: uint8 [pages, Hkv, page_bytes(page, d)], last dimension contiguous, the
+    # other strides multiples of 16
+
+    def sp_qk_norm_rope_q4(self, q, k, v, positions, inv_freq, q_out, cache, slots, k_out=None, v_out=None, q_weight=None,
+                           k_weight=None, eps=1e-6, interleaved=False, stream=None):
+        """As sp_qk_norm_rope; keys and values are quantised into `cache` on the way."""
+        code = (_native or _decode_calls()).qk_norm_rope_q4(
+            self._h.value, self.device, q, k, v, positions, inv_freq, q_out, k_out, v_out, cache, slots, q_weight, k_weight, eps,
+            interleaved, None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_qk_norm_rope_q4")
+
+    def sp_tree_attn_q4(self, q, cache, block_table, seq_lens, row_start, out, tree_mask=None, lse_out=None, stream=None):
+        """As sp_tree_attn, over a 4-bit cache."""
+        code = (_native or _decode_calls()).tree_attn_q4(
+            self._h.value, self.device, q, cache, block_table, seq_lens, row_start, out, tree_mask, lse_out,
+            None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_tree_attn_q4")
+
+    def sp_cache_keep_q4(self, cache, block_table, past_lens, kept, n_kept, lens_out, head_dim, stream=None):
+        """As sp_cache_keep, on a 4-bit cache of heads of `head_dim` elements."""
+        code = (_native or _decode_calls()).cache_keep_q4(
+            self._h.value, self.device, cache, block_table, past_lens, kept, n_kept, lens_out, head_dim,
+            None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_cache_keep_q4")
+
+    def sp_cache_read_q4(self, cache, block_table, seq_lens, row_start, k_out, v_out, stream=None):
+        """k_out, v_out bf16 [Hkv, rows, d]: row row_start[b] + i is token seq_lens[b] - (row_start[b + 1] - row_start[b]) + i."""
+        code = (_native or _decode_calls()).cache_read_q4(
+            self._h.value, self.device, cache, block_table, seq_lens, row_start, k_out, v_out,
+            None if stream is None else stream.cuda_stream)
+        if code:
+            _check(code, "sp_cache_read_q4")
+
+
 class PatternDict:
     """Cross-layer dictionary of pivotal patterns (cluster id -> mask, lists, representative)."""
 
@@ -402,6 +446,13 @@ def workspace_bytes_patterns(seq, n_q_heads, n_kv_heads, head_dim, block, n_pivo
                                               int(bool(pooled_construction)), ctypes.byref(a), ctypes.byref(b)),
            "sp_workspace_bytes_patterns")
     return a.value, b.value
+
+
+def page_bytes(page: int, head_dim: int) -> int:
+    """Bytes of one head's page in a 4-bit cache."""
+    out = ctypes.c_int64()
+    _check(load().sp_q4_page_bytes(page, head_dim, ctypes.byref(out)), "sp_q4_page_bytes")
+    return out.value
 
 
 def pair_work_order(heads, lists, n_q_heads, n_kv_heads, n_row_blocks, n_sm=148, pair_heads=True):

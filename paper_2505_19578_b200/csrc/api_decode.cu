@@ -3,7 +3,7 @@
 #include <string.h>
 
 #include "ctx.cuh"
-#include "decode.cuh"
+#include "q4.cuh"
 
 namespace {
 
@@ -83,6 +83,75 @@ uint64_t turns_per_position(double inv_freq) {
   return p[word] >> off | (word < 3 && off > 0 ? p[word + 1] << (64 - off) : 0);
 }
 
+// What sp_qk_norm_rope and its form for a 4-bit cache have in common: everything but the cache.  `elsewhere`: k and v have a
+// destination besides k_out, v_out.
+int rope_args(const sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const sp_tensor* v, const void* q_weight, const void* k_weight, float eps,
+              const double* inv_freq, int n_freq, int interleaved, const int32_t* positions, const sp_tensor* q_out, const sp_tensor* k_out,
+              const sp_tensor* v_out, bool elsewhere, RopeArgs* out) {
+  if (!ctx || !positions || n_freq < 0 || (n_freq > 0 && !inv_freq)) return SP_ERR_INVALID_ARG;
+  int rc;
+  if ((rc = check_view(q)) || (rc = check_view(k)) || (rc = check_view(v)) || (rc = check_view(q_out))) return rc;
+  if (!same_shape(q, q_out) || !same_shape(k, v)) return SP_ERR_INVALID_ARG;
+  if (q->shape[0] != 1 || k->shape[0] != 1) return SP_ERR_UNSUPPORTED;
+  if (q->shape[2] != k->shape[2] || q->shape[3] != k->shape[3]) return SP_ERR_INVALID_ARG;
+  const int64_t d = q->shape[3];
+  if ((d != 64 && d != 128) || q->shape[1] > kMaxHeads || k->shape[1] > kMaxHeads) return SP_ERR_UNSUPPORTED;
+  if (2 * (int64_t)n_freq > d || n_freq % 8 != 0) return SP_ERR_UNSUPPORTED;
+  if ((q_weight != nullptr) != (k_weight != nullptr)) return SP_ERR_INVALID_ARG;
+  if (((reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight)) & 15) != 0) return SP_ERR_INVALID_ARG;
+  if (q_weight && !(eps >= 0.f && eps < INFINITY)) return SP_ERR_INVALID_ARG;
+  if ((k_out != nullptr) != (v_out != nullptr)) return SP_ERR_INVALID_ARG;
+  if (!k_out && !elsewhere) return SP_ERR_INVALID_ARG;
+  if (k_out) {
+    if ((rc = check_view(k_out)) || (rc = check_view(v_out))) return rc;
+    if (!same_shape(k, k_out) || !same_shape(v, v_out)) return SP_ERR_INVALID_ARG;
+  }
+  RopeArgs& a = *out;
+  memset(&a, 0, sizeof(a));
+  for (int i = 0; i < n_freq; ++i) {
+    if (!(inv_freq[i] >= 0.0 && inv_freq[i] < 1e9)) return SP_ERR_INVALID_ARG;
+    a.phase[i] = turns_per_position(inv_freq[i]);
+  }
+  a.q = static_cast<const __nv_bfloat16*>(q->data);
+  a.k = static_cast<const __nv_bfloat16*>(k->data);
+  a.v = static_cast<const __nv_bfloat16*>(v->data);
+  a.q_out = static_cast<__nv_bfloat16*>(q_out->data);
+  a.q_sh = step(q, 1); a.q_sn = step(q, 2); a.k_sh = step(k, 1); a.k_sn = step(k, 2); a.v_sh = step(v, 1); a.v_sn = step(v, 2);
+  a.qo_sh = step(q_out, 1); a.qo_sn = step(q_out, 2);
+  if (k_out) {
+    a.k_out = static_cast<__nv_bfloat16*>(k_out->data);
+    a.v_out = static_cast<__nv_bfloat16*>(v_out->data);
+    a.ko_sh = step(k_out, 1); a.ko_sn = step(k_out, 2); a.vo_sh = step(v_out, 1); a.vo_sn = step(v_out, 2);
+  }
+  a.q_weight = static_cast<const __nv_bfloat16*>(q_weight);
+  a.k_weight = static_cast<const __nv_bfloat16*>(k_weight);
+  a.positions = positions;
+  a.hq = (int)q->shape[1]; a.hkv = (int)k->shape[1]; a.tokens = (int)q->shape[2]; a.d = (int)d;
+  a.rot = 2 * n_freq; a.interleaved = interleaved != 0; a.eps = eps; a.status = ctx->status;
+  return SP_OK;
+}
+
+// The 4-bit cache of a call.
+struct Q4Shape {
+  int pages, hkv, d, page_log2;
+};
+int check_q4(const sp_q4_cache* c, Q4Shape* s) {
+  if (!c || !c->data || (reinterpret_cast<uintptr_t>(c->data) & 15) != 0) return SP_ERR_INVALID_ARG;
+  for (const int64_t n : {c->pages, c->heads, c->page, c->head_dim})
+    if (n <= 0 || n > INT32_MAX) return SP_ERR_INVALID_ARG;
+  s->page_log2 = log2_of_page(c->page);
+  if (s->page_log2 < 0 || (c->head_dim != 64 && c->head_dim != 128) || c->heads > kMaxHeads) return SP_ERR_UNSUPPORTED;
+  const int64_t bytes = c->page / 16 * (17 * c->head_dim);
+  if (c->pages > 1 && (c->stride_page < bytes || c->stride_page % 16 != 0)) return SP_ERR_INVALID_ARG;
+  if (c->heads > 1 && (c->stride_head < bytes || c->stride_head % 16 != 0)) return SP_ERR_INVALID_ARG;
+  if (c->pages > (INT32_MAX >> s->page_log2)) return SP_ERR_UNSUPPORTED;       // slots are 32-bit
+  s->pages = (int)c->pages; s->hkv = (int)c->heads; s->d = (int)c->head_dim;
+  return SP_OK;
+}
+Q4Cache q4_of(const sp_q4_cache* c) {
+  return Q4Cache{static_cast<uint8_t*>(c->data), c->pages > 1 ? c->stride_page : 0, c->heads > 1 ? c->stride_head : 0};
+}
+
 // The workspace of sp_tree_attn, with the context's device current.
 int reserve_split(sp_ctx* ctx) {
   if (ctx->split_ws) return SP_OK;
@@ -136,57 +205,21 @@ int sp_qk_norm_rope(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const s
                     const void* k_weight, float eps, const double* inv_freq, int n_freq, int interleaved,
                     const int32_t* positions, const sp_tensor* q_out, const sp_tensor* k_out, const sp_tensor* v_out,
                     const sp_tensor* k_cache, const sp_tensor* v_cache, const int32_t* slots, void* stream) {
-  if (!ctx || !positions || n_freq < 0 || (n_freq > 0 && !inv_freq)) return SP_ERR_INVALID_ARG;
-  int rc;
-  if ((rc = check_view(q)) || (rc = check_view(k)) || (rc = check_view(v)) || (rc = check_view(q_out))) return rc;
-  if (!same_shape(q, q_out) || !same_shape(k, v)) return SP_ERR_INVALID_ARG;
-  if (q->shape[0] != 1 || k->shape[0] != 1) return SP_ERR_UNSUPPORTED;
-  if (q->shape[2] != k->shape[2] || q->shape[3] != k->shape[3]) return SP_ERR_INVALID_ARG;
-  const int64_t d = q->shape[3];
-  if ((d != 64 && d != 128) || q->shape[1] > kMaxHeads || k->shape[1] > kMaxHeads) return SP_ERR_UNSUPPORTED;
-  if (2 * (int64_t)n_freq > d || n_freq % 8 != 0) return SP_ERR_UNSUPPORTED;
-  if ((q_weight != nullptr) != (k_weight != nullptr)) return SP_ERR_INVALID_ARG;
-  if (((reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight)) & 15) != 0) return SP_ERR_INVALID_ARG;
-  if (q_weight && !(eps >= 0.f && eps < INFINITY)) return SP_ERR_INVALID_ARG;
-  if ((k_out != nullptr) != (v_out != nullptr) || (k_cache != nullptr) != (v_cache != nullptr)) return SP_ERR_INVALID_ARG;
-  if (!k_out && !k_cache) return SP_ERR_INVALID_ARG;
-  if (k_out) {
-    if ((rc = check_view(k_out)) || (rc = check_view(v_out))) return rc;
-    if (!same_shape(k, k_out) || !same_shape(v, v_out)) return SP_ERR_INVALID_ARG;
-  }
   RopeArgs a;
-  memset(&a, 0, sizeof(a));
+  int rc = rope_args(ctx, q, k, v, q_weight, k_weight, eps, inv_freq, n_freq, interleaved, positions, q_out, k_out, v_out, k_cache != nullptr, &a);
+  if (rc) return rc;
+  if ((k_cache != nullptr) != (v_cache != nullptr)) return SP_ERR_INVALID_ARG;
   if (k_cache) {
     CacheShape c;
     if (!slots) return SP_ERR_INVALID_ARG;
     if ((rc = check_cache(k_cache, v_cache, &c))) return rc;
-    if (c.hkv != k->shape[1] || c.d != d) return SP_ERR_INVALID_ARG;
+    if (c.hkv != a.hkv || c.d != a.d) return SP_ERR_INVALID_ARG;
     a.kc = cache_of(k_cache);
     a.vc = cache_of(v_cache);
     a.page_log2 = c.page_log2;
     a.n_slots = c.pages << c.page_log2;
     a.slots = slots;
   }
-  for (int i = 0; i < n_freq; ++i) {
-    if (!(inv_freq[i] >= 0.0 && inv_freq[i] < 1e9)) return SP_ERR_INVALID_ARG;
-    a.phase[i] = turns_per_position(inv_freq[i]);
-  }
-  a.q = static_cast<const __nv_bfloat16*>(q->data);
-  a.k = static_cast<const __nv_bfloat16*>(k->data);
-  a.v = static_cast<const __nv_bfloat16*>(v->data);
-  a.q_out = static_cast<__nv_bfloat16*>(q_out->data);
-  a.q_sh = step(q, 1); a.q_sn = step(q, 2); a.k_sh = step(k, 1); a.k_sn = step(k, 2); a.v_sh = step(v, 1); a.v_sn = step(v, 2);
-  a.qo_sh = step(q_out, 1); a.qo_sn = step(q_out, 2);
-  if (k_out) {
-    a.k_out = static_cast<__nv_bfloat16*>(k_out->data);
-    a.v_out = static_cast<__nv_bfloat16*>(v_out->data);
-    a.ko_sh = step(k_out, 1); a.ko_sn = step(k_out, 2); a.vo_sh = step(v_out, 1); a.vo_sn = step(v_out, 2);
-  }
-  a.q_weight = static_cast<const __nv_bfloat16*>(q_weight);
-  a.k_weight = static_cast<const __nv_bfloat16*>(k_weight);
-  a.positions = positions;
-  a.hq = (int)q->shape[1]; a.hkv = (int)k->shape[1]; a.tokens = (int)q->shape[2]; a.d = (int)d;
-  a.rot = 2 * n_freq; a.interleaved = interleaved != 0; a.eps = eps; a.status = ctx->status;
   DeviceGuard g(ctx->device);
   if (!g.ok) return SP_ERR_CUDA;
   if (launch_qk_norm_rope(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
@@ -266,6 +299,125 @@ int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cach
   KeepArgs a{cache_of(k_cache), cache_of(v_cache), block_table, past_lens, kept, n_kept, lens_out, n_req, max_pages, max_kept,
              c.hkv, c.d, c.page_log2, c.pages, ctx->status};
   if (launch_cache_keep(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+// ---------------------------------------------------------------- the cache held in 4 bits
+
+int sp_q4_page_bytes(int page, int head_dim, int64_t* bytes) {
+  if (!bytes) return SP_ERR_INVALID_ARG;
+  if (log2_of_page(page) < 0 || (head_dim != 64 && head_dim != 128)) return SP_ERR_UNSUPPORTED;
+  *bytes = (int64_t)page / 16 * (17 * head_dim);
+  return SP_OK;
+}
+
+int sp_qk_norm_rope_q4(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const sp_tensor* v, const void* q_weight,
+                       const void* k_weight, float eps, const double* inv_freq, int n_freq, int interleaved,
+                       const int32_t* positions, const sp_tensor* q_out, const sp_tensor* k_out, const sp_tensor* v_out,
+                       const sp_q4_cache* cache, const int32_t* slots, void* stream) {
+  RopeArgs a;
+  Q4Shape c;
+  int rc = rope_args(ctx, q, k, v, q_weight, k_weight, eps, inv_freq, n_freq, interleaved, positions, q_out, k_out, v_out, true, &a);
+  if (rc) return rc;
+  if (!slots) return SP_ERR_INVALID_ARG;
+  if ((rc = check_q4(cache, &c))) return rc;
+  if (c.hkv != a.hkv || c.d != a.d) return SP_ERR_INVALID_ARG;
+  const Q4Cache to = q4_of(cache);
+  a.q4 = to.data; a.q4_s_page = to.s_page; a.q4_s_head = to.s_head;
+  a.page_log2 = c.page_log2;
+  a.n_slots = c.pages << c.page_log2;
+  a.slots = slots;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  if (launch_qk_norm_rope_q4(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+int sp_tree_attn_q4(sp_ctx* ctx, const sp_tensor* q, const sp_q4_cache* cache, const int32_t* block_table, int max_pages,
+                    const int32_t* seq_lens, const int32_t* row_start, int n_req, const uint32_t* tree_mask, int mask_words,
+                    const sp_tensor* out, float* lse_out, void* stream) {
+  if (!ctx || n_req < 0) return SP_ERR_INVALID_ARG;
+  if (n_req == 0 && q && q->shape[2] == 0) return SP_OK;      // nobody, no rows: tensors without elements
+  int rc;
+  Q4Shape c;
+  if ((rc = check_view(q)) || (rc = check_view(out))) return rc;
+  if ((rc = check_q4(cache, &c))) return rc;
+  if (!same_shape(q, out) || q->shape[3] != c.d) return SP_ERR_INVALID_ARG;
+  if (q->shape[0] != 1 || q->shape[1] > kMaxHeads || q->shape[1] % c.hkv != 0) return SP_ERR_UNSUPPORTED;
+  if (q->shape[2] * (q->shape[1] / c.hkv) > INT32_MAX) return SP_ERR_UNSUPPORTED;
+  if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
+  if (tree_mask && (mask_words < 1 || mask_words > kMaxMaskWords)) return SP_ERR_UNSUPPORTED;
+  if (n_req == 0) return SP_OK;            // as in sp_page_tables
+  if (!block_table || !seq_lens || !row_start || max_pages <= 0) return SP_ERR_INVALID_ARG;
+  if (q->data == out->data) return SP_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  TreeAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = static_cast<const __nv_bfloat16*>(q->data);
+  a.o = static_cast<__nv_bfloat16*>(out->data);
+  a.lse = lse_out;
+  a.q_sh = step(q, 1); a.q_sn = step(q, 2); a.o_sh = step(out, 1); a.o_sn = step(out, 2);
+  a.table = block_table; a.seq_lens = seq_lens; a.row_start = row_start;
+  a.bits = tree_mask; a.words = tree_mask ? mask_words : 0;
+  a.hq = (int)q->shape[1]; a.hkv = c.hkv; a.group = a.hq / a.hkv; a.d = c.d; a.rows = (int)q->shape[2];
+  a.n_req = n_req; a.max_pages = max_pages; a.page_log2 = c.page_log2; a.n_pages = c.pages;
+  a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d));
+  a.status = ctx->status;
+  if (launch_tree_attn_q4_simt(a, q4_of(cache), static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+int sp_cache_keep_q4(sp_ctx* ctx, const sp_q4_cache* cache, const int32_t* block_table, int max_pages, const int32_t* past_lens, int n_req,
+                     const int32_t* kept, const int32_t* n_kept, int max_kept, int32_t* lens_out, void* stream) {
+  if (!ctx || n_req < 0) return SP_ERR_INVALID_ARG;
+  int rc;
+  Q4Shape c;
+  if ((rc = check_q4(cache, &c))) return rc;
+  if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
+  if (n_req == 0) return SP_OK;            // as in sp_page_tables
+  if (!block_table || !past_lens || !n_kept || !lens_out || max_pages <= 0) return SP_ERR_INVALID_ARG;
+  if (kept ? max_kept <= 0 : max_kept != 0) return SP_ERR_INVALID_ARG;     // no column: a list without elements
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  const Array arrays[] = {{block_table, (int64_t)n_req * max_pages, false}, {past_lens, n_req, false},
+                          {kept, (int64_t)n_req * max_kept, false}, {n_kept, n_req, false}, {lens_out, n_req, true}};
+  if (overlapping(arrays)) return SP_ERR_INVALID_ARG;
+  const KeepQ4Args a{q4_of(cache), block_table, past_lens, kept, n_kept, lens_out, n_req, max_pages, max_kept,
+                     c.hkv, c.d, c.page_log2, c.pages, ctx->status};
+  if (launch_cache_keep_q4(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
+  return SP_OK;
+}
+
+int sp_cache_read_q4(sp_ctx* ctx, const sp_q4_cache* cache, const int32_t* block_table, int max_pages, const int32_t* seq_lens,
+                     const int32_t* row_start, int n_req, const sp_tensor* k_out, const sp_tensor* v_out, void* stream) {
+  if (!ctx || n_req < 0) return SP_ERR_INVALID_ARG;
+  if (n_req == 0 && k_out && k_out->shape[2] == 0) return SP_OK;
+  int rc;
+  Q4Shape c;
+  if ((rc = check_view(k_out)) || (rc = check_view(v_out))) return rc;
+  if ((rc = check_q4(cache, &c))) return rc;
+  if (!same_shape(k_out, v_out) || k_out->shape[1] != c.hkv || k_out->shape[3] != c.d || k_out->data == v_out->data) return SP_ERR_INVALID_ARG;
+  if (k_out->shape[0] != 1) return SP_ERR_UNSUPPORTED;
+  if (n_req > kMaxRequests || max_pages > (INT32_MAX >> c.page_log2)) return SP_ERR_UNSUPPORTED;
+  if (n_req == 0) return SP_OK;            // as in sp_page_tables
+  if (!block_table || !seq_lens || !row_start || max_pages <= 0) return SP_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  ReadQ4Args a;
+  memset(&a, 0, sizeof(a));
+  a.c = q4_of(cache);
+  a.table = block_table; a.seq_lens = seq_lens; a.row_start = row_start;
+  a.k = static_cast<__nv_bfloat16*>(k_out->data);
+  a.v = static_cast<__nv_bfloat16*>(v_out->data);
+  a.k_sh = step(k_out, 1); a.k_sn = step(k_out, 2); a.v_sh = step(v_out, 1); a.v_sn = step(v_out, 2);
+  a.n_req = n_req; a.max_pages = max_pages; a.rows = (int)k_out->shape[2]; a.hkv = c.hkv; a.d = c.d;
+  a.page_log2 = c.page_log2; a.n_pages = c.pages; a.status = ctx->status;
+  if (launch_cache_read_q4(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
   ctx->launches += 1;
   return SP_OK;
 }

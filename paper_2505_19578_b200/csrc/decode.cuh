@@ -94,6 +94,8 @@ struct RopeArgs {
   __nv_bfloat16* v_out;        // may be null
   int64_t q_sh, q_sn, k_sh, k_sn, v_sh, v_sn, qo_sh, qo_sn, ko_sh, ko_sn, vo_sh, vo_sn;
   PagedCache kc, vc;           // data null: no cache
+  uint8_t* q4;                 // the 4-bit form's cache; strides in bytes
+  int64_t q4_s_page, q4_s_head;
   const __nv_bfloat16* q_weight;
   const __nv_bfloat16* k_weight;
   const int32_t* positions;

@@ -20,6 +20,10 @@ struct Functions {
   decltype(&sp_qk_norm_rope) qk_norm_rope;
   decltype(&sp_tree_attn) tree_attn;
   decltype(&sp_cache_keep) cache_keep;
+  decltype(&sp_qk_norm_rope_q4) qk_norm_rope_q4;
+  decltype(&sp_tree_attn_q4) tree_attn_q4;
+  decltype(&sp_cache_keep_q4) cache_keep_q4;
+  decltype(&sp_cache_read_q4) cache_read_q4;
 } fn{};
 
 struct Refused {};      // a Python exception has been set
@@ -105,14 +109,16 @@ PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, Body body) {
 }
 
 PyObject* set_functions(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) return PyErr_Format(PyExc_TypeError, "expected 4 addresses");
-  void* p[4];
-  for (int i = 0; i < 4; ++i) {
+  if (n != 8) return PyErr_Format(PyExc_TypeError, "expected 8 addresses");
+  void* p[8];
+  for (int i = 0; i < 8; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "a null address");
   }
   fn = {reinterpret_cast<decltype(fn.page_tables)>(p[0]), reinterpret_cast<decltype(fn.qk_norm_rope)>(p[1]),
-        reinterpret_cast<decltype(fn.tree_attn)>(p[2]), reinterpret_cast<decltype(fn.cache_keep)>(p[3])};
+        reinterpret_cast<decltype(fn.tree_attn)>(p[2]), reinterpret_cast<decltype(fn.cache_keep)>(p[3]),
+        reinterpret_cast<decltype(fn.qk_norm_rope_q4)>(p[4]), reinterpret_cast<decltype(fn.tree_attn_q4)>(p[5]),
+        reinterpret_cast<decltype(fn.cache_keep_q4)>(p[6]), reinterpret_cast<decltype(fn.cache_read_q4)>(p[7])};
   Py_RETURN_NONE;
 }
 
@@ -131,43 +137,106 @@ PyObject* page_tables(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   });
 }
 
+// The 4-bit cache: uint8 [pages, heads, bytes of a page]; the page's size follows from the head's.
+sp_q4_cache q4_view(PyObject* o, int device, int64_t head_dim) {
+  const at::Tensor& t = tensor(o, "cache", "a uint8 tensor", device, at::kByte);
+  const int64_t block = 17 * head_dim;               // 16 tokens
+  if (t.dim() != 3 || (t.size(2) != 1 && t.stride(2) != 1)) {
+    PyErr_SetString(PyExc_ValueError, "cache: expected [pages, heads, bytes of a page], the bytes contiguous");
+    throw Refused();
+  }
+  if (head_dim <= 0 || head_dim > 1024 || t.size(2) % block != 0) {
+    PyErr_Format(PyExc_ValueError, "cache: pages of %lld bytes do not hold heads of %lld elements", (long long)t.size(2), (long long)head_dim);
+    throw Refused();
+  }
+  return sp_q4_cache{t.data_ptr(), t.size(0), t.size(1), t.size(2) / block * 16, head_dim, t.stride(0), t.stride(1)};
+}
+
+// What the two forms of the norm and rotation share of their arguments.
+struct Turning {
+  const double* freq;
+  int n_freq;
+  const void* weight[2];
+  float eps;
+  int interleaved;
+};
+Turning turning(PyObject* inv_freq, PyObject* const* weights, PyObject* eps, PyObject* interleaved, int dev, int64_t d) {
+  Turning r;
+  if (!THPVariable_Check(inv_freq) || THPVariable_Unpack(inv_freq).is_cuda() || THPVariable_Unpack(inv_freq).scalar_type() != at::kDouble ||
+      THPVariable_Unpack(inv_freq).dim() != 1 || !THPVariable_Unpack(inv_freq).is_contiguous()) {
+    PyErr_SetString(PyExc_ValueError, "inv_freq: expected a contiguous one-dimensional float64 tensor on the host");
+    throw Refused();
+  }
+  const at::Tensor& freq = THPVariable_Unpack(inv_freq);
+  r.freq = static_cast<const double*>(freq.data_ptr());
+  r.n_freq = (int)std::min<int64_t>(freq.size(0), INT32_MAX);
+  for (int i = 0; i < 2; ++i) {
+    r.weight[i] = nullptr;
+    if (weights[i] == Py_None) continue;
+    const at::Tensor& w = tensor(weights[i], i ? "k_weight" : "q_weight", "a contiguous bf16 tensor of one head's size", dev, at::kBFloat16);
+    if (w.dim() != 1 || w.size(0) != d || !w.is_contiguous()) refuse(i ? "k_weight" : "q_weight", "a contiguous bf16 tensor of one head's size", dev);
+    r.weight[i] = w.data_ptr();
+  }
+  const double e = PyFloat_AsDouble(eps);
+  if (e == -1.0 && PyErr_Occurred()) throw Refused();
+  r.eps = (float)e;
+  r.interleaved = PyObject_IsTrue(interleaved);
+  if (r.interleaved < 0) throw Refused();
+  return r;
+}
+// Views of up to N arguments, some of them None.
+template <int N>
+struct Views {
+  sp_tensor t[N];
+  const sp_tensor* p[N];
+  Views(PyObject* const* a, const char* const* names, int dev, int first_cache) {
+    for (int i = 0; i < N; ++i) {
+      p[i] = nullptr;
+      if (a[i] == Py_None) continue;
+      t[i] = view(a[i], names[i], dev, i >= first_cache);
+      p[i] = &t[i];
+    }
+  }
+};
+const char* const kOutNames[4] = {"k_out", "v_out", "k_cache", "v_cache"};
+
 // ctx, device, q, k, v, positions, inv_freq, q_out, k_out, v_out, k_cache, v_cache, slots, q_weight, k_weight, eps, interleaved, stream
 PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded(n_args, 18, [&] {
     const int dev = small(a[1]);
     const sp_tensor q = view(a[2], "q", dev, false), k = view(a[3], "k", dev, false), v = view(a[4], "v", dev, false), q_out = view(a[7], "q_out", dev, false);
-    const int64_t rows = q.shape[2], d = q.shape[3];
-    sp_tensor opt[4];
-    const sp_tensor* given[4];
-    const char* names[4] = {"k_out", "v_out", "k_cache", "v_cache"};
-    for (int i = 0; i < 4; ++i) {
-      given[i] = nullptr;
-      if (a[8 + i] == Py_None) continue;
-      opt[i] = view(a[8 + i], names[i], dev, i >= 2);
-      given[i] = &opt[i];
-    }
-    if (!THPVariable_Check(a[6]) || THPVariable_Unpack(a[6]).is_cuda() || THPVariable_Unpack(a[6]).scalar_type() != at::kDouble ||
-        THPVariable_Unpack(a[6]).dim() != 1 || !THPVariable_Unpack(a[6]).is_contiguous()) {
-      PyErr_SetString(PyExc_ValueError, "inv_freq: expected a contiguous one-dimensional float64 tensor on the host");
-      throw Refused();
-    }
-    const at::Tensor& freq = THPVariable_Unpack(a[6]);
-    const void* weight[2];
-    for (int i = 0; i < 2; ++i) {
-      weight[i] = nullptr;
-      if (a[13 + i] == Py_None) continue;
-      const at::Tensor& w = tensor(a[13 + i], i ? "k_weight" : "q_weight", "a contiguous bf16 tensor of one head's size", dev, at::kBFloat16);
-      if (w.dim() != 1 || w.size(0) != d || !w.is_contiguous()) refuse(i ? "k_weight" : "q_weight", "a contiguous bf16 tensor of one head's size", dev);
-      weight[i] = w.data_ptr();
-    }
-    const double eps = PyFloat_AsDouble(a[15]);
-    if (eps == -1.0 && PyErr_Occurred()) throw Refused();
-    const int interleaved = PyObject_IsTrue(a[16]);
-    if (interleaved < 0) throw Refused();
-    return fn.qk_norm_rope(context(a[0]), &q, &k, &v, weight[0], weight[1], (float)eps, static_cast<const double*>(freq.data_ptr()),
-                           (int)std::min<int64_t>(freq.size(0), INT32_MAX), interleaved, ints(a[5], "positions", dev, 1, rows).p, &q_out, given[0], given[1],
-                           given[2], given[3], maybe_ints(a[12], "slots", dev, 1, rows).p, stream_of(a[17], dev));
+    const int64_t rows = q.shape[2];
+    const Views<4> to(a + 8, kOutNames, dev, 2);
+    const Turning r = turning(a[6], a + 13, a[15], a[16], dev, q.shape[3]);
+    return fn.qk_norm_rope(context(a[0]), &q, &k, &v, r.weight[0], r.weight[1], r.eps, r.freq, r.n_freq, r.interleaved, ints(a[5], "positions", dev, 1, rows).p,
+                           &q_out, to.p[0], to.p[1], to.p[2], to.p[3], maybe_ints(a[12], "slots", dev, 1, rows).p, stream_of(a[17], dev));
   });
+}
+
+// ctx, device, q, k, v, positions, inv_freq, q_out, k_out, v_out, cache, slots, q_weight, k_weight, eps, interleaved, stream
+PyObject* qk_norm_rope_q4(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded(n_args, 17, [&] {
+    const int dev = small(a[1]);
+    const sp_tensor q = view(a[2], "q", dev, false), k = view(a[3], "k", dev, false), v = view(a[4], "v", dev, false), q_out = view(a[7], "q_out", dev, false);
+    const int64_t rows = q.shape[2];
+    const Views<2> to(a + 8, kOutNames, dev, 2);
+    const sp_q4_cache cache = q4_view(a[10], dev, q.shape[3]);
+    const Turning r = turning(a[6], a + 12, a[14], a[15], dev, q.shape[3]);
+    return fn.qk_norm_rope_q4(context(a[0]), &q, &k, &v, r.weight[0], r.weight[1], r.eps, r.freq, r.n_freq, r.interleaved,
+                              ints(a[5], "positions", dev, 1, rows).p, &q_out, to.p[0], to.p[1], &cache, ints(a[11], "slots", dev, 1, rows).p, stream_of(a[16], dev));
+  });
+}
+
+float* lse_of(PyObject* o, const sp_tensor& q, int dev) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o, "lse_out", "a contiguous fp32 tensor [heads, rows]", dev, at::kFloat);
+  if (t.dim() != 2 || t.size(0) != q.shape[1] || t.size(1) != q.shape[2] || !t.is_contiguous()) refuse("lse_out", "a contiguous fp32 tensor [heads, rows]", dev);
+  return static_cast<float*>(t.data_ptr());
+}
+Ints tree_bits(PyObject* o, const sp_tensor& q, int dev) {
+  const Ints bits = maybe_ints(o, "tree_mask", dev, 2, q.shape[2]);
+  if (o != Py_None && bits.n1 < 1) { PyErr_SetString(PyExc_ValueError, "tree_mask: expected at least one word a row"); throw Refused(); }   // its address would be null: a chain
+  return bits;
 }
 
 // ctx, device, q, k_cache, v_cache, block_table, seq_lens, row_start, out, tree_mask, lse_out, stream
@@ -178,14 +247,8 @@ PyObject* tree_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const Ints lens = ints(a[6], "seq_lens", dev, 1, -1);
     const int n = lens.n0;
     const Ints table = ints(a[5], "block_table", dev, 2, n), start = ints(a[7], "row_start", dev, 1, (int64_t)n + 1);
-    const Ints bits = maybe_ints(a[9], "tree_mask", dev, 2, q.shape[2]);
-    if (a[9] != Py_None && bits.n1 < 1) { PyErr_SetString(PyExc_ValueError, "tree_mask: expected at least one word a row"); throw Refused(); }   // its address would be null: a chain
-    float* lse = nullptr;
-    if (a[10] != Py_None) {
-      const at::Tensor& t = tensor(a[10], "lse_out", "a contiguous fp32 tensor [heads, rows]", dev, at::kFloat);
-      if (t.dim() != 2 || t.size(0) != q.shape[1] || t.size(1) != q.shape[2] || !t.is_contiguous()) refuse("lse_out", "a contiguous fp32 tensor [heads, rows]", dev);
-      lse = static_cast<float*>(t.data_ptr());
-    }
+    const Ints bits = tree_bits(a[9], q, dev);
+    float* lse = lse_of(a[10], q, dev);
     return fn.tree_attn(context(a[0]), &q, &k, &v, table.p, table.n1, lens.p, start.p, n, reinterpret_cast<uint32_t*>(bits.p), bits.n1, &out, lse,
                         stream_of(a[11], dev));
   });
@@ -204,15 +267,61 @@ PyObject* cache_keep(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   });
 }
 
+// ctx, device, q, cache, block_table, seq_lens, row_start, out, tree_mask, lse_out, stream
+PyObject* tree_attn_q4(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded(n_args, 11, [&] {
+    const int dev = small(a[1]);
+    const sp_tensor q = view(a[2], "q", dev, false), out = view(a[7], "out", dev, false);
+    const sp_q4_cache cache = q4_view(a[3], dev, q.shape[3]);
+    const Ints lens = ints(a[5], "seq_lens", dev, 1, -1);
+    const int n = lens.n0;
+    const Ints table = ints(a[4], "block_table", dev, 2, n), start = ints(a[6], "row_start", dev, 1, (int64_t)n + 1);
+    const Ints bits = tree_bits(a[8], q, dev);
+    float* lse = lse_of(a[9], q, dev);
+    return fn.tree_attn_q4(context(a[0]), &q, &cache, table.p, table.n1, lens.p, start.p, n, reinterpret_cast<uint32_t*>(bits.p), bits.n1, &out, lse,
+                           stream_of(a[10], dev));
+  });
+}
+
+// ctx, device, cache, block_table, past_lens, kept, n_kept, lens_out, head_dim, stream
+PyObject* cache_keep_q4(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded(n_args, 10, [&] {
+    const int dev = small(a[1]);
+    const sp_q4_cache cache = q4_view(a[2], dev, integer(a[8]));
+    const Ints past = ints(a[4], "past_lens", dev, 1, -1);
+    const int n = past.n0;
+    const Ints table = ints(a[3], "block_table", dev, 2, n), kept = ints(a[5], "kept", dev, 2, n), n_kept = ints(a[6], "n_kept", dev, 1, n);
+    const Ints lens = ints(a[7], "lens_out", dev, 1, n);
+    return fn.cache_keep_q4(context(a[0]), &cache, table.p, table.n1, past.p, n, kept.p, n_kept.p, kept.n1, lens.p, stream_of(a[9], dev));
+  });
+}
+
+// ctx, device, cache, block_table, seq_lens, row_start, k_out, v_out, stream
+PyObject* cache_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded(n_args, 9, [&] {
+    const int dev = small(a[1]);
+    const sp_tensor k = view(a[6], "k_out", dev, false), v = view(a[7], "v_out", dev, false);
+    const sp_q4_cache cache = q4_view(a[2], dev, k.shape[3]);
+    const Ints lens = ints(a[4], "seq_lens", dev, 1, -1);
+    const int n = lens.n0;
+    const Ints table = ints(a[3], "block_table", dev, 2, n), start = ints(a[5], "row_start", dev, 1, (int64_t)n + 1);
+    return fn.cache_read_q4(context(a[0]), &cache, table.p, table.n1, lens.p, start.p, n, &k, &v, stream_of(a[8], dev));
+  });
+}
+
 template <typename F>
 PyCFunction method(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f)); }
 
 PyMethodDef methods[] = {
-    {"set_functions", method(set_functions), METH_FASTCALL, "addresses of sp_page_tables, sp_qk_norm_rope, sp_tree_attn, sp_cache_keep"},
+    {"set_functions", method(set_functions), METH_FASTCALL, "addresses of sp_page_tables, sp_qk_norm_rope, sp_tree_attn, sp_cache_keep, and of the last three's _q4 forms and sp_cache_read_q4"},
     {"page_tables", method(page_tables), METH_FASTCALL, "status code of sp_page_tables"},
     {"qk_norm_rope", method(qk_norm_rope), METH_FASTCALL, "status code of sp_qk_norm_rope"},
     {"tree_attn", method(tree_attn), METH_FASTCALL, "status code of sp_tree_attn"},
     {"cache_keep", method(cache_keep), METH_FASTCALL, "status code of sp_cache_keep"},
+    {"qk_norm_rope_q4", method(qk_norm_rope_q4), METH_FASTCALL, "status code of sp_qk_norm_rope_q4"},
+    {"tree_attn_q4", method(tree_attn_q4), METH_FASTCALL, "status code of sp_tree_attn_q4"},
+    {"cache_keep_q4", method(cache_keep_q4), METH_FASTCALL, "status code of sp_cache_keep_q4"},
+    {"cache_read_q4", method(cache_read_q4), METH_FASTCALL, "status code of sp_cache_read_q4"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_decode_calls", "Decode-side calls of the SharePrefill library on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

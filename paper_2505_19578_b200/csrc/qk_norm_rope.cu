@@ -14,7 +14,16 @@
 // position), so that position * frequency modulo one turn is one wrapping integer product; its top 32 bits (2^-32 cut off) go
 // to sincospif as fp32 half turns (24 bits: 2^-26 of a turn).  Under 2^-25 of a turn in all, at any position; fp32 products would be off by
 // 4e-3 rad at position 1e5.  Everything else is fp32, rounded once to bf16.
-#include "decode.cuh"
+//
+// The form for a cache held in 4 bits (q4.cuh has the format) stores keys and values as codes with a scale for each 32
+// elements of a head: a = max |y|, s = a / 7 to four significant bits, code = y / s to the nearest, both ties to even.  An
+// 8-element piece is a word of codes.  Keys are quantised from the fp32 values, not from their bf16 rounding.  The code is
+// the one that exact arithmetic gives: where the fp32 value lies within its own error of a border between two codes or two
+// scales (a per mille of the heads), the warp computes the pass again in 64 bits.  So the same token has the same codes
+// whichever kernel stored it, and a border decides nothing by chance.
+#include <math_constants.h>
+
+#include "q4.cuh"
 
 namespace sp {
 namespace {
@@ -96,12 +105,179 @@ __device__ __forceinline__ void angles(const uint64_t (&f)[2], int pos, const La
   }
 }
 
-// Norm and rotation of one pass (q and k; v goes through as it is) and its stores.  Whole warps.
+// The largest of the lanes' v0 (piece c0) and v1 (piece c1) over the pieces of each piece's group of 32 elements.  Whole warps.
+template <int D, typename T>
+__device__ __forceinline__ void group_max(const RopeArgs& a, const Lane<D>& ln, T& v0, T& v1) {
+  constexpr uint32_t kAll = 0xffffffffu;
+  auto larger = [](T x, T y) { return x > y ? x : y; };
+  if (a.interleaved || a.rot % 64 == 0) {          // a group's four pieces are those of four neighbouring lanes
+#pragma unroll
+    for (int o = 1; o <= 2; o <<= 1) {
+      v0 = larger(v0, __shfl_xor_sync(kAll, v0, o));
+      v1 = larger(v1, __shfl_xor_sync(kAll, v1, o));
+    }
+    return;
+  }
+  T m0 = 0, m1 = 0;
+#pragma unroll 1
+  for (int y = 0; y < D / 32; ++y) {
+    T m = larger(ln.c0 >> 2 == y ? v0 : (T)0, ln.c1 >> 2 == y ? v1 : (T)0);
+#pragma unroll
+    for (int o = 1; o < Lane<D>::LPH; o <<= 1) m = larger(m, __shfl_xor_sync(kAll, m, o));
+    if (ln.c0 >> 2 == y) m0 = m;
+    if (ln.c1 >> 2 == y) m1 = m;
+  }
+  v0 = m0;
+  v1 = m1;
+}
+
+struct Codes {                     // of a lane's two pieces: words of codes, and their groups' scale bytes
+  uint32_t word0, word1, scale0, scale1;
+};
+__device__ __forceinline__ uint32_t clamp_scale(uint32_t bits) { return min(max(bits, kScaleLeast), kScaleMost); }
+// Scale of a group whose largest magnitude is a, as fp32 bits: a / 7 to three bits behind the leading one, ties to even.
+__device__ __forceinline__ uint32_t scale_bits(float a) {
+  const uint32_t u = __float_as_uint(__fdiv_rn(a, 7.f));
+  return clamp_scale((u + 0x7ffffu + (u >> 20 & 1u)) & 0xfff00000u);
+}
+__device__ __forceinline__ uint32_t scale_byte(uint32_t bits) { return (bits - kScaleLeast) >> 20; }
+
+// Codes of eight elements, each off by at most e; `unsure` is set where that could change one.  e = 0: exact inputs, of few
+// enough bits for the remainder to be exact, and a tie goes to the even code.
+__device__ __forceinline__ uint32_t piece_codes(const float2 (&v)[4], float s, float e, bool& unsure) {
+  const float inv = __frcp_rn(s), half = 0.5f * s;
+  auto code = [&](float y) {
+    y = y == y ? y : 0.f;                          // a NaN counts as zero
+    float r = rintf(fminf(fmaxf(y * inv, -7.f), 7.f));
+    const float rem = fmaf(-r, s, y), d = half - fabsf(rem);
+    if (e > 0.f) unsure |= fabsf(d) <= e;
+    else if (d < 0.f || (d == 0.f && ((int)r & 1))) r = fminf(fmaxf(r + copysignf(1.f, rem), -7.f), 7.f);
+    return (uint32_t)((int)r + 8);
+  };
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w |= (code(v[i].x) | code(v[i].y) << 16) << (4 * i);
+  return w;
+}
+
+// The codes of a pass of keys in 64 bits, from its inputs.  Out of line and rare.  Whole warps.
 template <int D>
-__device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln, const Pass& p, bool is_v, bool is_q, int t, int slot, uint4 in0, uint4 in1,
+__device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0, uint4 in1) {
+  const Lane<D> ln(a, threadIdx.x & 31);
+  double y[2][8];
+  {
+    float2 x0[4], x1[4];
+    unpack8(in0, x0);
+    unpack8(in1, x1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { y[0][2 * i] = x0[i].x; y[0][2 * i + 1] = x0[i].y; y[1][2 * i] = x1[i].x; y[1][2 * i + 1] = x1[i].y; }
+  }
+  if (a.k_weight) {
+    double ss = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss += y[0][i] * y[0][i] + y[1][i] * y[1][i];
+#pragma unroll
+    for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    const double inv = 1.0 / sqrt(ss * (1.0 / D) + (double)a.eps);
+    float2 w0[4], w1[4];
+    unpack8(__ldg(reinterpret_cast<const uint4*>(a.k_weight + ln.c0 * 8)), w0);
+    unpack8(__ldg(reinterpret_cast<const uint4*>(a.k_weight + ln.c1 * 8)), w1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[0][2 * i] *= inv * w0[i].x; y[0][2 * i + 1] *= inv * w0[i].y;
+      y[1][2 * i] *= inv * w1[i].x; y[1][2 * i + 1] *= inv * w1[i].y;
+    }
+  }
+  auto turn = [&](double& u, double& v, int pair) {
+    const uint64_t turns = a.phase[pair] * (uint64_t)(int64_t)pos;
+    double c, s;
+    sincospi((double)(int64_t)turns * 1.0842021724855044e-19 /* 2^-63: half turns */, &s, &c);
+    const double w = u * c - v * s;
+    v = v * c + u * s;
+    u = w;
+  };
+  if (a.interleaved) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      if (x == 0 ? ln.turn0 : ln.turn1)
+        for (int i = 0; i < 4; ++i) turn(y[x][2 * i], y[x][2 * i + 1], 4 * (x == 0 ? ln.c0 : ln.c1) + i);
+  } else if (ln.turn0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn(y[0][i], y[1][i], 8 * ln.c0 + i);
+  }
+  double m[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    m[x] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[x] = fmax(m[x], fabs(y[x][i]));
+  }
+  group_max<D>(a, ln, m[0], m[1]);
+  Codes out;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    // the same rounding of a / 7 as scale_bits, on the bits of a double; clamped first, so that the result is one of fp32
+    const double f = fmin(fmax(m[x] / 7.0, 9.5367431640625e-07), 3840.0);
+    const unsigned long long u = (unsigned long long)__double_as_longlong(f), odd = u >> 49 & 1;
+    const double s = __longlong_as_double((long long)((u + ((1ull << 48) - 1) + odd) & ~((1ull << 49) - 1)));
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      double t = y[x][i] / s;
+      t = t == t ? fmin(fmax(t, -7.0), 7.0) : 0.0;
+      w |= (uint32_t)((int)rint(t) + 8) << (4 * (i >> 1) + 16 * (i & 1));
+    }
+    const uint32_t byte = scale_byte(clamp_scale(__float_as_uint((float)s)));
+    if (x == 0) { out.word0 = w; out.scale0 = byte; } else { out.word1 = w; out.scale1 = byte; }
+  }
+  return out;
+}
+
+// Codes of a pass of keys (`x`, `y`: its pieces in fp32, largest magnitude of the head before the rotation `top`) or values.
+template <int D>
+__device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, bool is_v, float top, int pos, uint4 in0, uint4 in1, const float2 (&x)[4],
+                                          const float2 (&y)[4]) {
+  // fp32: the norm is off by under 7.5e-7, relative (16 roundings of the sum of squares, halved by the root, its 2 ulp and the
+  // products), the angle by 1.9e-7, sine and cosine by 1.2e-7 and the rotation's two roundings by as much: 1.2e-6 of |a| + |b|,
+  // which is at most 2 top.
+  const bool normed = !is_v && a.k_weight != nullptr, turned = !is_v && a.rot > 0;
+  const float err = normed || turned ? 4e-6f * top : 0.f;
+  float a0 = 0.f, a1 = 0.f;                        // (a NaN drops out)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a0 = fmaxf(a0, fmaxf(fabsf(x[i].x), fabsf(x[i].y)));
+    a1 = fmaxf(a1, fmaxf(fabsf(y[i].x), fabsf(y[i].y)));
+  }
+  group_max<D>(a, ln, a0, a1);
+  const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
+  bool unsure = false;
+  if (err != 0.f)                                  // uniform over the lanes of a head
+    unsure = scale_bits(a0 + err) != scale_bits(fmaxf(a0 - err, 0.f)) || scale_bits(a1 + err) != scale_bits(fmaxf(a1 - err, 0.f));
+  Codes c;
+  c.word0 = piece_codes(x, __uint_as_float(s0), normed || ln.turn0 ? err : 0.f, unsure);
+  c.word1 = piece_codes(y, __uint_as_float(s1), normed || ln.turn1 ? err : 0.f, unsure);
+  c.scale0 = scale_byte(s0);
+  c.scale1 = scale_byte(s1);
+  if (!is_v && __any_sync(0xffffffffu, unsure || !(top < 1e38f))) c = exact_codes<D>(a, pos, in0, in1);
+  return c;
+}
+
+// Norm and rotation of one pass (q and k; v goes through as it is) and its stores.  Whole warps.  Q4: keys and values go into
+// the 4-bit cache.
+template <int D, bool Q4>
+__device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln, const Pass& p, bool is_v, bool is_q, int t, int slot, int pos, uint4 in0, uint4 in1,
                                             const float (&cs)[8], const float (&sn)[8]) {
+  Codes codes;
+  if (Q4 && is_v) {
+    float2 x[4], y[4];
+    unpack8(in0, x);
+    unpack8(in1, y);
+    codes = codes_of<D>(a, ln, true, 0.f, pos, in0, in1, x, y);
+  }
   if (!is_v) {                                     // uniform over the warp
     float2 x[4], y[4];
+    float top = 0.f;
+    bool odd = false;                              // the squares' sum left the range in which it is exact to the bound below
     unpack8(in0, x);
     unpack8(in1, y);
     const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
@@ -114,12 +290,20 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
       float ss = sum.x + sum.y;
 #pragma unroll
       for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      if (Q4 && !is_q) odd = !(ss <= 1e38f) || (ss < 1e-30f && a.eps < 1e-20f);
       const float2 inv = both(rsqrtf(ss * (1.f / D) + a.eps));       // 2 ulp of fp32
       float2 wx[4], wy[4];
       unpack8(__ldg(reinterpret_cast<const uint4*>(weight + ln.c0 * 8)), wx);
       unpack8(__ldg(reinterpret_cast<const uint4*>(weight + ln.c1 * 8)), wy);
 #pragma unroll
       for (int i = 0; i < 4; ++i) { x[i] = __fmul2_rn(x[i], __fmul2_rn(inv, wx[i])); y[i] = __fmul2_rn(y[i], __fmul2_rn(inv, wy[i])); }
+    }
+    if (Q4 && !is_q) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fmaxf(fabsf(x[i].x), fabsf(x[i].y)), fmaxf(fabsf(y[i].x), fabsf(y[i].y))));
+#pragma unroll
+      for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (odd) top = CUDART_INF_F;
     }
     if (ln.turn0 || ln.turn1) {
       if (a.interleaved) {
@@ -135,6 +319,7 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
         }
       }
     }
+    if (Q4 && !is_q) codes = codes_of<D>(a, ln, false, top, pos, in0, in1, x, y);
     in0 = pack8(x);
     in1 = pack8(y);
   }
@@ -150,6 +335,16 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
   const bool k = p.kind == 1;
   if (k ? a.k_out != nullptr : a.v_out != nullptr) put(k ? a.k_out + p.head * a.ko_sh + t * a.ko_sn : a.v_out + p.head * a.vo_sh + t * a.vo_sn);
   if (slot >= 0 && slot < a.n_slots) {             // a negative slot: a row that no request owns
+    if (Q4) {
+      using B = Block<D>;
+      const int in = slot & ((1 << a.page_log2) - 1), i = in & 15;
+      uint8_t* block = a.q4 + (int64_t)(slot >> a.page_log2) * a.q4_s_page + p.head * a.q4_s_head + (in >> 4) * B::BYTES;
+      *reinterpret_cast<uint32_t*>(block + (k ? B::k_word(i, ln.c0) : B::v_word(i, ln.c0))) = codes.word0;
+      *reinterpret_cast<uint32_t*>(block + (k ? B::k_word(i, ln.c1) : B::v_word(i, ln.c1))) = codes.word1;
+      if ((ln.c0 & 3) == 0) block[k ? B::k_scale(i, ln.c0 >> 2) : B::v_scale(i, ln.c0 >> 2)] = (uint8_t)codes.scale0;
+      if ((ln.c1 & 3) == 0) block[k ? B::k_scale(i, ln.c1 >> 2) : B::v_scale(i, ln.c1 >> 2)] = (uint8_t)codes.scale1;
+      return;
+    }
     const PagedCache& c = k ? a.kc : a.vc;
     put(c.data + (int64_t)(slot >> a.page_log2) * c.s_page + (slot & ((1 << a.page_log2) - 1)) * c.s_tok + p.head * c.s_head);
   }
@@ -157,8 +352,10 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
 
 // Few rows: as many warps per token as fill the device, each its share of the token's passes.
 constexpr int kRopeThreads = 128;
+template <bool Q4>
+__device__ __forceinline__ bool cached(const RopeArgs& a) { return Q4 || a.kc.data != nullptr; }
 
-template <int D>
+template <int D, bool Q4>
 __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int RUN = 2;                           // passes whose loads are in flight together
   const int lane = threadIdx.x & 31;
@@ -171,8 +368,8 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const __grid
   wait_for_previous();
   if (decode_poisoned(a.status) || t >= a.tokens) return;
   const int pq = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW, pkv = (a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW, passes = pq + 2 * pkv;
-  const int pos = a.positions[t], slot = a.kc.data ? a.slots[t] : -1;
-  if (slot >= a.n_slots && a.kc.data && lane == 0) report_range(a.status, kWhereRopeSlot);
+  const int pos = a.positions[t], slot = cached<Q4>(a) ? a.slots[t] : -1;
+  if (slot >= a.n_slots && cached<Q4>(a) && lane == 0) report_range(a.status, Q4 ? (int)kWhereRopeSlotQ4 : (int)kWhereRopeSlot);
   float cs[8], sn[8];
   bool have = false;
   for (int p0 = split; p0 < passes; p0 += RUN * a.splits) {
@@ -195,7 +392,7 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const __grid
 #pragma unroll
     for (int u = 0; u < RUN; ++u) {
       const int p = p0 + u * a.splits;
-      if (p < passes) finish_pass<D>(a, ln, pass[u], p >= pq + pkv, p < pq, t, slot, in0[u], in1[u], cs, sn);
+      if (p < passes) finish_pass<D, Q4>(a, ln, pass[u], p >= pq + pkv, p < pq, t, slot, pos, in0[u], in1[u], cs, sn);
     }
   }
 }
@@ -210,7 +407,7 @@ constexpr int kStreamItem = kStreamRun * 1024 + 32;        // bytes of an item: 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
 
-template <int D>
+template <int D, bool Q4>
 __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kernel(const __grid_constant__ RopeArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -254,7 +451,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
         }
       }
       if (lane == 0) copy4(at + kStreamRun * 1024, a.positions + ahead.t);
-      if (lane == 1 && a.kc.data) copy4(at + kStreamRun * 1024 + 4, a.slots + ahead.t);
+      if (lane == 1 && cached<Q4>(a)) copy4(at + kStreamRun * 1024 + 4, a.slots + ahead.t);
       next(ahead);
       if (++fstage == kStreamStages) fstage = 0;
     }
@@ -271,17 +468,17 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
     __syncwarp();                                  // position and slot were copied by lanes 0 and 1
     const uint8_t* at = mine + stage * kStreamItem;
     const int pos = *reinterpret_cast<const int*>(at + kStreamRun * 1024);
-    const int slot = a.kc.data ? *reinterpret_cast<const int*>(at + kStreamRun * 1024 + 4) : -1;
+    const int slot = cached<Q4>(a) ? *reinterpret_cast<const int*>(at + kStreamRun * 1024 + 4) : -1;
     if (angle_of != t) {
       angles<D>(f, pos, ln, cs, sn);
       angle_of = t;
-      if (slot >= a.n_slots && a.kc.data && lane == 0) report_range(a.status, kWhereRopeSlot);
+      if (slot >= a.n_slots && cached<Q4>(a) && lane == 0) report_range(a.status, Q4 ? (int)kWhereRopeSlotQ4 : (int)kWhereRopeSlot);
     }
 #pragma unroll
     for (int u = 0; u < kStreamRun; ++u) {
       const int p = x.b * kStreamRun + u;
       if (p < passes)
-        finish_pass<D>(a, ln, ln.pass(a, p), p >= pq + pkv, p < pq, t, slot, *reinterpret_cast<const uint4*>(at + u * 1024 + lane * 16),
+        finish_pass<D, Q4>(a, ln, ln.pass(a, p), p >= pq + pkv, p < pq, t, slot, pos, *reinterpret_cast<const uint4*>(at + u * 1024 + lane * 16),
                        *reinterpret_cast<const uint4*>(at + u * 1024 + 512 + lane * 16), cs, sn);
     }
     __syncwarp();                                  // all have read position and slot before the stage is filled again
@@ -289,7 +486,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
   }
 }
 
-template <int D>
+template <int D, bool Q4>
 cudaError_t launch(RopeArgs& a, cudaStream_t s) {
   // From an item for every other of the device's warps on, the streaming kernel (36 heads, with it and with the other one:
   // 250 rows 4.8 and 4.2 us, 500 rows 5.5 and 7.0, 1000 rows 7.6 and 8.8; 131072 rows of 48 heads, head-major and cached: 662
@@ -298,18 +495,19 @@ cudaError_t launch(RopeArgs& a, cudaStream_t s) {
   const long long items = (long long)a.tokens * ((passes + kStreamRun - 1) / kStreamRun);
   if (items >= 148 * kStreamWarps / 2) {
     constexpr int smem = kStreamWarps * kStreamStages * kStreamItem;
-    const cudaError_t e = cudaFuncSetAttribute(qk_norm_rope_stream_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e = cudaFuncSetAttribute(qk_norm_rope_stream_kernel<D, Q4>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return launch_dependent(qk_norm_rope_stream_kernel<D>, dim3(148), dim3(kStreamWarps * 32), smem, s, a);
+    return launch_dependent(qk_norm_rope_stream_kernel<D, Q4>, dim3(148), dim3(kStreamWarps * 32), smem, s, a);
   }
   const long long splits = (148ll * 32 + a.tokens - 1) / a.tokens;             // warps to fill the device
   a.splits = (int)(splits > passes ? passes : splits);
   const long long warps = (long long)a.tokens * a.splits;
-  return launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)((warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32))), dim3(kRopeThreads), 0, s, a);
+  return launch_dependent(qk_norm_rope_kernel<D, Q4>, dim3((unsigned)((warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32))), dim3(kRopeThreads), 0, s, a);
 }
 
 }  // namespace
 
-cudaError_t launch_qk_norm_rope(RopeArgs& a, cudaStream_t s) { return a.d == 128 ? launch<128>(a, s) : launch<64>(a, s); }
+cudaError_t launch_qk_norm_rope(RopeArgs& a, cudaStream_t s) { return a.d == 128 ? launch<128, false>(a, s) : launch<64, false>(a, s); }
+cudaError_t launch_qk_norm_rope_q4(RopeArgs& a, cudaStream_t s) { return a.d == 128 ? launch<128, true>(a, s) : launch<64, true>(a, s); }
 
 }  // namespace sp

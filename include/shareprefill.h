@@ -476,7 +476,7 @@ int sp_prefill_attn_layer(sp_ctx* ctx, sp_pattern_dict* dict, const sp_tensor* q
  *     status has been read.
  */
 
-/* Allocate the workspace of sp_tree_attn (39 MB with 148 SMs; it depends on the device alone and never moves).  Its
+/* Allocate the workspace of sp_tree_attn and sp_tree_attn_q4 (39 MB with 148 SMs; it depends on the device alone and never moves).  Its
  * first call does so otherwise; inside a stream capture that call returns SP_ERR_WORKSPACE and enqueues nothing. */
 int sp_ctx_reserve_decode(sp_ctx* ctx);
 

@@ -21,7 +21,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libshareprefill.so")
 LIB_DEBUG = os.path.join(HERE, "libshareprefill_debug.so")   # the same sources with -DSP_DEBUG: range-checked indices
 SOURCES = ["api.cu", "attn_pair.cu", "attn_tc.cu", "attn_simt.cu", "mask_kernel.cu", "pooled_pattern.cu", "vslash.cu",
-           "api_decode.cu", "page_tables.cu", "qk_norm_rope.cu", "tree_attn.cu", "tree_attn_simt.cu", "q4_cache.cu"]
+           "api_decode.cu", "page_tables.cu", "qk_norm_rope.cu", "tree_attn.cu", "tree_attn_simt.cu", "q4_cache.cu", "q4_attn.cu"]
 CALLS = os.path.join(HERE, "_decode_calls.so")
 CALLS_SOURCE = os.path.join(CSRC, "decode_calls.cpp")
 HEADERS = [os.path.join(CSRC, "common.cuh"), os.path.join(ROOT, "include", "shareprefill.h")]

@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "ctx.cuh"
 #include "q4.cuh"
 
@@ -152,16 +154,25 @@ Q4Cache q4_of(const sp_q4_cache* c) {
   return Q4Cache{static_cast<uint8_t*>(c->data), c->pages > 1 ? c->stride_page : 0, c->heads > 1 ? c->stride_head : 0};
 }
 
-// The workspace of sp_tree_attn, with the context's device current.
+// The workspace of sp_tree_attn and sp_tree_attn_q4, with the context's device current.
 int reserve_split(sp_ctx* ctx) {
   if (ctx->split_ws) return SP_OK;
   int n_sm = 0;
   if (cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, ctx->device) != cudaSuccess) return SP_ERR_CUDA;
   void* p = nullptr;
-  if (cudaMalloc(&p, tree_attn_workspace_bytes(n_sm)) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
+  if (cudaMalloc(&p, std::max(tree_attn_workspace_bytes(n_sm), tree_attn_q4_workspace_bytes(n_sm))) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
   ctx->split_ws = p;
   ctx->n_sm = n_sm;
   return SP_OK;
+}
+
+// ... for a call on this stream: an allocation inside a stream capture would spoil the capture.
+int need_split(sp_ctx* ctx, cudaStream_t s) {
+  if (ctx->split_ws) return SP_OK;
+  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
+  if (capturing != cudaStreamCaptureStatusNone) return SP_ERR_WORKSPACE;
+  return reserve_split(ctx);
 }
 
 }  // namespace
@@ -268,13 +279,7 @@ int sp_tree_attn(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k_cache, cons
     ctx->launches += 1;
     return SP_OK;
   }
-  if (!ctx->split_ws) {
-    // an allocation inside a stream capture would spoil the capture
-    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
-    if (capturing != cudaStreamCaptureStatusNone) return SP_ERR_WORKSPACE;
-    if ((rc = reserve_split(ctx))) return rc;
-  }
+  if ((rc = need_split(ctx, s))) return rc;
   if (launch_tree_attn(a, ctx->split_ws, ctx->n_sm, s) != cudaSuccess) return SP_ERR_CUDA;
   ctx->launches += 2;
   return SP_OK;
@@ -366,8 +371,15 @@ int sp_tree_attn_q4(sp_ctx* ctx, const sp_tensor* q, const sp_q4_cache* cache, c
   a.n_req = n_req; a.max_pages = max_pages; a.page_log2 = c.page_log2; a.n_pages = c.pages;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d));
   a.status = ctx->status;
-  if (launch_tree_attn_q4_simt(a, q4_of(cache), static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;
-  ctx->launches += 1;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (ctx->kernel == 1) {
+    if (launch_tree_attn_q4_simt(a, q4_of(cache), s) != cudaSuccess) return SP_ERR_CUDA;
+    ctx->launches += 1;
+    return SP_OK;
+  }
+  if ((rc = need_split(ctx, s))) return rc;
+  if (launch_tree_attn_q4(a, q4_of(cache), ctx->split_ws, ctx->n_sm, s) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 2;
   return SP_OK;
 }
 
@@ -381,11 +393,11 @@ int sp_cache_keep_q4(sp_ctx* ctx, const sp_q4_cache* cache, const int32_t* block
   if (n_req == 0) return SP_OK;            // as in sp_page_tables
   if (!block_table || !past_lens || !n_kept || !lens_out || max_pages <= 0) return SP_ERR_INVALID_ARG;
   if (kept ? max_kept <= 0 : max_kept != 0) return SP_ERR_INVALID_ARG;     // no column: a list without elements
-  DeviceGuard g(ctx->device);
-  if (!g.ok) return SP_ERR_CUDA;
   const Array arrays[] = {{block_table, (int64_t)n_req * max_pages, false}, {past_lens, n_req, false},
                           {kept, (int64_t)n_req * max_kept, false}, {n_kept, n_req, false}, {lens_out, n_req, true}};
   if (overlapping(arrays)) return SP_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
   const KeepQ4Args a{q4_of(cache), block_table, past_lens, kept, n_kept, lens_out, n_req, max_pages, max_kept,
                      c.hkv, c.d, c.page_log2, c.pages, ctx->status};
   if (launch_cache_keep_q4(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return SP_ERR_CUDA;

@@ -27,17 +27,17 @@
 namespace sp {
 namespace {
 
-constexpr int kKeys = 16;                        // keys of a block
-constexpr int kOwnSteps = 4;                     // steps of a unit besides those of its blocks
-constexpr int kLeastSteps = 8;                   // of a run, while there are warps to spare
+constexpr int kOwnSteps = 2;                     // steps of a unit besides those of its keys
+constexpr int kLeastSteps = 4;                   // of a run, while there are warps to spare
 
 template <int D, int NT>
 struct Plan {
   static constexpr int ROWS = 8 * NT;
-  static constexpr int WARPS = NT == 1 ? 16 : NT == 2 ? 12 : 8;
+  static constexpr int WARPS = NT == 1 ? 16 : 8;
+  static constexpr int BLOCKS = NT == 4 ? 1 : 2, KEYS = 16 * BLOCKS;      // of a step
   static constexpr bool MERGE = NT <= 2;         // the CTA's warps add up their parts of a unit in shared memory
-  static constexpr int BYTES = Block<D>::BYTES;
-  static constexpr int RING = (NT == 4 ? 7 : 4) * (D == 128 ? 1 : 2);
+  static constexpr int BLOCK = Block<D>::BYTES, BYTES = BLOCKS * BLOCK;   // of a step
+  static constexpr int RING = (NT == 1 ? 2 : NT == 2 ? 4 : 7) * (D == 128 ? 1 : 2);
   static constexpr int WORDS = D / 32;           // words of codes that a lane takes of a key
   static constexpr int STRIDE = D + 4;           // of a part's rows, floats
   static constexpr int RING_OFF = 0, RING_BYTES = WARPS * RING * BYTES;
@@ -47,9 +47,11 @@ struct Plan {
   static constexpr int INFO_OFF = ML_OFF + (MERGE ? WARPS * 2 * ROWS * 8 : 0);                            // PartInfo [WARPS][2]
   static constexpr int BAR_OFF = INFO_OFF + WARPS * 2 * 32;
   static constexpr int SCAN_OFF = BAR_OFF + WARPS * RING * 8;                                             // int64 [2][WARPS], int64 [WARPS], int [WARPS]
-  static constexpr int FLAG_OFF = SCAN_OFF + WARPS * (3 * 8 + 4);
+  static constexpr int STATE_OFF = SCAN_OFF + WARPS * (3 * 8 + 4 + 4);                                    // WarpState [WARPS]
+  static constexpr int FLAG_OFF = STATE_OFF + WARPS * 176;
   static constexpr int TOTAL = FLAG_OFF + 16;
   static_assert(!MERGE || RING * BYTES >= ROWS * STRIDE * 4, "a drained ring holds a part");
+  static_assert(RING <= 32, "");
   static_assert(TOTAL <= 232448 && BYTES % 16 == 0 && RING_BYTES % 16 == 0, "");
 };
 
@@ -71,15 +73,22 @@ struct Walk {
   int b;
   Request q;
 };
+// What a warp needs between the pieces of its run only: kept in shared memory, registers are short.
+struct WarpState {
+  Walk walk, ahead;                // of the products, and of the copies
+  Piece piece, f_piece;
+  int f_kt, pad;                   // step of f_piece to which the window was turned last
+};
+static_assert(sizeof(WarpState) <= 176 && sizeof(WarpState) % 8 == 0, "");
 template <int ROWS>
 __device__ __forceinline__ int passes(const TreeAttnArgs& a, const Request& q) { return (int)(((uint32_t)(q.n * a.group) + ROWS - 1) / ROWS); }
 template <int ROWS>
 __device__ __forceinline__ long long units_of(const TreeAttnArgs& a, const Request& q) { return (long long)a.hkv * passes<ROWS>(a, q); }
 
-template <int ROWS>
-__device__ __forceinline__ bool next_piece(const TreeAttnArgs& a, Walk& w, Piece& u) {
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool walk_on(const TreeAttnArgs& a, Walk& w, Piece& u) {
   while (w.left > 0) {
-    while (w.rem >= units_of<ROWS>(a, w.q) * (w.q.kt + kOwnSteps) && w.b + 1 < a.n_req) { w.rem = 0; w.q = request_of<kKeys>(a, ++w.b); }
+    while (w.rem >= units_of<ROWS>(a, w.q) * (w.q.kt + kOwnSteps) && w.b + 1 < a.n_req) { w.rem = 0; w.q = request_of<KEYS>(a, ++w.b); }
     if (w.rem >= units_of<ROWS>(a, w.q) * (w.q.kt + kOwnSteps)) return false;      // not reached while the lengths stand still
     const int all = w.q.kt + kOwnSteps, n_pass = passes<ROWS>(a, w.q);
     const int nth = (int)divide(w.rem, all), in = (int)(w.rem - (long long)nth * all);
@@ -102,6 +111,21 @@ __device__ __forceinline__ bool next_piece(const TreeAttnArgs& a, Walk& w, Piece
   return false;
 }
 
+// Whole warp: the walk's next piece; both in shared memory.
+template <int ROWS, int KEYS>
+__device__ __noinline__ bool next_piece(const TreeAttnArgs& a, Walk& walk, Piece& piece) {
+  Walk w = walk;
+  Piece u;
+  __syncwarp();
+  const bool more = walk_on<ROWS, KEYS>(a, w, u);
+  if ((threadIdx.x & 31) == 0) {
+    walk = w;
+    piece = u;
+  }
+  __syncwarp();
+  return more;
+}
+
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
@@ -122,9 +146,48 @@ __device__ __forceinline__ Scale2 scale2(uint32_t bytes) {         // in bits 0 
   return r;
 }
 __device__ __forceinline__ uint32_t values(uint32_t codes, int p, const Scale2& s) {     // codes in bits 4 p .. and 16 + 4 p ..
-  const uint32_t w = (codes >> (4 * p) & 0x000f000fu) | 0x43004300u;
+  uint32_t w;                      // (left to the compiler, the mask and the or are two instructions: 13 instead of 7 a word)
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(w) : "r"(codes >> (4 * p)), "r"(0x000f000fu), "r"(0x43004300u));
   const __nv_bfloat162 y = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w), s.s, s.off);
   return *reinterpret_cast<const uint32_t*>(&y);
+}
+
+// The copies of a warp, RING steps ahead of the products: each lane holds the address of one of the next 32 blocks and issues
+// its copy when the block's turn comes, and the page of one of the 32 after them.
+struct Window {
+  const uint8_t* src;              // null: nothing to copy
+  int id;                          // page of this lane's block in the next window
+  int at, left;                    // next step in the window, steps until the window has to be turned
+};
+template <int D, int NT>
+__device__ __noinline__ Window turn_window(const TreeAttnArgs& a, const Q4Cache& cache, WarpState& st, int id) {
+  using P = Plan<D, NT>;
+  constexpr int STEPS = 32 / P::BLOCKS;
+  const int lane = threadIdx.x & 31;
+  int kt = st.f_kt + STEPS;
+  const bool fresh = kt >= st.f_piece.kt0 + st.f_piece.n;
+  if (fresh) {
+    if (!next_piece<P::ROWS, P::KEYS>(a, st.ahead, st.f_piece)) return {nullptr, -1, 0, -1};
+    kt = st.f_piece.kt0;
+  }
+  const Piece u = st.f_piece;
+  __syncwarp();
+  if (lane == 0) st.f_kt = kt;
+  __syncwarp();
+  const int32_t* row = a.table + (size_t)u.b * a.max_pages;
+  auto lookup = [&](long long key) { return key < u.len ? row[key >> a.page_log2] : 0; };
+  const long long key = (long long)kt * P::KEYS + lane * 16;
+  if (fresh) id = lookup(key);
+  Window w{nullptr, 0, 0, min(STEPS, u.kt0 + u.n - kt)};
+  // no such page, or no key at all: whatever lies in the slot is finite
+  if (key < u.len) {
+    if (id >= 0 && id < a.n_pages)
+      w.src = cache.data + u.g * cache.s_head + id * cache.s_page + (((int)key & ((1 << a.page_log2) - 1)) >> 4) * P::BLOCK;
+    else if (lane / P::BLOCKS < w.left)
+      report_range(a.status, kWhereTreePageQ4);
+  }
+  w.id = lookup(key + 512);
+  return w;
 }
 
 template <int D, int NT>
@@ -146,7 +209,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
   auto bar = [&](int slot) { return base + P::BAR_OFF + (warp * P::RING + slot) * 8; };
 
   let_next_start();
-  if (lane < P::RING) mbar_init(bar(lane), 1);
+  if (lane < P::RING) mbar_init(bar(lane), P::BLOCKS);
   if (lane < 2) infos[warp * 2 + lane].rows = 0;
   if (threadIdx.x == 0) *abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -158,7 +221,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
   const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
   long long mine = 0;
   for (int b = b_lo; b < b_hi; ++b) {
-    const Request r = request_of<kKeys>(a, b);
+    const Request r = request_of<P::KEYS>(a, b);
     mine += units_of<ROWS>(a, r) * (r.kt + kOwnSteps);
   }
   long long incl = mine;
@@ -185,7 +248,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
     if (before <= w && w < before + mine) {
       long long step = before;
       for (int b = b_lo; b < b_hi; ++b) {
-        const Request r = request_of<kKeys>(a, b);
+        const Request r = request_of<P::KEYS>(a, b);
         const long long n = units_of<ROWS>(a, r) * (r.kt + kOwnSteps);
         if (w < step + n) { start_b[i] = b; start_rem[i] = w - step; break; }
         step += n;
@@ -206,57 +269,43 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
   bool ok = true;
   if (steps > 0) {
     const uint32_t ring = base + P::RING_OFF + warp * (P::RING * P::BYTES);
-    const uint8_t* ring_at = smem + P::RING_OFF + warp * (P::RING * P::BYTES);
-    Walk walk{start_rem[warp], steps, start_b[warp], {}};
-    walk.q = request_of<kKeys>(a, walk.b);
-
-    // ---- fetching: a walk of its own, RING blocks ahead.  A lane holds the page of one of 32 blocks, and of the 32 after them.
-    Walk ahead = walk;
-    const int32_t* f_row = nullptr;
-    const uint8_t* f_base = nullptr;
-    int f_kt = 0, f_end = 0, f_len = 0, f_win = 0, id_now = -1, id_next = -1, f_slot = 0, pending = 0;
-    bool f_more = true;
-    auto lookup = [&](int kt) {                    // of block kt + lane
-      const long long key = (long long)(kt + lane) * kKeys;
-      return kt + lane < f_end && key < f_len ? f_row[key >> a.page_log2] : -1;
-    };
-    auto fetch = [&] {                             // whole warp; the next block into slot f_slot, if there is one
-      if (f_kt == f_end) {
-        Piece u;
-        f_more = f_more && next_piece<ROWS>(a, ahead, u);
-        if (!f_more) return;
-        f_row = a.table + (size_t)u.b * a.max_pages;
-        f_base = cache.data + u.g * cache.s_head;
-        f_kt = f_win = u.kt0; f_end = u.kt0 + u.n; f_len = u.len;
-        id_now = lookup(f_win);
-        id_next = lookup(f_win + 32);
-      } else if (f_kt - f_win == 32) {
-        f_win = f_kt;
-        id_now = id_next;
-        id_next = lookup(f_win + 32);
-      }
-      const int id = __shfl_sync(0xffffffffu, id_now, f_kt - f_win), key = f_kt * kKeys;
-      if (lane == 0) {
-        if (key < f_len && id >= 0 && id < a.n_pages) {
-          mbar_expect_tx(bar(f_slot), P::BYTES);
-          bulk_copy(ring + f_slot * P::BYTES, f_base + id * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * P::BYTES, P::BYTES, bar(f_slot));
+    const int ring_at = P::RING_OFF + warp * (P::RING * P::BYTES);
+    WarpState& st = reinterpret_cast<WarpState*>(smem + P::STATE_OFF)[warp];
+    if (lane == 0) {
+      const Walk walk{start_rem[warp], steps, start_b[warp], request_of<P::KEYS>(a, start_b[warp])};
+      st.walk = st.ahead = walk;
+      st.f_piece.kt0 = st.f_piece.n = 0;
+      st.f_kt = 0;
+    }
+    __syncwarp();
+    Window win{nullptr, 0, 0, 0};
+    int fetched = 0, taken = 0;
+    auto fetch = [&](int slot) {                   // whole warp; the next step into a slot, if there is one
+      if (win.left == 0) win = turn_window<D, NT>(a, cache, st, win.id);
+      if (win.left < 0) return;
+      if (lane / P::BLOCKS == win.at) {
+        if (win.src) {
+          mbar_expect_tx(bar(slot), P::BLOCK);
+          bulk_copy(ring + slot * P::BYTES + lane % P::BLOCKS * P::BLOCK, win.src, P::BLOCK, bar(slot));
         } else {
-          // no such page, or no key at all: whatever lies in the slot is finite
-          if (key < f_len) report_range(a.status, kWhereTreePageQ4);
-          mbar_arrive(bar(f_slot));
+          mbar_arrive(bar(slot));
         }
       }
-      ++f_kt;
-      ++pending;
-      if (++f_slot == P::RING) f_slot = 0;
+      __syncwarp();
+      ++win.at;
+      --win.left;
+      ++fetched;
     };
 #pragma unroll 1
-    for (int i = 0; i < P::RING; ++i) fetch();
+    for (int i = 0; i < P::RING; ++i) fetch(i);
 
-    Piece u;
+    // this lane's part of a block: bytes from the step's begin
+    const int k_at = B::k_word(g, q * WORDS), ks_at = B::k_scale(g, q * WORDS / 4), v_at = B::v_word(2 * q, g * (D / 64)), vs_at = B::v_scale(2 * q, g * (D / 8) / 32);
+    constexpr int V1 = B::v_word(1, 0) - B::v_word(0, 0), V2 = B::v_word(8, 0) - B::v_word(0, 0);      // from token 2 q to 2 q + 1, 2 q + 8
     int slot = 0;
     uint32_t phase = 0;
-    while (ok && next_piece<ROWS>(a, walk, u)) {
+    while (ok && next_piece<ROWS, P::KEYS>(a, st.walk, st.piece)) {
+      const Piece& u = st.piece;
       if (lane == 0 && u.kt0 == 0 && a.seq_lens[u.b] > u.len) report_range(a.status, kWhereTreePageQ4);   // longer than its table row
       // ---- queries: of row nt * 8 + g elements q D / 4 ..
       uint4 qf[P::MERGE ? NT : 1][WORDS];
@@ -286,123 +335,149 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
       }
       const int no_mask = min(u.past, u.len), tiles = (u.rows + 7) / 8;
 #pragma unroll 1
-      for (int t = 0; t < u.n; ++t) {
-        const int k0 = (u.kt0 + t) * kKeys;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(slot), phase, ab, 100));
-        if (!ok) break;
-        const uint8_t* blk = ring_at + slot * P::BYTES;
+      for (int k0 = u.kt0 * P::KEYS, left = u.n; left > 0; k0 += P::KEYS, --left) {
+        if (!__all_sync(0xffffffffu, mbar_try_wait(bar(slot), phase))) {
+          ok = __all_sync(0xffffffffu, mbar_wait_slow(bar(slot), phase, ab.flag, ab.status, 100, kWaitCycles));
+          if (!ok) break;
+        }
+        const int step_at = ring_at + slot * P::BYTES;
         // ---- S^T = K Q^T
-        uint32_t kw[2][WORDS];
+        float s[P::BLOCKS][NT][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint8_t* row = blk + B::k_word(g + 8 * h, q * WORDS);
-          if constexpr (WORDS == 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(row);
-            kw[h][0] = x.x; kw[h][1] = x.y; kw[h][2] = x.z; kw[h][3] = x.w;
-          } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(row);
-            kw[h][0] = x.x; kw[h][1] = x.y;
-          }
-        }
-        const uint32_t kb = *reinterpret_cast<const uint16_t*>(blk + B::k_scale(g, q * WORDS / 4));
-        const Scale2 ks[2] = {scale2(permute(kb, 0u, 0x4040u)), scale2(permute(kb, 0u, 0x4141u))};
-        float s[NT][4], s2[NT][4];                 // two sums: the products of one chain are dependent
+        for (int h = 0; h < P::BLOCKS; ++h) {
+          const uint8_t* blk = smem + step_at + h * P::BLOCK;
+          uint32_t kw[2][WORDS];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[nt][i] = s2[nt][i] = 0.f;
-#pragma unroll
-        for (int w = 0; w < WORDS; ++w) {
-          const uint32_t f0[4] = {values(kw[0][w], 0, ks[0]), values(kw[1][w], 0, ks[1]), values(kw[0][w], 1, ks[0]), values(kw[1][w], 1, ks[1])};
-          const uint32_t f1[4] = {values(kw[0][w], 2, ks[0]), values(kw[1][w], 2, ks[1]), values(kw[0][w], 3, ks[0]), values(kw[1][w], 3, ks[1])};
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (NT > 1 && nt >= tiles) break;
-            const uint4 x = P::MERGE ? qf[P::MERGE ? nt : 0][w] : *reinterpret_cast<const uint4*>(q_at + (nt * WORDS + w) * 512);
-            mma16816(s[nt], f0, x.x, x.y);
-            mma16816(s2[nt], f1, x.z, x.w);
-          }
-        }
-        // ---- softmax: lane has keys g, g + 8 and rows 2 q, 2 q + 1 of each tile
-        const bool special = k0 + kKeys > no_mask;
-        uint32_t p[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (NT > 1 && nt >= tiles) break;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[nt][i] = (s[nt][i] + s2[nt][i]) * a.scale_log2;
-          if (special) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int row = nt * 8 + 2 * q + i;
-              const uint32_t seen = row < u.rows ? seen32(a, u, (u.r0 + row) / a.group, k0) : 0u;
-              if (!(seen >> g & 1)) s[nt][i] = -CUDART_INF_F;
-              if (!(seen >> (g + 8) & 1)) s[nt][2 + i] = -CUDART_INF_F;
+          for (int x = 0; x < 2; ++x) {
+            const uint8_t* row = blk + k_at + x * B::k_word(8, 0);
+            if constexpr (WORDS == 4) {
+              const uint4 y = *reinterpret_cast<const uint4*>(row);
+              kw[x][0] = y.x; kw[x][1] = y.y; kw[x][2] = y.z; kw[x][3] = y.w;
+            } else {
+              const uint2 y = *reinterpret_cast<const uint2*>(row);
+              kw[x][0] = y.x; kw[x][1] = y.y;
             }
           }
-          const float x0 = fmaxf(s[nt][0], s[nt][2]), x1 = fmaxf(s[nt][1], s[nt][3]);
-          if (__any_sync(0xffffffffu, x0 > m[nt][0] + 8.f || x1 > m[nt][1] + 8.f)) {
-            // the rows' maxima over the lanes that have them; references are whole numbers, so nothing is rounded again
-            float t0 = x0, t1 = x1;
+          const uint32_t kb = *reinterpret_cast<const uint16_t*>(blk + ks_at);
+          const Scale2 ks[2] = {scale2(permute(kb, 0u, 0x4040u)), scale2(permute(kb, 0u, 0x4141u))};
 #pragma unroll
-            for (int e = 4; e < 32; e <<= 1) {
-              t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, e));
-              t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, e));
-            }
-            const float n0 = t0 > m[nt][0] + 8.f ? ceilf(t0) : m[nt][0], n1 = t1 > m[nt][1] + 8.f ? ceilf(t1) : m[nt][1];
-            const float f0 = ex2_approx(m[nt][0] - n0), f1 = ex2_approx(m[nt][1] - n1);
-            l[nt][0] *= f0;
-            l[nt][1] *= f1;
-            m[nt][0] = n0;
-            m[nt][1] = n1;
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) { o[nt][i][0] *= f0; o[nt][i][1] *= f1; o[nt][i][2] *= f0; o[nt][i][3] *= f1; }
-          }
-          s[nt][0] = ex2_approx(s[nt][0] - m[nt][0]);
-          s[nt][1] = ex2_approx(s[nt][1] - m[nt][1]);
-          s[nt][2] = ex2_approx(s[nt][2] - m[nt][0]);
-          s[nt][3] = ex2_approx(s[nt][3] - m[nt][1]);
-          l[nt][0] += s[nt][0] + s[nt][2];
-          l[nt][1] += s[nt][1] + s[nt][3];
-          p[nt][0] = transpose8(cvt_bf16x2(s[nt][0], s[nt][1]));
-          p[nt][1] = transpose8(cvt_bf16x2(s[nt][2], s[nt][3]));
-        }
-        // ---- O^T += V^T P^T: lane has tokens 2 q, 2 q + 1 and 2 q + 8, 2 q + 9, elements g D / 8 ..
-        const uint32_t vb = *reinterpret_cast<const uint32_t*>(blk + B::v_scale(2 * q, g * (D / 8) / 32));
-        const Scale2 v01 = scale2(vb & 0x00ff00ffu), v23 = scale2(vb >> 8 & 0x00ff00ffu);
-        uint32_t vw[4][D / 64];
+            for (int i = 0; i < 4; ++i) s[h][nt][i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint8_t* row = blk + B::v_word(2 * q + (i & 1) + 8 * (i >> 1), g * (D / 64));
-          if constexpr (D == 128) {
-            const uint2 x = *reinterpret_cast<const uint2*>(row);
-            vw[i][0] = x.x; vw[i][D / 64 - 1] = x.y;
-          } else {
-            vw[i][0] = *reinterpret_cast<const uint32_t*>(row);
-          }
-        }
-#pragma unroll
-        for (int w = 0; w < D / 64; ++w) {
-          const uint32_t even01 = permute(vw[0][w], vw[1][w], 0x5410u), odd01 = permute(vw[0][w], vw[1][w], 0x7632u);
-          const uint32_t even23 = permute(vw[2][w], vw[3][w], 0x5410u), odd23 = permute(vw[2][w], vw[3][w], 0x7632u);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t f[4] = {values(even01, e, v01), values(odd01, e, v01), values(even23, e, v23), values(odd23, e, v23)};
+          for (int w = 0; w < WORDS; ++w) {
+            const uint32_t f0[4] = {values(kw[0][w], 0, ks[0]), values(kw[1][w], 0, ks[1]), values(kw[0][w], 1, ks[0]), values(kw[1][w], 1, ks[1])};
+            const uint32_t f1[4] = {values(kw[0][w], 2, ks[0]), values(kw[1][w], 2, ks[1]), values(kw[0][w], 3, ks[0]), values(kw[1][w], 3, ks[1])};
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               if (NT > 1 && nt >= tiles) break;
-              mma16816(o[nt][w * 4 + e], f, p[nt][0], p[nt][1]);
+              const uint4 x = P::MERGE ? qf[P::MERGE ? nt : 0][w] : *reinterpret_cast<const uint4*>(q_at + (nt * WORDS + w) * 512);
+              mma16816(s[h][nt], f0, x.x, x.y);
+              mma16816(s[h][nt], f1, x.z, x.w);
             }
           }
         }
-        __syncwarp();                              // all have read the block
-        --pending;
-        fetch();
+        // ---- softmax: lane has keys g, g + 8 of each block and rows 2 q, 2 q + 1 of each tile
+        if (k0 + P::KEYS > no_mask) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            if (NT > 1 && nt >= tiles) break;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int row = nt * 8 + 2 * q + i;
+              const uint32_t seen = row < u.rows ? seen32(a, u, (u.r0 + row) / a.group, k0) >> g : 0u;
+#pragma unroll
+              for (int h = 0; h < P::BLOCKS; ++h) {
+                if (!(seen >> (16 * h) & 1)) s[h][nt][i] = -CUDART_INF_F;
+                if (!(seen >> (16 * h + 8) & 1)) s[h][nt][2 + i] = -CUDART_INF_F;
+              }
+            }
+          }
+        }
+        uint32_t p[P::BLOCKS][NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (NT > 1 && nt >= tiles) break;
+          float y[P::BLOCKS][4], top = -CUDART_INF_F;
+          auto weigh = [&] {
+#pragma unroll
+            for (int h = 0; h < P::BLOCKS; ++h)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[h][i] = fmaf(s[h][nt][i], a.scale_log2, -m[nt][i & 1]);
+          };
+          weigh();
+#pragma unroll
+          for (int h = 0; h < P::BLOCKS; ++h) top = max3(max3(top, y[h][0], y[h][1]), y[h][2], y[h][3]);
+          if (__any_sync(0xffffffffu, top > 8.f)) {
+            // a row's logits are 2^8 above its reference: the rows' maxima over the lanes that have them; references are whole
+            // numbers, so nothing is rounded again
+            float x[2], f[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              x[i] = fmaxf(s[0][nt][i], s[0][nt][2 + i]);
+              if (P::BLOCKS > 1) x[i] = max3(x[i], s[P::BLOCKS - 1][nt][i], s[P::BLOCKS - 1][nt][2 + i]);
+#pragma unroll
+              for (int e = 4; e < 32; e <<= 1) x[i] = fmaxf(x[i], __shfl_xor_sync(0xffffffffu, x[i], e));
+              x[i] *= a.scale_log2;
+              const float now = x[i] > m[nt][i] + 8.f ? ceilf(x[i]) : m[nt][i];
+              f[i] = ex2_approx(m[nt][i] - now);
+              l[nt][i] *= f[i];
+              m[nt][i] = now;
+            }
+#pragma unroll
+            for (int t2 = 0; t2 < D / 16; ++t2) { o[nt][t2][0] *= f[0]; o[nt][t2][1] *= f[1]; o[nt][t2][2] *= f[0]; o[nt][t2][3] *= f[1]; }
+            weigh();
+          }
+#pragma unroll
+          for (int h = 0; h < P::BLOCKS; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[h][i] = ex2_approx(y[h][i]);
+            l[nt][0] += y[h][0] + y[h][2];
+            l[nt][1] += y[h][1] + y[h][3];
+            p[h][nt][0] = transpose8(cvt_bf16x2(y[h][0], y[h][1]));
+            p[h][nt][1] = transpose8(cvt_bf16x2(y[h][2], y[h][3]));
+          }
+        }
+        // ---- O^T += V^T P^T: lane has tokens 2 q, 2 q + 1 and 2 q + 8, 2 q + 9 of a block, elements g D / 8 ..
+#pragma unroll
+        for (int h = 0; h < P::BLOCKS; ++h) {
+          const uint8_t* blk = smem + step_at + h * P::BLOCK;
+          const uint32_t vb = *reinterpret_cast<const uint32_t*>(blk + vs_at);
+          const Scale2 v01 = scale2(vb & 0x00ff00ffu), v23 = scale2(vb >> 8 & 0x00ff00ffu);
+          uint32_t vw[4][D / 64];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint8_t* row = blk + v_at + (i & 1) * V1 + (i >> 1) * V2;
+            if constexpr (D == 128) {
+              const uint2 x = *reinterpret_cast<const uint2*>(row);
+              vw[i][0] = x.x; vw[i][D / 64 - 1] = x.y;
+            } else {
+              vw[i][0] = *reinterpret_cast<const uint32_t*>(row);
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < D / 64; ++w) {
+            const uint32_t even01 = permute(vw[0][w], vw[1][w], 0x5410u), odd01 = permute(vw[0][w], vw[1][w], 0x7632u);
+            const uint32_t even23 = permute(vw[2][w], vw[3][w], 0x5410u), odd23 = permute(vw[2][w], vw[3][w], 0x7632u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t f[4] = {values(even01, e, v01), values(odd01, e, v01), values(even23, e, v23), values(odd23, e, v23)};
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                if (NT > 1 && nt >= tiles) break;
+                mma16816(o[nt][w * 4 + e], f, p[h][nt][0], p[h][nt][1]);
+              }
+            }
+          }
+        }
+        __syncwarp();                              // all have read the step's keys
+        ++taken;
+        fetch(slot);
         if (++slot == P::RING) { slot = 0; phase ^= 1; }
       }
       if (!ok) break;
 
-      // ---- the unit's rows: results, or a part
+      // ---- the piece's rows: results, or a part
       const bool whole = u.kt0 == 0 && u.n == u.kt_all;
       const int which = u.kt0 > 0 ? 0 : 1;
       float* part = P::MERGE ? reinterpret_cast<float*>(which == 0 ? smem + P::PART_OFF + warp * P::PART_BYTES : smem + P::RING_OFF + warp * (P::RING * P::BYTES)) : nullptr;
@@ -451,7 +526,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
     if (*abort_flag) {
       // let the copies already in flight land before the CTA gives its shared memory back
       const long long t0 = clock64();
-      for (int i = slot; i < slot + pending; ++i)
+      for (int i = slot; i < slot + fetched - taken; ++i)
         while (!mbar_try_wait(bar(i % P::RING), i < P::RING ? phase : phase ^ 1) && clock64() - t0 < kWaitCycles / 8) {}
     }
   }

@@ -289,6 +289,7 @@ int sp_get_status(sp_ctx* ctx, int* code, int* where) {
   if (!g.ok) return SP_ERR_CUDA;
   int host[2] = {0, 0};
   if (cudaMemcpy(host, ctx->status, sizeof(host), cudaMemcpyDeviceToHost) != cudaSuccess) return SP_ERR_CUDA;
+  if (host[0] == SP_ERR_TIMEOUT && reset_arrived(ctx) != cudaSuccess) return SP_ERR_CUDA;
   if (host[0] != 0 && cudaMemset(ctx->status, 0, sizeof(host)) != cudaSuccess) return SP_ERR_CUDA;
   if (code) *code = host[0];
   if (where) *where = host[1];

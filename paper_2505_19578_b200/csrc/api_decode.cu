@@ -160,9 +160,12 @@ int reserve_split(sp_ctx* ctx) {
   int n_sm = 0;
   if (cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, ctx->device) != cudaSuccess) return SP_ERR_CUDA;
   void* p = nullptr;
-  if (cudaMalloc(&p, std::max(tree_attn_workspace_bytes(n_sm), tree_attn_q4_workspace_bytes(n_sm))) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
-  ctx->split_ws = p;
+  const size_t parts = (std::max(tree_attn_workspace_bytes(n_sm), tree_attn_q4_workspace_bytes(n_sm)) + 15) / 16 * 16;
+  if (cudaMalloc(&p, parts + n_sm * sizeof(int)) != cudaSuccess) { cudaGetLastError(); return SP_ERR_WORKSPACE; }
   ctx->n_sm = n_sm;
+  ctx->arrived = reinterpret_cast<int*>(static_cast<char*>(p) + parts);
+  if (reset_arrived(ctx) != cudaSuccess) { cudaGetLastError(); cudaFree(p); ctx->arrived = nullptr; return SP_ERR_CUDA; }
+  ctx->split_ws = p;
   return SP_OK;
 }
 
@@ -176,6 +179,13 @@ int need_split(sp_ctx* ctx, cudaStream_t s) {
 }
 
 }  // namespace
+
+// (the device is synchronised: the caller's streams do not wait for the default one)
+cudaError_t sp::reset_arrived(sp_ctx* ctx) {
+  if (!ctx->arrived) return cudaSuccess;
+  const cudaError_t e = cudaMemset(ctx->arrived, 0, ctx->n_sm * sizeof(int));
+  return e != cudaSuccess ? e : cudaDeviceSynchronize();
+}
 
 extern "C" {
 
@@ -378,8 +388,8 @@ int sp_tree_attn_q4(sp_ctx* ctx, const sp_tensor* q, const sp_q4_cache* cache, c
     return SP_OK;
   }
   if ((rc = need_split(ctx, s))) return rc;
-  if (launch_tree_attn_q4(a, q4_of(cache), ctx->split_ws, ctx->n_sm, s) != cudaSuccess) return SP_ERR_CUDA;
-  ctx->launches += 2;
+  if (launch_tree_attn_q4(a, q4_of(cache), ctx->split_ws, ctx->arrived, ctx->n_sm, s) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += 1;
   return SP_OK;
 }
 

@@ -22,10 +22,13 @@ struct sp_ctx {
   // sp_tree_attn: partial results of units that several CTAs share.  Sized by the device alone, allocated once and never
   // moved, so that captured graphs keep a valid address.
   void* split_ws = nullptr;
+  int* arrived = nullptr; // behind it: sp_tree_attn_q4's counters of units that CTAs share, [n_sm], zero between calls
   int n_sm = 0;           // set with it
 };
 
 namespace sp {
+
+cudaError_t reset_arrived(sp_ctx* ctx);   // after a timeout: kernels may have stopped half-way (the context's device is current)
 
 struct DeviceGuard {
   int prev = -1;

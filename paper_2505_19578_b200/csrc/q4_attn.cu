@@ -3,11 +3,12 @@
 //   out_r = sum_c p_rc v_c / sum_c p_rc,  p_rc = 2^(scale q_r.k_c - m_r) over the visible keys c.
 //
 // The rows of a unit are the new tokens of one request times the query heads that share a KV head (row = token * group +
-// head), 8 NT at most.  Work is counted in steps, one for each block of 16 keys of a unit and kOwnSteps for the unit itself;
-// the steps of all units stand in one line, which is cut into one equal run per WARP.  A warp is on its own: it copies its
-// blocks into a ring of its own in shared memory (one bulk copy of 17 D bytes each, several ahead), turns codes into bf16
-// fragments in registers and multiplies them by mma.sync m16n8k16.  Nothing is exchanged between warps until the runs are
-// done; then the warps of a CTA add up what they have of the same unit, and a second kernel joins what CTAs have.
+// head), 8 NT at most.  Work is counted in steps, one for each 32 keys of a unit and kOwnSteps for the unit itself; the steps
+// of all units stand in one line, which is cut into one equal run per WARP.  A warp is on its own: its blocks of codes come
+// into a ring of its own in shared memory (a producer warp, a lane for each of the others, issues the bulk copies of 17 D
+// bytes a block), it turns codes into bf16 fragments in registers and multiplies them by mma.sync m16n8k16.  Nothing is
+// exchanged between warps until the runs are done; then the warps of a CTA add up what they have of the same unit, and of a
+// unit that several CTAs have, the CTA that comes last adds up theirs, in the order of the keys.
 //
 // Keys are the rows of A:  S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (D x 8 rows), so that 8 rows fill an instruction;
 // with the rows as A's, 16 would, and a single token of a group of 4 leave three quarters empty.  S^T's fragment becomes
@@ -33,34 +34,40 @@ constexpr int kLeastSteps = 4;                   // of a run, while there are wa
 template <int D, int NT>
 struct Plan {
   static constexpr int ROWS = 8 * NT;
-  static constexpr int WARPS = NT == 1 ? 16 : 8;
-  static constexpr int BLOCKS = NT == 4 ? 1 : 2, KEYS = 16 * BLOCKS;      // of a step
-  static constexpr bool MERGE = NT <= 2;         // the CTA's warps add up their parts of a unit in shared memory
-  static constexpr int BLOCK = Block<D>::BYTES, BYTES = BLOCKS * BLOCK;   // of a step
-  static constexpr int RING = (NT == 1 ? 2 : NT == 2 ? 4 : 7) * (D == 128 ? 1 : 2);
+  static constexpr int WARPS = NT == 1 ? 11 : 7, THREADS = (WARPS + 1) * 32;      // that multiply; the producer is one more
+  static constexpr int BLOCKS = 2, KEYS = 16 * BLOCKS;                            // of a step
+  static constexpr int BLOCK = Block<D>::BYTES, BYTES = BLOCKS * BLOCK;
+  static constexpr int RING = (NT == 1 ? 3 : 4) * (D == 128 ? 1 : 2);             // steps
   static constexpr int WORDS = D / 32;           // words of codes that a lane takes of a key
   static constexpr int STRIDE = D + 4;           // of a part's rows, floats
   static constexpr int RING_OFF = 0, RING_BYTES = WARPS * RING * BYTES;
-  static constexpr int PART_OFF = RING_OFF + RING_BYTES, PART_BYTES = MERGE ? ROWS * STRIDE * 4 : 0;      // a warp's part of a unit that an earlier run began
-  static constexpr int Q_OFF = PART_OFF + WARPS * PART_BYTES, Q_BYTES = MERGE ? 0 : NT * WORDS * 512;     // a warp's queries, in fragments
-  static constexpr int ML_OFF = Q_OFF + WARPS * Q_BYTES;                                                  // float2 [WARPS][2][ROWS]
-  static constexpr int INFO_OFF = ML_OFF + (MERGE ? WARPS * 2 * ROWS * 8 : 0);                            // PartInfo [WARPS][2]
-  static constexpr int BAR_OFF = INFO_OFF + WARPS * 2 * 32;
-  static constexpr int SCAN_OFF = BAR_OFF + WARPS * RING * 8;                                             // int64 [2][WARPS], int64 [WARPS], int [WARPS]
-  static constexpr int STATE_OFF = SCAN_OFF + WARPS * (3 * 8 + 4 + 4);                                    // WarpState [WARPS]
-  static constexpr int FLAG_OFF = STATE_OFF + WARPS * 176;
+  static constexpr int PART_OFF = RING_OFF + RING_BYTES, PART_BYTES = ROWS * STRIDE * 4;      // a warp's part of a unit that an earlier run began
+  static constexpr int ML_OFF = PART_OFF + WARPS * PART_BYTES;                                // float2 [WARPS][2][ROWS]
+  static constexpr int INFO_OFF = ML_OFF + WARPS * 2 * ROWS * 8;                              // PartInfo [WARPS][2]
+  static constexpr int BAR_OFF = INFO_OFF + WARPS * 2 * 32;                                   // full, free [WARPS][RING]
+  static constexpr int SCAN_OFF = BAR_OFF + 2 * WARPS * RING * 8;                             // int64 [WARPS + 1], int64 [WARPS], int [WARPS]
+  static constexpr int STATE_OFF = SCAN_OFF + (2 * WARPS + 2) * 8 + (WARPS + 1) / 2 * 8;      // WarpState [WARPS]
+  static constexpr int FLAG_OFF = STATE_OFF + WARPS * 80;
   static constexpr int TOTAL = FLAG_OFF + 16;
-  static_assert(!MERGE || RING * BYTES >= ROWS * STRIDE * 4, "a drained ring holds a part");
-  static_assert(RING <= 32, "");
-  static_assert(TOTAL <= 232448 && BYTES % 16 == 0 && RING_BYTES % 16 == 0, "");
+  static_assert(RING * BYTES >= ROWS * STRIDE * 4, "a drained ring holds a part");
+  static_assert(TOTAL <= 232448 && BYTES % 16 == 0 && RING_BYTES % 16 == 0 && STATE_OFF % 8 == 0, "");
 };
 
 struct PartInfo {  // of a warp's part 0 (of a unit that an earlier run began) or 1 (of one that goes on in a later run)
   int rows;        // 0: there is none
   int ends;        // the unit's last block is in it
-  int start, r0, g, pad[3];
+  int start, r0, g;
+  int first, last; // CTAs that have the unit's first and last blocks
+  int pad;
 };
 static_assert(sizeof(PartInfo) == 32, "");
+
+// What CTAs have of units that several of them share.
+struct CtaParts {
+  float* part;     // [cta][2][ROWS][D] unnormalised sums: part 0 of a unit begun by an earlier CTA, part 1 of one begun here
+  float2* ml;      // [cta][2][ROWS] reference, weight
+  int* arrived;    // [cta] CTAs that are done with the unit that begins here and goes on later; zero between calls
+};
 
 // Blocks of a unit that a run has.
 struct Piece {
@@ -75,11 +82,10 @@ struct Walk {
 };
 // What a warp needs between the pieces of its run only: kept in shared memory, registers are short.
 struct WarpState {
-  Walk walk, ahead;                // of the products, and of the copies
-  Piece piece, f_piece;
-  int f_kt, pad;                   // step of f_piece to which the window was turned last
+  Walk walk;
+  Piece piece;
 };
-static_assert(sizeof(WarpState) <= 176 && sizeof(WarpState) % 8 == 0, "");
+static_assert(sizeof(WarpState) == 80, "");
 template <int ROWS>
 __device__ __forceinline__ int passes(const TreeAttnArgs& a, const Request& q) { return (int)(((uint32_t)(q.n * a.group) + ROWS - 1) / ROWS); }
 template <int ROWS>
@@ -152,66 +158,105 @@ __device__ __forceinline__ uint32_t values(uint32_t codes, int p, const Scale2& 
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// The copies of a warp, RING steps ahead of the products: each lane holds the address of one of the next 32 blocks and issues
-// its copy when the block's turn comes, and the page of one of the 32 after them.
-struct Window {
-  const uint8_t* src;              // null: nothing to copy
-  int id;                          // page of this lane's block in the next window
-  int at, left;                    // next step in the window, steps until the window has to be turned
-};
+// The producer: lane w issues the copies of warp w's run, RING steps ahead of the products.
 template <int D, int NT>
-__device__ __noinline__ Window turn_window(const TreeAttnArgs& a, const Q4Cache& cache, WarpState& st, int id) {
+__device__ __noinline__ void produce(const TreeAttnArgs& a, const Q4Cache& cache, uint32_t base, const Abort& ab, Walk walk, int w) {
   using P = Plan<D, NT>;
-  constexpr int STEPS = 32 / P::BLOCKS;
-  const int lane = threadIdx.x & 31;
-  int kt = st.f_kt + STEPS;
-  const bool fresh = kt >= st.f_piece.kt0 + st.f_piece.n;
-  if (fresh) {
-    if (!next_piece<P::ROWS, P::KEYS>(a, st.ahead, st.f_piece)) return {nullptr, -1, 0, -1};
-    kt = st.f_piece.kt0;
+  auto full = [&](int slot) { return base + P::BAR_OFF + (w * P::RING + slot) * 16; };
+  const uint32_t ring = base + P::RING_OFF + w * (P::RING * P::BYTES);
+  const bool one_copy = (1 << a.page_log2) >= P::KEYS;                 // a step's blocks lie together
+  Piece u;
+  u.kt0 = u.n = 0;
+  int kt = 0, issued = 0, slot = 0, id0 = -1, id1 = -1, idle = 0;
+  uint32_t lap = 0;
+  long long since = 0;
+  bool more = true, ready = false;                                     // ready: ids of step kt are on their way
+  const int32_t* row = nullptr;
+  const uint8_t* head = nullptr;
+  while (more) {
+    if (!ready) {
+      if (kt == u.kt0 + u.n) {
+        more = walk_on<P::ROWS, P::KEYS>(a, walk, u);
+        if (!more) break;
+        kt = u.kt0;
+        row = a.table + (size_t)u.b * a.max_pages;
+        head = cache.data + u.g * cache.s_head;
+      }
+      const long long key = (long long)kt * P::KEYS;
+      id0 = key < u.len ? row[key >> a.page_log2] : -1;
+      id1 = key + 16 < u.len ? row[(key + 16) >> a.page_log2] : -1;
+      ready = true;
+    }
+    if (lap > 0 && !mbar_test(full(slot) + 8, (lap - 1) & 1)) {
+      if (*ab.flag) break;
+      if ((++idle & 63) == 0) {
+        const int code = *reinterpret_cast<volatile int*>(ab.status);
+        if (code != 0 && code != (int)SP_ERR_RANGE) { *ab.flag = 1; break; }
+        const long long now = clock64();
+        if (since == 0) since = now;
+        else if (now - since > kWaitCycles) {
+          *ab.flag = 1;
+          report_timeout(ab.status, 101);
+          break;
+        }
+      }
+      __nanosleep(100);
+      continue;
+    }
+    idle = 0;
+    since = 0;
+    // no such page, or no key at all: nothing is copied, whatever lies in the slot is finite
+    const int key = kt * P::KEYS, in = key & ((1 << a.page_log2) - 1);
+    const bool have0 = key < u.len && id0 >= 0 && id0 < a.n_pages, have1 = key + 16 < u.len && id1 >= 0 && id1 < a.n_pages;
+    if ((key < u.len && !have0) || (key + 16 < u.len && !have1)) report_range(a.status, kWhereTreePageQ4);
+    const uint32_t dst = ring + slot * P::BYTES;
+    mbar_expect_tx(full(slot), (have0 + have1) * P::BLOCK);
+    const uint8_t* src0 = head + id0 * cache.s_page + (in >> 4) * P::BLOCK;
+    if (one_copy) {
+      if (have0) bulk_copy(dst, src0, (have0 + have1) * P::BLOCK, full(slot));
+    } else {
+      if (have0) bulk_copy(dst, src0, P::BLOCK, full(slot));
+      if (have1) bulk_copy(dst + P::BLOCK, head + id1 * cache.s_page + (((in + 16) & ((1 << a.page_log2) - 1)) >> 4) * P::BLOCK, P::BLOCK, full(slot));
+    }
+    ready = false;
+    ++kt;
+    ++issued;
+    if (++slot == P::RING) { slot = 0; ++lap; }
   }
-  const Piece u = st.f_piece;
-  __syncwarp();
-  if (lane == 0) st.f_kt = kt;
-  __syncwarp();
-  const int32_t* row = a.table + (size_t)u.b * a.max_pages;
-  auto lookup = [&](long long key) { return key < u.len ? row[key >> a.page_log2] : 0; };
-  const long long key = (long long)kt * P::KEYS + lane * 16;
-  if (fresh) id = lookup(key);
-  Window w{nullptr, 0, 0, min(STEPS, u.kt0 + u.n - kt)};
-  // no such page, or no key at all: whatever lies in the slot is finite
-  if (key < u.len) {
-    if (id >= 0 && id < a.n_pages)
-      w.src = cache.data + u.g * cache.s_head + id * cache.s_page + (((int)key & ((1 << a.page_log2) - 1)) >> 4) * P::BLOCK;
-    else if (lane / P::BLOCKS < w.left)
-      report_range(a.status, kWhereTreePageQ4);
+  if (*ab.flag) {
+    // let the copies already in flight land before the CTA gives its shared memory back
+    const long long t0 = clock64();
+    for (int i = max(issued - P::RING, 0); i < issued; ++i)
+      while (!mbar_try_wait(full(i % P::RING), (i / P::RING) & 1) && clock64() - t0 < kWaitCycles / 8) {}
   }
-  w.id = lookup(key + 512);
-  return w;
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kernel(const __grid_constant__ TreeAttnArgs a, const Q4Cache cache, const Parts work) {
+__global__ void __launch_bounds__(Plan<D, NT>::THREADS, 1) tree_attn_q4_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ Q4Cache cache,
+                                                                              const CtaParts work) {
   using P = Plan<D, NT>;
   using B = Block<D>;
-  constexpr int WARPS = P::WARPS, ROWS = P::ROWS, THREADS = WARPS * 32, WORDS = P::WORDS;
+  constexpr int WARPS = P::WARPS, ROWS = P::ROWS, THREADS = P::THREADS, WORDS = P::WORDS;
   extern __shared__ __align__(128) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
   float2* part_ml = reinterpret_cast<float2*>(smem + P::ML_OFF);
   PartInfo* infos = reinterpret_cast<PartInfo*>(smem + P::INFO_OFF);
   long long* scan = reinterpret_cast<long long*>(smem + P::SCAN_OFF);
-  long long* start_rem = scan + 2 * WARPS;
-  int* start_b = reinterpret_cast<int*>(start_rem + WARPS);
+  long long* start_rem = scan + WARPS + 1;
+  int* start_b = reinterpret_cast<int*>(start_rem + WARPS + 1);
   volatile int* abort_flag = reinterpret_cast<int*>(smem + P::FLAG_OFF);
+  volatile int* last_flags = abort_flag + 1;      // [2]: this CTA is the last of the unit of its part 0, 1
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int cta = blockIdx.x;
   const Abort ab{abort_flag, a.status};
-  auto bar = [&](int slot) { return base + P::BAR_OFF + (warp * P::RING + slot) * 8; };
+  auto bar = [&](int slot) { return base + P::BAR_OFF + (warp * P::RING + slot) * 16; };       // full; + 8: free
 
   let_next_start();
-  if (lane < P::RING) mbar_init(bar(lane), P::BLOCKS);
-  if (lane < 2) infos[warp * 2 + lane].rows = 0;
-  if (threadIdx.x == 0) *abort_flag = 0;
+  if (warp < WARPS) {
+    if (lane < 2 * P::RING) mbar_init(base + P::BAR_OFF + (warp * 2 * P::RING + lane) * 8, 1);
+    if (lane < 2) infos[warp * 2 + lane].rows = 0;
+  }
+  if (threadIdx.x == 0) *abort_flag = last_flags[0] = last_flags[1] = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   wait_for_previous();
   const bool idle = decode_poisoned(a.status);
@@ -234,15 +279,19 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
   __syncthreads();
   long long before = incl - mine, total = 0;
 #pragma unroll
-  for (int w = 0; w < WARPS; ++w) {
+  for (int w = 0; w <= WARPS; ++w) {
     if (w < warp) before += scan[w];
     total += scan[w];
   }
-  // as many warps of each CTA as have kLeastSteps to do (a part costs its join)
+  // as many warps of each CTA as have kLeastSteps to do (a part costs its addition)
   const long long want = divide(total, (long long)gridDim.x * kLeastSteps);
   const int warps = (int)max(1ll, min((long long)WARPS, want)), n_runs = gridDim.x * warps;
   const long long quota = divide(total, n_runs), extra = total - quota * n_runs;      // the first `extra` runs are one step longer
   auto run_begin = [&](int r) { return r * quota + min((long long)r, extra); };
+  auto cta_of = [&](long long z) {                 // that has step z
+    const long long cut = extra * (quota + 1);
+    return (int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota)) / warps;
+  };
   for (int i = 0; i < warps; ++i) {
     const long long w = run_begin(cta * warps + i);
     if (before <= w && w < before + mine) {
@@ -255,51 +304,20 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
       }
     }
   }
-  // units that go on in later CTAs (in later runs, where the warps' parts are joined one by one): none yet
-  const int run = cta * warps + warp;
-  if (P::MERGE) {
-    if (threadIdx.x == 0) work.meta[cta].last = -1;
-  } else {
-    if (lane == 0 && warp < warps) work.meta[run].last = -1;
-    for (int i = n_runs + cta * THREADS + threadIdx.x; i < (int)gridDim.x * WARPS; i += gridDim.x * THREADS) work.meta[i].last = -1;
-  }
   __syncthreads();
 
-  const long long w0 = run_begin(run), steps = warp < warps && !idle ? run_begin(run + 1) - w0 : 0;
+  const int mine_w = warp == WARPS ? lane : warp;                      // the run that a warp, or a lane of the producer, looks after
+  const long long w0 = run_begin(cta * warps + mine_w), steps = mine_w < warps && !idle ? run_begin(cta * warps + mine_w + 1) - w0 : 0;
   bool ok = true;
-  if (steps > 0) {
-    const uint32_t ring = base + P::RING_OFF + warp * (P::RING * P::BYTES);
+  if (warp == WARPS) {
+    if (steps > 0) produce<D, NT>(a, cache, base, ab, Walk{start_rem[lane], steps, start_b[lane], request_of<P::KEYS>(a, start_b[lane])}, lane);
+    __syncwarp();
+  } else if (steps > 0) {
     const int ring_at = P::RING_OFF + warp * (P::RING * P::BYTES);
     WarpState& st = reinterpret_cast<WarpState*>(smem + P::STATE_OFF)[warp];
-    if (lane == 0) {
-      const Walk walk{start_rem[warp], steps, start_b[warp], request_of<P::KEYS>(a, start_b[warp])};
-      st.walk = st.ahead = walk;
-      st.f_piece.kt0 = st.f_piece.n = 0;
-      st.f_kt = 0;
-    }
+    if (lane == 0) st.walk = Walk{start_rem[warp], steps, start_b[warp], request_of<P::KEYS>(a, start_b[warp])};
     __syncwarp();
-    Window win{nullptr, 0, 0, 0};
-    int fetched = 0, taken = 0;
-    auto fetch = [&](int slot) {                   // whole warp; the next step into a slot, if there is one
-      if (win.left == 0) win = turn_window<D, NT>(a, cache, st, win.id);
-      if (win.left < 0) return;
-      if (lane / P::BLOCKS == win.at) {
-        if (win.src) {
-          mbar_expect_tx(bar(slot), P::BLOCK);
-          bulk_copy(ring + slot * P::BYTES + lane % P::BLOCKS * P::BLOCK, win.src, P::BLOCK, bar(slot));
-        } else {
-          mbar_arrive(bar(slot));
-        }
-      }
-      __syncwarp();
-      ++win.at;
-      --win.left;
-      ++fetched;
-    };
-#pragma unroll 1
-    for (int i = 0; i < P::RING; ++i) fetch(i);
-
-    // this lane's part of a block: bytes from the step's begin
+    // this lane's part of a block: bytes from its begin
     const int k_at = B::k_word(g, q * WORDS), ks_at = B::k_scale(g, q * WORDS / 4), v_at = B::v_word(2 * q, g * (D / 64)), vs_at = B::v_scale(2 * q, g * (D / 8) / 32);
     constexpr int V1 = B::v_word(1, 0) - B::v_word(0, 0), V2 = B::v_word(8, 0) - B::v_word(0, 0);      // from token 2 q to 2 q + 1, 2 q + 8
     int slot = 0;
@@ -308,18 +326,15 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
       const Piece& u = st.piece;
       if (lane == 0 && u.kt0 == 0 && a.seq_lens[u.b] > u.len) report_range(a.status, kWhereTreePageQ4);   // longer than its table row
       // ---- queries: of row nt * 8 + g elements q D / 4 ..
-      uint4 qf[P::MERGE ? NT : 1][WORDS];
-      uint8_t* q_at = smem + P::Q_OFF + warp * P::Q_BYTES + lane * 16;
+      uint4 qf[NT][WORDS];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int row = nt * 8 + g, abs_row = u.r0 + row;
         const __nv_bfloat16* src = a.q + (int64_t)(u.g * a.group + abs_row % a.group) * a.q_sh + (int64_t)(u.start + abs_row / a.group) * a.q_sn + q * (D / 4);
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (row < u.rows) x = *reinterpret_cast<const uint4*>(src + w * 8);
-          if (P::MERGE) qf[P::MERGE ? nt : 0][w] = x;
-          else *reinterpret_cast<uint4*>(q_at + (nt * WORDS + w) * 512) = x;
+          qf[nt][w] = make_uint4(0, 0, 0, 0);
+          if (row < u.rows) qf[nt][w] = *reinterpret_cast<const uint4*>(src + w * 8);
         }
       }
       float o[NT][D / 16][4], m[NT][2], l[NT][2];
@@ -371,9 +386,8 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               if (NT > 1 && nt >= tiles) break;
-              const uint4 x = P::MERGE ? qf[P::MERGE ? nt : 0][w] : *reinterpret_cast<const uint4*>(q_at + (nt * WORDS + w) * 512);
-              mma16816(s[h][nt], f0, x.x, x.y);
-              mma16816(s[h][nt], f1, x.z, x.w);
+              mma16816(s[h][nt], f0, qf[nt][w].x, qf[nt][w].y);
+              mma16816(s[h][nt], f1, qf[nt][w].z, qf[nt][w].w);
             }
           }
         }
@@ -471,8 +485,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
           }
         }
         __syncwarp();                              // all have read the step's keys
-        ++taken;
-        fetch(slot);
+        if (lane == 0) mbar_arrive(bar(slot) + 8);
         if (++slot == P::RING) { slot = 0; phase ^= 1; }
       }
       if (!ok) break;
@@ -480,7 +493,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
       // ---- the piece's rows: results, or a part
       const bool whole = u.kt0 == 0 && u.n == u.kt_all;
       const int which = u.kt0 > 0 ? 0 : 1;
-      float* part = P::MERGE ? reinterpret_cast<float*>(which == 0 ? smem + P::PART_OFF + warp * P::PART_BYTES : smem + P::RING_OFF + warp * (P::RING * P::BYTES)) : nullptr;
+      float* part = reinterpret_cast<float*>(which == 0 ? smem + P::PART_OFF + warp * P::PART_BYTES : smem + ring_at);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         if (NT > 1 && nt >= tiles) break;
@@ -502,49 +515,45 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
             if (a.lse && g == 0)
               a.lse[(size_t)head * a.rows + u.start + token] = sum != 0.f ? (m[nt][i] + log2f(sum)) * 0.6931471805599453f : -CUDART_INF_F;
           } else {
-            const size_t at = ((size_t)run * 2 + which) * ROWS + row;
-            float4* dst = reinterpret_cast<float4*>((P::MERGE ? part + row * P::STRIDE : work.part + at * D) + g * (D / 8));
+            float4* dst = reinterpret_cast<float4*>(part + row * P::STRIDE + g * (D / 8));
 #pragma unroll
             for (int w = 0; w < D / 32; ++w)
               dst[w] = make_float4(o[nt][2 * w][i], o[nt][2 * w][2 + i], o[nt][2 * w + 1][i], o[nt][2 * w + 1][2 + i]);
-            if (g == 0) (P::MERGE ? part_ml[(warp * 2 + which) * ROWS + row] : work.ml[at]) = make_float2(m[nt][i], sum);
+            if (g == 0) part_ml[(warp * 2 + which) * ROWS + row] = make_float2(m[nt][i], sum);
           }
         }
       }
       if (!whole && lane == 0) {
-        if (P::MERGE) infos[warp * 2 + which] = PartInfo{u.rows, u.kt0 + u.n == u.kt_all, u.start, u.r0, u.g, {0, 0, 0}};
-        if (which == 1) {
-          // the run that has the unit's last step: this one's end is the unit's step kOwnSteps + n
-          const long long z = w0 + steps - 1 + (u.kt_all - u.n), cut = extra * (quota + 1);
-          const int last = (int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota));
-          const int here = P::MERGE ? cta : run, to = P::MERGE ? last / warps : last;
-          if (to > here) work.meta[here] = Meta{to, u.start, u.r0, u.rows, u.g, {0, 0, 0}};
-        }
+        const long long end = w0 + steps - st.walk.left;                // the step behind the piece's last
+        infos[warp * 2 + which] = PartInfo{u.rows, u.kt0 + u.n == u.kt_all, u.start, u.r0, u.g, cta_of(end - u.n - u.kt0), cta_of(end - 1 + u.kt_all - u.kt0 - u.n), 0};
       }
       __syncwarp();
     }
-    if (*abort_flag) {
-      // let the copies already in flight land before the CTA gives its shared memory back
-      const long long t0 = clock64();
-      for (int i = slot; i < slot + fetched - taken; ++i)
-        while (!mbar_try_wait(bar(i % P::RING), i < P::RING ? phase : phase ^ 1) && clock64() - t0 < kWaitCycles / 8) {}
-    }
   }
-  if (!P::MERGE) return;
 
   // ---- the CTA's parts, in the order of the keys: warp 0's part 0, its part 1 or warp 1's part 0, ...
   __syncthreads();
   if (*abort_flag || idle) return;
-  int task = 0;
+  // a row's result, or nothing seen
+  auto result = [&](const PartInfo& u, int row, float top, float sum, const float (&y)[WORDS]) {
+    const int abs_row = u.r0 + row, token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(a.o + head * a.o_sh + (int64_t)(u.start + token) * a.o_sn + lane * WORDS);
+#pragma unroll
+    for (int e = 0; e < WORDS; e += 2) dst[e / 2] = pack_bf16(y[e] * inv, y[e + 1] * inv);
+    if (a.lse && lane == 0) a.lse[(size_t)head * a.rows + u.start + token] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -CUDART_INF_F;
+  };
+  int task = 0, shared_part[2] = {-1, -1};         // the parts that this CTA leaves: indices into infos
   for (int i = 0; i < 2 * warps; ++i) {
     if (infos[i].rows == 0 || !((i & 1) || i == 0)) continue;          // not the first of its unit here
     const PartInfo u = infos[i];
-    int end = (i | 1) + 1;                                             // parts of the unit: i, then `end` - 2, .. - the part 0 of the warps after it
+    int end = (i | 1) + 1;                                             // parts of the unit: i, then the part 0 of the warps after it, up to `end`
     bool ends = u.ends;
     while (!ends && end < 2 * warps && infos[end].rows != 0) { ends = infos[end].ends; end += 2; }
     const bool whole = (i & 1) && ends;
+    if (!whole) shared_part[i & 1] = i;
     for (int row = 0; row < u.rows; ++row) {
-      if (task++ % WARPS != warp) continue;
+      if (task++ % (WARPS + 1) != warp) continue;
       float top = kNoMax, sum = 0.f, y[WORDS];
 #pragma unroll
       for (int e = 0; e < WORDS; ++e) y[e] = 0.f;
@@ -558,13 +567,8 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
 #pragma unroll
         for (int e = 0; e < WORDS; ++e) y[e] += part[lane * WORDS + e] * f;
       }
-      const int abs_row = u.r0 + row, token = abs_row / a.group, head = u.g * a.group + abs_row % a.group;
       if (whole) {
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        uint32_t* dst = reinterpret_cast<uint32_t*>(a.o + head * a.o_sh + (int64_t)(u.start + token) * a.o_sn + lane * WORDS);
-#pragma unroll
-        for (int e = 0; e < WORDS; e += 2) dst[e / 2] = pack_bf16(y[e] * inv, y[e + 1] * inv);
-        if (a.lse && lane == 0) a.lse[(size_t)head * a.rows + u.start + token] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -CUDART_INF_F;
+        result(u, row, top, sum, y);
       } else {
         const size_t at = ((size_t)cta * 2 + (i & 1)) * ROWS + row;
 #pragma unroll
@@ -573,46 +577,120 @@ __global__ void __launch_bounds__(Plan<D, NT>::WARPS * 32, 1) tree_attn_q4_kerne
       }
     }
   }
+  if (shared_part[0] < 0 && shared_part[1] < 0) return;
+
+  // ---- units that several CTAs have: the last to arrive adds up their parts
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int x = 0; x < 2; ++x) {
+      if (shared_part[x] < 0) continue;
+      const PartInfo u = infos[shared_part[x]];
+      if (atomicAdd(work.arrived + u.first, 1) == u.last - u.first) {
+        work.arrived[u.first] = 0;                 // nobody else comes; for the next call
+        last_flags[x] = 1;
+      }
+    }
+    __threadfence();
+  }
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(smem + P::RING_OFF);          // [warp][STRIDE]
+  float2* sums_ml = reinterpret_cast<float2*>(smem + P::ML_OFF);
+  for (int x = 0; x < 2; ++x) {
+    if (!last_flags[x]) continue;
+    const PartInfo u = infos[shared_part[x]];
+    const int parts = u.last - u.first + 1;
+    int share = 1;                                 // warps for a row
+    while (2 * share * u.rows <= WARPS && 2 * share < parts) share *= 2;
+    for (int row0 = 0; row0 < u.rows; row0 += WARPS / share) {
+      const int row = row0 + warp / share, turn = warp % share;
+      const bool live = warp < WARPS / share * share && row < u.rows;
+      float top = kNoMax, sum = 0.f, y[WORDS];
+#pragma unroll
+      for (int e = 0; e < WORDS; ++e) y[e] = 0.f;
+      if (live) {
+        constexpr int RUN = 8;                     // parts in flight
+        for (int p0 = turn; p0 < parts; p0 += RUN * share) {
+          float2 ml[RUN];
+          float z[RUN][WORDS];
+#pragma unroll
+          for (int i = 0; i < RUN; ++i) {
+            const int p = p0 + i * share;
+            ml[i] = make_float2(kNoMax, 0.f);
+#pragma unroll
+            for (int e = 0; e < WORDS; ++e) z[i][e] = 0.f;
+            if (p < parts) {
+              const size_t at = ((size_t)(u.first + p) * 2 + (p == 0 ? 1 : 0)) * ROWS + row;
+              ml[i] = __ldcg(work.ml + at);
+              if constexpr (WORDS == 4) {
+                const float4 t = __ldcg(reinterpret_cast<const float4*>(work.part + at * D) + lane);
+                z[i][0] = t.x; z[i][1] = t.y; z[i][2] = t.z; z[i][3] = t.w;
+              } else {
+                const float2 t = __ldcg(reinterpret_cast<const float2*>(work.part + at * D) + lane);
+                z[i][0] = t.x; z[i][1] = t.y;
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < RUN; ++i) {
+            const float now = fmaxf(top, ml[i].x), f_old = ex2_approx(top - now), f = ex2_approx(ml[i].x - now);
+            sum = sum * f_old + ml[i].y * f;
+#pragma unroll
+            for (int e = 0; e < WORDS; ++e) y[e] = y[e] * f_old + z[i][e] * f;
+            top = now;
+          }
+        }
+      }
+      if (share > 1) {
+        __syncthreads();                           // the last rows' sums have been read
+        if (live) {
+#pragma unroll
+          for (int e = 0; e < WORDS; ++e) sums[warp * P::STRIDE + lane * WORDS + e] = y[e];
+          if (lane == 0) sums_ml[warp] = make_float2(top, sum);
+        }
+        __syncthreads();
+        if (live && turn == 0) {
+          for (int w = warp + 1; w < warp + share; ++w) {
+            const float2 ml = sums_ml[w];
+            const float now = fmaxf(top, ml.x), f_old = ex2_approx(top - now), f = ex2_approx(ml.x - now);
+            sum = sum * f_old + ml.y * f;
+#pragma unroll
+            for (int e = 0; e < WORDS; ++e) y[e] = y[e] * f_old + sums[w * P::STRIDE + lane * WORDS + e] * f;
+            top = now;
+          }
+        }
+      }
+      if (live && turn == 0) result(u, row, top, sum, y);
+    }
+    __syncthreads();
+  }
 }
 
 template <int D, int NT>
-cudaError_t launch(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int n_sm, cudaStream_t s) {
+cudaError_t launch(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s) {
   using P = Plan<D, NT>;
-  const int parts = P::MERGE ? n_sm : n_sm * P::WARPS;
-  Parts w;
+  CtaParts w;
   w.part = static_cast<float*>(ws);
-  w.ml = reinterpret_cast<float2*>(w.part + (size_t)parts * 2 * P::ROWS * D);
-  w.meta = reinterpret_cast<Meta*>(w.ml + (size_t)parts * 2 * P::ROWS);
-  cudaError_t e = cudaFuncSetAttribute(tree_attn_q4_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, P::TOTAL);
+  w.ml = reinterpret_cast<float2*>(w.part + (size_t)n_sm * 2 * P::ROWS * D);
+  w.arrived = arrived;
+  const cudaError_t e = cudaFuncSetAttribute(tree_attn_q4_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, P::TOTAL);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(tree_attn_q4_kernel<D, NT>, dim3(n_sm), dim3(P::WARPS * 32), P::TOTAL, s, a, c, w);
-  if (e != cudaSuccess) return e;
-  return launch_dependent(tree_attn_join_kernel<D, P::ROWS>, dim3(n_sm * kJoinBlocksPerSm), dim3(kJoinWarps * 32), 0, s, a, w, parts);
+  return launch_dependent(tree_attn_q4_kernel<D, NT>, dim3(n_sm), dim3(P::THREADS), P::TOTAL, s, a, c, w);
 }
 
 template <int D>
-cudaError_t launch_rows(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int n_sm, cudaStream_t s) {
+cudaError_t launch_rows(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s) {
   // rows of a request if all have as many; requests of more rows are several units, which is right for any lengths
   const long long rows = ((long long)a.rows + a.n_req - 1) / a.n_req * a.group;
-  return rows <= 8 ? launch<D, 1>(a, c, ws, n_sm, s) : rows <= 16 ? launch<D, 2>(a, c, ws, n_sm, s) : launch<D, 4>(a, c, ws, n_sm, s);
-}
-
-template <int D, int NT>
-constexpr size_t workspace_per_sm() {
-  using P = Plan<D, NT>;
-  return (P::MERGE ? 1 : P::WARPS) * (2 * P::ROWS * (D * sizeof(float) + sizeof(float2)) + sizeof(Meta));
+  return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : launch<D, 2>(a, c, ws, arrived, n_sm, s);
 }
 
 }  // namespace
 
-size_t tree_attn_q4_workspace_bytes(int n_sm) {
-  size_t most = workspace_per_sm<128, 4>();
-  for (const size_t x : {workspace_per_sm<128, 1>(), workspace_per_sm<128, 2>(), workspace_per_sm<64, 4>()}) most = x > most ? x : most;
-  return most * n_sm;
-}
+size_t tree_attn_q4_workspace_bytes(int n_sm) { return (size_t)n_sm * 2 * 16 * (128 * sizeof(float) + sizeof(float2)); }
 
-cudaError_t launch_tree_attn_q4(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int n_sm, cudaStream_t s) {
-  return a.d == 128 ? launch_rows<128>(a, c, ws, n_sm, s) : launch_rows<64>(a, c, ws, n_sm, s);
+cudaError_t launch_tree_attn_q4(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s) {
+  return a.d == 128 ? launch_rows<128>(a, c, ws, arrived, n_sm, s) : launch_rows<64>(a, c, ws, arrived, n_sm, s);
 }
 
 }  // namespace sp

@@ -129,17 +129,6 @@ __device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) { retur
 // units of the request per KV head, of 128 or 256 rows (n * group fits 32 bits: the host has checked)
 __device__ __forceinline__ int passes(const TreeAttnArgs& a, const Request& q, int rows) { return (int)(((uint32_t)(q.n * a.group) + rows - 1) >> (rows == 128 ? 7 : 8)); }
 __device__ __forceinline__ long long units_of(const TreeAttnArgs& a, const Request& q, int rows) { return (long long)a.hkv * passes(a, q, rows); }
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
 // Three barriers polled at once (bit i: phase of barrier i over): the round trips overlap.
 __device__ __forceinline__ uint32_t mbar_test3(uint32_t b0, uint32_t par0, uint32_t b1, uint32_t par1, uint32_t b2, uint32_t par2) {
   uint32_t r0, r1, r2;

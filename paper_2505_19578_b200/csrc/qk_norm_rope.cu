@@ -135,29 +135,33 @@ struct Codes {                     // of a lane's two pieces: words of codes, an
   uint32_t word0, word1, scale0, scale1;
 };
 __device__ __forceinline__ uint32_t clamp_scale(uint32_t bits) { return min(max(bits, kScaleLeast), kScaleMost); }
+// x / y, where r is 1 / y to an ulp: exact where the quotient has an fp32 (ties between codes and scales do).
+__device__ __forceinline__ float quotient(float x, float y, float r) {
+  const float q = x * r;
+  return fmaf(fmaf(-q, y, x), r, q);
+}
 // Scale of a group whose largest magnitude is a, as fp32 bits: a / 7 to three bits behind the leading one, ties to even.
 __device__ __forceinline__ uint32_t scale_bits(float a) {
-  const uint32_t u = __float_as_uint(__fdiv_rn(a, 7.f));
+  const uint32_t u = __float_as_uint(quotient(a, 7.f, 1.f / 7.f));
   return clamp_scale((u + 0x7ffffu + (u >> 20 & 1u)) & 0xfff00000u);
 }
 __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) { return (bits - kScaleLeast) >> 20; }
 
-// Codes of eight elements, each off by at most e; `unsure` is set where that could change one.  e = 0: exact inputs, of few
-// enough bits for the remainder to be exact, and a tie goes to the even code.
-__device__ __forceinline__ uint32_t piece_codes(const float2 (&v)[4], float s, float e, bool& unsure) {
-  const float inv = __frcp_rn(s), half = 0.5f * s;
-  auto code = [&](float y) {
-    y = y == y ? y : 0.f;                          // a NaN counts as zero
-    float r = rintf(fminf(fmaxf(y * inv, -7.f), 7.f));
-    const float rem = fmaf(-r, s, y), d = half - fabsf(rem);
-    if (e > 0.f) unsure |= fabsf(d) <= e;
-    else if (d < 0.f || (d == 0.f && ((int)r & 1))) r = fminf(fmaxf(r + copysignf(1.f, rem), -7.f), 7.f);
-    return (uint32_t)((int)r + 8);
-  };
-  uint32_t w = 0;
+// Codes of eight elements of at most 7.5 s; `far`: the largest distance of one from its code's value.  Sums with 1.5 * 2^23 + 8
+// round to whole numbers, ties to even, and leave the code in the low bits (rounding and conversion instructions run at a
+// sixteenth of the rate).
+__device__ __forceinline__ uint32_t piece_codes(const float2 (&v)[4], float s, float& far) {
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  uint32_t pair[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w |= (code(v[i].x) | code(v[i].y) << 16) << (4 * i);
-  return w;
+  for (int i = 0; i < 4; ++i) {
+    const float2 q = __fmul2_rn(v[i], both(inv)), t = __ffma2_rn(__ffma2_rn(q, both(-s), v[i]), both(inv), q);
+    const float2 c = __fadd2_rn(t, both(12582920.f)), r = __ffma2_rn(__fadd2_rn(c, both(-12582920.f)), both(-s), v[i]);
+    far = fmaxf(fmaxf(far, fabsf(r.x)), fabsf(r.y));
+    pair[i] = __byte_perm(__float_as_uint(c.x), __float_as_uint(c.y), 0x5410);
+  }
+  return ((pair[3] * 16 + pair[2]) * 16 + pair[1]) * 16 + pair[0];
 }
 
 // The codes of a pass of keys in 64 bits, from its inputs.  Out of line and rare.  Whole warps.
@@ -233,32 +237,59 @@ __device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0,
   return out;
 }
 
-// Codes of a pass of keys (`x`, `y`: its pieces in fp32, largest magnitude of the head before the rotation `top`) or values.
+struct Pieces {                    // a lane's two
+  float2 x[4], y[4];
+};
+__device__ __forceinline__ Pieces pieces(const float2 (&x)[4], const float2 (&y)[4]) {
+  return {{x[0], x[1], x[2], x[3]}, {y[0], y[1], y[2], y[3]}};
+}
+// Codes of a pass of keys (its pieces in fp32, `top` the largest magnitude of the head before the rotation) or values.  Out of
+// line: it is called from every pass, and the loops around it have to stay in the instruction cache.  Whole warps.
 template <int D>
-__device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, bool is_v, float top, int pos, uint4 in0, uint4 in1, const float2 (&x)[4],
-                                          const float2 (&y)[4]) {
+__device__ __noinline__ Codes codes_of(const RopeArgs& a, Pieces v, bool is_v, float top, int pos, uint4 in0, uint4 in1) {
+  const Lane<D> ln(a, threadIdx.x & 31);
   // fp32: the norm is off by under 7.5e-7, relative (16 roundings of the sum of squares, halved by the root, its 2 ulp and the
   // products), the angle by 1.9e-7, sine and cosine by 1.2e-7 and the rotation's two roundings by as much: 1.2e-6 of |a| + |b|,
   // which is at most 2 top.
   const bool normed = !is_v && a.k_weight != nullptr, turned = !is_v && a.rot > 0;
   const float err = normed || turned ? 4e-6f * top : 0.f;
   float a0 = 0.f, a1 = 0.f;                        // (a NaN drops out)
+  float2 odd = both(0.f);                          // becomes a NaN by a NaN or an infinity
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    a0 = fmaxf(a0, fmaxf(fabsf(x[i].x), fabsf(x[i].y)));
-    a1 = fmaxf(a1, fmaxf(fabsf(y[i].x), fabsf(y[i].y)));
+    a0 = fmaxf(fmaxf(a0, fabsf(v.x[i].x)), fabsf(v.x[i].y));
+    a1 = fmaxf(fmaxf(a1, fabsf(v.y[i].x)), fabsf(v.y[i].y));
+    odd = __ffma2_rn(v.x[i], both(0.f), __ffma2_rn(v.y[i], both(0.f), odd));
   }
   group_max<D>(a, ln, a0, a1);
   const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
-  bool unsure = false;
-  if (err != 0.f)                                  // uniform over the lanes of a head
-    unsure = scale_bits(a0 + err) != scale_bits(fmaxf(a0 - err, 0.f)) || scale_bits(a1 + err) != scale_bits(fmaxf(a1 - err, 0.f));
+  if (odd.x + odd.y != 0.f || a0 > 7.f * __uint_as_float(kScaleMost) || a1 > 7.f * __uint_as_float(kScaleMost)) {
+    // what is not finite, or beyond the largest scale: a NaN counts as zero, the rest as 7 times the scale
+    const float most = 7.f * __uint_as_float(kScaleMost);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      auto in_range = [&](float z) { return z == z ? fminf(fmaxf(z, -most), most) : 0.f; };
+      v.x[i] = make_float2(in_range(v.x[i].x), in_range(v.x[i].y));
+      v.y[i] = make_float2(in_range(v.y[i].x), in_range(v.y[i].y));
+    }
+  }
+  const float f0 = __uint_as_float(s0), f1 = __uint_as_float(s1);
+  float far0 = 0.f, far1 = 0.f;
   Codes c;
-  c.word0 = piece_codes(x, __uint_as_float(s0), normed || ln.turn0 ? err : 0.f, unsure);
-  c.word1 = piece_codes(y, __uint_as_float(s1), normed || ln.turn1 ? err : 0.f, unsure);
+  c.word0 = piece_codes(v.x, f0, far0);
+  c.word1 = piece_codes(v.y, f1, far1);
   c.scale0 = scale_byte(s0);
   c.scale1 = scale_byte(s1);
-  if (!is_v && __any_sync(0xffffffffu, unsure || !(top < 1e38f))) c = exact_codes<D>(a, pos, in0, in1);
+  bool unsure = !(top < 1e38f);
+  if (err != 0.f) {                                // uniform over the lanes of a head
+    unsure |= scale_bits(a0 + err) != scale_bits(fmaxf(a0 - err, 0.f)) || scale_bits(a1 + err) != scale_bits(fmaxf(a1 - err, 0.f));
+    // within the error of a border (what is beyond the largest scale is far from its code, and sure)
+    unsure |= (normed || ln.turn0) && far0 >= 0.5f * f0 - err && s0 < kScaleMost;
+    unsure |= (normed || ln.turn1) && far1 >= 0.5f * f1 - err && s1 < kScaleMost;
+  }
+  // (next to the largest scale's borders all is computed again)
+  unsure |= err != 0.f && (s0 == kScaleMost || s1 == kScaleMost);
+  if (!is_v && __any_sync(0xffffffffu, unsure)) c = exact_codes<D>(a, pos, in0, in1);
   return c;
 }
 
@@ -272,7 +303,7 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
     float2 x[4], y[4];
     unpack8(in0, x);
     unpack8(in1, y);
-    codes = codes_of<D>(a, ln, true, 0.f, pos, in0, in1, x, y);
+    codes = codes_of<D>(a, pieces(x, y), true, 0.f, pos, in0, in1);
   }
   if (!is_v) {                                     // uniform over the warp
     float2 x[4], y[4];
@@ -319,7 +350,7 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
         }
       }
     }
-    if (Q4 && !is_q) codes = codes_of<D>(a, ln, false, top, pos, in0, in1, x, y);
+    if (Q4 && !is_q) codes = codes_of<D>(a, pieces(x, y), false, top, pos, in0, in1);
     in0 = pack8(x);
     in1 = pack8(y);
   }
@@ -474,7 +505,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
       angle_of = t;
       if (slot >= a.n_slots && cached<Q4>(a) && lane == 0) report_range(a.status, Q4 ? (int)kWhereRopeSlotQ4 : (int)kWhereRopeSlot);
     }
-#pragma unroll
+#pragma unroll(Q4 ? 1 : kStreamRun)
     for (int u = 0; u < kStreamRun; ++u) {
       const int p = x.b * kStreamRun + u;
       if (p < passes)

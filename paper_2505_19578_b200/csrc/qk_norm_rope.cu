@@ -106,10 +106,15 @@ __device__ __forceinline__ void angles(const uint64_t (&f)[2], int pos, const La
 }
 
 // The largest of the lanes' v0 (piece c0) and v1 (piece c1) over the pieces of each piece's group of 32 elements.  Whole warps.
+__device__ __forceinline__ double larger(double x, double y) { return fmax(x, y); }
+__device__ __forceinline__ float larger(float x, float y) {            // a NaN if either is one
+  float z;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+  return z;
+}
 template <int D, typename T>
 __device__ __forceinline__ void group_max(const RopeArgs& a, const Lane<D>& ln, T& v0, T& v1) {
   constexpr uint32_t kAll = 0xffffffffu;
-  auto larger = [](T x, T y) { return x > y ? x : y; };
   if (a.interleaved || a.rot % 64 == 0) {          // a group's four pieces are those of four neighbouring lanes
 #pragma unroll
     for (int o = 1; o <= 2; o <<= 1) {
@@ -237,58 +242,52 @@ __device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0,
   return out;
 }
 
-struct Pieces {                    // a lane's two
-  float2 x[4], y[4];
-};
-__device__ __forceinline__ Pieces pieces(const float2 (&x)[4], const float2 (&y)[4]) {
-  return {{x[0], x[1], x[2], x[3]}, {y[0], y[1], y[2], y[3]}};
-}
-// Codes of a pass of keys (its pieces in fp32, `top` the largest magnitude of the head before the rotation) or values.  Out of
-// line: it is called from every pass, and the loops around it have to stay in the instruction cache.  Whole warps.
+// Codes of a pass of keys (its pieces x, y in fp32, each off by 2e-6 `pair` at most, any of the head by 2e-6 `top`) or values
+// (pair, top: 0).  Whole warps.
 template <int D>
-__device__ __noinline__ Codes codes_of(const RopeArgs& a, Pieces v, bool is_v, float top, int pos, uint4 in0, uint4 in1) {
-  const Lane<D> ln(a, threadIdx.x & 31);
-  // fp32: the norm is off by under 7.5e-7, relative (16 roundings of the sum of squares, halved by the root, its 2 ulp and the
-  // products), the angle by 1.9e-7, sine and cosine by 1.2e-7 and the rotation's two roundings by as much: 1.2e-6 of |a| + |b|,
-  // which is at most 2 top.
-  const bool normed = !is_v && a.k_weight != nullptr, turned = !is_v && a.rot > 0;
-  const float err = normed || turned ? 4e-6f * top : 0.f;
-  float a0 = 0.f, a1 = 0.f;                        // (a NaN drops out)
-  float2 odd = both(0.f);                          // becomes a NaN by a NaN or an infinity
+__device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, bool is_v, bool normed, float pair, float top, int pos, uint4 in0, uint4 in1,
+                                          const float2 (&x)[4], const float2 (&y)[4]) {
+  float a0 = 0.f, a1 = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    a0 = fmaxf(fmaxf(a0, fabsf(v.x[i].x)), fabsf(v.x[i].y));
-    a1 = fmaxf(fmaxf(a1, fabsf(v.y[i].x)), fabsf(v.y[i].y));
-    odd = __ffma2_rn(v.x[i], both(0.f), __ffma2_rn(v.y[i], both(0.f), odd));
+    a0 = larger(larger(a0, fabsf(x[i].x)), fabsf(x[i].y));
+    a1 = larger(larger(a1, fabsf(y[i].x)), fabsf(y[i].y));
   }
   group_max<D>(a, ln, a0, a1);
-  const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
-  if (odd.x + odd.y != 0.f || a0 > 7.f * __uint_as_float(kScaleMost) || a1 > 7.f * __uint_as_float(kScaleMost)) {
-    // what is not finite, or beyond the largest scale: a NaN counts as zero, the rest as 7 times the scale
-    const float most = 7.f * __uint_as_float(kScaleMost);
+  constexpr float kMost = 7.f * 3840.f;            // 7 times the largest scale
+  Codes c;
+  bool unsure = !(top < 1e38f);
+  if (__any_sync(0xffffffffu, !(a0 <= kMost && a1 <= kMost))) {
+    // something is not finite, or beyond the largest scale: a NaN counts as zero, the rest as 7 times the scale at most
+    float2 u[4], v[4];
+    auto in_range = [&](float z) { return z == z ? fminf(fmaxf(z, -kMost), kMost) : 0.f; };
+    a0 = a1 = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      auto in_range = [&](float z) { return z == z ? fminf(fmaxf(z, -most), most) : 0.f; };
-      v.x[i] = make_float2(in_range(v.x[i].x), in_range(v.x[i].y));
-      v.y[i] = make_float2(in_range(v.y[i].x), in_range(v.y[i].y));
+      u[i] = make_float2(in_range(x[i].x), in_range(x[i].y));
+      v[i] = make_float2(in_range(y[i].x), in_range(y[i].y));
+      a0 = fmaxf(fmaxf(a0, fabsf(u[i].x)), fabsf(u[i].y));
+      a1 = fmaxf(fmaxf(a1, fabsf(v[i].x)), fabsf(v[i].y));
+    }
+    group_max<D>(a, ln, a0, a1);
+    float far = 0.f;
+    const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
+    c = {piece_codes(u, __uint_as_float(s0), far), piece_codes(v, __uint_as_float(s1), far), scale_byte(s0), scale_byte(s1)};
+    unsure |= top > 0.f;
+  } else {
+    const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
+    const float f0 = __uint_as_float(s0), f1 = __uint_as_float(s1);
+    float far0 = 0.f, far1 = 0.f;
+    c = {piece_codes(x, f0, far0), piece_codes(y, f1, far1), scale_byte(s0), scale_byte(s1)};
+    if (!is_v) {
+      // a border between two codes or two scales within the error
+      const float err = 2e-6f * pair, group_err = 2e-6f * top;
+      if (normed || ln.turn0) unsure |= far0 >= 0.5f * f0 - err;
+      if (normed || ln.turn1) unsure |= far1 >= 0.5f * f1 - err;
+      if (group_err > 0.f)
+        unsure |= scale_bits(a0 + group_err) != scale_bits(fmaxf(a0 - group_err, 0.f)) || scale_bits(a1 + group_err) != scale_bits(fmaxf(a1 - group_err, 0.f));
     }
   }
-  const float f0 = __uint_as_float(s0), f1 = __uint_as_float(s1);
-  float far0 = 0.f, far1 = 0.f;
-  Codes c;
-  c.word0 = piece_codes(v.x, f0, far0);
-  c.word1 = piece_codes(v.y, f1, far1);
-  c.scale0 = scale_byte(s0);
-  c.scale1 = scale_byte(s1);
-  bool unsure = !(top < 1e38f);
-  if (err != 0.f) {                                // uniform over the lanes of a head
-    unsure |= scale_bits(a0 + err) != scale_bits(fmaxf(a0 - err, 0.f)) || scale_bits(a1 + err) != scale_bits(fmaxf(a1 - err, 0.f));
-    // within the error of a border (what is beyond the largest scale is far from its code, and sure)
-    unsure |= (normed || ln.turn0) && far0 >= 0.5f * f0 - err && s0 < kScaleMost;
-    unsure |= (normed || ln.turn1) && far1 >= 0.5f * f1 - err && s1 < kScaleMost;
-  }
-  // (next to the largest scale's borders all is computed again)
-  unsure |= err != 0.f && (s0 == kScaleMost || s1 == kScaleMost);
   if (!is_v && __any_sync(0xffffffffu, unsure)) c = exact_codes<D>(a, pos, in0, in1);
   return c;
 }
@@ -299,18 +298,14 @@ template <int D, bool Q4>
 __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln, const Pass& p, bool is_v, bool is_q, int t, int slot, int pos, uint4 in0, uint4 in1,
                                             const float (&cs)[8], const float (&sn)[8]) {
   Codes codes;
-  if (Q4 && is_v) {
-    float2 x[4], y[4];
+  float2 x[4], y[4];
+  float pair = 0.f, top = 0.f;
+  if (!is_v || Q4) {                               // uniform over the warp, as is all that depends on the kind
     unpack8(in0, x);
     unpack8(in1, y);
-    codes = codes_of<D>(a, pieces(x, y), true, 0.f, pos, in0, in1);
   }
-  if (!is_v) {                                     // uniform over the warp
-    float2 x[4], y[4];
-    float top = 0.f;
-    bool odd = false;                              // the squares' sum left the range in which it is exact to the bound below
-    unpack8(in0, x);
-    unpack8(in1, y);
+  if (!is_v) {
+    bool odd = false;                              // the squares' sum left the range in which fp32 has it to the bound below
     const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
     if (weight) {
       float2 sum = __fmul2_rn(x[0], x[0]);
@@ -329,9 +324,17 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
 #pragma unroll
       for (int i = 0; i < 4; ++i) { x[i] = __fmul2_rn(x[i], __fmul2_rn(inv, wx[i])); y[i] = __fmul2_rn(y[i], __fmul2_rn(inv, wy[i])); }
     }
-    if (Q4 && !is_q) {
+    if (Q4 && !is_q && (weight || a.rot > 0)) {
+      // fp32: the norm is off by under 7.5e-7, relative (16 roundings of the sum of squares, halved by the root, its 2 ulp and
+      // the products), the angle by 1.9e-7, sine and cosine by 1.2e-7 and the rotation's two roundings by as much: 1.2e-6 of
+      // |a| + |b| for each pair
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fmaxf(fabsf(x[i].x), fabsf(x[i].y)), fmaxf(fabsf(y[i].x), fabsf(y[i].y))));
+      for (int i = 0; i < 4; ++i) {
+        const float2 u = a.interleaved ? make_float2(fabsf(x[i].x) + fabsf(x[i].y), fabsf(y[i].x) + fabsf(y[i].y)) :
+                                         make_float2(fabsf(x[i].x) + fabsf(y[i].x), fabsf(x[i].y) + fabsf(y[i].y));
+        pair = fmaxf(fmaxf(pair, u.x), u.y);
+      }
+      top = pair;
 #pragma unroll
       for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       if (odd) top = CUDART_INF_F;
@@ -350,7 +353,9 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
         }
       }
     }
-    if (Q4 && !is_q) codes = codes_of<D>(a, pieces(x, y), false, top, pos, in0, in1);
+  }
+  if (Q4 && !is_q) codes = codes_of<D>(a, ln, is_v, !is_v && a.k_weight != nullptr, pair, top, pos, in0, in1, x, y);
+  if (!is_v) {
     in0 = pack8(x);
     in1 = pack8(y);
   }

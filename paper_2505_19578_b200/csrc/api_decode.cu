@@ -388,8 +388,9 @@ int sp_tree_attn_q4(sp_ctx* ctx, const sp_tensor* q, const sp_q4_cache* cache, c
     return SP_OK;
   }
   if ((rc = need_split(ctx, s))) return rc;
-  if (launch_tree_attn_q4(a, q4_of(cache), ctx->split_ws, ctx->arrived, ctx->n_sm, s) != cudaSuccess) return SP_ERR_CUDA;
-  ctx->launches += 1;
+  int launched = 0;
+  if (launch_tree_attn_q4(a, q4_of(cache), ctx->split_ws, ctx->arrived, ctx->n_sm, s, &launched) != cudaSuccess) return SP_ERR_CUDA;
+  ctx->launches += launched;
   return SP_OK;
 }
 

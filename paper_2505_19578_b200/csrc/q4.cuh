@@ -76,7 +76,8 @@ cudaError_t launch_cache_keep_q4(const KeepQ4Args& a, cudaStream_t s);
 cudaError_t launch_cache_read_q4(ReadQ4Args& a, cudaStream_t s);
 // a.kc and a.vc are not used.  arrived: [n_sm] zeros, and zeros again afterwards (not after a timeout).
 size_t tree_attn_q4_workspace_bytes(int n_sm);
-cudaError_t launch_tree_attn_q4(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s);
+cudaError_t launch_tree_attn_q4(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s, int* launched);
+cudaError_t launch_tree_attn_q4_tall(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int n_sm, cudaStream_t s);      // ws as sp_tree_attn's
 cudaError_t launch_tree_attn_q4_simt(const TreeAttnArgs& a, const Q4Cache& c, cudaStream_t s);
 
 }  // namespace sp

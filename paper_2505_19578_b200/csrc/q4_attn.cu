@@ -679,18 +679,20 @@ cudaError_t launch(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arriv
 }
 
 template <int D>
-cudaError_t launch_rows(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s) {
-  // rows of a request if all have as many; requests of more rows are several units, which is right for any lengths
+cudaError_t launch_rows(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s, int* launched) {
+  // Rows of a request if all have as many: more than 16 make tiles of 128 for the tensor cores' own memory.  (Requests of more
+  // rows than a form's units have are several units, which is right for any lengths.)
   const long long rows = ((long long)a.rows + a.n_req - 1) / a.n_req * a.group;
-  return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : launch<D, 2>(a, c, ws, arrived, n_sm, s);
+  *launched = rows <= 16 ? 1 : 2;
+  return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : rows <= 16 ? launch<D, 2>(a, c, ws, arrived, n_sm, s) : launch_tree_attn_q4_tall(a, c, ws, n_sm, s);
 }
 
 }  // namespace
 
 size_t tree_attn_q4_workspace_bytes(int n_sm) { return (size_t)n_sm * 2 * 16 * (128 * sizeof(float) + sizeof(float2)); }
 
-cudaError_t launch_tree_attn_q4(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s) {
-  return a.d == 128 ? launch_rows<128>(a, c, ws, arrived, n_sm, s) : launch_rows<64>(a, c, ws, arrived, n_sm, s);
+cudaError_t launch_tree_attn_q4(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s, int* launched) {
+  return a.d == 128 ? launch_rows<128>(a, c, ws, arrived, n_sm, s, launched) : launch_rows<64>(a, c, ws, arrived, n_sm, s, launched);
 }
 
 }  // namespace sp

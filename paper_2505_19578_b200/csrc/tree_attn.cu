@@ -61,7 +61,9 @@
 // Every wait is bounded as in the other tensor-core kernels: a wait that runs out raises the abort flag and the status
 // word, and all roles fall through to the common end.
 #include <limits.h>
+#include <string.h>
 
+#include "q4.cuh"
 #include "tree_rows.cuh"
 
 namespace sp {
@@ -71,8 +73,10 @@ using namespace tc;
 
 constexpr int kTile = 128;                       // keys of a tile
 constexpr int kUnitRows = 256;
-constexpr int kThreads = 384, kWarps = kThreads / 32;
+constexpr int kWarps = 12, kDecoders = 4;        // the decoders, of the form for a 4-bit cache, are warps 12 to 15
 constexpr int kProducer = 8, kIssuer = 9, kLoader = 10, kIssuer1 = 11;
+template <bool Q4>
+constexpr int kThreads = (kWarps + (Q4 ? kDecoders : 0)) * 32;
 constexpr int kUnitRing = 4;
 constexpr int kNarrowSteps = 2, kTallSteps = 4;  // steps of a unit besides those of its tiles (narrow; tall and wide); measured at head_dim 128
 constexpr int kNarrowRows = 16;
@@ -99,8 +103,8 @@ struct Plan {
                        BAR_OFULL = BAR_REF + 1, BAR_OFREE = BAR_OFULL + 1, BAR_QFULL = BAR_OFREE + 1, BAR_QFREE = BAR_QFULL + 2,
                        BAR_UNIT = BAR_QFREE + 2, BAR_UFREE = BAR_UNIT + kUnitRing, BARS = BAR_UFREE + kUnitRing;
   static constexpr int UNIT_OFF = MISC_OFF + 2 * BARS * 8, UNIT_BYTES = 48;                  // a second set of barriers: for a run walked again
-  static constexpr int SCAN_OFF = (UNIT_OFF + kUnitRing * UNIT_BYTES + 15) / 16 * 16;        // int64 [2][kWarps]
-  static constexpr int RUN_OFF = SCAN_OFF + 2 * kWarps * 8;                           // int64 [3], int [4]
+  static constexpr int SCAN_OFF = (UNIT_OFF + kUnitRing * UNIT_BYTES + 15) / 16 * 16;        // int64 [2][kWarps + kDecoders]
+  static constexpr int RUN_OFF = SCAN_OFF + 2 * (kWarps + kDecoders) * 8;                           // int64 [3], int [4]
   static constexpr int TAG_OFF = RUN_OFF + 3 * 8 + 4 * 4;                             // int [8]
   static constexpr int EX_OFF = (TAG_OFF + 8 * 4 + 15) / 16 * 16;                     // narrow: float2 [8][16]; tall: float [2][128]
   static constexpr int REF_OFF = EX_OFF + 1024;                                       // tall: float [128]
@@ -818,8 +822,8 @@ __device__ __noinline__ void issue_wide(const TreeAttnArgs& a, uint8_t* smem, ui
   }
 }
 
-// Softmax and epilogue, wide: a group for each half of the rows.
-template <int D>
+// Softmax and epilogue, wide: a group for each half of the rows.  (Q4: no value is infinite or a NaN, nothing has to be cleaned.)
+template <int D, bool Q4>
 __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& work, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
   using P = Plan<D>;
   const uint32_t base = smem_u32(smem);
@@ -915,7 +919,7 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
         l += sum;
         tmem_wait_st();
       }
-      if (special && ok) ok = clean(done + (t >> 1), u, k0, half, no_mask, seq);
+      if (!Q4 && special && ok) ok = clean(done + (t >> 1), u, k0, half, no_mask, seq);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(P::BAR_P + 2 * x + half));
@@ -927,7 +931,7 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
       float* part = p.whole ? nullptr : work.part + p.slot * D;
       write_columns(t_o, 0, D, !p.whole ? 1.f : l != 0.f ? 1.f / l : 0.f, live, p.out, part);
       if (live) {
-        if (bad_tag[(seq + 1) % 8] == seq + 1) {
+        if (!Q4 && bad_tag[(seq + 1) % 8] == seq + 1) {
           if (p.whole) add_nonfinite(a, u, p.token, p.out, 0, D);
           else add_nonfinite(a, u, p.token, part, 0, D);
         }
@@ -943,7 +947,7 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
 }
 
 // Softmax and epilogue, tall: the groups take the tiles in turn.
-template <int D>
+template <int D, bool Q4>
 __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& work, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
   using P = Plan<D>;
   const uint32_t base = smem_u32(smem);
@@ -1023,7 +1027,7 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
         }
         tmem_wait_st();
       }
-      if (special) ok = clean(i, u, k0, no_mask, seq);
+      if (!Q4 && special) ok = clean(i, u, k0, no_mask, seq);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(P::BAR_P + buf));
@@ -1046,7 +1050,7 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
       const bool finite = write_columns(t_o, lo, lo + D / 2, !p.whole ? 1.f : l != 0.f ? 1.f / l : 0.f, live, p.out, part);
       if (live) {
         if (seen && (l > kTallMost || l < kTallLeast || (l > 256.f && !finite))) *redo = 1;
-        if (bad_tag[(seq + 1) % 8] == seq + 1) {
+        if (!Q4 && bad_tag[(seq + 1) % 8] == seq + 1) {
           if (p.whole) add_nonfinite(a, u, p.token, p.out, lo, lo + D / 2);
           else add_nonfinite(a, u, p.token, part, lo, lo + D / 2);
         }
@@ -1064,10 +1068,144 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
   }
 }
 
+// Form for a 4-bit cache: what the producer is otherwise.  Four warps take 32 keys of each tile, K or V, in the ring's order:
+// codes and scales from global memory (a lane a run of 32 elements of a token's head, which has one scale; eight neighbouring
+// lanes eight tokens, so that their 16-byte stores go to different banks), two loads ahead of the one that is being decoded,
+// bf16 values into the tile's swizzled rows.  4 loads of 16 bytes, 2 of scales and 32 stores of 16 bytes a lane and tile; 7
+// integer and 4 packed multiply-add instructions for 8 elements (see q4_attn.cu): 450 instructions a warp and tile in all, of
+// the 1000 to 1100 cycles that its products and its exponentials take.
+struct CodedRun {                  // a lane's part of 32 keys: of two blocks, D / 64 runs each
+  uint4 codes[2][2];
+  uint32_t scales[2];
+};
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ Work work, const __grid_constant__ CUtensorMap tm_k,
-                 const __grid_constant__ CUtensorMap tm_v) {
+__device__ __forceinline__ void decode_run(const uint4& c, uint32_t byte, uint32_t row_at, int piece0, int r7) {
+  const uint32_t sb = (byte << 4 | byte << 20) + 0x35803580u;
+  const __nv_bfloat162 s = *reinterpret_cast<const __nv_bfloat162*>(&sb), off = __hmul2(s, __floats2bfloat162_rn(-136.f, -136.f));
+  const uint32_t words[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t y[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      uint32_t w;
+      asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(w) : "r"(words[j] >> (4 * p)), "r"(0x000f000fu), "r"(0x43004300u));
+      const __nv_bfloat162 z = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w), s, off);
+      y[p] = *reinterpret_cast<const uint32_t*>(&z);
+    }
+    const int piece = piece0 + j;
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row_at + (piece >> 3) * Plan<D>::BOX + (((piece ^ r7) & 7) << 4)), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3])
+                 : "memory");
+  }
+}
+template <int D>
+__device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles, uint32_t lead) {
+  using P = Plan<D>;
+  using B = Block<D>;
+  constexpr int RUNS = D / 64, AHEAD = 2;          // runs of a lane and block; loads under way
+  const uint32_t ring = smem_u32(smem) + P::RING_OFF;
+  auto bar = [&](int which) { return bars + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  const int warp = (int)(threadIdx.x >> 5) - kWarps, lane = threadIdx.x & 31;
+  const int token = D == 128 ? lane & 7 : lane & 15, group = D == 128 ? lane >> 3 : lane >> 4;      // and token + 8
+  // of this lane's runs in a block, and of their scales (tokens i and i + 8 have theirs side by side)
+  const int k_at = B::k_word(token, group * 4), v_at = B::v_word(token, group * 4), ks_at = B::k_scale(token & 7, group), vs_at = B::v_scale(token & 7, group);
+  constexpr int K8 = B::k_word(8, 0), V8 = B::v_word(8, 0) - B::v_word(0, 0);
+  // ---- fetching.  (A unit's first tile is waited for with two loads fetched but not decoded: with more, four units of one tile
+  // each would wait for one another.)
+  const uint8_t* at[3][2];                         // blocks of the last tiles whose K was fetched; null: no such page, or no key
+#pragma unroll
+  for (int i = 0; i < 3; ++i) at[i][0] = at[i][1] = nullptr;
+  int seq = 0, kt = 0, kt_end = 0, len = 0, id[2] = {0, 0};
+  const int32_t* row = nullptr;
+  const uint8_t* head = nullptr;
+  uint32_t fk = 0, fv = 0;                         // tiles whose K, V have been fetched
+  bool ok = true;
+  auto lookup = [&] {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int key = kt * kTile + warp * 32 + x * 16;
+      id[x] = key < len ? row[key >> a.page_log2] : 0;
+    }
+  };
+  auto fetch = [&](CodedRun& c) {
+    const bool is_k = fk < n_tiles && fk - fv <= lead;
+    if (!is_k && fv >= n_tiles) return;
+    if (is_k) {
+      if (kt == kt_end) {
+        const int e = seq % kUnitRing;
+        ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
+        if (!ok) return;
+        const Unit& u = units[e];
+        kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = u.len;
+        row = a.table + (size_t)u.b * a.max_pages;
+        head = cache.data + u.g * cache.s_head;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+        ++seq;
+        lookup();
+      }
+#pragma unroll
+      for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int key = kt * kTile + warp * 32 + x * 16;
+        at[0][x] = nullptr;
+        if (key < len) {
+          if (id[x] >= 0 && id[x] < a.n_pages) at[0][x] = head + id[x] * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES;
+          else if (lane == 0) report_range(a.status, kWhereTreePageQ4);
+        }
+      }
+      ++kt;
+      if (kt < kt_end) lookup();
+      ++fk;
+    }
+    const uint32_t back = is_k ? 0 : fk - 1 - fv;  // at most lead
+    if (!is_k) ++fv;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint8_t* blk = back == 0 ? at[0][x] : back == 1 ? at[1][x] : at[2][x];
+      c.codes[x][0] = c.codes[x][1] = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);      // zeros
+      c.scales[x] = 0;
+      if (blk) {
+        const uint8_t* src = blk + (is_k ? k_at : v_at);
+        c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(src));
+        if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(src + (is_k ? K8 : V8)));
+        c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk + (is_k ? ks_at : vs_at)));
+      }
+    }
+  };
+  CodedRun c[AHEAD + 1];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (ok) fetch(c[i]);
+  uint32_t slot = 0, lap = 0;
+  for (uint32_t i0 = 0; i0 < 2 * n_tiles && ok; i0 += AHEAD + 1) {
+#pragma unroll
+    for (int i = 0; i <= AHEAD; ++i) {
+      if (i0 + i >= 2 * n_tiles || !ok) break;
+      fetch(c[(i + AHEAD) % (AHEAD + 1)]);
+      if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
+      if (!ok) break;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < RUNS; ++y) {
+          const int r = warp * 32 + x * 16 + token + 8 * y;
+          const uint32_t byte = RUNS == 2 ? c[i].scales[x] >> (8 * y) & 0xffu : c[i].scales[x] >> (token & 8) & 0xffu;
+          decode_run<D>(c[i].codes[x][y], byte, ring + slot * P::SLOT + (r >> 3) * P::GROUP + (r & 7) * 128, group * 4, r & 7);
+        }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_FULL + slot));
+      if (++slot == P::SLOTS) { slot = 0; ++lap; }
+    }
+  }
+}
+
+template <int D, bool Q4>
+__device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work& work, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Q4Cache& cache) {
+  constexpr int THREADS = kThreads<Q4>, WARPS = THREADS / 32;
   using P = Plan<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
@@ -1091,7 +1229,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
 
   let_next_start();
   const bool misplaced = (base & 1023u) != 0;      // the tiles' swizzle needs the window's alignment
-  if (warp == kProducer && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
+  if (!Q4 && warp == kProducer && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
   if (threadIdx.x == 0) {
     *abort_flag = *redo = 0;
     for (int i = 0; i < 8; ++i) bad_tag[i] = 0;
@@ -1100,7 +1238,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   const bool poisoned = decode_poisoned(a.status);
 
   // ---- where the run begins
-  const int per = (a.n_req + kThreads - 1) / kThreads;
+  const int per = (a.n_req + THREADS - 1) / THREADS;
   const int b_lo = min((int)threadIdx.x * per, a.n_req), b_hi = min(b_lo + per, a.n_req);
   int unit_rows = kUnitRows;
   long long mine_t = 0, mine_u = 0, more_t = 0;    // tiles, units; tiles in addition with units of 128 rows
@@ -1123,24 +1261,24 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       const long long up_t = __shfl_up_sync(0xffffffffu, incl_t, o), up_u = __shfl_up_sync(0xffffffffu, incl_u, o);
       if (lane >= o) { incl_t += up_t; incl_u += up_u; }
     }
-    if (lane == 31) { scan[warp] = incl_t; scan[kWarps + warp] = incl_u; }
+    if (lane == 31) { scan[warp] = incl_t; scan[WARPS + warp] = incl_u; }
   };
   sums();
   if (threadIdx.x == 0 && misplaced && atomicCAS(a.status, 0, (int)SP_ERR_UNSUPPORTED) == 0) a.status[1] = 90;
   bool wide = __syncthreads_or(many) != 0;
-  const bool narrow = __syncthreads_or(some) == 0;
+  const bool narrow = !Q4 && __syncthreads_or(some) == 0;
   if (wide) {
     // Units of 256 rows take half as many tiles again of the time of those of 128 (2.5 and 1.6 us a tile): tall, if cutting
     // them adds no more than that half (one chunk of a prompt among many single tokens, or 257 to 384 rows each: a request of
     // 256 rows among 255 of one token 251 us so, 317 as wide; one of 1024 rows 297 and 487).
     long long tiles = 0;
-    for (int w = 0; w < kWarps; ++w) tiles += scan[w];
+    for (int w = 0; w < WARPS; ++w) tiles += scan[w];
     __syncthreads();
     for (int o = 16; o > 0; o >>= 1) more_t += __shfl_down_sync(0xffffffffu, more_t, o);
     if (lane == 0) scan[warp] = more_t;
     __syncthreads();
     long long more = 0;
-    for (int w = 0; w < kWarps; ++w) more += scan[w];
+    for (int w = 0; w < WARPS; ++w) more += scan[w];
     __syncthreads();
     wide = 2 * more > tiles;
     if (!wide) {
@@ -1158,16 +1296,16 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   if (!narrow) {
     if (warp == kIssuer) tmem_alloc(smem_u32(tmem_slot), 512);
     // rows of the Q area that no unit fills stay zero: products of whatever lay there would cost power, and with it clock
-    for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < 2 * P::QHALF / 16; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
     fence_async_smem();
   }
   const int own = narrow ? kNarrowSteps : kTallSteps;         // a unit's steps besides its tiles'
   long long before_t = incl_t - mine_t, before_u = incl_u - mine_u, total_t = 0, total = 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) { before_t += scan[w]; before_u += scan[kWarps + w]; }
+  for (int w = 0; w < WARPS; ++w) {
+    if (w < warp) { before_t += scan[w]; before_u += scan[WARPS + w]; }
     total_t += scan[w];
-    total += scan[w] + own * scan[kWarps + w];
+    total += scan[w] + own * scan[WARPS + w];
   }
   const long long quota = divide(total, n_cta), extra = total - quota * n_cta;      // the first `extra` runs are one step longer
   auto run_begin = [&](int w) { return w * quota + min((long long)w, extra); };
@@ -1193,7 +1331,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   }
   auto init_barriers = [&](uint32_t bars, bool wide) {
     auto bar = [&](int which) { return bars + which * 8; };
-    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), 1);
+    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), Q4 ? kDecoders : 1);
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(P::BAR_S + i), 1);
       mbar_init(bar(P::BAR_P + i), 4);
@@ -1211,7 +1349,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
     }
     for (int e = 0; e < kUnitRing; ++e) {
       mbar_init(bar(P::BAR_UNIT + e), 1);
-      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : wide ? 11 : 10);
+      mbar_init(bar(P::BAR_UFREE + e), (narrow ? 9 : wide ? 11 : 10) + (Q4 ? kDecoders - 1 : 0));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   };
@@ -1266,7 +1404,7 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
               Meta m{(int)(z < cut ? divide(z, quota + 1) : extra + divide(z - cut, quota)), u.start, u.r0, u.rows, u.g, {0, 0, 0}};
               work.meta[cta] = m;
             }
-            if (a.seq_lens[b] > q.len) report_range(a.status, kWhereTreePage);   // longer than its table row
+            if (a.seq_lens[b] > q.len) report_range(a.status, Q4 ? (int)kWhereTreePageQ4 : (int)kWhereTreePage);   // longer than its table row
           }
           // its queries: rows of 128-byte boxes, 16-byte pieces swizzled as the MMA descriptors say.  A lane keeps its
           // piece of every (32 / pieces)-th row, whose token and head advance without division (one division a piece:
@@ -1308,7 +1446,11 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
         units[e].n_tiles = 0;
         mbar_arrive(bar(P::BAR_UNIT + e));
       }
-    } else if (warp == kProducer) {
+    } else if (Q4 && (warp == kProducer || warp >= kWarps)) {
+      if constexpr (Q4) {
+        if (warp != kProducer) decode<D>(a, cache, smem, bars, ab, n_tiles_cta, lead);
+      }
+    } else if (!Q4 && warp == kProducer) {
       // ------------------------------------------------------------ K and V tiles
       bool ok = true;
       const uint32_t ring = base + (narrow ? P::NRING_OFF : P::RING_OFF), slots = narrow ? P::NSLOTS : P::SLOTS;
@@ -1380,11 +1522,11 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
       else if (lane == 0 && !narrow && warp == kIssuer) issue_tall<D>(a, smem, ab, tmem, n_tiles_cta);
       __syncwarp();
     } else if (narrow) {
-      narrow_warps<D>(a, work, smem, ab);
+      if constexpr (!Q4) narrow_warps<D>(a, work, smem, ab);
     } else if (wide) {
-      softmax_wide<D>(a, work, smem, bars, ab, tmem, n_tiles_cta);
+      softmax_wide<D, Q4>(a, work, smem, bars, ab, tmem, n_tiles_cta);
     } else {
-      softmax_tall<D>(a, work, smem, ab, tmem, n_tiles_cta);
+      softmax_tall<D, Q4>(a, work, smem, ab, tmem, n_tiles_cta);
     }
 
     tc_fence_before();
@@ -1401,6 +1543,18 @@ tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__
   if (warp == kIssuer && !narrow) {
     tmem_dealloc(tmem, 512);
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads<false>, 1)
+tree_attn_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ Work work, const __grid_constant__ CUtensorMap tm_k,
+                 const __grid_constant__ CUtensorMap tm_v) {
+  tree_attn_body<D, false>(a, work, tm_k, tm_v, Q4Cache{});
+}
+template <int D>
+__global__ void __launch_bounds__(kThreads<true>, 1)
+tree_attn_q4_tall_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ Work work, const __grid_constant__ Q4Cache cache) {
+  tree_attn_body<D, true>(a, work, CUtensorMap{}, CUtensorMap{}, cache);
 }
 
 // ------------------------------------------------------------------ host side
@@ -1432,7 +1586,23 @@ cudaError_t launch(const TreeAttnArgs& a, void* ws, int n_cta, cudaStream_t s) {
   static_assert(smem <= 232448, "");
   cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(tree_attn_kernel<D>, dim3(n_cta), dim3(kThreads), smem, s, a, w, tk, tv);
+  e = launch_dependent(tree_attn_kernel<D>, dim3(n_cta), dim3(kThreads<false>), smem, s, a, w, tk, tv);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(tree_attn_join_kernel<D, kUnitRows>, dim3(n_cta * kJoinBlocksPerSm), dim3(kJoinWarps * 32), 0, s, a, static_cast<const Parts&>(w), n_cta);
+}
+
+template <int D>
+cudaError_t launch_q4_tall(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int n_cta, cudaStream_t s) {
+  Work w;
+  memset(&w, 0, sizeof(w));
+  const size_t slots = (size_t)n_cta * 2 * kUnitRows;
+  w.part = static_cast<float*>(ws);
+  w.ml = reinterpret_cast<float2*>(w.part + slots * 128);
+  w.meta = reinterpret_cast<Meta*>(w.ml + slots);
+  constexpr int smem = Plan<D>::TOTAL > 120 * 1024 ? Plan<D>::TOTAL : 120 * 1024;
+  cudaError_t e = cudaFuncSetAttribute(tree_attn_q4_tall_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  e = launch_dependent(tree_attn_q4_tall_kernel<D>, dim3(n_cta), dim3(kThreads<true>), smem, s, a, w, c);
   if (e != cudaSuccess) return e;
   return launch_dependent(tree_attn_join_kernel<D, kUnitRows>, dim3(n_cta * kJoinBlocksPerSm), dim3(kJoinWarps * 32), 0, s, a, static_cast<const Parts&>(w), n_cta);
 }
@@ -1445,6 +1615,10 @@ size_t tree_attn_workspace_bytes(int n_sm) {
 
 cudaError_t launch_tree_attn(const TreeAttnArgs& a, void* ws, int n_sm, cudaStream_t s) {
   return a.d == 128 ? launch<128>(a, ws, n_sm, s) : launch<64>(a, ws, n_sm, s);
+}
+
+cudaError_t launch_tree_attn_q4_tall(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int n_sm, cudaStream_t s) {
+  return a.d == 128 ? launch_q4_tall<128>(a, c, ws, n_sm, s) : launch_q4_tall<64>(a, c, ws, n_sm, s);
 }
 
 }  // namespace sp

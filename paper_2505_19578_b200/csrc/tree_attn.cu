@@ -1077,7 +1077,9 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
 struct CodedRun {                  // a lane's part of 32 keys: of two blocks, D / 64 runs each
   uint4 codes[2][2];
   uint32_t scales[2];
+  bool live[2];                    // else there is no such page, or no key: the values are zeros
 };
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) { asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory"); }
 template <int D>
 __device__ __forceinline__ void decode_run(const uint4& c, uint32_t byte, uint32_t row_at, int piece0, int r7) {
   const uint32_t sb = (byte << 4 | byte << 20) + 0x35803580u;
@@ -1102,7 +1104,7 @@ template <int D>
 __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles, uint32_t lead) {
   using P = Plan<D>;
   using B = Block<D>;
-  constexpr int RUNS = D / 64, AHEAD = 2;          // runs of a lane and block; loads under way
+  constexpr int RUNS = D / 64, AHEAD = 2, kFar = 5;       // runs of a lane and block; loads under way; tiles prefetched
   const uint32_t ring = smem_u32(smem) + P::RING_OFF;
   auto bar = [&](int which) { return bars + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
@@ -1112,93 +1114,104 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
   const int k_at = B::k_word(token, group * 4), v_at = B::v_word(token, group * 4), ks_at = B::k_scale(token & 7, group), vs_at = B::v_scale(token & 7, group);
   constexpr int K8 = B::k_word(8, 0), V8 = B::v_word(8, 0) - B::v_word(0, 0);
   // ---- fetching.  (A unit's first tile is waited for with two loads fetched but not decoded: with more, four units of one tile
-  // each would wait for one another.)
-  const uint8_t* at[3][2];                         // blocks of the last tiles whose K was fetched; null: no such page, or no key
+  // each would wait for one another.  Two loads cover the latency of L2, and that of HBM is covered by prefetches into L2 a few
+  // tiles ahead.)
+  const uint8_t* at[3][2];                         // blocks of the last tiles whose K was fetched
+  bool live[3][2];
 #pragma unroll
-  for (int i = 0; i < 3; ++i) at[i][0] = at[i][1] = nullptr;
-  int seq = 0, kt = 0, kt_end = 0, len = 0, id[2] = {0, 0};
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) { at[i][x] = cache.data; live[i][x] = false; }
+  int seq = 0, kt = 0, kt_end = 0, len = 0, id[2] = {0, 0}, far_id = 0;
   const int32_t* row = nullptr;
   const uint8_t* head = nullptr;
   uint32_t fk = 0, fv = 0;                         // tiles whose K, V have been fetched
   bool ok = true;
-  auto lookup = [&] {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int key = kt * kTile + warp * 32 + x * 16;
-      id[x] = key < len ? row[key >> a.page_log2] : 0;
-    }
-  };
+  auto page_of = [&](int key) { return key < len ? row[key >> a.page_log2] : -1; };
+  auto block_of = [&](int page, int key) { return head + page * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES; };
   auto fetch = [&](CodedRun& c) {
     const bool is_k = fk < n_tiles && fk - fv <= lead;
-    if (!is_k && fv >= n_tiles) return;
     if (is_k) {
+      const int mine = warp * 32 + (lane & 1) * 16;
       if (kt == kt_end) {
         const int e = seq % kUnitRing;
         ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
-        if (!ok) return;
         const Unit& u = units[e];
-        kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = u.len;
+        kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = ok ? u.len : 0;
         row = a.table + (size_t)u.b * a.max_pages;
         head = cache.data + u.g * cache.s_head;
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
         ++seq;
-        lookup();
-      }
 #pragma unroll
-      for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
+        for (int x = 0; x < 2; ++x) id[x] = page_of(kt * kTile + warp * 32 + x * 16);
+        // this warp's blocks of the tiles up to kFar ahead, a lane a block
+        const int t = kt + 1 + (lane >> 1), key = t * kTile + mine;
+        if (t < min(kt + kFar, kt_end)) {
+          const int far = page_of(key);
+          if (far >= 0 && far < a.n_pages) prefetch_l2(block_of(far, key), B::BYTES);
+        }
+        far_id = page_of((kt + kFar) * kTile + mine);
+      }
+      if (lane < 2 && kt + kFar < kt_end && far_id >= 0 && far_id < a.n_pages) prefetch_l2(block_of(far_id, (kt + kFar) * kTile + mine), B::BYTES);
+#pragma unroll
+      for (int i = 2; i > 0; --i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) { at[i][x] = at[i - 1][x]; live[i][x] = live[i - 1][x]; }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int key = kt * kTile + warp * 32 + x * 16;
-        at[0][x] = nullptr;
-        if (key < len) {
-          if (id[x] >= 0 && id[x] < a.n_pages) at[0][x] = head + id[x] * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES;
-          else if (lane == 0) report_range(a.status, kWhereTreePageQ4);
-        }
+        live[0][x] = key < len && id[x] >= 0 && id[x] < a.n_pages;
+        if (key < len && !live[0][x] && lane == 0) report_range(a.status, kWhereTreePageQ4);
+        at[0][x] = live[0][x] ? block_of(id[x], key) : cache.data;
       }
       ++kt;
-      if (kt < kt_end) lookup();
+#pragma unroll
+      for (int x = 0; x < 2; ++x) id[x] = page_of(kt * kTile + warp * 32 + x * 16);
+      far_id = page_of((kt + kFar) * kTile + mine);
       ++fk;
     }
-    const uint32_t back = is_k ? 0 : fk - 1 - fv;  // at most lead
+    const uint32_t back = is_k || fv >= n_tiles ? 0 : fk - 1 - fv;     // tiles back from the last K: at most lead
     if (!is_k) ++fv;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
+      // (always a load, of the cache's first block where there is nothing to read: a load under a condition would be waited for)
       const uint8_t* blk = back == 0 ? at[0][x] : back == 1 ? at[1][x] : at[2][x];
-      c.codes[x][0] = c.codes[x][1] = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);      // zeros
-      c.scales[x] = 0;
-      if (blk) {
-        const uint8_t* src = blk + (is_k ? k_at : v_at);
-        c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(src));
-        if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(src + (is_k ? K8 : V8)));
-        c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk + (is_k ? ks_at : vs_at)));
-      }
+      c.live[x] = back == 0 ? live[0][x] : back == 1 ? live[1][x] : live[2][x];
+      const uint8_t* src = blk + (is_k ? k_at : v_at);
+      c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(src));
+      if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(src + (is_k ? K8 : V8)));
+      c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk + (is_k ? ks_at : vs_at)));
     }
   };
   CodedRun c[AHEAD + 1];
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
-    if (ok) fetch(c[i]);
+  for (int i = 0; i <= AHEAD; ++i) c[i] = CodedRun{};
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(c[i]);
   uint32_t slot = 0, lap = 0;
-  for (uint32_t i0 = 0; i0 < 2 * n_tiles && ok; i0 += AHEAD + 1) {
+  for (uint32_t i0 = 0; i0 < 2 * n_tiles; i0 += AHEAD + 1) {
 #pragma unroll
     for (int i = 0; i <= AHEAD; ++i) {
-      if (i0 + i >= 2 * n_tiles || !ok) break;
       fetch(c[(i + AHEAD) % (AHEAD + 1)]);
-      if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
-      if (!ok) break;
+      if (i0 + i < 2 * n_tiles) {
+        if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
+        if (!ok) return;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int y = 0; y < RUNS; ++y) {
-          const int r = warp * 32 + x * 16 + token + 8 * y;
-          const uint32_t byte = RUNS == 2 ? c[i].scales[x] >> (8 * y) & 0xffu : c[i].scales[x] >> (token & 8) & 0xffu;
-          decode_run<D>(c[i].codes[x][y], byte, ring + slot * P::SLOT + (r >> 3) * P::GROUP + (r & 7) * 128, group * 4, r & 7);
-        }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_FULL + slot));
-      if (++slot == P::SLOTS) { slot = 0; ++lap; }
+          for (int y = 0; y < RUNS; ++y) {
+            const int r = warp * 32 + x * 16 + token + 8 * y;
+            const uint32_t byte = RUNS == 2 ? c[i].scales[x] >> (8 * y) & 0xffu : c[i].scales[x] >> (token & 8) & 0xffu;
+            uint4 codes = c[i].codes[x][y];
+            if (!c[i].live[x]) codes = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+            decode_run<D>(codes, byte, ring + slot * P::SLOT + (r >> 3) * P::GROUP + (r & 7) * 128, group * 4, r & 7);
+          }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(P::BAR_FULL + slot));
+        if (++slot == P::SLOTS) { slot = 0; ++lap; }
+      }
     }
   }
 }

@@ -108,7 +108,8 @@ struct Plan {
   static constexpr int TAG_OFF = RUN_OFF + 3 * 8 + 4 * 4;                             // int [8]
   static constexpr int EX_OFF = (TAG_OFF + 8 * 4 + 15) / 16 * 16;                     // narrow: float2 [8][16]; tall: float [2][128]
   static constexpr int REF_OFF = EX_OFF + 1024;                                       // tall: float [128]
-  static constexpr int TOTAL = REF_OFF + 512;
+  static constexpr int PROGRESS_OFF = REF_OFF + 512;                                  // 4-bit cache: int
+  static constexpr int TOTAL = PROGRESS_OFF + 16;
   // TMEM columns: S 128 each; O: wide behind two S, tall behind three
   static constexpr int S_COL = 0, O_COL = 256, O_STEP = D, TALL_O_COL = 384;
 };
@@ -1070,16 +1071,15 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
 
 // Form for a 4-bit cache: what the producer is otherwise.  Four warps take 32 keys of each tile, K or V, in the ring's order:
 // codes and scales from global memory (a lane a run of 32 elements of a token's head, which has one scale; eight neighbouring
-// lanes eight tokens, so that their 16-byte stores go to different banks), two loads ahead of the one that is being decoded,
+// lanes eight tokens, so that their 16-byte stores go to different banks), a tile ahead of the one that is being decoded,
 // bf16 values into the tile's swizzled rows.  4 loads of 16 bytes, 2 of scales and 32 stores of 16 bytes a lane and tile; 7
 // integer and 4 packed multiply-add instructions for 8 elements (see q4_attn.cu): 450 instructions a warp and tile in all, of
 // the 1000 to 1100 cycles that its products and its exponentials take.
-struct CodedRun {                  // a lane's part of 32 keys: of two blocks, D / 64 runs each
+struct Coded {                     // a lane's part of 32 keys: of two blocks, D / 64 runs each, and their scales
   uint4 codes[2][2];
   uint32_t scales[2];
-  bool live[2];                    // else there is no such page, or no key: the values are zeros
 };
-__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) { asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory"); }
+constexpr int kFar = 6;            // tiles that are brought into L2 ahead of the decoders
 template <int D>
 __device__ __forceinline__ void decode_run(const uint4& c, uint32_t byte, uint32_t row_at, int piece0, int r7) {
   const uint32_t sb = (byte << 4 | byte << 20) + 0x35803580u;
@@ -1104,35 +1104,44 @@ template <int D>
 __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles, uint32_t lead) {
   using P = Plan<D>;
   using B = Block<D>;
-  constexpr int RUNS = D / 64, AHEAD = 2, kFar = 5;       // runs of a lane and block; loads under way; tiles prefetched
+  constexpr int RUNS = D / 64;                     // of a lane and block
   const uint32_t ring = smem_u32(smem) + P::RING_OFF;
   auto bar = [&](int which) { return bars + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  volatile int* progress = reinterpret_cast<int*>(smem + P::PROGRESS_OFF);
   const int warp = (int)(threadIdx.x >> 5) - kWarps, lane = threadIdx.x & 31;
   const int token = D == 128 ? lane & 7 : lane & 15, group = D == 128 ? lane >> 3 : lane >> 4;      // and token + 8
   // of this lane's runs in a block, and of their scales (tokens i and i + 8 have theirs side by side)
   const int k_at = B::k_word(token, group * 4), v_at = B::v_word(token, group * 4), ks_at = B::k_scale(token & 7, group), vs_at = B::v_scale(token & 7, group);
   constexpr int K8 = B::k_word(8, 0), V8 = B::v_word(8, 0) - B::v_word(0, 0);
-  // ---- fetching.  (A unit's first tile is waited for with two loads fetched but not decoded: with more, four units of one tile
-  // each would wait for one another.  Two loads cover the latency of L2, and that of HBM is covered by prefetches into L2 a few
-  // tiles ahead.)
+  // this lane's rows in a tile: warp * 32 + token, and 8 (16, 24) rows further
+  const uint32_t row_at = ring + (warp * 4 + (token >> 3)) * P::GROUP + (token & 7) * 128;
+  // ---- fetching: K of the next tile and V of the one `lead` before it.  (A unit's first tile is waited for with one such pair
+  // fetched but not decoded: with more, four units of one tile each would wait for one another.)
   const uint8_t* at[3][2];                         // blocks of the last tiles whose K was fetched
-  bool live[3][2];
 #pragma unroll
-  for (int i = 0; i < 3; ++i)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) { at[i][x] = cache.data; live[i][x] = false; }
-  int seq = 0, kt = 0, kt_end = 0, len = 0, id[2] = {0, 0}, far_id = 0;
+  for (int i = 0; i < 3; ++i) at[i][0] = at[i][1] = cache.data;
+  int seq = 0, kt = 0, kt_end = 0, len = 0, id[2] = {0, 0};
   const int32_t* row = nullptr;
   const uint8_t* head = nullptr;
-  uint32_t fk = 0, fv = 0;                         // tiles whose K, V have been fetched
   bool ok = true;
-  auto page_of = [&](int key) { return key < len ? row[key >> a.page_log2] : -1; };
-  auto block_of = [&](int page, int key) { return head + page * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES; };
-  auto fetch = [&](CodedRun& c) {
-    const bool is_k = fk < n_tiles && fk - fv <= lead;
-    if (is_k) {
-      const int mine = warp * 32 + (lane & 1) * 16;
+  auto lookup = [&] {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int key = kt * kTile + warp * 32 + x * 16;
+      id[x] = key < len ? row[key >> a.page_log2] : -1;
+    }
+  };
+  auto load = [&](Coded& c, const uint8_t* (&blk)[2], int code_at, int eight, int scale_at) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(blk[x] + code_at));
+      if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(blk[x] + code_at + eight));
+      c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk[x] + scale_at));
+    }
+  };
+  auto fetch = [&](uint32_t j, Coded& k, Coded& v) {
+    if (j < n_tiles) {
       if (kt == kt_end) {
         const int e = seq % kUnitRing;
         ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
@@ -1143,75 +1152,92 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
         ++seq;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) id[x] = page_of(kt * kTile + warp * 32 + x * 16);
-        // this warp's blocks of the tiles up to kFar ahead, a lane a block
-        const int t = kt + 1 + (lane >> 1), key = t * kTile + mine;
-        if (t < min(kt + kFar, kt_end)) {
-          const int far = page_of(key);
-          if (far >= 0 && far < a.n_pages) prefetch_l2(block_of(far, key), B::BYTES);
-        }
-        far_id = page_of((kt + kFar) * kTile + mine);
+        lookup();
       }
-      if (lane < 2 && kt + kFar < kt_end && far_id >= 0 && far_id < a.n_pages) prefetch_l2(block_of(far_id, (kt + kFar) * kTile + mine), B::BYTES);
+      if (warp == 0 && lane == 0) *progress = (int)j;
 #pragma unroll
-      for (int i = 2; i > 0; --i)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) { at[i][x] = at[i - 1][x]; live[i][x] = live[i - 1][x]; }
+      for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        // (no such page, or no key: any block will do, all that is stored is finite.  A load under a condition would be waited for.)
         const int key = kt * kTile + warp * 32 + x * 16;
-        live[0][x] = key < len && id[x] >= 0 && id[x] < a.n_pages;
-        if (key < len && !live[0][x] && lane == 0) report_range(a.status, kWhereTreePageQ4);
-        at[0][x] = live[0][x] ? block_of(id[x], key) : cache.data;
+        const bool there = id[x] >= 0 && id[x] < a.n_pages;
+        at[0][x] = there ? head + id[x] * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES : cache.data;
+        if (!there && key < len && lane == 0) report_range(a.status, kWhereTreePageQ4);
       }
       ++kt;
+      lookup();
+    } else {
 #pragma unroll
-      for (int x = 0; x < 2; ++x) id[x] = page_of(kt * kTile + warp * 32 + x * 16);
-      far_id = page_of((kt + kFar) * kTile + mine);
-      ++fk;
+      for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
     }
-    const uint32_t back = is_k || fv >= n_tiles ? 0 : fk - 1 - fv;     // tiles back from the last K: at most lead
-    if (!is_k) ++fv;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      // (always a load, of the cache's first block where there is nothing to read: a load under a condition would be waited for)
-      const uint8_t* blk = back == 0 ? at[0][x] : back == 1 ? at[1][x] : at[2][x];
-      c.live[x] = back == 0 ? live[0][x] : back == 1 ? live[1][x] : live[2][x];
-      const uint8_t* src = blk + (is_k ? k_at : v_at);
-      c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(src));
-      if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(src + (is_k ? K8 : V8)));
-      c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk + (is_k ? ks_at : vs_at)));
-    }
+    load(k, at[0], k_at, K8, ks_at);
+    if (lead == 2) load(v, at[2], v_at, V8, vs_at);
+    else load(v, at[1], v_at, V8, vs_at);
   };
-  CodedRun c[AHEAD + 1];
-#pragma unroll
-  for (int i = 0; i <= AHEAD; ++i) c[i] = CodedRun{};
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fetch(c[i]);
   uint32_t slot = 0, lap = 0;
-  for (uint32_t i0 = 0; i0 < 2 * n_tiles; i0 += AHEAD + 1) {
+  auto decode_tile = [&](const Coded& c) {         // into the next slot
+    if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
+    if (!ok) return;
+    const uint32_t to = row_at + slot * P::SLOT;
 #pragma unroll
-    for (int i = 0; i <= AHEAD; ++i) {
-      fetch(c[(i + AHEAD) % (AHEAD + 1)]);
-      if (i0 + i < 2 * n_tiles) {
-        if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
-        if (!ok) return;
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int y = 0; y < RUNS; ++y) {
-            const int r = warp * 32 + x * 16 + token + 8 * y;
-            const uint32_t byte = RUNS == 2 ? c[i].scales[x] >> (8 * y) & 0xffu : c[i].scales[x] >> (token & 8) & 0xffu;
-            uint4 codes = c[i].codes[x][y];
-            if (!c[i].live[x]) codes = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
-            decode_run<D>(codes, byte, ring + slot * P::SLOT + (r >> 3) * P::GROUP + (r & 7) * 128, group * 4, r & 7);
-          }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(P::BAR_FULL + slot));
-        if (++slot == P::SLOTS) { slot = 0; ++lap; }
+      for (int y = 0; y < RUNS; ++y) {
+        const uint32_t byte = RUNS == 2 ? c.scales[x] >> (8 * y) & 0xffu : c.scales[x] >> (token & 8) & 0xffu;
+        decode_run<D>(c.codes[x][y], byte, to + (2 * x + y) * P::GROUP, group * 4, token & 7);
       }
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(P::BAR_FULL + slot));
+    if (++slot == P::SLOTS) { slot = 0; ++lap; }
+  };
+  Coded k[2], v[2];
+  if (n_tiles > 0) fetch(0, k[0], v[0]);
+  for (uint32_t j0 = 0; j0 < n_tiles + lead; j0 += 2) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t j = j0 + i;
+      fetch(j + 1, k[i ^ 1], v[i ^ 1]);
+      if (!ok) return;
+      if (j < n_tiles) decode_tile(k[i]);
+      if (ok && j >= lead && j < n_tiles + lead) decode_tile(v[i]);
+    }
+  }
+}
+
+// Brings the blocks of the tiles up to kFar ahead of the decoders into L2: their loads then cover its latency, not that of HBM.
+// One warp, a lane a block.
+template <int D>
+__device__ __noinline__ void prefetch_blocks(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles) {
+  using P = Plan<D>;
+  auto bar = [&](int which) { return bars + which * 8; };
+  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
+  volatile int* progress = reinterpret_cast<int*>(smem + P::PROGRESS_OFF);
+  const int lane = threadIdx.x & 31;
+  int seq = 0, kt = 0, kt_end = 0, len = 0, g = 0, b = 0;
+  for (uint32_t j = 0; j < n_tiles; ++j) {
+    if (kt == kt_end) {
+      const int e = seq % kUnitRing;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 52))) return;
+      const Unit& u = units[e];
+      kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = u.len; g = u.g; b = u.b;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+      ++seq;
+    }
+    const int key = kt * kTile + lane * 16;
+    if (lane < kTile / 16 && key < len) {
+      const int id = a.table[(size_t)b * a.max_pages + (key >> a.page_log2)];
+      if (id >= 0 && id < a.n_pages)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(cache.data + g * cache.s_head + id * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * Block<D>::BYTES),
+                     "r"(Block<D>::BYTES) : "memory");
+    }
+    __syncwarp();
+    ++kt;
+    while ((int)j + 1 > *progress + kFar) {        // ends: the decoders go on, or the abort flag is raised
+      if (*ab.flag) return;
+      __nanosleep(200);
     }
   }
 }
@@ -1245,6 +1271,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
   if (!Q4 && warp == kProducer && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
   if (threadIdx.x == 0) {
     *abort_flag = *redo = 0;
+    *reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF) = 0;
     for (int i = 0; i < 8; ++i) bad_tag[i] = 0;
   }
   wait_for_previous();
@@ -1362,7 +1389,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
     }
     for (int e = 0; e < kUnitRing; ++e) {
       mbar_init(bar(P::BAR_UNIT + e), 1);
-      mbar_init(bar(P::BAR_UFREE + e), (narrow ? 9 : wide ? 11 : 10) + (Q4 ? kDecoders - 1 : 0));
+      mbar_init(bar(P::BAR_UFREE + e), (narrow ? 9 : wide ? 11 : 10) + (Q4 ? kDecoders : 0));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   };
@@ -1461,7 +1488,8 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
       }
     } else if (Q4 && (warp == kProducer || warp >= kWarps)) {
       if constexpr (Q4) {
-        if (warp != kProducer) decode<D>(a, cache, smem, bars, ab, n_tiles_cta, lead);
+        if (warp == kProducer) prefetch_blocks<D>(a, cache, smem, bars, ab, n_tiles_cta);
+        else decode<D>(a, cache, smem, bars, ab, n_tiles_cta, lead);
       }
     } else if (!Q4 && warp == kProducer) {
       // ------------------------------------------------------------ K and V tiles
@@ -1549,6 +1577,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
     // Tall, and a reference did not serve: the run once more, wide, with barriers of its own (some of the first walk's end in
     // odd phases).  All products of the first walk are in O, which has been read.
     if (threadIdx.x < 8) bad_tag[threadIdx.x] = 0;
+    if (threadIdx.x == 8) *reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF) = 0;
     bars += P::BARS * 8;
     wide = true;
     __syncthreads();

@@ -1116,8 +1116,9 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
   constexpr int K8 = B::k_word(8, 0), V8 = B::v_word(8, 0) - B::v_word(0, 0);
   // this lane's rows in a tile: warp * 32 + token, and 8 (16, 24) rows further
   const uint32_t row_at = ring + (warp * 4 + (token >> 3)) * P::GROUP + (token & 7) * 128;
-  // ---- fetching: K of the next tile and V of the one `lead` before it.  (A unit's first tile is waited for with one such pair
-  // fetched but not decoded: with more, four units of one tile each would wait for one another.)
+  // ---- fetching: K of the next tile, while V of an earlier one is decoded, and the other way round.  (One set of registers for
+  // each: with two they were spilled, and a load that is spilled is waited for.  A unit's first tile is waited for with no more
+  // than the K before it decoded ahead of its V: further ahead, four units of one tile each would wait for one another.)
   const uint8_t* at[3][2];                         // blocks of the last tiles whose K was fetched
 #pragma unroll
   for (int i = 0; i < 3; ++i) at[i][0] = at[i][1] = cache.data;
@@ -1140,44 +1141,37 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
       c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk[x] + scale_at));
     }
   };
-  auto fetch = [&](uint32_t j, Coded& k, Coded& v) {
-    if (j < n_tiles) {
-      if (kt == kt_end) {
-        const int e = seq % kUnitRing;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
-        const Unit& u = units[e];
-        kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = ok ? u.len : 0;
-        row = a.table + (size_t)u.b * a.max_pages;
-        head = cache.data + u.g * cache.s_head;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
-        ++seq;
-        lookup();
-      }
-      if (warp == 0 && lane == 0) *progress = (int)j;
+  auto next_tile = [&](uint32_t j) {
 #pragma unroll
-      for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        // (no such page, or no key: any block will do, all that is stored is finite.  A load under a condition would be waited for.)
-        const int key = kt * kTile + warp * 32 + x * 16;
-        const bool there = id[x] >= 0 && id[x] < a.n_pages;
-        at[0][x] = there ? head + id[x] * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES : cache.data;
-        if (!there && key < len && lane == 0) report_range(a.status, kWhereTreePageQ4);
-      }
-      ++kt;
+    for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
+    if (j >= n_tiles) return;
+    if (kt == kt_end) {
+      const int e = seq % kUnitRing;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
+      const Unit& u = units[e];
+      kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = ok ? u.len : 0;
+      row = a.table + (size_t)u.b * a.max_pages;
+      head = cache.data + u.g * cache.s_head;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
+      ++seq;
       lookup();
-    } else {
-#pragma unroll
-      for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
     }
-    load(k, at[0], k_at, K8, ks_at);
-    if (lead == 2) load(v, at[2], v_at, V8, vs_at);
-    else load(v, at[1], v_at, V8, vs_at);
+    if (warp == 0 && lane == 0) *progress = (int)j;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      // (no such page, or no key: any block will do, all that is stored is finite.  A load under a condition would be waited for.)
+      const int key = kt * kTile + warp * 32 + x * 16;
+      const bool there = id[x] >= 0 && id[x] < a.n_pages;
+      at[0][x] = there ? head + id[x] * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES : cache.data;
+      if (!there && key < len && lane == 0) report_range(a.status, kWhereTreePageQ4);
+    }
+    ++kt;
+    lookup();
   };
   uint32_t slot = 0, lap = 0;
   auto decode_tile = [&](const Coded& c) {         // into the next slot
-    if (ok && lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
+    if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
     if (!ok) return;
     const uint32_t to = row_at + slot * P::SLOT;
 #pragma unroll
@@ -1192,17 +1186,19 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
     if (lane == 0) mbar_arrive(bar(P::BAR_FULL + slot));
     if (++slot == P::SLOTS) { slot = 0; ++lap; }
   };
-  Coded k[2], v[2];
-  if (n_tiles > 0) fetch(0, k[0], v[0]);
-  for (uint32_t j0 = 0; j0 < n_tiles + lead; j0 += 2) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t j = j0 + i;
-      fetch(j + 1, k[i ^ 1], v[i ^ 1]);
+  Coded k{}, v{};
+  next_tile(0);
+  load(k, at[0], k_at, K8, ks_at);
+  for (uint32_t j = 0; j < n_tiles + lead && ok; ++j) {
+    if (j < n_tiles) {
+      decode_tile(k);
       if (!ok) return;
-      if (j < n_tiles) decode_tile(k[i]);
-      if (ok && j >= lead && j < n_tiles + lead) decode_tile(v[i]);
     }
+    next_tile(j + 1);
+    load(k, at[0], k_at, K8, ks_at);
+    if (j >= lead) decode_tile(v);
+    if (lead == 2) load(v, at[2], v_at, V8, vs_at);
+    else load(v, at[1], v_at, V8, vs_at);
   }
 }
 

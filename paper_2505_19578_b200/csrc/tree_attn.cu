@@ -1170,9 +1170,9 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
     lookup();
   };
   uint32_t slot = 0, lap = 0;
-  auto decode_tile = [&](const Coded& c) {         // into the next slot
+  auto decode_tile = [&](const Coded& c) {         // into the next slot; which one, or -1
     if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
-    if (!ok) return;
+    if (!ok) return -1;
     const uint32_t to = row_at + slot * P::SLOT;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -1181,24 +1181,28 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
         const uint32_t byte = RUNS == 2 ? c.scales[x] >> (8 * y) & 0xffu : c.scales[x] >> (token & 8) & 0xffu;
         decode_run<D>(c.codes[x][y], byte, to + (2 * x + y) * P::GROUP, group * 4, token & 7);
       }
-    fence_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar(P::BAR_FULL + slot));
+    const int used = (int)slot;
     if (++slot == P::SLOTS) { slot = 0; ++lap; }
+    return used;
   };
   Coded k{}, v{};
   next_tile(0);
   load(k, at[0], k_at, K8, ks_at);
   for (uint32_t j = 0; j < n_tiles + lead && ok; ++j) {
+    int k_slot = -1, v_slot = -1;
     if (j < n_tiles) {
-      decode_tile(k);
+      k_slot = decode_tile(k);
       if (!ok) return;
     }
     next_tile(j + 1);
     load(k, at[0], k_at, K8, ks_at);
-    if (j >= lead) decode_tile(v);
+    if (j >= lead) v_slot = decode_tile(v);
     if (lead == 2) load(v, at[2], v_at, V8, vs_at);
     else load(v, at[1], v_at, V8, vs_at);
+    fence_async_smem();                            // one for both (a fence is 200 cycles)
+    __syncwarp();
+    if (lane == 0 && k_slot >= 0) mbar_arrive(bar(P::BAR_FULL + k_slot));
+    if (lane == 0 && v_slot >= 0) mbar_arrive(bar(P::BAR_FULL + v_slot));
   }
 }
 

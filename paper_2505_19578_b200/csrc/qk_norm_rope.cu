@@ -169,10 +169,17 @@ __device__ __forceinline__ uint32_t piece_codes(const float2 (&v)[4], float s, f
   return ((pair[3] * 16 + pair[2]) * 16 + pair[1]) * 16 + pair[0];
 }
 
-// The codes of a pass of keys in 64 bits, from its inputs.  Out of line and rare.  Whole warps.
+__device__ __forceinline__ double quotient(double x, double y, double r) {
+  const double q = x * r;
+  return fma(fma(-q, y, x), r, q);
+}
+// The codes of a pass of keys in 64 bits, from its inputs.  Out of line and rare, but a step of a few tokens waits for it: sines
+// and cosines are shared by the warp's lanes as in fp32, and nothing is divided.  Whole warps.
 template <int D>
 __device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0, uint4 in1) {
-  const Lane<D> ln(a, threadIdx.x & 31);
+  constexpr uint32_t kAll = 0xffffffffu;
+  const int lane = threadIdx.x & 31;
+  const Lane<D> ln(a, lane);
   double y[2][8];
   {
     float2 x0[4], x1[4];
@@ -182,12 +189,13 @@ __device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0,
     for (int i = 0; i < 4; ++i) { y[0][2 * i] = x0[i].x; y[0][2 * i + 1] = x0[i].y; y[1][2 * i] = x1[i].x; y[1][2 * i + 1] = x1[i].y; }
   }
   if (a.k_weight) {
-    double ss = 0;
+    double ss[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss += y[0][i] * y[0][i] + y[1][i] * y[1][i];
+    for (int i = 0; i < 4; ++i) ss[i] = fma(y[0][i], y[0][i], fma(y[0][4 + i], y[0][4 + i], fma(y[1][i], y[1][i], y[1][4 + i] * y[1][4 + i])));
+    double sum = (ss[0] + ss[1]) + (ss[2] + ss[3]);
 #pragma unroll
-    for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const double inv = 1.0 / sqrt(ss * (1.0 / D) + (double)a.eps);
+    for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+    const double inv = rsqrt(sum * (1.0 / D) + (double)a.eps);
     float2 w0[4], w1[4];
     unpack8(__ldg(reinterpret_cast<const uint4*>(a.k_weight + ln.c0 * 8)), w0);
     unpack8(__ldg(reinterpret_cast<const uint4*>(a.k_weight + ln.c1 * 8)), w1);
@@ -197,22 +205,24 @@ __device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0,
       y[1][2 * i] *= inv * w1[i].x; y[1][2 * i + 1] *= inv * w1[i].y;
     }
   }
-  auto turn = [&](double& u, double& v, int pair) {
-    const uint64_t turns = a.phase[pair] * (uint64_t)(int64_t)pos;
-    double c, s;
-    sincospi((double)(int64_t)turns * 1.0842021724855044e-19 /* 2^-63: half turns */, &s, &c);
-    const double w = u * c - v * s;
-    v = v * c + u * s;
-    u = w;
-  };
-  if (a.interleaved) {
+  if (a.rot > 0) {
+    double c[2], s[2];                             // of pairs 2 lane, 2 lane + 1
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-      if (x == 0 ? ln.turn0 : ln.turn1)
-        for (int i = 0; i < 4; ++i) turn(y[x][2 * i], y[x][2 * i + 1], 4 * (x == 0 ? ln.c0 : ln.c1) + i);
-  } else if (ln.turn0) {
+    for (int i = 0; i < 2; ++i) {
+      const uint64_t f = 2 * lane + i < a.rot / 2 ? a.phase[2 * lane + i] : 0;
+      sincospi((double)(int64_t)(f * (uint64_t)(int64_t)pos) * 1.0842021724855044e-19 /* 2^-63: half turns */, &s[i], &c[i]);
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(y[0][i], y[1][i], 8 * ln.c0 + i);
+    for (int e = 0; e < 8; ++e) {
+      const int from = ((e < 4 ? ln.from0 : ln.from1) + ((e & 3) >> 1)) & 31;
+      const double ce = __shfl_sync(kAll, c[e & 1], from), se = __shfl_sync(kAll, s[e & 1], from);
+      if (!(e < 4 ? ln.turn0 : ln.turn1)) continue;
+      double& u = a.interleaved ? y[e >> 2][2 * (e & 3)] : y[0][e];
+      double& v = a.interleaved ? y[e >> 2][2 * (e & 3) + 1] : y[1][e];
+      const double w = u * ce - v * se;
+      v = v * ce + u * se;
+      u = w;
+    }
   }
   double m[2];
 #pragma unroll
@@ -226,15 +236,14 @@ __device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0,
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     // the same rounding of a / 7 as scale_bits, on the bits of a double; clamped first, so that the result is one of fp32
-    const double f = fmin(fmax(m[x] / 7.0, 9.5367431640625e-07), 3840.0);
+    const double f = quotient(fmin(fmax(m[x], 7 * 9.5367431640625e-07), 7 * 3840.0), 7.0, 1.0 / 7);
     const unsigned long long u = (unsigned long long)__double_as_longlong(f), odd = u >> 49 & 1;
-    const double s = __longlong_as_double((long long)((u + ((1ull << 48) - 1) + odd) & ~((1ull << 49) - 1)));
+    const double s = __longlong_as_double((long long)((u + ((1ull << 48) - 1) + odd) & ~((1ull << 49) - 1))), r = 1.0 / s;
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      double t = y[x][i] / s;
-      t = t == t ? fmin(fmax(t, -7.0), 7.0) : 0.0;
-      w |= (uint32_t)((int)rint(t) + 8) << (4 * (i >> 1) + 16 * (i & 1));
+      const double z = y[x][i], t = rint(quotient(z == z ? fmin(fmax(z, -7 * s), 7 * s) : 0.0, s, r));
+      w |= (uint32_t)(__double2int_rn(t) + 8) << (4 * (i >> 1) + 16 * (i & 1));
     }
     const uint32_t byte = scale_byte(clamp_scale(__float_as_uint((float)s)));
     if (x == 0) { out.word0 = w; out.scale0 = byte; } else { out.word1 = w; out.scale1 = byte; }
@@ -242,10 +251,10 @@ __device__ __noinline__ Codes exact_codes(const RopeArgs& a, int pos, uint4 in0,
   return out;
 }
 
-// Codes of a pass of keys (its pieces x, y in fp32, each off by 2e-6 `pair` at most, any of the head by 2e-6 `top`) or values
-// (pair, top: 0).  Whole warps.
+// Codes of a pass of keys (its pieces x, y in fp32, each off by `err` at most, any of the head by `top_err`) or values (0, 0).
+// Whole warps.
 template <int D>
-__device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, bool is_v, bool normed, float pair, float top, int pos, uint4 in0, uint4 in1,
+__device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, bool is_v, bool normed, float err, float top_err, int pos, uint4 in0, uint4 in1,
                                           const float2 (&x)[4], const float2 (&y)[4]) {
   float a0 = 0.f, a1 = 0.f;
 #pragma unroll
@@ -256,7 +265,7 @@ __device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, 
   group_max<D>(a, ln, a0, a1);
   constexpr float kMost = 7.f * 3840.f;            // 7 times the largest scale
   Codes c;
-  bool unsure = !(top < 1e38f);
+  bool unsure = !(top_err < 1e30f);
   if (__any_sync(0xffffffffu, !(a0 <= kMost && a1 <= kMost))) {
     // something is not finite, or beyond the largest scale: a NaN counts as zero, the rest as 7 times the scale at most
     float2 u[4], v[4];
@@ -273,7 +282,7 @@ __device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, 
     float far = 0.f;
     const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
     c = {piece_codes(u, __uint_as_float(s0), far), piece_codes(v, __uint_as_float(s1), far), scale_byte(s0), scale_byte(s1)};
-    unsure |= top > 0.f;
+    unsure |= top_err > 0.f;
   } else {
     const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
     const float f0 = __uint_as_float(s0), f1 = __uint_as_float(s1);
@@ -281,11 +290,10 @@ __device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, 
     c = {piece_codes(x, f0, far0), piece_codes(y, f1, far1), scale_byte(s0), scale_byte(s1)};
     if (!is_v) {
       // a border between two codes or two scales within the error
-      const float err = 2e-6f * pair, group_err = 2e-6f * top;
       if (normed || ln.turn0) unsure |= far0 >= 0.5f * f0 - err;
       if (normed || ln.turn1) unsure |= far1 >= 0.5f * f1 - err;
-      if (group_err > 0.f)
-        unsure |= scale_bits(a0 + group_err) != scale_bits(fmaxf(a0 - group_err, 0.f)) || scale_bits(a1 + group_err) != scale_bits(fmaxf(a1 - group_err, 0.f));
+      if (top_err > 0.f)
+        unsure |= scale_bits(a0 + top_err) != scale_bits(fmaxf(a0 - top_err, 0.f)) || scale_bits(a1 + top_err) != scale_bits(fmaxf(a1 - top_err, 0.f));
     }
   }
   if (!is_v && __any_sync(0xffffffffu, unsure)) c = exact_codes<D>(a, pos, in0, in1);
@@ -299,7 +307,7 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
                                             const float (&cs)[8], const float (&sn)[8]) {
   Codes codes;
   float2 x[4], y[4];
-  float pair = 0.f, top = 0.f;
+  float err = 0.f, top_err = 0.f;
   if (!is_v || Q4) {                               // uniform over the warp, as is all that depends on the kind
     unpack8(in0, x);
     unpack8(in1, y);
@@ -325,19 +333,20 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
       for (int i = 0; i < 4; ++i) { x[i] = __fmul2_rn(x[i], __fmul2_rn(inv, wx[i])); y[i] = __fmul2_rn(y[i], __fmul2_rn(inv, wy[i])); }
     }
     if (Q4 && !is_q && (weight || a.rot > 0)) {
-      // fp32: the norm is off by under 7.5e-7, relative (16 roundings of the sum of squares, halved by the root, its 2 ulp and
-      // the products), the angle by 1.9e-7, sine and cosine by 1.2e-7 and the rotation's two roundings by as much: 1.2e-6 of
-      // |a| + |b| for each pair
+      // fp32: the angle is off by 2^-26 of a turn, 1e-7, sine and cosine by 1.2e-7 and the rotation's two roundings by as much,
+      // 3.4e-7 of |a| + |b| for each pair; the norm by 7.5e-7, relative (16 roundings of the sum of squares, halved by the root,
+      // its 2 ulp and the products), 1.1e-6 with it
+      float pair = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 u = a.interleaved ? make_float2(fabsf(x[i].x) + fabsf(x[i].y), fabsf(y[i].x) + fabsf(y[i].y)) :
                                          make_float2(fabsf(x[i].x) + fabsf(y[i].x), fabsf(x[i].y) + fabsf(y[i].y));
         pair = fmaxf(fmaxf(pair, u.x), u.y);
       }
-      top = pair;
+      err = top_err = pair * (weight ? 1.5e-6f : 6e-7f);
 #pragma unroll
-      for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (odd) top = CUDART_INF_F;
+      for (int o = Lane<D>::LPH / 2; o > 0; o >>= 1) top_err = fmaxf(top_err, __shfl_xor_sync(0xffffffffu, top_err, o));
+      if (odd) top_err = CUDART_INF_F;
     }
     if (ln.turn0 || ln.turn1) {
       if (a.interleaved) {
@@ -354,7 +363,7 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
       }
     }
   }
-  if (Q4 && !is_q) codes = codes_of<D>(a, ln, is_v, !is_v && a.k_weight != nullptr, pair, top, pos, in0, in1, x, y);
+  if (Q4 && !is_q) codes = codes_of<D>(a, ln, is_v, !is_v && a.k_weight != nullptr, err, top_err, pos, in0, in1, x, y);
   if (!is_v) {
     in0 = pack8(x);
     in1 = pack8(y);

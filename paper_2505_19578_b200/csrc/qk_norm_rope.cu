@@ -535,16 +535,19 @@ template <int D, bool Q4>
 cudaError_t launch(RopeArgs& a, cudaStream_t s) {
   // From an item for every other of the device's warps on, the streaming kernel (36 heads, with it and with the other one:
   // 250 rows 4.8 and 4.2 us, 500 rows 5.5 and 7.0, 1000 rows 7.6 and 8.8; 131072 rows of 48 heads, head-major and cached: 662
-  // and 688).
+  // and 688).  The 4-bit form from four items a warp on (36 heads, written and read back: 1000 rows 19.5 us with it and 15.6 with
+  // the other one, 3000 rows 32.3 and 30.1, 16384 rows 109 and 131).
   const int passes = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW + 2 * ((a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW);
   const long long items = (long long)a.tokens * ((passes + kStreamRun - 1) / kStreamRun);
-  if (items >= 148 * kStreamWarps / 2) {
+  if (items >= (Q4 ? 148 * kStreamWarps * 4 : 148 * kStreamWarps / 2)) {
     constexpr int smem = kStreamWarps * kStreamStages * kStreamItem;
     const cudaError_t e = cudaFuncSetAttribute(qk_norm_rope_stream_kernel<D, Q4>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     return launch_dependent(qk_norm_rope_stream_kernel<D, Q4>, dim3(148), dim3(kStreamWarps * 32), smem, s, a);
   }
-  const long long splits = (148ll * 32 + a.tokens - 1) / a.tokens;             // warps to fill the device
+  // warps to fill the device; of the 4-bit form's (156 registers) 12 fit an SM, and more would come in a second wave (1000 rows
+  // of 36 heads, written and read back: 15.6 us so, 18.5 with 32)
+  const long long splits = (148ll * (Q4 ? 12 : 32) + a.tokens - 1) / a.tokens;
   a.splits = (int)(splits > passes ? passes : splits);
   const long long warps = (long long)a.tokens * a.splits;
   return launch_dependent(qk_norm_rope_kernel<D, Q4>, dim3((unsigned)((warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32))), dim3(kRopeThreads), 0, s, a);

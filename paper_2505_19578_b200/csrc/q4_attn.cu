@@ -28,7 +28,7 @@
 namespace sp {
 namespace {
 
-constexpr int kOwnSteps = 2;                     // steps of a unit besides those of its keys
+constexpr int kOwnSteps = 4;                     // steps of a unit besides those of its keys
 constexpr int kLeastSteps = 4;                   // of a run, while there are warps to spare
 
 template <int D, int NT>

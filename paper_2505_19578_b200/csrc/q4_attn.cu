@@ -680,11 +680,14 @@ cudaError_t launch(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arriv
 
 template <int D>
 cudaError_t launch_rows(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s, int* launched) {
-  // Rows of a request if all have as many: more than 16 make tiles of 128 for the tensor cores' own memory.  (Requests of more
-  // rows than a form's units have are several units, which is right for any lengths.)
+  // Rows of a request if all have as many.  More than 32 make tiles of 128 for the tensor cores' own memory; up to 32 are two
+  // units of 16 at most, which read the cache twice, from L2 the second time, but cost far less for each unit (with it and with
+  // the tiles: 256 chats with trees of 6, 24 rows, 229 and 349 us; 32 ragged requests with 28 rows 233 and 212; 32 rows over 131000
+  // keys 138 and 120.  In one unit of up to 32 rows: 273, 252, 160.)  Requests of more rows than a form's units have are
+  // several units, which is right for any lengths.
   const long long rows = ((long long)a.rows + a.n_req - 1) / a.n_req * a.group;
-  *launched = rows <= 16 ? 1 : 2;
-  return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : rows <= 16 ? launch<D, 2>(a, c, ws, arrived, n_sm, s) : launch_tree_attn_q4_tall(a, c, ws, n_sm, s);
+  *launched = rows <= 32 ? 1 : 2;
+  return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : rows <= 32 ? launch<D, 2>(a, c, ws, arrived, n_sm, s) : launch_tree_attn_q4_tall(a, c, ws, n_sm, s);
 }
 
 }  // namespace

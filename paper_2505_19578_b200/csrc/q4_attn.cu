@@ -18,8 +18,13 @@
 // Codes to bf16, two at a time: 0x4300 | c is 128 + c; times s, minus 136 s: (c - 8) s, exactly, one rounding that rounds
 // nothing.  A shift, a mask-or and an FMA for two elements; V, whose pairs are of two tokens, one byte-permute more for 16.
 //
-// What bounds it: the cache's bytes, 2176 a block of 128-element heads: 94 cycles of an SM's share of the measured HBM rate,
-// in which its schedulers issue 376 instructions.
+// What bounds it: the cache's bytes are 2176 a block of 128-element heads, 94 cycles of an SM's share of the measured HBM rate.
+// A block takes 330 instructions of a warp, 170 of them on the integer pipe, which takes two cycles for each: 85 cycles of
+// the SM's four.  Measured 170 cycles (131000 keys, 8 KV heads, a token of 4 rows each: 45 us, 6 of them before the first and
+// 3 behind the last block; without turning codes into values 38).  Dequantisation is 112 of the integer instructions.  What was
+// tried against it: shifts as high products (slower: 47 us), fp16 instead of bf16 values (fewer masks, twice the multiply-adds, no
+// gain in a loop of nothing else), 15 warps of 128 registers (48), 7 (49).  Steps of one block: 58; the copies issued by the
+// warps themselves: 53; the parts joined by a second kernel: 51.
 #include <limits.h>
 
 #include "q4.cuh"
@@ -28,16 +33,19 @@
 namespace sp {
 namespace {
 
-constexpr int kOwnSteps = 4;                     // steps of a unit besides those of its keys
-constexpr int kLeastSteps = 4;                   // of a run, while there are warps to spare
+// Steps of a unit besides those of its keys, and least steps of a run while there are warps to spare.  (With 1, 2, 4, 6: 256 chats
+// 82.4, 78.4, 78.0, 79.5 us; 32 chats 24.8, 24.6, 23.2, 23.1; 2000 keys of 8 small heads 13.5, 12.3, 10.6, 10.6.  Runs of 1, 2, 4, 8 steps
+// and more, with 2 of a unit's own: 8 chats 17.6, 15.9, 16.1, 22.3.)
+constexpr int kOwnSteps = 4;
+constexpr int kLeastSteps = 4;
 
 template <int D, int NT>
 struct Plan {
   static constexpr int ROWS = 8 * NT;
-  static constexpr int WARPS = NT == 1 ? 11 : 7, THREADS = (WARPS + 1) * 32;      // that multiply; the producer is one more
+  static constexpr int WARPS = 11, THREADS = (WARPS + 1) * 32;                    // that multiply; the producer is one more (168 registers each)
   static constexpr int BLOCKS = 2, KEYS = 16 * BLOCKS;                            // of a step
   static constexpr int BLOCK = Block<D>::BYTES, BYTES = BLOCKS * BLOCK;
-  static constexpr int RING = (NT == 1 ? 3 : 4) * (D == 128 ? 1 : 2);             // steps
+  static constexpr int RING = (NT == 1 ? 3 : 2) * (D == 128 ? 1 : 2);             // steps
   static constexpr int WORDS = D / 32;           // words of codes that a lane takes of a key
   static constexpr int STRIDE = D + 4;           // of a part's rows, floats
   static constexpr int RING_OFF = 0, RING_BYTES = WARPS * RING * BYTES;
@@ -681,10 +689,11 @@ cudaError_t launch(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arriv
 template <int D>
 cudaError_t launch_rows(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s, int* launched) {
   // Rows of a request if all have as many.  More than 32 make tiles of 128 for the tensor cores' own memory; up to 32 are two
-  // units of 16 at most, which read the cache twice, from L2 the second time, but cost far less for each unit (with it and with
-  // the tiles: 256 chats with trees of 6, 24 rows, 229 and 349 us; 32 ragged requests with 28 rows 233 and 212; 32 rows over 131000
-  // keys 138 and 120.  In one unit of up to 32 rows: 273, 252, 160.)  Requests of more rows than a form's units have are
-  // several units, which is right for any lengths.
+  // units of 16 at most, which read the cache twice, from L2 the second time, but cost less for each unit (so, and with the
+  // tiles: 256 chats with 24 rows each 205 and 351 us, with 32 rows 244 and 352, with 48 rows as three units 316 and 354; 32 ragged
+  // requests with 28 rows 199 and 211; over 131000 keys 20 rows 116 and 120, 32 rows 120 and 120, 48 rows 164 and 122.  In one unit of up
+  // to 32 rows, of the registers of seven warps: 24 rows in chats 273, 28 ragged 252, 32 rows over 131000 keys 160).  Requests of more
+  // rows than a form's units have are several units, which is right for any lengths.
   const long long rows = ((long long)a.rows + a.n_req - 1) / a.n_req * a.group;
   *launched = rows <= 32 ? 1 : 2;
   return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : rows <= 32 ? launch<D, 2>(a, c, ws, arrived, n_sm, s) : launch_tree_attn_q4_tall(a, c, ws, n_sm, s);

@@ -1071,10 +1071,17 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
 
 // Form for a 4-bit cache: what the producer is otherwise.  Four warps take 32 keys of each tile, K or V, in the ring's order:
 // codes and scales from global memory (a lane a run of 32 elements of a token's head, which has one scale; eight neighbouring
-// lanes eight tokens, so that their 16-byte stores go to different banks), a tile ahead of the one that is being decoded,
-// bf16 values into the tile's swizzled rows.  4 loads of 16 bytes, 2 of scales and 32 stores of 16 bytes a lane and tile; 7
-// integer and 4 packed multiply-add instructions for 8 elements (see q4_attn.cu): 450 instructions a warp and tile in all, of
-// the 1000 to 1100 cycles that its products and its exponentials take.
+// lanes eight tokens, so that their 16-byte stores go to different banks), K of the next tile while V of an earlier one is
+// decoded, bf16 values into the tile's swizzled rows.  7 integer and 4 packed multiply-add instructions for 8 elements (see
+// q4_attn.cu), 32 stores of 16 bytes a lane and tile.
+//
+// It is the decoders that bound the tall form: a round (K of one tile, V of another) takes them 3100 to 3600 cycles, 1100 to
+// 1400 of them the decoding itself, the rest waits for the ring, a fence and the control of one warp that has three others on its
+// scheduler.  (32 ragged requests with trees of 16: 219 us; 181 if nothing is loaded or decoded, 172 over a bf16 cache with
+// four times the bytes.)  Measured on the way there: loads under a condition are waited for where they are issued (503 us);
+// registers that are spilled likewise (343 with two sets of them, 307 two tiles ahead); decoding by calls 272; a fence for
+// each of K and V 229.  The wide form is bound by its own chain (a tree of 64 over 131000 keys: 168 to 174 us, 153 if nothing is
+// decoded; as two tall units 236).
 struct Coded {                     // a lane's part of 32 keys: of two blocks, D / 64 runs each, and their scales
   uint4 codes[2][2];
   uint32_t scales[2];

@@ -23,8 +23,8 @@
 // the SM's four.  Measured 170 cycles (131000 keys, 8 KV heads, a token of 4 rows each: 45 us, 6 of them before the first and
 // 3 behind the last block; without turning codes into values 38).  Dequantisation is 112 of the integer instructions.  What was
 // tried against it: shifts as high products (slower: 47 us), fp16 instead of bf16 values (fewer masks, twice the multiply-adds, no
-// gain in a loop of nothing else), 15 warps of 128 registers (48), 7 (49).  Steps of one block: 58; the copies issued by the
-// warps themselves: 53; the parts joined by a second kernel: 51.
+// gain in a loop of nothing else), 15 warps of 128 registers (48), 7 (49).  Before that, steps of two blocks instead of one
+// brought 64 -> 59, the producer and the addition by the last CTA (instead of copies by each warp and a second kernel) 53 -> 45.
 #include <limits.h>
 
 #include "q4.cuh"

@@ -108,8 +108,10 @@ struct Plan {
   static constexpr int TAG_OFF = RUN_OFF + 3 * 8 + 4 * 4;                             // int [8]
   static constexpr int EX_OFF = (TAG_OFF + 8 * 4 + 15) / 16 * 16;                     // narrow: float2 [8][16]; tall: float [2][128]
   static constexpr int REF_OFF = EX_OFF + 1024;                                       // tall: float [128]
-  static constexpr int PROGRESS_OFF = REF_OFF + 512;                                  // 4-bit cache: int
-  static constexpr int TOTAL = PROGRESS_OFF + 16;
+  static constexpr int PROGRESS_OFF = REF_OFF + 512;                                  // 4-bit cache: int, tiles that were found; int [4], of which each decoder has fetched K
+  static constexpr int BLOCKS_OFF = PROGRESS_OFF + 32;                                // and addresses, half of a ring [8][8] of which the rest is at SCAN_OFF
+  static constexpr int TOTAL = BLOCKS_OFF + 256;
+  static_assert(2 * (kWarps + kDecoders) * 8 >= 256, "");
   // TMEM columns: S 128 each; O: wide behind two S, tall behind three
   static constexpr int S_COL = 0, O_COL = 256, O_STEP = D, TALL_O_COL = 384;
 };
@@ -1086,7 +1088,7 @@ struct Coded {                     // a lane's part of 32 keys: of two blocks, D
   uint4 codes[2][2];
   uint32_t scales[2];
 };
-constexpr int kFar = 6;            // tiles that are brought into L2 ahead of the decoders
+constexpr int kFar = 4;            // tiles from the one that is looked up to the one that is brought into L2
 template <int D>
 __device__ __forceinline__ void decode_run(const uint4& c, uint32_t byte, uint32_t row_at, int piece0, int r7) {
   const uint32_t sb = (byte << 4 | byte << 20) + 0x35803580u;
@@ -1107,76 +1109,44 @@ __device__ __forceinline__ void decode_run(const uint4& c, uint32_t byte, uint32
                  : "memory");
   }
 }
+// Addresses of the last tiles' blocks, [tile % 8][block]: the first four tiles' where the scan of the lengths was.
 template <int D>
-__device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles, uint32_t lead) {
+__device__ __forceinline__ const uint8_t* volatile* block_ring(uint8_t* smem, uint32_t tile) {
+  return reinterpret_cast<const uint8_t* volatile*>(smem + (tile & 4 ? Plan<D>::BLOCKS_OFF : Plan<D>::SCAN_OFF)) + (tile & 3) * 8;
+}
+template <int D>
+__device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles, uint32_t lead) {
   using P = Plan<D>;
   using B = Block<D>;
   constexpr int RUNS = D / 64;                     // of a lane and block
-  const uint32_t ring = smem_u32(smem) + P::RING_OFF;
   auto bar = [&](int which) { return bars + which * 8; };
-  Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
-  volatile int* progress = reinterpret_cast<int*>(smem + P::PROGRESS_OFF);
+  volatile int* ready = reinterpret_cast<int*>(smem + P::PROGRESS_OFF);
   const int warp = (int)(threadIdx.x >> 5) - kWarps, lane = threadIdx.x & 31;
   const int token = D == 128 ? lane & 7 : lane & 15, group = D == 128 ? lane >> 3 : lane >> 4;      // and token + 8
   // of this lane's runs in a block, and of their scales (tokens i and i + 8 have theirs side by side)
   const int k_at = B::k_word(token, group * 4), v_at = B::v_word(token, group * 4), ks_at = B::k_scale(token & 7, group), vs_at = B::v_scale(token & 7, group);
   constexpr int K8 = B::k_word(8, 0), V8 = B::v_word(8, 0) - B::v_word(0, 0);
   // this lane's rows in a tile: warp * 32 + token, and 8 (16, 24) rows further
-  const uint32_t row_at = ring + (warp * 4 + (token >> 3)) * P::GROUP + (token & 7) * 128;
-  // ---- fetching: K of the next tile, while V of an earlier one is decoded, and the other way round.  (One set of registers for
-  // each: with two they were spilled, and a load that is spilled is waited for.  A unit's first tile is waited for with no more
-  // than the K before it decoded ahead of its V: further ahead, four units of one tile each would wait for one another.)
-  const uint8_t* at[3][2];                         // blocks of the last tiles whose K was fetched
-#pragma unroll
-  for (int i = 0; i < 3; ++i) at[i][0] = at[i][1] = cache.data;
-  int seq = 0, kt = 0, kt_end = 0, len = 0, id[2] = {0, 0};
-  const int32_t* row = nullptr;
-  const uint8_t* head = nullptr;
+  const uint32_t row_at = smem_u32(smem) + P::RING_OFF + (warp * 4 + (token >> 3)) * P::GROUP + (token & 7) * 128;
   bool ok = true;
-  auto lookup = [&] {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int key = kt * kTile + warp * 32 + x * 16;
-      id[x] = key < len ? row[key >> a.page_log2] : -1;
-    }
-  };
-  auto load = [&](Coded& c, const uint8_t* (&blk)[2], int code_at, int eight, int scale_at) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(blk[x] + code_at));
-      if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(blk[x] + code_at + eight));
-      c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk[x] + scale_at));
-    }
-  };
-  auto next_tile = [&](uint32_t j) {
-#pragma unroll
-    for (int i = 2; i > 0; --i) { at[i][0] = at[i - 1][0]; at[i][1] = at[i - 1][1]; }
-    if (j >= n_tiles) return;
-    if (kt == kt_end) {
-      const int e = seq % kUnitRing;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50));
-      const Unit& u = units[e];
-      kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = ok ? u.len : 0;
-      row = a.table + (size_t)u.b * a.max_pages;
-      head = cache.data + u.g * cache.s_head;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
-      ++seq;
-      lookup();
-    }
-    if (warp == 0 && lane == 0) *progress = (int)j;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      // (no such page, or no key: any block will do, all that is stored is finite.  A load under a condition would be waited for.)
-      const int key = kt * kTile + warp * 32 + x * 16;
-      const bool there = id[x] >= 0 && id[x] < a.n_pages;
-      at[0][x] = there ? head + id[x] * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * B::BYTES : cache.data;
-      if (!there && key < len && lane == 0) report_range(a.status, kWhereTreePageQ4);
-    }
-    ++kt;
-    lookup();
-  };
   uint32_t slot = 0, lap = 0;
+  // (Always a load, of some block where there is nothing to read: a load under a condition would be waited for.)
+  auto load = [&](Coded& c, uint32_t tile, int code_at, int eight, int scale_at) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint8_t* blk = block_ring<D>(smem, tile)[warp * 2 + x];
+      c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(blk + code_at));
+      if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(blk + code_at + eight));
+      c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk + scale_at));
+    }
+  };
+  auto load_k = [&](Coded& c, uint32_t tile) {     // waits for the tile's addresses
+    if (tile >= n_tiles) tile = n_tiles - 1;       // behind the last: its blocks again
+    while (*ready <= (int)tile)
+      if (*ab.flag) { ok = false; return; }
+    load(c, tile, k_at, K8, ks_at);
+    if (lane == 0) ready[1 + warp] = (int)tile + 1;
+  };
   auto decode_tile = [&](const Coded& c) {         // into the next slot; which one, or -1
     if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
     if (!ok) return -1;
@@ -1192,20 +1162,26 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
     if (++slot == P::SLOTS) { slot = 0; ++lap; }
     return used;
   };
+  if (n_tiles == 0) return;
+  // K of the next tile comes while V of an earlier one is decoded, and the other way round.  (One set of registers for each.  A
+  // tile's addresses are waited for with no more than the K before it decoded ahead of its V: further ahead, four units of one
+  // tile each would wait for one another.)
   Coded k{}, v{};
-  next_tile(0);
-  load(k, at[0], k_at, K8, ks_at);
-  for (uint32_t j = 0; j < n_tiles + lead && ok; ++j) {
+  load_k(k, 0);
+  for (uint32_t j = 0; j < n_tiles + lead; ++j) {
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return;
     int k_slot = -1, v_slot = -1;
     if (j < n_tiles) {
       k_slot = decode_tile(k);
       if (!ok) return;
     }
-    next_tile(j + 1);
-    load(k, at[0], k_at, K8, ks_at);
-    if (j >= lead) v_slot = decode_tile(v);
-    if (lead == 2) load(v, at[2], v_at, V8, vs_at);
-    else load(v, at[1], v_at, V8, vs_at);
+    load_k(k, j + 1);
+    if (j >= lead) {
+      v_slot = decode_tile(v);
+      if (!ok) return;
+    }
+    if (j + 1 >= lead) load(v, min(j + 1 - lead, n_tiles - 1), v_at, V8, vs_at);
     fence_async_smem();                            // one for both (a fence is 200 cycles)
     __syncwarp();
     if (lane == 0 && k_slot >= 0) mbar_arrive(bar(P::BAR_FULL + k_slot));
@@ -1213,39 +1189,58 @@ __device__ __noinline__ void decode(const TreeAttnArgs& a, const Q4Cache& cache,
   }
 }
 
-// Brings the blocks of the tiles up to kFar ahead of the decoders into L2: their loads then cover its latency, not that of HBM.
-// One warp, a lane a block.
+// Looks up the pages of the tiles for the decoders, up to three tiles ahead of them, and brings blocks into L2 some tiles further ahead,
+// so that their loads cover its latency and not that of HBM.  One warp, a lane a block.  (Each decoder looking up its own: 850 of its
+// 3100 cycles a round, 219 us for the ragged trees.)
 template <int D>
-__device__ __noinline__ void prefetch_blocks(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles) {
+__device__ __noinline__ void find_blocks(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles) {
   using P = Plan<D>;
+  constexpr int PER = kTile / 16;                  // blocks of a tile
   auto bar = [&](int which) { return bars + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
-  volatile int* progress = reinterpret_cast<int*>(smem + P::PROGRESS_OFF);
-  const int lane = threadIdx.x & 31;
-  int seq = 0, kt = 0, kt_end = 0, len = 0, g = 0, b = 0;
+  volatile int* ready = reinterpret_cast<int*>(smem + P::PROGRESS_OFF);
+  const int lane = threadIdx.x & 31, block = lane % PER, turn = lane / PER;
+  int seq = 0, kt = 0, kt_end = 0, len = 0;
+  const int32_t* row = nullptr;
+  const uint8_t* head = nullptr;
+  auto page_of = [&](int key) { return key < len ? row[key >> a.page_log2] : -1; };
+  auto address = [&](int id, int key) { return head + id * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * Block<D>::BYTES; };
+  auto into_l2 = [&](int tile) {
+    const int key = tile * kTile + block * 16;
+    const int id = tile < kt_end ? page_of(key) : -1;
+    if (id >= 0 && id < a.n_pages)
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(address(id, key)), "r"(Block<D>::BYTES) : "memory");
+  };
   for (uint32_t j = 0; j < n_tiles; ++j) {
-    if (kt == kt_end) {
+    const bool first = kt == kt_end;
+    if (first) {
       const int e = seq % kUnitRing;
-      if (!__all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 52))) return;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 50))) return;
       const Unit& u = units[e];
-      kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = u.len; g = u.g; b = u.b;
+      kt = u.kt0; kt_end = u.kt0 + u.n_tiles; len = u.len;
+      row = a.table + (size_t)u.b * a.max_pages;
+      head = cache.data + u.g * cache.s_head;
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(P::BAR_UFREE + e));
       ++seq;
     }
-    const int key = kt * kTile + lane * 16;
-    if (lane < kTile / 16 && key < len) {
-      const int id = a.table[(size_t)b * a.max_pages + (key >> a.page_log2)];
-      if (id >= 0 && id < a.n_pages)
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(cache.data + g * cache.s_head + id * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * Block<D>::BYTES),
-                     "r"(Block<D>::BYTES) : "memory");
-    }
-    __syncwarp();
-    ++kt;
-    while ((int)j + 1 > *progress + kFar) {        // ends: the decoders go on, or the abort flag is raised
+    const int key = kt * kTile + block * 16, id = turn == 0 ? page_of(key) : -1;
+    if (first && turn > 0) into_l2(kt + turn);
+    if (turn == 1) into_l2(kt + kFar);
+    // A decoder that has fetched K of n tiles may still read the addresses of tile n - 3 (V): tile j takes the place of tile j - 8.
+    // (The wait ends: the decoders go on, or the abort flag is raised.)
+    while ((int)j > min(min(ready[1], ready[2]), min(ready[3], ready[4])) + 3)
       if (*ab.flag) return;
-      __nanosleep(200);
+    if (turn == 0) {
+      const bool there = id >= 0 && id < a.n_pages;
+      // (no such page, or no key: any block will do, all that is stored is finite)
+      block_ring<D>(smem, j)[block] = there ? address(id, key) : cache.data;
+      if (!there && key < len) report_range(a.status, kWhereTreePageQ4);
     }
+    __threadfence_block();
+    __syncwarp();
+    if (lane == 0) *ready = (int)j + 1;
+    ++kt;
   }
 }
 
@@ -1278,7 +1273,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
   if (!Q4 && warp == kProducer && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
   if (threadIdx.x == 0) {
     *abort_flag = *redo = 0;
-    *reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF) = 0;
+    for (int i = 0; i <= kDecoders; ++i) reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF)[i] = 0;
     for (int i = 0; i < 8; ++i) bad_tag[i] = 0;
   }
   wait_for_previous();
@@ -1396,7 +1391,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
     }
     for (int e = 0; e < kUnitRing; ++e) {
       mbar_init(bar(P::BAR_UNIT + e), 1);
-      mbar_init(bar(P::BAR_UFREE + e), (narrow ? 9 : wide ? 11 : 10) + (Q4 ? kDecoders : 0));
+      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : wide ? 11 : 10);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   };
@@ -1495,8 +1490,8 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
       }
     } else if (Q4 && (warp == kProducer || warp >= kWarps)) {
       if constexpr (Q4) {
-        if (warp == kProducer) prefetch_blocks<D>(a, cache, smem, bars, ab, n_tiles_cta);
-        else decode<D>(a, cache, smem, bars, ab, n_tiles_cta, lead);
+        if (warp == kProducer) find_blocks<D>(a, cache, smem, bars, ab, n_tiles_cta);
+        else decode<D>(cache, smem, bars, ab, n_tiles_cta, lead);
       }
     } else if (!Q4 && warp == kProducer) {
       // ------------------------------------------------------------ K and V tiles
@@ -1584,7 +1579,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
     // Tall, and a reference did not serve: the run once more, wide, with barriers of its own (some of the first walk's end in
     // odd phases).  All products of the first walk are in O, which has been read.
     if (threadIdx.x < 8) bad_tag[threadIdx.x] = 0;
-    if (threadIdx.x == 8) *reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF) = 0;
+    if (threadIdx.x <= kDecoders) reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF)[threadIdx.x] = 0;
     bars += P::BARS * 8;
     wide = true;
     __syncthreads();

@@ -1077,13 +1077,13 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
 // decoded, bf16 values into the tile's swizzled rows.  7 integer and 4 packed multiply-add instructions for 8 elements (see
 // q4_attn.cu), 32 stores of 16 bytes a lane and tile.
 //
-// It is the decoders that bound the tall form: a round (K of one tile, V of another) takes them 3100 to 3600 cycles, 1100 to
-// 1400 of them the decoding itself, the rest waits for the ring, a fence and the control of one warp that has three others on its
-// scheduler.  (32 ragged requests with trees of 16: 219 us; 181 if nothing is loaded or decoded, 172 over a bf16 cache with
-// four times the bytes.)  Measured on the way there: loads under a condition are waited for where they are issued (503 us);
-// registers that are spilled likewise (343 with two sets of them, 307 two tiles ahead); decoding by calls 272; a fence for
-// each of K and V 229.  The wide form is bound by its own chain (a tree of 64 over 131000 keys: 168 to 174 us, 153 if nothing is
-// decoded; as two tall units 236).
+// It is the decoders that bound the tall form: a round (K of one tile, V of another) takes them 3550 cycles with stamps taken,
+// 1000 to 1400 of them the decoding itself; 600 are a wait for V's place in the ring, 450 the loads, 450 the control of one warp
+// that has three others on its scheduler, 75 the fence.  The softmax groups are idle for two thirds of the time.  (32 ragged
+// requests with trees of 16: 203 us; 172 to 178 over a bf16 cache with four times the bytes.)  Measured on the way there: loads under a
+// condition are waited for where they are issued (503 us); registers that are spilled likewise (343 with two sets of them, 307 two
+// tiles ahead); decoding by calls 272; a fence for each of K and V 229; each decoder looking up its own blocks 219.  The wide
+// form is bound by its own chain (a tree of 64 over 131000 keys: 168 to 172 us, 153 if nothing is decoded; as two tall units 236).
 struct Coded {                     // a lane's part of 32 keys: of two blocks, D / 64 runs each, and their scales
   uint4 codes[2][2];
   uint32_t scales[2];
@@ -1190,8 +1190,7 @@ __device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_
 }
 
 // Looks up the pages of the tiles for the decoders, up to three tiles ahead of them, and brings blocks into L2 some tiles further ahead,
-// so that their loads cover its latency and not that of HBM.  One warp, a lane a block.  (Each decoder looking up its own: 850 of its
-// 3100 cycles a round, 219 us for the ragged trees.)
+// so that their loads cover its latency and not that of HBM.  One warp, a lane a block.
 template <int D>
 __device__ __noinline__ void find_blocks(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles) {
   using P = Plan<D>;

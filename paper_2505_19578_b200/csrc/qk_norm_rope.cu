@@ -146,22 +146,29 @@ __device__ __forceinline__ float quotient(float x, float y, float r) {
   return fmaf(fmaf(-q, y, x), r, q);
 }
 // Scale of a group whose largest magnitude is a, as fp32 bits: a / 7 to three bits behind the leading one, ties to even.
-__device__ __forceinline__ uint32_t scale_bits(float a) {
-  const uint32_t u = __float_as_uint(quotient(a, 7.f, 1.f / 7.f));
-  return clamp_scale((u + 0x7ffffu + (u >> 20 & 1u)) & 0xfff00000u);
+__device__ __forceinline__ uint32_t seventh(float a) { return __float_as_uint(quotient(a, 7.f, 1.f / 7.f)); }
+__device__ __forceinline__ uint32_t scale_bits(uint32_t u) { return clamp_scale((u + 0x7ffffu + (u >> 20 & 1u)) & 0xfff00000u); }
+// An error of at most err > 0 in a could change the scale that u, a / 7, is rounded to.  The border in the middle of u's own
+// interval is the one in question where the error is below a 128th of a; below 7 * 2^-20 * (1 + 1/16) there is none.
+__device__ __forceinline__ bool near_border(uint32_t u, float a, float err) {
+  const float border = __uint_as_float((u & 0xfff00000u) | 0x80000u);
+  return (fabsf(__uint_as_float(u) - border) <= err * 0.143f || err * 128.f > a) && err > 0.f && a + err > 7e-6f;
 }
 __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) { return (bits - kScaleLeast) >> 20; }
 
 // Codes of eight elements of at most 7.5 s; `far`: the largest distance of one from its code's value.  Sums with 1.5 * 2^23 + 8
 // round to whole numbers, ties to even, and leave the code in the low bits (rounding and conversion instructions run at a
-// sixteenth of the rate).
+// sixteenth of the rate).  Without EXACT the quotient is off by 2.4e-7 of itself, relative, which is less than the error that
+// an element of a normed or rotated key is taken to have: whatever that could change is computed again.
+template <bool EXACT>
 __device__ __forceinline__ uint32_t piece_codes(const float2 (&v)[4], float s, float& far) {
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
   uint32_t pair[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 q = __fmul2_rn(v[i], both(inv)), t = __ffma2_rn(__ffma2_rn(q, both(-s), v[i]), both(inv), q);
+    float2 t = __fmul2_rn(v[i], both(inv));
+    if (EXACT) t = __ffma2_rn(__ffma2_rn(t, both(-s), v[i]), both(inv), t);
     const float2 c = __fadd2_rn(t, both(12582920.f)), r = __ffma2_rn(__fadd2_rn(c, both(-12582920.f)), both(-s), v[i]);
     far = fmaxf(fmaxf(far, fabsf(r.x)), fabsf(r.y));
     pair[i] = __byte_perm(__float_as_uint(c.x), __float_as_uint(c.y), 0x5410);
@@ -280,20 +287,27 @@ __device__ __forceinline__ Codes codes_of(const RopeArgs& a, const Lane<D>& ln, 
     }
     group_max<D>(a, ln, a0, a1);
     float far = 0.f;
-    const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
-    c = {piece_codes(u, __uint_as_float(s0), far), piece_codes(v, __uint_as_float(s1), far), scale_byte(s0), scale_byte(s1)};
+    const uint32_t s0 = scale_bits(seventh(a0)), s1 = scale_bits(seventh(a1));
+    c = {piece_codes<true>(u, __uint_as_float(s0), far), piece_codes<true>(v, __uint_as_float(s1), far), scale_byte(s0), scale_byte(s1)};
     unsure |= top_err > 0.f;
   } else {
-    const uint32_t s0 = scale_bits(a0), s1 = scale_bits(a1);
+    const uint32_t u0 = seventh(a0), u1 = seventh(a1), s0 = scale_bits(u0), s1 = scale_bits(u1);
     const float f0 = __uint_as_float(s0), f1 = __uint_as_float(s1);
     float far0 = 0.f, far1 = 0.f;
-    c = {piece_codes(x, f0, far0), piece_codes(y, f1, far1), scale_byte(s0), scale_byte(s1)};
+    c.scale0 = scale_byte(s0);
+    c.scale1 = scale_byte(s1);
+    if (is_v || !(normed || a.rot == D)) {         // elements that are as they came lie on borders between codes
+      c.word0 = piece_codes<true>(x, f0, far0);
+      c.word1 = piece_codes<true>(y, f1, far1);
+    } else {
+      c.word0 = piece_codes<false>(x, f0, far0);
+      c.word1 = piece_codes<false>(y, f1, far1);
+    }
     if (!is_v) {
       // a border between two codes or two scales within the error
       if (normed || ln.turn0) unsure |= far0 >= 0.5f * f0 - err;
       if (normed || ln.turn1) unsure |= far1 >= 0.5f * f1 - err;
-      if (top_err > 0.f)
-        unsure |= scale_bits(a0 + top_err) != scale_bits(fmaxf(a0 - top_err, 0.f)) || scale_bits(a1 + top_err) != scale_bits(fmaxf(a1 - top_err, 0.f));
+      unsure |= near_border(u0, a0, top_err) || near_border(u1, a1, top_err);
     }
   }
   if (!is_v && __any_sync(0xffffffffu, unsure)) c = exact_codes<D>(a, pos, in0, in1);
@@ -519,12 +533,32 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
       angle_of = t;
       if (slot >= a.n_slots && cached<Q4>(a) && lane == 0) report_range(a.status, Q4 ? (int)kWhereRopeSlotQ4 : (int)kWhereRopeSlot);
     }
-#pragma unroll(Q4 ? 1 : kStreamRun)
-    for (int u = 0; u < kStreamRun; ++u) {
-      const int p = x.b * kStreamRun + u;
-      if (p < passes)
-        finish_pass<D, Q4>(a, ln, ln.pass(a, p), p >= pq + pkv, p < pq, t, slot, pos, *reinterpret_cast<const uint4*>(at + u * 1024 + lane * 16),
-                       *reinterpret_cast<const uint4*>(at + u * 1024 + 512 + lane * 16), cs, sn);
+    const int p0 = x.b * kStreamRun;
+    auto finish = [&](const Pass& p, bool is_v, bool is_q, int u) {
+      finish_pass<D, Q4>(a, ln, p, is_v, is_q, t, slot, pos, *reinterpret_cast<const uint4*>(at + u * 1024 + lane * 16),
+                         *reinterpret_cast<const uint4*>(at + u * 1024 + 512 + lane * 16), cs, sn);
+    };
+    if (!Q4) {
+#pragma unroll
+      for (int u = 0; u < kStreamRun; ++u)
+        if (p0 + u < passes) finish(ln.pass(a, p0 + u), p0 + u >= pq + pkv, p0 + u < pq, u);
+    } else {
+      // code of its own for each kind, and for items that are all queries
+      auto kind = [&](int k, int first, int heads, int u) {
+        const int head = (p0 + u - first) * Lane<D>::HPW + ln.hw;
+        finish(Pass{head < heads ? k : -1, head}, k == 2, k == 0, u);
+      };
+      if (p0 + kStreamRun <= pq) {
+#pragma unroll
+        for (int u = 0; u < kStreamRun; ++u) kind(0, 0, a.hq, u);
+      } else {
+#pragma unroll 1
+        for (int u = 0; u < kStreamRun && p0 + u < passes; ++u) {
+          if (p0 + u < pq) kind(0, 0, a.hq, u);
+          else if (p0 + u < pq + pkv) kind(1, pq, a.hkv, u);
+          else kind(2, pq + pkv, a.hkv, u);
+        }
+      }
     }
     __syncwarp();                                  // all have read position and slot before the stage is filled again
     if (++stage == kStreamStages) stage = 0;

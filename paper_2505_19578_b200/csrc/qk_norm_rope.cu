@@ -21,6 +21,9 @@
 // the one that exact arithmetic gives: where the fp32 value lies within its own error of a border between two codes or two
 // scales (a per mille of the heads), the warp computes the pass again in 64 bits.  So the same token has the same codes
 // whichever kernel stored it, and a border decides nothing by chance.
+// That form is bound by instructions: a warp's pass over four heads of 128 elements is 250 for queries and 480 for keys and values (K with
+// its borders more, V less), and the schedulers issue in half of the cycles, four warps of long chains each.  131072 rows of 48 heads
+// 855 us (2.8 GB: 431 at the copy rate), 16384 rows 111, 1000 rows of 36 heads 9.7, one row 2.4.
 #include <math_constants.h>
 
 #include "q4.cuh"
@@ -460,7 +463,7 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(const __grid
 // a ring of its own in shared memory (cp.async; a lane reads back only what it has copied, so nothing is synchronised).
 // 16 warps have 144 KB under way then, which registers could not hold.  Four passes, two items ahead: 2 % faster for
 // 131072 rows of 48 heads, 7 % slower for 1000 rows of 36, whose 9 passes do not divide.
-constexpr int kStreamWarps = 16, kStreamStages = 4, kStreamRun = 3;
+constexpr int kStreamSms = 148, kStreamWarps = 16, kStreamStages = 4, kStreamRun = 3;
 constexpr int kStreamItem = kStreamRun * 1024 + 32;        // bytes of an item: 32 lanes x two pieces a pass, position and slot
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
@@ -478,7 +481,11 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
   // The warps' tokens (items, if there are fewer tokens than warps) in turn, so that what is read and written at a time lies
   // together (a run of tokens for each warp: 695 us instead of 640 for 131072 rows).
   const int n_warps = gridDim.x * kStreamWarps, me = warp * gridDim.x + blockIdx.x, span = a.tokens >= n_warps ? per_token : 1;
-  const int jump_t = span > 1 ? n_warps : n_warps / per_token, jump_b = span > 1 ? 1 - per_token : n_warps % per_token;
+  // Passes that quantise take three times as long as the others.  Where a token's items would fall to the same SMs in every round,
+  // the item that a warp takes is turned on from four warps to the next and from round to round, so that every scheduler has of each
+  // (2000 rows of 48 heads: 18.1 instead of 22.1 us).
+  const bool turned = Q4 && span == 1 && n_warps % per_token == 0;
+  const int jump_t = span > 1 ? n_warps : n_warps / per_token, jump_b = span > 1 ? 1 - per_token : turned ? 1 : n_warps % per_token;
   struct At {                                      // an item
     int t, b;
   };
@@ -486,7 +493,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
     if (span > 1 && x.b + 1 < per_token) { ++x.b; return; }
     x.t += jump_t;
     x.b += jump_b;
-    if (x.b >= per_token) { x.b -= per_token; ++x.t; }
+    if (x.b >= per_token) { x.b -= per_token; x.t += turned ? 0 : 1; }
   };
   uint8_t* mine = smem + warp * kStreamStages * kStreamItem;
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
@@ -494,7 +501,8 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
   wait_for_previous();
   if (decode_poisoned(a.status)) return;
 
-  const At begin = span > 1 ? At{me, 0} : At{me / per_token, me % per_token};
+  At begin = span > 1 ? At{me, 0} : At{me / per_token, me % per_token};
+  if (turned) begin.b = (begin.b + begin.t / max(4 * (int)gridDim.x / per_token, 1)) % per_token;
   At ahead = begin;                                // the item to fetch next
   int fstage = 0;
   auto fetch = [&] {
@@ -569,18 +577,19 @@ template <int D, bool Q4>
 cudaError_t launch(RopeArgs& a, cudaStream_t s) {
   // From an item for every other of the device's warps on, the streaming kernel (36 heads, with it and with the other one:
   // 250 rows 4.8 and 4.2 us, 500 rows 5.5 and 7.0, 1000 rows 7.6 and 8.8; 131072 rows of 48 heads, head-major and cached: 662
-  // and 688).  The 4-bit form from four items a warp on (36 heads, written and read back: 1000 rows 19.5 us with it and 15.6 with
-  // the other one, 3000 rows 32.3 and 30.1, 16384 rows 109 and 131).
+  // and 688.  The 4-bit form, 36 heads: 300 rows 7.4 and 6.7, 500 rows 7.7 and 10.2, 1000 rows 9.7 and 11.0, 4000 rows 20.4 and 30.8;
+  // 48 heads: 300 rows 7.7 and 6.9, 500 rows 8.2 and 9.4.  What follows can start earlier beside the other one: 1000 rows of 36
+  // heads and their attention 56.6 and 57.2, and reading them back 16.7 and 15.9).
   const int passes = (a.hq + Lane<D>::HPW - 1) / Lane<D>::HPW + 2 * ((a.hkv + Lane<D>::HPW - 1) / Lane<D>::HPW);
   const long long items = (long long)a.tokens * ((passes + kStreamRun - 1) / kStreamRun);
-  if (items >= (Q4 ? 148 * kStreamWarps * 4 : 148 * kStreamWarps / 2)) {
+  if (items >= kStreamSms * kStreamWarps / 2) {
     constexpr int smem = kStreamWarps * kStreamStages * kStreamItem;
     const cudaError_t e = cudaFuncSetAttribute(qk_norm_rope_stream_kernel<D, Q4>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return launch_dependent(qk_norm_rope_stream_kernel<D, Q4>, dim3(148), dim3(kStreamWarps * 32), smem, s, a);
+    return launch_dependent(qk_norm_rope_stream_kernel<D, Q4>, dim3(kStreamSms), dim3(kStreamWarps * 32), smem, s, a);
   }
-  // warps to fill the device; of the 4-bit form's (156 registers) 12 fit an SM, and more would come in a second wave (1000 rows
-  // of 36 heads, written and read back: 15.6 us so, 18.5 with 32)
+  // warps to fill the device; of the 4-bit form's (over 128 registers) 12 fit an SM, and more would come in a second wave (1000
+  // rows of 36 heads, written and read back: 15.6 us so, 18.5 with 32)
   const long long splits = (148ll * (Q4 ? 12 : 32) + a.tokens - 1) / a.tokens;
   a.splits = (int)(splits > passes ? passes : splits);
   const long long warps = (long long)a.tokens * a.splits;

@@ -23,7 +23,7 @@
 // whichever kernel stored it, and a border decides nothing by chance.
 // That form is bound by instructions: a warp's pass over four heads of 128 elements is 250 for queries and 480 for keys and values (K with
 // its borders more, V less), and the schedulers issue in half of the cycles, four warps of long chains each.  131072 rows of 48 heads
-// 855 us (2.8 GB: 431 at the copy rate), 16384 rows 111, 1000 rows of 36 heads 9.7, one row 2.4.
+// 711 us (2.8 GB: 431 at the copy rate), 16384 rows 98, 1000 rows of 36 heads 9.6, one row 2.4.
 #include <math_constants.h>
 
 #include "q4.cuh"
@@ -551,21 +551,17 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) qk_norm_rope_stream_kern
       for (int u = 0; u < kStreamRun; ++u)
         if (p0 + u < passes) finish(ln.pass(a, p0 + u), p0 + u >= pq + pkv, p0 + u < pq, u);
     } else {
-      // code of its own for each kind, and for items that are all queries
+      // code of its own for each kind, once: with the three passes of an item of queries side by side it outgrows the instruction
+      // cache (131072 rows: 864 instead of 713 us)
       auto kind = [&](int k, int first, int heads, int u) {
         const int head = (p0 + u - first) * Lane<D>::HPW + ln.hw;
         finish(Pass{head < heads ? k : -1, head}, k == 2, k == 0, u);
       };
-      if (p0 + kStreamRun <= pq) {
-#pragma unroll
-        for (int u = 0; u < kStreamRun; ++u) kind(0, 0, a.hq, u);
-      } else {
 #pragma unroll 1
-        for (int u = 0; u < kStreamRun && p0 + u < passes; ++u) {
-          if (p0 + u < pq) kind(0, 0, a.hq, u);
-          else if (p0 + u < pq + pkv) kind(1, pq, a.hkv, u);
-          else kind(2, pq + pkv, a.hkv, u);
-        }
+      for (int u = 0; u < kStreamRun && p0 + u < passes; ++u) {
+        if (p0 + u < pq) kind(0, 0, a.hq, u);
+        else if (p0 + u < pq + pkv) kind(1, pq, a.hkv, u);
+        else kind(2, pq + pkv, a.hkv, u);
       }
     }
     __syncwarp();                                  // all have read position and slot before the stage is filled again

@@ -180,11 +180,16 @@ int need_split(sp_ctx* ctx, cudaStream_t s) {
 
 }  // namespace
 
-// (the device is synchronised: the caller's streams do not wait for the default one)
+// On a stream of its own: the default one, and synchronising the device, would spoil a capture that another thread has under way.
 cudaError_t sp::reset_arrived(sp_ctx* ctx) {
   if (!ctx->arrived) return cudaSuccess;
-  const cudaError_t e = cudaMemset(ctx->arrived, 0, ctx->n_sm * sizeof(int));
-  return e != cudaSuccess ? e : cudaDeviceSynchronize();
+  cudaStream_t s = nullptr;
+  cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+  if (e != cudaSuccess) return e;
+  e = cudaMemsetAsync(ctx->arrived, 0, ctx->n_sm * sizeof(int), s);
+  const cudaError_t done = cudaStreamSynchronize(s);
+  cudaStreamDestroy(s);
+  return e != cudaSuccess ? e : done;
 }
 
 extern "C" {

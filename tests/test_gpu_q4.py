@@ -517,6 +517,29 @@ def test_tree_attn_first_call_inside_a_capture(binding):  # noqa: F811
     s.check()
 
 
+def test_workspaces_are_made_while_another_stream_is_captured(binding):  # noqa: F811
+    """A first call on a stream that is not being captured leaves a capture on another one as it is."""
+    from tests import test_gpu_decode as bf
+    a, b = Step(73, 4, 2, 64, 16, [(100, 2)], "chain"), bf.Step(74, 4, 2, 64, 16, [(100, 2)], "chain")
+    c, d = binding.Context(), binding.Context()
+    x = torch.zeros(4, device="cuda")
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, capture_error_mode="relaxed"):
+        x.add_(1)
+        with torch.cuda.stream(other):
+            a.call(c)
+            b.call(d)
+        x.add_(1)
+    g.replay()
+    torch.cuda.synchronize()
+    assert x.tolist() == [2.0] * 4
+    for ctx, step in ((c, a), (d, b)):
+        clean(ctx)
+        step.check()
+
+
 def test_tree_attn_beside_the_bf16_one_in_one_workspace(binding):  # noqa: F811
     """The two forms take turns with one context's workspace, in a graph that holds both."""
     from tests import test_gpu_decode as bf

@@ -74,6 +74,7 @@ using namespace tc;
 constexpr int kTile = 128;                       // keys of a tile
 constexpr int kUnitRows = 256;
 constexpr int kWarps = 12, kDecoders = 4;        // the decoders, of the form for a 4-bit cache, are warps 12 to 15
+constexpr int kTallDecoders = kDecoders + 4;     // and, tall, 4 to 7
 constexpr int kProducer = 8, kIssuer = 9, kLoader = 10, kIssuer1 = 11;
 template <bool Q4>
 constexpr int kThreads = (kWarps + (Q4 ? kDecoders : 0)) * 32;
@@ -108,8 +109,8 @@ struct Plan {
   static constexpr int TAG_OFF = RUN_OFF + 3 * 8 + 4 * 4;                             // int [8]
   static constexpr int EX_OFF = (TAG_OFF + 8 * 4 + 15) / 16 * 16;                     // narrow: float2 [8][16]; tall: float [2][128]
   static constexpr int REF_OFF = EX_OFF + 1024;                                       // tall: float [128]
-  static constexpr int PROGRESS_OFF = REF_OFF + 512;                                  // 4-bit cache: int, tiles that were found; int [4], of which each decoder has fetched K
-  static constexpr int BLOCKS_OFF = PROGRESS_OFF + 32;                                // and addresses, half of a ring [8][8] of which the rest is at SCAN_OFF
+  static constexpr int PROGRESS_OFF = REF_OFF + 512;                                  // 4-bit cache: int, tiles that were found; int [8], of which each decoder has fetched K
+  static constexpr int BLOCKS_OFF = PROGRESS_OFF + 48;                                // and addresses, half of a ring [8][8] of which the rest is at SCAN_OFF
   static constexpr int TOTAL = BLOCKS_OFF + 256;
   static_assert(2 * (kWarps + kDecoders) * 8 >= 256, "");
   // TMEM columns: S 128 each; O: wide behind two S, tall behind three
@@ -949,17 +950,18 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
   }
 }
 
-// Softmax and epilogue, tall: the groups take the tiles in turn.
+// Softmax and epilogue, tall: the groups take the tiles in turn.  (Over a 4-bit cache there is one; the other's warps decode.)
 template <int D, bool Q4>
 __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& work, uint8_t* smem, const Abort& ab, uint32_t tmem, uint32_t n_tiles_cta) {
   using P = Plan<D>;
+  constexpr int GROUPS = Q4 ? 1 : 2;
   const uint32_t base = smem_u32(smem);
   auto bar = [&](int which) { return base + P::MISC_OFF + which * 8; };
   Unit* units = reinterpret_cast<Unit*>(smem + P::UNIT_OFF);
   volatile int* abort_flag = reinterpret_cast<int*>(smem + P::RUN_OFF + 3 * 8) + 1;
   volatile int* bad_tag = reinterpret_cast<int*>(smem + P::TAG_OFF);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int x = warp >> 2;                          // group
+  const int x = Q4 ? 0 : warp >> 2;                 // group
   const int row = threadIdx.x & 127;                // TMEM lane, row of the group
   const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
   const float scale = a.scale_log2;
@@ -985,18 +987,18 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
   for (int seq = 0;; ++seq) {
     const int e = seq % kUnitRing;
     ok = __all_sync(0xffffffffu, ok && mbar_wait(bar(P::BAR_UNIT + e), (seq / kUnitRing) & 1, ab, 30));
-    // the eight warps go on together or stop together: none is left at the barriers below
-    if (!bar_and(1, 256, ok)) break;
+    // the warps go on together or stop together: none is left at the barriers below
+    if (!bar_and(1, GROUPS * 128, ok)) break;
     const Unit& u = units[e];
     const int n_tiles = u.n_tiles;
     if (n_tiles == 0) break;
     const bool warp_live = (warp & 3) * 32 < u.rows, live = row < u.rows;
     const int token = (u.r0 + row) / a.group;
     const int kt0 = u.kt0, no_mask = min(u.past, u.len);
-    const int t0 = (int)((done + x) & 1);         // the CTA's tiles in turn: tile i is of group i & 1, in buffer i % 3
+    const int t0 = GROUPS == 1 ? 0 : (int)((done + x) & 1);      // the CTA's tiles in turn: tile i is of group i & 1, in buffer i % 3
     float m_ref = -kNoMax, l = 0.f;
     bool have_ref = false, saw = false;
-    for (int t = t0; t < n_tiles && ok; t += 2) {
+    for (int t = t0; t < n_tiles && ok; t += GROUPS) {
       const uint32_t i = done + t, buf = i % 3;
       const uint32_t t_s = lanes + P::S_COL + buf * 128;
       const int k0 = (kt0 + t) * kTile;
@@ -1041,21 +1043,22 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
     }
     if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_OFULL), seq & 1, ab, 33));
     ex[x * 128 + row] = saw ? l : -1.f;
-    if (!bar_and(1, 256, ok)) break;
+    if (!bar_and(1, GROUPS * 128, ok)) break;
     tc_fence_after();
     if (warp_live) {
-      const float l0 = ex[row], l1 = ex[128 + row];
+      const float l0 = ex[row], l1 = GROUPS == 1 ? -1.f : ex[128 + row];
       const bool seen = l0 != -1.f || l1 != -1.f;
       l = (l0 == -1.f ? 0.f : l0) + (l1 == -1.f ? 0.f : l1);
       const Place p = place_of(a, u, row);
       float* part = p.whole ? nullptr : work.part + p.slot * D;
-      const int lo = x * (D / 2);                 // each group half of the columns
-      const bool finite = write_columns(t_o, lo, lo + D / 2, !p.whole ? 1.f : l != 0.f ? 1.f / l : 0.f, live, p.out, part);
+      constexpr int WIDE = D / GROUPS;            // each group its share of the columns
+      const int lo = x * WIDE;
+      const bool finite = write_columns(t_o, lo, lo + WIDE, !p.whole ? 1.f : l != 0.f ? 1.f / l : 0.f, live, p.out, part);
       if (live) {
         if (seen && (l > kTallMost || l < kTallLeast || (l > 256.f && !finite))) *redo = 1;
         if (!Q4 && bad_tag[(seq + 1) % 8] == seq + 1) {
-          if (p.whole) add_nonfinite(a, u, p.token, p.out, lo, lo + D / 2);
-          else add_nonfinite(a, u, p.token, part, lo, lo + D / 2);
+          if (p.whole) add_nonfinite(a, u, p.token, p.out, lo, lo + WIDE);
+          else add_nonfinite(a, u, p.token, part, lo, lo + WIDE);
         }
         if (x == 0) write_weight(a, work, u, p, l != 0.f ? m_ref : kNoMax, l);
       }
@@ -1084,9 +1087,10 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
 // condition are waited for where they are issued (503 us); registers that are spilled likewise (343 with two sets of them, 307 two
 // tiles ahead); decoding by calls 272; a fence for each of K and V 229; each decoder looking up its own blocks 219.  The wide
 // form is bound by its own chain (a tree of 64 over 131000 keys: 168 to 172 us, 153 if nothing is decoded; as two tall units 236).
-struct Coded {                     // a lane's part of 32 keys: of two blocks, D / 64 runs each, and their scales
-  uint4 codes[2][2];
-  uint32_t scales[2];
+template <int BLOCKS>
+struct Coded {                     // a lane's part of the keys: of one or two blocks, D / 64 runs each, and their scales
+  uint4 codes[BLOCKS][2];
+  uint32_t scales[BLOCKS];
 };
 constexpr int kFar = 4;            // tiles from the one that is looked up to the one that is brought into L2
 template <int D>
@@ -1114,45 +1118,45 @@ template <int D>
 __device__ __forceinline__ const uint8_t* volatile* block_ring(uint8_t* smem, uint32_t tile) {
   return reinterpret_cast<const uint8_t* volatile*>(smem + (tile & 4 ? Plan<D>::BLOCKS_OFF : Plan<D>::SCAN_OFF)) + (tile & 3) * 8;
 }
-template <int D>
+template <int D, int BLOCKS>
 __device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles, uint32_t lead) {
   using P = Plan<D>;
   using B = Block<D>;
   constexpr int RUNS = D / 64;                     // of a lane and block
   auto bar = [&](int which) { return bars + which * 8; };
   volatile int* ready = reinterpret_cast<int*>(smem + P::PROGRESS_OFF);
-  const int warp = (int)(threadIdx.x >> 5) - kWarps, lane = threadIdx.x & 31;
+  const int warp = (int)(threadIdx.x >> 5) >= kWarps ? (int)(threadIdx.x >> 5) - kWarps : (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int token = D == 128 ? lane & 7 : lane & 15, group = D == 128 ? lane >> 3 : lane >> 4;      // and token + 8
   // of this lane's runs in a block, and of their scales (tokens i and i + 8 have theirs side by side)
   const int k_at = B::k_word(token, group * 4), v_at = B::v_word(token, group * 4), ks_at = B::k_scale(token & 7, group), vs_at = B::v_scale(token & 7, group);
   constexpr int K8 = B::k_word(8, 0), V8 = B::v_word(8, 0) - B::v_word(0, 0);
-  // this lane's rows in a tile: warp * 32 + token, and 8 (16, 24) rows further
-  const uint32_t row_at = smem_u32(smem) + P::RING_OFF + (warp * 4 + (token >> 3)) * P::GROUP + (token & 7) * 128;
+  // this lane's rows in a tile: token of the warp's blocks, and 8 (16, 24) rows further
+  const uint32_t row_at = smem_u32(smem) + P::RING_OFF + (warp * 2 * BLOCKS + (token >> 3)) * P::GROUP + (token & 7) * 128;
   bool ok = true;
   uint32_t slot = 0, lap = 0;
   // (Always a load, of some block where there is nothing to read: a load under a condition would be waited for.)
-  auto load = [&](Coded& c, uint32_t tile, int code_at, int eight, int scale_at) {
+  auto load = [&](Coded<BLOCKS>& c, uint32_t tile, int code_at, int eight, int scale_at) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const uint8_t* blk = block_ring<D>(smem, tile)[warp * 2 + x];
+    for (int x = 0; x < BLOCKS; ++x) {
+      const uint8_t* blk = block_ring<D>(smem, tile)[warp * BLOCKS + x];
       c.codes[x][0] = __ldcg(reinterpret_cast<const uint4*>(blk + code_at));
       if (RUNS == 2) c.codes[x][1] = __ldcg(reinterpret_cast<const uint4*>(blk + code_at + eight));
       c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk + scale_at));
     }
   };
-  auto load_k = [&](Coded& c, uint32_t tile) {     // waits for the tile's addresses
+  auto load_k = [&](Coded<BLOCKS>& c, uint32_t tile) {     // waits for the tile's addresses
     if (tile >= n_tiles) tile = n_tiles - 1;       // behind the last: its blocks again
     while (*ready <= (int)tile)
       if (*ab.flag) { ok = false; return; }
     load(c, tile, k_at, K8, ks_at);
     if (lane == 0) ready[1 + warp] = (int)tile + 1;
   };
-  auto decode_tile = [&](const Coded& c) {         // into the next slot; which one, or -1
+  auto decode_tile = [&](const Coded<BLOCKS>& c) {         // into the next slot; which one, or -1
     if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
     if (!ok) return -1;
     const uint32_t to = row_at + slot * P::SLOT;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < BLOCKS; ++x)
 #pragma unroll
       for (int y = 0; y < RUNS; ++y) {
         const uint32_t byte = RUNS == 2 ? c.scales[x] >> (8 * y) & 0xffu : c.scales[x] >> (token & 8) & 0xffu;
@@ -1166,7 +1170,7 @@ __device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_
   // K of the next tile comes while V of an earlier one is decoded, and the other way round.  (One set of registers for each.  A
   // tile's addresses are waited for with no more than the K before it decoded ahead of its V: further ahead, four units of one
   // tile each would wait for one another.)
-  Coded k{}, v{};
+  Coded<BLOCKS> k{}, v{};
   load_k(k, 0);
   for (uint32_t j = 0; j < n_tiles + lead; ++j) {
     ok = __all_sync(0xffffffffu, ok);
@@ -1192,7 +1196,7 @@ __device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_
 // Looks up the pages of the tiles for the decoders, up to three tiles ahead of them, and brings blocks into L2 some tiles further ahead,
 // so that their loads cover its latency and not that of HBM.  One warp, a lane a block.
 template <int D>
-__device__ __noinline__ void find_blocks(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles) {
+__device__ __noinline__ void find_blocks(const TreeAttnArgs& a, const Q4Cache& cache, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t n_tiles, int decoders) {
   using P = Plan<D>;
   constexpr int PER = kTile / 16;                  // blocks of a tile
   auto bar = [&](int which) { return bars + which * 8; };
@@ -1228,8 +1232,8 @@ __device__ __noinline__ void find_blocks(const TreeAttnArgs& a, const Q4Cache& c
     if (turn == 1) into_l2(kt + kFar);
     // A decoder that has fetched K of n tiles may still read the addresses of tile n - 3 (V): tile j takes the place of tile j - 8.
     // (The wait ends: the decoders go on, or the abort flag is raised.)
-    while ((int)j > min(min(ready[1], ready[2]), min(ready[3], ready[4])) + 3)
-      if (*ab.flag) return;
+    while (__any_sync(0xffffffffu, lane < decoders && (int)j > ready[1 + lane] + 3))
+      if (__any_sync(0xffffffffu, *ab.flag)) return;
     if (turn == 0) {
       const bool there = id >= 0 && id < a.n_pages;
       // (no such page, or no key: any block will do, all that is stored is finite)
@@ -1272,7 +1276,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
   if (!Q4 && warp == kProducer && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tm_k : &tm_v) : "memory");
   if (threadIdx.x == 0) {
     *abort_flag = *redo = 0;
-    for (int i = 0; i <= kDecoders; ++i) reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF)[i] = 0;
+    for (int i = 0; i <= kTallDecoders; ++i) reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF)[i] = 0;
     for (int i = 0; i < 8; ++i) bad_tag[i] = 0;
   }
   wait_for_previous();
@@ -1372,7 +1376,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
   }
   auto init_barriers = [&](uint32_t bars, bool wide) {
     auto bar = [&](int which) { return bars + which * 8; };
-    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), Q4 ? kDecoders : 1);
+    for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FULL + s), !Q4 ? 1 : wide ? kDecoders : kTallDecoders);
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(P::BAR_S + i), 1);
       mbar_init(bar(P::BAR_P + i), 4);
@@ -1380,9 +1384,9 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
     }
     mbar_init(bar(P::BAR_REF), 4);
     mbar_init(bar(P::BAR_OFULL), 1);
-    mbar_init(bar(P::BAR_OFREE), 8);
+    mbar_init(bar(P::BAR_OFREE), Q4 ? 4 : 8);
     // who lets a tile go: the issuer once, or (wide) for each group, or the eight warps; likewise the queries, which come
-    // from 32 lanes' copies when narrow; a unit is read by the eight warps, the producer and the issuers, if it has work
+    // from 32 lanes' copies when narrow; a unit is read by the softmax warps, the producer and the issuers, if it has work
     for (int s = 0; s < P::NSLOTS; ++s) mbar_init(bar(P::BAR_FREE + s), narrow ? 8 : wide ? 2 : 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(bar(P::BAR_QFULL + x), narrow ? 32 : 1);
@@ -1390,7 +1394,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
     }
     for (int e = 0; e < kUnitRing; ++e) {
       mbar_init(bar(P::BAR_UNIT + e), 1);
-      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : wide ? 11 : 10);
+      mbar_init(bar(P::BAR_UFREE + e), narrow ? 9 : wide ? 11 : Q4 ? 6 : 10);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   };
@@ -1487,10 +1491,11 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
         units[e].n_tiles = 0;
         mbar_arrive(bar(P::BAR_UNIT + e));
       }
-    } else if (Q4 && (warp == kProducer || warp >= kWarps)) {
+    } else if (Q4 && (warp == kProducer || warp >= kWarps || (!wide && warp >= 4 && warp < 8))) {
       if constexpr (Q4) {
-        if (warp == kProducer) find_blocks<D>(a, cache, smem, bars, ab, n_tiles_cta);
-        else decode<D>(cache, smem, bars, ab, n_tiles_cta, lead);
+        if (warp == kProducer) find_blocks<D>(a, cache, smem, bars, ab, n_tiles_cta, wide ? kDecoders : kTallDecoders);
+        else if (wide) decode<D, kTile / 16 / kDecoders>(cache, smem, bars, ab, n_tiles_cta, lead);
+        else decode<D, kTile / 16 / kTallDecoders>(cache, smem, bars, ab, n_tiles_cta, lead);
       }
     } else if (!Q4 && warp == kProducer) {
       // ------------------------------------------------------------ K and V tiles
@@ -1578,7 +1583,7 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
     // Tall, and a reference did not serve: the run once more, wide, with barriers of its own (some of the first walk's end in
     // odd phases).  All products of the first walk are in O, which has been read.
     if (threadIdx.x < 8) bad_tag[threadIdx.x] = 0;
-    if (threadIdx.x <= kDecoders) reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF)[threadIdx.x] = 0;
+    if (threadIdx.x <= kTallDecoders) reinterpret_cast<volatile int*>(smem + P::PROGRESS_OFF)[threadIdx.x] = 0;
     bars += P::BARS * 8;
     wide = true;
     __syncthreads();

@@ -688,15 +688,16 @@ cudaError_t launch(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arriv
 
 template <int D>
 cudaError_t launch_rows(const TreeAttnArgs& a, const Q4Cache& c, void* ws, int* arrived, int n_sm, cudaStream_t s, int* launched) {
-  // Rows of a request if all have as many.  More than 32 make tiles of 128 for the tensor cores' own memory; up to 32 are two
+  // Rows of a request if all have as many.  More than 24 make tiles of 128 for the tensor cores' own memory; up to 24 are two
   // units of 16 at most, which read the cache twice, from L2 the second time, but cost less for each unit (so, and with the
-  // tiles: 256 chats with 24 rows each 205 and 351 us, with 32 rows 244 and 352, with 48 rows as three units 316 and 354; 32 ragged
-  // requests with 28 rows 199 and 211; over 131000 keys 20 rows 116 and 120, 32 rows 120 and 120, 48 rows 164 and 122.  In one unit of up
-  // to 32 rows, of the registers of seven warps: 24 rows in chats 273, 28 ragged 252, 32 rows over 131000 keys 160).  Requests of more
-  // rows than a form's units have are several units, which is right for any lengths.
+  // tiles: 256 chats with 20 rows each 191 and 253 us, with 24 rows 206 and 252, with 32 rows 242 and 253, with 48 rows as three units 316
+  // and 264; 32 chats with 32 rows 55 and 49; 32 ragged requests with 21 rows 196 and 174, with 28 rows 199 and 174; over 131000
+  // keys 20 rows 116 and 101, 32 rows 120 and 102, 48 rows 164 and 107.  In one unit of up to 32 rows, of the registers of seven warps: 24 rows in
+  // chats 273, 28 ragged 252, 32 rows over 131000 keys 160).  Requests of more rows than a form's units have are several units, which is
+  // right for any lengths.
   const long long rows = ((long long)a.rows + a.n_req - 1) / a.n_req * a.group;
-  *launched = rows <= 32 ? 1 : 2;
-  return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : rows <= 32 ? launch<D, 2>(a, c, ws, arrived, n_sm, s) : launch_tree_attn_q4_tall(a, c, ws, n_sm, s);
+  *launched = rows <= 24 ? 1 : 2;
+  return rows <= 8 ? launch<D, 1>(a, c, ws, arrived, n_sm, s) : rows <= 24 ? launch<D, 2>(a, c, ws, arrived, n_sm, s) : launch_tree_attn_q4_tall(a, c, ws, n_sm, s);
 }
 
 }  // namespace

@@ -24,6 +24,9 @@
 //   warps 9, 11     issuers (one thread each; warp 11 in wide units only): S = Q K^T and O += P V
 //   warp 10         loader: walks the run, publishes units, gathers their Q rows into shared memory
 //
+// Over a 4-bit cache warp 8 looks up blocks of codes instead, warps 12-15 decode them into the ring, and warps 4-7 too in tall units,
+// whose softmax is then the other group's; there is no narrow mode (q4_attn.cu has those).
+//
 // Three modes, by the largest number of rows that any request has (wide only where it saves enough tiles, see the kernel):
 //
 // Wide (more than 128): units have up to 256 rows, the groups are their halves and walk the same tiles 64 keys at a time,
@@ -1074,19 +1077,20 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
   }
 }
 
-// Form for a 4-bit cache: what the producer is otherwise.  Four warps take 32 keys of each tile, K or V, in the ring's order:
-// codes and scales from global memory (a lane a run of 32 elements of a token's head, which has one scale; eight neighbouring
-// lanes eight tokens, so that their 16-byte stores go to different banks), K of the next tile while V of an earlier one is
-// decoded, bf16 values into the tile's swizzled rows.  7 integer and 4 packed multiply-add instructions for 8 elements (see
-// q4_attn.cu), 32 stores of 16 bytes a lane and tile.
+// Form for a 4-bit cache: what the producer is otherwise.  Four warps (eight if tall, where one group of four takes the softmax of all
+// tiles) take 32 (16) keys of each tile, K or V, in the ring's order: codes and scales from global memory (a lane a run of 32
+// elements of a token's head, which has one scale; eight neighbouring lanes eight tokens, so that their 16-byte stores go to
+// different banks), K of the next tile while V of an earlier one is decoded, bf16 values into the tile's swizzled rows.  7
+// integer and 4 packed multiply-add instructions for 8 elements (see q4_attn.cu), 32 (16) stores of 16 bytes a lane and tile.
 //
-// It is the decoders that bound the tall form: a round (K of one tile, V of another) takes them 3550 cycles with stamps taken,
-// 1000 to 1400 of them the decoding itself; 600 are a wait for V's place in the ring, 450 the loads, 450 the control of one warp
-// that has three others on its scheduler, 75 the fence.  The softmax groups are idle for two thirds of the time.  (32 ragged
-// requests with trees of 16: 203 us; 172 to 178 over a bf16 cache with four times the bytes.)  Measured on the way there: loads under a
-// condition are waited for where they are issued (503 us); registers that are spilled likewise (343 with two sets of them, 307 two
-// tiles ahead); decoding by calls 272; a fence for each of K and V 229; each decoder looking up its own blocks 219.  The wide
-// form is bound by its own chain (a tree of 64 over 131000 keys: 168 to 172 us, 153 if nothing is decoded; as two tall units 236).
+// Tall: 32 ragged requests with trees of 16 (112 rows) 189 us, 3000 cycles a tile; 176 if nothing is decoded, 184 if no exponential is
+// taken: the tile's hand-overs bound it, and the queries (28 rows: 174).  Over a bf16 cache with four times the bytes 172 to 178.
+// With two groups for the softmax and four decoders 202, a round of K and V 3550 cycles of a decoder, of which 1000 to 1400
+// were the decoding itself and the rest waits and control.  Measured on the way there: loads under a condition are waited for where
+// they are issued (503 us); registers that are spilled likewise (343 with two sets of them, 307 two tiles ahead); decoding by calls 272;
+// a fence for each of K and V 229; each decoder looking up its own blocks 219.  V one tile behind K instead of two: 191.
+// Wide: bound by its own chain (a tree of 64 over 131000 keys: 157 us, called in a row 172; 153 if nothing is decoded; as two
+// tall units 236 when they took 343 for the ragged trees).
 template <int BLOCKS>
 struct Coded {                     // a lane's part of the keys: of one or two blocks, D / 64 runs each, and their scales
   uint4 codes[BLOCKS][2];

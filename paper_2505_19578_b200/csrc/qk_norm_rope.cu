@@ -22,7 +22,7 @@
 // scales (a per mille of the heads), the warp computes the pass again in 64 bits.  So the same token has the same codes
 // whichever kernel stored it, and a border decides nothing by chance.
 // That form is bound by instructions: a warp's pass over four heads of 128 elements is 250 for queries and 480 for keys and values (K with
-// its borders more, V less), and the schedulers issue in half of the cycles, four warps of long chains each.  131072 rows of 48 heads
+// its borders more, V less), and the schedulers issue in 60 % of the cycles, four warps of long chains each.  131072 rows of 48 heads
 // 711 us (2.8 GB: 431 at the copy rate), 16384 rows 98, 1000 rows of 36 heads 9.6, one row 2.4.
 #include <math_constants.h>
 

@@ -48,7 +48,7 @@ def rope(lib, **over):
 
 
 def keep(lib, **over):
-    a = dict(ctx=CTX, c=cache(), table=ADDR, max_pages=4, past=ADDR + 1024, n=3, kept=ADDR + 2048, n_kept=ADDR + 1280, max_kept=4, lens=ADDR + 3072, stream=None)
+    a = dict(ctx=CTX, c=cache(), table=ADDR, max_pages=4, past=ADDR + 1024, n=3, kept=ADDR + 2048, n_kept=ADDR + 1280, max_kept=4, lens=ADDR + 4096, stream=None)
     a.update(over)
     return lib.sp_cache_keep_q4(*a.values())
 

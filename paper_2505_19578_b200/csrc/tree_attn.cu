@@ -1097,6 +1097,24 @@ struct Coded {                     // a lane's part of the keys: of one or two b
   uint32_t scales[BLOCKS];
 };
 constexpr int kFar = 4;            // tiles from the one that is looked up to the one that is brought into L2
+// Bounded wait of a whole warp for words in shared memory that other warps write.  The lanes go on together or stop together: each
+// sees the words and the flag when it happens to look, and what follows has votes that all have to reach.
+template <typename There>
+__device__ __forceinline__ bool warp_wait(There there, const Abort& ab, int where) {
+  long long since = 0;
+  for (uint32_t polls = 1; !__all_sync(0xffffffffu, there()); ++polls) {
+    if (__any_sync(0xffffffffu, *ab.flag != 0)) return false;
+    if ((polls & 4095u) != 0u) continue;
+    const long long now = clock64();
+    if (since == 0) since = now;
+    if (__any_sync(0xffffffffu, now - since > kWaitCycles)) {
+      *ab.flag = 1;
+      report_timeout(ab.status, where);
+      return false;
+    }
+  }
+  return true;
+}
 template <int D>
 __device__ __forceinline__ void decode_run(const uint4& c, uint32_t byte, uint32_t row_at, int piece0, int r7) {
   const uint32_t sb = (byte << 4 | byte << 20) + 0x35803580u;
@@ -1136,7 +1154,6 @@ __device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_
   constexpr int K8 = B::k_word(8, 0), V8 = B::v_word(8, 0) - B::v_word(0, 0);
   // this lane's rows in a tile: token of the warp's blocks, and 8 (16, 24) rows further
   const uint32_t row_at = smem_u32(smem) + P::RING_OFF + (warp * 2 * BLOCKS + (token >> 3)) * P::GROUP + (token & 7) * 128;
-  bool ok = true;
   uint32_t slot = 0, lap = 0;
   // (Always a load, of some block where there is nothing to read: a load under a condition would be waited for.)
   auto load = [&](Coded<BLOCKS>& c, uint32_t tile, int code_at, int eight, int scale_at) {
@@ -1148,16 +1165,17 @@ __device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_
       c.scales[x] = __ldcg(reinterpret_cast<const unsigned short*>(blk + scale_at));
     }
   };
-  auto load_k = [&](Coded<BLOCKS>& c, uint32_t tile) {     // waits for the tile's addresses
+  // Waits for the tile's addresses.  False: stop, here and now; the addresses of this tile and of later ones may never come, and what
+  // lies in their places is none.
+  auto load_k = [&](Coded<BLOCKS>& c, uint32_t tile) {
     if (tile >= n_tiles) tile = n_tiles - 1;       // behind the last: its blocks again
-    while (*ready <= (int)tile)
-      if (*ab.flag) { ok = false; return; }
+    if (!warp_wait([&] { return *ready > (int)tile; }, ab, 52)) return false;
     load(c, tile, k_at, K8, ks_at);
     if (lane == 0) ready[1 + warp] = (int)tile + 1;
+    return true;
   };
-  auto decode_tile = [&](const Coded<BLOCKS>& c) {         // into the next slot; which one, or -1
-    if (lap > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51));
-    if (!ok) return -1;
+  auto decode_tile = [&](const Coded<BLOCKS>& c) {         // into the next slot; which one, or -1: stop
+    if (lap > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(P::BAR_FREE + slot), (lap - 1) & 1, ab, 51))) return -1;
     const uint32_t to = row_at + slot * P::SLOT;
 #pragma unroll
     for (int x = 0; x < BLOCKS; ++x)
@@ -1175,19 +1193,17 @@ __device__ __noinline__ void decode(const Q4Cache& cache, uint8_t* smem, uint32_
   // tile's addresses are waited for with no more than the K before it decoded ahead of its V: further ahead, four units of one
   // tile each would wait for one another.)
   Coded<BLOCKS> k{}, v{};
-  load_k(k, 0);
+  if (!load_k(k, 0)) return;
   for (uint32_t j = 0; j < n_tiles + lead; ++j) {
-    ok = __all_sync(0xffffffffu, ok);
-    if (!ok) return;
     int k_slot = -1, v_slot = -1;
     if (j < n_tiles) {
       k_slot = decode_tile(k);
-      if (!ok) return;
+      if (k_slot < 0) return;
     }
-    load_k(k, j + 1);
+    if (!load_k(k, j + 1)) return;
     if (j >= lead) {
       v_slot = decode_tile(v);
-      if (!ok) return;
+      if (v_slot < 0) return;
     }
     if (j + 1 >= lead) load(v, min(j + 1 - lead, n_tiles - 1), v_at, V8, vs_at);
     fence_async_smem();                            // one for both (a fence is 200 cycles)
@@ -1235,9 +1251,8 @@ __device__ __noinline__ void find_blocks(const TreeAttnArgs& a, const Q4Cache& c
     if (first && turn > 0) into_l2(kt + turn);
     if (turn == 1) into_l2(kt + kFar);
     // A decoder that has fetched K of n tiles may still read the addresses of tile n - 3 (V): tile j takes the place of tile j - 8.
-    // (The wait ends: the decoders go on, or the abort flag is raised.)
-    while (__any_sync(0xffffffffu, lane < decoders && (int)j > ready[1 + lane] + 3))
-      if (__any_sync(0xffffffffu, *ab.flag)) return;
+    // (The wait ends by itself: the decoders go on.)
+    if (!warp_wait([&] { return lane >= decoders || (int)j <= ready[1 + lane] + 3; }, ab, 53)) return;
     if (turn == 0) {
       const bool there = id >= 0 && id < a.n_pages;
       // (no such page, or no key: any block will do, all that is stored is finite)

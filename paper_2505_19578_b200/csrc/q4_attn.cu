@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::THREADS, 1) tree_attn_q4_kernel(c
   if (threadIdx.x == 0) *abort_flag = last_flags[0] = last_flags[1] = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   wait_for_previous();
-  const bool idle = decode_poisoned(a.status);
+  const bool poisoned = decode_poisoned(a.status);
 
   // ---- where the warps' runs begin
   const int per = (a.n_req + THREADS - 1) / THREADS;
@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::THREADS, 1) tree_attn_q4_kernel(c
     if (lane >= o) incl += up;
   }
   if (lane == 31) scan[warp] = incl;
-  __syncthreads();
+  const bool idle = __syncthreads_or(poisoned) != 0;                   // all or none: there are barriers and votes ahead
   long long before = incl - mine, total = 0;
 #pragma unroll
   for (int w = 0; w <= WARPS; ++w) {

@@ -1,5 +1,7 @@
 """How the attentions over a 4-bit cache end when a wait has run out somewhere: nothing is read that nobody wrote, no lane is left
 behind, no copy is left in flight.  The functions run on the host (see _warp_emulation); no GPU, and no fault anywhere."""
+import re
+
 import pytest
 
 from tests import _warp_emulation as emu
@@ -117,3 +119,16 @@ int main() {
   std::puts("ok");
 }
 ''')
+
+
+@pytest.mark.parametrize("name", ["q4_attn.cu", "tree_attn.cu"])
+def test_the_status_word_is_voted_on_before_anything_depends_on_it(name):
+    """Each thread reads the status word for itself, and another kernel may write it in between: what threads with barriers and votes
+    ahead of them do about it is the same for the whole CTA.  (A thread that ends at once, as in the other kernels, is waited for nowhere.)"""
+    src = re.sub(r"//.*", "", emu.text(name))
+    own = re.findall(r"\b(\w+) = decode_poisoned\(", src)
+    ends = re.findall(r"if \(decode_poisoned\([^)]*\)[^;]*\) return;", src)
+    assert own and len(own) + len(ends) == src.count("decode_poisoned(")
+    for var in own:
+        uses = re.findall(rf"[^\n]*\b{var}\b[^\n]*", src)
+        assert len(uses) == 2 and "__syncthreads_or(" in uses[1], uses

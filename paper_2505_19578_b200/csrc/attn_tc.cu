@@ -148,15 +148,14 @@ attn_tc_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap tm_q, const
         ++issued_v;
         trace(0, 21, t);
       }
-      if (*abort_flag) {
-        // let the copies already in flight land before the CTA gives its shared memory back
-        const long long t0 = clock64();
-        while (clock64() - t0 < kWaitCycles / 8) {
-          bool done = mbar_try_wait(bar(BAR_Q_FULL), 0);
-          if (issued_k) done = done && mbar_try_wait(bar(BAR_K_FULL), (issued_k - 1) & 1);
-          if (issued_v) done = done && mbar_try_wait(bar(BAR_V_FULL), (issued_v - 1) & 1);
-          if (done) break;
-        }
+      // let the copies already in flight land before the CTA gives its shared memory back (its other warps may stop before they
+      // have waited for them, also after this one is through)
+      const long long t0 = clock64();
+      while (clock64() - t0 < kWaitCycles / 8) {
+        bool done = mbar_try_wait(bar(BAR_Q_FULL), 0);
+        if (issued_k) done = done && mbar_try_wait(bar(BAR_K_FULL), (issued_k - 1) & 1);
+        if (issued_v) done = done && mbar_try_wait(bar(BAR_V_FULL), (issued_v - 1) & 1);
+        if (done) break;
       }
     }
   } else if (warp == 5) {

@@ -166,7 +166,7 @@ __device__ __forceinline__ uint32_t values(uint32_t codes, int p, const Scale2& 
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// The producer: lane w issues the copies of warp w's run, RING steps ahead of the products.
+// The producer, a whole warp: lane w issues the copies of warp w's run, if it has one, RING steps ahead of the products.
 template <int D, int NT>
 __device__ __noinline__ void produce(const TreeAttnArgs& a, const Q4Cache& cache, uint32_t base, const Abort& ab, Walk walk, int w) {
   using P = Plan<D, NT>;
@@ -231,12 +231,13 @@ __device__ __noinline__ void produce(const TreeAttnArgs& a, const Q4Cache& cache
     ++issued;
     if (++slot == P::RING) { slot = 0; ++lap; }
   }
-  if (*ab.flag) {
-    // let the copies already in flight land before the CTA gives its shared memory back
-    const long long t0 = clock64();
-    for (int i = max(issued - P::RING, 0); i < issued; ++i)
-      while (!mbar_try_wait(full(i % P::RING), (i / P::RING) & 1) && clock64() - t0 < kWaitCycles / 8) {}
-  }
+  // The copies that are still in flight land before the CTA can give its shared memory back: also those of a run that was issued to its
+  // end, whose warp may give up, or stop with others, before it has waited for them.  (Behind all lanes' runs: a lane that polls
+  // holds up the others.)
+  __syncwarp();
+  const long long t0 = clock64();
+  for (int i = max(issued - P::RING, 0); i < issued; ++i)
+    while (!mbar_test(full(i % P::RING), (i / P::RING) & 1) && clock64() - t0 < kWaitCycles / 8) __nanosleep(500);
 }
 
 template <int D, int NT>
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::THREADS, 1) tree_attn_q4_kernel(c
   const long long w0 = run_begin(cta * warps + mine_w), steps = mine_w < warps && !idle ? run_begin(cta * warps + mine_w + 1) - w0 : 0;
   bool ok = true;
   if (warp == WARPS) {
-    if (steps > 0) produce<D, NT>(a, cache, base, ab, Walk{start_rem[lane], steps, start_b[lane], request_of<P::KEYS>(a, start_b[lane])}, lane);
+    produce<D, NT>(a, cache, base, ab, steps > 0 ? Walk{start_rem[lane], steps, start_b[lane], request_of<P::KEYS>(a, start_b[lane])} : Walk{}, lane);
     __syncwarp();
   } else if (steps > 0) {
     const int ring_at = P::RING_OFF + warp * (P::RING * P::BYTES);

@@ -1575,12 +1575,13 @@ __device__ __forceinline__ void tree_attn_body(const TreeAttnArgs& a, const Work
       }
       if (n_tiles_cta > 1 && lead > 1) load(last1, tm_v, work.v);
       if (n_tiles_cta > 0 && lead > 0) load(now, tm_v, work.v);
-      if (*abort_flag && lane == 0) {
-        // let the copies already in flight land before the CTA gives its shared memory back
+      if (lane == 0) {
+        // let the copies already in flight land before the CTA gives its shared memory back (its other warps may stop before they
+        // have waited for them, also after this one is through)
         const long long t0 = clock64();
         for (uint32_t i = 0; i < slots; ++i) {
           const uint32_t laps = lap + (i < s);          // loads that this slot has been given
-          while (laps > 0 && !mbar_test(bar(P::BAR_FULL + i), (laps - 1) & 1) && clock64() - t0 < kWaitCycles / 8) {}
+          while (laps > 0 && !mbar_test(bar(P::BAR_FULL + i), (laps - 1) & 1) && clock64() - t0 < kWaitCycles / 8) __nanosleep(500);
         }
       }
     } else if (warp == kIssuer || warp == kIssuer1) {

@@ -88,8 +88,8 @@ inline bool __any_sync(uint32_t, bool p) { warp.meet(p); return warp.was_any; }
 inline void __syncwarp() { warp.meet(true); }
 inline void __threadfence_block() {}
 inline void __nanosleep(unsigned) {}
-std::atomic<long long> now{0};
-inline long long clock64() { return now += 100000000; }
+std::atomic<long long> now{0}, tick{100000000};     // the clock moves when it is looked at
+inline long long clock64() { return now += tick; }
 inline int atomicCAS(int* p, int expected, int x) { const int old = *p; if (old == expected) *p = x; return old; }
 enum { SP_ERR_RANGE = -6, SP_ERR_TIMEOUT = -5 };
 struct Abort { volatile int* flag; int* status; };

@@ -121,6 +121,62 @@ int main() {
 ''')
 
 
+# Stand-ins for what a producer lane calls: a run of one piece, copies that land some polls of their barrier after they were issued.
+PRODUCER = r"""
+struct TreeAttnArgs { const int32_t* table; int max_pages, page_log2, n_pages; int* status; };
+struct Q4Cache { uint8_t* data; int64_t s_page, s_head; };
+constexpr int kWhereTreePageQ4 = 71;
+struct Plan1 { static constexpr int ROWS = 8, KEYS = 32, BLOCK = 17 * 128, BYTES = 2 * BLOCK, RING = 3, RING_OFF = 0, BAR_OFF = 1 << 20; };
+template <int D, int NT> using Plan = Plan1;
+struct Request { int start, n, len, past, kt; };
+struct Piece { int start, r0, rows, g, b, len, past, kt0, n, kt_all; };
+struct Walk { long long rem, left; int b; Request q; };
+int steps = 0, issued[3], landed[3], released[3], polls = 0, slow = 0, gives_up_at = 1 << 30;
+volatile int abort_flag = 0;
+template <int ROWS, int KEYS>
+bool walk_on(const TreeAttnArgs&, Walk& w, Piece& u) {
+  if (w.left <= 0) return false;
+  u.b = u.g = 0; u.len = (int)w.left * 32; u.kt0 = 0; u.n = (int)w.left;
+  w.left = 0;
+  return true;
+}
+inline void mbar_expect_tx(uint32_t bar, uint32_t) { ++issued[(bar - Plan1::BAR_OFF) / 16 % 3]; }
+inline void bulk_copy(uint32_t, const void*, uint32_t, uint32_t) {}
+inline bool mbar_test(uint32_t bar, uint32_t parity) {
+  const int slot = (bar - Plan1::BAR_OFF) / 16 % 3;
+  ++polls;
+  if (bar & 8) {                   // free: the consumer has read what landed, until it gives up
+    if (issued[0] + issued[1] + issued[2] >= gives_up_at) { abort_flag = 1; return false; }
+    landed[slot] = issued[slot];
+    return true;
+  }
+  if (slow >= 0 && polls > slow && landed[slot] < issued[slot]) { polls = 0; ++landed[slot]; }
+  return (uint32_t)(landed[slot] & 1) != parity;
+}
+inline bool mbar_try_wait(uint32_t bar, uint32_t parity) { return mbar_test(bar, parity); }
+"""
+
+
+@pytest.mark.parametrize("steps,gives_up,slow", [(1, 99, 9), (2, 99, 9), (3, 99, 9), (20, 99, 9), (20, 7, 9), (20, 3, 9), (0, 99, 9), (3, 99, -1), (20, 7, -1)])
+def test_a_producer_leaves_no_copy_in_flight(tmp_path, steps, gives_up, slow):
+    """Whether it has issued all of its copies or met the abort flag: they have landed when it returns, as a warp that gives up after
+    that ends the CTA at once.  (slow -1: they never land; it returns all the same.)"""
+    emu.run(tmp_path, PRODUCER + emu.definition(emu.text("q4_attn.cu"), r"^template <int D, int NT>\n__device__ __noinline__ void produce\(") + f"""
+int main() {{
+  int status[2] = {{0, 0}}, table[64] = {{}};
+  uint8_t data[16];
+  slow = {slow}; gives_up_at = {gives_up}; tick = 1000;
+  run_lanes(1, [&](int) {{
+    produce<128, 1>(TreeAttnArgs{{table, 64, 5, 1, status}}, Q4Cache{{data, 0, 0}}, 0, Abort{{&abort_flag, status}}, Walk{{0, {steps}, 0, Request{{}}}}, 0);
+  }});
+  for (int i = 0; i < 3; ++i)
+    if (slow >= 0 && landed[i] != issued[i]) fail("a copy is still in flight");
+  if (issued[0] + issued[1] + issued[2] != std::min({steps}, {gives_up})) fail("not all copies were issued");
+  std::puts("ok");
+}}
+""")
+
+
 @pytest.mark.parametrize("name", ["q4_attn.cu", "tree_attn.cu"])
 def test_the_status_word_is_voted_on_before_anything_depends_on_it(name):
     """Each thread reads the status word for itself, and another kernel may write it in between: what threads with barriers and votes
@@ -132,3 +188,14 @@ def test_the_status_word_is_voted_on_before_anything_depends_on_it(name):
     for var in own:
         uses = re.findall(rf"[^\n]*\b{var}\b[^\n]*", src)
         assert len(uses) == 2 and "__syncthreads_or(" in uses[1], uses
+
+
+@pytest.mark.parametrize("name", ["tree_attn.cu", "attn_tc.cu"])
+def test_other_producers_wait_for_their_copies_whether_or_not_the_flag_is_up_yet(name):
+    """(The paired kernel's producer waits for each copy as it relays it, so that only a run that it broke off itself leaves any.)"""
+    src = emu.text(name)
+    at = [m.start() for m in re.finditer("let the copies already in flight land", src)]
+    assert at
+    for x in at:
+        condition = [line for line in src[:x].splitlines()[:-1] if line.strip()][-1]
+        assert "abort_flag" not in condition, condition

@@ -154,9 +154,18 @@ Q4Cache q4_of(const sp_q4_cache* c) {
   return Q4Cache{static_cast<uint8_t*>(c->data), c->pages > 1 ? c->stride_page : 0, c->heads > 1 ? c->stride_head : 0};
 }
 
+// While this lives, this thread may allocate and synchronise although another stream is being captured in a mode that forbids it (to
+// this thread, or to all): such a call would fail, and end that capture.  What is done meanwhile has nothing to do with the capture.
+struct BesideCaptures {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  BesideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode); }
+  ~BesideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
 // The workspace of sp_tree_attn and sp_tree_attn_q4, with the context's device current.
 int reserve_split(sp_ctx* ctx) {
   if (ctx->split_ws) return SP_OK;
+  const BesideCaptures beside;
   int n_sm = 0;
   if (cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, ctx->device) != cudaSuccess) return SP_ERR_CUDA;
   void* p = nullptr;
@@ -180,9 +189,10 @@ int need_split(sp_ctx* ctx, cudaStream_t s) {
 
 }  // namespace
 
-// On a stream of its own: the default one, and synchronising the device, would spoil a capture that another thread has under way.
+// On a stream of its own: the default one, and synchronising the device, would spoil a capture that is under way on another stream.
 cudaError_t sp::reset_arrived(sp_ctx* ctx) {
   if (!ctx->arrived) return cudaSuccess;
+  const BesideCaptures beside;
   cudaStream_t s = nullptr;
   cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
   if (e != cudaSuccess) return e;

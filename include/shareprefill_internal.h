@@ -52,6 +52,11 @@ int sp_ctx_set_trace(sp_ctx* ctx, int64_t* events, int events_per_role);
 int sp_internal_pair_work_order(const int32_t* heads, const int32_t* lists, int n_heads, int n_q_heads, int n_kv_heads,
                                 int n_row_blocks, int n_sm, int pair_heads, int32_t* tiles_out, int* n_groups_out);
 
+/* The counters of units that several CTAs share in sp_tree_attn_q4: one for each SM, zero between calls.  Reads them into
+ * counters[0 .. n) (host; *n in: its room, out: how many there are), or with `write` sets them from there.  SP_ERR_WORKSPACE
+ * before the workspace has been made.  For tests of what a timeout leaves behind. */
+int sp_internal_split_counters(sp_ctx* ctx, int32_t* counters, int* n, int write);
+
 /* Number of kernels this context has launched since creation (for callers
  * that account for launches). */
 int64_t sp_ctx_launch_count(const sp_ctx* ctx);

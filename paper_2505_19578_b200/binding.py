@@ -36,7 +36,7 @@ EXPORTS = (
     "sp_determine_pattern", "sp_vertical_slash_pattern", "sp_prefill_attn_auto",
     "sp_dict_create", "sp_dict_destroy", "sp_dict_clear", "sp_dict_count", "sp_prefill_attn_layer",
     "sp_selftest_wait_timeout", "sp_fixed_scratch_status", "sp_workspace_bytes_patterns",
-    "sp_internal_pair_work_order",
+    "sp_internal_pair_work_order", "sp_internal_split_counters",
     "sp_page_tables", "sp_qk_norm_rope", "sp_tree_attn", "sp_cache_keep", "sp_ctx_reserve_decode",
     "sp_q4_page_bytes", "sp_qk_norm_rope_q4", "sp_tree_attn_q4", "sp_cache_keep_q4", "sp_cache_read_q4",
 )
@@ -95,6 +95,7 @@ def load() -> ctypes.CDLL:
     lib.sp_dict_count.argtypes = [P]
     lib.sp_prefill_attn_layer.argtypes = [P, P, T, T, T, IP, F, F, F, I, I, T, P, P, P]
     lib.sp_ctx_reserve_decode.argtypes = [P]
+    lib.sp_internal_split_counters.argtypes = [P, IP, ctypes.POINTER(I), I]
     lib.sp_page_tables.argtypes = [P, P, P, I, I, P, I, P, I, P, P, P, P, P, P, I, I, P, P]
     lib.sp_qk_norm_rope.argtypes = [P, P, P, P, P, P, F, P, I, I, P, P, P, P, P, P, P, P]
     lib.sp_tree_attn.argtypes = [P, P, P, P, P, I, P, P, I, P, I, P, P, P]

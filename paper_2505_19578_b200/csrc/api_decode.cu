@@ -211,6 +211,17 @@ int sp_ctx_reserve_decode(sp_ctx* ctx) {
   return reserve_split(ctx);
 }
 
+int sp_internal_split_counters(sp_ctx* ctx, int32_t* counters, int* n, int write) {
+  if (!ctx || !counters || !n || *n < 0) return SP_ERR_INVALID_ARG;
+  if (!ctx->split_ws) return SP_ERR_WORKSPACE;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SP_ERR_CUDA;
+  const size_t bytes = std::min(*n, ctx->n_sm) * sizeof(int);
+  const cudaError_t e = write ? cudaMemcpy(ctx->arrived, counters, bytes, cudaMemcpyHostToDevice) : cudaMemcpy(counters, ctx->arrived, bytes, cudaMemcpyDeviceToHost);
+  *n = ctx->n_sm;
+  return e == cudaSuccess ? SP_OK : SP_ERR_CUDA;
+}
+
 int sp_page_tables(sp_ctx* ctx, const int32_t* past_lens, const int32_t* new_lens, int n_req, int page,
                    const int32_t* free_pages, int n_free, int32_t* block_table, int max_pages, const int32_t* parents,
                    int32_t* seq_lens, int32_t* row_start, int32_t* positions, int32_t* slots, uint32_t* tree_mask,

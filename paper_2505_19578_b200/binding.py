@@ -367,8 +367,13 @@ class Context:
         if code:
             _check(code, "sp_tree_attn_q4")
 
-    def sp_cache_keep_q4(self, cache, block_table, past_lens, kept, n_kept, lens_out, head_dim, stream=None):
-        """As sp_cache_keep, on a 4-bit cache of heads of `head_dim` elements."""
+    def sp_cache_keep_q4(self, cache, block_table, past_lens, kept, n_kept, lens_out, head_dim, stream=None, page=None):
+        """As sp_cache_keep, on a 4-bit cache of heads of `head_dim` elements.
+
+        A page of n tokens of 128 elements has as many bytes as one of 2 n tokens of 64, and no other argument tells the two apart:
+        with the wrong `head_dim` the wrong bytes would move.  `page`, the tokens of a page, has it checked."""
+        if page is not None and cache.shape[-1] != page_bytes(page, head_dim):
+            raise ValueError(f"cache: pages of {cache.shape[-1]} bytes are not {page} tokens of {head_dim} elements")
         code = (_native or _decode_calls()).cache_keep_q4(
             self._h.value, self.device, cache, block_table, past_lens, kept, n_kept, lens_out, head_dim,
             None if stream is None else stream.cuda_stream)

@@ -127,3 +127,27 @@ def test_counters_are_zero_after_a_bad_page_in_a_shared_unit(binding):  # noqa: 
         t.call(ctx)
         clean(ctx)
         t.check()
+
+
+def test_keep_refuses_a_head_dim_that_is_not_the_caches(binding):  # noqa: F811
+    """Pages of 16 tokens of 128 elements and of 32 of 64 have the same bytes: with `page` given, they are told apart."""
+    ctx = binding.Context()
+    table, past, kept, count = i32([[1, 0]]), i32([3]), i32([[1, 4]]), i32([2])
+    for page, d, wrong_page, wrong_d in ((16, 128, 32, 64), (64, 64, 32, 128)):
+        before = torch.randint(0, 256, (2, 3, q4.page_bytes(page, d)), dtype=torch.uint8).cuda()
+        cache, lens = before.clone(), i32([-7])
+        with pytest.raises(ValueError, match=f"pages of {q4.page_bytes(page, d)} bytes are not {page} tokens of {wrong_d} elements"):
+            ctx.sp_cache_keep_q4(cache, table, past, kept, count, lens, wrong_d, page=page)
+        with pytest.raises(ValueError, match="are not"):
+            ctx.sp_cache_keep_q4(cache, table, past, kept, count, lens, d, page=wrong_page)
+        with pytest.raises(binding.SpError, match="-2"):
+            ctx.sp_cache_keep_q4(cache, table, past, kept, count, lens, d, page=24)
+        clean(ctx)
+        assert torch.equal(cache, before) and lens.tolist() == [-7]
+        ctx.sp_cache_keep_q4(cache, table, past, kept, count, lens, d, page=page)
+        clean(ctx)
+        whole = cache.clone()
+        cache.copy_(before)
+        ctx.sp_cache_keep_q4(cache, table, past, kept, count, lens, d)
+        clean(ctx)
+        assert torch.equal(cache, whole) and not torch.equal(cache, before) and lens.tolist() == [5]

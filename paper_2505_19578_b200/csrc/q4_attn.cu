@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(Plan<D, NT>::THREADS, 1) tree_attn_q4_kernel(c
           }
         }
         // ---- softmax: lane has keys g, g + 8 of each block and rows 2 q, 2 q + 1 of each tile
-        if (k0 + P::KEYS > no_mask) {
+        if (no_mask - k0 < P::KEYS) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             if (NT > 1 && nt >= tiles) break;

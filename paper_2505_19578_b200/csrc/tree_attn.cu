@@ -215,7 +215,7 @@ __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) ==
 // (they were left out of the products): bf16 results, or fp32 partial sums.
 template <typename T>
 __device__ __noinline__ void add_nonfinite(const TreeAttnArgs& a, const Unit& u, int token, T* out, int lo, int hi) {
-  const int k_from = max(u.kt0 * kTile, u.past), k_to = min((u.kt0 + u.n_tiles) * kTile, u.len);
+  const int k_from = max(u.kt0 * kTile, u.past), k_to = u.kt0 + u.n_tiles == u.kt_all ? u.len : (u.kt0 + u.n_tiles) * kTile;
   for (int key = k_from; key < k_to; ++key) {
     const int id = a.table[(size_t)u.b * a.max_pages + (key >> a.page_log2)];
     if (id < 0 || id >= a.n_pages || !(seen32(a, u, token, key) & 1)) continue;
@@ -441,7 +441,7 @@ __device__ __noinline__ void narrow_warps(const TreeAttnArgs& a, const Work& wor
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[n][i] *= scale;
-      const bool special = k0 + kTile > no_mask;
+      const bool special = no_mask - k0 < kTile;
       if (special) {
         const int key = k0 + warp * 16;
         const uint32_t seen0 = g < rows ? seen32(a, u, g / a.group, key) : 0u, seen1 = g + 8 < rows ? seen32(a, u, (g + 8) / a.group, key) : 0u;
@@ -874,7 +874,7 @@ __device__ __noinline__ void softmax_wide(const TreeAttnArgs& a, const Work& wor
     for (int t = 0; t < 2 * n_tiles && ok; ++t) {
       const int k0 = (kt0 + (t >> 1)) * kTile, half = t & 1;      // half a tile in buffer `half`
       const uint32_t t_s = lanes + P::S_COL + x * 128 + half * 64, phase = (done + (t >> 1)) & 1;
-      const bool special = k0 + half * 64 + 64 > no_mask;
+      const bool special = no_mask - k0 < half * 64 + 64;
       ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + 2 * x + half), phase, ab, 31));
       if (!ok) break;
       tc_fence_after();
@@ -1005,7 +1005,7 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
       const uint32_t i = done + t, buf = i % 3;
       const uint32_t t_s = lanes + P::S_COL + buf * 128;
       const int k0 = (kt0 + t) * kTile;
-      const bool special = k0 + kTile > no_mask;
+      const bool special = no_mask - k0 < kTile;
       ok = __all_sync(0xffffffffu, mbar_wait(bar(P::BAR_S + buf), (i / 3) & 1, ab, 31));
       if (!ok) break;
       tc_fence_after();
@@ -1229,8 +1229,8 @@ __device__ __noinline__ void find_blocks(const TreeAttnArgs& a, const Q4Cache& c
   auto page_of = [&](int key) { return key < len ? row[key >> a.page_log2] : -1; };
   auto address = [&](int id, int key) { return head + id * cache.s_page + ((key & ((1 << a.page_log2) - 1)) >> 4) * Block<D>::BYTES; };
   auto into_l2 = [&](int tile) {
-    const int key = tile * kTile + block * 16;
-    const int id = tile < kt_end ? page_of(key) : -1;
+    const int key = tile < kt_end ? tile * kTile + block * 16 : len;
+    const int id = page_of(key);
     if (id >= 0 && id < a.n_pages)
       asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(address(id, key)), "r"(Block<D>::BYTES) : "memory");
   };

@@ -34,7 +34,7 @@ __device__ __forceinline__ Request request_of(const TreeAttnArgs& a, int b) {
   q.n = s0 < 0 ? 0 : max(min(s1, a.rows) - q.start, 0);
   q.len = min(max(seq, 0), a.max_pages << a.page_log2);
   q.past = seq - (s1 - s0);
-  q.kt = max((q.len + TILE - 1) / TILE, 1);
+  q.kt = max((int)(((uint32_t)q.len + (TILE - 1)) / TILE), 1);     // (lengths go up to 2^31 - 16)
   return q;
 }
 __device__ __forceinline__ long long divide(long long x, long long y) {       // both are small as a rule

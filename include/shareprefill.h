@@ -477,7 +477,8 @@ int sp_prefill_attn_layer(sp_ctx* ctx, sp_pattern_dict* dict, const sp_tensor* q
  */
 
 /* Allocate the workspace of sp_tree_attn and sp_tree_attn_q4 (39 MB with 148 SMs; it depends on the device alone and never moves).  Its
- * first call does so otherwise; inside a stream capture that call returns SP_ERR_WORKSPACE and enqueues nothing. */
+ * first call does so otherwise; on a stream that is being captured that call returns SP_ERR_WORKSPACE and enqueues nothing.
+ * Captures on other streams, in whatever mode, are left as they are. */
 int sp_ctx_reserve_decode(sp_ctx* ctx);
 
 /*
@@ -589,7 +590,9 @@ int sp_cache_keep(sp_ctx* ctx, const sp_tensor* k_cache, const sp_tensor* v_cach
 /* ------------------------------------------------------------------------
  * The same over a paged cache held in 4 bits.  (No counterpart in the paper.)  A step is sp_page_tables, then per layer
  * sp_qk_norm_rope_q4 and sp_tree_attn_q4, and sp_cache_keep_q4 after verification; sp_cache_read_q4 gives cached tokens
- * back as the bf16 tensors that sp_prefill_attn reads.  At head_dim 128 a token and head take 136 bytes instead of 512.
+ * back as bf16 rows, head by head.  At head_dim 128 a token and head take 136 bytes instead of 512.
+ * The next chunk of a prompt behind a cached prefix goes through sp_tree_attn_q4 as a chain (tree_mask NULL): the prefill
+ * calls take as many queries as keys, a multiple of the block, and so read a cached prompt only whole, with its own queries.
  *
  * Conventions on top of those above
  *   - A value is (c - 8) * s: c a code of 4 bits, s a scale for 32 neighbouring elements of a token's head, one byte
@@ -616,7 +619,8 @@ int sp_q4_page_bytes(int page, int head_dim, int64_t* bytes /* host, out */);
  * sp_qk_norm_rope_q4 - sp_qk_norm_rope with the 4-bit cache as destination of keys and values: they are quantised on the
  *   way.  Arguments as there; k_out and v_out (bf16, unquantised) or both NULL.  The codes are those of exact arithmetic on
  *   the bf16 inputs, not of k_out's rounding: a key within fp32's error of the border between two codes is computed again
- *   in 64 bits.  cache and slots must be given.  The outputs may not overlap the cache.
+ *   in 64 bits (the angle then within 2^-33 of a turn at any 32-bit position).  cache and slots must be given.  The outputs
+ *   may not overlap the cache.
  */
 int sp_qk_norm_rope_q4(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, const sp_tensor* v, const void* q_weight,
                        const void* k_weight, float eps, const double* inv_freq /* host */, int n_freq, int interleaved,
@@ -626,6 +630,10 @@ int sp_qk_norm_rope_q4(sp_ctx* ctx, const sp_tensor* q, const sp_tensor* k, cons
 /*
  * sp_tree_attn_q4 - sp_tree_attn over a 4-bit cache: the same rows, masks, results and roundings, the products' keys and
  *   values being the stored ones exactly.  out must not overlap q or the cache.
+ *   The form of a call is chosen on the host, by the mean of its rows per request (q's rows, padded ones included, over
+ *   n_req, rounded up) times the query heads per KV head: to 8, to 24, and above.  Any lengths are right in every form, but
+ *   a request with more rows than the form has in a unit (8, 16, 128 or 256) is read once for every unit.  So a long chunk
+ *   or tree beside many single tokens, or beside many empty requests, is faster in a call of its own.
  */
 int sp_tree_attn_q4(sp_ctx* ctx, const sp_tensor* q, const sp_q4_cache* cache, const int32_t* block_table, int max_pages,
                     const int32_t* seq_lens, const int32_t* row_start, int n_req, const uint32_t* tree_mask, int mask_words,

@@ -19,7 +19,8 @@
 // elements of a head: a = max |y|, s = a / 7 to four significant bits, code = y / s to the nearest, both ties to even.  An
 // 8-element piece is a word of codes.  Keys are quantised from the fp32 values, not from their bf16 rounding.  The code is
 // the one that exact arithmetic gives: where the fp32 value lies within its own error of a border between two codes or two
-// scales (a per mille of the heads), the warp computes the pass again in 64 bits.  So the same token has the same codes
+// scales, the warp computes the pass again in 64 bits (of the passes of four heads of 128 elements 1.4 %, 0.5 % without a
+// norm, by the bounds below on normal values).  So the same token has the same codes
 // whichever kernel stored it, and a border decides nothing by chance.
 // That form is bound by instructions: a warp's pass over four heads of 128 elements is 250 for queries and 480 for keys and values (K with
 // its borders more, V less), and the schedulers issue in 60 % of the cycles, four warps of long chains each.  131072 rows of 48 heads
@@ -351,8 +352,8 @@ __device__ __forceinline__ void finish_pass(const RopeArgs& a, const Lane<D>& ln
     }
     if (Q4 && !is_q && (weight || a.rot > 0)) {
       // fp32: the angle is off by 2^-26 of a turn, 1e-7, sine and cosine by 1.2e-7 and the rotation's two roundings by as much,
-      // 3.4e-7 of |a| + |b| for each pair; the norm by 7.5e-7, relative (16 roundings of the sum of squares, halved by the root,
-      // its 2 ulp and the products), 1.1e-6 with it
+      // 3.4e-7 of |a| + |b| for each pair; the norm by 8.4e-7, relative (16 roundings of the sum of squares, halved by the root: 4.8e-7,
+      // its 2 ulp: 2.4e-7, and two products: 1.2e-7), 1.2e-6 with it.  Taken to be 6e-7 and 1.5e-6
       float pair = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {

@@ -1083,7 +1083,7 @@ __device__ __noinline__ void softmax_tall(const TreeAttnArgs& a, const Work& wor
 // different banks), K of the next tile while V of an earlier one is decoded, bf16 values into the tile's swizzled rows.  7
 // integer and 4 packed multiply-add instructions for 8 elements (see q4_attn.cu), 32 (16) stores of 16 bytes a lane and tile.
 //
-// Tall: 32 ragged requests with trees of 16 (112 rows) 189 us, 3000 cycles a tile; 176 if nothing is decoded, 184 if no exponential is
+// Tall: 32 ragged requests with trees of 16 (112 rows) 187 us, 3000 cycles a tile; 176 if nothing is decoded, 184 if no exponential is
 // taken: the tile's hand-overs bound it, and the queries (28 rows: 174).  Over a bf16 cache with four times the bytes 172 to 178.
 // With two groups for the softmax and four decoders 202, a round of K and V 3550 cycles of a decoder, of which 1000 to 1400
 // were the decoding itself and the rest waits and control.  Measured on the way there: loads under a condition are waited for where
